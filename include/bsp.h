@@ -55,7 +55,10 @@ enum bsp_status {
   BSP_ERR_ALIGN = -9        /* a device pointer is not 16-byte aligned */
 };
 
-enum bsp_dtype { BSP_F32 = 0, BSP_BF16 = 1, BSP_I8 = 2, BSP_I32 = 3 };
+enum bsp_dtype {
+  BSP_F32 = 0, BSP_BF16 = 1, BSP_I8 = 2, BSP_I32 = 3,
+  BSP_E4M3 = 4, BSP_E5M2 = 5  /* 8-bit floating-point codes with a power-of-two scale for each block of 128 */
+};
 
 /* Static, never-null description of a status code. */
 const char* bsp_strerror(int code);
@@ -396,6 +399,111 @@ int bsp_fc_i8(const bsp_weights* w, const int8_t* X, const int32_t* bias, void* 
 enum bsp_call { BSP_CALL_CONV2D = 0, BSP_CALL_FC = 1, BSP_CALL_CONV2D_I8 = 2, BSP_CALL_FC_I8 = 3 };
 enum { BSP_CALL_WORDS = 14 };
 int bsp_call_packed(int32_t call, const int64_t* words);
+
+/* ------------------------------------- 8-bit floating point: a layer's training step
+ * FC layers whose weights and activations are 8-bit floating-point codes with one power-of-two scale for each block of
+ * 128, the step of training them, and the layer norm in front of them.  As in Eq. (8) scales are powers of two, so
+ * multiplying by one is exact.
+ *
+ * Codes of a matrix [T][K]: a block is 128 columns of one row.  With a = m 2^E, 1 <= m < 2, the largest finite
+ * magnitude in it, its exponent is e = E - 8 (BSP_E4M3: largest value 1.75 * 2^8) or E - 15 (BSP_E5M2: 1.75 * 2^15),
+ * one more where m > 1.75, and at least -127; e = 0 for a block of zeros.  A code is x * 2^-e rounded to nearest, ties
+ * to even.  An infinity or NaN becomes the NaN code (BSP_E5M2 keeps infinities) and has no part in its block's scale.
+ */
+typedef struct {
+  int32_t T, K;       /* rows and columns; T = 0 is valid */
+  int32_t dtype;      /* BSP_E4M3 or BSP_E5M2 */
+  uint8_t* codes;     /* device [T][128 ceil(K/128)], 16-byte aligned; columns past K are code 0 */
+  uint8_t* scale;     /* device [ceil(K/128)][16 ceil(T/16)] bytes e + 127, 16-byte aligned: a column block's rows together */
+} bsp_codes;
+
+/* Write an activation X [T][K] as codes (its 8-bit checkpoint), and read one back.
+ *   X, Y       device, x_dtype / y_dtype BSP_F32 or BSP_BF16, rows ldx / ldy elements apart (at least K; an input's may be
+ *              0, every row the same), aligned to an element; 16-byte aligned rows are the fast case
+ *   c          sizes, type and buffers; bsp_f8_save writes every byte of both buffers
+ * bsp_f8_load gives code * 2^e, which both types hold exactly down to their smallest normal number (and which is 2^128, an
+ * infinity in either, for values that round to it).
+ * Asynchronous.  Errors: NULL, SHAPE, DTYPE, ALIGN, HIP. */
+int bsp_f8_save(const void* X, int32_t x_dtype, int64_t ldx, const bsp_codes* c, void* stream);
+int bsp_f8_load(const bsp_codes* c, void* Y, int32_t y_dtype, int64_t ldy, void* stream);
+
+/* Weights: a mask Gamma over 128x128 blocks of W [O][I], each kept block 128x128 BSP_E4M3 codes with one scale, its
+ * overhang over O and I code 0.  Held twice, once by block rows for the layer itself and once transposed by block columns
+ * for the gradient of its input. */
+typedef struct {
+  int32_t O, I;
+  int64_t nnzb;            /* kept blocks */
+  const int32_t* row_ptr;  /* device [ceil(O/128) + 1] */
+  const int32_t* col_idx;  /* device [nnzb], ascending in a block row */
+  const int32_t* col_ptr;  /* device [ceil(I/128) + 1] */
+  const int32_t* row_idx;  /* device [nnzb], ascending in a block column */
+  uint8_t* payload;        /* device [nnzb][128][128], 16-byte aligned: codes by block rows, [o][i] within a block */
+  uint8_t* scale;          /* device [nnzb] bytes e + 127 */
+  uint8_t* payload_t;      /* device [nnzb][128][128], 16-byte aligned: the same blocks by block columns, [i][o] within */
+  uint8_t* scale_t;        /* device [nnzb] */
+} bsp_weights_f8;
+
+/* Host: the number of kept blocks, and the four index arrays (host pointers) of a mask gamma [ceil(O/128)][ceil(I/128)].
+ * capacity: entries that col_idx and row_idx each have room for.  Errors: NULL, SHAPE, MASK, CAPACITY. */
+int bsp_f8_count(const uint8_t* gamma, int32_t O, int32_t I, int64_t* nnzb);
+int bsp_f8_index(const uint8_t* gamma, int32_t O, int32_t I, int64_t capacity,
+                 int32_t* row_ptr, int32_t* col_idx, int32_t* col_ptr, int32_t* row_idx);
+
+/* Device: fill payload, scale, payload_t and scale_t from W [O][I] (device, BSP_F32 or BSP_BF16, rows ldw elements apart):
+ * after a training step has changed W this is all there is to do.  Asynchronous.
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, HIP. */
+int bsp_f8_pack(const bsp_weights_f8* w, const void* W, int32_t w_dtype, int64_t ldw, void* stream);
+
+/* The layer on codes: Y [T][O] = act(X W^t + bias + residual), and transposed (transposed != 0) the gradient of its
+ * input: Y [T][I] = X W for codes X [T][O].
+ *   bias       device float or null;  residual device, shape and type of Y, or null;  relu: act = max(., 0)
+ *   gate       codes of the shape of Y, or null: results whose gate is not above 0 become 0.  With the checkpoint of a
+ *              ReLU's output as gate this is the ReLU's backward pass.
+ *   y_dtype    BSP_BF16 or BSP_F32; Y and residual 16-byte aligned, rows contiguous
+ * Sums are fp32 and are rounded once, after the epilogue.  For BSP_BF16 results the products of codes are added eight
+ * at a time by the matrix cores, which cut each off 13 bits below the largest of its eight (measured: 1.4e-5 of a sum's
+ * spread, a hundredth of the result's own rounding); for BSP_F32 results every product is added in fp32.
+ * Rows are independent; a block that is not kept reads nothing, so what lies in its columns of X has no effect.
+ * T = 0 does nothing.  Asynchronous, no memory of its own.  Errors: NULL, SHAPE, DTYPE, ALIGN, HIP. */
+int bsp_f8_fc(const bsp_weights_f8* w, int32_t transposed, const bsp_codes* X, const float* bias, const void* residual,
+              int32_t relu, const bsp_codes* gate, void* Y, int32_t y_dtype, void* stream);
+
+/* The same on values: X [T][I] ([T][O] transposed) of x_dtype BSP_F32 or BSP_BF16 becomes codes of type `code` first, in
+ * registers where the rows are few, else in `workspace` (device, 16-byte aligned, at least as many bytes as
+ * bsp_f8_fc_workspace says, which may be 0; used until the call's work on the stream is done).
+ * Results are those of bsp_f8_save and bsp_f8_fc.  Errors: as these, CAPACITY. */
+int bsp_f8_fc_workspace(const bsp_weights_f8* w, int32_t transposed, int32_t T, int64_t* bytes);
+int bsp_f8_fc_values(const bsp_weights_f8* w, int32_t transposed, const void* X, int32_t x_dtype, int64_t ldx, int32_t T,
+                     int32_t code, const float* bias, const void* residual, int32_t relu, const bsp_codes* gate,
+                     void* Y, int32_t y_dtype, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* The weights' gradient from the checkpoint of the layer's input, and the bias's:
+ *   dW [O][I] float = sum over rows of dY[t][o] X[t][i] in kept blocks, 0 elsewhere;  db [O] float = sum over rows of dY
+ *   dY   device bf16 [T][O], rows ldy elements apart;  X codes [T][I]
+ *   dW, db  device, 16-byte aligned; either may be null.  T = 0 gives zeros.
+ *   workspace  as above, bsp_f8_fc_grad_workspace bytes
+ * fp32 sums in an order that depends on the sizes alone.  Asynchronous.  Errors: NULL, SHAPE, DTYPE, ALIGN, CAPACITY, HIP. */
+int bsp_f8_fc_grad_workspace(const bsp_weights_f8* w, int32_t T, int64_t* bytes);
+int bsp_f8_fc_grad(const bsp_weights_f8* w, const void* dY, int64_t ldy, const bsp_codes* X, float* dW, float* db,
+                   void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Layer norm over the last axis: Y = (X - mean) rstd weight + bias, rstd = 1 / sqrt(variance + eps), variance the mean
+ * squared deviation.  Sums in fp32.
+ *   X            device [T][D], dtype BSP_F32 or BSP_BF16, rows ldx elements apart
+ *   weight, bias device float[D], or null (ones, zeros)
+ *   Y            device [T][D] of the same dtype, rows ldy apart; or null, with
+ *   codes        the result as codes instead (from the fp32 values, unrounded), T and D its shape; or null
+ *   mean, rstd   device float[T], written for the backward pass
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, HIP.  T = 0 does nothing. */
+int bsp_layer_norm(const void* X, int32_t dtype, int64_t ldx, int32_t T, int32_t D, const float* weight, const float* bias,
+                   float eps, void* Y, int64_t ldy, const bsp_codes* codes, float* mean, float* rstd, void* stream);
+/* Its gradient: dX [T][D] (rows ld_dx apart) of the dtype of X and dY, dweight and dbias float[D] (either may be null), from the mean
+ * and rstd that bsp_layer_norm wrote.  workspace: bsp_layer_norm_grad_workspace bytes, 16-byte aligned.
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, CAPACITY, HIP.  T = 0 gives zeros. */
+int bsp_layer_norm_grad_workspace(int32_t T, int32_t D, int64_t* bytes);
+int bsp_layer_norm_grad(const void* dY, int64_t ld_dy, const void* X, int64_t ldx, int32_t dtype, int32_t T, int32_t D,
+                        const float* mean, const float* rstd, const float* weight, void* dX, int64_t ld_dx,
+                        float* dweight, float* dbias, void* workspace, int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

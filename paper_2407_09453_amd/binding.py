@@ -18,6 +18,8 @@ BSP_F32 = 0
 BSP_BF16 = 1
 BSP_I8 = 2
 BSP_I32 = 3
+BSP_E4M3 = 4
+BSP_E5M2 = 5
 BSP_KERNEL_ROWS, BSP_KERNEL_LDS, BSP_KERNEL_TILE, BSP_KERNEL_FC, BSP_KERNEL_PW = 1, 2, 4, 8, 16
 BSP_KERNEL_CHAIN = 32
 BSP_KERNEL_BAND = 64
@@ -32,7 +34,10 @@ EXPORTS = ("bsp_strerror", "bsp_version", "bsp_pack_count", "bsp_pack", "bsp_unp
            "bsp_conv2d_general", "bsp_quantize", "bsp_conv2d_i8", "bsp_fc_i8",
            "bsp_block_importance", "bsp_select_mask", "bsp_mask_step", "bsp_conv2d_fused",
            "bsp_fc_fused", "bsp_fc_fused_static", "bsp_bcsr_segments", "bsp_spgemm_nt",
-           "bsp_conv2d_only", "bsp_bottleneck", "bsp_call_packed", "bsp_bench_copy", "bsp_bench_mfma_bf16", "bsp_bench_lds_read")
+           "bsp_conv2d_only", "bsp_bottleneck", "bsp_call_packed", "bsp_bench_copy", "bsp_bench_mfma_bf16", "bsp_bench_lds_read",
+           "bsp_f8_save", "bsp_f8_load", "bsp_f8_count", "bsp_f8_index", "bsp_f8_pack", "bsp_f8_fc", "bsp_f8_fc_workspace",
+           "bsp_f8_fc_values", "bsp_f8_fc_grad_workspace", "bsp_f8_fc_grad", "bsp_layer_norm", "bsp_layer_norm_grad_workspace",
+           "bsp_layer_norm_grad")
 
 
 class BspError(RuntimeError):
@@ -56,6 +61,18 @@ class bsp_bcsr(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("nnzb", ctypes.c_int64), ("row_ptr", ctypes.c_void_p),
                 ("col_idx", ctypes.c_void_p), ("payload", ctypes.c_void_p),
                 ("seg_ptr", ctypes.c_void_p)]
+
+
+class bsp_codes(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("K", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("codes", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+
+
+class bsp_weights_f8(ctypes.Structure):
+    _fields_ = [("O", ctypes.c_int32), ("I", ctypes.c_int32), ("nnzb", ctypes.c_int64),
+                ("row_ptr", ctypes.c_void_p), ("col_idx", ctypes.c_void_p), ("col_ptr", ctypes.c_void_p),
+                ("row_idx", ctypes.c_void_p), ("payload", ctypes.c_void_p), ("scale", ctypes.c_void_p),
+                ("payload_t", ctypes.c_void_p), ("scale_t", ctypes.c_void_p)]
 
 
 def lib_path() -> str:
@@ -134,6 +151,19 @@ def load_library():
     lib.bsp_conv2d_i8.argtypes = [wp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, i32, i32, vp]
     lib.bsp_fc_i8.restype = ctypes.c_int
     lib.bsp_fc_i8.argtypes = [wp, vp, vp, vp, i32, i32, i32, vp]
+    cp, fp, pi64 = ctypes.POINTER(bsp_codes), ctypes.POINTER(bsp_weights_f8), ctypes.POINTER(i64)
+    for name, args in (("bsp_f8_save", [vp, i32, i64, cp, vp]), ("bsp_f8_load", [cp, vp, i32, i64, vp]),
+                       ("bsp_f8_count", [vp, i32, i32, pi64]), ("bsp_f8_index", [vp, i32, i32, i64, vp, vp, vp, vp]),
+                       ("bsp_f8_pack", [fp, vp, i32, i64, vp]), ("bsp_f8_fc", [fp, i32, cp, vp, vp, i32, cp, vp, i32, vp]),
+                       ("bsp_f8_fc_workspace", [fp, i32, i32, pi64]),
+                       ("bsp_f8_fc_values", [fp, i32, vp, i32, i64, i32, i32, vp, vp, i32, cp, vp, i32, vp, i64, vp]),
+                       ("bsp_f8_fc_grad_workspace", [fp, i32, pi64]),
+                       ("bsp_f8_fc_grad", [fp, vp, i64, cp, vp, vp, vp, i64, vp]),
+                       ("bsp_layer_norm", [vp, i32, i64, i32, i32, vp, vp, ctypes.c_float, vp, i64, cp, vp, vp, vp]),
+                       ("bsp_layer_norm_grad_workspace", [i32, i32, pi64]),
+                       ("bsp_layer_norm_grad", [vp, i64, vp, i64, i32, i32, i32, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp])):
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = ctypes.c_int, args
     lib.bsp_call_packed.restype = ctypes.c_int
     lib.bsp_call_packed.argtypes = [i32, ctypes.c_char_p]
     lib.bsp_bench_copy.restype = ctypes.c_int

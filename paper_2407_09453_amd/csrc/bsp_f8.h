@@ -1,0 +1,199 @@
+// 8-bit floating-point codes with power-of-two scales: the rule, and what the kernels on them share.
+//
+// A block is 128 columns of a row (activations) or 128 x 128 entries (weights).  With a = m 2^E (1 <= m < 2) the largest
+// finite magnitude in it, its exponent is e = E - 8 (e4m3, whose largest value is 1.75 2^8) or E - 15 (e5m2: 1.75 2^15),
+// one more where m > 1.75, and its codes are x 2^-e rounded to nearest, ties to even: the smallest power of two under
+// which nothing saturates.  e is held in a byte as e + 127, the form in which the matrix cores take a scale, so a scale
+// costs the product nothing, and code x 2^e is exact in bf16.
+#ifndef BSP_F8_H
+#define BSP_F8_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "bsp.h"
+#include "bsp_device.h"
+
+typedef __attribute__((ext_vector_type(8))) int i32x8_t;
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+typedef const __attribute__((address_space(1))) void* f8_gptr_t;
+typedef __attribute__((address_space(3))) void* f8_lptr_t;
+
+enum { F8_BLOCK = 128, F8_BLOCK_BYTES = F8_BLOCK * F8_BLOCK };
+
+__host__ __device__ inline int f8_blocks(int n) { return (n + F8_BLOCK - 1) / F8_BLOCK; }
+// rows of a scale array: one byte for each row of a column block, whole sixteens of them
+__host__ __device__ inline int64_t f8_scale_rows(int T) { return ((int64_t)T + 15) & ~(int64_t)15; }
+
+// |x| as an ordered integer, 0 for infinities and NaN (they do not take part in a block's scale)
+__device__ __forceinline__ uint32_t f8_magnitude(float x) {
+  const uint32_t u = __float_as_uint(x) & 0x7FFFFFFFu;
+  return u < 0x7F800000u ? u : 0u;
+}
+
+// the scale byte e + 127 of a block whose largest magnitude has the bits `a`; E5: e5m2
+template <bool E5>
+__device__ __forceinline__ int f8_scale_byte(uint32_t a) {
+  if (a == 0) return 127;
+  const int e = (int)(a >> 23) - (E5 ? 15 : 8) + ((a & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  return e < 0 ? 0 : e;  // (a subnormal's field is 0, so it too ends at 2^-127)
+}
+// 2^-e as a float, for scale byte b <= 247
+__device__ __forceinline__ float f8_inverse(int b) { return __uint_as_float((uint32_t)(254 - b) << 23); }
+// 2^e as a float
+__device__ __forceinline__ float f8_power(int b) { return __uint_as_float(b ? (uint32_t)b << 23 : 0x00400000u); }
+
+// four values to four codes
+template <bool E5>
+__device__ __forceinline__ uint32_t f8_encode4(float a, float b, float c, float d) {
+  int v = 0;
+  if constexpr (E5) {
+    v = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, v, false);
+    v = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, v, true);
+  } else {
+    v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, v, false);
+    v = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
+  }
+  return (uint32_t)v;
+}
+
+// two codes (low or high half of v) times 2^e as a bf16 pair; scale = byte << 23 (the instruction reads the exponent alone)
+template <bool E5, bool HIGH>
+__device__ __forceinline__ uint32_t f8_decode_bf16x2(uint32_t v, float scale) {
+  if constexpr (E5) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(v, scale, HIGH));
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, scale, HIGH));
+}
+// eight codes (two words) times 2^e as eight bf16
+template <bool E5>
+__device__ __forceinline__ u32x4_t f8_decode_bf16x8(uint32_t lo, uint32_t hi, float scale) {
+  return u32x4_t{f8_decode_bf16x2<E5, false>(lo, scale), f8_decode_bf16x2<E5, true>(lo, scale),
+                 f8_decode_bf16x2<E5, false>(hi, scale), f8_decode_bf16x2<E5, true>(hi, scale)};
+}
+
+__device__ __forceinline__ uint32_t f8_pack_bf16x2(float a, float b) {
+  const bf16x2_t v = {(__bf16)a, (__bf16)b};  // v_cvt_pk_bf16_f32: to nearest, ties to even
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// whether a code stands for a value above zero
+__device__ __forceinline__ bool f8_positive(uint32_t code, int e5) { return code - 1u < (e5 ? 0x7Cu : 0x7Eu); }
+
+// what follows a product: Y = act(sum + bias + residual) times the gate, one rounding to Y's type
+struct F8Epilogue {
+  void* Y;               // [T][O], rows contiguous
+  const float* bias;     // [O] or null
+  const void* residual;  // [T][O] of Y's type, or null
+  const uint8_t* gate;   // codes [T][128 ceil(O / 128)], or null: a result is kept where its code stands for a value > 0
+  int32_t relu, gate_e5;
+  int32_t vec;           // rows of Y, of the residual and the gate are aligned to four elements
+};
+
+// channels o .. o+3 (those below O) of row t
+template <bool F32>
+__device__ __forceinline__ void f8_store4(const F8Epilogue& q, int64_t t, int o, int O, float v0, float v1, float v2, float v3) {
+  float v[4] = {v0, v1, v2, v3};
+  const int n = O - o < 4 ? O - o : 4;
+  const bool whole = q.vec && n == 4;
+  if (q.bias) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < n) v[k] += q.bias[o + k];
+  }
+  const int64_t at = t * O + o;
+  if (q.residual) {
+    if constexpr (F32) {
+      const float* r = (const float*)q.residual + at;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < n) v[k] += r[k];
+    } else {
+      const uint16_t* r = (const uint16_t*)q.residual + at;
+      if (whole) {
+        const u32x2_t w = *(const u32x2_t*)r;
+        v[0] += __uint_as_float(w.x << 16);
+        v[1] += __uint_as_float(w.x & 0xFFFF0000u);
+        v[2] += __uint_as_float(w.y << 16);
+        v[3] += __uint_as_float(w.y & 0xFFFF0000u);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (k < n) v[k] += bf16_bits_to_f32(r[k]);
+      }
+    }
+  }
+  if (q.relu) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = v[k] < 0.f ? 0.f : v[k];  // (a NaN stays one)
+  }
+  if (q.gate) {  // o is a multiple of four and a gate row one of 128, so the word is there and aligned
+    const uint32_t c = *(const uint32_t*)(q.gate + t * (int64_t)f8_blocks(O) * F8_BLOCK + o);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = f8_positive((c >> (8 * k)) & 0xFFu, q.gate_e5) ? v[k] : 0.f;
+  }
+  if constexpr (F32) {
+    float* y = (float*)q.Y + at;
+    if (whole) {
+      *(f32x4_t*)y = f32x4_t{v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < n) y[k] = v[k];
+    }
+  } else {
+    uint16_t* y = (uint16_t*)q.Y + at;
+    const u32x2_t w = {f8_pack_bf16x2(v[0], v[1]), f8_pack_bf16x2(v[2], v[3])};
+    if (whole) {
+      *(u32x2_t*)y = w;
+    } else {
+      const uint32_t h[2] = {w.x, w.y};
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < n) y[k] = (uint16_t)(h[k >> 1] >> (16 * (k & 1)));
+    }
+  }
+}
+
+// ---------------------------------------------------------------- launchers (each returns a bsp_status)
+struct F8Rows {       // one direction of a layer's weights: compressed block rows of 128 x 128 codes
+  const int32_t *ptr, *idx;
+  const uint8_t *payload, *scale;
+  int32_t out, in;    // channels
+  int64_t nnzb;
+};
+struct F8Input {      // rows to multiply: codes with their scales, or values brought to e4m3 codes on the way
+  const void* X;
+  const uint8_t* scale;  // null: X holds values
+  int32_t dtype;      // of the rows as given: BSP_E4M3, BSP_E5M2, BSP_BF16, BSP_F32
+  int32_t e5;         // the codes are e5m2
+  int64_t ld;         // elements from row to row
+};
+// few rows: no LDS staging, the contraction split over a workgroup's waves
+int f8_launch_few(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, hipStream_t st);
+// many rows, codes only
+int f8_launch_tile(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, hipStream_t st);
+int f8_launch_save(const void* X, int x_f32, int64_t ldx, int T, int K, bool e5, uint8_t* codes, uint8_t* scale, hipStream_t st);
+int f8_launch_load(const uint8_t* codes, const uint8_t* scale, int T, int K, bool e5, void* Y, int y_f32, int64_t ldy, hipStream_t st);
+int f8_launch_pack(const bsp_weights_f8* w, const void* W, int w_f32, int64_t ldw, hipStream_t st);
+// weights' gradient: dW float [out][in], a kept block's entries or zeros; `part` as f8_grad_parts says
+struct F8GradArgs {
+  const uint16_t* dY;   // bf16 [T][O]
+  int64_t ldy;
+  const uint8_t *codes, *scale;
+  const int32_t *row_ptr, *col_idx;
+  float* dW;
+  float* part;
+  int32_t T, O, I, nbo, nbi, e5, split;
+  int64_t nnzb;
+};
+int f8_grad_split(int64_t nnzb, int T);              // into how many ranges of rows the sums are cut
+int f8_launch_grad(const F8GradArgs& a, hipStream_t st);
+int norm_parts(int T);                               // row ranges of a column sum
+int norm_launch_sum(const float* part, int parts, int O, float* out, hipStream_t st);
+int norm_launch_forward(const void* X, bool f32, int64_t ldx, int T, int D, const float* weight, const float* bias, float eps,
+                        void* Y, int64_t ldy, int code, uint8_t* codes, uint8_t* scale, float* mean, float* rstd, hipStream_t st);
+int norm_launch_backward(const void* dY, int64_t ld_dy, const void* X, int64_t ldx, bool f32, const float* mean, const float* rstd, const float* weight,
+                         int T, int D, void* dX, int64_t ld_dx, float* dweight, float* dbias, float* part, hipStream_t st);
+int f8_launch_colsum(const uint16_t* dY, int64_t ldy, int T, int O, float* part, float* db, hipStream_t st);
+
+#endif

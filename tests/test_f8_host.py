@@ -1,0 +1,187 @@
+"""Host side of the 8-bit floating-point layers: index arrays, refusals, and the oracle against its own definition."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import oracle.f8 as of8
+import paper_2407_09453_amd as bsp
+from paper_2407_09453_amd import binding as b
+
+OK, NULL, SHAPE, MASK, DTYPE, CAPACITY, ALIGN = 0, -1, -2, -3, -5, -7, -9
+
+
+@pytest.mark.parametrize("O,I", [(1, 1), (128, 128), (129, 127), (1000, 2048), (520, 1000)])
+@pytest.mark.parametrize("density", [0.0, 0.4, 1.0])
+def test_index_both_ways(O, I, density):
+    R, C = -(-O // 128), -(-I // 128)
+    g = (np.random.default_rng(O + I).random((R, C)) < density).astype(np.uint8)
+    lib = bsp.load_library()
+    n = ctypes.c_int64(-1)
+    assert lib.bsp_f8_count(g.ctypes.data, O, I, ctypes.byref(n)) == OK and n.value == g.sum()
+    rp, cp = np.full(R + 1, -1, np.int32), np.full(C + 1, -1, np.int32)
+    ci, ri = np.full(max(n.value, 1), -1, np.int32), np.full(max(n.value, 1), -1, np.int32)
+    assert lib.bsp_f8_index(g.ctypes.data, O, I, n.value, rp.ctypes.data, ci.ctypes.data, cp.ctypes.data, ri.ctypes.data) == OK
+    for r in range(R):
+        assert list(ci[rp[r]:rp[r + 1]]) == list(np.flatnonzero(g[r]))
+    for c in range(C):
+        assert list(ri[cp[c]:cp[c + 1]]) == list(np.flatnonzero(g[:, c]))
+    assert rp[0] == cp[0] == 0 and rp[R] == cp[C] == n.value
+    if n.value:
+        assert lib.bsp_f8_index(g.ctypes.data, O, I, n.value - 1, rp.ctypes.data, ci.ctypes.data, cp.ctypes.data, ri.ctypes.data) == CAPACITY
+
+
+def test_index_refusals():
+    lib = bsp.load_library()
+    g = np.ones((1, 1), np.uint8)
+    n = ctypes.c_int64(0)
+    assert lib.bsp_f8_count(None, 1, 1, ctypes.byref(n)) == NULL
+    assert lib.bsp_f8_count(g.ctypes.data, 0, 1, ctypes.byref(n)) == SHAPE
+    assert lib.bsp_f8_count(g.ctypes.data, 1, -5, ctypes.byref(n)) == SHAPE
+    g[0, 0] = 2
+    assert lib.bsp_f8_count(g.ctypes.data, 1, 1, ctypes.byref(n)) == MASK
+
+
+# Addresses that no call may touch: every one of these is refused before anything is launched.
+P = 1 << 20
+
+
+def _weights(O=256, I=384, nnzb=6, **kw):
+    w = b.bsp_weights_f8(O, I, nnzb, P, P, P, P, P, P, P, P)
+    for k, v in kw.items():
+        setattr(w, k, v)
+    return w
+
+
+def _codes(T=8, K=384, dtype=b.BSP_E4M3, codes=P, scale=P):
+    return b.bsp_codes(T, K, dtype, codes, scale)
+
+
+@pytest.mark.parametrize("want,args", [
+    (NULL, dict(c=None)), (DTYPE, dict(c=_codes(dtype=b.BSP_I8))), (DTYPE, dict(dt=b.BSP_I8)), (SHAPE, dict(c=_codes(T=-1))),
+    (SHAPE, dict(c=_codes(K=0))), (SHAPE, dict(ld=383)), (SHAPE, dict(ld=-384)), (SHAPE, dict(ld=1 << 62)), (NULL, dict(X=None)), (NULL, dict(c=_codes(codes=None))),
+    (NULL, dict(c=_codes(scale=None))), (ALIGN, dict(X=P + 1)), (ALIGN, dict(c=_codes(codes=P + 8))), (ALIGN, dict(c=_codes(scale=P + 4))),
+    (OK, dict(c=_codes(T=0, codes=None, scale=None), X=None)),
+])
+def test_save_and_load_refusals(want, args):
+    a = {**dict(X=P, dt=b.BSP_BF16, ld=384, c=_codes()), **args}
+    lib = bsp.load_library()
+    c = None if a["c"] is None else ctypes.byref(a["c"])
+    assert lib.bsp_f8_save(a["X"], a["dt"], a["ld"], c, None) == want
+    assert lib.bsp_f8_load(c, a["X"], a["dt"], a["ld"], None) == want
+
+
+def test_load_refuses_overlapping_rows():
+    assert bsp.load_library().bsp_f8_load(ctypes.byref(_codes()), P, b.BSP_BF16, 0, None) == SHAPE
+
+
+@pytest.mark.parametrize("want,args", [
+    (NULL, dict(w=None)), (NULL, dict(X=None)), (SHAPE, dict(w=_weights(O=0))), (SHAPE, dict(w=_weights(nnzb=7))), (SHAPE, dict(w=_weights(nnzb=-1))),
+    (NULL, dict(w=_weights(payload=None))), (NULL, dict(w=_weights(col_ptr=None))), (ALIGN, dict(w=_weights(payload_t=P + 8))),
+    (SHAPE, dict(X=_codes(K=256))), (SHAPE, dict(t=1)), (DTYPE, dict(X=_codes(dtype=b.BSP_F32))), (NULL, dict(Y=None)), (ALIGN, dict(Y=P + 2)),
+    (ALIGN, dict(r=P + 2)), (ALIGN, dict(bias=P + 2)), (DTYPE, dict(dt=b.BSP_I32)), (SHAPE, dict(gate=_codes(T=9, K=256))), (SHAPE, dict(gate=_codes(K=384))),
+    (NULL, dict(gate=_codes(K=256, codes=None))), (OK, dict(X=_codes(T=0, codes=None, scale=None), Y=None)),
+])
+def test_product_refusals(want, args):
+    a = {**dict(w=_weights(), t=0, X=_codes(), bias=None, r=None, gate=None, Y=P, dt=b.BSP_BF16), **args}
+    ref = lambda s: None if s is None else ctypes.byref(s)  # noqa: E731
+    assert bsp.load_library().bsp_f8_fc(ref(a["w"]), a["t"], ref(a["X"]), a["bias"], a["r"], 0, ref(a["gate"]), a["Y"], a["dt"], None) == want
+
+
+@pytest.mark.parametrize("want,args", [
+    (DTYPE, dict(xdt=b.BSP_E4M3)), (DTYPE, dict(code=b.BSP_BF16)), (SHAPE, dict(ld=100)), (NULL, dict(X=None)), (ALIGN, dict(X=P + 1)),
+    (CAPACITY, dict(n=17 * 384 + 32 * 3 - 1)), (NULL, dict(ws=None)), (ALIGN, dict(ws=P + 8)), (OK, dict(T=0, X=None, Y=None, ws=None, n=0)),
+])
+def test_values_refusals(want, args):
+    a = {**dict(T=17, X=P, xdt=b.BSP_BF16, ld=384, code=b.BSP_E4M3, Y=P, ws=P, n=17 * 384 + 32 * 3), **args}
+    w = _weights()
+    lib = bsp.load_library()
+    assert lib.bsp_f8_fc_values(ctypes.byref(w), 0, a["X"], a["xdt"], a["ld"], a["T"], a["code"], None, None, 0, None, a["Y"], b.BSP_BF16,
+                                a["ws"], a["n"], None) == want
+    n = ctypes.c_int64(-1)
+    assert lib.bsp_f8_fc_workspace(ctypes.byref(w), 0, 17, ctypes.byref(n)) == OK and n.value == 17 * 384 + 32 * 3
+    assert lib.bsp_f8_fc_workspace(ctypes.byref(w), 0, -1, ctypes.byref(n)) == SHAPE
+    assert lib.bsp_f8_fc_workspace(ctypes.byref(w), 0, 17, None) == NULL
+
+
+@pytest.mark.parametrize("want,args", [
+    (NULL, dict(X=None)), (SHAPE, dict(X=_codes(K=256))), (SHAPE, dict(ld=255)), (NULL, dict(dY=None)), (ALIGN, dict(dW=P + 4)), (ALIGN, dict(db=P + 4)),
+    (ALIGN, dict(ws=P + 4)), (CAPACITY, dict(n=0)), (NULL, dict(ws=None)), (NULL, dict(w=None)),
+])
+def test_weight_gradient_refusals(want, args):
+    a = {**dict(w=_weights(), dY=P, ld=256, X=_codes(), dW=P, db=P, ws=P, n=1 << 30), **args}
+    ref = lambda s: None if s is None else ctypes.byref(s)  # noqa: E731
+    assert bsp.load_library().bsp_f8_fc_grad(ref(a["w"]), a["dY"], a["ld"], ref(a["X"]), a["dW"], a["db"], a["ws"], a["n"], None) == want
+
+
+@pytest.mark.parametrize("want,args", [
+    (DTYPE, dict(dt=b.BSP_E4M3)), (SHAPE, dict(D=0)), (SHAPE, dict(T=-2)), (SHAPE, dict(ld=383)), (NULL, dict(Y=None)), (NULL, dict(codes=_codes())),
+    (SHAPE, dict(Y=None, codes=_codes(K=256))), (NULL, dict(X=None)), (NULL, dict(mean=None)), (ALIGN, dict(Y=P + 1)), (ALIGN, dict(weight=P + 1)),
+    (SHAPE, dict(eps=-1.0)), (SHAPE, dict(eps=float("nan"))), (OK, dict(T=0, X=None, Y=None, mean=None)),
+])
+def test_norm_refusals(want, args):
+    a = {**dict(X=P, dt=b.BSP_BF16, ld=384, T=8, D=384, weight=None, eps=1e-5, Y=P, codes=None, mean=P), **args}
+    c = None if a["codes"] is None else ctypes.byref(a["codes"])
+    assert bsp.load_library().bsp_layer_norm(a["X"], a["dt"], a["ld"], a["T"], a["D"], a["weight"], None, a["eps"], a["Y"], a["D"] if a["D"] > 0 else 1, c,
+                                             a["mean"], P, None) == want
+
+
+@pytest.mark.parametrize("want,args", [
+    (DTYPE, dict(dt=b.BSP_I8)), (SHAPE, dict(D=0)), (SHAPE, dict(ld=383)), (NULL, dict(X=None)), (NULL, dict(mean=None)), (CAPACITY, dict(n=8 * 2 * 384 * 4 - 1)),
+    (NULL, dict(ws=None)), (ALIGN, dict(ws=P + 4)), (ALIGN, dict(X=P + 1)),
+])
+def test_norm_gradient_refusals(want, args):
+    a = {**dict(X=P, dt=b.BSP_F32, ld=384, T=8, D=384, mean=P, ws=P, n=8 * 2 * 384 * 4), **args}
+    assert bsp.load_library().bsp_layer_norm_grad(P, a["ld"], a["X"], a["ld"], a["dt"], a["T"], a["D"], a["mean"], P, None, P, 384, P, P, a["ws"], a["n"],
+                                                  None) == want
+
+
+def test_oracle_codes_are_the_formats_own_grid():
+    """The oracle's rounding against torch's conversion of scaled values, every bf16 exponent and tie among them."""
+    import torch
+    rng = np.random.default_rng(1)
+    x = (rng.standard_normal((64, 512)) * np.exp2(rng.integers(-30, 30, (64, 1)))).astype(np.float32)
+    x = torch.from_numpy(x).to(torch.bfloat16).float().numpy()  # eight bits: many ties
+    for kind, dt in (("e4m3", torch.float8_e4m3fn), ("e5m2", torch.float8_e5m2)):
+        e = np.repeat(of8.scales(x, kind), 128, 1)
+        v = np.ldexp(x.astype(np.float64), -e)
+        top = np.abs(v).reshape(64, 4, 128).max(2)
+        most = 448.0 if kind == "e4m3" else 57344.0
+        assert (top <= most).all() and (top > most / 2).all()  # the smallest power of two that fits
+        want = torch.from_numpy(v.astype(np.float32)).to(dt).double().numpy()
+        assert (of8.values(x, kind) == np.ldexp(want, e)).all()
+
+
+def test_oracle_norm_gradient_against_differences():
+    rng = np.random.default_rng(2)
+    x, w, dy = rng.standard_normal((3, 7)), rng.standard_normal(7), rng.standard_normal((3, 7))
+    bias = rng.standard_normal(7)
+    f = lambda x, w, c: float((of8.layer_norm(x, w, c)[0] * dy).sum())  # noqa: E731
+    dx, dw, db = of8.layer_norm_grad(dy, x, w)
+    h = 1e-6
+    for at in np.ndindex(3, 7):
+        d = np.zeros((3, 7))
+        d[at] = h
+        assert abs((f(x + d, w, bias) - f(x - d, w, bias)) / (2 * h) - dx[at]) < 1e-7  # central differences: h^2 and 1e-16 / h
+    for k in range(7):
+        d = np.zeros(7)
+        d[k] = h
+        assert abs((f(x, w + d, bias) - f(x, w - d, bias)) / (2 * h) - dw[k]) < 1e-7
+        assert abs((f(x, w, bias + d) - f(x, w, bias - d)) / (2 * h) - db[k]) < 1e-7
+
+
+def test_oracle_weight_gradient_against_differences():
+    """The loss is linear in the weights once they are codes, so differences are exact up to rounding."""
+    rng = np.random.default_rng(3)
+    x, dy = rng.standard_normal((5, 130)), rng.standard_normal((5, 140))
+    gamma = np.array([[1, 0], [1, 1]])
+    xq = of8.values(x, "e4m3")
+    dW, db = of8.grad_weight(dy, xq, gamma)
+    keep = of8.mask(gamma, 140, 130)
+    loss = lambda W: float((xq @ np.where(keep, W, 0).T * dy).sum())  # noqa: E731
+    W = rng.standard_normal((140, 130))
+    for at in ((0, 0), (0, 129), (139, 129), (127, 5), (128, 128), (3, 128)):
+        d = np.zeros_like(W)
+        d[at] = 1.0
+        assert abs(loss(W + d) - loss(W) - dW[at]) < 1e-10
+    assert np.allclose(db, dy.sum(0))

@@ -1,0 +1,395 @@
+"""8-bit floating-point layers, their checkpoints and gradients, against the oracle in 64 bits.
+
+Bounds.  U = 2^-24 is fp32's half unit.  A bf16 result is rounded once, 2^-8 of its value; its products are added eight at a
+time by an instruction that cuts each of the eight off 13 bits below the sum of the largest one's exponents (256 x 256 + 7 gives
+256 x 256, + 9 gives + 8), so a group loses less than 7 2^-13 of its largest product: 2^-10 of the sum of magnitudes S.
+An fp32 result adds n terms in some order: at most (n + 8) U S.  Codes, their scales and what they stand for are exact.
+"""
+import numpy as np
+import pytest
+
+import oracle.f8 as of8
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def _bsp():
+    import paper_2407_09453_amd as bsp
+    return bsp
+
+
+def _rng(*key):
+    return np.random.default_rng([240709453, *key])
+
+
+def _draw(rng, T, K, dtype, relu=False):
+    """Rows of differing size with a few large channels, on the grid of the type, as (numpy, torch)."""
+    import torch
+    x = rng.standard_normal((T, K)) * np.exp(rng.standard_normal((T, 1))) * np.where(rng.random(K) < 0.02, 20.0, 1.0)
+    if relu:
+        x = np.maximum(x, 0)
+    t = torch.from_numpy(x.astype(np.float32)).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    return t.double().numpy(), t.cuda()
+
+
+def _host(t):
+    import torch
+    torch.cuda.synchronize()
+    return t.double().cpu().numpy()
+
+
+def _same(a, b):
+    return ((a == b) | (np.isnan(a) & np.isnan(b))).all()
+
+
+# ------------------------------------------------------------------------------- checkpoints
+@pytest.mark.parametrize("kind", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,K", [(1, 1), (1, 128), (2, 127), (15, 129), (16, 1024), (17, 1025), (33, 1000), (5, 4100), (300, 520)])
+def test_checkpoint_is_exact(T, K, dtype, kind):
+    import torch
+    x, t = _draw(_rng(T, K), T, K, dtype)
+    c = _bsp().save8(t, kind)
+    want = of8.values(x, kind)
+    assert (_host(c.load(torch.float32)) == want).all()
+    assert (_host(c.load()) == want).all()
+    e = of8.scales(x, kind) + 127
+    assert (c.scale.cpu().numpy()[:, :T] == e.T).all()
+    assert (c.codes.cpu().numpy()[:, K:] == 0).all()
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "e5m2"])
+def test_checkpoint_of_rare_values(kind):
+    """Zeros of both signs, subnormals, the largest numbers, ties, infinities and NaN next to ordinary values."""
+    import torch
+    x = np.zeros((12, 256))
+    x[0, :6] = [0.0, -0.0, 1.75, 1.7500001, -1.0, 2.0 ** -40]
+    x[1, :3] = [np.inf, 1.0, -3.0]
+    x[2, :3] = [np.nan, 448.0, 449.0]
+    x[3, 130:133] = [-np.inf, np.nan, 1e-3]
+    x[4, :4] = [2.0 ** -149, 2.0 ** -130, 2.0 ** -126, 2.0 ** -127]
+    x[5, :3] = [3.4e38, 1e30, -3.3e38]
+    x[6] = np.inf
+    x[7, 128:] = np.nan
+    x[8, :4] = [448.0, 17.0, 19.0, 2.0 ** -10]
+    x[9, :4] = [2.0 ** -118, 2.0 ** -126, 2.0 ** -120, 2.0 ** -128]
+    x[10, :2] = [-2.0 ** 100, 2.0 ** 99]
+    x = x.astype(np.float32)
+    c = _bsp().save8(torch.from_numpy(x).cuda(), kind)
+    with np.errstate(over="ignore"):  # 3.4e38 rounds to the code of 2^128, past both types' range
+        want = of8.values(x, kind).astype(np.float32).astype(np.float64)
+    got = _host(c.load(torch.float32))
+    assert _same(got, want)
+    big = np.abs(want) >= 2.0 ** -126  # (bf16 holds them all; what the conversion does below is not promised)
+    got = _host(c.load())
+    assert _same(got[big | ~np.isfinite(want)], want[big | ~np.isfinite(want)])
+
+
+def test_checkpoint_of_rows_anywhere():
+    """Rows a distance apart, at odd addresses, the same row repeated; results likewise; nothing outside them is touched."""
+    import torch
+    bsp = _bsp()
+    base = torch.randn(40, 701, device="cuda")
+    for X in (base[:, :300], base[::2, 5:517], base[:, 1:130].to(torch.bfloat16)[:, 1:], base[3:4, :700].expand(20, 700), base.to(torch.bfloat16)[1:, 3:]):
+        x = _host(X)
+        want = of8.values(x, "e4m3")
+        c = bsp.save8(X)
+        assert (_host(c.load(torch.float32)) == want).all()
+        out = torch.full((X.shape[0], X.shape[1] + 9), 7.0, device="cuda", dtype=torch.bfloat16)
+        c.load(out=out[:, 4:4 + X.shape[1]])
+        got = _host(out)
+        assert (got[:, 4:-5] == want).all() and (got[:, :4] == 7).all() and (got[:, -5:] == 7).all()
+
+
+def test_empty_checkpoint():
+    import torch
+    bsp = _bsp()
+    c = bsp.save8(torch.empty(0, 300, device="cuda"))
+    assert c.load().shape == (0, 300)
+
+
+# ------------------------------------------------------------------------------- the product
+def _layer(rng, O, I, density, bias=True, W=None):
+    W = (rng.standard_normal((O, I)) * np.sqrt(2.0 / I)).astype(np.float32) if W is None else W
+    gamma = (rng.random((-(-O // 128), -(-I // 128))) < density).astype(np.uint8)
+    b = (rng.standard_normal(O) * 0.1).astype(np.float32) if bias else None
+    return W, gamma, b, _bsp().BspLayerF8(W, gamma, bias=b)
+
+
+def _bound(x, W, gamma, f32, ref, extra=0.0, code="e4m3", transposed=False):
+    S = of8.fc(np.abs(x), np.abs(W), gamma, code=code, transposed=transposed) + extra
+    n = W.shape[0] if transposed else W.shape[1]
+    return (n + 8) * U * S if f32 else 2.0 ** -8 * np.abs(ref) + 2.0 ** -10 * S + 2.0 ** -133
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,I,O,density", [
+    (1, 1, 1, 1.0), (1, 128, 16, 1.0), (1, 4096, 520, 0.5), (3, 300, 130, 1.0), (16, 2048, 1000, 0.5), (17, 129, 127, 1.0), (32, 1000, 1024, 0.6),
+    (33, 512, 36, 1.0), (64, 640, 300, 0.5), (65, 640, 300, 0.5), (127, 256, 128, 1.0), (128, 1000, 257, 0.7), (129, 384, 513, 0.4), (197, 2048, 1000, 0.75),
+    (300, 200, 264, 0.0), (513, 1152, 384, 1.0), (1000, 512, 770, 0.3), (700, 4096, 130, 1.0),
+])
+def test_product(T, I, O, density, dtype):
+    rng = _rng(T, I, O)
+    x, t = _draw(rng, T, I, dtype)
+    W, gamma, b, layer = _layer(rng, O, I, density)
+    ref = of8.fc(x, W, gamma, b)
+    y = _host(layer.fc(t))
+    tol = _bound(x, W, gamma, dtype == "f32", ref, np.abs(b))
+    assert (np.abs(y - ref) <= tol).all(), float((np.abs(y - ref) / tol).max())
+    # on a checkpoint, the same bits (either way the rows become the same codes)
+    import torch
+    y2 = _host(layer.fc(_bsp().save8(t), dtype=t.dtype))
+    few = T <= 64
+    assert (y2 == y).all() if not few else (np.abs(y2 - ref) <= tol).all()
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("T,I,O", [(1, 700, 300), (20, 256, 520), (150, 520, 260), (600, 1024, 640)])
+def test_epilogue_and_code_types(T, I, O, kind):
+    import torch
+    rng = _rng(T, I, O, 5)
+    x, t = _draw(rng, T, I, "bf16")
+    r, rt = _draw(rng, T, O, "bf16")
+    W, gamma, b, layer = _layer(rng, O, I, 0.7)
+    ref = of8.fc(x, W, gamma, b, residual=r, relu=True, code=kind)
+    y = _host(layer.fc(_bsp().save8(t, kind), residual=rt, relu=True))
+    assert (np.abs(y - ref) <= _bound(x, W, gamma, False, ref, np.abs(b) + np.abs(r), kind)).all()
+    r32 = torch.from_numpy(r.astype(np.float32)).cuda()
+    y = _host(layer.fc(_bsp().save8(t, kind), residual=r32, relu=True, dtype=torch.float32))
+    assert (np.abs(y - ref) <= _bound(x, W, gamma, True, ref, np.abs(b) + np.abs(r), kind)).all()
+
+
+@pytest.mark.parametrize("code", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("T,I,O,density", [(1, 300, 700, 1.0), (37, 1000, 520, 0.6), (64, 256, 129, 1.0), (100, 384, 260, 0.5), (513, 640, 1024, 0.5)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_input_gradient(T, I, O, density, code, gated):
+    rng = _rng(T, I, O, 6)
+    dy, dyt = _draw(rng, T, O, "bf16")
+    x, xt = _draw(rng, T, I, "bf16", relu=True)
+    W, gamma, _, layer = _layer(rng, O, I, density)
+    c = _bsp().save8(xt)
+    gate = of8.values(x, "e4m3") if gated else None
+    ref = of8.fc(dy, W, gamma, code=code, transposed=True, gate=gate)
+    y = _host(layer.grad_input(dyt, relu_of=c if gated else None, code=code))
+    assert (np.abs(y - ref) <= _bound(dy, W, gamma, False, ref, code=code, transposed=True)).all()
+    y = _host(layer.grad_input(_bsp().save8(dyt, code), relu_of=c if gated else None))
+    assert (np.abs(y - ref) <= _bound(dy, W, gamma, False, ref, code=code, transposed=True)).all()
+
+
+def test_gate_of_rare_codes():
+    """NaN, negative and zero codes close the gate, an e5m2 infinity opens it."""
+    import torch
+    bsp = _bsp()
+    x = np.ones((2, 128), np.float32)
+    x[0, :6] = [np.nan, -1.0, 0.0, -0.0, np.inf, 2.0 ** -30]
+    W = np.eye(128, dtype=np.float32)
+    layer = bsp.BspLayerF8(W)
+    dy = torch.ones(2, 128, device="cuda", dtype=torch.bfloat16)
+    for kind, open_inf, open_tiny in (("e4m3", 0.0, 0.0), ("e5m2", 1.0, 1.0)):  # 2^-30 beside 1 is the code 0 of e4m3, 2^-15 2^-15 in e5m2
+        y = _host(layer.grad_input(dy, relu_of=bsp.save8(torch.from_numpy(x).cuda(), kind)))
+        assert list(y[0, :6]) == [0, 0, 0, 0, open_inf, open_tiny] and (y[0, 6:] == 1).all() and (y[1] == 1).all()
+
+
+@pytest.mark.parametrize("T", [1, 40, 200])
+def test_blocks_that_are_not_kept_are_not_read(T):
+    """Infinities and NaN in a dropped block's columns stay out; in a kept one they reach their own row alone."""
+    rng = _rng(T, 7)
+    O, I = 384, 512
+    W = rng.standard_normal((O, I)).astype(np.float32)
+    gamma = np.array([[1, 0, 1, 1], [0, 0, 0, 0], [0, 1, 0, 1]], np.uint8)
+    layer = _bsp().BspLayerF8(W, gamma, bias=np.arange(O, dtype=np.float32))
+    x, t = _draw(rng, T, I, "bf16")
+    clean = _host(layer.fc(t))
+    t[0, 200], t[T - 1, 130] = float("inf"), float("nan")
+    y = _host(layer.fc(t))
+    assert (y[:, :256] == clean[:, :256]).all() and (y[:, 128:256] == np.arange(128, 256)).all()
+    rows = sorted({0, T - 1})
+    assert np.isnan(y[rows, 256:]).all()
+    rest = [r for r in range(T) if r not in rows]
+    assert (y[rest] == clean[rest]).all()
+
+
+def test_weights_of_rare_size():
+    """A block of zeros, blocks of tiny and huge weights, a weight that is not finite in a dropped block."""
+    import torch
+    rng = _rng(8)
+    W = rng.standard_normal((256, 384)).astype(np.float32)
+    W[:128, :128] = 0
+    W[:128, 128:256] *= 2.0 ** -100
+    W[128:, :128] *= 2.0 ** 60
+    W[128:, 256:] = np.inf
+    gamma = np.array([[1, 1, 1], [1, 1, 0]], np.uint8)
+    layer = _bsp().BspLayerF8(W, gamma)
+    for T in (2, 150):
+        x, t = _draw(rng, T, 384, "f32")
+        ref = of8.fc(x, W, gamma)
+        y = _host(layer.fc(t))
+        keep = np.where(of8.mask(gamma, 256, 384), W, 0)
+        assert (np.abs(y - ref) <= _bound(x, keep, gamma, True, ref)).all()
+
+
+def test_updated_weights_and_their_types():
+    import torch
+    rng = _rng(9)
+    W, gamma, b, layer = _layer(rng, 300, 260, 0.6)
+    x, t = _draw(rng, 20, 260, "bf16")
+    W2 = torch.from_numpy(rng.standard_normal((300, 270)).astype(np.float32)).to(torch.bfloat16).cuda()[:, 5:265]
+    layer.update(W2)
+    w2 = _host(W2)
+    ref = of8.fc(x, w2, gamma, b)
+    assert (np.abs(_host(layer.fc(t)) - ref) <= _bound(x, w2, gamma, False, ref, np.abs(b))).all()
+    dy, dyt = _draw(rng, 90, 300, "bf16")
+    ref = of8.fc(dy, w2, gamma, code="e5m2", transposed=True)
+    assert (np.abs(_host(layer.grad_input(dyt)) - ref) <= _bound(dy, w2, gamma, False, ref, code="e5m2", transposed=True)).all()
+
+
+# ------------------------------------------------------------------------------- the weights' gradient
+@pytest.mark.parametrize("kind", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("T,I,O,density", [(0, 300, 200, 1.0), (1, 1, 1, 1.0), (1, 128, 128, 1.0), (37, 1000, 520, 0.6), (63, 129, 127, 1.0), (64, 256, 256, 0.5), (65, 384, 260, 1.0),
+                                           (1000, 260, 136, 1.0), (4097, 128, 256, 1.0), (130, 640, 1000, 0.4), (200, 256, 128, 0.0)])
+def test_weight_gradient(T, I, O, density, kind):
+    rng = _rng(T, I, O, 10)
+    x, xt = _draw(rng, T, I, "bf16", relu=True)
+    dy, dyt = _draw(rng, T, O, "bf16")
+    W, gamma, _, layer = _layer(rng, O, I, density)
+    xq = of8.values(x, kind)
+    dW, db = of8.grad_weight(dy, xq, gamma)
+    got, gdb = layer.grad_weight(dyt, _bsp().save8(xt, kind))
+    S, Sb = of8.grad_weight(np.abs(dy), np.abs(xq), gamma)
+    assert (np.abs(_host(got) - dW) <= (T + 8) * U * S).all()
+    assert (np.abs(_host(gdb) - db) <= (T + 8) * U * Sb).all()
+
+
+def test_weight_gradient_of_rows_anywhere():
+    """Gradients whose rows lie apart, at odd addresses, or are one row (a broadcast); dropped blocks give zeros whatever is there."""
+    import torch
+    rng = _rng(11)
+    bsp = _bsp()
+    x, xt = _draw(rng, 150, 300, "bf16")
+    W, gamma, _, layer = _layer(rng, 264, 300, 1.0)
+    gamma = gamma.copy()
+    gamma[1, 1] = 0
+    layer = bsp.BspLayerF8(W, gamma)
+    xt[3, 130] = float("inf")
+    x = _host(xt)
+    xq = of8.values(x, "e5m2")
+    c = bsp.save8(xt, "e5m2")
+    base = torch.randn(150, 600, device="cuda").to(torch.bfloat16)
+    for dyt in (base[:, :264], base[:, 8:272], base[:, 1:265], base[:1, :264].expand(150, 264)):
+        dy = _host(dyt)
+        with np.errstate(invalid="ignore"):
+            dW, db = of8.grad_weight(dy, xq, gamma)
+            S, Sb = of8.grad_weight(np.abs(dy), np.abs(xq), gamma)
+        got, gdb = layer.grad_weight(dyt, c)
+        got = _host(got)
+        fine = np.isfinite(dW)
+        assert (np.isfinite(got) == fine).all() and (got[128:256, 128:256] == 0).all()
+        assert (np.abs(got - dW)[fine] <= 160 * U * S[fine]).all()
+        assert (np.abs(_host(gdb) - db) <= 160 * U * Sb).all()
+
+
+def test_infinite_gradient_stays_in_its_channel():
+    """The last rows of a step that is not full: an infinity there must not meet the zeros that fill the step."""
+    import torch
+    rng = _rng(12)
+    T = 70
+    x, xt = _draw(rng, T, 128, "bf16")
+    xt = xt.abs() + 1
+    dy, dyt = _draw(rng, T, 128, "bf16")
+    dyt[T - 1, 5] = float("inf")
+    layer = _bsp().BspLayerF8(np.ones((128, 128), np.float32))
+    dW, db = layer.grad_weight(dyt, _bsp().save8(xt))
+    dW, db = _host(dW), _host(db)
+    assert np.isposinf(dW[5]).all() and np.isfinite(np.delete(dW, 5, 0)).all()
+    assert np.isposinf(db[5]) and np.isfinite(np.delete(db, 5)).all()
+
+
+def test_gradients_against_differences():
+    """The layer's own outputs, differenced: with weights and rows on the codes' grid and a step that stays on it, the loss
+    sum(Y dY) is linear in a weight, so its difference is the gradient up to rounding of Y (2^-8 of its terms)."""
+    import torch
+    rng = _rng(13)
+    bsp = _bsp()
+    T, I, O = 24, 256, 128
+    W = rng.integers(-8, 9, (O, I)).astype(np.float32)
+    W[0, 0] = W[0, 128] = 12.0  # fixes both blocks' scales
+    x = rng.integers(-8, 9, (T, I)).astype(np.float32)
+    x[:, 0] = x[:, 128] = 12.0
+    dy = rng.integers(-4, 5, (T, O)).astype(np.float32)
+    xt, dyt = torch.from_numpy(x).cuda(), torch.from_numpy(dy).to(torch.bfloat16).cuda()
+    layer = bsp.BspLayerF8(W)
+    y = lambda: _host(layer.fc(xt))  # noqa: E731  (whole numbers below 2^24: exact)
+    base = y()
+    dW, db = layer.grad_weight(dyt, bsp.save8(xt))
+    dX = _host(layer.grad_input(dyt, code="e4m3", dtype=torch.float32))
+    for o, i in ((1, 1), (0, 5), (127, 255), (64, 130), (3, 127)):
+        W2 = W.copy()
+        W2[o, i] += 1.0
+        layer.update(W2)
+        assert ((y() - base) * dy).sum() == _host(dW)[o, i]
+        layer.update(W)
+    for t, i in ((0, 1), (5, 255), (23, 129)):
+        x[t, i] += 1.0
+        xt = torch.from_numpy(x).cuda()
+        assert ((_host(layer.fc(xt)) - base) * dy).sum() == dX[t, i]
+        x[t, i] -= 1.0
+    assert (_host(db) == dy.sum(0)).all()
+
+
+# ------------------------------------------------------------------------------- streams, graphs, long offsets
+def test_on_another_stream_and_in_a_graph():
+    import torch
+    rng = _rng(14)
+    bsp = _bsp()
+    x, t = _draw(rng, 130, 512, "bf16")
+    W, gamma, b, layer = _layer(rng, 384, 512, 0.6)
+    dy, dyt = _draw(rng, 130, 384, "bf16")
+
+    def step(t, dyt):
+        c = bsp.save8(t)
+        return [layer.fc(c, relu=True), layer.fc(t), layer.grad_input(dyt, relu_of=c), *layer.grad_weight(dyt, c)]
+    want = [_host(v) for v in step(t, dyt)]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = step(t, dyt)
+    assert all((_host(g) == w).all() for g, w in zip(got, want))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = step(t, dyt)
+    for k in range(3):
+        for o in got:
+            o.fill_(float("nan"))
+        t.copy_(torch.from_numpy(x * (k + 1)).to(torch.bfloat16))  # powers of two and not: other inputs each time
+        want = step(t, dyt)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_offsets_past_32_bits():
+    """A checkpoint of more than 2^31 codes: its last rows, and the gradients that read them."""
+    import torch
+    bsp = _bsp()
+    T, K = 270000, 8192
+    X = torch.zeros(1, K, device="cuda", dtype=torch.bfloat16).expand(T, K)
+    c = bsp.save8(X)
+    rng = _rng(15)
+    x, t = _draw(rng, 16, K, "bf16")
+    bsp_tail = bsp.save8(t)
+    c.codes[-16:] = bsp_tail.codes
+    c.scale[:, :T][:, -16:] = bsp_tail.scale[:, :16]
+    W = rng.standard_normal((128, K)).astype(np.float32) / 64
+    layer = bsp.BspLayerF8(W)
+    y = layer.fc(c, dtype=torch.bfloat16)
+    gamma = np.ones((1, K // 128), np.uint8)
+    ref = of8.fc(x, W, gamma)
+    assert (np.abs(_host(y[-16:]) - ref) <= _bound(x, W, gamma, False, ref)).all() and not bool(y[:-16].any())
+    dy = torch.zeros(T, 128, device="cuda", dtype=torch.bfloat16)
+    dy[-16:] = torch.randn(16, 128, device="cuda").to(torch.bfloat16)
+    dW, _ = layer.grad_weight(dy, c)
+    want, _ = of8.grad_weight(_host(dy[-16:]), of8.values(x, "e4m3"), gamma)
+    S, _ = of8.grad_weight(np.abs(_host(dy[-16:])), np.abs(of8.values(x, "e4m3")), gamma)
+    assert (np.abs(_host(dW) - want) <= 600 * U * S).all()  # 16 terms, up to 512 partial sums of zeros
+    assert (_host(c.load()[-16:]) == of8.values(x, "e4m3")).all()
