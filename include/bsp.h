@@ -411,7 +411,7 @@ int bsp_call_packed(int32_t call, const int64_t* words);
  * to even.  An infinity or NaN becomes the NaN code (BSP_E5M2 keeps infinities) and has no part in its block's scale.
  */
 typedef struct {
-  int32_t T, K;       /* rows and columns; T = 0 is valid */
+  int32_t T, K;       /* rows and columns (K <= 2^24); T = 0 is valid */
   int32_t dtype;      /* BSP_E4M3 or BSP_E5M2 */
   uint8_t* codes;     /* device [T][128 ceil(K/128)], 16-byte aligned; columns past K are code 0 */
   uint8_t* scale;     /* device [ceil(K/128)][16 ceil(T/16)] bytes e + 127, 16-byte aligned: a column block's rows together */
@@ -431,7 +431,7 @@ int bsp_f8_load(const bsp_codes* c, void* Y, int32_t y_dtype, int64_t ldy, void*
  * overhang over O and I code 0.  Held twice, once by block rows for the layer itself and once transposed by block columns
  * for the gradient of its input. */
 typedef struct {
-  int32_t O, I;
+  int32_t O, I;            /* <= 2^24 each */
   int64_t nnzb;            /* kept blocks */
   const int32_t* row_ptr;  /* device [ceil(O/128) + 1] */
   const int32_t* col_idx;  /* device [nnzb], ascending in a block row */
@@ -468,9 +468,10 @@ int bsp_f8_pack(const bsp_weights_f8* w, const void* W, int32_t w_dtype, int64_t
 int bsp_f8_fc(const bsp_weights_f8* w, int32_t transposed, const bsp_codes* X, const float* bias, const void* residual,
               int32_t relu, const bsp_codes* gate, void* Y, int32_t y_dtype, void* stream);
 
-/* The same on values: X [T][I] ([T][O] transposed) of x_dtype BSP_F32 or BSP_BF16 becomes codes of type `code` first, in
- * registers where the rows are few, else in `workspace` (device, 16-byte aligned, at least as many bytes as
- * bsp_f8_fc_workspace says, which may be 0; used until the call's work on the stream is done).
+/* The same on values: X [T][I] ([T][O] transposed) of x_dtype BSP_F32 or BSP_BF16 becomes codes of type `code` first.  Up to 16
+ * rows that are whole 16-byte pieces at 16-byte addresses, T (129 ceil(K/128) + 16) <= 73728, do so inside the product's kernel;
+ * others in `workspace` (device, 16-byte aligned, as many bytes as bsp_f8_fc_workspace says; used until the call's work
+ * on the stream is done; null and 0 for the former).
  * Results are those of bsp_f8_save and bsp_f8_fc.  Errors: as these, CAPACITY. */
 int bsp_f8_fc_workspace(const bsp_weights_f8* w, int32_t transposed, int32_t T, int64_t* bytes);
 int bsp_f8_fc_values(const bsp_weights_f8* w, int32_t transposed, const void* X, int32_t x_dtype, int64_t ldx, int32_t T,

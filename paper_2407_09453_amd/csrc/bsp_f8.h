@@ -86,7 +86,7 @@ struct F8Epilogue {
   const void* residual;  // [T][O] of Y's type, or null
   const uint8_t* gate;   // codes [T][128 ceil(O / 128)], or null: a result is kept where its code stands for a value > 0
   int32_t relu, gate_e5;
-  int32_t vec;           // rows of Y, of the residual and the gate are aligned to four elements
+  int32_t vec, vec8;     // rows of Y, of the residual and the gate are aligned to four, to eight elements
 };
 
 // channels o .. o+3 (those below O) of row t
@@ -168,7 +168,10 @@ struct F8Input {      // rows to multiply: codes with their scales, or values br
   int32_t e5;         // the codes are e5m2
   int64_t ld;         // elements from row to row
 };
-// few rows: no LDS staging, the contraction split over a workgroup's waves
+// Few rows: the contraction split over a workgroup's waves.  Rows given as values become codes in each workgroup's LDS, T <= 16 of them and
+// no more than kFewStaged bytes.
+enum { kFewStaged = 72 * 1024 };
+inline int64_t f8_few_staged(int T, int K) { return (int64_t)T * (f8_blocks(K) * (F8_BLOCK + 1) + 16); }
 int f8_launch_few(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, hipStream_t st);
 // many rows, codes only
 int f8_launch_tile(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, hipStream_t st);

@@ -8,6 +8,7 @@ inline bool value_type(int d) { return d == BSP_F32 || d == BSP_BF16; }
 inline bool code_type(int d) { return d == BSP_E4M3 || d == BSP_E5M2; }
 inline unsigned size_of(int d) { return d == BSP_F32 ? 4 : 2; }
 constexpr int32_t kMost = INT32_MAX - 65536;  // rows and columns: sizes rounded up stay in 32 bits
+constexpr int32_t kWide = 1 << 24;            // columns of codes: 256 rows' offsets stay in 32 bits
 
 // a matrix of values whose rows are `ld` elements apart; rows of an input may be the same one (ld = 0)
 int check_values(const void* p, int dtype, int64_t ld, int T, int K, bool input) {
@@ -21,14 +22,14 @@ int check_values(const void* p, int dtype, int64_t ld, int T, int K, bool input)
 int check_codes(const bsp_codes* c) {
   if (!c) return BSP_ERR_NULL;
   if (!code_type(c->dtype)) return BSP_ERR_DTYPE;
-  if (c->T < 0 || c->T > kMost || c->K < 1 || c->K > kMost) return BSP_ERR_SHAPE;
+  if (c->T < 0 || c->T > kMost || c->K < 1 || c->K > kWide) return BSP_ERR_SHAPE;
   if (c->T > 0 && (!c->codes || !c->scale)) return BSP_ERR_NULL;
   return aligned(c->codes, 16) && aligned(c->scale, 16) ? BSP_OK : BSP_ERR_ALIGN;
 }
 
 int check_weights(const bsp_weights_f8* w) {
   if (!w) return BSP_ERR_NULL;
-  if (w->O < 1 || w->O > kMost || w->I < 1 || w->I > kMost) return BSP_ERR_SHAPE;
+  if (w->O < 1 || w->O > kWide || w->I < 1 || w->I > kWide) return BSP_ERR_SHAPE;
   if (w->nnzb < 0 || w->nnzb > INT32_MAX || w->nnzb > (int64_t)f8_blocks(w->O) * f8_blocks(w->I)) return BSP_ERR_SHAPE;
   if (!w->row_ptr || !w->col_ptr) return BSP_ERR_NULL;
   if (w->nnzb > 0 && (!w->col_idx || !w->row_idx || !w->payload || !w->scale || !w->payload_t || !w->scale_t)) return BSP_ERR_NULL;
@@ -43,9 +44,14 @@ F8Rows rows_of(const bsp_weights_f8* w, bool transposed) {
   return F8Rows{w->row_ptr, w->col_idx, w->payload, w->scale, w->O, w->I, w->nnzb};
 }
 
-// up to here values become codes in the registers of the kernel that multiplies them
-constexpr int kInRegisters = 16;
-constexpr int kFewRows = 64;
+// Whether values become codes inside the kernel that multiplies them: few rows, of whole aligned pieces of 16 bytes, that fit its LDS.
+bool in_kernel(const void* X, int dtype, int64_t ld, int T, int K) {
+  return T <= 16 && f8_few_staged(T, K) <= kFewStaged &&
+         ((reinterpret_cast<uintptr_t>(X) | (uintptr_t)(ld * size_of(dtype)) | (uintptr_t)(K * (int64_t)size_of(dtype))) & 15u) == 0;
+}
+// up to here the kernel without LDS tiles (us, it and the smallest tile: 32 x 4096 -> 4096 8.8 and 10.7, 64 x 4096 -> 4096 12.5 and 11.0,
+// 64 x 16384 -> 1024 38.8 and 34.8, 64 x 512 -> 16384 9.3 and 5.7)
+constexpr int kFewRows = 32;
 
 int check_product(const bsp_weights_f8* w, int32_t transposed, int32_t T, const float* bias, const void* residual, int32_t relu,
                   const bsp_codes* gate, void* Y, int32_t y_dtype, F8Epilogue* q) {
@@ -60,7 +66,7 @@ int check_product(const bsp_weights_f8* w, int32_t transposed, int32_t T, const 
   }
   if (T > 0 && !Y) return BSP_ERR_NULL;
   if (!aligned(Y, 16) || !aligned(residual, 16) || !aligned(bias, 4)) return BSP_ERR_ALIGN;
-  *q = F8Epilogue{Y, bias, residual, gate ? gate->codes : nullptr, relu != 0, gate ? gate->dtype == BSP_E5M2 : 0, out % 4 == 0};
+  *q = F8Epilogue{Y, bias, residual, gate ? gate->codes : nullptr, relu != 0, gate ? gate->dtype == BSP_E5M2 : 0, out % 4 == 0, out % 8 == 0};
   return BSP_OK;
 }
 
@@ -117,7 +123,7 @@ int bsp_f8_fc_workspace(const bsp_weights_f8* w, int32_t transposed, int32_t T, 
   const int rc = check_weights(w);
   if (rc != BSP_OK) return rc;
   if (T < 0 || T > kMost) return BSP_ERR_SHAPE;
-  *bytes = T <= kInRegisters ? 0 : codes_bytes(T, transposed ? w->O : w->I);
+  *bytes = codes_bytes(T, transposed ? w->O : w->I);
   return BSP_OK;
 }
 
@@ -133,7 +139,7 @@ int bsp_f8_fc_values(const bsp_weights_f8* w, int32_t transposed, const void* X,
   if (rc != BSP_OK || T == 0) return rc;
   const bool e5 = code == BSP_E5M2;
   hipStream_t st = (hipStream_t)stream;
-  if (T <= kInRegisters) return multiply(w, transposed, F8Input{X, nullptr, x_dtype, e5, ldx}, T, q, y_dtype, st);
+  if (in_kernel(X, x_dtype, ldx, T, K)) return multiply(w, transposed, F8Input{X, nullptr, x_dtype, e5, ldx}, T, q, y_dtype, st);
   if (workspace_bytes < codes_bytes(T, K)) return BSP_ERR_CAPACITY;
   if (!workspace) return BSP_ERR_NULL;
   if (!aligned(workspace, 16)) return BSP_ERR_ALIGN;

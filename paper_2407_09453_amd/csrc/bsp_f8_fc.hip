@@ -7,6 +7,7 @@
 // A staged row of 128 bytes is eight pieces of 16; piece p of row r lies at place p ^ (r / 2 mod 8), so sixteen rows' same
 // piece, which sixteen lanes read together, lie in sixteen different bank groups.
 #include "bsp_f8.h"
+#include <type_traits>
 
 namespace {
 
@@ -27,6 +28,90 @@ __device__ __forceinline__ f32x16_t mfma_bf16_32x32x16(u32x4_t a, u32x4_t b, f32
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 
+// A wave's results, 32 MO channels of 32 MT rows, to Y.  In the accumulators a lane holds four channels of a row, and stored from there a
+// request would touch 32 rows.  So 32 rows at a time pass through LDS (the wave's own part, each row 16 bytes longer than
+// its values, in fp32 where a residual is still to be added) and leave as whole 64 MO-byte pieces of rows.
+template <int MO>
+constexpr int kStoreBytes = 32 * (32 * MO * 4 + 16);
+
+template <int MO, int MT>
+__device__ __forceinline__ void store_tile(const F8Epilogue& q, f32x16_t (&acc)[MO][MT], uint8_t* lds, int T, int O, int64_t t0, int o0) {
+  const int lane = threadIdx.x & 63;
+  constexpr int kLanes = 4 * MO;  // lanes that hold a row's piece, eight channels each
+  const int c = o0 + (lane % kLanes) * 8;
+  if (q.residual || !q.vec8) {  // fp32 through LDS, then four channels at a time
+    constexpr int kRow = 32 * MO * 4 + 16;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+#pragma unroll
+      for (int o = 0; o < MO; ++o)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          *(f32x4_t*)(lds + (lane & 31) * kRow + (o * 32 + k * 8 + (lane >> 5) * 4) * 4) =
+              f32x4_t{acc[o][m][4 * k], acc[o][m][4 * k + 1], acc[o][m][4 * k + 2], acc[o][m][4 * k + 3]};
+#pragma unroll 1
+      for (int r = lane / (8 * MO); r < 32; r += 8 / MO) {
+        const int64_t t = t0 + m * 32 + r;
+        const int ch = o0 + (lane % (8 * MO)) * 4;
+        const f32x4_t v = *(const f32x4_t*)(lds + r * kRow + (lane % (8 * MO)) * 16);
+        if (t < T && ch < O) f8_store4<false>(q, t, ch, O, v[0], v[1], v[2], v[3]);
+      }
+    }
+    return;
+  }
+  constexpr int kRow = 32 * MO * 2 + 16;
+  f32x4_t bias[MO][4] = {};
+  if (q.bias) {
+#pragma unroll
+    for (int o = 0; o < MO; ++o)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int ch = o0 + o * 32 + k * 8 + (lane >> 5) * 4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bias[o][k][e] = q.bias[ch + e < O ? ch + e : O - 1];
+      }
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+#pragma unroll
+    for (int o = 0; o < MO; ++o)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = acc[o][m][4 * k + e] + bias[o][k][e];
+          if (q.relu) v[e] = v[e] < 0.f ? 0.f : v[e];
+        }
+        *(u32x2_t*)(lds + (lane & 31) * kRow + (o * 32 + k * 8 + (lane >> 5) * 4) * 2) = u32x2_t{f8_pack_bf16x2(v[0], v[1]), f8_pack_bf16x2(v[2], v[3])};
+      }
+#pragma unroll 4
+    for (int r = lane / kLanes; r < 32; r += 64 / kLanes) {
+      const int64_t t = t0 + m * 32 + r;
+      u32x4_t v = *(const u32x4_t*)(lds + r * kRow + (lane % kLanes) * 16);
+      if (t >= T || c >= O) continue;
+      if (q.gate) {
+        const u32x2_t g = *(const u32x2_t*)(q.gate + t * (int64_t)f8_blocks(O) * F8_BLOCK + c);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (!f8_positive((g[e >> 2] >> (8 * (e & 3))) & 0xFFu, q.gate_e5)) v[e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+      }
+      __builtin_nontemporal_store(v, (u32x4_t*)((uint16_t*)q.Y + t * O + c));
+    }
+  }
+}
+
+// Which tile a workgroup takes: workgroups go to the eight XCDs in turn, an XCD takes an eighth of the tiles, and its tiles follow one another
+// in bands of four tiles of channels, so that what it runs at one time (32) shares four tiles' weights and eight tiles' rows in its L2.
+__device__ __forceinline__ void place_tile(int b, int tiles_o, int tiles_t, int* to, int* tt) {
+  const int total = tiles_o * tiles_t, each = total >> 3, more = total & 7, xcd = b & 7;
+  const int j = xcd * each + (xcd < more ? xcd : more) + (b >> 3);
+  const int band = j / (4 * tiles_t), r = j - band * 4 * tiles_t;
+  const int wide = tiles_o - band * 4 < 4 ? tiles_o - band * 4 : 4;
+  *to = band * 4 + r % wide;
+  *tt = r / wide;
+}
+
 // MO x MT tiles of 32 x 32 a wave, WO x WT waves; R block rows
 template <int MO, int MT, int WO, int WT, bool E5, bool F32>
 __global__ __launch_bounds__(64 * WO * WT) void f8_tile(TileArgs a) {
@@ -36,7 +121,8 @@ __global__ __launch_bounds__(64 * WO * WT) void f8_tile(TileArgs a) {
   extern __shared__ uint8_t lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wo = wave / WT, wt = wave % WT;
-  const int tile_o = blockIdx.x % a.tiles_o, tile_t = blockIdx.x / a.tiles_o;
+  int tile_o, tile_t;
+  place_tile(blockIdx.x, a.tiles_o, a.tiles_t, &tile_o, &tile_t);
   const int br = tile_o * R;
   const int64_t t0 = (int64_t)tile_t * NT;
   const int n0 = a.w.ptr[br], n1 = a.w.ptr[br + 1];
@@ -134,24 +220,264 @@ __global__ __launch_bounds__(64 * WO * WT) void f8_tile(TileArgs a) {
   }
 }
 
-template <int MO, int MT, int WO, int WT, bool E5, bool F32>
-int launch(TileArgs a, hipStream_t st) {
-  constexpr int NO = 32 * MO * WO, NT = 32 * MT * WT;
-  constexpr int lds = 2 * (NO + NT) * F8_BLOCK;
-  static const bool raised = hipFuncSetAttribute((const void*)&f8_tile<MO, MT, WO, WT, E5, F32>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
+// ------------------------------------------------------------------ the kernel
+// A wave overlaps its own work: it reads one half of a step (64 columns) while it multiplies the other, and one barrier a step,
+// between the halves, both frees the buffer that all have read and hands over the one that has landed.  The copies of the
+// step BUFS later then go into the buffer just freed and have BUFS - 1 steps to arrive; a wave waits for its own copies of
+// the next step by their count, not for all that it has asked for.
+template <int MO, int MT, int WO, int WT, int BUFS>
+struct Wide {
+  static constexpr int NO = 32 * MO * WO, NT = 32 * MT * WT, WAVES = WO * WT, R = NO / F8_BLOCK;
+  static constexpr int QO = NO / 8 / WAVES, QT = NT / 8 / WAVES, COPIES = QO + QT + 1;  // requests a wave and step: weights, rows, the rows' scales
+  static constexpr int SCALES = (NO + NT) * F8_BLOCK;                                   // where they lie in a buffer
+  static constexpr int STAGE = SCALES + WAVES * 256;  // (a request is 256 bytes, 32 MT of them scales that the wave wants)
+  static constexpr int kStored = WAVES * kStoreBytes<MO>;
+  static constexpr int kLds = BUFS * STAGE > kStored ? BUFS * STAGE : kStored;
+  static_assert(WAVES % 2 == 0 && NO % F8_BLOCK == 0 && NO % (8 * WAVES) == 0 && NT % (8 * WAVES) == 0 && kLds <= 160 * 1024);
+
+  const uint8_t *payload, *X, *S;  // first block; the tile's rows, and their scales
+  int64_t srows;
+  int cnt, wave;
+  uint32_t from_w, from_x[QT], from_s;  // this lane's places in a request
+  int at[2][2], at_s, at_w, at_x;
+
+  // 64 lanes x 16 bytes from `base` (the same in every lane) + at.  The base is hidden from the optimiser, which would keep base + at
+  // of every request in two registers a lane each through the loop.
+  static __device__ __forceinline__ void request(const uint8_t* base, uint32_t at, uint8_t* to) {
+    asm volatile("" : "+s"(base));
+    __builtin_amdgcn_global_load_lds((f8_gptr_t)(base + at), (f8_lptr_t)to, 16, 0, 0);
+  }
+  __device__ __forceinline__ void copy(uint8_t* to, int i, int kb) const {
+    const uint8_t* w = payload + (int64_t)i * F8_BLOCK_BYTES;
+    const uint8_t* x = X + (int64_t)kb * F8_BLOCK;
+#pragma unroll
+    for (int q = 0; q < QO; ++q) {
+      const int row = q * 8 * WAVES;
+      request(w + (R == 1 ? 0 : (int64_t)(row >> 7) * cnt * F8_BLOCK_BYTES) + (row & 127) * F8_BLOCK, from_w, to + wave * 1024 + row * F8_BLOCK);
+    }
+#pragma unroll
+    for (int q = 0; q < QT; ++q) request(x, from_x[q], to + wave * 1024 + (NO + q * 8 * WAVES) * F8_BLOCK);
+    const uint8_t* s = S + (int64_t)kb * srows;
+    asm volatile("" : "+s"(s));
+    __builtin_amdgcn_global_load_lds((f8_gptr_t)(s + from_s), (f8_lptr_t)(to + SCALES + wave * 256), 4, 0, 0);
+  }
+  __device__ __forceinline__ void read(const uint8_t* from, int h, i32x8_t (&w)[MO], i32x8_t (&x)[MT]) const {
+#pragma unroll
+    for (int o = 0; o < MO; ++o) w[o] = read_fragment(from + at_w + o * 32 * F8_BLOCK, at[h][0], at[h][1]);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) x[m] = read_fragment(from + at_x + m * 32 * F8_BLOCK, at[h][0], at[h][1]);
+  }
+  __device__ __forceinline__ void read_scales(const uint8_t* from, int (&s)[MT]) const {
+#pragma unroll
+    for (int m = 0; m < MT; ++m) s[m] = from[at_s + m * 32];
+  }
+  template <bool E5>
+  static __device__ __forceinline__ void multiply(i32x8_t (&w)[MO], i32x8_t (&x)[MT], int sw, int (&sx)[MT], f32x16_t (&acc)[MO][MT]) {
+#pragma unroll
+    for (int o = 0; o < MO; ++o)
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+        acc[o][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[o], x[m], acc[o][m], 0, E5 ? 1 : 0, 0, sw, 0, sx[m]);
+  }
+
+  // Step i, whose first half has been read.  LATER: steps to come that have been asked for (all of the BUFS - 1 that fit in the
+  // main loop, where this step asks for one more).  `to` is written behind the barrier alone, `from` and `next` are other
+  // bytes by then: the compiler need not order its reads of LDS behind copies in flight, the waits here do.
+  template <bool E5, int LATER, bool MORE>
+  __device__ __forceinline__ void step(uint8_t* __restrict__ to, const uint8_t* __restrict__ from, const uint8_t* __restrict__ next, int i, int sw, int kb,
+                                       i32x8_t (&w)[2][MO], i32x8_t (&x)[2][MT], int (&sx)[2][MT], f32x16_t (&acc)[MO][MT]) const {
+    constexpr int N = MO * MT, kRead = 2 * (MO + MT);
+    read(from, 1, w[1], x[1]);
+    multiply<E5>(w[0], x[0], sw, sx[0], acc);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                   // one matrix instruction,
+      __builtin_amdgcn_sched_group_barrier(0x100, (kRead + N - 1) / N, 0);  // and what it hides: reads of LDS
+    }
+    constexpr int kLeft = LATER > 0 ? (LATER - 1) * COPIES : 0;
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLeft) : "memory");  // step i + 1 has landed, and this wave has read step i
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    constexpr int kHalf = (N + 1) / 2;
+    if constexpr (LATER > 0) {
+      read_scales(next, sx[1]);
+      read(next, 0, w[0], x[0]);
+    }
+    if constexpr (MORE) copy(to, i + BUFS, kb);
+    multiply<E5>(w[1], x[1], sw, sx[0], acc);
+#pragma unroll
+    for (int k = 0; k < kHalf; ++k) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if constexpr (LATER > 0) __builtin_amdgcn_sched_group_barrier(0x100, (kRead + MT + kHalf - 1) / kHalf, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < kHalf; ++k) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if constexpr (MORE) __builtin_amdgcn_sched_group_barrier(0x020, (COPIES + kHalf - 1) / kHalf, 0);  // copies to LDS
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) sx[0][m] = sx[1][m];
+  }
+};
+
+template <int MO, int MT, int WO, int WT, int BUFS, bool E5>
+__global__ __launch_bounds__(64 * WO * WT) void f8_wide(TileArgs a) {
+  using K = Wide<MO, MT, WO, WT, BUFS>;
+  extern __shared__ uint8_t lds[];
+  kernarg_touch<TileArgs>();
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wo = wave / WT, wt = wave % WT;
+  int tile_o, tile_t;
+  place_tile(blockIdx.x, a.tiles_o, a.tiles_t, &tile_o, &tile_t);
+  const int br = tile_o * K::R;
+  const int64_t t0 = (int64_t)tile_t * K::NT;
+  const int n0 = __builtin_amdgcn_readfirstlane(a.w.ptr[br]), cnt = __builtin_amdgcn_readfirstlane(a.w.ptr[br + 1]) - n0;
+  const int last = (int)(a.T - 1 - t0 < K::NT - 1 ? a.T - 1 - t0 : K::NT - 1);  // rows past the last: its bytes, their results go nowhere
+
+  K k;
+  k.payload = a.w.payload + (int64_t)n0 * F8_BLOCK_BYTES;
+  k.X = a.X + t0 * a.ld;
+  k.S = a.scale + t0;
+  k.srows = a.srows;
+  k.cnt = cnt;
+  k.wave = wave;
+  // this lane's 16 bytes of a request of eight rows
+  const int srow = wave * 8 + (lane >> 3), piece = ((lane & 7) ^ ((srow >> 1) & 7)) * 16;
+  k.from_w = srow * F8_BLOCK + piece;
+#pragma unroll
+  for (int q = 0; q < K::QT; ++q) {
+    const int row = srow + q * 8 * K::WAVES;
+    k.from_x[q] = (uint32_t)(row < last ? row : last) * (uint32_t)a.ld + piece;
+  }
+  // four rows' scales a lane; a scale array's last four bytes for rows past it
+  const int64_t s_end = a.srows - 4 - t0;
+  k.from_s = (uint32_t)(wt * MT * 32 + lane * 4 < s_end ? wt * MT * 32 + lane * 4 : s_end);
+  // the pieces that this lane reads of its row of a fragment, for the two halves of a step
+  const int f = (lane >> 1) & 7, g2 = (lane >> 5) * 2;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int q = 0; q < 2; ++q) k.at[h][q] = (lane & 31) * F8_BLOCK + (((4 * h + g2 + q) ^ f) << 4);
+  k.at_w = wo * MO * 32 * F8_BLOCK;
+  k.at_x = (K::NO + wt * MT * 32) * F8_BLOCK;
+  k.at_s = K::SCALES + wave * 256 + (lane & 31);
+
+  f32x16_t acc[MO][MT] = {};
+  if (cnt > 0) {
+    const int32_t* idx = a.w.idx + n0;
+    const uint8_t* scl = a.w.scale + n0 + (K::R == 1 ? 0 : ((wo * MO * 32) >> 7) * cnt);
+    const int col0 = idx[lane < cnt ? lane : cnt - 1];
+#pragma unroll
+    for (int j = 0; j < BUFS; ++j)
+      if (j < cnt) k.copy(lds + j * K::STAGE, j, __builtin_amdgcn_readlane(col0, j));
+    i32x8_t w[2][MO], x[2][MT];
+    int sx[2][MT];
+    // the last steps' weight scales, one a lane
+    const int tail = cnt > BUFS ? cnt - BUFS : 0;
+    const int tail_scales = scl[tail + lane < cnt ? tail + lane : cnt - 1];
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    k.read_scales(lds, sx[0]);
+    k.read(lds, 0, w[0], x[0]);
+    int cur = 0;
+    auto following = [](int b) { return b == (BUFS - 1) * K::STAGE ? 0 : b + K::STAGE; };
+    // block columns and weight scales of 64 steps at a time, one a lane
+    for (int c = 0; c < cnt - BUFS; c += 64) {
+      const int l = c + lane;
+      int cols = idx[l + BUFS < cnt ? l + BUFS : cnt - 1], scales = scl[l < cnt ? l : cnt - 1];
+      asm volatile("s_waitcnt vmcnt(0)" : "+v"(cols), "+v"(scales)::"memory");
+      const int end = c + 64 < cnt - BUFS ? c + 64 : cnt - BUFS;
+      for (int i = c; i < end; ++i) {
+        const int nxt = following(cur);
+        k.template step<E5, BUFS - 1, true>(lds + cur, lds + cur, lds + nxt, i, __builtin_amdgcn_readlane(scales, i - c),
+                                            __builtin_amdgcn_readlane(cols, i - c), w, x, sx, acc);
+        cur = nxt;
+      }
+    }
+    auto rest = [&](auto later) {  // the step with `later` steps behind it
+      constexpr int L = decltype(later)::value;
+      if (cnt > L) {
+        const int nxt = following(cur);
+        k.template step<E5, L, false>(lds + cur, lds + cur, lds + nxt, 0, __builtin_amdgcn_readlane(tail_scales, cnt - 1 - L - tail), 0, w, x, sx, acc);
+        cur = nxt;
+      }
+    };
+    if constexpr (BUFS > 3) rest(std::integral_constant<int, 3>{});
+    if constexpr (BUFS > 2) rest(std::integral_constant<int, 2>{});
+    rest(std::integral_constant<int, 1>{});
+    rest(std::integral_constant<int, 0>{});
+  }
+  __syncthreads();
+  store_tile<MO, MT>(a.q, acc, lds + wave * kStoreBytes<MO>, a.T, a.w.out, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32);
+}
+
+template <int NO, int NT>
+int launch(void (*kernel)(TileArgs), bool raised, int threads, int lds, TileArgs a, hipStream_t st) {
   if (!raised) return BSP_ERR_HIP;
   a.tiles_o = (a.w.out + NO - 1) / NO;
-  a.tiles_t = (a.T + NT - 1) / NT;
-  if ((int64_t)a.tiles_o * a.tiles_t > INT32_MAX) return BSP_ERR_SHAPE;
-  hipLaunchKernelGGL((f8_tile<MO, MT, WO, WT, E5, F32>), dim3((unsigned)(a.tiles_o * a.tiles_t)), dim3(64 * WO * WT), lds, st, a);
+  a.tiles_t = (int)(((int64_t)a.T + NT - 1) / NT);
+  if ((int64_t)a.tiles_o * a.tiles_t > INT32_MAX / 8) return BSP_ERR_SHAPE;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(a.tiles_o * a.tiles_t)), dim3(threads), lds, st, a);
   return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP;
+}
+bool raise(const void* kernel, int lds) { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess; }
+
+template <int MO, int MT, int WO, int WT, bool E5, bool F32>
+int launch_tile(const TileArgs& a, hipStream_t st) {
+  constexpr int NO = 32 * MO * WO, NT = 32 * MT * WT;
+  static const bool raised = raise((const void*)&f8_tile<MO, MT, WO, WT, E5, F32>, 2 * (NO + NT) * F8_BLOCK);
+  return launch<NO, NT>(f8_tile<MO, MT, WO, WT, E5, F32>, raised, 64 * WO * WT, 2 * (NO + NT) * F8_BLOCK, a, st);
+}
+template <int MO, int MT, int WO, int WT, int BUFS, bool E5>
+int launch_wide(const TileArgs& a, hipStream_t st) {
+  using K = Wide<MO, MT, WO, WT, BUFS>;
+  static const bool raised = raise((const void*)&f8_wide<MO, MT, WO, WT, BUFS, E5>, K::kLds);
+  return launch<K::NO, K::NT>(f8_wide<MO, MT, WO, WT, BUFS, E5>, raised, 64 * K::WAVES, K::kLds, a, st);
+}
+
+// Which tile: the smaller of the chip's rate on it and of the steps' own latency, one after the other.  `alone`: us a step where a CU has one
+// workgroup, `shared`: where it has as many as fit; `rate`: TFLOP/s of padded work with the chip full.  Measured on
+// T x I -> O of 65 .. 16384 x 512 .. 16384 -> 512 .. 16384, all blocks kept and half of them (us; 256x256, 128x256, 128x128, 128x64, 128x32):
+//   16384 x 4096 -> 16384  873 1079 1062 1307 2439     2048 x 4096 -> 4096  44 35 34 43 80     512 x 4096 -> 4096  43 30 23 15 21
+//   65 x 4096 -> 4096  37 29 18 13.5 11     4096 x 512 -> 512  12 9.5 6.6 5.8 7.2     2048 x 4096 -> 4096, half kept  - 24 25 29 57
+struct Tile {
+  int o, t, fit;
+  double alone, shared, rate;
+};
+constexpr Tile kTiles[] = {{256, 256, 1, 1.15, 1.15, 2500}, {128, 256, 1, 0.75, 0.75, 2150}, {128, 128, 2, 0.40, 0.85, 2200}, {128, 64, 2, 0.25, 0.50, 1700}, {128, 32, 1, 0.18, 0.18, 1000}};
+
+int pick_tile(int O, int64_t nnzb, int T, bool full) {
+  const double steps = (double)nnzb / f8_blocks(O);
+  int best = 2;
+  double least = 1e30;
+  for (int k = full && f8_blocks(O) % 2 == 0 ? 0 : 1; k < 5; ++k) {
+    const Tile& v = kTiles[k];
+    const double groups = (double)((f8_blocks(O) * F8_BLOCK + v.o - 1) / v.o) * (double)(((int64_t)T + v.t - 1) / v.t);
+    const double rounds = groups <= 256 ? v.alone : v.shared * (double)(int64_t)((groups + 256 * v.fit - 1) / (256 * v.fit));
+    const double us = rounds * steps, at_rate = groups * steps * v.o * v.t * 256e-6 / v.rate;
+    const double worse = us > at_rate ? us : at_rate;
+    if (worse < least) least = worse, best = k;
+  }
+  return best;
+}
+
+template <bool E5>
+int launch_any(const TileArgs& a, bool f32, hipStream_t st) {
+  if (f32) return launch_tile<2, 2, 2, 2, E5, true>(a, st);
+  const bool full = a.w.nnzb == (int64_t)f8_blocks(a.w.out) * f8_blocks(a.w.in);
+  switch (pick_tile(a.w.out, a.w.nnzb, a.T, full)) {
+    case 0: return launch_wide<4, 2, 2, 4, 2, E5>(a, st);
+    case 1: return launch_wide<4, 2, 1, 4, 3, E5>(a, st);
+    case 2: return launch_wide<2, 2, 2, 2, 2, E5>(a, st);
+    case 3: return launch_wide<2, 1, 2, 2, 3, E5>(a, st);
+    default: return launch_wide<1, 1, 4, 1, 4, E5>(a, st);
+  }
 }
 
 }  // namespace
 
 int f8_launch_tile(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, hipStream_t st) {
   TileArgs a{w, (const uint8_t*)x.X, x.scale, q, x.ld, f8_scale_rows(T), T, 0, 0};
-  const bool e5 = x.e5;
-  if (f32) return e5 ? launch<2, 2, 2, 2, true, true>(a, st) : launch<2, 2, 2, 2, false, true>(a, st);
-  return e5 ? launch<2, 2, 2, 2, true, false>(a, st) : launch<2, 2, 2, 2, false, false>(a, st);
+  return x.e5 ? launch_any<true>(a, f32, st) : launch_any<false>(a, f32, st);
 }

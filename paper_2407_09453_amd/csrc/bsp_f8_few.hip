@@ -2,10 +2,12 @@
 //
 // A workgroup owns 16 output channels and 16 MT rows; its waves share out the kept blocks of the channels' block row, each
 // adding its blocks' products in its own accumulators, and the waves' sums meet in LDS: the long axis is split inside the
-// workgroup, with no second launch and no memory for partial sums.  Operands go from memory to registers: a lane's 32 bytes of
-// a weight row are two loads, sixteen rows are 2 KB in one piece, and a block's lines are each asked for once in the chip.
-// Rows given as bf16 or fp32 are brought to codes in registers (MT = 1): a lane reads the 32 columns that it feeds to
-// the matrix core, the four lanes of a row exchange their largest magnitudes, and the codes are where they are wanted.
+// workgroup, with no second launch and no memory for partial sums.  Operands go from memory to registers, kAhead blocks
+// before they are multiplied: a lane's 32 bytes of a weight row are pieces g and 4 + g of sixteen, so that a request covers whole
+// 64-byte halves of sixteen lines that follow one another, and a block's lines are each asked for once in the chip.
+// Up to 16 rows given as bf16 or fp32, in whole aligned pieces of 16 bytes, become codes in LDS first, in every workgroup for itself, while the
+// first weights are on their way: less than a launch of its own takes
+// (us, 1 x 4096 -> 4096: 5.8, with rows that are codes 5.4; 1 x 25088 -> 4096, half of the blocks kept, 13.9; 1 x 4096 -> 16384 14.6, 4.6 TB/s).
 #include "bsp_f8.h"
 
 namespace {
@@ -15,7 +17,8 @@ struct FewArgs {
   F8Input x;
   F8Epilogue q;
   int64_t srows;   // rows of x.scale
-  int32_t T, xvec;
+  int32_t T, rows;  // rows: how many become codes in LDS
+  int32_t full;    // blocks in a block row, where all are kept; else 0
 };
 
 // 128 products per lane row: scaled codes, or (F32) both sides as bf16 so that nothing is lost in the sum.  The instruction on
@@ -35,82 +38,136 @@ __device__ __forceinline__ f32x4_t few_mfma(i32x8_t a, int sa, i32x8_t b, int sb
 }
 
 enum { kCodes, kBf16, kF32 };  // what the rows are given as
+
+// A workgroup's rows as codes in LDS: [row][Kp + 16] (sixteen rows' same piece then lies in different banks), behind them the scales [row][blocks].
+// Eight lanes take a block of a row, sixteen values each; a row ends between two pieces of 16 bytes, those past it are zeros.
 template <int SRC, bool E5>
-__device__ __forceinline__ i32x8_t few_input(const FewArgs& a, int64_t t, int kb, int g, int* scale) {
-  if constexpr (SRC == kCodes) {
-    *scale = a.x.scale[kb * a.srows + t];
-    const i32x8_t* p = (const i32x8_t*)((const uint8_t*)a.x.X + t * a.x.ld + kb * F8_BLOCK + g * 32);
-    return *p;
-  } else {
-    float v[32];
-    const int k0 = kb * F8_BLOCK + g * 32, left = a.w.in - k0;
-    if (a.xvec && left >= 32) {
-      if constexpr (SRC == kBf16) {
-        const u32x4_t* p = (const u32x4_t*)((const uint16_t*)a.x.X + t * a.x.ld + k0);
+__device__ __forceinline__ void few_stage(const FewArgs& a, uint8_t* codes, uint8_t* scale, int64_t t0, int rows) {
+  constexpr int kBytes = SRC == kBf16 ? 2 : 4, kPieces = kBytes;
+  const int nb = f8_blocks(a.w.in), per_row = nb * 8;
+  for (int i = threadIdx.x; i < rows * per_row; i += blockDim.x) {  // (whole groups of eight lanes)
+    const int row = i / per_row, k0 = (i - row * per_row) * 16;
+    const uint8_t* p = (const uint8_t*)a.x.X + ((t0 + row) * a.x.ld + k0) * kBytes;
+    float v[16];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const u32x4_t w = p[k];
+    for (int k = 0; k < kPieces; ++k) {
+      const bool in = k0 + k * (16 / kBytes) < a.w.in;
+      u32x4_t w = *(const u32x4_t*)(in ? p + k * 16 : (const uint8_t*)a.x.X);
+      w = in ? w : u32x4_t{0, 0, 0, 0};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            v[8 * k + 2 * j] = __uint_as_float(w[j] << 16);
-            v[8 * k + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-          }
-        }
-      } else {
-        const f32x4_t* p = (const f32x4_t*)((const float*)a.x.X + t * a.x.ld + k0);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const f32x4_t w = p[k];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[4 * k + j] = w[j];
-        }
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < 32; ++k) {
-        v[k] = 0.f;
-        if (k < left) v[k] = SRC == kF32 ? ((const float*)a.x.X)[t * a.x.ld + k0 + k] : bf16_bits_to_f32(((const uint16_t*)a.x.X)[t * a.x.ld + k0 + k]);
-      }
+      for (int e = 0; e < 16 / kBytes; ++e)
+        v[k * (16 / kBytes) + e] = __uint_as_float(SRC == kF32 ? w[e & 3] : e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
     }
     uint32_t m = 0;
 #pragma unroll
-    for (int k = 0; k < 32; ++k) m = max(m, f8_magnitude(v[k]));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 16));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 32));
+    for (int k = 0; k < 16; ++k) m = max(m, f8_magnitude(v[k]));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 1));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 2));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 4));
     const int b = f8_scale_byte<E5>(m);
     const float s = f8_inverse(b);
-    i32x8_t q;
+    u32x4_t q;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) q[k] = (int)f8_encode4<E5>(v[4 * k] * s, v[4 * k + 1] * s, v[4 * k + 2] * s, v[4 * k + 3] * s);
-    *scale = b;
-    return q;
+    for (int k = 0; k < 4; ++k) q[k] = f8_encode4<E5>(v[4 * k] * s, v[4 * k + 1] * s, v[4 * k + 2] * s, v[4 * k + 3] * s);
+    *(u32x4_t*)(codes + row * (nb * F8_BLOCK + 16) + k0) = q;
+    if ((k0 & 127) == 0) scale[row * nb + (k0 >> 7)] = (uint8_t)b;
   }
 }
 
+// Waves a workgroup may have: sixteen leave each 128 registers, eight 256.
+template <int MT>
+constexpr int kMostWaves = MT == 1 ? 16 : 8;
+
 template <int MT, int SRC, bool E5, bool F32>
-__global__ __launch_bounds__(1024) void f8_few(FewArgs a) {
-  extern __shared__ float sums[];  // [waves][MT][64][4]
+__global__ __launch_bounds__((64 * kMostWaves<MT>)) void f8_few(FewArgs a) {
+  constexpr int kAhead = MT == 1 && F32 ? 3 : 4;
+  extern __shared__ float sums[];  // [waves][MT][64][4], behind them the rows' codes
+  kernarg_touch<FewArgs>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int r = lane & 15, g = lane >> 4;
   const int br = blockIdx.x >> 3;
-  const int n1 = a.w.ptr[br + 1];
-  const uint8_t* wp = a.w.payload + ((blockIdx.x & 7) * 16 + r) * F8_BLOCK + g * 32;
-  int64_t t[MT];
+  // (where all blocks are kept their places need not be read)
+  const int n0 = a.full ? br * a.full : __builtin_amdgcn_readfirstlane(a.w.ptr[br]);
+  const int cnt = a.full ? a.full : __builtin_amdgcn_readfirstlane(a.w.ptr[br + 1]) - n0;
+  const int mine = cnt > wave ? (cnt - wave + waves - 1) / waves : 0;
+  const uint8_t* wp = a.w.payload + (int64_t)n0 * F8_BLOCK_BYTES + ((blockIdx.x & 7) * 16 + r) * F8_BLOCK + g * 16;
+  const int64_t t0 = (int64_t)blockIdx.y * (16 * MT);
+  // rows past the last: the last one's bytes, their results go nowhere
+  const uint8_t *xp[MT], *xs[MT];
+  const int nb = f8_blocks(a.w.in);
+  uint8_t *staged = (uint8_t*)(sums + waves * MT * 256), *staged_scale = staged + a.rows * (nb * F8_BLOCK + 16);
+  int64_t scale_step;
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    const int64_t row = (int64_t)blockIdx.y * (16 * MT) + m * 16 + r;
-    t[m] = row < a.T ? row : a.T - 1;  // rows past the last read the last one's bytes; their results go nowhere
-  }
-  f32x4_t acc[MT] = {};
-  for (int n = a.w.ptr[br] + wave; n < n1; n += waves) {
-    const int kb = a.w.idx[n], sw = a.w.scale[n];
-    const i32x8_t w = *(const i32x8_t*)(wp + (int64_t)n * F8_BLOCK_BYTES);
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      int sx;
-      const i32x8_t x = few_input<SRC, E5>(a, t[m], kb, g, &sx);
-      acc[m] = few_mfma<F32, E5>(w, sw, x, sx, acc[m]);
+    const int64_t row = t0 + m * 16 + r < a.T ? t0 + m * 16 + r : a.T - 1;
+    if constexpr (SRC == kCodes) {
+      xp[m] = (const uint8_t*)a.x.X + row * a.x.ld + g * 16;
+      xs[m] = a.x.scale + row;
+      scale_step = a.srows;
+    } else {
+      xp[m] = staged + (int)(row - t0) * (nb * F8_BLOCK + 16) + g * 16;
+      xs[m] = staged_scale + (int)(row - t0) * nb;
+      scale_step = 1;
     }
+  }
+  u32x4_t w[kAhead][2], x[kAhead][MT][2];
+  int ws[kAhead], col[kAhead], sx[kAhead][MT];
+  f32x4_t acc[MT] = {};
+  for (int c = 0; c < mine || c == 0; c += 64) {  // the wave's block columns, 64 at a time, one a lane
+    const int of = wave + (c + lane) * waves < cnt ? wave + (c + lane) * waves : cnt - 1;
+    const int cols = a.full ? of : cnt > 0 ? a.w.idx[n0 + of] : 0;
+    const int end = mine - c < 64 ? mine - c : 64;
+    auto rows = [&](int j) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        x[j][m][0] = *(const u32x4_t*)(xp[m] + (int64_t)col[j] * F8_BLOCK);
+        x[j][m][1] = *(const u32x4_t*)(xp[m] + (int64_t)col[j] * F8_BLOCK + 64);
+        sx[j][m] = xs[m][col[j] * scale_step];
+      }
+    };
+    auto load = [&](int s, int j) {
+      const int n = wave + (c + s) * waves;
+      const u32x4_t* p = (const u32x4_t*)(wp + (int64_t)n * F8_BLOCK_BYTES);
+      w[j][0] = p[0];
+      w[j][1] = p[4];
+      ws[j] = a.w.scale[n0 + n];
+      col[j] = __builtin_amdgcn_readlane(cols, s);
+      if constexpr (SRC == kCodes) rows(j);
+    };
+    auto multiply = [&](int j) {
+      if constexpr (SRC != kCodes) rows(j);
+      const i32x8_t wv = {(int)w[j][0].x, (int)w[j][0].y, (int)w[j][0].z, (int)w[j][0].w, (int)w[j][1].x, (int)w[j][1].y, (int)w[j][1].z, (int)w[j][1].w};
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const i32x8_t xv = {(int)x[j][m][0].x, (int)x[j][m][0].y, (int)x[j][m][0].z, (int)x[j][m][0].w, (int)x[j][m][1].x, (int)x[j][m][1].y, (int)x[j][m][1].z, (int)x[j][m][1].w};
+        acc[m] = few_mfma<F32, E5>(wv, ws[j], xv, sx[j][m], acc[m]);
+      }
+    };
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (j < end) load(j, j);
+    if constexpr (SRC != kCodes) {
+      if (c == 0) {  // the first weights are on their way
+        few_stage<SRC, E5>(a, staged, staged_scale, t0, a.rows);
+        __syncthreads();
+      }
+    }
+    int s = 0;
+    for (; s + 2 * kAhead <= end; s += kAhead)
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        multiply(j);
+        load(s + kAhead + j, j);
+      }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (s + j < end) {
+        multiply(j);
+        if (s + kAhead + j < end) load(s + kAhead + j, j);
+      }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (s + kAhead + j < end) multiply(j);
   }
 #pragma unroll
   for (int m = 0; m < MT; ++m) *(f32x4_t*)(sums + ((wave * MT + m) * 64 + lane) * 4) = acc[m];
@@ -118,38 +175,44 @@ __global__ __launch_bounds__(1024) void f8_few(FewArgs a) {
   for (int i = threadIdx.x; i < MT * 64; i += blockDim.x) {
     f32x4_t s = *(const f32x4_t*)(sums + i * 4);
     for (int w = 1; w < waves; ++w) s += *(const f32x4_t*)(sums + (w * MT * 64 + i) * 4);
-    const int64_t row = (int64_t)blockIdx.y * (16 * MT) + (i >> 6) * 16 + (i & 15);
+    const int64_t row = t0 + (i >> 6) * 16 + (i & 15);
     const int o = blockIdx.x * 16 + ((i >> 4) & 3) * 4;
     if (row < a.T && o < a.w.out) f8_store4<F32>(a.q, row, o, a.w.out, s[0], s[1], s[2], s[3]);
   }
 }
 
-template <int MT, int SRC, bool E5>
-int launch(const FewArgs& a, bool f32, hipStream_t st) {
-  const int strips = (a.w.out + 15) / 16;
-  const int per_row = (int)(a.w.nnzb / f8_blocks(a.w.out)) + 1;
+template <int MT, int SRC, bool E5, bool F32>
+int launch(FewArgs a, hipStream_t st) {
+  const int strips = (a.w.out + 15) / 16, tiles = (a.T + 16 * MT - 1) / (16 * MT);
+  const int64_t per_row = (a.w.nnzb + f8_blocks(a.w.out) - 1) / f8_blocks(a.w.out);
+  // as many waves as a CU holds, on every CU; a wave for every block is enough
+  constexpr int most = kMostWaves<MT>;
   int waves = 1;
-  while (waves < 16 && waves < per_row) waves *= 2;
-  const dim3 grid((unsigned)strips, (unsigned)((a.T + 16 * MT - 1) / (16 * MT))), block((unsigned)(64 * waves));
-  const size_t lds = (size_t)waves * MT * 1024;
-  if (f32) hipLaunchKernelGGL((f8_few<MT, SRC, E5, true>), grid, block, lds, st, a);
-  else hipLaunchKernelGGL((f8_few<MT, SRC, E5, false>), grid, block, lds, st, a);
+  while (waves < most && waves < per_row && (waves < 2 || (int64_t)strips * tiles * waves < 256 * most)) waves *= 2;
+  int lds = waves * MT * 1024;
+  if constexpr (SRC != kCodes) {
+    a.rows = a.T;
+    lds += (f8_few_staged(a.T, a.w.in) + 15) & ~15;
+    static const bool raised = hipFuncSetAttribute((const void*)&f8_few<MT, SRC, E5, F32>, hipFuncAttributeMaxDynamicSharedMemorySize, kFewStaged + 16 * 1024 + 16) == hipSuccess;
+    if (!raised) return BSP_ERR_HIP;
+  }
+  hipLaunchKernelGGL((f8_few<MT, SRC, E5, F32>), dim3((unsigned)strips, (unsigned)tiles), dim3((unsigned)(64 * waves)), (size_t)lds, st, a);
   return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP;
 }
 
-template <bool E5>
-int launch_rows(const FewArgs& a, bool f32, hipStream_t st) {
-  if (a.x.dtype == BSP_BF16) return launch<1, kBf16, E5>(a, f32, st);
-  if (a.x.dtype == BSP_F32) return launch<1, kF32, E5>(a, f32, st);
-  if (a.T <= 16) return launch<1, kCodes, E5>(a, f32, st);
-  if (a.T <= 32) return launch<2, kCodes, E5>(a, f32, st);
-  return launch<4, kCodes, E5>(a, f32, st);
+template <bool E5, bool F32>
+int launch_rows(const FewArgs& a, hipStream_t st) {
+  if (a.x.dtype == BSP_BF16) return launch<1, kBf16, E5, F32>(a, st);
+  if (a.x.dtype == BSP_F32) return launch<1, kF32, E5, F32>(a, st);
+  if (a.T <= 16) return launch<1, kCodes, E5, F32>(a, st);
+  return launch<2, kCodes, E5, F32>(a, st);
 }
 
 }  // namespace
 
 int f8_launch_few(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, hipStream_t st) {
-  FewArgs a{w, x, q, f8_scale_rows(T), T, 0};
-  a.xvec = ((reinterpret_cast<uintptr_t>(x.X) | (uintptr_t)(x.ld * (x.dtype == BSP_F32 ? 4 : 2))) & 15u) == 0;
-  return x.e5 ? launch_rows<true>(a, f32, st) : launch_rows<false>(a, f32, st);
+  FewArgs a{w, x, q, f8_scale_rows(T), T, 0, 0};
+  if (w.nnzb == (int64_t)f8_blocks(w.out) * f8_blocks(w.in)) a.full = f8_blocks(w.in);
+  if (f32) return x.e5 ? launch_rows<true, true>(a, st) : launch_rows<false, true>(a, st);
+  return x.e5 ? launch_rows<true, false>(a, st) : launch_rows<false, false>(a, st);
 }

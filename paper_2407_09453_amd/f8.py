@@ -149,7 +149,8 @@ class BspLayerF8:
             _check(lib.bsp_f8_fc(self.struct, transposed, X.struct, *rest, st), "bsp_f8_fc")
             return out
         n = ctypes.c_int64(0)
-        _check(lib.bsp_f8_fc_workspace(self.struct, transposed, T, n), "bsp_f8_fc_workspace")
+        if not (T <= 16 and T * (_blocks(K) * 129 + 16) <= 73728 and (X.data_ptr() | ld * X.element_size() | K * X.element_size()) % 16 == 0):
+            _check(lib.bsp_f8_fc_workspace(self.struct, transposed, T, n), "bsp_f8_fc_workspace")
         ws = torch.empty(n.value, dtype=torch.uint8, device=out.device) if n.value else None
         _check(lib.bsp_f8_fc_values(self.struct, transposed, X.data_ptr() or None, _type(X), ld, T, CODES[code], *rest,
                                     None if ws is None else ws.data_ptr(), n.value, st), "bsp_f8_fc_values")
