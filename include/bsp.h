@@ -480,7 +480,7 @@ int bsp_f8_fc_values(const bsp_weights_f8* w, int32_t transposed, const void* X,
 
 /* The weights' gradient from the checkpoint of the layer's input, and the bias's:
  *   dW [O][I] float = sum over rows of dY[t][o] X[t][i] in kept blocks, 0 elsewhere;  db [O] float = sum over rows of dY
- *   dY   device bf16 [T][O], rows ldy elements apart;  X codes [T][I]
+ *   dY   device bf16 [T][O], rows ldy <= 2^25 elements apart;  X codes [T][I]
  *   dW, db  device, 16-byte aligned; either may be null.  T = 0 gives zeros.
  *   workspace  as above, bsp_f8_fc_grad_workspace bytes
  * fp32 sums in an order that depends on the sizes alone.  Asynchronous.  Errors: NULL, SHAPE, DTYPE, ALIGN, CAPACITY, HIP. */

@@ -26,6 +26,32 @@ __host__ __device__ inline int f8_blocks(int n) { return (n + F8_BLOCK - 1) / F8
 // rows of a scale array: one byte for each row of a column block, whole sixteens of them
 __host__ __device__ inline int64_t f8_scale_rows(int T) { return ((int64_t)T + 15) & ~(int64_t)15; }
 
+// Exchanges between neighbouring lanes without LDS: the lane whose number differs in bit 0, in bit 1; the mirrored lane of eight, of
+// sixteen; the lane 16 away in a pair of rows, 32 away.
+enum { kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140 };
+template <int CTRL>
+__device__ __forceinline__ uint32_t f8_from_lane(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true); }
+// the largest of eight or sixteen lanes, in each of them
+template <int LANES>
+__device__ __forceinline__ uint32_t f8_most(uint32_t m) {
+  m = max(m, f8_from_lane<kXor1>(m));
+  m = max(m, f8_from_lane<kXor2>(m));
+  m = max(m, f8_from_lane<kMirror8>(m));
+  if constexpr (LANES == 16) m = max(m, f8_from_lane<kMirror16>(m));
+  return m;
+}
+// a wave's sum, in every lane
+__device__ __forceinline__ float f8_wave_sum(float v) {
+  v += __uint_as_float(f8_from_lane<kXor1>(__float_as_uint(v)));
+  v += __uint_as_float(f8_from_lane<kXor2>(__float_as_uint(v)));
+  v += __uint_as_float(f8_from_lane<kMirror8>(__float_as_uint(v)));
+  v += __uint_as_float(f8_from_lane<kMirror16>(__float_as_uint(v)));
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
 // |x| as an ordered integer, 0 for infinities and NaN (they do not take part in a block's scale)
 __device__ __forceinline__ uint32_t f8_magnitude(float x) {
   const uint32_t u = __float_as_uint(x) & 0x7FFFFFFFu;
@@ -74,6 +100,79 @@ __device__ __forceinline__ u32x4_t f8_decode_bf16x8(uint32_t lo, uint32_t hi, fl
 __device__ __forceinline__ uint32_t f8_pack_bf16x2(float a, float b) {
   const bf16x2_t v = {(__bf16)a, (__bf16)b};  // v_cvt_pk_bf16_f32: to nearest, ties to even
   return __builtin_bit_cast(uint32_t, v);
+}
+
+// Eight values of a row of n >= 8, from column c, at any address that suits their type: one or two loads with no branch.  At the row's end
+// they are its last eight; f8_unpack8 moves them down by the `past` of them that lie before c, and fills up with zeros.
+template <bool F32>
+struct F8Raw8 {
+  u32x4_t v[F32 ? 2 : 1];
+};
+typedef u32x4_t __attribute__((aligned(2))) f8_any2_t;
+typedef u32x4_t __attribute__((aligned(4))) f8_any4_t;
+template <bool F32>
+__device__ __forceinline__ F8Raw8<F32> f8_raw8(const void* row, int c, int n) {
+  const int at = c + 8 <= n ? c : n - 8;
+  F8Raw8<F32> r;
+  if constexpr (F32) {
+    const f8_any4_t* p = (const f8_any4_t*)((const float*)row + at);
+    r.v[0] = p[0];
+    r.v[1] = p[1];
+  } else {
+    r.v[0] = *(const f8_any2_t*)((const uint16_t*)row + at);
+  }
+  return r;
+}
+__device__ __forceinline__ int f8_past(int c, int n) { return c + 8 <= n ? 0 : c < n ? c + 8 - n : 8; }
+// `ragged`: n is no multiple of eight (the same in all lanes)
+template <bool F32>
+__device__ __forceinline__ void f8_unpack8(const F8Raw8<F32>& r, int past, bool ragged, float* v) {
+  if constexpr (F32) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(r.v[k >> 2][k & 3]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[2 * k] = __uint_as_float(r.v[0][k] << 16);
+      v[2 * k + 1] = __uint_as_float(r.v[0][k] & 0xFFFF0000u);
+    }
+  }
+  if (ragged) {
+#pragma unroll
+    for (int d = 1; d < 8; d *= 2)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float up = k + d < 8 ? v[k + d < 8 ? k + d : 7] : 0.f;
+        v[k] = past & d ? up : v[k];
+      }
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = past == 8 ? 0.f : v[k];
+}
+// the first `left` of eight values to a row, at any address that suits their type
+template <bool F32>
+__device__ __forceinline__ void f8_store8(void* row, int c, int left, const float* v) {
+  if constexpr (F32) {
+    float* y = (float*)row + c;
+    if (left >= 8) {
+      ((f8_any4_t*)y)[0] = u32x4_t{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+      ((f8_any4_t*)y)[1] = u32x4_t{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
+      return;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < left) y[k] = v[k];
+  } else {
+    uint16_t* y = (uint16_t*)row + c;
+    const u32x4_t w = {f8_pack_bf16x2(v[0], v[1]), f8_pack_bf16x2(v[2], v[3]), f8_pack_bf16x2(v[4], v[5]), f8_pack_bf16x2(v[6], v[7])};
+    if (left >= 8) {
+      *(f8_any2_t*)y = w;
+      return;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < left) y[k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+  }
 }
 
 // whether a code stands for a value above zero
@@ -178,25 +277,23 @@ int f8_launch_tile(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q
 int f8_launch_save(const void* X, int x_f32, int64_t ldx, int T, int K, bool e5, uint8_t* codes, uint8_t* scale, hipStream_t st);
 int f8_launch_load(const uint8_t* codes, const uint8_t* scale, int T, int K, bool e5, void* Y, int y_f32, int64_t ldy, hipStream_t st);
 int f8_launch_pack(const bsp_weights_f8* w, const void* W, int w_f32, int64_t ldw, hipStream_t st);
-// weights' gradient: dW float [out][in], a kept block's entries or zeros; `part` as f8_grad_parts says
+// weights' and bias's gradient: dW float [O][I], a kept block's entries or zeros; db float [O]; either may be null
 struct F8GradArgs {
   const uint16_t* dY;   // bf16 [T][O]
   int64_t ldy;
   const uint8_t *codes, *scale;
   const int32_t *row_ptr, *col_idx;
-  float* dW;
-  float* part;
-  int32_t T, O, I, nbo, nbi, e5, split;
+  float *dW, *db;
+  float *part, *part_db;  // split > 1: [split][nnzb][128][128] and [split][O]
+  int32_t T, O, I, nbo, nbi, groups, e5, split;
   int64_t nnzb;
 };
 int f8_grad_split(int64_t nnzb, int T);              // into how many ranges of rows the sums are cut
 int f8_launch_grad(const F8GradArgs& a, hipStream_t st);
 int norm_parts(int T);                               // row ranges of a column sum
-int norm_launch_sum(const float* part, int parts, int O, float* out, hipStream_t st);
 int norm_launch_forward(const void* X, bool f32, int64_t ldx, int T, int D, const float* weight, const float* bias, float eps,
                         void* Y, int64_t ldy, int code, uint8_t* codes, uint8_t* scale, float* mean, float* rstd, hipStream_t st);
 int norm_launch_backward(const void* dY, int64_t ld_dy, const void* X, int64_t ldx, bool f32, const float* mean, const float* rstd, const float* weight,
                          int T, int D, void* dX, int64_t ld_dx, float* dweight, float* dbias, float* part, hipStream_t st);
-int f8_launch_colsum(const uint16_t* dY, int64_t ldy, int T, int O, float* part, float* db, hipStream_t st);
 
 #endif

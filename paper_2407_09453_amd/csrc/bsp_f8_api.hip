@@ -155,9 +155,8 @@ int bsp_f8_fc_grad_workspace(const bsp_weights_f8* w, int32_t T, int64_t* bytes)
   const int rc = check_weights(w);
   if (rc != BSP_OK) return rc;
   if (T < 0 || T > kMost) return BSP_ERR_SHAPE;
-  const int split = f8_grad_split(w->nnzb, T);
-  const int64_t sums = (((int64_t)norm_parts(T) * w->O * 4) + 15) & ~(int64_t)15;
-  *bytes = sums + (split > 1 ? (int64_t)split * w->nnzb * F8_BLOCK_BYTES * 4 : 0);
+  const int64_t split = f8_grad_split(w->nnzb, T);
+  *bytes = split > 1 ? split * (w->nnzb * F8_BLOCK_BYTES + w->O) * 4 : 0;
   return BSP_OK;
 }
 
@@ -170,21 +169,17 @@ int bsp_f8_fc_grad(const bsp_weights_f8* w, const void* dY, int64_t ldy, const b
   if (rc != BSP_OK) return rc;
   rc = check_values(dY, BSP_BF16, ldy, X->T, w->O, true);
   if (rc != BSP_OK) return rc;
-  if (X->K != w->I || f8_blocks(w->O) * (int64_t)f8_blocks(w->I) > INT32_MAX) return BSP_ERR_SHAPE;
+  if (X->K != w->I || ldy > (1 << 25) || f8_blocks(w->O) * (int64_t)f8_blocks(w->I) > INT32_MAX) return BSP_ERR_SHAPE;
   if (!aligned(dW, 16) || !aligned(db, 16) || !aligned(workspace, 16)) return BSP_ERR_ALIGN;
   if (workspace_bytes < need) return BSP_ERR_CAPACITY;
   if (need > 0 && !workspace) return BSP_ERR_NULL;
-  hipStream_t st = (hipStream_t)stream;
-  const int64_t sums = (((int64_t)norm_parts(X->T) * w->O * 4) + 15) & ~(int64_t)15;
-  if (dW) {
-    F8GradArgs a{};
-    a.dY = (const uint16_t*)dY, a.ldy = ldy, a.codes = X->codes, a.scale = X->scale, a.row_ptr = w->row_ptr, a.col_idx = w->col_idx;
-    a.dW = dW, a.part = (float*)((uint8_t*)workspace + sums), a.T = X->T, a.O = w->O, a.I = w->I;
-    a.nbo = f8_blocks(w->O), a.nbi = f8_blocks(w->I), a.e5 = X->dtype == BSP_E5M2, a.split = f8_grad_split(w->nnzb, X->T), a.nnzb = w->nnzb;
-    rc = f8_launch_grad(a, st);
-    if (rc != BSP_OK) return rc;
-  }
-  return db ? f8_launch_colsum((const uint16_t*)dY, ldy, X->T, w->O, (float*)workspace, db, st) : BSP_OK;
+  if (!dW && !db) return BSP_OK;
+  F8GradArgs a{};
+  a.dY = (const uint16_t*)dY, a.ldy = ldy, a.codes = X->codes, a.scale = X->scale, a.row_ptr = w->row_ptr, a.col_idx = w->col_idx;
+  a.dW = dW, a.db = db, a.T = X->T, a.O = w->O, a.I = w->I, a.nnzb = w->nnzb;
+  a.nbo = f8_blocks(w->O), a.nbi = f8_blocks(w->I), a.e5 = X->dtype == BSP_E5M2, a.split = f8_grad_split(w->nnzb, X->T);
+  a.part = (float*)workspace, a.part_db = a.part + (int64_t)a.split * w->nnzb * F8_BLOCK_BYTES;
+  return f8_launch_grad(a, (hipStream_t)stream);
 }
 
 int bsp_layer_norm(const void* X, int32_t dtype, int64_t ldx, int32_t T, int32_t D, const float* weight, const float* bias,

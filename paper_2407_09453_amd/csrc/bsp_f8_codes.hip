@@ -8,35 +8,28 @@
 
 namespace {
 
+// sixteen values of a row of n >= 8 from column c, as they are
 template <bool F32>
-__device__ __forceinline__ void load16(const void* X, int64_t at, int left, bool vec, float* v) {
-  if (vec && left >= 16) {
-    if constexpr (F32) {
-      const f32x4_t* p = (const f32x4_t*)((const float*)X + at);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const f32x4_t w = p[k];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[4 * k + j] = w[j];
-      }
-    } else {
-      const u32x4_t* p = (const u32x4_t*)((const uint16_t*)X + at);
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const u32x4_t w = p[k];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[8 * k + 2 * j] = __uint_as_float(w[j] << 16);
-          v[8 * k + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-        }
-      }
-    }
-    return;
-  }
+struct Raw16 {
+  F8Raw8<F32> v[2];
+};
+template <bool F32>
+__device__ __forceinline__ Raw16<F32> raw16(const void* X, int64_t at, int c, int n) {
+  const void* row = F32 ? (const void*)((const float*)X + at) : (const void*)((const uint16_t*)X + at);
+  return Raw16<F32>{{f8_raw8<F32>(row, c, n), f8_raw8<F32>(row, c + 8, n)}};
+}
+template <bool F32>
+__device__ __forceinline__ void unpack16(const Raw16<F32>& r, int c, int n, float* v) {
+  f8_unpack8<F32>(r.v[0], f8_past(c, n), (n & 7) != 0, v);
+  f8_unpack8<F32>(r.v[1], f8_past(c + 8, n), (n & 7) != 0, v + 8);
+}
+// the same of a row shorter than eight, one by one
+template <bool F32>
+__device__ __forceinline__ void thin16(const void* X, int64_t at, int c, int n, float* v) {
 #pragma unroll
   for (int k = 0; k < 16; ++k) {
     v[k] = 0.f;
-    if (k < left) v[k] = F32 ? ((const float*)X)[at + k] : bf16_bits_to_f32(((const uint16_t*)X)[at + k]);
+    if (c + k < n) v[k] = F32 ? ((const float*)X)[at + c + k] : bf16_bits_to_f32(((const uint16_t*)X)[at + c + k]);
   }
 }
 
@@ -44,7 +37,7 @@ struct SaveArgs {
   const void* X;
   uint8_t *codes, *scale;
   int64_t ldx, srows;
-  int32_t T, K, Kp, vec;
+  int32_t T, K, Kp;
 };
 
 template <bool F32, bool E5>
@@ -53,30 +46,29 @@ __global__ __launch_bounds__(256) void f8_save(SaveArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c0 = blockIdx.y * 1024 + lane * 16;
   const int64_t row0 = (int64_t)blockIdx.x * 16 + wave * 4;
-  float v[4][16];
-  bool in[4];
+  Raw16<F32> raw[4] = {};
+  const bool thin = a.K < 8;
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    in[r] = row0 + r < a.T && c0 < a.Kp;
-    load16<F32>(a.X, in[r] ? (row0 + r) * a.ldx + c0 : 0, in[r] ? a.K - c0 : 0, a.vec, v[r]);
-  }
+  for (int r = 0; r < 4; ++r)
+    if (!thin) raw[r] = raw16<F32>(a.X, (row0 + r < a.T ? row0 + r : a.T - 1) * a.ldx, c0, a.K);
   uint32_t bytes = 0;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
+    float v[16];
+    if (thin) thin16<F32>(a.X, (row0 + r < a.T ? row0 + r : a.T - 1) * a.ldx, c0, a.K, v);
+    else unpack16<F32>(raw[r], c0, a.K, v);
     uint32_t m = 0;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) m = max(m, f8_magnitude(v[r][k]));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 1));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 2));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 4));
+    for (int k = 0; k < 16; ++k) m = max(m, f8_magnitude(v[k]));
+    m = f8_most<8>(m);
     const int b = f8_scale_byte<E5>(m);
     const float s = f8_inverse(b);
     bytes |= (uint32_t)b << (8 * r);
     u32x4_t q;
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      q[k] = f8_encode4<E5>(v[r][4 * k] * s, v[r][4 * k + 1] * s, v[r][4 * k + 2] * s, v[r][4 * k + 3] * s);
-    if (in[r]) *(u32x4_t*)(a.codes + (row0 + r) * a.Kp + c0) = q;
+      q[k] = f8_encode4<E5>(v[4 * k] * s, v[4 * k + 1] * s, v[4 * k + 2] * s, v[4 * k + 3] * s);
+    if (row0 + r < a.T && c0 < a.Kp) *(u32x4_t*)(a.codes + (row0 + r) * a.Kp + c0) = q;
   }
   if ((lane & 7) == 0) sc[lane >> 3][wave] = bytes;
   __syncthreads();
@@ -90,7 +82,7 @@ struct LoadArgs {
   const uint8_t *codes, *scale;
   void* Y;
   int64_t ldy, srows;
-  int32_t T, K, Kp, vec;
+  int32_t T, K, Kp;
 };
 
 template <bool F32, bool E5>
@@ -123,9 +115,10 @@ __global__ __launch_bounds__(256) void f8_load(LoadArgs a) {
         v[4 * k] = lo.x * s, v[4 * k + 1] = lo.y * s, v[4 * k + 2] = hi.x * s, v[4 * k + 3] = hi.y * s;
       }
       float* y = (float*)a.Y + at;
-      if (a.vec && left >= 16) {
+      if (left >= 16) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) ((f32x4_t*)y)[k] = f32x4_t{v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]};
+        for (int k = 0; k < 4; ++k)
+          ((f8_any4_t*)y)[k] = u32x4_t{__float_as_uint(v[4 * k]), __float_as_uint(v[4 * k + 1]), __float_as_uint(v[4 * k + 2]), __float_as_uint(v[4 * k + 3])};
       } else {
 #pragma unroll
         for (int k = 0; k < 16; ++k)
@@ -135,9 +128,9 @@ __global__ __launch_bounds__(256) void f8_load(LoadArgs a) {
       const float s = __uint_as_float((uint32_t)b[r] << 23);
       const u32x4_t lo = f8_decode_bf16x8<E5>(q[r][0], q[r][1], s), hi = f8_decode_bf16x8<E5>(q[r][2], q[r][3], s);
       uint16_t* y = (uint16_t*)a.Y + at;
-      if (a.vec && left >= 16) {
-        ((u32x4_t*)y)[0] = lo;
-        ((u32x4_t*)y)[1] = hi;
+      if (left >= 16) {
+        ((f8_any2_t*)y)[0] = lo;
+        ((f8_any2_t*)y)[1] = hi;
       } else {
 #pragma unroll
         for (int k = 0; k < 16; ++k)
@@ -152,7 +145,7 @@ struct PackArgs {
   int64_t ldw;
   const int32_t *row_ptr, *col_idx, *col_ptr, *row_idx;
   uint8_t *payload, *scale, *payload_t, *scale_t;
-  int32_t O, I, nbr, vec;
+  int32_t O, I, nbr;
 };
 
 // One kept block a workgroup: its codes in row order, and through LDS in column order at the block's place among its column's.
@@ -185,8 +178,11 @@ __global__ __launch_bounds__(256) void f8_pack(PackArgs a) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int o = br * F8_BLOCK + r0 + 32 * j, i = c * F8_BLOCK + k0;
-    const bool in = o < a.O && i < a.I;
-    load16<F32>(a.W, in ? o * a.ldw + i : 0, in ? a.I - i : 0, a.vec, v[j]);
+    const int64_t at = (o < a.O ? o : a.O - 1) * a.ldw;
+    if (a.I < 8) thin16<F32>(a.W, at, i, a.I, v[j]);
+    else unpack16<F32>(raw16<F32>(a.W, at, i, a.I), i, a.I, v[j]);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[j][k] = o < a.O ? v[j][k] : 0.f;
 #pragma unroll
     for (int k = 0; k < 16; ++k) m = max(m, f8_magnitude(v[j][k]));
   }
@@ -230,13 +226,12 @@ __global__ __launch_bounds__(256) void f8_pack(PackArgs a) {
 }
 
 inline int launched() { return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP; }
-inline bool aligned(const void* p, int64_t stride_bytes) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)stride_bytes) & 15u) == 0; }
 
 }  // namespace
 
 int f8_launch_save(const void* X, int x_f32, int64_t ldx, int T, int K, bool e5, uint8_t* codes, uint8_t* scale, hipStream_t st) {
   const int Kp = f8_blocks(K) * F8_BLOCK;
-  SaveArgs a{X, codes, scale, ldx, f8_scale_rows(T), T, K, Kp, aligned(X, ldx * (x_f32 ? 4 : 2))};
+  SaveArgs a{X, codes, scale, ldx, f8_scale_rows(T), T, K, Kp};
   const dim3 grid((unsigned)((T + 15) / 16), (unsigned)((Kp + 1023) / 1024)), block(256);
   if (x_f32) {
     if (e5) hipLaunchKernelGGL((f8_save<true, true>), grid, block, 0, st, a);
@@ -250,7 +245,7 @@ int f8_launch_save(const void* X, int x_f32, int64_t ldx, int T, int K, bool e5,
 
 int f8_launch_load(const uint8_t* codes, const uint8_t* scale, int T, int K, bool e5, void* Y, int y_f32, int64_t ldy, hipStream_t st) {
   const int Kp = f8_blocks(K) * F8_BLOCK;
-  LoadArgs a{codes, scale, Y, ldy, f8_scale_rows(T), T, K, Kp, aligned(Y, ldy * (y_f32 ? 4 : 2))};
+  LoadArgs a{codes, scale, Y, ldy, f8_scale_rows(T), T, K, Kp};
   const dim3 grid((unsigned)((T + 15) / 16), (unsigned)((Kp + 1023) / 1024)), block(256);
   if (y_f32) {
     if (e5) hipLaunchKernelGGL((f8_load<true, true>), grid, block, 0, st, a);
@@ -264,7 +259,7 @@ int f8_launch_load(const uint8_t* codes, const uint8_t* scale, int T, int K, boo
 
 int f8_launch_pack(const bsp_weights_f8* w, const void* W, int w_f32, int64_t ldw, hipStream_t st) {
   PackArgs a{W, ldw, w->row_ptr, w->col_idx, w->col_ptr, w->row_idx, w->payload, w->scale, w->payload_t, w->scale_t,
-             w->O, w->I, f8_blocks(w->O), aligned(W, ldw * (w_f32 ? 4 : 2))};
+             w->O, w->I, f8_blocks(w->O)};
   const dim3 grid((unsigned)w->nnzb), block(256);
   if (w_f32) hipLaunchKernelGGL((f8_pack<true>), grid, block, 0, st, a);
   else hipLaunchKernelGGL((f8_pack<false>), grid, block, 0, st, a);

@@ -61,9 +61,7 @@ __device__ __forceinline__ void few_stage(const FewArgs& a, uint8_t* codes, uint
     uint32_t m = 0;
 #pragma unroll
     for (int k = 0; k < 16; ++k) m = max(m, f8_magnitude(v[k]));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 1));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 2));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 4));
+    m = f8_most<8>(m);
     const int b = f8_scale_byte<E5>(m);
     const float s = f8_inverse(b);
     u32x4_t q;

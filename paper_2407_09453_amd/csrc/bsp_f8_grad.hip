@@ -1,19 +1,27 @@
 // The weights' gradient of an FC layer from the 8-bit checkpoint of its input: dW[o][i] = sum_t dY[t][o] X[t][i] for kept blocks
-// only, and the bias's, db[o] = sum_t dY[t][o].
+// only, and the bias's, db[o] = sum_t dY[t][o].  Bound by the matrix cores on many rows.
 //
 // A scale of the checkpoint belongs to a row t and 128 columns, and t is what the product sums over, so no scaled matrix
 // instruction fits; code x power of two is exact in bf16, and the product runs on the bf16 matrix cores with fp32 sums.
-// Codes become bf16 on their way into LDS (a conversion of two values takes the scale along).  Both operands are
-// summed over their rows: LDS holds them as they lie in memory, row after row, and the transposing LDS read hands a lane
-// four rows of its column.  It takes four rows of 32 bytes from a group of sixteen lanes, so the 32-byte chunks of a
-// row are permuted by the row (bits 0, 1 and 3): four rows' same chunk, and those of two groups, lie in different banks.
+// A workgroup takes one block row (128 outputs) and C of its kept blocks, whichever they are: the gradients' 128 columns are
+// staged once for all of them.  Codes become bf16 on their way into LDS (a conversion of two values takes the scale along).
+// Both operands are summed over their rows: LDS holds them as they lie in memory, row after row, and the transposing LDS read
+// hands a lane four rows of its column.  It takes four rows of 32 bytes from a group of sixteen lanes, and half a wave two
+// neighbouring chunks of them: the chunks of a row are permuted by the row (bits 0 and 1, then 3), so that these eight lie in different banks.
+// Two buffers of 32 rows; what is written into one was asked for, into registers, kAhead steps before.
+// Where a matrix has too few blocks for the chip the rows are cut into ranges whose sums meet in a second launch, in order.
 #include "bsp_f8.h"
+
+#include <type_traits>
 
 namespace {
 
-constexpr int kStep = 64;  // rows a step
+constexpr int kStep = 32, kThreads = 512, kAhead = 2;  // rows a step; steps that are on their way to registers
+constexpr int kTile = kStep * 256;                     // 32 rows of 128 bf16
 
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef const __attribute__((address_space(1))) uint8_t* global_t;
+typedef u32x4_t __attribute__((aligned(2))) u32x4_any;  // sixteen bytes at any bf16's address
 
 __device__ __forceinline__ u32x4_t read_columns(const uint8_t* p) {  // rows +0..3 and +4..7 of this lane's column
   auto* q = (__attribute__((address_space(3))) s16x4_t*)(uintptr_t)p;
@@ -22,178 +30,314 @@ __device__ __forceinline__ u32x4_t read_columns(const uint8_t* p) {  // rows +0.
   return u32x4_t{a.x, a.y, b.x, b.y};
 }
 
-__device__ __forceinline__ int chunk_key(int t) { return (t & 3) | (((t >> 3) & 1) << 2); }
+__device__ __forceinline__ int chunk_key(int t) { return (t & 3) << 1 | ((t >> 3) & 1); }
 
-template <bool E5, bool VEC>
-__global__ __launch_bounds__(256) void f8_grad(F8GradArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t ly[kStep * 256], lx[kStep * 256];
-  __shared__ int place;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n = blockIdx.x;
-  if (tid == 0) {
-    int lo = 0, hi = a.nbo;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (a.row_ptr[mid] <= n) lo = mid; else hi = mid;
-    }
-    place = lo;
+// eight gradients o .. o+7 of a row, those past the last channel 0
+__device__ __forceinline__ u32x4_t gradients8(const uint16_t* row, int o, int O) {
+  if (o + 8 <= O) return *(const u32x4_any*)(row + o);
+  uint32_t v[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    v[k] = row[o + k < O ? o + k : O - 1];
+    v[k] = o + k < O ? v[k] : 0;
   }
+  return u32x4_t{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16};
+}
+
+// Column sums of one block row's gradients over one range of rows: a thread adds eight columns of every 32nd row.
+__device__ __forceinline__ void column_sums(const F8GradArgs& a, int br, int64_t t_begin, int64_t t_end, float* sums) {
+  const int piece = threadIdx.x & 15, o = br * F8_BLOCK + piece * 8;
+  float s[8] = {};
+  if (o < a.O)
+#pragma unroll 4
+    for (int64_t t = t_begin + (threadIdx.x >> 4); t < t_end; t += kThreads / 16) {
+      const u32x4_t v = gradients8(a.dY + t * a.ldy, o, a.O);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s[k] += __uint_as_float(k & 1 ? v[k >> 1] & 0xFFFF0000u : v[k >> 1] << 16);
+    }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sums[(threadIdx.x >> 4) * 129 + piece * 8 + k] = s[k];
   __syncthreads();
-  const int br = place, kb = a.col_idx[n];
-  const int Kp = f8_blocks(a.I) * F8_BLOCK;
-  const int64_t srows = f8_scale_rows(a.T);
-  const int steps = (a.T + kStep - 1) / kStep, per = (steps + a.split - 1) / a.split;
+  if (threadIdx.x < F8_BLOCK && br * F8_BLOCK + (int)threadIdx.x < a.O) {
+    float v = 0.f;
+    for (int r = 0; r < kThreads / 16; ++r) v += sums[r * 129 + threadIdx.x];
+    (a.split == 1 ? a.db : a.part_db + (int64_t)blockIdx.y * a.O)[br * F8_BLOCK + threadIdx.x] = v;
+  }
+}
+
+// THIN: fewer than eight outputs, read one by one
+template <int C, bool E5, bool THIN>
+__global__ __launch_bounds__(kThreads) void f8_grad(F8GradArgs a) {
+  constexpr int MO = C, WO = 4 / MO;  // 32-row tiles of outputs a wave, waves side by side over the 128 outputs
+  constexpr int kBuffer = (1 + C) * kTile;
+  constexpr int kPieces = C > 1 ? C / 2 : 1, kCodes = C > 1 ? 16 : 8, kWords = kCodes / 4;  // runs of codes a thread brings, of a block each
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  kernarg_touch<F8GradArgs>();
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int groups = a.groups;  // of C blocks in a block row; 0: the column sums alone are wanted
+  const int steps = (int)(((int64_t)a.T + kStep - 1) / kStep), per = (steps + a.split - 1) / a.split;
   const int64_t t_begin = (int64_t)blockIdx.y * per * kStep;
   const int64_t t_end = t_begin + (int64_t)per * kStep < a.T ? t_begin + (int64_t)per * kStep : a.T;
-  const int wo = wave >> 1, wi = wave & 1;
-  const int key = ((lane & 15) >> 2) | ((lane >> 5) << 2);
-  const int trow = (lane >> 5) * 8 + ((lane & 15) >> 2);
-  int ao[2], ai[2];
-#pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    ao[m] = trow * 256 + (((wo * 4 + m * 2 + ((lane >> 4) & 1)) ^ key) << 5) + (lane & 3) * 8;
-    ai[m] = trow * 256 + (((wi * 4 + m * 2 + ((lane >> 4) & 1)) ^ key) << 5) + (lane & 3) * 8;
+  // Workgroups go to the eight XCDs in turn.  Four neighbouring groups of a block row go to one, with the same groups of seven other rows: what an
+  // XCD runs at one time shares eight rows' gradients and four groups' codes in its L2.  Block rows are dealt to the XCDs one by
+  // one, so that rows that keep more blocks than others do not meet on one.
+  const int b = blockIdx.x, quads = (groups + 3) >> 2, clusters = quads * a.nbo, behind = (clusters + 7) / 8 * 32;
+  if (b >= behind) {  // the workgroups behind: one block row's column sums each
+    column_sums(a, b - behind, t_begin, t_end, (float*)lds);
+    return;
   }
-  f32x16_t acc[2][2] = {};
-  for (int64_t t0 = t_begin; t0 < t_end; t0 += kStep) {
-    // gradients: a request is four rows of 256 bytes
+  const int cluster = (b >> 5) * 8 + (b & 7), quad = cluster / a.nbo, br = cluster - quad * a.nbo;
+  const int first = (quad * 4 + ((b >> 3) & 3)) * C;
+  if (cluster >= clusters || first >= a.nbi) return;
+  const int n0 = __builtin_amdgcn_readfirstlane(a.row_ptr[br]), cnt = __builtin_amdgcn_readfirstlane(a.row_ptr[br + 1]) - n0;
+  if (a.split == 1 && cnt < a.nbi) {  // of the C block columns from `first` those that are not kept become zeros
+    for (int c = first; c < first + C && c < a.nbi; ++c) {
+      bool kept = false;
+      for (int i = lane; i < cnt; i += 64) kept |= a.col_idx[n0 + i] == c;
+      if (__ballot(kept)) continue;
+      const int col = c * F8_BLOCK + (tid & 127);
+      if (col < a.I)
+        for (int r = tid >> 7; r < F8_BLOCK && br * F8_BLOCK + r < a.O; r += kThreads / 128) a.dW[((int64_t)br * F8_BLOCK + r) * a.I + col] = 0.f;
+    }
+  }
+  const int has = cnt - first < C ? cnt - first : C;  // kept blocks first .. first + has - 1 of the row
+  if (has <= 0) return;
+
+  // what this thread brings: eight gradients, and 8 C codes of one row
+  const int row = tid >> 4, piece = tid & 15;
+  const int o = br * F8_BLOCK + piece * 8;
+  // eight gradients at once: at a row's end its last eight, which are moved into place when they are written
+  const uint32_t col_y = (uint32_t)(o + 8 <= a.O || THIN ? o : a.O - 8) * 2;
+  const int past = o + 8 <= a.O || (THIN && piece == 0) ? 0 : o + 8 - a.O < 8 ? o + 8 - a.O : 8;  // of them
+  const int64_t Kp = (int64_t)f8_blocks(a.I) * F8_BLOCK, srows = f8_scale_rows(a.T);
+  const int j_in = piece * kCodes >> 7, at_in = (piece * kCodes) & 127;  // the first run's block, and its columns in that; the next lies two blocks on
+  uint32_t col_x[kPieces], col_s[kPieces];
 #pragma unroll
-    for (int q = 0; q < kStep / 16; ++q) {
-      const int row = (q * 4 + wave) * 4 + (lane >> 4);
-      const int slot = lane & 15, piece = (((slot >> 1) ^ chunk_key(row)) << 1) | (slot & 1);
-      const int o = br * F8_BLOCK + piece * 8;
-      uint8_t* to = ly + (q * 4 + wave) * 1024;
-      if constexpr (VEC) {
-        if (t0 + row < t_end) {
-          const uint16_t* src = a.dY + (t0 + row) * a.ldy + (o < a.O ? o : 0);  // past the last channel: results that go nowhere
-          __builtin_amdgcn_global_load_lds((f8_gptr_t)src, (f8_lptr_t)(uintptr_t)to, 16, 0, 0);
-        } else {
-          *(u32x4_t*)(to + lane * 16) = u32x4_t{0, 0, 0, 0};
-        }
+  for (int p = 0; p < kPieces; ++p) {
+    const int kb = a.col_idx[n0 + first + (j_in + 2 * p < has ? j_in + 2 * p : 0)];
+    col_x[p] = (uint32_t)kb * F8_BLOCK + at_in;
+    col_s[p] = (uint32_t)(kb * srows);
+  }
+  u32x4_t y_in[kAhead];
+  uint32_t x_in[kAhead][kPieces][kWords];
+  int s_in[kAhead][kPieces], rows_in[kAhead];
+  // Step i's values to registers; past the range's end the last row's, which `write` drops.  Nothing here looks at what it loads: that would
+  // wait for it.  Every address is the same 64 bits in all lanes and 32 of a lane's own.
+  auto load = [&](int i, int j) {
+    const int64_t t0 = t_begin + (int64_t)i * kStep;
+    const int64_t from = t0 < t_end ? t0 : t_end - 1;
+    rows_in[j] = t0 < t_end ? (int)(t_end - t0 < kStep ? t_end - t0 : kStep) : 0;
+    const int most = rows_in[j] > 0 ? rows_in[j] - 1 : 0;
+    const uint32_t r = row < most ? row : most;
+    auto *by = (global_t)(a.dY + from * a.ldy), *bx = (global_t)(a.codes + from * Kp), *bs = (global_t)(a.scale + from);
+    asm volatile("" : "+s"(by), "+s"(bx), "+s"(bs));
+    if constexpr (THIN) y_in[j] = gradients8((const uint16_t*)by + r * a.ldy, 0, a.O);
+    else y_in[j] = *(const __attribute__((address_space(1))) u32x4_any*)(by + (r * (uint32_t)a.ldy * 2 + col_y));
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      auto* c = bx + (r * (uint32_t)Kp + col_x[p]);
+      if constexpr (kWords == 2) {
+        const u32x2_t v = *(const __attribute__((address_space(1))) u32x2_t*)c;
+        x_in[j][p][0] = v.x, x_in[j][p][1] = v.y;
       } else {
-        uint32_t v[8];
+        const u32x4_t v = *(const __attribute__((address_space(1))) u32x4_t*)c;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = t0 + row < t_end && o + k < a.O ? a.dY[(t0 + row) * a.ldy + o + k] : 0;
-        *(u32x4_t*)(to + lane * 16) = u32x4_t{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16};
+        for (int e = 0; e < 4; ++e) x_in[j][p][e] = v[e];
+      }
+      s_in[j][p] = bs[r + col_s[p]];
+    }
+  };
+  const int key = chunk_key(row);
+  const int to_y = row * 256 + ((piece >> 1) ^ key) * 32 + (piece & 1) * 16;
+  // A run of sixteen codes becomes a chunk of 32 bytes in two writes; every other row writes its second half first, so that a write of
+  // four rows touches all banks.
+  const bool swap = kCodes == 16 && (row & 1);
+  const int to_x = (1 + j_in) * kTile + row * 256 + ((at_in >> 4) ^ key) * 32 + (kCodes == 8 ? (at_in & 8) * 2 : swap ? 16 : 0);
+  auto write = [&](int buf, int j, auto ENDS) {  // rows past the range add nothing, whatever they hold; ENDS: the last outputs' block row
+    const bool in = row < rows_in[j];
+    u32x4_t y = in ? y_in[j] : u32x4_t{0, 0, 0, 0};
+    if constexpr (decltype(ENDS)::value) {
+#pragma unroll
+      for (int d = 1; d < 8; d *= 2) {  // down by `past` values of two bytes, zeros from above
+        const u32x4_t v = d == 1 ? u32x4_t{y.x >> 16 | y.y << 16, y.y >> 16 | y.z << 16, y.z >> 16 | y.w << 16, y.w >> 16}
+                        : d == 2 ? u32x4_t{y.y, y.z, y.w, 0} : u32x4_t{y.z, y.w, 0, 0};
+        y = past & d ? v : y;
+      }
+      y = past == 8 ? u32x4_t{0, 0, 0, 0} : y;
+    }
+    *(u32x4_t*)(lds + buf * kBuffer + to_y) = y;
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      const float s = __uint_as_float((uint32_t)s_in[j][p] << 23);
+      const bool brings = in && j_in + 2 * p < has;
+      uint32_t v[kWords];
+#pragma unroll
+      for (int e = 0; e < kWords; ++e) v[e] = brings ? x_in[j][p][e] : 0;
+      uint8_t* to = lds + buf * kBuffer + 2 * p * kTile;
+      if constexpr (kCodes == 8) {
+        *(u32x4_t*)(to + to_x) = f8_decode_bf16x8<E5>(v[0], v[1], s);
+      } else {
+        const uint32_t lo0 = swap ? v[2] : v[0], lo1 = swap ? v[3] : v[1], hi0 = swap ? v[0] : v[2], hi1 = swap ? v[1] : v[3];
+        *(u32x4_t*)(to + to_x) = f8_decode_bf16x8<E5>(lo0, lo1, s);
+        *(u32x4_t*)(to + (to_x ^ 16)) = f8_decode_bf16x8<E5>(hi0, hi1, s);
       }
     }
-    // the checkpoint: 32 codes a thread
-    {
-      const int row = tid >> 2, part = tid & 3;
-      u32x4_t c[2] = {};
-      float s = 0.f;
-      if (t0 + row < t_end) {
-        const u32x4_t* src = (const u32x4_t*)(a.codes + (t0 + row) * Kp + kb * F8_BLOCK + part * 32);
-        c[0] = src[0];
-        c[1] = src[1];
-        s = __uint_as_float((uint32_t)a.scale[kb * srows + t0 + row] << 23);
-      }
+  };
+
+  const int wo = wave % WO, wi = wave / WO;  // wi: 64 columns of the C blocks'
+  const int key_r = ((lane & 15) >> 2) << 1 | (lane >> 5), trow = (lane >> 5) * 8 + ((lane & 15) >> 2);
+  int at_o[MO], at_i[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        u32x4_t* to = (u32x4_t*)(lx + row * 256 + (((part * 2 + h) ^ chunk_key(row)) << 5));
-        to[0] = f8_decode_bf16x8<E5>(c[h].x, c[h].y, s);
-        to[1] = f8_decode_bf16x8<E5>(c[h].z, c[h].w, s);
+  for (int m = 0; m < MO; ++m) at_o[m] = trow * 256 + (((wo * MO * 2 + m * 2 + ((lane >> 4) & 1)) ^ key_r) << 5) + (lane & 3) * 8;
+#pragma unroll
+  for (int m = 0; m < 2; ++m) at_i[m] = (1 + (wi >> 1)) * kTile + trow * 256 + ((((wi & 1) * 4 + m * 2 + ((lane >> 4) & 1)) ^ key_r) << 5) + (lane & 3) * 8;
+  f32x16_t acc[MO][2] = {};
+  auto read = [&](int buf, int k, u32x4_t (&y)[MO], u32x4_t (&x)[2]) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m) x[m] = read_columns(lds + buf * kBuffer + k * 256 + at_i[m]);
+#pragma unroll
+    for (int m = 0; m < MO; ++m) y[m] = read_columns(lds + buf * kBuffer + k * 256 + at_o[m]);
+  };
+  auto multiply = [&](u32x4_t (&y)[MO], u32x4_t (&x)[2]) {
+#pragma unroll
+    for (int m = 0; m < MO; ++m)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        acc[m][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, y[m]), __builtin_bit_cast(bf16x8_t, x[i]), acc[m][i], 0, 0, 0);
+  };
+
+  // Step i in buffer i mod 2, a half of it (sixteen rows) read while the other is multiplied; one barrier, between the halves, behind which
+  // the next step's buffer is whole and this one's is free for the step after that.  Nothing inside is conditional, so that
+  // a wait for what a register asked for covers no more than that.
+  auto run = [&](int n, auto ENDS) {
+    u32x4_t y[2][MO], x[2][2];
+    auto meet = [&]() {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    };
+    constexpr int kReads = 2 * (MO + 2), kMul = 2 * MO;
+    auto step = [&](int i, auto U) {
+      constexpr int u = decltype(U)::value;
+      read(u, 16, y[1], x[1]);
+      multiply(y[0], x[0]);
+#pragma unroll
+      for (int k = 0; k < kMul; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                             // a matrix instruction,
+        __builtin_amdgcn_sched_group_barrier(0x100, (kReads + kMul - 1) / kMul, 0);  // reads of LDS behind it
       }
+      meet();
+      read(u ^ 1, 0, y[0], x[0]);
+      write(u, u, ENDS);
+      load(i + 2 + kAhead, u);
+      multiply(y[1], x[1]);
+#pragma unroll
+      for (int k = 0; k < kMul; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, (kReads + kMul / 2 - 1) / (kMul / 2), 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);  // conversions, and the writes that follow the reads
+        if (k >= kMul / 2) __builtin_amdgcn_sched_group_barrier(0x200, 2, 0);
+      }
+    };
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) load(j, j);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      write(j, j, ENDS);
+      load(j + kAhead, j);
     }
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kStep; k += 16) {
-      u32x4_t y[2], x[2];
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        y[m] = read_columns(ly + k * 256 + ao[m]);
-        x[m] = read_columns(lx + k * 256 + ai[m]);
-      }
-#pragma unroll
-      for (int o = 0; o < 2; ++o)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          acc[o][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, y[o]), __builtin_bit_cast(bf16x8_t, x[i]), acc[o][i], 0, 0, 0);
+    meet();
+    read(0, 0, y[0], x[0]);
+    for (int i = 0; i < n; i += 2) {  // (behind an odd number of steps one of zeros)
+      step(i, std::integral_constant<int, 0>{});
+      step(i + 1, std::integral_constant<int, 1>{});
     }
-    __syncthreads();
+  };
+  if (t_begin < t_end) {
+    const int n = (int)((t_end - t_begin + kStep - 1) / kStep);
+    if (br == a.nbo - 1 && (a.O & 127)) run(n, std::true_type{});
+    else run(n, std::false_type{});
   }
+
+  if (wi >> 1 >= has) return;
+  const int kb = a.col_idx[n0 + first + (wi >> 1)];
   const bool whole = a.split == 1;
   float* out = whole ? a.dW + (int64_t)br * F8_BLOCK * a.I + (int64_t)kb * F8_BLOCK
-                     : a.part + ((int64_t)blockIdx.y * a.nnzb + n) * F8_BLOCK_BYTES;
+                     : a.part + ((int64_t)blockIdx.y * a.nnzb + n0 + first + (wi >> 1)) * F8_BLOCK_BYTES;
   const int64_t ld = whole ? a.I : F8_BLOCK;
   const int rows = whole ? a.O - br * F8_BLOCK : F8_BLOCK, cols = whole ? a.I - kb * F8_BLOCK : F8_BLOCK;
 #pragma unroll
-  for (int o = 0; o < 2; ++o)
+  for (int m = 0; m < MO; ++m)
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int c = wi * 64 + i * 32 + (lane & 31);
+      const int c = (wi & 1) * 64 + i * 32 + (lane & 31);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int row = wo * 64 + o * 32 + (r >> 2) * 8 + (lane >> 5) * 4 + (r & 3);
-        if (row < rows && c < cols) out[row * ld + c] = acc[o][i][r];
+        const int q = (wo * MO + m) * 32 + (r >> 2) * 8 + (lane >> 5) * 4 + (r & 3);
+        if (q < rows && c < cols) out[q * ld + c] = acc[m][i][r];
       }
     }
 }
 
-// Blocks that are not kept become zeros; those that are get the sum over the ranges of rows, in their order.
+// The sums over the ranges of rows, in their order: a kept block's entries, zeros for the others, and the bias's gradient.  A workgroup
+// takes two rows of a block, a thread one entry.
 __global__ __launch_bounds__(256) void f8_grad_finish(F8GradArgs a) {
-  const int kb = blockIdx.x % a.nbi, br = blockIdx.x / a.nbi;
-  int n = a.row_ptr[br];
-  const int n1 = a.row_ptr[br + 1];
-  while (n < n1 && a.col_idx[n] < kb) ++n;
-  const bool kept = n < n1 && a.col_idx[n] == kb;
-  if (kept && a.split == 1) return;
-  const int c = threadIdx.x & 127;
-  if (kb * F8_BLOCK + c >= a.I) return;
-  for (int r = threadIdx.x >> 7; r < F8_BLOCK; r += 2) {
-    const int64_t o = (int64_t)br * F8_BLOCK + r;
-    if (o >= a.O) return;
+  const int cell = blockIdx.x, br = cell / a.nbi, kb = cell - br * a.nbi, c = threadIdx.x & 127;
+  auto sum = [&](const float* p, int64_t step) {
     float v = 0.f;
-    if (kept)
-      for (int s = 0; s < a.split; ++s) v += a.part[((int64_t)s * a.nnzb + n) * F8_BLOCK_BYTES + r * F8_BLOCK + c];
-    a.dW[o * a.I + kb * F8_BLOCK + c] = v;
-  }
+#pragma unroll 16
+    for (int s = 0; s < a.split; ++s) v += p[s * step];
+    return v;
+  };
+  if (a.db && kb == 0 && blockIdx.y == 0 && threadIdx.x < F8_BLOCK && br * F8_BLOCK + c < a.O) a.db[br * F8_BLOCK + c] = sum(a.part_db + br * F8_BLOCK + c, a.O);
+  const int n0 = a.row_ptr[br], n1 = a.row_ptr[br + 1], r = (int)blockIdx.y * 2 + (threadIdx.x >> 7);
+  int n = -1;
+  for (int i = n0 + (threadIdx.x & 63); i < n1; i += 64) n = a.col_idx[i] == kb ? i : n;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) n = max(n, __shfl_xor(n, d));
+  const int64_t o = (int64_t)br * F8_BLOCK + r;
+  if (!a.dW || o >= a.O || kb * F8_BLOCK + c >= a.I) return;
+  a.dW[o * a.I + kb * F8_BLOCK + c] = n < 0 ? 0.f : sum(a.part + (int64_t)n * F8_BLOCK_BYTES + r * F8_BLOCK + c, a.nnzb * F8_BLOCK_BYTES);
 }
 
-// Column sums of dY over one range of rows a workgroup: a thread owns two columns' sums.
-__global__ __launch_bounds__(256) void f8_colsum(const uint16_t* dY, int64_t ldy, int T, int O, int parts, float* part) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= O) return;
-  const int64_t per = ((int64_t)T + parts - 1) / parts;
-  const int64_t t0 = blockIdx.y * per, t1 = t0 + per < T ? t0 + per : T;
-  float s = 0.f;
-  for (int64_t t = t0; t < t1; ++t) s += bf16_bits_to_f32(dY[t * ldy + c]);
-  part[(int64_t)blockIdx.y * O + c] = s;
+// The largest number of kept blocks a workgroup, 4 at most, that still gives every CU one ...
+int blocks_each(int64_t nnzb, int nbo) {
+  const int64_t row = nnzb / nbo;
+  for (int c = 4; c > 1; c /= 2)
+    if (row >= c && nbo * ((row + c - 1) / c) >= 256) return c;
+  return 1;
+}
+
+template <int C, bool E5, bool THIN = false>
+int launch(F8GradArgs a, hipStream_t st) {
+  constexpr int lds = 2 * (1 + C) * kTile;
+  static const bool raised = hipFuncSetAttribute((const void*)&f8_grad<C, E5, THIN>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
+  if (!raised) return BSP_ERR_HIP;
+  a.groups = a.dW ? (a.nbi + C - 1) / C : 0;
+  const int64_t groups = ((int64_t)a.nbo * ((a.groups + 3) / 4) + 7) / 8 * 32;
+  if (groups + a.nbo > INT32_MAX) return BSP_ERR_SHAPE;
+  hipLaunchKernelGGL((f8_grad<C, E5, THIN>), dim3((unsigned)(groups + (a.db ? a.nbo : 0)), (unsigned)a.split), dim3(kThreads), lds, st, a);
+  return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP;
 }
 
 }  // namespace
 
+// ... and where even single blocks are too few, ranges of at least four steps that together give the chip a workgroup a CU.
 int f8_grad_split(int64_t nnzb, int T) {
-  const int64_t steps = ((int64_t)T + 2 * kStep - 1) / (2 * kStep);
-  int64_t s = nnzb > 0 ? 512 / nnzb : 1;
-  if (s > steps) s = steps;
+  const int64_t most = (int64_t)T / (4 * kStep), want = nnzb > 0 ? 256 / nnzb : 1;
+  const int64_t s = want < most ? want : most;
   return s < 1 ? 1 : (int)s;
 }
 
 int f8_launch_grad(const F8GradArgs& a, hipStream_t st) {
-  const bool vec = ((reinterpret_cast<uintptr_t>(a.dY) | (uintptr_t)(a.ldy * 2)) & 15u) == 0 && a.O % 8 == 0;
-  if (a.nnzb > 0) {
-    const dim3 grid((unsigned)a.nnzb, (unsigned)a.split), block(256);
-    if (a.e5) {
-      if (vec) hipLaunchKernelGGL((f8_grad<true, true>), grid, block, 0, st, a);
-      else hipLaunchKernelGGL((f8_grad<true, false>), grid, block, 0, st, a);
-    } else {
-      if (vec) hipLaunchKernelGGL((f8_grad<false, true>), grid, block, 0, st, a);
-      else hipLaunchKernelGGL((f8_grad<false, false>), grid, block, 0, st, a);
-    }
-    if (hipGetLastError() != hipSuccess) return BSP_ERR_HIP;
+  int rc;
+  if (a.O < 8) rc = a.e5 ? launch<1, true, true>(a, st) : launch<1, false, true>(a, st);
+  else switch (blocks_each(a.nnzb, a.nbo)) {
+    case 4: rc = a.e5 ? launch<4, true>(a, st) : launch<4, false>(a, st); break;
+    case 2: rc = a.e5 ? launch<2, true>(a, st) : launch<2, false>(a, st); break;
+    default: rc = a.e5 ? launch<1, true>(a, st) : launch<1, false>(a, st);
   }
-  if (a.split > 1 || a.nnzb < (int64_t)a.nbo * a.nbi) {
-    hipLaunchKernelGGL(f8_grad_finish, dim3((unsigned)(a.nbo * a.nbi)), dim3(256), 0, st, a);
-    if (hipGetLastError() != hipSuccess) return BSP_ERR_HIP;
-  }
-  return BSP_OK;
-}
-
-int f8_launch_colsum(const uint16_t* dY, int64_t ldy, int T, int O, float* part, float* db, hipStream_t st) {
-  const int parts = norm_parts(T);
-  hipLaunchKernelGGL(f8_colsum, dim3((unsigned)((O + 255) / 256), (unsigned)parts), dim3(256), 0, st, dY, ldy, T, O, parts, part);
-  if (hipGetLastError() != hipSuccess) return BSP_ERR_HIP;
-  return norm_launch_sum(part, parts, O, db, st);
+  if (rc != BSP_OK || a.split == 1) return rc;
+  hipLaunchKernelGGL(f8_grad_finish, dim3((unsigned)(a.nbo * a.nbi), F8_BLOCK / 2), dim3(256), 0, st, a);
+  return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP;
 }

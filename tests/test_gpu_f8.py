@@ -247,7 +247,9 @@ def test_updated_weights_and_their_types():
 # ------------------------------------------------------------------------------- the weights' gradient
 @pytest.mark.parametrize("kind", ["e4m3", "e5m2"])
 @pytest.mark.parametrize("T,I,O,density", [(0, 300, 200, 1.0), (1, 1, 1, 1.0), (1, 128, 128, 1.0), (37, 1000, 520, 0.6), (63, 129, 127, 1.0), (64, 256, 256, 0.5), (65, 384, 260, 1.0),
-                                           (1000, 260, 136, 1.0), (4097, 128, 256, 1.0), (130, 640, 1000, 0.4), (200, 256, 128, 0.0)])
+                                           (1000, 260, 136, 1.0), (4097, 128, 256, 1.0), (130, 640, 1000, 0.4), (200, 256, 128, 0.0),
+                                           (70, 1200, 8300, 1.0), (70, 2200, 8192, 0.5), (33, 4300, 4096, 1.0), (90, 8190, 4096, 0.6),
+                                           (50, 200, 5, 1.0), (40, 130, 8, 1.0), (70, 256, 133, 1.0), (45, 128, 263, 1.0)])
 def test_weight_gradient(T, I, O, density, kind):
     rng = _rng(T, I, O, 10)
     x, xt = _draw(rng, T, I, "bf16", relu=True)
