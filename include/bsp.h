@@ -506,6 +506,24 @@ int bsp_layer_norm_grad(const void* dY, int64_t ld_dy, const void* X, int64_t ld
                         const float* mean, const float* rstd, const float* weight, void* dX, int64_t ld_dx,
                         float* dweight, float* dbias, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* The calls above in packed form (as bsp_call_packed, for callers that pay for every argument): one array of words, pointers as
+ * addresses, other arguments as signed integers in the order of the call's own arguments, with these differences: a
+ * bsp_codes is five words (T, K, dtype, codes, scale), all zero for a null one; eps is the bits of a double in its word.
+ *   BSP_F8_CALL_SAVE       X, x_dtype, ldx, codes c, stream                                                  9 words
+ *   BSP_F8_CALL_LOAD       codes c, Y, y_dtype, ldy, stream                                                  9
+ *   BSP_F8_CALL_FC         w, transposed, codes X, bias, residual, relu, codes gate, Y, y_dtype, stream     18
+ *   BSP_F8_CALL_VALUES     w, transposed, X, x_dtype, ldx, T, code, bias, residual, relu, codes gate, Y, y_dtype,
+ *                          workspace, workspace_bytes, stream                                               20
+ *   BSP_F8_CALL_GRAD       w, dY, ldy, codes X, dW, db, workspace, workspace_bytes, stream                  13
+ *   BSP_F8_CALL_NORM       X, dtype, ldx, T, D, weight, bias, eps, Y, ldy, codes, mean, rstd, stream        18
+ *   BSP_F8_CALL_NORM_GRAD  the seventeen of bsp_layer_norm_grad                                             17
+ * Errors: NULL (words), SHAPE (unknown call), otherwise those of the call. */
+enum bsp_f8_call {
+  BSP_F8_CALL_SAVE = 0, BSP_F8_CALL_LOAD = 1, BSP_F8_CALL_FC = 2, BSP_F8_CALL_VALUES = 3, BSP_F8_CALL_GRAD = 4,
+  BSP_F8_CALL_NORM = 5, BSP_F8_CALL_NORM_GRAD = 6
+};
+int bsp_f8_call_packed(int32_t call, const int64_t* words);
+
 #ifdef __cplusplus
 }
 #endif

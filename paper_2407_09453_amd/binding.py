@@ -37,7 +37,7 @@ EXPORTS = ("bsp_strerror", "bsp_version", "bsp_pack_count", "bsp_pack", "bsp_unp
            "bsp_conv2d_only", "bsp_bottleneck", "bsp_call_packed", "bsp_bench_copy", "bsp_bench_mfma_bf16", "bsp_bench_lds_read",
            "bsp_f8_save", "bsp_f8_load", "bsp_f8_count", "bsp_f8_index", "bsp_f8_pack", "bsp_f8_fc", "bsp_f8_fc_workspace",
            "bsp_f8_fc_values", "bsp_f8_fc_grad_workspace", "bsp_f8_fc_grad", "bsp_layer_norm", "bsp_layer_norm_grad_workspace",
-           "bsp_layer_norm_grad")
+           "bsp_layer_norm_grad", "bsp_f8_call_packed")
 
 
 class BspError(RuntimeError):
@@ -164,6 +164,7 @@ def load_library():
                        ("bsp_layer_norm_grad", [vp, i64, vp, i64, i32, i32, i32, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp])):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = ctypes.c_int, args
+    lib.bsp_f8_call_packed.restype, lib.bsp_f8_call_packed.argtypes = ctypes.c_int, [i32, ctypes.c_char_p]
     lib.bsp_call_packed.restype = ctypes.c_int
     lib.bsp_call_packed.argtypes = [i32, ctypes.c_char_p]
     lib.bsp_bench_copy.restype = ctypes.c_int

@@ -166,7 +166,7 @@ __device__ __forceinline__ void f8_store8(void* row, int c, int left, const floa
     uint16_t* y = (uint16_t*)row + c;
     const u32x4_t w = {f8_pack_bf16x2(v[0], v[1]), f8_pack_bf16x2(v[2], v[3]), f8_pack_bf16x2(v[4], v[5]), f8_pack_bf16x2(v[6], v[7])};
     if (left >= 8) {
-      *(f8_any2_t*)y = w;
+      __builtin_nontemporal_store(w, (f8_any2_t*)y);
       return;
     }
 #pragma unroll

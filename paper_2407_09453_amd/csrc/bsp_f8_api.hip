@@ -1,6 +1,8 @@
 // extern "C" entry points of the 8-bit floating-point layers and of layer norm: argument checks and dispatch.
 #include "bsp_f8.h"
 
+#include <string.h>
+
 namespace {
 
 inline bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -206,7 +208,7 @@ int bsp_layer_norm(const void* X, int32_t dtype, int64_t ldx, int32_t T, int32_t
 int bsp_layer_norm_grad_workspace(int32_t T, int32_t D, int64_t* bytes) {
   if (!bytes) return BSP_ERR_NULL;
   if (T < 0 || T > kMost || D < 1 || D > kMost) return BSP_ERR_SHAPE;
-  *bytes = (int64_t)norm_parts(T) * 2 * D * 4;
+  *bytes = norm_parts(T) > 1 ? (int64_t)norm_parts(T) * 2 * D * 4 : 0;
   return BSP_OK;
 }
 
@@ -225,8 +227,52 @@ int bsp_layer_norm_grad(const void* dY, int64_t ld_dy, const void* X, int64_t ld
   if (T > 0 && (!mean || !rstd)) return BSP_ERR_NULL;
   if (!aligned(mean, 4) || !aligned(rstd, 4) || !aligned(weight, 4) || !aligned(dweight, 4) || !aligned(dbias, 4) || !aligned(workspace, 16)) return BSP_ERR_ALIGN;
   if (workspace_bytes < need) return BSP_ERR_CAPACITY;
-  if (!workspace) return BSP_ERR_NULL;
+  if (need > 0 && !workspace) return BSP_ERR_NULL;
   return norm_launch_backward(dY, ld_dy, X, ldx, dtype == BSP_F32, mean, rstd, weight, T, D, dX, ld_dx, dweight, dbias, (float*)workspace, (hipStream_t)stream);
+}
+
+int bsp_f8_call_packed(int32_t call, const int64_t* w) {
+  if (!w) return BSP_ERR_NULL;
+  auto ptr = [&](int i) { return (void*)(intptr_t)w[i]; };
+  auto num = [&](int i) { return (int32_t)w[i]; };
+  // sizes that do not fit 32 bits are as wrong as negative ones
+  auto size = [&](int i) { return w[i] < 0 || w[i] > INT32_MAX ? -1 : (int32_t)w[i]; };
+  auto codes = [&](int i) { return bsp_codes{size(i), size(i + 1), num(i + 2), (uint8_t*)ptr(i + 3), (uint8_t*)ptr(i + 4)}; };
+  auto none = [&](int i) { return !(w[i] | w[i + 1] | w[i + 2] | w[i + 3] | w[i + 4]); };
+  switch (call) {
+    case BSP_F8_CALL_SAVE: {
+      const bsp_codes c = codes(3);
+      return bsp_f8_save(ptr(0), num(1), w[2], &c, ptr(8));
+    }
+    case BSP_F8_CALL_LOAD: {
+      const bsp_codes c = codes(0);
+      return bsp_f8_load(&c, ptr(5), num(6), w[7], ptr(8));
+    }
+    case BSP_F8_CALL_FC: {
+      const bsp_codes x = codes(2), g = codes(10);
+      return bsp_f8_fc((const bsp_weights_f8*)ptr(0), num(1), &x, (const float*)ptr(7), ptr(8), num(9), none(10) ? nullptr : &g, ptr(15), num(16), ptr(17));
+    }
+    case BSP_F8_CALL_VALUES: {
+      const bsp_codes g = codes(10);
+      return bsp_f8_fc_values((const bsp_weights_f8*)ptr(0), num(1), ptr(2), num(3), w[4], size(5), num(6), (const float*)ptr(7), ptr(8), num(9),
+                              none(10) ? nullptr : &g, ptr(15), num(16), ptr(17), w[18], ptr(19));
+    }
+    case BSP_F8_CALL_GRAD: {
+      const bsp_codes x = codes(3);
+      return bsp_f8_fc_grad((const bsp_weights_f8*)ptr(0), ptr(1), w[2], &x, (float*)ptr(8), (float*)ptr(9), ptr(10), w[11], ptr(12));
+    }
+    case BSP_F8_CALL_NORM: {
+      const bsp_codes c = codes(10);
+      double eps;
+      memcpy(&eps, &w[7], sizeof eps);
+      return bsp_layer_norm(ptr(0), num(1), w[2], size(3), size(4), (const float*)ptr(5), (const float*)ptr(6), (float)eps, ptr(8), w[9],
+                            none(10) ? nullptr : &c, (float*)ptr(15), (float*)ptr(16), ptr(17));
+    }
+    case BSP_F8_CALL_NORM_GRAD:
+      return bsp_layer_norm_grad(ptr(0), w[1], ptr(2), w[3], num(4), size(5), size(6), (const float*)ptr(7), (const float*)ptr(8), (const float*)ptr(9),
+                                 ptr(10), w[11], (float*)ptr(12), (float*)ptr(13), ptr(14), w[15], ptr(16));
+  }
+  return BSP_ERR_SHAPE;
 }
 
 }  // extern "C"

@@ -44,8 +44,9 @@ template <bool F32, bool E5>
 __global__ __launch_bounds__(256) void f8_save(SaveArgs a) {
   __shared__ uint32_t sc[8][4];  // [column block][sixteen rows' bytes]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int c0 = blockIdx.y * 1024 + lane * 16;
-  const int64_t row0 = (int64_t)blockIdx.x * 16 + wave * 4;
+  const int across = (a.Kp + 1023) / 1024, down = blockIdx.x / across, chunk = blockIdx.x - down * across;
+  const int c0 = chunk * 1024 + lane * 16;
+  const int64_t row0 = (int64_t)down * 16 + wave * 4;
   Raw16<F32> raw[4] = {};
   const bool thin = a.K < 8;
 #pragma unroll
@@ -72,9 +73,9 @@ __global__ __launch_bounds__(256) void f8_save(SaveArgs a) {
   }
   if ((lane & 7) == 0) sc[lane >> 3][wave] = bytes;
   __syncthreads();
-  const int kb = blockIdx.y * 8 + threadIdx.x;
+  const int kb = chunk * 8 + threadIdx.x;
   if (threadIdx.x < 8 && kb * F8_BLOCK < a.Kp)
-    *(u32x4_t*)(a.scale + kb * a.srows + (int64_t)blockIdx.x * 16) =
+    *(u32x4_t*)(a.scale + kb * a.srows + (int64_t)down * 16) =
         u32x4_t{sc[threadIdx.x][0], sc[threadIdx.x][1], sc[threadIdx.x][2], sc[threadIdx.x][3]};
 }
 
@@ -88,8 +89,9 @@ struct LoadArgs {
 template <bool F32, bool E5>
 __global__ __launch_bounds__(256) void f8_load(LoadArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int c0 = blockIdx.y * 1024 + lane * 16;
-  const int64_t row0 = (int64_t)blockIdx.x * 16 + wave * 4;
+  const int across = (a.Kp + 1023) / 1024, down = blockIdx.x / across, chunk = blockIdx.x - down * across;
+  const int c0 = chunk * 1024 + lane * 16;
+  const int64_t row0 = (int64_t)down * 16 + wave * 4;
   if (c0 >= a.K) return;
   const int left = a.K - c0;
   u32x4_t q[4];
@@ -232,7 +234,9 @@ inline int launched() { return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ER
 int f8_launch_save(const void* X, int x_f32, int64_t ldx, int T, int K, bool e5, uint8_t* codes, uint8_t* scale, hipStream_t st) {
   const int Kp = f8_blocks(K) * F8_BLOCK;
   SaveArgs a{X, codes, scale, ldx, f8_scale_rows(T), T, K, Kp};
-  const dim3 grid((unsigned)((T + 15) / 16), (unsigned)((Kp + 1023) / 1024)), block(256);
+  const int64_t groups = ((int64_t)T + 15) / 16 * ((Kp + 1023) / 1024);
+  if (groups > INT32_MAX) return BSP_ERR_SHAPE;
+  const dim3 grid((unsigned)groups), block(256);
   if (x_f32) {
     if (e5) hipLaunchKernelGGL((f8_save<true, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((f8_save<true, false>), grid, block, 0, st, a);
@@ -246,7 +250,9 @@ int f8_launch_save(const void* X, int x_f32, int64_t ldx, int T, int K, bool e5,
 int f8_launch_load(const uint8_t* codes, const uint8_t* scale, int T, int K, bool e5, void* Y, int y_f32, int64_t ldy, hipStream_t st) {
   const int Kp = f8_blocks(K) * F8_BLOCK;
   LoadArgs a{codes, scale, Y, ldy, f8_scale_rows(T), T, K, Kp};
-  const dim3 grid((unsigned)((T + 15) / 16), (unsigned)((Kp + 1023) / 1024)), block(256);
+  const int64_t groups = ((int64_t)T + 15) / 16 * ((Kp + 1023) / 1024);
+  if (groups > INT32_MAX) return BSP_ERR_SHAPE;
+  const dim3 grid((unsigned)groups), block(256);
   if (y_f32) {
     if (e5) hipLaunchKernelGGL((f8_load<true, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((f8_load<true, false>), grid, block, 0, st, a);

@@ -1,11 +1,12 @@
 // FC layers on many rows, weights and activations in 8-bit codes: Y = act(X W^t + b + residual), bound by the matrix cores.
 //
-// A workgroup owns BT rows by R block rows of 128 channels and walks the block columns that its block rows keep; a step is 128
-// columns, both operands staged in LDS with 16-byte asynchronous copies (two buffers: a step is multiplied while the
-// next one arrives).  The weights are the matrix core's rows and the activations its columns, so a lane's four
-// neighbouring results are neighbouring channels of one row of Y, and an activation's scale is one byte a lane.
+// A workgroup owns 32 to 256 rows by one or two block rows of 128 channels and walks the block columns that its block rows keep (two: where
+// all are kept); a step is 128 columns, both operands staged in LDS with 16-byte asynchronous copies, two to four buffers
+// deep.  The weights are the matrix core's rows and the activations its columns, so a lane's four neighbouring results
+// are neighbouring channels of one row of Y, and an activation's scale is one byte a lane.
 // A staged row of 128 bytes is eight pieces of 16; piece p of row r lies at place p ^ (r / 2 mod 8), so sixteen rows' same
 // piece, which sixteen lanes read together, lie in sixteen different bank groups.
+// MO x MT tiles of 32 x 32 a wave, WO x WT waves.
 #include "bsp_f8.h"
 #include <type_traits>
 
@@ -34,12 +35,12 @@ __device__ __forceinline__ f32x16_t mfma_bf16_32x32x16(u32x4_t a, u32x4_t b, f32
 template <int MO>
 constexpr int kStoreBytes = 32 * (32 * MO * 4 + 16);
 
-template <int MO, int MT>
+template <int MO, int MT, bool F32>
 __device__ __forceinline__ void store_tile(const F8Epilogue& q, f32x16_t (&acc)[MO][MT], uint8_t* lds, int T, int O, int64_t t0, int o0) {
   const int lane = threadIdx.x & 63;
   constexpr int kLanes = 4 * MO;  // lanes that hold a row's piece, eight channels each
   const int c = o0 + (lane % kLanes) * 8;
-  if (q.residual || !q.vec8) {  // fp32 through LDS, then four channels at a time
+  if (F32 || q.residual || !q.vec8) {  // fp32 through LDS, then four channels at a time
     constexpr int kRow = 32 * MO * 4 + 16;
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -54,7 +55,7 @@ __device__ __forceinline__ void store_tile(const F8Epilogue& q, f32x16_t (&acc)[
         const int64_t t = t0 + m * 32 + r;
         const int ch = o0 + (lane % (8 * MO)) * 4;
         const f32x4_t v = *(const f32x4_t*)(lds + r * kRow + (lane % (8 * MO)) * 16);
-        if (t < T && ch < O) f8_store4<false>(q, t, ch, O, v[0], v[1], v[2], v[3]);
+        if (t < T && ch < O) f8_store4<F32>(q, t, ch, O, v[0], v[1], v[2], v[3]);
       }
     }
     return;
@@ -112,114 +113,6 @@ __device__ __forceinline__ void place_tile(int b, int tiles_o, int tiles_t, int*
   *tt = r / wide;
 }
 
-// MO x MT tiles of 32 x 32 a wave, WO x WT waves; R block rows
-template <int MO, int MT, int WO, int WT, bool E5, bool F32>
-__global__ __launch_bounds__(64 * WO * WT) void f8_tile(TileArgs a) {
-  constexpr int NO = 32 * MO * WO, NT = 32 * MT * WT, WAVES = WO * WT, R = NO / F8_BLOCK;
-  constexpr int STAGE = (NO + NT) * F8_BLOCK;
-  static_assert(NO % F8_BLOCK == 0 && (NO + NT) % (8 * WAVES) == 0);
-  extern __shared__ uint8_t lds[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wo = wave / WT, wt = wave % WT;
-  int tile_o, tile_t;
-  place_tile(blockIdx.x, a.tiles_o, a.tiles_t, &tile_o, &tile_t);
-  const int br = tile_o * R;
-  const int64_t t0 = (int64_t)tile_t * NT;
-  const int n0 = a.w.ptr[br], n1 = a.w.ptr[br + 1];
-
-  // this lane's part of a request of eight staged rows: row lane / 8 at place lane % 8
-  const int srow = lane >> 3;
-  // pieces that this lane reads of its row of a fragment, for the two halves of a step
-  const int f = (lane >> 1) & 7, g2 = (lane >> 5) * 2;
-  int at[2][2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int q = 0; q < 2; ++q) at[h][q] = (lane & 31) * F8_BLOCK + (((4 * h + g2 + q) ^ f) << 4);
-
-  int64_t trow[MT];
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int64_t t = t0 + (wt * MT + m) * 32 + (lane & 31);
-    trow[m] = t < a.T ? t : a.T - 1;
-  }
-
-  auto stage = [&](int n, int buf) {
-    uint8_t* base = lds + buf * STAGE;
-    const int kb = a.w.idx[n];
-#pragma unroll
-    for (int q = wave; q < (NO + NT) / 8; q += WAVES) {
-      const int row = q * 8 + srow;
-      const int piece = (lane & 7) ^ ((row >> 1) & 7);
-      const uint8_t* src;
-      if (row < NO) {
-        const int64_t blk = R == 1 ? n : n + (int64_t)(row >> 7) * (n1 - n0);
-        src = a.w.payload + blk * F8_BLOCK_BYTES + (row & 127) * F8_BLOCK + piece * 16;
-      } else {
-        int64_t t = t0 + row - NO;
-        t = t < a.T ? t : a.T - 1;  // rows past the last: the last one's bytes, their results go nowhere
-        src = a.X + t * a.ld + (int64_t)kb * F8_BLOCK + piece * 16;
-      }
-      __builtin_amdgcn_global_load_lds((f8_gptr_t)src, (f8_lptr_t)(base + q * 1024), 16, 0, 0);
-    }
-  };
-
-  f32x16_t acc[MO][MT] = {};
-  if (n0 < n1) stage(n0, 0);
-  for (int n = n0; n < n1; ++n) {
-    const int buf = (n - n0) & 1;
-    int sx[MT];
-    const int kb = a.w.idx[n];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) sx[m] = a.scale[kb * a.srows + trow[m]];
-    const int sw = a.w.scale[R == 1 ? n : n + (int64_t)((wo * MO * 32) >> 7) * (n1 - n0)];
-    __builtin_amdgcn_s_waitcnt(0);  // this wave's requests have landed,
-    __builtin_amdgcn_s_barrier();   // and every wave's; the other buffer has been read
-    asm volatile("" ::: "memory");
-    if (n + 1 < n1) stage(n + 1, buf ^ 1);
-    const uint8_t* W = lds + buf * STAGE + wo * MO * 32 * F8_BLOCK;
-    const uint8_t* X = lds + buf * STAGE + (NO + wt * MT * 32) * F8_BLOCK;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      i32x8_t x[MT];
-#pragma unroll
-      for (int m = 0; m < MT; ++m) x[m] = read_fragment(X + m * 32 * F8_BLOCK, at[h][0], at[h][1]);
-#pragma unroll
-      for (int o = 0; o < MO; ++o) {
-        const i32x8_t w = read_fragment(W + o * 32 * F8_BLOCK, at[h][0], at[h][1]);
-        if constexpr (F32) {  // as bf16, so that nothing is lost in the sum (see f8_few)
-          const float fw = __uint_as_float((uint32_t)sw << 23);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const u32x4_t wj = f8_decode_bf16x8<false>(w[2 * j], w[2 * j + 1], fw);
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-              acc[o][m] = mfma_bf16_32x32x16(wj, f8_decode_bf16x8<E5>(x[m][2 * j], x[m][2 * j + 1], __uint_as_float((uint32_t)sx[m] << 23)), acc[o][m]);
-          }
-        } else {
-#pragma unroll
-          for (int m = 0; m < MT; ++m)
-            acc[o][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x[m], acc[o][m], 0, E5 ? 1 : 0, 0, sw, 0, sx[m]);
-        }
-      }
-    }
-  }
-
-  const int ob = tile_o * NO + wo * MO * 32 + (lane >> 5) * 4;
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int64_t t = t0 + (wt * MT + m) * 32 + (lane & 31);
-    if (t >= a.T) continue;
-#pragma unroll
-    for (int o = 0; o < MO; ++o)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int c = ob + o * 32 + q * 8;
-        if (c < a.w.out) f8_store4<F32>(a.q, t, c, a.w.out, acc[o][m][4 * q], acc[o][m][4 * q + 1], acc[o][m][4 * q + 2], acc[o][m][4 * q + 3]);
-      }
-  }
-}
-
 // ------------------------------------------------------------------ the kernel
 // A wave overlaps its own work: it reads one half of a step (64 columns) while it multiplies the other, and one barrier a step,
 // between the halves, both frees the buffer that all have read and hands over the one that has landed.  The copies of the
@@ -271,8 +164,25 @@ struct Wide {
 #pragma unroll
     for (int m = 0; m < MT; ++m) s[m] = from[at_s + m * 32];
   }
-  template <bool E5>
+  // F32: as bf16, so that nothing is lost in the sum (see f8_few)
+  template <bool E5, bool F32>
   static __device__ __forceinline__ void multiply(i32x8_t (&w)[MO], i32x8_t (&x)[MT], int sw, int (&sx)[MT], f32x16_t (&acc)[MO][MT]) {
+    if constexpr (F32) {
+      const float fw = __uint_as_float((uint32_t)sw << 23);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        u32x4_t wj[MO], xj[MT];
+#pragma unroll
+        for (int o = 0; o < MO; ++o) wj[o] = f8_decode_bf16x8<false>(w[o][2 * j], w[o][2 * j + 1], fw);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) xj[m] = f8_decode_bf16x8<E5>(x[m][2 * j], x[m][2 * j + 1], __uint_as_float((uint32_t)sx[m] << 23));
+#pragma unroll
+        for (int o = 0; o < MO; ++o)
+#pragma unroll
+          for (int m = 0; m < MT; ++m) acc[o][m] = mfma_bf16_32x32x16(wj[o], xj[m], acc[o][m]);
+      }
+      return;
+    }
 #pragma unroll
     for (int o = 0; o < MO; ++o)
 #pragma unroll
@@ -283,12 +193,13 @@ struct Wide {
   // Step i, whose first half has been read.  LATER: steps to come that have been asked for (all of the BUFS - 1 that fit in the
   // main loop, where this step asks for one more).  `to` is written behind the barrier alone, `from` and `next` are other
   // bytes by then: the compiler need not order its reads of LDS behind copies in flight, the waits here do.
-  template <bool E5, int LATER, bool MORE>
+  template <bool E5, bool F32, int LATER, bool MORE>
   __device__ __forceinline__ void step(uint8_t* __restrict__ to, const uint8_t* __restrict__ from, const uint8_t* __restrict__ next, int i, int sw, int kb,
                                        i32x8_t (&w)[2][MO], i32x8_t (&x)[2][MT], int (&sx)[2][MT], f32x16_t (&acc)[MO][MT]) const {
     constexpr int N = MO * MT, kRead = 2 * (MO + MT);
     read(from, 1, w[1], x[1]);
-    multiply<E5>(w[0], x[0], sw, sx[0], acc);
+    multiply<E5, F32>(w[0], x[0], sw, sx[0], acc);
+    if constexpr (!F32)
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                   // one matrix instruction,
@@ -304,7 +215,8 @@ struct Wide {
       read(next, 0, w[0], x[0]);
     }
     if constexpr (MORE) copy(to, i + BUFS, kb);
-    multiply<E5>(w[1], x[1], sw, sx[0], acc);
+    multiply<E5, F32>(w[1], x[1], sw, sx[0], acc);
+    if constexpr (!F32) {
 #pragma unroll
     for (int k = 0; k < kHalf; ++k) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -315,12 +227,13 @@ struct Wide {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       if constexpr (MORE) __builtin_amdgcn_sched_group_barrier(0x020, (COPIES + kHalf - 1) / kHalf, 0);  // copies to LDS
     }
+    }
 #pragma unroll
     for (int m = 0; m < MT; ++m) sx[0][m] = sx[1][m];
   }
 };
 
-template <int MO, int MT, int WO, int WT, int BUFS, bool E5>
+template <int MO, int MT, int WO, int WT, int BUFS, bool E5, bool F32>
 __global__ __launch_bounds__(64 * WO * WT) void f8_wide(TileArgs a) {
   using K = Wide<MO, MT, WO, WT, BUFS>;
   extern __shared__ uint8_t lds[];
@@ -390,7 +303,7 @@ __global__ __launch_bounds__(64 * WO * WT) void f8_wide(TileArgs a) {
       const int end = c + 64 < cnt - BUFS ? c + 64 : cnt - BUFS;
       for (int i = c; i < end; ++i) {
         const int nxt = following(cur);
-        k.template step<E5, BUFS - 1, true>(lds + cur, lds + cur, lds + nxt, i, __builtin_amdgcn_readlane(scales, i - c),
+        k.template step<E5, F32, BUFS - 1, true>(lds + cur, lds + cur, lds + nxt, i, __builtin_amdgcn_readlane(scales, i - c),
                                             __builtin_amdgcn_readlane(cols, i - c), w, x, sx, acc);
         cur = nxt;
       }
@@ -399,7 +312,7 @@ __global__ __launch_bounds__(64 * WO * WT) void f8_wide(TileArgs a) {
       constexpr int L = decltype(later)::value;
       if (cnt > L) {
         const int nxt = following(cur);
-        k.template step<E5, L, false>(lds + cur, lds + cur, lds + nxt, 0, __builtin_amdgcn_readlane(tail_scales, cnt - 1 - L - tail), 0, w, x, sx, acc);
+        k.template step<E5, F32, L, false>(lds + cur, lds + cur, lds + nxt, 0, __builtin_amdgcn_readlane(tail_scales, cnt - 1 - L - tail), 0, w, x, sx, acc);
         cur = nxt;
       }
     };
@@ -409,7 +322,7 @@ __global__ __launch_bounds__(64 * WO * WT) void f8_wide(TileArgs a) {
     rest(std::integral_constant<int, 0>{});
   }
   __syncthreads();
-  store_tile<MO, MT>(a.q, acc, lds + wave * kStoreBytes<MO>, a.T, a.w.out, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32);
+  store_tile<MO, MT, F32>(a.q, acc, lds + wave * kStoreBytes<MO>, a.T, a.w.out, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32);
 }
 
 template <int NO, int NT>
@@ -423,17 +336,11 @@ int launch(void (*kernel)(TileArgs), bool raised, int threads, int lds, TileArgs
 }
 bool raise(const void* kernel, int lds) { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess; }
 
-template <int MO, int MT, int WO, int WT, bool E5, bool F32>
-int launch_tile(const TileArgs& a, hipStream_t st) {
-  constexpr int NO = 32 * MO * WO, NT = 32 * MT * WT;
-  static const bool raised = raise((const void*)&f8_tile<MO, MT, WO, WT, E5, F32>, 2 * (NO + NT) * F8_BLOCK);
-  return launch<NO, NT>(f8_tile<MO, MT, WO, WT, E5, F32>, raised, 64 * WO * WT, 2 * (NO + NT) * F8_BLOCK, a, st);
-}
-template <int MO, int MT, int WO, int WT, int BUFS, bool E5>
+template <int MO, int MT, int WO, int WT, int BUFS, bool E5, bool F32>
 int launch_wide(const TileArgs& a, hipStream_t st) {
   using K = Wide<MO, MT, WO, WT, BUFS>;
-  static const bool raised = raise((const void*)&f8_wide<MO, MT, WO, WT, BUFS, E5>, K::kLds);
-  return launch<K::NO, K::NT>(f8_wide<MO, MT, WO, WT, BUFS, E5>, raised, 64 * K::WAVES, K::kLds, a, st);
+  static const bool raised = raise((const void*)&f8_wide<MO, MT, WO, WT, BUFS, E5, F32>, K::kLds);
+  return launch<K::NO, K::NT>(f8_wide<MO, MT, WO, WT, BUFS, E5, F32>, raised, 64 * K::WAVES, K::kLds, a, st);
 }
 
 // Which tile: the smaller of the chip's rate on it and of the steps' own latency, one after the other.  `alone`: us a step where a CU has one
@@ -464,14 +371,21 @@ int pick_tile(int O, int64_t nnzb, int T, bool full) {
 
 template <bool E5>
 int launch_any(const TileArgs& a, bool f32, hipStream_t st) {
-  if (f32) return launch_tile<2, 2, 2, 2, E5, true>(a, st);
   const bool full = a.w.nnzb == (int64_t)f8_blocks(a.w.out) * f8_blocks(a.w.in);
-  switch (pick_tile(a.w.out, a.w.nnzb, a.T, full)) {
-    case 0: return launch_wide<4, 2, 2, 4, 2, E5>(a, st);
-    case 1: return launch_wide<4, 2, 1, 4, 3, E5>(a, st);
-    case 2: return launch_wide<2, 2, 2, 2, 2, E5>(a, st);
-    case 3: return launch_wide<2, 1, 2, 2, 3, E5>(a, st);
-    default: return launch_wide<1, 1, 4, 1, 4, E5>(a, st);
+  const int k = pick_tile(a.w.out, a.w.nnzb, a.T, full);
+  if (f32) {
+    switch (k) {
+      case 3: return launch_wide<2, 1, 2, 2, 3, E5, true>(a, st);
+      case 4: return launch_wide<1, 1, 4, 1, 4, E5, true>(a, st);
+      default: return launch_wide<2, 2, 2, 2, 2, E5, true>(a, st);
+    }
+  }
+  switch (k) {
+    case 0: return launch_wide<4, 2, 2, 4, 2, E5, false>(a, st);
+    case 1: return launch_wide<4, 2, 1, 4, 3, E5, false>(a, st);
+    case 2: return launch_wide<2, 2, 2, 2, 2, E5, false>(a, st);
+    case 3: return launch_wide<2, 1, 2, 2, 3, E5, false>(a, st);
+    default: return launch_wide<1, 1, 4, 1, 4, E5, false>(a, st);
   }
 }
 

@@ -23,6 +23,8 @@ typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 typedef const __attribute__((address_space(1))) uint8_t* global_t;
 typedef u32x4_t __attribute__((aligned(2))) u32x4_any;  // sixteen bytes at any bf16's address
 
+static_assert(kAhead == 2);
+
 __device__ __forceinline__ u32x4_t read_columns(const uint8_t* p) {  // rows +0..3 and +4..7 of this lane's column
   auto* q = (__attribute__((address_space(3))) s16x4_t*)(uintptr_t)p;
   const u32x2_t a = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(q));
@@ -70,7 +72,7 @@ template <int C, bool E5, bool THIN>
 __global__ __launch_bounds__(kThreads) void f8_grad(F8GradArgs a) {
   constexpr int MO = C, WO = 4 / MO;  // 32-row tiles of outputs a wave, waves side by side over the 128 outputs
   constexpr int kBuffer = (1 + C) * kTile;
-  constexpr int kPieces = C > 1 ? C / 2 : 1, kCodes = C > 1 ? 16 : 8, kWords = kCodes / 4;  // runs of codes a thread brings, of a block each
+  constexpr int kPieces = C > 1 ? C / 2 : 1, kCodes = C > 1 ? 16 : 8;  // runs of codes a thread brings, of a block each
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   kernarg_touch<F8GradArgs>();
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -110,7 +112,7 @@ __global__ __launch_bounds__(kThreads) void f8_grad(F8GradArgs a) {
   const uint32_t col_y = (uint32_t)(o + 8 <= a.O || THIN ? o : a.O - 8) * 2;
   const int past = o + 8 <= a.O || (THIN && piece == 0) ? 0 : o + 8 - a.O < 8 ? o + 8 - a.O : 8;  // of them
   const int64_t Kp = (int64_t)f8_blocks(a.I) * F8_BLOCK, srows = f8_scale_rows(a.T);
-  const int j_in = piece * kCodes >> 7, at_in = (piece * kCodes) & 127;  // the first run's block, and its columns in that; the next lies two blocks on
+  const int j_in = (piece * kCodes) >> 7, at_in = (piece * kCodes) & 127;  // the first run's block, and its columns in that; the next lies two blocks on
   uint32_t col_x[kPieces], col_s[kPieces];
 #pragma unroll
   for (int p = 0; p < kPieces; ++p) {
@@ -119,42 +121,41 @@ __global__ __launch_bounds__(kThreads) void f8_grad(F8GradArgs a) {
     col_s[p] = (uint32_t)(kb * srows);
   }
   u32x4_t y_in[kAhead];
-  uint32_t x_in[kAhead][kPieces][kWords];
-  int s_in[kAhead][kPieces], rows_in[kAhead];
-  // Step i's values to registers; past the range's end the last row's, which `write` drops.  Nothing here looks at what it loads: that would
-  // wait for it.  Every address is the same 64 bits in all lanes and 32 of a lane's own.
-  auto load = [&](int i, int j) {
-    const int64_t t0 = t_begin + (int64_t)i * kStep;
-    const int64_t from = t0 < t_end ? t0 : t_end - 1;
-    rows_in[j] = t0 < t_end ? (int)(t_end - t0 < kStep ? t_end - t0 : kStep) : 0;
-    const int most = rows_in[j] > 0 ? rows_in[j] - 1 : 0;
-    const uint32_t r = row < most ? row : most;
-    auto *by = (global_t)(a.dY + from * a.ldy), *bx = (global_t)(a.codes + from * Kp), *bs = (global_t)(a.scale + from);
+  u32x2_t x_in[kAhead][kPieces][kCodes / 8];
+  int s_in[kAhead][kPieces];
+  const int key = chunk_key(row);
+  // A run of sixteen codes becomes a chunk of 32 bytes in two writes; every other row takes its second half first, so that a write of
+  // four rows touches all banks.
+  const uint32_t swap = kCodes == 16 && (row & 1) ? 8 : 0;
+  const int to_y = row * 256 + ((piece >> 1) ^ key) * 32 + (piece & 1) * 16;
+  const int to_x = (1 + j_in) * kTile + row * 256 + ((at_in >> 4) ^ key) * 32 + (kCodes == 8 ? (at_in & 8) * 2 : swap * 2);
+  // To registers: eight gradients and the codes of row r of those that follow by, bx, bs, which are the same in all lanes.  Nothing here looks
+  // at what it asks for: that would wait for it.
+  auto ask = [&](global_t by, global_t bx, global_t bs, uint32_t r, int j) {
     asm volatile("" : "+s"(by), "+s"(bx), "+s"(bs));
     if constexpr (THIN) y_in[j] = gradients8((const uint16_t*)by + r * a.ldy, 0, a.O);
     else y_in[j] = *(const __attribute__((address_space(1))) u32x4_any*)(by + (r * (uint32_t)a.ldy * 2 + col_y));
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
-      auto* c = bx + (r * (uint32_t)Kp + col_x[p]);
-      if constexpr (kWords == 2) {
-        const u32x2_t v = *(const __attribute__((address_space(1))) u32x2_t*)c;
-        x_in[j][p][0] = v.x, x_in[j][p][1] = v.y;
-      } else {
-        const u32x4_t v = *(const __attribute__((address_space(1))) u32x4_t*)c;
+      const uint32_t at = r * (uint32_t)Kp + col_x[p];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x_in[j][p][e] = v[e];
-      }
+      for (int h = 0; h < kCodes / 8; ++h) x_in[j][p][h] = *(const __attribute__((address_space(1))) u32x2_t*)(bx + (at + (swap ^ 8 * h)));
       s_in[j][p] = bs[r + col_s[p]];
     }
   };
-  const int key = chunk_key(row);
-  const int to_y = row * 256 + ((piece >> 1) ^ key) * 32 + (piece & 1) * 16;
-  // A run of sixteen codes becomes a chunk of 32 bytes in two writes; every other row writes its second half first, so that a write of
-  // four rows touches all banks.
-  const bool swap = kCodes == 16 && (row & 1);
-  const int to_x = (1 + j_in) * kTile + row * 256 + ((at_in >> 4) ^ key) * 32 + (kCodes == 8 ? (at_in & 8) * 2 : swap ? 16 : 0);
-  auto write = [&](int buf, int j, auto ENDS) {  // rows past the range add nothing, whatever they hold; ENDS: the last outputs' block row
-    const bool in = row < rows_in[j];
+  // Rows of step i in the range; `load` is `ask` for any step: past the range's end the last row's values, which `write` drops.
+  auto rows_of = [&](int i) {
+    const int64_t left = t_end - (t_begin + (int64_t)i * kStep);
+    return left < 0 ? 0 : left < kStep ? (int)left : kStep;
+  };
+  auto load = [&](int i, int j) {
+    const int rows = rows_of(i), most = rows > 0 ? rows - 1 : 0;
+    const int64_t from = rows > 0 ? t_begin + (int64_t)i * kStep : t_end - 1;
+    ask((global_t)(a.dY + from * a.ldy), (global_t)(a.codes + from * Kp), (global_t)(a.scale + from), row < most ? row : most, j);
+  };
+  // To LDS.  CHECK: rows past the range add nothing, whatever they hold.  ENDS: the last outputs' block row.
+  auto write = [&](int buf, int j, auto ENDS, auto CHECK, int rows) {
+    const bool in = !decltype(CHECK)::value || row < rows;
     u32x4_t y = in ? y_in[j] : u32x4_t{0, 0, 0, 0};
     if constexpr (decltype(ENDS)::value) {
 #pragma unroll
@@ -167,19 +168,12 @@ __global__ __launch_bounds__(kThreads) void f8_grad(F8GradArgs a) {
     }
     *(u32x4_t*)(lds + buf * kBuffer + to_y) = y;
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p) {
+    for (int p = 0; p < kPieces; ++p) {  // (a block more than there are: sums that go nowhere)
       const float s = __uint_as_float((uint32_t)s_in[j][p] << 23);
-      const bool brings = in && j_in + 2 * p < has;
-      uint32_t v[kWords];
 #pragma unroll
-      for (int e = 0; e < kWords; ++e) v[e] = brings ? x_in[j][p][e] : 0;
-      uint8_t* to = lds + buf * kBuffer + 2 * p * kTile;
-      if constexpr (kCodes == 8) {
-        *(u32x4_t*)(to + to_x) = f8_decode_bf16x8<E5>(v[0], v[1], s);
-      } else {
-        const uint32_t lo0 = swap ? v[2] : v[0], lo1 = swap ? v[3] : v[1], hi0 = swap ? v[0] : v[2], hi1 = swap ? v[1] : v[3];
-        *(u32x4_t*)(to + to_x) = f8_decode_bf16x8<E5>(lo0, lo1, s);
-        *(u32x4_t*)(to + (to_x ^ 16)) = f8_decode_bf16x8<E5>(hi0, hi1, s);
+      for (int h = 0; h < kCodes / 8; ++h) {
+        const u32x2_t c = in ? x_in[j][p][h] : u32x2_t{0, 0};
+        *(u32x4_t*)(lds + buf * kBuffer + 2 * p * kTile + (to_x ^ 16 * h)) = f8_decode_bf16x8<E5>(c.x, c.y, s);
       }
     }
   };
@@ -217,25 +211,33 @@ __global__ __launch_bounds__(kThreads) void f8_grad(F8GradArgs a) {
       asm volatile("" ::: "memory");
     };
     constexpr int kReads = 2 * (MO + 2), kMul = 2 * MO;
-    auto step = [&](int i, auto U) {
+    const int full = (int)((t_end - t_begin) / kStep);
+    const int64_t ahead = t_begin + 2 * kAhead * kStep;  // the first row that the loop asks for
+    global_t by = (global_t)(a.dY + ahead * a.ldy), bx = (global_t)(a.codes + ahead * Kp), bs = (global_t)(a.scale + ahead);
+    auto step = [&](int i, auto U, auto CHECK) {
       constexpr int u = decltype(U)::value;
       read(u, 16, y[1], x[1]);
       multiply(y[0], x[0]);
 #pragma unroll
       for (int k = 0; k < kMul; ++k) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                             // a matrix instruction,
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                           // a matrix instruction,
         __builtin_amdgcn_sched_group_barrier(0x100, (kReads + kMul - 1) / kMul, 0);  // reads of LDS behind it
       }
       meet();
       read(u ^ 1, 0, y[0], x[0]);
-      write(u, u, ENDS);
-      load(i + 2 + kAhead, u);
+      write(u, u, ENDS, CHECK, decltype(CHECK)::value ? rows_of(i + kAhead) : kStep);
+      if constexpr (decltype(CHECK)::value) {
+        load(i + 2 * kAhead, u);
+      } else {
+        ask(by, bx, bs, row, u);
+        by += kStep * 2 * a.ldy, bx += kStep * Kp, bs += kStep;
+      }
       multiply(y[1], x[1]);
 #pragma unroll
       for (int k = 0; k < kMul; ++k) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, (kReads + kMul / 2 - 1) / (kMul / 2), 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);  // conversions, and the writes that follow the reads
+        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);  // conversions, and the writes that follow the reads
         if (k >= kMul / 2) __builtin_amdgcn_sched_group_barrier(0x200, 2, 0);
       }
     };
@@ -243,14 +245,22 @@ __global__ __launch_bounds__(kThreads) void f8_grad(F8GradArgs a) {
     for (int j = 0; j < kAhead; ++j) load(j, j);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      write(j, j, ENDS);
+      write(j, j, ENDS, std::true_type{}, rows_of(j));
       load(j + kAhead, j);
     }
     meet();
     read(0, 0, y[0], x[0]);
-    for (int i = 0; i < n; i += 2) {  // (behind an odd number of steps one of zeros)
-      step(i, std::integral_constant<int, 0>{});
-      step(i + 1, std::integral_constant<int, 1>{});
+    constexpr std::integral_constant<int, 0> even{};
+    constexpr std::integral_constant<int, 1> odd{};
+    int i = 0;
+    for (; i + 2 * kAhead + 1 < full; i += 2) {  // steps all of whose rows, and of those asked for, are there
+      step(i, even, std::false_type{});
+      step(i + 1, odd, std::false_type{});
+    }
+#pragma unroll 1
+    for (; i < n; i += 2) {  // (behind an odd number of steps one of zeros)
+      step(i, even, std::true_type{});
+      step(i + 1, odd, std::true_type{});
     }
   };
   if (t_begin < t_end) {

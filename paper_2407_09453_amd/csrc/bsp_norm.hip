@@ -17,7 +17,7 @@ struct NormArgs {
   const float *weight, *bias;
   void *Y, *dX;
   uint8_t *codes, *scale;
-  float *mean, *rstd, *part;
+  float *mean, *rstd, *part, *dweight, *dbias;  // part: [parts][2][D]; with one part the sums themselves
   int64_t ldx, ldy, ld_dy, ld_dx, srows;
   int32_t T, D, Dp, e5, parts;
   float eps;
@@ -227,8 +227,9 @@ __global__ __launch_bounds__(256) void norm_backward(NormArgs a) {
   for (int j = 0; j < NV; ++j) {
     const int c = (tid + j * ROWT) * 8;
     if (c >= a.D) continue;
-    f8_store8<true>(a.part + (int64_t)group * 2 * a.D, c, a.D - c, dw[j]);
-    f8_store8<true>(a.part + ((int64_t)group * 2 + 1) * a.D, c, a.D - c, db[j]);
+    float *to_w = a.parts == 1 ? a.dweight : a.part + (int64_t)group * 2 * a.D, *to_b = a.parts == 1 ? a.dbias : a.part + ((int64_t)group * 2 + 1) * a.D;
+    if (to_w) f8_store8<true>(to_w, c, a.D - c, dw[j]);
+    if (to_b) f8_store8<true>(to_b, c, a.D - c, db[j]);
   }
 }
 
@@ -272,8 +273,9 @@ __global__ __launch_bounds__(256) void norm_columns_long(NormArgs a) {
     dw += g * (x - a.mean[row]) * a.rstd[row];
     db += g;
   }
-  a.part[(int64_t)blockIdx.y * 2 * a.D + c] = dw;
-  a.part[((int64_t)blockIdx.y * 2 + 1) * a.D + c] = db;
+  float *to_w = a.parts == 1 ? a.dweight : a.part + (int64_t)blockIdx.y * 2 * a.D, *to_b = a.parts == 1 ? a.dbias : a.part + ((int64_t)blockIdx.y * 2 + 1) * a.D;
+  if (to_w) to_w[c] = dw;
+  if (to_b) to_b[c] = db;
 }
 
 // out[c] = sum of part[p][c] over p: 64 columns a workgroup, sixteen threads a column whose sums are added in their order
@@ -334,7 +336,8 @@ int sum(const float* part, int parts, int64_t width, int64_t split_at, float* ou
 
 }  // namespace
 
-int norm_parts(int T) { return T < 1 ? 1 : T < 512 ? T : 512; }
+// Up to eight rows one workgroup takes them all, and its sums are the result: a launch less than eight that each take one.
+int norm_parts(int T) { return T <= 8 ? 1 : T < 512 ? T : 512; }
 
 int norm_launch_forward(const void* X, bool f32, int64_t ldx, int T, int D, const float* weight, const float* bias, float eps,
                         void* Y, int64_t ldy, int code, uint8_t* codes, uint8_t* scale, float* mean, float* rstd, hipStream_t st) {
@@ -348,9 +351,9 @@ int norm_launch_forward(const void* X, bool f32, int64_t ldx, int T, int D, cons
 int norm_launch_backward(const void* dY, int64_t ld_dy, const void* X, int64_t ldx, bool f32, const float* mean, const float* rstd, const float* weight,
                          int T, int D, void* dX, int64_t ld_dx, float* dweight, float* dbias, float* part, hipStream_t st) {
   NormArgs a{};
-  a.X = X, a.dY = dY, a.weight = weight, a.dX = dX, a.mean = (float*)mean, a.rstd = (float*)rstd, a.part = part;
+  a.X = X, a.dY = dY, a.weight = weight, a.dX = dX, a.mean = (float*)mean, a.rstd = (float*)rstd, a.part = part, a.dweight = dweight, a.dbias = dbias;
   a.ldx = ldx, a.ld_dy = ld_dy, a.ld_dx = ld_dx, a.T = T, a.D = D, a.parts = norm_parts(T);
   const int rc = f32 ? backward<true>(a, st) : backward<false>(a, st);
-  if (rc != BSP_OK) return rc;
+  if (rc != BSP_OK || a.parts == 1) return rc;
   return sum(part, a.parts, 2 * (int64_t)D, D, dweight, dbias, st);
 }

@@ -1,65 +1,110 @@
 """FC layers in 8-bit floating point, the 8-bit checkpoints of their inputs, their gradients, and layer norm, on torch
-tensors.  Marshalling only: every call launches on the current stream (or ``stream``) of its tensors' device and returns
-before it is done; tensors that it makes come from torch's allocator on that stream."""
+tensors.  Marshalling only: every call launches on the current stream (or ``stream``, a handle as an integer) of its tensors'
+device and returns before it is done; tensors that it makes come from torch's allocator on the current stream.
+
+A call's arguments go to the library as one string of words: of a small layer's 9 us on the host ctypes' conversion of 16 arguments
+one by one took 2, and a tensor of torch's takes 1.5 us to make, so a checkpoint is one allocation."""
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Optional
 
 import numpy as np
 
-from .binding import (BSP_BF16, BSP_E4M3, BSP_E5M2, BSP_F32, _check, _current_stream, _np_ptr, bsp_codes, bsp_weights_f8,
-                      load_library)
+from .binding import (BSP_BF16, BSP_E4M3, BSP_E5M2, BSP_F32, BspError, _check, _current_stream, _np_ptr, bsp_codes,
+                      bsp_weights_f8, load_library)
 
 CODES = {"e4m3": BSP_E4M3, "e5m2": BSP_E5M2}
+_SAVE, _LOAD, _FC, _VALUES, _GRAD, _NORM, _NORM_GRAD = range(7)
+_pack9, _pack13, _pack17, _pack18, _pack20 = (struct.Struct("=%dq" % n).pack for n in (9, 13, 17, 18, 20))
+_pack_norm = struct.Struct("=7qd10q").pack
+_NO_CODES = (0, 0, 0, 0, 0)
+_types = None
 
 
 def _type(t) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
-        return BSP_BF16
-    assert t.dtype == torch.float32, t.dtype
-    return BSP_F32
+    global _types
+    if _types is None:
+        import torch
+        _types = {torch.bfloat16: BSP_BF16, torch.float32: BSP_F32}
+    code = _types.get(t.dtype)
+    assert code is not None, t.dtype
+    return code
 
 
 def _rows(t):
     """(T, K, elements from row to row) of a matrix whose rows are contiguous; rows may lie any distance apart."""
     T, K = t.shape
-    assert t.is_cuda and (t.stride(1) == 1 or K == 1 or T == 0)
-    return T, K, t.stride(0) if T > 1 else K
+    ld, one = t.stride()
+    assert t.is_cuda and (one == 1 or K == 1 or T == 0), "a matrix on a GPU with contiguous rows"
+    return T, K, ld if T > 1 else K
 
 
 def _blocks(n: int) -> int:
-    return -(-n // 128)
+    return (n + 127) >> 7
 
 
 def _on(t, *others):
-    assert all(o is None or o.device == t.device for o in others)
+    at = t.get_device()
+    for o in others:
+        assert o is None or o.get_device() == at, "tensors on different devices"
+
+
+def _call(call, words, name):
+    rc = load_library().bsp_f8_call_packed(call, words)
+    if rc:
+        raise BspError(rc, name)
+
+
+def _keep(t, stream):
+    """A workspace that is dropped while its kernels may still wait in a stream other than torch's current one."""
+    if stream is not None and t is not None:
+        import torch
+        t.record_stream(torch.cuda.ExternalStream(int(stream), device=t.device))
 
 
 class BspCodes:
     """A matrix [T][K] held as 8-bit floating-point codes with a power-of-two scale for each row's 128 columns: the form in
     which a layer's input is kept for the backward pass.  ``codes`` [T][128 ceil(K/128)] and ``scale``
-    [ceil(K/128)][16 ceil(T/16)] (exponent + 127) are uint8 tensors; ``kind`` is "e4m3" or "e5m2"."""
+    [ceil(K/128)][16 ceil(T/16)] (exponent + 127) are uint8 views of one buffer; ``kind`` is "e4m3" or "e5m2"."""
+
+    __slots__ = ("T", "K", "kind", "buffer", "words")
 
     def __init__(self, T: int, K: int, kind: str = "e4m3", device="cuda:0"):
         import torch
         self.T, self.K, self.kind = T, K, kind
         nb = _blocks(K)
-        self.codes = torch.empty((T, nb * 128), dtype=torch.uint8, device=device)
-        self.scale = torch.empty((nb, (T + 15) // 16 * 16), dtype=torch.uint8, device=device)
-        self.struct = bsp_codes(T, K, CODES[kind], self.codes.data_ptr() or None, self.scale.data_ptr() or None)
+        self.buffer = torch.empty(nb * (128 * T + (T + 15 & ~15)), dtype=torch.uint8, device=device)
+        p = self.buffer.data_ptr()
+        self.words = (T, K, CODES[kind], p, p + nb * 128 * T)
+
+    @property
+    def codes(self):
+        n = _blocks(self.K) * 128
+        return self.buffer[:self.T * n].view(self.T, n)
+
+    @property
+    def scale(self):
+        nb = _blocks(self.K)
+        return self.buffer[self.T * nb * 128:].view(nb, self.T + 15 & ~15)
+
+    @property
+    def struct(self):
+        return bsp_codes(*self.words[:3], self.words[3] or None, self.words[4] or None)
 
     def load(self, dtype=None, out=None, stream=None):
         """The values, as bf16 (or torch.float32)."""
-        import torch
         if out is None:
-            out = torch.empty((self.T, self.K), dtype=dtype or torch.bfloat16, device=self.codes.device)
-        T, K, ld = _rows(out)
-        assert (T, K) == (self.T, self.K)
-        _on(self.codes, out)
+            import torch
+            out = torch.empty((self.T, self.K), dtype=dtype or torch.bfloat16, device=self.buffer.device)
+            ld = self.K
+        else:
+            T, K, ld = _rows(out)
+            assert (T, K) == (self.T, self.K)
+            _on(self.buffer, out)
         st = _current_stream(out) if stream is None else stream
-        _check(load_library().bsp_f8_load(self.struct, out.data_ptr(), _type(out), ld, st), "bsp_f8_load")
+        _call(_LOAD, _pack9(*self.words, out.data_ptr(), _type(out), ld, st), "bsp_f8_load")
         return out
 
 
@@ -68,10 +113,11 @@ def save8(X, kind: str = "e4m3", out: Optional[BspCodes] = None, stream=None) ->
     T, K, ld = _rows(X)
     if out is None:
         out = BspCodes(T, K, kind, X.device)
-    assert (out.T, out.K) == (T, K)
-    _on(X, out.codes)
+    else:
+        assert (out.T, out.K) == (T, K)
+        _on(X, out.buffer)
     st = _current_stream(X) if stream is None else stream
-    _check(load_library().bsp_f8_save(X.data_ptr(), _type(X), ld, out.struct, st), "bsp_f8_save")
+    _call(_SAVE, _pack9(X.data_ptr(), _type(X), ld, *out.words, st), "bsp_f8_save")
     return out
 
 
@@ -102,11 +148,13 @@ class BspLayerF8:
         _check(lib.bsp_f8_index(_np_ptr(gamma), O, I, self.col_idx.size, _np_ptr(self.row_ptr), _np_ptr(self.col_idx),
                                 _np_ptr(self.col_ptr), _np_ptr(self.row_idx)), "bsp_f8_index")
         self.d_index = [torch.from_numpy(a).to(self.device) for a in (self.row_ptr, self.col_idx, self.col_ptr, self.row_idx)]
-        # (one block more than is kept, so that an empty layer has addresses)
+        # (a block where none is kept, so that an empty layer has addresses)
         self.payload, self.payload_t = (torch.empty((max(self.nnzb, 1), 128, 128), dtype=torch.uint8, device=self.device) for _ in range(2))
         self.scale, self.scale_t = (torch.empty(max(self.nnzb, 1), dtype=torch.uint8, device=self.device) for _ in range(2))
         self.struct = bsp_weights_f8(O, I, self.nnzb, *(t.data_ptr() for t in self.d_index), self.payload.data_ptr(),
                                      self.scale.data_ptr(), self.payload_t.data_ptr(), self.scale_t.data_ptr())
+        self._address = ctypes.addressof(self.struct)
+        self._workspace = {}  # bytes that a call takes, by its kind and rows
         self.d_bias = None
         if bias is not None:
             b = torch.as_tensor(bias, dtype=torch.float32).to(self.device).contiguous()
@@ -124,38 +172,53 @@ class BspLayerF8:
         assert (O, I) == (self.O, self.I)
         st = _current_stream(W) if stream is None else stream
         _check(load_library().bsp_f8_pack(self.struct, W.data_ptr(), _type(W), ld, st), "bsp_f8_pack")
+        _keep(W, stream)
+
+    def _bytes(self, kind, T):
+        n = self._workspace.get((kind, T))
+        if n is None:
+            lib, n = load_library(), ctypes.c_int64(0)
+            if kind == "grad":
+                _check(lib.bsp_f8_fc_grad_workspace(self.struct, T, n), "bsp_f8_fc_grad_workspace")
+            else:
+                _check(lib.bsp_f8_fc_workspace(self.struct, kind, T, n), "bsp_f8_fc_workspace")
+            if len(self._workspace) > 4096:
+                self._workspace.clear()
+            n = self._workspace[(kind, T)] = n.value
+        return n
 
     def _multiply(self, transposed, X, code, bias, residual, relu, gate, dtype, out, stream):
         import torch
-        lib = load_library()
         codes = isinstance(X, BspCodes)
         if codes:
-            T, K, at = X.T, X.K, X.codes
+            T, K, at = X.T, X.K, X.buffer
         else:
             T, K, ld = _rows(X)
             at = X
-        width = self.I if transposed else self.O
-        assert K == (self.O if transposed else self.I)
+        width, inner = (self.I, self.O) if transposed else (self.O, self.I)
+        assert K == inner, (K, inner)
         if out is None:
             out = torch.empty((T, width), dtype=dtype or (torch.bfloat16 if codes else X.dtype), device=at.device)
-        assert out.shape == (T, width) and out.is_contiguous()
-        _on(self.payload, at, out, residual, None if gate is None else gate.codes)
+        else:
+            assert out.shape == (T, width) and out.is_contiguous()
+        _on(self.payload, at, out, residual, None if gate is None else gate.buffer)
         if residual is not None:
             assert residual.shape == out.shape and residual.dtype == out.dtype and residual.is_contiguous()
         st = _current_stream(out) if stream is None else stream
-        rest = (None if bias is None else bias.data_ptr(), None if residual is None else residual.data_ptr(),
-                1 if relu else 0, None if gate is None else gate.struct, out.data_ptr() or None, _type(out))
+        rest = (0 if bias is None else bias.data_ptr(), 0 if residual is None else residual.data_ptr(), 1 if relu else 0,
+                *(_NO_CODES if gate is None else gate.words), out.data_ptr(), _type(out))
         if codes:
-            _check(lib.bsp_f8_fc(self.struct, transposed, X.struct, *rest, st), "bsp_f8_fc")
+            _call(_FC, _pack18(self._address, transposed, *X.words, *rest, st), "bsp_f8_fc")
             return out
-        n = ctypes.c_int64(0)
-        if not (T <= 16 and T * (_blocks(K) * 129 + 16) <= 73728 and (X.data_ptr() | ld * X.element_size() | K * X.element_size()) % 16 == 0):
-            _check(lib.bsp_f8_fc_workspace(self.struct, transposed, T, n), "bsp_f8_fc_workspace")
-        ws = torch.empty(n.value, dtype=torch.uint8, device=out.device) if n.value else None
-        _check(lib.bsp_f8_fc_values(self.struct, transposed, X.data_ptr() or None, _type(X), ld, T, CODES[code], *rest,
-                                    None if ws is None else ws.data_ptr(), n.value, st), "bsp_f8_fc_values")
-        if ws is not None and stream is not None:
-            ws.record_stream(torch.cuda.ExternalStream(st, device=ws.device))
+        x, size = X.data_ptr(), X.element_size()
+        ws, n = None, 0
+        # (few whole rows become codes inside the product's kernel)
+        if T > 16 or T * (_blocks(K) * 129 + 16) > 73728 or (x | ld * size | K * size) & 15:
+            n = self._bytes(transposed, T)
+            ws = torch.empty(n, dtype=torch.uint8, device=out.device)
+        _call(_VALUES, _pack20(self._address, transposed, x, _type(X), ld, T, CODES[code], *rest, 0 if ws is None else ws.data_ptr(), n, st),
+              "bsp_f8_fc_values")
+        _keep(ws, stream)
         return out
 
     def fc(self, X, relu=False, residual=None, dtype=None, out=None, stream=None):
@@ -173,30 +236,28 @@ class BspLayerF8:
         """(dW, db) from dY (bf16 [T][O]) and the checkpoint of the layer's input: dW float [O][I], zero where the mask is; db
         float [O], or None."""
         import torch
-        lib = load_library()
         T, O, ld = _rows(dY)
         assert dY.dtype == torch.bfloat16 and (T, O) == (X.T, self.O)
-        _on(self.payload, dY, X.codes, out)
+        _on(self.payload, dY, X.buffer, out)
         if out is None:
             out = torch.empty((self.O, self.I), dtype=torch.float32, device=dY.device)
-        assert out.shape == (self.O, self.I) and out.dtype == torch.float32 and out.is_contiguous()
+        else:
+            assert out.shape == (self.O, self.I) and out.dtype == torch.float32 and out.is_contiguous()
         db = torch.empty(self.O, dtype=torch.float32, device=dY.device) if bias else None
-        n = ctypes.c_int64(0)
-        _check(lib.bsp_f8_fc_grad_workspace(self.struct, T, n), "bsp_f8_fc_grad_workspace")
-        ws = torch.empty(n.value, dtype=torch.uint8, device=dY.device)
+        n = self._bytes("grad", T)
+        ws = torch.empty(n, dtype=torch.uint8, device=dY.device) if n else None
         st = _current_stream(dY) if stream is None else stream
-        _check(lib.bsp_f8_fc_grad(self.struct, dY.data_ptr() or None, ld, X.struct, out.data_ptr(),
-                                  None if db is None else db.data_ptr(), ws.data_ptr(), n.value, st), "bsp_f8_fc_grad")
-        if stream is not None:
-            ws.record_stream(torch.cuda.ExternalStream(st, device=ws.device))
+        _call(_GRAD, _pack13(self._address, dY.data_ptr(), ld, *X.words, out.data_ptr(), 0 if db is None else db.data_ptr(),
+                             0 if ws is None else ws.data_ptr(), n, st), "bsp_f8_fc_grad")
+        _keep(ws, stream)
         return out, db
 
 
 def _vector(t, D):
-    import torch
-    if t is not None:
-        assert t.is_cuda and t.dtype == torch.float32 and t.shape == (D,) and t.is_contiguous()
-    return None if t is None else t.data_ptr()
+    if t is None:
+        return 0
+    assert t.is_cuda and _type(t) == BSP_F32 and t.shape == (D,) and t.is_contiguous()
+    return t.data_ptr()
 
 
 def layer_norm(X, weight=None, bias=None, eps: float = 1e-5, code: Optional[str] = None, stream=None):
@@ -205,34 +266,47 @@ def layer_norm(X, weight=None, bias=None, eps: float = 1e-5, code: Optional[str]
     import torch
     T, D, ld = _rows(X)
     _on(X, weight, bias)
-    mean = torch.empty((2, T), dtype=torch.float32, device=X.device)
-    rstd, mean = mean[1], mean[0]
-    Y = torch.empty((T, D), dtype=X.dtype, device=X.device) if code is None else BspCodes(T, D, code, X.device)
+    mean, rstd = torch.empty((2, T), dtype=torch.float32, device=X.device).unbind(0)
+    if code is None:
+        Y = torch.empty((T, D), dtype=X.dtype, device=X.device)
+        y, words = Y.data_ptr(), _NO_CODES
+    else:
+        Y = BspCodes(T, D, code, X.device)
+        y, words = 0, Y.words
     st = _current_stream(X) if stream is None else stream
-    _check(load_library().bsp_layer_norm(X.data_ptr() or None, _type(X), ld, T, D, _vector(weight, D), _vector(bias, D), eps,
-                                         (Y.data_ptr() or None) if code is None else None, D, None if code is None else Y.struct,
-                                         mean.data_ptr() or None, rstd.data_ptr() or None, st), "bsp_layer_norm")
+    _call(_NORM, _pack_norm(X.data_ptr(), _type(X), ld, T, D, _vector(weight, D), _vector(bias, D), eps, y, D, *words, mean.data_ptr(),
+                            rstd.data_ptr(), st), "bsp_layer_norm")
     return Y, mean, rstd
 
 
 def layer_norm_grad(dY, X, mean, rstd, weight=None, stream=None):
     """(dX, dweight, dbias) from the gradient of Y, the input and what ``layer_norm`` returned with it."""
     import torch
-    lib = load_library()
     T, D, ld = _rows(X)
     T2, D2, ld_dy = _rows(dY)
     assert (T2, D2) == (T, D) and dY.dtype == X.dtype and mean.shape == rstd.shape == (T,)
-    assert mean.dtype == rstd.dtype == torch.float32 and (T < 2 or mean.stride(0) == rstd.stride(0) == 1)
+    assert _type(mean) == _type(rstd) == BSP_F32 and (T < 2 or mean.stride() == rstd.stride() == (1,))
     _on(X, dY, mean, rstd, weight)
     dX = torch.empty((T, D), dtype=X.dtype, device=X.device)
     dw, db = torch.empty((2, D), dtype=torch.float32, device=X.device).unbind(0)
-    n = ctypes.c_int64(0)
-    _check(lib.bsp_layer_norm_grad_workspace(T, D, n), "bsp_layer_norm_grad_workspace")
-    ws = torch.empty(n.value, dtype=torch.uint8, device=X.device)
+    n = _norm_bytes(T, D)
+    ws = torch.empty(n, dtype=torch.uint8, device=X.device) if n else None
     st = _current_stream(X) if stream is None else stream
-    _check(lib.bsp_layer_norm_grad(dY.data_ptr() or None, ld_dy, X.data_ptr() or None, ld, _type(X), T, D, mean.data_ptr() or None,
-                                   rstd.data_ptr() or None, _vector(weight, D), dX.data_ptr() or None, D, dw.data_ptr(), db.data_ptr(),
-                                   ws.data_ptr(), n.value, st), "bsp_layer_norm_grad")
-    if stream is not None:
-        ws.record_stream(torch.cuda.ExternalStream(st, device=ws.device))
+    _call(_NORM_GRAD, _pack17(dY.data_ptr(), ld_dy, X.data_ptr(), ld, _type(X), T, D, mean.data_ptr(), rstd.data_ptr(), _vector(weight, D),
+                              dX.data_ptr(), D, dw.data_ptr(), db.data_ptr(), 0 if ws is None else ws.data_ptr(), n, st), "bsp_layer_norm_grad")
+    _keep(ws, stream)
     return dX, dw, db
+
+
+_norm_sizes = {}
+
+
+def _norm_bytes(T, D):
+    n = _norm_sizes.get((T, D))
+    if n is None:
+        n = ctypes.c_int64(0)
+        _check(load_library().bsp_layer_norm_grad_workspace(T, D, n), "bsp_layer_norm_grad_workspace")
+        if len(_norm_sizes) > 4096:
+            _norm_sizes.clear()
+        n = _norm_sizes[(T, D)] = n.value
+    return n

@@ -106,7 +106,8 @@ def test_values_refusals(want, args):
 
 @pytest.mark.parametrize("want,args", [
     (NULL, dict(X=None)), (SHAPE, dict(X=_codes(K=256))), (SHAPE, dict(ld=255)), (NULL, dict(dY=None)), (ALIGN, dict(dW=P + 4)), (ALIGN, dict(db=P + 4)),
-    (ALIGN, dict(ws=P + 4)), (CAPACITY, dict(n=0)), (NULL, dict(ws=None)), (NULL, dict(w=None)),
+    (ALIGN, dict(ws=P + 4)), (CAPACITY, dict(X=_codes(T=1024), n=8 * (6 * 16384 + 256) * 4 - 1)), (NULL, dict(X=_codes(T=1024), ws=None)), (NULL, dict(w=None)),
+    (SHAPE, dict(ld=(1 << 25) + 1)),
 ])
 def test_weight_gradient_refusals(want, args):
     a = {**dict(w=_weights(), dY=P, ld=256, X=_codes(), dW=P, db=P, ws=P, n=1 << 30), **args}
@@ -127,11 +128,11 @@ def test_norm_refusals(want, args):
 
 
 @pytest.mark.parametrize("want,args", [
-    (DTYPE, dict(dt=b.BSP_I8)), (SHAPE, dict(D=0)), (SHAPE, dict(ld=383)), (NULL, dict(X=None)), (NULL, dict(mean=None)), (CAPACITY, dict(n=8 * 2 * 384 * 4 - 1)),
+    (DTYPE, dict(dt=b.BSP_I8)), (SHAPE, dict(D=0)), (SHAPE, dict(ld=383)), (NULL, dict(X=None)), (NULL, dict(mean=None)), (CAPACITY, dict(n=9 * 2 * 384 * 4 - 1)),
     (NULL, dict(ws=None)), (ALIGN, dict(ws=P + 4)), (ALIGN, dict(X=P + 1)),
 ])
 def test_norm_gradient_refusals(want, args):
-    a = {**dict(X=P, dt=b.BSP_F32, ld=384, T=8, D=384, mean=P, ws=P, n=8 * 2 * 384 * 4), **args}
+    a = {**dict(X=P, dt=b.BSP_F32, ld=384, T=9, D=384, mean=P, ws=P, n=9 * 2 * 384 * 4), **args}
     assert bsp.load_library().bsp_layer_norm_grad(P, a["ld"], a["X"], a["ld"], a["dt"], a["T"], a["D"], a["mean"], P, None, P, 384, P, P, a["ws"], a["n"],
                                                   None) == want
 
