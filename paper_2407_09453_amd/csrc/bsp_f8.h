@@ -40,12 +40,15 @@ __device__ __forceinline__ uint32_t f8_most(uint32_t m) {
   if constexpr (LANES == 16) m = max(m, f8_from_lane<kMirror16>(m));
   return m;
 }
-// a wave's sum, in every lane
-__device__ __forceinline__ float f8_wave_sum(float v) {
+// the sum of a row of sixteen lanes, of a wave, in every lane of it
+__device__ __forceinline__ float f8_row16_sum(float v) {
   v += __uint_as_float(f8_from_lane<kXor1>(__float_as_uint(v)));
   v += __uint_as_float(f8_from_lane<kXor2>(__float_as_uint(v)));
   v += __uint_as_float(f8_from_lane<kMirror8>(__float_as_uint(v)));
-  v += __uint_as_float(f8_from_lane<kMirror16>(__float_as_uint(v)));
+  return v + __uint_as_float(f8_from_lane<kMirror16>(__float_as_uint(v)));
+}
+__device__ __forceinline__ float f8_wave_sum(float v) {
+  v = f8_row16_sum(v);
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -290,7 +293,7 @@ struct F8GradArgs {
 };
 int f8_grad_split(int64_t nnzb, int T);              // into how many ranges of rows the sums are cut
 int f8_launch_grad(const F8GradArgs& a, hipStream_t st);
-int norm_parts(int T);                               // row ranges of a column sum
+int norm_parts(int T, int D);                        // workgroups that share the rows of a column sum
 int norm_launch_forward(const void* X, bool f32, int64_t ldx, int T, int D, const float* weight, const float* bias, float eps,
                         void* Y, int64_t ldy, int code, uint8_t* codes, uint8_t* scale, float* mean, float* rstd, hipStream_t st);
 int norm_launch_backward(const void* dY, int64_t ld_dy, const void* X, int64_t ldx, bool f32, const float* mean, const float* rstd, const float* weight,

@@ -208,7 +208,8 @@ int bsp_layer_norm(const void* X, int32_t dtype, int64_t ldx, int32_t T, int32_t
 int bsp_layer_norm_grad_workspace(int32_t T, int32_t D, int64_t* bytes) {
   if (!bytes) return BSP_ERR_NULL;
   if (T < 0 || T > kMost || D < 1 || D > kMost) return BSP_ERR_SHAPE;
-  *bytes = norm_parts(T) > 1 ? (int64_t)norm_parts(T) * 2 * D * 4 : 0;
+  const int64_t parts = norm_parts(T, D);
+  *bytes = parts > 1 ? parts * 2 * D * 4 : 0;
   return BSP_OK;
 }
 

@@ -8,7 +8,7 @@
 // Both operands are summed over their rows: LDS holds them as they lie in memory, row after row, and the transposing LDS read
 // hands a lane four rows of its column.  It takes four rows of 32 bytes from a group of sixteen lanes, and half a wave two
 // neighbouring chunks of them: the chunks of a row are permuted by the row (bits 0 and 1, then 3), so that these eight lie in different banks.
-// Two buffers of 32 rows; what is written into one was asked for, into registers, kAhead steps before.
+// Two buffers of 32 rows; what is written into one was asked for, into registers, two or four steps before.
 // Where a matrix has too few blocks for the chip the rows are cut into ranges whose sums meet in a second launch, in order.
 #include "bsp_f8.h"
 
@@ -16,14 +16,12 @@
 
 namespace {
 
-constexpr int kStep = 32, kThreads = 512, kAhead = 2;  // rows a step; steps that are on their way to registers
+constexpr int kStep = 32, kThreads = 512;  // rows a step
 constexpr int kTile = kStep * 256;                     // 32 rows of 128 bf16
 
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 typedef const __attribute__((address_space(1))) uint8_t* global_t;
 typedef u32x4_t __attribute__((aligned(2))) u32x4_any;  // sixteen bytes at any bf16's address
-
-static_assert(kAhead == 2);
 
 __device__ __forceinline__ u32x4_t read_columns(const uint8_t* p) {  // rows +0..3 and +4..7 of this lane's column
   auto* q = (__attribute__((address_space(3))) s16x4_t*)(uintptr_t)p;
@@ -69,9 +67,10 @@ __device__ __forceinline__ void column_sums(const F8GradArgs& a, int br, int64_t
 
 // THIN: fewer than eight outputs, read one by one
 template <int C, bool E5, bool THIN>
-__global__ __launch_bounds__(kThreads) void f8_grad(F8GradArgs a) {
+__global__ __launch_bounds__(kThreads, C == 1 ? 4 : 2) void f8_grad(F8GradArgs a) {
   constexpr int MO = C, WO = 4 / MO;  // 32-row tiles of outputs a wave, waves side by side over the 128 outputs
   constexpr int kBuffer = (1 + C) * kTile;
+  constexpr int kAhead = C == 4 ? 2 : 4;  // steps that are on their way to registers (the accumulators of four blocks leave room for two)
   constexpr int kPieces = C > 1 ? C / 2 : 1, kCodes = C > 1 ? 16 : 8;  // runs of codes a thread brings, of a block each
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   kernarg_touch<F8GradArgs>();
@@ -143,19 +142,17 @@ __global__ __launch_bounds__(kThreads) void f8_grad(F8GradArgs a) {
       s_in[j][p] = bs[r + col_s[p]];
     }
   };
-  // Rows of step i in the range; `load` is `ask` for any step: past the range's end the last row's values, which `write` drops.
-  auto rows_of = [&](int i) {
-    const int64_t left = t_end - (t_begin + (int64_t)i * kStep);
-    return left < 0 ? 0 : left < kStep ? (int)left : kStep;
-  };
-  auto load = [&](int i, int j) {
-    const int rows = rows_of(i), most = rows > 0 ? rows - 1 : 0;
-    const int64_t from = rows > 0 ? t_begin + (int64_t)i * kStep : t_end - 1;
+  // The range's rows that make no whole step come first, as step 0; n steps in all.
+  const int total = t_begin < t_end ? (int)(t_end - t_begin) : 0, n = (total + kStep - 1) / kStep, odd = total - (n - 1) * kStep;
+  auto load = [&](int i, int j) {  // step i, or the last
+    const int s = i < n ? i : n - 1;
+    const int64_t from = t_begin + (s > 0 ? odd + (s - 1) * kStep : 0);
+    const int most = s > 0 ? kStep - 1 : odd - 1;
     ask((global_t)(a.dY + from * a.ldy), (global_t)(a.codes + from * Kp), (global_t)(a.scale + from), row < most ? row : most, j);
   };
-  // To LDS.  CHECK: rows past the range add nothing, whatever they hold.  ENDS: the last outputs' block row.
-  auto write = [&](int buf, int j, auto ENDS, auto CHECK, int rows) {
-    const bool in = !decltype(CHECK)::value || row < rows;
+  // To LDS.  CHECK: step 0, whose missing rows add nothing.  ENDS: the last outputs' block row.
+  auto write = [&](int buf, int j, auto ENDS, auto CHECK) {
+    const bool in = !decltype(CHECK)::value || row < odd;
     u32x4_t y = in ? y_in[j] : u32x4_t{0, 0, 0, 0};
     if constexpr (decltype(ENDS)::value) {
 #pragma unroll
@@ -203,7 +200,7 @@ __global__ __launch_bounds__(kThreads) void f8_grad(F8GradArgs a) {
   // Step i in buffer i mod 2, a half of it (sixteen rows) read while the other is multiplied; one barrier, between the halves, behind which
   // the next step's buffer is whole and this one's is free for the step after that.  Nothing inside is conditional, so that
   // a wait for what a register asked for covers no more than that.
-  auto run = [&](int n, auto ENDS) {
+  auto run = [&](auto ENDS) {
     u32x4_t y[2][MO], x[2][2];
     auto meet = [&]() {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -211,11 +208,13 @@ __global__ __launch_bounds__(kThreads) void f8_grad(F8GradArgs a) {
       asm volatile("" ::: "memory");
     };
     constexpr int kReads = 2 * (MO + 2), kMul = 2 * MO;
-    const int full = (int)((t_end - t_begin) / kStep);
-    const int64_t ahead = t_begin + 2 * kAhead * kStep;  // the first row that the loop asks for
+    // where the loop's copies come from: the step 2 + kAhead further on, or the last
+    int behind = n - 3 - kAhead;  // steps after that one
+    const int64_t ahead = t_begin + (behind > 0 ? odd + (1 + kAhead) * (int64_t)kStep : n > 1 ? odd + (n - 2) * (int64_t)kStep : 0);
+    const uint32_t r_ahead = n > 1 || row < odd ? row : odd - 1;
     global_t by = (global_t)(a.dY + ahead * a.ldy), bx = (global_t)(a.codes + ahead * Kp), bs = (global_t)(a.scale + ahead);
-    auto step = [&](int i, auto U, auto CHECK) {
-      constexpr int u = decltype(U)::value;
+    auto step = [&](auto U) {  // U: its number mod kAhead
+      constexpr int u = decltype(U)::value & 1, slot = (decltype(U)::value + 2) % kAhead;
       read(u, 16, y[1], x[1]);
       multiply(y[0], x[0]);
 #pragma unroll
@@ -225,13 +224,11 @@ __global__ __launch_bounds__(kThreads) void f8_grad(F8GradArgs a) {
       }
       meet();
       read(u ^ 1, 0, y[0], x[0]);
-      write(u, u, ENDS, CHECK, decltype(CHECK)::value ? rows_of(i + kAhead) : kStep);
-      if constexpr (decltype(CHECK)::value) {
-        load(i + 2 * kAhead, u);
-      } else {
-        ask(by, bx, bs, row, u);
-        by += kStep * 2 * a.ldy, bx += kStep * Kp, bs += kStep;
-      }
+      write(u, slot, ENDS, std::false_type{});
+      ask(by, bx, bs, r_ahead, slot);
+      const int64_t on = behind > 0 ? kStep : 0;
+      by += on * 2 * a.ldy, bx += on * Kp, bs += on;
+      --behind;
       multiply(y[1], x[1]);
 #pragma unroll
       for (int k = 0; k < kMul; ++k) {
@@ -243,30 +240,33 @@ __global__ __launch_bounds__(kThreads) void f8_grad(F8GradArgs a) {
     };
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) load(j, j);
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      write(j, j, ENDS, std::true_type{}, rows_of(j));
-      load(j + kAhead, j);
-    }
+    write(0, 0, ENDS, std::true_type{});
+    load(kAhead, 0);
+    write(1, 1, ENDS, std::false_type{});
+    load(1 + kAhead, 1);
     meet();
     read(0, 0, y[0], x[0]);
-    constexpr std::integral_constant<int, 0> even{};
-    constexpr std::integral_constant<int, 1> odd{};
+    constexpr std::integral_constant<int, 0> k0{};
+    constexpr std::integral_constant<int, 1> k1{};
+    constexpr std::integral_constant<int, 2> k2{};
+    constexpr std::integral_constant<int, 3> k3{};
     int i = 0;
-    for (; i + 2 * kAhead + 1 < full; i += 2) {  // steps all of whose rows, and of those asked for, are there
-      step(i, even, std::false_type{});
-      step(i + 1, odd, std::false_type{});
+    for (; i + kAhead <= n; i += kAhead) {
+      step(k0);
+      step(k1);
+      if constexpr (kAhead == 4) {
+        step(k2);
+        step(k3);
+      }
     }
-#pragma unroll 1
-    for (; i < n; i += 2) {  // (behind an odd number of steps one of zeros)
-      step(i, even, std::true_type{});
-      step(i + 1, odd, std::true_type{});
-    }
+    if (i < n) step(k0);
+    if (i + 1 < n) step(k1);
+    if constexpr (kAhead == 4)
+      if (i + 2 < n) step(k2);
   };
-  if (t_begin < t_end) {
-    const int n = (int)((t_end - t_begin + kStep - 1) / kStep);
-    if (br == a.nbo - 1 && (a.O & 127)) run(n, std::true_type{});
-    else run(n, std::false_type{});
+  if (n > 0) {
+    if (br == a.nbo - 1 && (a.O & 127)) run(std::true_type{});
+    else run(std::false_type{});
   }
 
   if (wi >> 1 >= has) return;

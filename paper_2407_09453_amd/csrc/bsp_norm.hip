@@ -42,11 +42,11 @@ __device__ __forceinline__ void load8(const void* row, int c, int n, float* v) {
   else each8<F32>(row, c, n, v);
 }
 
-// sums of N values over the threads of a row (64: a wave, 256: the workgroup)
+// sums of N values over the threads of a row (16 lanes, a wave, the workgroup)
 template <int ROWT, int N>
 __device__ __forceinline__ void row_sum(float* v, float (*sh)[N]) {
 #pragma unroll
-  for (int k = 0; k < N; ++k) v[k] = f8_wave_sum(v[k]);
+  for (int k = 0; k < N; ++k) v[k] = ROWT == 16 ? f8_row16_sum(v[k]) : f8_wave_sum(v[k]);
   if constexpr (ROWT == 256) {
     __syncthreads();  // the last use of sh is over
     if ((threadIdx.x & 63) == 0)
@@ -86,8 +86,8 @@ template <bool F32, bool CODES, int ROWT, int NV>
 __global__ __launch_bounds__(256) void norm_forward(NormArgs a) {
   __shared__ float sh[4][1];
   const int tid = threadIdx.x % ROWT;
-  const int64_t row = ROWT == 256 ? blockIdx.x : (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= a.T) return;  // (whole waves)
+  const int64_t row = (int64_t)blockIdx.x * (256 / ROWT) + threadIdx.x / ROWT;
+  if (row >= a.T) return;  // (whole groups of ROWT)
   const void* x = row_of<F32>(a.X, row, a.ldx);
   const float inv = 1.f / (float)a.D;
   const bool ragged = a.D & 7;
@@ -167,7 +167,9 @@ template <bool F32, int ROWT, int NV>
 __global__ __launch_bounds__(256) void norm_backward(NormArgs a) {
   __shared__ float sh[4][2];
   const int tid = threadIdx.x % ROWT;
-  const int group = ROWT == 256 ? blockIdx.x : blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int kGroups = 256 / ROWT;  // rows that a workgroup has in work
+  const int in_group = threadIdx.x / ROWT;
+  const int64_t group = (int64_t)blockIdx.x * kGroups + in_group, step = (int64_t)a.parts * kGroups;
   const float inv = 1.f / (float)a.D;
   const bool ragged = a.D & 7;
   float w[NV][8], dw[NV][8], db[NV][8];
@@ -191,7 +193,7 @@ __global__ __launch_bounds__(256) void norm_backward(NormArgs a) {
     }
   };
   if (group < a.T) ask(group);
-  for (int64_t row = group; row < a.T; row += a.parts) {
+  for (int64_t row = group; row < a.T; row += step) {
     const float mean = next_mean, rstd = next_rstd;
     float h[NV][8], g[NV][8], s[2] = {0.f, 0.f};
 #pragma unroll
@@ -200,7 +202,7 @@ __global__ __launch_bounds__(256) void norm_backward(NormArgs a) {
       f8_unpack8<F32>(rx[j], past, ragged, h[j]);
       f8_unpack8<F32>(ry[j], past, ragged, g[j]);
     }
-    ask(row + a.parts);
+    ask(row + step);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -222,14 +224,33 @@ __global__ __launch_bounds__(256) void norm_backward(NormArgs a) {
       if (c < a.D) f8_store8<F32>((void*)row_of<F32>(a.dX, row, a.ld_dx), c, a.D - c, g[j]);
     }
   }
-  if (group >= a.parts) return;
+  float *to_w = a.parts == 1 ? a.dweight : a.part + (int64_t)blockIdx.x * 2 * a.D, *to_b = a.parts == 1 ? a.dbias : a.part + ((int64_t)blockIdx.x * 2 + 1) * a.D;
+  if constexpr (kGroups == 1) {
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int c = (tid + j * ROWT) * 8;
-    if (c >= a.D) continue;
-    float *to_w = a.parts == 1 ? a.dweight : a.part + (int64_t)group * 2 * a.D, *to_b = a.parts == 1 ? a.dbias : a.part + ((int64_t)group * 2 + 1) * a.D;
-    if (to_w) f8_store8<true>(to_w, c, a.D - c, dw[j]);
-    if (to_b) f8_store8<true>(to_b, c, a.D - c, db[j]);
+    for (int j = 0; j < NV; ++j) {
+      const int c = (tid + j * ROWT) * 8;
+      if (c >= a.D) continue;
+      if (to_w) f8_store8<true>(to_w, c, a.D - c, dw[j]);
+      if (to_b) f8_store8<true>(to_b, c, a.D - c, db[j]);
+    }
+  } else {  // the groups' sums, in their order
+    constexpr int kWide = ROWT * NV * 8;
+    __shared__ float sums[2][kGroups][kWide];
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        sums[0][in_group][(tid + j * ROWT) * 8 + k] = dw[j][k];
+        sums[1][in_group][(tid + j * ROWT) * 8 + k] = db[j][k];
+      }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.D; c += 256) {
+      float w = 0.f, b = 0.f;
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) w += sums[0][g][c], b += sums[1][g][c];
+      if (to_w) to_w[c] = w;
+      if (to_b) to_b[c] = b;
+    }
   }
 }
 
@@ -303,8 +324,10 @@ inline int launched() { return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ER
 
 template <bool F32, bool CODES>
 int forward(const NormArgs& a, hipStream_t st) {
-  const dim3 block(256), rows((unsigned)a.T), quads((unsigned)((a.T + 3) / 4));
+  const dim3 block(256), rows((unsigned)a.T), quads((unsigned)(((int64_t)a.T + 3) / 4)), sixteens((unsigned)(((int64_t)a.T + 15) / 16));
   if (a.D < 8 || a.Dp > 16384) hipLaunchKernelGGL((norm_forward<F32, CODES, 256, 0>), rows, block, 0, st, a);
+  else if (a.Dp <= 128) hipLaunchKernelGGL((norm_forward<F32, CODES, 16, 1>), sixteens, block, 0, st, a);
+  else if (a.Dp <= 256) hipLaunchKernelGGL((norm_forward<F32, CODES, 16, 2>), sixteens, block, 0, st, a);
   else if (a.Dp <= 512) hipLaunchKernelGGL((norm_forward<F32, CODES, 64, 1>), quads, block, 0, st, a);
   else if (a.Dp <= 1024) hipLaunchKernelGGL((norm_forward<F32, CODES, 64, 2>), quads, block, 0, st, a);
   else if (a.Dp <= 2048) hipLaunchKernelGGL((norm_forward<F32, CODES, 256, 1>), rows, block, 0, st, a);
@@ -314,10 +337,15 @@ int forward(const NormArgs& a, hipStream_t st) {
   return launched();
 }
 
+// rows that a workgroup of the backward pass has in work at one time
+int rows_at_once(int D) { return D < 8 || D > 512 ? 1 : D <= 256 ? 16 : 4; }
+
 template <bool F32>
 int backward(const NormArgs& a, hipStream_t st) {
-  const dim3 block(256), parts((unsigned)a.parts), quads((unsigned)((a.parts + 3) / 4));
-  if (a.D >= 8 && a.D <= 512) hipLaunchKernelGGL((norm_backward<F32, 64, 1>), quads, block, 0, st, a);
+  const dim3 block(256), parts((unsigned)a.parts);
+  if (a.D >= 8 && a.D <= 128) hipLaunchKernelGGL((norm_backward<F32, 16, 1>), parts, block, 0, st, a);
+  else if (a.D >= 8 && a.D <= 256) hipLaunchKernelGGL((norm_backward<F32, 16, 2>), parts, block, 0, st, a);
+  else if (a.D >= 8 && a.D <= 512) hipLaunchKernelGGL((norm_backward<F32, 64, 1>), parts, block, 0, st, a);
   else if (a.D >= 8 && a.D <= 2048) hipLaunchKernelGGL((norm_backward<F32, 256, 1>), parts, block, 0, st, a);
   else if (a.D >= 8 && a.D <= 4096) hipLaunchKernelGGL((norm_backward<F32, 256, 2>), parts, block, 0, st, a);
   else if (a.D >= 8 && a.D <= 8192) hipLaunchKernelGGL((norm_backward<F32, 256, 4>), parts, block, 0, st, a);
@@ -336,8 +364,11 @@ int sum(const float* part, int parts, int64_t width, int64_t split_at, float* ou
 
 }  // namespace
 
-// Up to eight rows one workgroup takes them all, and its sums are the result: a launch less than eight that each take one.
-int norm_parts(int T) { return T <= 8 ? 1 : T < 512 ? T : 512; }
+// Workgroups that share the rows.  Where one is done with all of them in eight turns its sums are the result: a launch less.
+int norm_parts(int T, int D) {
+  const int64_t turns = ((int64_t)T + rows_at_once(D) - 1) / rows_at_once(D);
+  return turns <= 8 ? 1 : turns < 512 ? (int)turns : 512;
+}
 
 int norm_launch_forward(const void* X, bool f32, int64_t ldx, int T, int D, const float* weight, const float* bias, float eps,
                         void* Y, int64_t ldy, int code, uint8_t* codes, uint8_t* scale, float* mean, float* rstd, hipStream_t st) {
@@ -352,7 +383,7 @@ int norm_launch_backward(const void* dY, int64_t ld_dy, const void* X, int64_t l
                          int T, int D, void* dX, int64_t ld_dx, float* dweight, float* dbias, float* part, hipStream_t st) {
   NormArgs a{};
   a.X = X, a.dY = dY, a.weight = weight, a.dX = dX, a.mean = (float*)mean, a.rstd = (float*)rstd, a.part = part, a.dweight = dweight, a.dbias = dbias;
-  a.ldx = ldx, a.ld_dy = ld_dy, a.ld_dx = ld_dx, a.T = T, a.D = D, a.parts = norm_parts(T);
+  a.ldx = ldx, a.ld_dy = ld_dy, a.ld_dx = ld_dx, a.T = T, a.D = D, a.parts = norm_parts(T, D);
   const int rc = f32 ? backward<true>(a, st) : backward<false>(a, st);
   if (rc != BSP_OK || a.parts == 1) return rc;
   return sum(part, a.parts, 2 * (int64_t)D, D, dweight, dbias, st);

@@ -128,11 +128,11 @@ def test_norm_refusals(want, args):
 
 
 @pytest.mark.parametrize("want,args", [
-    (DTYPE, dict(dt=b.BSP_I8)), (SHAPE, dict(D=0)), (SHAPE, dict(ld=383)), (NULL, dict(X=None)), (NULL, dict(mean=None)), (CAPACITY, dict(n=9 * 2 * 384 * 4 - 1)),
+    (DTYPE, dict(dt=b.BSP_I8)), (SHAPE, dict(D=0)), (SHAPE, dict(ld=383)), (NULL, dict(X=None)), (NULL, dict(mean=None)), (CAPACITY, dict(n=15 * 2 * 384 * 4 - 1)),
     (NULL, dict(ws=None)), (ALIGN, dict(ws=P + 4)), (ALIGN, dict(X=P + 1)),
 ])
 def test_norm_gradient_refusals(want, args):
-    a = {**dict(X=P, dt=b.BSP_F32, ld=384, T=9, D=384, mean=P, ws=P, n=9 * 2 * 384 * 4), **args}
+    a = {**dict(X=P, dt=b.BSP_F32, ld=384, T=60, D=384, mean=P, ws=P, n=15 * 2 * 384 * 4), **args}
     assert bsp.load_library().bsp_layer_norm_grad(P, a["ld"], a["X"], a["ld"], a["dt"], a["T"], a["D"], a["mean"], P, None, P, 384, P, P, a["ws"], a["n"],
                                                   None) == want
 

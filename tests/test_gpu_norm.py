@@ -41,7 +41,7 @@ def _check(x, w, b, dtype, eps, y, mean, rstd):
 
 
 SHAPES = [(1, 1), (1, 7), (3, 64), (5, 127), (2, 128), (9, 512), (4, 520), (6, 1000), (3, 1024), (4, 1032), (7, 2048), (3, 2050), (5, 4096), (2, 4104), (3, 8192),
-          (2, 8200), (2, 16384), (2, 16392), (1, 30001), (1021, 260), (700, 1000), (513, 4096)]
+          (2, 8200), (2, 16384), (2, 16392), (1, 30001), (1021, 260), (700, 1000), (513, 4096), (3000, 96), (9000, 130), (8300, 8), (2500, 300), (130, 129), (129, 256), (33, 384)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
