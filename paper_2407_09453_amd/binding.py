@@ -154,8 +154,8 @@ def load_library():
     cp, fp, pi64 = ctypes.POINTER(bsp_codes), ctypes.POINTER(bsp_weights_f8), ctypes.POINTER(i64)
     for name, args in (("bsp_f8_save", [vp, i32, i64, cp, vp]), ("bsp_f8_load", [cp, vp, i32, i64, vp]),
                        ("bsp_f8_count", [vp, i32, i32, pi64]), ("bsp_f8_index", [vp, i32, i32, i64, vp, vp, vp, vp]),
-                       ("bsp_f8_pack", [fp, vp, i32, i64, vp]), ("bsp_f8_fc", [fp, i32, cp, vp, vp, i32, cp, vp, i32, vp]),
-                       ("bsp_f8_fc_workspace", [fp, i32, i32, pi64]),
+                       ("bsp_f8_pack", [fp, vp, i32, i64, vp]), ("bsp_f8_fc", [fp, i32, cp, vp, vp, i32, cp, vp, i32, vp, i64, vp]),
+                       ("bsp_f8_fc_workspace", [fp, i32, i32, i32, pi64]),
                        ("bsp_f8_fc_values", [fp, i32, vp, i32, i64, i32, i32, vp, vp, i32, cp, vp, i32, vp, i64, vp]),
                        ("bsp_f8_fc_grad_workspace", [fp, i32, pi64]),
                        ("bsp_f8_fc_grad", [fp, vp, i64, cp, vp, vp, vp, i64, vp]),

@@ -274,9 +274,13 @@ struct F8Input {      // rows to multiply: codes with their scales, or values br
 // no more than kFewStaged bytes.
 enum { kFewStaged = 72 * 1024 };
 inline int64_t f8_few_staged(int T, int K) { return (int64_t)T * (f8_blocks(K) * (F8_BLOCK + 1) + 16); }
-int f8_launch_few(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, hipStream_t st);
+// `part`, here and below: [split][T][4 ceil(out / 4)] floats where *_split says more than one, to be joined
+int f8_few_split(const F8Rows& w, int T);
+int f8_launch_few(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, float* part, hipStream_t st);
 // many rows, codes only
-int f8_launch_tile(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, hipStream_t st);
+int f8_tile_split(const F8Rows& w, int T);
+int f8_launch_tile(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, float* part, hipStream_t st);
+int f8_launch_join(const float* part, int split, int T, int O, const F8Epilogue& q, bool f32, hipStream_t st);
 int f8_launch_save(const void* X, int x_f32, int64_t ldx, int T, int K, bool e5, uint8_t* codes, uint8_t* scale, hipStream_t st);
 int f8_launch_load(const uint8_t* codes, const uint8_t* scale, int T, int K, bool e5, void* Y, int y_f32, int64_t ldy, hipStream_t st);
 int f8_launch_pack(const bsp_weights_f8* w, const void* W, int w_f32, int64_t ldw, hipStream_t st);

@@ -72,9 +72,25 @@ int check_product(const bsp_weights_f8* w, int32_t transposed, int32_t T, const 
   return BSP_OK;
 }
 
-int multiply(const bsp_weights_f8* w, int32_t transposed, const F8Input& x, int T, const F8Epilogue& q, int32_t y_dtype, hipStream_t st) {
-  const F8Rows rows = rows_of(w, transposed != 0);
-  return T <= kFewRows ? f8_launch_few(rows, x, T, q, y_dtype == BSP_F32, st) : f8_launch_tile(rows, x, T, q, y_dtype == BSP_F32, st);
+int split_of(const F8Rows& rows, int T) { return T <= kFewRows ? f8_few_split(rows, T) : f8_tile_split(rows, T); }
+
+int64_t sums_bytes(const F8Rows& rows, int T) {
+  const int64_t split = T > 0 ? split_of(rows, T) : 1;
+  return split > 1 ? split * T * ((rows.out + 3) / 4) * 16 : 0;
+}
+
+int multiply(const F8Rows& rows, const F8Input& x, int T, const F8Epilogue& q, int32_t y_dtype, void* sums, hipStream_t st) {
+  const bool f32 = y_dtype == BSP_F32;
+  const int rc = T <= kFewRows ? f8_launch_few(rows, x, T, q, f32, (float*)sums, st) : f8_launch_tile(rows, x, T, q, f32, (float*)sums, st);
+  if (rc != BSP_OK) return rc;
+  const int split = split_of(rows, T);
+  return split > 1 ? f8_launch_join((const float*)sums, split, T, rows.out, q, f32, st) : BSP_OK;
+}
+
+int check_workspace(const void* workspace, int64_t bytes, int64_t need) {
+  if (bytes < need) return BSP_ERR_CAPACITY;
+  if (need > 0 && !workspace) return BSP_ERR_NULL;
+  return aligned(workspace, 16) ? BSP_OK : BSP_ERR_ALIGN;
 }
 
 int64_t codes_bytes(int T, int K) { return ((int64_t)T * f8_blocks(K) * F8_BLOCK) + f8_scale_rows(T) * f8_blocks(K); }
@@ -108,7 +124,7 @@ int bsp_f8_pack(const bsp_weights_f8* w, const void* W, int32_t w_dtype, int64_t
 }
 
 int bsp_f8_fc(const bsp_weights_f8* w, int32_t transposed, const bsp_codes* X, const float* bias, const void* residual,
-              int32_t relu, const bsp_codes* gate, void* Y, int32_t y_dtype, void* stream) {
+              int32_t relu, const bsp_codes* gate, void* Y, int32_t y_dtype, void* workspace, int64_t workspace_bytes, void* stream) {
   int rc = check_codes(X);
   if (rc != BSP_OK) return rc;
   F8Epilogue q;
@@ -117,15 +133,17 @@ int bsp_f8_fc(const bsp_weights_f8* w, int32_t transposed, const bsp_codes* X, c
   if (X->K != (transposed ? w->O : w->I)) return BSP_ERR_SHAPE;
   if (X->T == 0) return BSP_OK;
   const F8Input x{X->codes, X->scale, X->dtype, X->dtype == BSP_E5M2, (int64_t)f8_blocks(X->K) * F8_BLOCK};
-  return multiply(w, transposed, x, X->T, q, y_dtype, (hipStream_t)stream);
+  const F8Rows rows = rows_of(w, transposed != 0);
+  rc = check_workspace(workspace, workspace_bytes, sums_bytes(rows, X->T));
+  return rc != BSP_OK ? rc : multiply(rows, x, X->T, q, y_dtype, workspace, (hipStream_t)stream);
 }
 
-int bsp_f8_fc_workspace(const bsp_weights_f8* w, int32_t transposed, int32_t T, int64_t* bytes) {
+int bsp_f8_fc_workspace(const bsp_weights_f8* w, int32_t transposed, int32_t T, int32_t coded, int64_t* bytes) {
   if (!bytes) return BSP_ERR_NULL;
   const int rc = check_weights(w);
   if (rc != BSP_OK) return rc;
   if (T < 0 || T > kMost) return BSP_ERR_SHAPE;
-  *bytes = codes_bytes(T, transposed ? w->O : w->I);
+  *bytes = sums_bytes(rows_of(w, transposed != 0), T) + (coded ? 0 : codes_bytes(T, transposed ? w->O : w->I));
   return BSP_OK;
 }
 
@@ -141,15 +159,17 @@ int bsp_f8_fc_values(const bsp_weights_f8* w, int32_t transposed, const void* X,
   if (rc != BSP_OK || T == 0) return rc;
   const bool e5 = code == BSP_E5M2;
   hipStream_t st = (hipStream_t)stream;
-  if (in_kernel(X, x_dtype, ldx, T, K)) return multiply(w, transposed, F8Input{X, nullptr, x_dtype, e5, ldx}, T, q, y_dtype, st);
-  if (workspace_bytes < codes_bytes(T, K)) return BSP_ERR_CAPACITY;
-  if (!workspace) return BSP_ERR_NULL;
-  if (!aligned(workspace, 16)) return BSP_ERR_ALIGN;
+  const F8Rows rows = rows_of(w, transposed != 0);
+  const int64_t sums = sums_bytes(rows, T);
+  const bool inside = in_kernel(X, x_dtype, ldx, T, K);
+  rc = check_workspace(workspace, workspace_bytes, sums + (inside ? 0 : codes_bytes(T, K)));
+  if (rc != BSP_OK) return rc;
+  if (inside) return multiply(rows, F8Input{X, nullptr, x_dtype, e5, ldx}, T, q, y_dtype, workspace, st);
   const int64_t ld = (int64_t)f8_blocks(K) * F8_BLOCK;
-  uint8_t *codes = (uint8_t*)workspace, *scale = codes + T * ld;
+  uint8_t *codes = (uint8_t*)workspace + sums, *scale = codes + T * ld;
   rc = f8_launch_save(X, x_dtype == BSP_F32, ldx, T, K, e5, codes, scale, st);
   if (rc != BSP_OK) return rc;
-  return multiply(w, transposed, F8Input{codes, scale, code, e5, ld}, T, q, y_dtype, st);
+  return multiply(rows, F8Input{codes, scale, code, e5, ld}, T, q, y_dtype, workspace, st);
 }
 
 int bsp_f8_fc_grad_workspace(const bsp_weights_f8* w, int32_t T, int64_t* bytes) {
@@ -251,7 +271,7 @@ int bsp_f8_call_packed(int32_t call, const int64_t* w) {
     }
     case BSP_F8_CALL_FC: {
       const bsp_codes x = codes(2), g = codes(10);
-      return bsp_f8_fc((const bsp_weights_f8*)ptr(0), num(1), &x, (const float*)ptr(7), ptr(8), num(9), none(10) ? nullptr : &g, ptr(15), num(16), ptr(17));
+      return bsp_f8_fc((const bsp_weights_f8*)ptr(0), num(1), &x, (const float*)ptr(7), ptr(8), num(9), none(10) ? nullptr : &g, ptr(15), num(16), ptr(17), w[18], ptr(19));
     }
     case BSP_F8_CALL_VALUES: {
       const bsp_codes g = codes(10);

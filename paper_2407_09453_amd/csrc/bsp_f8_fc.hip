@@ -18,6 +18,8 @@ struct TileArgs {
   F8Epilogue q;
   int64_t ld, srows;
   int32_t T, tiles_t, tiles_o;
+  float* part;  // split > 1: sums of each share of the block columns, [split][T][4 ceil(out / 4)], instead of results
+  int32_t split;
 };
 
 __device__ __forceinline__ i32x8_t read_fragment(const uint8_t* p, int at0, int at1) {
@@ -240,11 +242,19 @@ __global__ __launch_bounds__(64 * WO * WT) void f8_wide(TileArgs a) {
   kernarg_touch<TileArgs>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wo = wave / WT, wt = wave % WT;
+  // a share of the block columns, and the tile
+  constexpr bool kSplits = MO * MT <= 4;
+  const int tiles = a.tiles_o * a.tiles_t, share = kSplits ? (int)blockIdx.x / tiles : 0;
   int tile_o, tile_t;
-  place_tile(blockIdx.x, a.tiles_o, a.tiles_t, &tile_o, &tile_t);
+  place_tile((int)blockIdx.x - share * tiles, a.tiles_o, a.tiles_t, &tile_o, &tile_t);
   const int br = tile_o * K::R;
   const int64_t t0 = (int64_t)tile_t * K::NT;
-  const int n0 = __builtin_amdgcn_readfirstlane(a.w.ptr[br]), cnt = __builtin_amdgcn_readfirstlane(a.w.ptr[br + 1]) - n0;
+  int n0 = __builtin_amdgcn_readfirstlane(a.w.ptr[br]), cnt = __builtin_amdgcn_readfirstlane(a.w.ptr[br + 1]) - n0;
+  if constexpr (kSplits) {
+    const int from = (int)((int64_t)cnt * share / a.split), to = (int)((int64_t)cnt * (share + 1) / a.split);
+    n0 += from;
+    cnt = to - from;
+  }
   const int last = (int)(a.T - 1 - t0 < K::NT - 1 ? a.T - 1 - t0 : K::NT - 1);  // rows past the last: its bytes, their results go nowhere
 
   K k;
@@ -322,7 +332,27 @@ __global__ __launch_bounds__(64 * WO * WT) void f8_wide(TileArgs a) {
     rest(std::integral_constant<int, 0>{});
   }
   __syncthreads();
+  if constexpr (kSplits) {
+    if (a.split > 1) {
+      const int ld = (a.w.out + 3) & ~3;
+      const F8Epilogue sums{a.part + (int64_t)share * a.T * ld, nullptr, nullptr, nullptr, 0, 0, 1, 0};
+      store_tile<MO, MT, true>(sums, acc, lds + wave * kStoreBytes<MO>, a.T, ld, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32);
+      return;
+    }
+  }
   store_tile<MO, MT, F32>(a.q, acc, lds + wave * kStoreBytes<MO>, a.T, a.w.out, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32);
+}
+
+// The shares' sums, in their order, and what follows a product: a thread takes four channels of a row.
+template <bool F32>
+__global__ __launch_bounds__(256) void f8_join(const float* part, int split, int T, int O, F8Epilogue q) {
+  const int quads = (O + 3) >> 2;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, t = i / quads, rows = (int64_t)T * quads;
+  if (i >= rows) return;
+  f32x4_t s = {};
+#pragma unroll 8
+  for (int k = 0; k < split; ++k) s += *(const f32x4_t*)(part + (k * rows + i) * 4);
+  f8_store4<F32>(q, t, (int)(i - t * quads) * 4, O, s[0], s[1], s[2], s[3]);
 }
 
 template <int NO, int NT>
@@ -330,8 +360,8 @@ int launch(void (*kernel)(TileArgs), bool raised, int threads, int lds, TileArgs
   if (!raised) return BSP_ERR_HIP;
   a.tiles_o = (a.w.out + NO - 1) / NO;
   a.tiles_t = (int)(((int64_t)a.T + NT - 1) / NT);
-  if ((int64_t)a.tiles_o * a.tiles_t > INT32_MAX / 8) return BSP_ERR_SHAPE;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(a.tiles_o * a.tiles_t)), dim3(threads), lds, st, a);
+  if ((int64_t)a.tiles_o * a.tiles_t * a.split > INT32_MAX / 8) return BSP_ERR_SHAPE;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(a.tiles_o * a.tiles_t * a.split)), dim3(threads), lds, st, a);
   return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP;
 }
 bool raise(const void* kernel, int lds) { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess; }
@@ -354,25 +384,32 @@ struct Tile {
 };
 constexpr Tile kTiles[] = {{256, 256, 1, 1.15, 1.15, 2500}, {128, 256, 1, 0.75, 0.75, 2150}, {128, 128, 2, 0.40, 0.85, 2200}, {128, 64, 2, 0.25, 0.50, 1700}, {128, 32, 1, 0.18, 0.18, 1000}};
 
-int pick_tile(int O, int64_t nnzb, int T, bool full) {
+struct Plan {
+  int tile, split;
+};
+// Where tiles are too few for the chip the block columns are cut into shares, of at least four steps each, whose sums a second launch joins: that
+// costs it 3 us and the memory's time (us, one share and as planned: 243 x 18816 -> 384 , 256 x 16384 -> 1024 ).
+Plan plan_of(int O, int64_t nnzb, int T, bool full) {
   const double steps = (double)nnzb / f8_blocks(O);
-  int best = 2;
+  Plan best{2, 1};
   double least = 1e30;
   for (int k = full && f8_blocks(O) % 2 == 0 ? 0 : 1; k < 5; ++k) {
     const Tile& v = kTiles[k];
     const double groups = (double)((f8_blocks(O) * F8_BLOCK + v.o - 1) / v.o) * (double)(((int64_t)T + v.t - 1) / v.t);
-    const double rounds = groups <= 256 ? v.alone : v.shared * (double)(int64_t)((groups + 256 * v.fit - 1) / (256 * v.fit));
-    const double us = rounds * steps, at_rate = groups * steps * v.o * v.t * 256e-6 / v.rate;
-    const double worse = us > at_rate ? us : at_rate;
-    if (worse < least) least = worse, best = k;
+    for (int split = 1; split == 1 || (k >= 2 && groups * split <= 256 && steps >= 4.0 * split && split <= 64); split *= 2) {
+      const double all = groups * split;
+      const double rounds = all <= 256 ? v.alone : v.shared * (double)(int64_t)((all + 256 * v.fit - 1) / (256 * v.fit));
+      const double us = rounds * steps / split, at_rate = groups * steps * v.o * v.t * 256e-6 / v.rate;
+      const double join = split > 1 ? 3.0 + (double)T * O * 4 * 2 * split / 3e6 : 0;
+      const double worse = (us > at_rate ? us : at_rate) + join;
+      if (worse < least) least = worse, best = Plan{k, split};
+    }
   }
   return best;
 }
 
 template <bool E5>
-int launch_any(const TileArgs& a, bool f32, hipStream_t st) {
-  const bool full = a.w.nnzb == (int64_t)f8_blocks(a.w.out) * f8_blocks(a.w.in);
-  const int k = pick_tile(a.w.out, a.w.nnzb, a.T, full);
+int launch_any(const TileArgs& a, int k, bool f32, hipStream_t st) {
   if (f32) {
     switch (k) {
       case 3: return launch_wide<2, 1, 2, 2, 3, E5, true>(a, st);
@@ -391,7 +428,20 @@ int launch_any(const TileArgs& a, bool f32, hipStream_t st) {
 
 }  // namespace
 
-int f8_launch_tile(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, hipStream_t st) {
-  TileArgs a{w, (const uint8_t*)x.X, x.scale, q, x.ld, f8_scale_rows(T), T, 0, 0};
-  return x.e5 ? launch_any<true>(a, f32, st) : launch_any<false>(a, f32, st);
+int f8_tile_split(const F8Rows& w, int T) {
+  return plan_of(w.out, w.nnzb, T, w.nnzb == (int64_t)f8_blocks(w.out) * f8_blocks(w.in)).split;
+}
+
+int f8_launch_tile(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, float* part, hipStream_t st) {
+  const Plan plan = plan_of(w.out, w.nnzb, T, w.nnzb == (int64_t)f8_blocks(w.out) * f8_blocks(w.in));
+  TileArgs a{w, (const uint8_t*)x.X, x.scale, q, x.ld, f8_scale_rows(T), T, 0, 0, part, plan.split};
+  return x.e5 ? launch_any<true>(a, plan.tile, f32, st) : launch_any<false>(a, plan.tile, f32, st);
+}
+
+int f8_launch_join(const float* part, int split, int T, int O, const F8Epilogue& q, bool f32, hipStream_t st) {
+  const int64_t groups = ((int64_t)T * ((O + 3) / 4) + 255) / 256;
+  if (groups > INT32_MAX) return BSP_ERR_SHAPE;
+  if (f32) hipLaunchKernelGGL(f8_join<true>, dim3((unsigned)groups), dim3(256), 0, st, part, split, T, O, q);
+  else hipLaunchKernelGGL(f8_join<false>, dim3((unsigned)groups), dim3(256), 0, st, part, split, T, O, q);
+  return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP;
 }

@@ -19,6 +19,8 @@ struct FewArgs {
   int64_t srows;   // rows of x.scale
   int32_t T, rows;  // rows: how many become codes in LDS
   int32_t full;    // blocks in a block row, where all are kept; else 0
+  int32_t split;
+  float* part;     // split > 1: sums of each share of the block columns, as f8_join reads them
 };
 
 // 128 products per lane row: scaled codes, or (F32) both sides as bf16 so that nothing is lost in the sum.  The instruction on
@@ -85,8 +87,10 @@ __global__ __launch_bounds__((64 * kMostWaves<MT>)) void f8_few(FewArgs a) {
   const int r = lane & 15, g = lane >> 4;
   const int br = blockIdx.x >> 3;
   // (where all blocks are kept their places need not be read)
-  const int n0 = a.full ? br * a.full : __builtin_amdgcn_readfirstlane(a.w.ptr[br]);
-  const int cnt = a.full ? a.full : __builtin_amdgcn_readfirstlane(a.w.ptr[br + 1]) - n0;
+  const int row0 = a.full ? br * a.full : __builtin_amdgcn_readfirstlane(a.w.ptr[br]);
+  const int row_cnt = a.full ? a.full : __builtin_amdgcn_readfirstlane(a.w.ptr[br + 1]) - row0;
+  const int first = (int)((int64_t)row_cnt * blockIdx.z / a.split), n0 = row0 + first;
+  const int cnt = (int)((int64_t)row_cnt * (blockIdx.z + 1) / a.split) - first;
   const int mine = cnt > wave ? (cnt - wave + waves - 1) / waves : 0;
   const uint8_t* wp = a.w.payload + (int64_t)n0 * F8_BLOCK_BYTES + ((blockIdx.x & 7) * 16 + r) * F8_BLOCK + g * 16;
   const int64_t t0 = (int64_t)blockIdx.y * (16 * MT);
@@ -113,7 +117,7 @@ __global__ __launch_bounds__((64 * kMostWaves<MT>)) void f8_few(FewArgs a) {
   f32x4_t acc[MT] = {};
   for (int c = 0; c < mine || c == 0; c += 64) {  // the wave's block columns, 64 at a time, one a lane
     const int of = wave + (c + lane) * waves < cnt ? wave + (c + lane) * waves : cnt - 1;
-    const int cols = a.full ? of : cnt > 0 ? a.w.idx[n0 + of] : 0;
+    const int cols = a.full ? first + of : cnt > 0 ? a.w.idx[n0 + of] : 0;
     const int end = mine - c < 64 ? mine - c : 64;
     auto rows = [&](int j) {
 #pragma unroll
@@ -175,18 +179,20 @@ __global__ __launch_bounds__((64 * kMostWaves<MT>)) void f8_few(FewArgs a) {
     for (int w = 1; w < waves; ++w) s += *(const f32x4_t*)(sums + (w * MT * 64 + i) * 4);
     const int64_t row = t0 + (i >> 6) * 16 + (i & 15);
     const int o = blockIdx.x * 16 + ((i >> 4) & 3) * 4;
-    if (row < a.T && o < a.w.out) f8_store4<F32>(a.q, row, o, a.w.out, s[0], s[1], s[2], s[3]);
+    if (row >= a.T || o >= a.w.out) continue;
+    if (a.split > 1) *(f32x4_t*)(a.part + (((int64_t)blockIdx.z * a.T + row) * ((a.w.out + 3) >> 2) + (o >> 2)) * 4) = s;
+    else f8_store4<F32>(a.q, row, o, a.w.out, s[0], s[1], s[2], s[3]);
   }
 }
 
 template <int MT, int SRC, bool E5, bool F32>
 int launch(FewArgs a, hipStream_t st) {
   const int strips = (a.w.out + 15) / 16, tiles = (a.T + 16 * MT - 1) / (16 * MT);
-  const int64_t per_row = (a.w.nnzb + f8_blocks(a.w.out) - 1) / f8_blocks(a.w.out);
+  const int64_t per_row = (a.w.nnzb + (int64_t)f8_blocks(a.w.out) * a.split - 1) / ((int64_t)f8_blocks(a.w.out) * a.split);
   // as many waves as a CU holds, on every CU; a wave for every block is enough
   constexpr int most = kMostWaves<MT>;
   int waves = 1;
-  while (waves < most && waves < per_row && (waves < 2 || (int64_t)strips * tiles * waves < 256 * most)) waves *= 2;
+  while (waves < most && waves < per_row && (waves < 2 || (int64_t)strips * tiles * a.split * waves < 256 * most)) waves *= 2;
   int lds = waves * MT * 1024;
   if constexpr (SRC != kCodes) {
     a.rows = a.T;
@@ -194,7 +200,7 @@ int launch(FewArgs a, hipStream_t st) {
     static const bool raised = hipFuncSetAttribute((const void*)&f8_few<MT, SRC, E5, F32>, hipFuncAttributeMaxDynamicSharedMemorySize, kFewStaged + 16 * 1024 + 16) == hipSuccess;
     if (!raised) return BSP_ERR_HIP;
   }
-  hipLaunchKernelGGL((f8_few<MT, SRC, E5, F32>), dim3((unsigned)strips, (unsigned)tiles), dim3((unsigned)(64 * waves)), (size_t)lds, st, a);
+  hipLaunchKernelGGL((f8_few<MT, SRC, E5, F32>), dim3((unsigned)strips, (unsigned)tiles, (unsigned)a.split), dim3((unsigned)(64 * waves)), (size_t)lds, st, a);
   return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP;
 }
 
@@ -208,8 +214,17 @@ int launch_rows(const FewArgs& a, hipStream_t st) {
 
 }  // namespace
 
-int f8_launch_few(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, hipStream_t st) {
-  FewArgs a{w, x, q, f8_scale_rows(T), T, 0, 0};
+// Where a workgroup's sixteen waves would each have six blocks or more and many CUs have none, shares of two blocks a wave whose sums a second launch joins.
+int f8_few_split(const F8Rows& w, int T) {
+  const int64_t groups = (int64_t)((w.out + 15) / 16) * ((T + 31) / 32), row = w.nnzb / f8_blocks(w.out);
+  int split = 1;
+  if (row >= 6 * 16)
+    while (groups * split * 2 <= 256 && row >= 2 * 16 * split * 2) split *= 2;
+  return split;
+}
+
+int f8_launch_few(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, float* part, hipStream_t st) {
+  FewArgs a{w, x, q, f8_scale_rows(T), T, 0, 0, f8_few_split(w, T), part};
   if (w.nnzb == (int64_t)f8_blocks(w.out) * f8_blocks(w.in)) a.full = f8_blocks(w.in);
   if (f32) return x.e5 ? launch_rows<true, true>(a, st) : launch_rows<false, true>(a, st);
   return x.e5 ? launch_rows<true, false>(a, st) : launch_rows<false, false>(a, st);

@@ -181,7 +181,7 @@ class BspLayerF8:
             if kind == "grad":
                 _check(lib.bsp_f8_fc_grad_workspace(self.struct, T, n), "bsp_f8_fc_grad_workspace")
             else:
-                _check(lib.bsp_f8_fc_workspace(self.struct, kind, T, n), "bsp_f8_fc_workspace")
+                _check(lib.bsp_f8_fc_workspace(self.struct, kind >> 1, T, kind & 1, n), "bsp_f8_fc_workspace")
             if len(self._workspace) > 4096:
                 self._workspace.clear()
             n = self._workspace[(kind, T)] = n.value
@@ -207,17 +207,16 @@ class BspLayerF8:
         st = _current_stream(out) if stream is None else stream
         rest = (0 if bias is None else bias.data_ptr(), 0 if residual is None else residual.data_ptr(), 1 if relu else 0,
                 *(_NO_CODES if gate is None else gate.words), out.data_ptr(), _type(out))
+        if not codes:  # (few whole rows become codes inside the product's kernel)
+            x, size = X.data_ptr(), X.element_size()
+            inside = T <= 16 and not (x | ld * size | K * size) & 15 and T * (_blocks(K) * 129 + 16) <= 73728
+        n = self._bytes(transposed * 2 + (codes or inside), T)
+        ws = torch.empty(n, dtype=torch.uint8, device=out.device) if n else None
+        rest += (0 if ws is None else ws.data_ptr(), n, st)
         if codes:
-            _call(_FC, _pack18(self._address, transposed, *X.words, *rest, st), "bsp_f8_fc")
-            return out
-        x, size = X.data_ptr(), X.element_size()
-        ws, n = None, 0
-        # (few whole rows become codes inside the product's kernel)
-        if T > 16 or T * (_blocks(K) * 129 + 16) > 73728 or (x | ld * size | K * size) & 15:
-            n = self._bytes(transposed, T)
-            ws = torch.empty(n, dtype=torch.uint8, device=out.device)
-        _call(_VALUES, _pack20(self._address, transposed, x, _type(X), ld, T, CODES[code], *rest, 0 if ws is None else ws.data_ptr(), n, st),
-              "bsp_f8_fc_values")
+            _call(_FC, _pack20(self._address, transposed, *X.words, *rest), "bsp_f8_fc")
+        else:
+            _call(_VALUES, _pack20(self._address, transposed, x, _type(X), ld, T, CODES[code], *rest), "bsp_f8_fc_values")
         _keep(ws, stream)
         return out
 

@@ -80,12 +80,14 @@ def test_load_refuses_overlapping_rows():
     (NULL, dict(w=_weights(payload=None))), (NULL, dict(w=_weights(col_ptr=None))), (ALIGN, dict(w=_weights(payload_t=P + 8))),
     (SHAPE, dict(X=_codes(K=256))), (SHAPE, dict(t=1)), (DTYPE, dict(X=_codes(dtype=b.BSP_F32))), (NULL, dict(Y=None)), (ALIGN, dict(Y=P + 2)),
     (ALIGN, dict(r=P + 2)), (ALIGN, dict(bias=P + 2)), (DTYPE, dict(dt=b.BSP_I32)), (SHAPE, dict(gate=_codes(T=9, K=256))), (SHAPE, dict(gate=_codes(K=384))),
-    (NULL, dict(gate=_codes(K=256, codes=None))), (OK, dict(X=_codes(T=0, codes=None, scale=None), Y=None)),
+    (NULL, dict(gate=_codes(K=256, codes=None))), (ALIGN, dict(ws=P + 8)),
+    (CAPACITY, dict(w=_weights(I=16384, nnzb=256), X=_codes(K=16384), ws=P, n=15)), (NULL, dict(w=_weights(I=16384, nnzb=256), X=_codes(K=16384), n=1 << 30)), (OK, dict(X=_codes(T=0, codes=None, scale=None), Y=None)),
 ])
 def test_product_refusals(want, args):
-    a = {**dict(w=_weights(), t=0, X=_codes(), bias=None, r=None, gate=None, Y=P, dt=b.BSP_BF16), **args}
+    a = {**dict(w=_weights(), t=0, X=_codes(), bias=None, r=None, gate=None, Y=P, dt=b.BSP_BF16, ws=None, n=0), **args}
     ref = lambda s: None if s is None else ctypes.byref(s)  # noqa: E731
-    assert bsp.load_library().bsp_f8_fc(ref(a["w"]), a["t"], ref(a["X"]), a["bias"], a["r"], 0, ref(a["gate"]), a["Y"], a["dt"], None) == want
+    assert bsp.load_library().bsp_f8_fc(ref(a["w"]), a["t"], ref(a["X"]), a["bias"], a["r"], 0, ref(a["gate"]), a["Y"], a["dt"],
+                                           a["ws"], a["n"], None) == want
 
 
 @pytest.mark.parametrize("want,args", [
@@ -99,9 +101,10 @@ def test_values_refusals(want, args):
     assert lib.bsp_f8_fc_values(ctypes.byref(w), 0, a["X"], a["xdt"], a["ld"], a["T"], a["code"], None, None, 0, None, a["Y"], b.BSP_BF16,
                                 a["ws"], a["n"], None) == want
     n = ctypes.c_int64(-1)
-    assert lib.bsp_f8_fc_workspace(ctypes.byref(w), 0, 17, ctypes.byref(n)) == OK and n.value == 17 * 384 + 32 * 3
-    assert lib.bsp_f8_fc_workspace(ctypes.byref(w), 0, -1, ctypes.byref(n)) == SHAPE
-    assert lib.bsp_f8_fc_workspace(ctypes.byref(w), 0, 17, None) == NULL
+    assert lib.bsp_f8_fc_workspace(ctypes.byref(w), 0, 17, 0, ctypes.byref(n)) == OK and n.value == 17 * 384 + 32 * 3
+    assert lib.bsp_f8_fc_workspace(ctypes.byref(w), 0, -1, 0, ctypes.byref(n)) == SHAPE
+    assert lib.bsp_f8_fc_workspace(ctypes.byref(w), 0, 17, 0, None) == NULL
+    assert lib.bsp_f8_fc_workspace(ctypes.byref(w), 0, 17, 1, ctypes.byref(n)) == OK and n.value == 0
 
 
 @pytest.mark.parametrize("want,args", [

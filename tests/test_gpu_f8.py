@@ -128,6 +128,7 @@ def _bound(x, W, gamma, f32, ref, extra=0.0, code="e4m3", transposed=False):
     (1, 1, 1, 1.0), (1, 128, 16, 1.0), (1, 4096, 520, 0.5), (3, 300, 130, 1.0), (16, 2048, 1000, 0.5), (17, 129, 127, 1.0), (32, 1000, 1024, 0.6),
     (33, 512, 36, 1.0), (64, 640, 300, 0.5), (65, 640, 300, 0.5), (127, 256, 128, 1.0), (128, 1000, 257, 0.7), (129, 384, 513, 0.4), (197, 2048, 1000, 0.75),
     (300, 200, 264, 0.0), (513, 1152, 384, 1.0), (1000, 512, 770, 0.3), (700, 4096, 130, 1.0),
+    (1, 16500, 130, 1.0), (13, 16500, 35, 0.8), (30, 13000, 260, 0.9), (40, 5000, 133, 1.0), (243, 8200, 384, 0.6), (100, 9000, 70, 1.0),
 ])
 def test_product(T, I, O, density, dtype):
     rng = _rng(T, I, O)
