@@ -310,12 +310,23 @@ __global__ __launch_bounds__(256) void f8_grad_finish(F8GradArgs a) {
   a.dW[o * a.I + kb * F8_BLOCK + c] = n < 0 ? 0.f : sum(a.part + (int64_t)n * F8_BLOCK_BYTES + r * F8_BLOCK + c, a.nnzb * F8_BLOCK_BYTES);
 }
 
-// The largest number of kept blocks a workgroup, 4 at most, that still gives every CU one ...
-int blocks_each(int64_t nnzb, int nbo) {
-  const int64_t row = nnzb / nbo;
-  for (int c = 4; c > 1; c /= 2)
-    if (row >= c && nbo * ((row + c - 1) / c) >= 256) return c;
-  return 1;
+// Kept blocks a workgroup: more of them share a block row's gradients and take longer, so it goes by how often the chip is filled.  A CU holds two workgroups of
+// one block or one of more; us a step where it is full: 0.64, 0.55, 0.94 (843, 984, 1148 TFLOP/s on 8192 x 8192 -> 8192), and 6 a workgroup to begin and end
+// (us for one, two, four blocks: 8192 x 4096 -> 16384 1306 1179 1007, 2048 x 4096 -> 4096 88 86 76, half of it kept 62 74 66, 2048 x 4096 -> 4097 105 115 127).
+int blocks_each(const F8GradArgs& a) {
+  const double steps = (double)(((int64_t)a.T + kStep - 1) / kStep), row = (double)a.nnzb / a.nbo;
+  const bool full = a.nnzb == (int64_t)a.nbo * a.nbi;
+  int best = 1;
+  double least = 1e30;
+  for (int c = 1; c <= 4; c *= 2) {
+    // (of rows that keep differing numbers of blocks the last group is half full on average)
+    const double groups = a.nbo * (full ? (double)((a.nbi + c - 1) / c) : row / c + (c - 1) / (2.0 * c));
+    const double slots = c == 1 ? 512 : 256, rounds = (double)(int64_t)((groups + slots - 1) / slots);
+    const double step = c == 1 ? (groups <= 256 ? 0.32 : 0.64) : c == 2 ? 0.55 : 0.94;
+    const double us = rounds * (steps * step + 6);
+    if (us < least) least = us, best = c;
+  }
+  return best;
 }
 
 template <int C, bool E5, bool THIN = false>
@@ -342,7 +353,7 @@ int f8_grad_split(int64_t nnzb, int T) {
 int f8_launch_grad(const F8GradArgs& a, hipStream_t st) {
   int rc;
   if (a.O < 8) rc = a.e5 ? launch<1, true, true>(a, st) : launch<1, false, true>(a, st);
-  else switch (blocks_each(a.nnzb, a.nbo)) {
+  else switch (a.split > 1 ? 1 : blocks_each(a)) {
     case 4: rc = a.e5 ? launch<4, true>(a, st) : launch<4, false>(a, st); break;
     case 2: rc = a.e5 ? launch<2, true>(a, st) : launch<2, false>(a, st); break;
     default: rc = a.e5 ? launch<1, true>(a, st) : launch<1, false>(a, st);
