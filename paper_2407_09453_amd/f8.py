@@ -162,9 +162,11 @@ class BspLayerF8:
             self.d_bias = b
         self.update(W)
 
-    def update(self, W, stream=None) -> None:
-        """Take new weights (same shape, same mask), as after a step of an optimiser."""
+    def update(self, W, bias=None, stream=None) -> None:
+        """Take new weights (same shape, same mask), and a new bias where one is given, as after a step of an optimiser."""
         import torch
+        if bias is not None:
+            self.d_bias.copy_(torch.as_tensor(bias, dtype=torch.float32))
         if not isinstance(W, torch.Tensor):
             W = torch.from_numpy(np.ascontiguousarray(W, dtype=np.float32))
         W = W.to(self.device)
