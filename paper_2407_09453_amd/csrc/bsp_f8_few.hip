@@ -87,8 +87,9 @@ __global__ __launch_bounds__((64 * kMostWaves<MT>)) void f8_few(FewArgs a) {
   const int r = lane & 15, g = lane >> 4;
   const int br = blockIdx.x >> 3;
   // (where all blocks are kept their places need not be read)
-  const int row0 = a.full ? br * a.full : __builtin_amdgcn_readfirstlane(a.w.ptr[br]);
-  const int row_cnt = a.full ? a.full : __builtin_amdgcn_readfirstlane(a.w.ptr[br + 1]) - row0;
+  const auto* ptr = (const __attribute__((address_space(4))) int32_t*)a.w.ptr;
+  const int row0 = a.full ? br * a.full : ptr[br];
+  const int row_cnt = a.full ? a.full : ptr[br + 1] - row0;
   const int first = (int)((int64_t)row_cnt * blockIdx.z / a.split), n0 = row0 + first;
   const int cnt = (int)((int64_t)row_cnt * (blockIdx.z + 1) / a.split) - first;
   const int mine = cnt > wave ? (cnt - wave + waves - 1) / waves : 0;

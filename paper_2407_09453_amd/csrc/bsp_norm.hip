@@ -3,7 +3,7 @@
 //   mu = mean x, v = mean (x - mu)^2, r = 1 / sqrt(v + eps), h = (x - mu) r, y = h w + b
 //   g = dy w, dx = r (g - mean g - h mean(g h)), dw = sum over rows of dy h, db = sum over rows of dy
 //
-// A row is read once and stays in the registers of the 64 or 256 threads that own it, so the mean is known before the
+// A row is read once and stays in the registers of the 16 to 1024 threads that own it, so the mean is known before the
 // deviations are squared (no difference of large sums); everything is summed in fp32.  Rows too long for that are read again.
 // The gradient's threads own columns: each adds its columns' dw and db over all the rows that its workgroup takes, and
 // a second launch adds the workgroups' sums in a fixed order (no atomics: the same inputs give the same bits).
@@ -47,14 +47,18 @@ template <int ROWT, int N>
 __device__ __forceinline__ void row_sum(float* v, float (*sh)[N]) {
 #pragma unroll
   for (int k = 0; k < N; ++k) v[k] = ROWT == 16 ? f8_row16_sum(v[k]) : f8_wave_sum(v[k]);
-  if constexpr (ROWT == 256) {
+  if constexpr (ROWT >= 256) {
     __syncthreads();  // the last use of sh is over
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
       for (int k = 0; k < N; ++k) sh[threadIdx.x >> 6][k] = v[k];
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = (sh[0][k] + sh[1][k]) + (sh[2][k] + sh[3][k]);
+    for (int k = 0; k < N; ++k) {
+      v[k] = 0.f;
+#pragma unroll
+      for (int w = 0; w < ROWT / 64; ++w) v[k] += sh[w][k];
+    }
   }
 }
 
@@ -83,10 +87,10 @@ __device__ __forceinline__ void put8(const NormArgs& a, int64_t row, int c, floa
 
 // NV: groups of eight columns a thread holds; 0: rows of any length, read three times
 template <bool F32, bool CODES, int ROWT, int NV>
-__global__ __launch_bounds__(256) void norm_forward(NormArgs a) {
-  __shared__ float sh[4][1];
+__global__ __launch_bounds__(ROWT > 256 ? ROWT : 256) void norm_forward(NormArgs a) {
+  __shared__ float sh[ROWT > 256 ? ROWT / 64 : 4][1];
   const int tid = threadIdx.x % ROWT;
-  const int64_t row = (int64_t)blockIdx.x * (256 / ROWT) + threadIdx.x / ROWT;
+  const int64_t row = ROWT >= 256 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (256 / ROWT) + threadIdx.x / ROWT;
   if (row >= a.T) return;  // (whole groups of ROWT)
   const void* x = row_of<F32>(a.X, row, a.ldx);
   const float inv = 1.f / (float)a.D;
@@ -164,22 +168,26 @@ __global__ __launch_bounds__(256) void norm_forward(NormArgs a) {
 }
 
 template <bool F32, int ROWT, int NV>
-__global__ __launch_bounds__(256) void norm_backward(NormArgs a) {
-  __shared__ float sh[4][2];
+__global__ __launch_bounds__(ROWT > 256 ? ROWT : 256) void norm_backward(NormArgs a) {
+  __shared__ float sh[ROWT > 256 ? ROWT / 64 : 4][2];
   const int tid = threadIdx.x % ROWT;
-  constexpr int kGroups = 256 / ROWT;  // rows that a workgroup has in work
+  constexpr int kGroups = ROWT >= 256 ? 1 : 256 / ROWT;  // rows that a workgroup has in work
   const int in_group = threadIdx.x / ROWT;
   const int64_t group = (int64_t)blockIdx.x * kGroups + in_group, step = (int64_t)a.parts * kGroups;
   const float inv = 1.f / (float)a.D;
   const bool ragged = a.D & 7;
-  float w[NV][8], dw[NV][8], db[NV][8];
+  // sixteen waves a workgroup leave each 128 registers: not enough for the weight, nor for a row that is asked for ahead
+  constexpr bool kKeep = ROWT < 1024;
+  constexpr int kWeights = kKeep ? NV : 1;
+  float w[kWeights][8], dw[NV][8] = {}, db[NV][8] = {};
+  auto weights = [&](int j, float (&to)[8]) {
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int c = (tid + j * ROWT) * 8;
+    for (int k = 0; k < 8; ++k) to[k] = 1.f;
+    if (a.weight) load8<true>(a.weight, (tid + j * ROWT) * 8, a.D, to);
+  };
+  if constexpr (kKeep)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) w[j][k] = 1.f, dw[j][k] = 0.f, db[j][k] = 0.f;
-    if (a.weight) load8<true>(a.weight, c, a.D, w[j]);
-  }
+    for (int j = 0; j < NV; ++j) weights(j, w[j]);
   // a row's values are asked for while the row before it is worked on
   F8Raw8<F32> rx[NV], ry[NV];
   float next_mean = 0.f, next_rstd = 0.f;
@@ -192,8 +200,9 @@ __global__ __launch_bounds__(256) void norm_backward(NormArgs a) {
       ry[j] = f8_raw8<F32>(row_of<F32>(a.dY, row, a.ld_dy), (tid + j * ROWT) * 8, a.D);
     }
   };
-  if (group < a.T) ask(group);
+  if (kKeep && group < a.T) ask(group);
   for (int64_t row = group; row < a.T; row += step) {
+    if constexpr (!kKeep) ask(row);
     const float mean = next_mean, rstd = next_rstd;
     float h[NV][8], g[NV][8], s[2] = {0.f, 0.f};
 #pragma unroll
@@ -202,18 +211,20 @@ __global__ __launch_bounds__(256) void norm_backward(NormArgs a) {
       f8_unpack8<F32>(rx[j], past, ragged, h[j]);
       f8_unpack8<F32>(ry[j], past, ragged, g[j]);
     }
-    ask(row + step);
+    if constexpr (kKeep) ask(row + step);
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
+      if constexpr (!kKeep) weights(j, w[0]);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         h[j][k] = (tid + j * ROWT) * 8 + k < a.D ? (h[j][k] - mean) * rstd : 0.f;
         dw[j][k] += g[j][k] * h[j][k];
         db[j][k] += g[j][k];
-        g[j][k] *= w[j][k];
+        g[j][k] *= w[kKeep ? j : 0][k];
         s[0] += g[j][k];
         s[1] += g[j][k] * h[j][k];
       }
+    }
     row_sum<ROWT, 2>(s, sh);
     const float mg = s[0] * inv, mh = s[1] * inv;
 #pragma unroll
@@ -332,8 +343,8 @@ int forward(const NormArgs& a, hipStream_t st) {
   else if (a.Dp <= 1024) hipLaunchKernelGGL((norm_forward<F32, CODES, 64, 2>), quads, block, 0, st, a);
   else if (a.Dp <= 2048) hipLaunchKernelGGL((norm_forward<F32, CODES, 256, 1>), rows, block, 0, st, a);
   else if (a.Dp <= 4096) hipLaunchKernelGGL((norm_forward<F32, CODES, 256, 2>), rows, block, 0, st, a);
-  else if (a.Dp <= 8192) hipLaunchKernelGGL((norm_forward<F32, CODES, 256, 4>), rows, block, 0, st, a);
-  else hipLaunchKernelGGL((norm_forward<F32, CODES, 256, 8>), rows, block, 0, st, a);
+  else if (a.Dp <= 8192) hipLaunchKernelGGL((norm_forward<F32, CODES, 512, 2>), rows, dim3(512), 0, st, a);
+  else hipLaunchKernelGGL((norm_forward<F32, CODES, 1024, 2>), rows, dim3(1024), 0, st, a);
   return launched();
 }
 
@@ -348,7 +359,8 @@ int backward(const NormArgs& a, hipStream_t st) {
   else if (a.D >= 8 && a.D <= 512) hipLaunchKernelGGL((norm_backward<F32, 64, 1>), parts, block, 0, st, a);
   else if (a.D >= 8 && a.D <= 2048) hipLaunchKernelGGL((norm_backward<F32, 256, 1>), parts, block, 0, st, a);
   else if (a.D >= 8 && a.D <= 4096) hipLaunchKernelGGL((norm_backward<F32, 256, 2>), parts, block, 0, st, a);
-  else if (a.D >= 8 && a.D <= 8192) hipLaunchKernelGGL((norm_backward<F32, 256, 4>), parts, block, 0, st, a);
+  else if (a.D >= 8 && a.D <= 8192) hipLaunchKernelGGL((norm_backward<F32, 512, 2>), parts, dim3(512), 0, st, a);
+  else if (a.D >= 8 && a.D <= 16384) hipLaunchKernelGGL((norm_backward<F32, 1024, 2>), parts, dim3(1024), 0, st, a);
   else {
     if (a.T > 0) hipLaunchKernelGGL((norm_backward_long<F32>), dim3((unsigned)a.T), block, 0, st, a);
     if (launched() != BSP_OK) return BSP_ERR_HIP;
@@ -367,7 +379,8 @@ int sum(const float* part, int parts, int64_t width, int64_t split_at, float* ou
 // Workgroups that share the rows.  Where one is done with all of them in eight turns its sums are the result: a launch less.
 int norm_parts(int T, int D) {
   const int64_t turns = ((int64_t)T + rows_at_once(D) - 1) / rows_at_once(D);
-  return turns <= 8 ? 1 : turns < 512 ? (int)turns : 512;
+  const int most = D > 4096 ? 256 : 512;  // as many as the chip holds at one time
+  return turns <= 8 ? 1 : turns < most ? (int)turns : most;
 }
 
 int norm_launch_forward(const void* X, bool f32, int64_t ldx, int T, int D, const float* weight, const float* bias, float eps,
