@@ -20,7 +20,7 @@ _SAVE, _LOAD, _FC, _VALUES, _GRAD, _NORM, _NORM_GRAD = range(7)
 _pack9, _pack13, _pack17, _pack18, _pack20 = (struct.Struct("=%dq" % n).pack for n in (9, 13, 17, 18, 20))
 _pack_norm = struct.Struct("=7qd10q").pack
 _NO_CODES = (0, 0, 0, 0, 0)
-_types = None
+_types = _torch = None
 
 
 def _type(t) -> int:
@@ -129,6 +129,8 @@ class BspLayerF8:
 
     def __init__(self, W, gamma=None, bias=None, device="cuda:0"):
         import torch
+        global _torch
+        _torch = torch
         lib = load_library()
         self.device = torch.device(device)
         O, I = W.shape
@@ -154,6 +156,7 @@ class BspLayerF8:
         self.struct = bsp_weights_f8(O, I, self.nnzb, *(t.data_ptr() for t in self.d_index), self.payload.data_ptr(),
                                      self.scale.data_ptr(), self.payload_t.data_ptr(), self.scale_t.data_ptr())
         self._address = ctypes.addressof(self.struct)
+        self.device, self._index = self.payload.device, self.payload.get_device()
         self._workspace = {}  # bytes that a call takes, by its kind and rows
         self.d_bias = None
         if bias is not None:
@@ -190,8 +193,7 @@ class BspLayerF8:
         return n
 
     def _multiply(self, transposed, X, code, bias, residual, relu, gate, dtype, out, stream):
-        import torch
-        codes = isinstance(X, BspCodes)
+        codes = type(X) is BspCodes
         if codes:
             T, K, at = X.T, X.K, X.buffer
         else:
@@ -199,27 +201,37 @@ class BspLayerF8:
             at = X
         width, inner = (self.I, self.O) if transposed else (self.O, self.I)
         assert K == inner, (K, inner)
+        assert at.get_device() == self._index, "tensors on different devices"
         if out is None:
-            out = torch.empty((T, width), dtype=dtype or (torch.bfloat16 if codes else X.dtype), device=at.device)
+            if dtype is None:
+                dtype = _torch.bfloat16 if codes else X.dtype
+            out = _torch.empty((T, width), dtype=dtype, device=self.device)
         else:
             assert out.shape == (T, width) and out.is_contiguous()
-        _on(self.payload, at, out, residual, None if gate is None else gate.buffer)
+            _on(at, out)
+        r, g = 0, _NO_CODES
         if residual is not None:
             assert residual.shape == out.shape and residual.dtype == out.dtype and residual.is_contiguous()
+            _on(at, residual)
+            r = residual.data_ptr()
+        if gate is not None:
+            _on(at, gate.buffer)
+            g = gate.words
         st = _current_stream(out) if stream is None else stream
-        rest = (0 if bias is None else bias.data_ptr(), 0 if residual is None else residual.data_ptr(), 1 if relu else 0,
-                *(_NO_CODES if gate is None else gate.words), out.data_ptr(), _type(out))
-        if not codes:  # (few whole rows become codes inside the product's kernel)
+        if codes:
+            n = self._bytes(transposed * 2 + 1, T)
+        else:  # (few whole rows become codes inside the product's kernel)
             x, size = X.data_ptr(), X.element_size()
             inside = T <= 16 and not (x | ld * size | K * size) & 15 and T * (_blocks(K) * 129 + 16) <= 73728
-        n = self._bytes(transposed * 2 + (codes or inside), T)
-        ws = torch.empty(n, dtype=torch.uint8, device=out.device) if n else None
-        rest += (0 if ws is None else ws.data_ptr(), n, st)
+            n = self._bytes(transposed * 2 + inside, T)
+        ws = _torch.empty(n, dtype=_torch.uint8, device=self.device) if n else None
+        rest = (0 if bias is None else bias.data_ptr(), r, 1 if relu else 0, *g, out.data_ptr(), _type(out), 0 if ws is None else ws.data_ptr(), n, st)
         if codes:
             _call(_FC, _pack20(self._address, transposed, *X.words, *rest), "bsp_f8_fc")
         else:
             _call(_VALUES, _pack20(self._address, transposed, x, _type(X), ld, T, CODES[code], *rest), "bsp_f8_fc_values")
-        _keep(ws, stream)
+        if stream is not None:
+            _keep(ws, stream)
         return out
 
     def fc(self, X, relu=False, residual=None, dtype=None, out=None, stream=None):
