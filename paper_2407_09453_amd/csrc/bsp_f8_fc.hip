@@ -20,6 +20,7 @@ struct TileArgs {
   int32_t T, tiles_t, tiles_o;
   float* part;  // split > 1: sums of each share of the block columns, [split][T][4 ceil(out / 4)], instead of results
   int32_t split;
+  int32_t full;  // blocks in a block row, where all are kept; else 0
 };
 
 __device__ __forceinline__ i32x8_t read_fragment(const uint8_t* p, int at0, int at1) {
@@ -249,10 +250,13 @@ __global__ __launch_bounds__(64 * WO * WT) void f8_wide(TileArgs a) {
   place_tile((int)blockIdx.x - share * tiles, a.tiles_o, a.tiles_t, &tile_o, &tile_t);
   const int br = tile_o * K::R;
   const int64_t t0 = (int64_t)tile_t * K::NT;
-  int n0 = __builtin_amdgcn_readfirstlane(a.w.ptr[br]), cnt = __builtin_amdgcn_readfirstlane(a.w.ptr[br + 1]) - n0;
+  // (where all blocks are kept their places need not be read)
+  const auto* ptr = (const __attribute__((address_space(4))) int32_t*)a.w.ptr;
+  int n0 = a.full ? br * a.full : ptr[br], cnt = a.full ? a.full : ptr[br + 1] - n0, col_first = 0;
   if constexpr (kSplits) {
     const int from = (int)((int64_t)cnt * share / a.split), to = (int)((int64_t)cnt * (share + 1) / a.split);
     n0 += from;
+    col_first = from;
     cnt = to - from;
   }
   const int last = (int)(a.T - 1 - t0 < K::NT - 1 ? a.T - 1 - t0 : K::NT - 1);  // rows past the last: its bytes, their results go nowhere
@@ -289,27 +293,29 @@ __global__ __launch_bounds__(64 * WO * WT) void f8_wide(TileArgs a) {
   if (cnt > 0) {
     const int32_t* idx = a.w.idx + n0;
     const uint8_t* scl = a.w.scale + n0 + (K::R == 1 ? 0 : ((wo * MO * 32) >> 7) * cnt);
-    const int col0 = idx[lane < cnt ? lane : cnt - 1];
+    // block columns and weight scales, one a lane: of the first steps, of those that the loop below asks for (64 at a time) and goes through, of the last
+    auto column = [&](int i) { return a.full ? col_first + (i < cnt ? i : cnt - 1) : idx[i < cnt ? i : cnt - 1]; };
+    auto scale = [&](int i) { return (int)scl[i < cnt ? i : cnt - 1]; };
+    const int tail = cnt > BUFS ? cnt - BUFS : 0;
+    const int col0 = column(lane);
+    int cols = column(lane + BUFS), scales = scale(lane), tail_scales = scale(tail + lane);
 #pragma unroll
     for (int j = 0; j < BUFS; ++j)
       if (j < cnt) k.copy(lds + j * K::STAGE, j, __builtin_amdgcn_readlane(col0, j));
     i32x8_t w[2][MO], x[2][MT];
     int sx[2][MT];
-    // the last steps' weight scales, one a lane
-    const int tail = cnt > BUFS ? cnt - BUFS : 0;
-    const int tail_scales = scl[tail + lane < cnt ? tail + lane : cnt - 1];
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(cols), "+v"(scales), "+v"(tail_scales)::"memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     k.read_scales(lds, sx[0]);
     k.read(lds, 0, w[0], x[0]);
     int cur = 0;
     auto following = [](int b) { return b == (BUFS - 1) * K::STAGE ? 0 : b + K::STAGE; };
-    // block columns and weight scales of 64 steps at a time, one a lane
     for (int c = 0; c < cnt - BUFS; c += 64) {
-      const int l = c + lane;
-      int cols = idx[l + BUFS < cnt ? l + BUFS : cnt - 1], scales = scl[l < cnt ? l : cnt - 1];
-      asm volatile("s_waitcnt vmcnt(0)" : "+v"(cols), "+v"(scales)::"memory");
+      if (c > 0) {
+        cols = column(c + lane + BUFS), scales = scale(c + lane);
+        asm volatile("s_waitcnt vmcnt(0)" : "+v"(cols), "+v"(scales)::"memory");
+      }
       const int end = c + 64 < cnt - BUFS ? c + 64 : cnt - BUFS;
       for (int i = c; i < end; ++i) {
         const int nxt = following(cur);
@@ -388,7 +394,7 @@ struct Plan {
   int tile, split;
 };
 // Where tiles are too few for the chip the block columns are cut into shares, of at least four steps each, whose sums a second launch joins: that
-// costs it 3 us and the memory's time (us, one share and as planned: 243 x 18816 -> 384 , 256 x 16384 -> 1024 ).
+// costs it 3 us and the memory's time (us, one share and as planned: 243 x 18816 -> 384 40 and 15.3, 256 x 16384 -> 1024 35 and 19.5).
 Plan plan_of(int O, int64_t nnzb, int T, bool full) {
   const double steps = (double)nnzb / f8_blocks(O);
   Plan best{2, 1};
@@ -434,7 +440,8 @@ int f8_tile_split(const F8Rows& w, int T) {
 
 int f8_launch_tile(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, float* part, hipStream_t st) {
   const Plan plan = plan_of(w.out, w.nnzb, T, w.nnzb == (int64_t)f8_blocks(w.out) * f8_blocks(w.in));
-  TileArgs a{w, (const uint8_t*)x.X, x.scale, q, x.ld, f8_scale_rows(T), T, 0, 0, part, plan.split};
+  const bool full = w.nnzb == (int64_t)f8_blocks(w.out) * f8_blocks(w.in);
+  TileArgs a{w, (const uint8_t*)x.X, x.scale, q, x.ld, f8_scale_rows(T), T, 0, 0, part, plan.split, full ? f8_blocks(w.in) : 0};
   return x.e5 ? launch_any<true>(a, plan.tile, f32, st) : launch_any<false>(a, plan.tile, f32, st);
 }
 
