@@ -129,17 +129,27 @@ __global__ __launch_bounds__(kThreads, C == 1 ? 4 : 2) void f8_grad(F8GradArgs a
   const int to_y = row * 256 + ((piece >> 1) ^ key) * 32 + (piece & 1) * 16;
   const int to_x = (1 + j_in) * kTile + row * 256 + ((at_in >> 4) ^ key) * 32 + (kCodes == 8 ? (at_in & 8) * 2 : swap * 2);
   // To registers: eight gradients and the codes of row r of those that follow by, bx, bs, which are the same in all lanes.  Nothing here looks
-  // at what it asks for: that would wait for it.
+  // at what it asks for: that would wait for it.  (A lane's places are hidden from the optimiser, which would keep each in two registers
+  // and add the base there.)
   auto ask = [&](global_t by, global_t bx, global_t bs, uint32_t r, int j) {
     asm volatile("" : "+s"(by), "+s"(bx), "+s"(bs));
     if constexpr (THIN) y_in[j] = gradients8((const uint16_t*)by + r * a.ldy, 0, a.O);
-    else y_in[j] = *(const __attribute__((address_space(1))) u32x4_any*)(by + (r * (uint32_t)a.ldy * 2 + col_y));
+    else {
+      uint32_t at = r * (uint32_t)a.ldy * 2 + col_y;
+      asm volatile("" : "+v"(at));
+      y_in[j] = *(const __attribute__((address_space(1))) u32x4_any*)(by + at);
+    }
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
-      const uint32_t at = r * (uint32_t)Kp + col_x[p];
+      uint32_t at[kCodes / 8], at_s = r + col_s[p];
 #pragma unroll
-      for (int h = 0; h < kCodes / 8; ++h) x_in[j][p][h] = *(const __attribute__((address_space(1))) u32x2_t*)(bx + (at + (swap ^ 8 * h)));
-      s_in[j][p] = bs[r + col_s[p]];
+      for (int h = 0; h < kCodes / 8; ++h) {
+        at[h] = r * (uint32_t)Kp + col_x[p] + (swap ^ 8 * h);
+        asm volatile("" : "+v"(at[h]));
+        x_in[j][p][h] = *(const __attribute__((address_space(1))) u32x2_t*)(bx + at[h]);
+      }
+      asm volatile("" : "+v"(at_s));
+      s_in[j][p] = bs[at_s];
     }
   };
   // The range's rows that make no whole step come first, as step 0; n steps in all.
@@ -311,8 +321,9 @@ __global__ __launch_bounds__(256) void f8_grad_finish(F8GradArgs a) {
 }
 
 // Kept blocks a workgroup: more of them share a block row's gradients and take longer, so it goes by how often the chip is filled.  A CU holds two workgroups of
-// one block or one of more; us a step where it is full: 0.64, 0.55, 0.94 (843, 984, 1148 TFLOP/s on 8192 x 8192 -> 8192), and 6 a workgroup to begin and end
-// (us for one, two, four blocks: 8192 x 4096 -> 16384 1306 1179 1007, 2048 x 4096 -> 4096 88 86 76, half of it kept 62 74 66, 2048 x 4096 -> 4097 105 115 127).
+// one block or one of more; us a step where it is full: 0.64, 0.55, 0.94, and 6 a workgroup to begin and end.  Measured (us for one, two, four
+// blocks): 8192 x 4096 -> 16384 1241 1115 1017, 8192 x 8192 -> 8192 1183 1060 971 (930, 1037, 1133 TFLOP/s), half of it kept 663 607 645, 2048 x 4096 -> 4096 84 83 75,
+// half of it kept 59 70 67, 2048 x 4096 -> 4097 104 110 121.
 int blocks_each(const F8GradArgs& a) {
   const double steps = (double)(((int64_t)a.T + kStep - 1) / kStep), row = (double)a.nnzb / a.nbo;
   const bool full = a.nnzb == (int64_t)a.nbo * a.nbi;
