@@ -278,7 +278,7 @@ inline int64_t f8_few_staged(int T, int K) { return (int64_t)T * (f8_blocks(K) *
 int f8_few_split(const F8Rows& w, int T);
 int f8_launch_few(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, float* part, hipStream_t st);
 // many rows, codes only
-int f8_tile_split(const F8Rows& w, int T);
+int f8_tile_split(const F8Rows& w, int T, bool f32);
 int f8_launch_tile(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, float* part, hipStream_t st);
 int f8_launch_join(const float* part, int split, int T, int O, const F8Epilogue& q, bool f32, hipStream_t st);
 int f8_launch_save(const void* X, int x_f32, int64_t ldx, int T, int K, bool e5, uint8_t* codes, uint8_t* scale, hipStream_t st);

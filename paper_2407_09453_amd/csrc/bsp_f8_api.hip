@@ -72,10 +72,14 @@ int check_product(const bsp_weights_f8* w, int32_t transposed, int32_t T, const 
   return BSP_OK;
 }
 
-int split_of(const F8Rows& rows, int T) { return T <= kFewRows ? f8_few_split(rows, T) : f8_tile_split(rows, T); }
+int split_of(const F8Rows& rows, int T, bool f32) { return T <= kFewRows ? f8_few_split(rows, T) : f8_tile_split(rows, T, f32); }
 
 int64_t sums_bytes(const F8Rows& rows, int T) {
-  const int64_t split = T > 0 ? split_of(rows, T) : 1;
+  int64_t split = 1;
+  for (int f32 = 0; f32 < 2 && T > 0; ++f32) {  // results of either type fit
+    const int64_t s = split_of(rows, T, f32);
+    if (s > split) split = s;
+  }
   return split > 1 ? split * T * ((rows.out + 3) / 4) * 16 : 0;
 }
 
@@ -83,7 +87,7 @@ int multiply(const F8Rows& rows, const F8Input& x, int T, const F8Epilogue& q, i
   const bool f32 = y_dtype == BSP_F32;
   const int rc = T <= kFewRows ? f8_launch_few(rows, x, T, q, f32, (float*)sums, st) : f8_launch_tile(rows, x, T, q, f32, (float*)sums, st);
   if (rc != BSP_OK) return rc;
-  const int split = split_of(rows, T);
+  const int split = split_of(rows, T, f32);
   return split > 1 ? f8_launch_join((const float*)sums, split, T, rows.out, q, f32, st) : BSP_OK;
 }
 

@@ -395,11 +395,12 @@ struct Plan {
 };
 // Where tiles are too few for the chip the block columns are cut into shares, of at least four steps each, whose sums a second launch joins: that
 // costs it 3 us and the memory's time (us, one share and as planned: 243 x 18816 -> 384 40 and 15.3, 256 x 16384 -> 1024 35 and 19.5).
-Plan plan_of(int O, int64_t nnzb, int T, bool full) {
+// fp32 results take twice the time a step, at half the rate (64 x 4096 -> 4096 fp32 17.2 us in one share, 13.6 in two, 8192 x 4096 -> 4096 1180 TFLOP/s).
+Plan plan_of(int O, int64_t nnzb, int T, bool full, bool f32) {
   const double steps = (double)nnzb / f8_blocks(O);
   Plan best{2, 1};
   double least = 1e30;
-  for (int k = full && f8_blocks(O) % 2 == 0 ? 0 : 1; k < 5; ++k) {
+  for (int k = f32 ? 2 : full && f8_blocks(O) % 2 == 0 ? 0 : 1; k < 5; ++k) {
     const Tile& v = kTiles[k];
     const double groups = (double)((f8_blocks(O) * F8_BLOCK + v.o - 1) / v.o) * (double)(((int64_t)T + v.t - 1) / v.t);
     for (int split = 1; split == 1 || (k >= 2 && groups * split <= 256 && steps >= 4.0 * split && split <= 64); split *= 2) {
@@ -407,7 +408,7 @@ Plan plan_of(int O, int64_t nnzb, int T, bool full) {
       const double rounds = all <= 256 ? v.alone : v.shared * (double)(int64_t)((all + 256 * v.fit - 1) / (256 * v.fit));
       const double us = rounds * steps / split, at_rate = groups * steps * v.o * v.t * 256e-6 / v.rate;
       const double join = split > 1 ? 3.0 + (double)T * O * 4 * 2 * split / 3e6 : 0;
-      const double worse = (us > at_rate ? us : at_rate) + join;
+      const double worse = (us > at_rate ? us : at_rate) * (f32 ? 2.1 : 1) + join;
       if (worse < least) least = worse, best = Plan{k, split};
     }
   }
@@ -434,13 +435,15 @@ int launch_any(const TileArgs& a, int k, bool f32, hipStream_t st) {
 
 }  // namespace
 
-int f8_tile_split(const F8Rows& w, int T) {
-  return plan_of(w.out, w.nnzb, T, w.nnzb == (int64_t)f8_blocks(w.out) * f8_blocks(w.in)).split;
-}
+namespace {
+bool all_kept(const F8Rows& w) { return w.nnzb == (int64_t)f8_blocks(w.out) * f8_blocks(w.in); }
+}  // namespace
+
+int f8_tile_split(const F8Rows& w, int T, bool f32) { return plan_of(w.out, w.nnzb, T, all_kept(w), f32).split; }
 
 int f8_launch_tile(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, float* part, hipStream_t st) {
-  const Plan plan = plan_of(w.out, w.nnzb, T, w.nnzb == (int64_t)f8_blocks(w.out) * f8_blocks(w.in));
-  const bool full = w.nnzb == (int64_t)f8_blocks(w.out) * f8_blocks(w.in);
+  const bool full = all_kept(w);
+  const Plan plan = plan_of(w.out, w.nnzb, T, full, f32);
   TileArgs a{w, (const uint8_t*)x.X, x.scale, q, x.ld, f8_scale_rows(T), T, 0, 0, part, plan.split, full ? f8_blocks(w.in) : 0};
   return x.e5 ? launch_any<true>(a, plan.tile, f32, st) : launch_any<false>(a, plan.tile, f32, st);
 }
