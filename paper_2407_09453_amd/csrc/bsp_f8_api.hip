@@ -259,7 +259,7 @@ int bsp_layer_norm_grad(const void* dY, int64_t ld_dy, const void* X, int64_t ld
 int bsp_f8_call_packed(int32_t call, const int64_t* w) {
   if (!w) return BSP_ERR_NULL;
   auto ptr = [&](int i) { return (void*)(intptr_t)w[i]; };
-  auto num = [&](int i) { return (int32_t)w[i]; };
+  auto num = [&](int i) { return w[i] == (int32_t)w[i] ? (int32_t)w[i] : -1; };  // (no type has that number)
   // sizes that do not fit 32 bits are as wrong as negative ones
   auto size = [&](int i) { return w[i] < 0 || w[i] > INT32_MAX ? -1 : (int32_t)w[i]; };
   auto codes = [&](int i) { return bsp_codes{size(i), size(i + 1), num(i + 2), (uint8_t*)ptr(i + 3), (uint8_t*)ptr(i + 4)}; };

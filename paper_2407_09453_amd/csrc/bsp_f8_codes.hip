@@ -4,6 +4,9 @@
 // rows by 1024 columns: a wave reads a row's 1024 columns as whole lines, sixteen consecutive values a lane, so a block
 // of 128 lies in eight neighbouring lanes and its maximum takes three exchanges; the sixteen rows' scales of a column
 // block are gathered in LDS and leave as one 16-byte piece, since they are neighbours in memory.
+// Measured at 16384 x 4096 bf16: write 38 us (5.3 TB/s), read back 32 us (6.4 TB/s), where a copy runs at 6.2; 1 x 4096 3.4 and 2.0 us.
+// (Codes written past the caches gave the writer 10 % and cost the product that reads them more.)
+// The weights' 16384 x 4096 from fp32, in both directions, take 79 us (5.1 TB/s).
 #include "bsp_f8.h"
 
 namespace {

@@ -1,5 +1,6 @@
 """Host side of the 8-bit floating-point layers: index arrays, refusals, and the oracle against its own definition."""
 import ctypes
+import struct
 
 import numpy as np
 import pytest
@@ -189,3 +190,20 @@ def test_oracle_weight_gradient_against_differences():
         d[at] = 1.0
         assert abs(loss(W + d) - loss(W) - dW[at]) < 1e-10
     assert np.allclose(db, dy.sum(0))
+
+
+def test_packed_call_refusals():
+    """What the calls refuse one by one they refuse in words too, and sizes and types that no 32 bits hold are none."""
+    call = bsp.load_library().bsp_f8_call_packed
+    words = lambda *w: struct.pack("=%dq" % len(w), *w)
+    assert call(0, None) == NULL
+    assert call(-1, words(*[0] * 20)) == SHAPE and call(7, words(*[0] * 20)) == SHAPE
+    save = [P, b.BSP_BF16, 384, 8, 384, b.BSP_E4M3, P, P, 0]
+    for at, value, want in ((0, 0, NULL), (6, 0, NULL), (3, 2**32 + 8, SHAPE), (4, -2**32 + 384, SHAPE), (1, 2**32 + b.BSP_BF16, DTYPE),
+                            (5, 2**32 + b.BSP_E4M3, DTYPE), (1, 77, DTYPE), (0, P + 1, ALIGN), (2, 383, SHAPE)):
+        w = list(save)
+        w[at] = value
+        assert call(0, words(*w)) == want, (at, value)
+    assert call(1, words(8, 384, b.BSP_E4M3, P, P, 0, b.BSP_BF16, 384, 0)) == NULL  # nowhere to
+    for c, n, want in ((2, 20, DTYPE), (3, 20, NULL), (4, 13, DTYPE)):  # the codes are looked at first; values, behind the weights
+        assert call(c, words(*[0] * n)) == want, c
