@@ -16,7 +16,7 @@
 
 namespace {
 
-constexpr int kStep = 32, kThreads = 512;  // rows a step
+constexpr int kStep = 32;  // rows a step
 constexpr int kTile = kStep * 256;                     // 32 rows of 128 bf16
 
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
@@ -45,12 +45,13 @@ __device__ __forceinline__ u32x4_t gradients8(const uint16_t* row, int o, int O)
 }
 
 // Column sums of one block row's gradients over one range of rows: a thread adds eight columns of every 32nd row.
+template <int THREADS>
 __device__ __forceinline__ void column_sums(const F8GradArgs& a, int br, int64_t t_begin, int64_t t_end, float* sums) {
   const int piece = threadIdx.x & 15, o = br * F8_BLOCK + piece * 8;
   float s[8] = {};
   if (o < a.O)
 #pragma unroll 4
-    for (int64_t t = t_begin + (threadIdx.x >> 4); t < t_end; t += kThreads / 16) {
+    for (int64_t t = t_begin + (threadIdx.x >> 4); t < t_end; t += THREADS / 16) {
       const u32x4_t v = gradients8(a.dY + t * a.ldy, o, a.O);
 #pragma unroll
       for (int k = 0; k < 8; ++k) s[k] += __uint_as_float(k & 1 ? v[k >> 1] & 0xFFFF0000u : v[k >> 1] << 16);
@@ -60,18 +61,24 @@ __device__ __forceinline__ void column_sums(const F8GradArgs& a, int br, int64_t
   __syncthreads();
   if (threadIdx.x < F8_BLOCK && br * F8_BLOCK + (int)threadIdx.x < a.O) {
     float v = 0.f;
-    for (int r = 0; r < kThreads / 16; ++r) v += sums[r * 129 + threadIdx.x];
+    for (int r = 0; r < THREADS / 16; ++r) v += sums[r * 129 + threadIdx.x];
     (a.split == 1 ? a.db : a.part_db + (int64_t)blockIdx.y * a.O)[br * F8_BLOCK + threadIdx.x] = v;
   }
 }
 
 // THIN: fewer than eight outputs, read one by one
+// Eight waves; of two blocks four, and two such workgroups on a CU, whose barriers then do not keep all waves of a SIMD in step (us at 8192 x 4096 -> 16384 and on half
+// of the blocks of 8192 x 8192 -> 8192: 1115 and 607 with eight waves of half as many outputs, 1051 and 583).
+template <int C>
+constexpr int kThreads = C == 2 ? 256 : 512;
 template <int C, bool E5, bool THIN>
-__global__ __launch_bounds__(kThreads, C == 1 ? 4 : 2) void f8_grad(F8GradArgs a) {
-  constexpr int MO = C, WO = 4 / MO;  // 32-row tiles of outputs a wave, waves side by side over the 128 outputs
+__global__ __launch_bounds__(kThreads<C>, C == 1 ? 4 : 2) void f8_grad(F8GradArgs a) {
+  constexpr int THREADS = kThreads<C>;
+  constexpr int MO = C == 2 ? 4 : C, WO = 4 / MO;  // 32-row tiles of outputs a wave, waves side by side over the 128 outputs
   constexpr int kBuffer = (1 + C) * kTile;
-  constexpr int kAhead = C == 4 ? 2 : 4;  // steps that are on their way to registers (the accumulators of four blocks leave room for two)
-  constexpr int kPieces = C > 1 ? C / 2 : 1, kCodes = C > 1 ? 16 : 8;  // runs of codes a thread brings, of a block each
+  constexpr int kAhead = C >= 2 ? 2 : 4;  // steps that are on their way to registers (the accumulators of four blocks leave room for two)
+  constexpr int kRow = THREADS / kStep, kYs = 16 / kRow;  // threads that bring a row; of eight gradients each
+  constexpr int kCodes = C > 1 ? 16 : 8, kPieces = C * F8_BLOCK / kCodes / kRow, kApart = kRow * kCodes / F8_BLOCK;  // runs of codes a thread brings, each a block, or two, on
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   kernarg_touch<F8GradArgs>();
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -84,7 +91,7 @@ __global__ __launch_bounds__(kThreads, C == 1 ? 4 : 2) void f8_grad(F8GradArgs a
   // one, so that rows that keep more blocks than others do not meet on one.
   const int b = blockIdx.x, quads = (groups + 3) >> 2, clusters = quads * a.nbo, behind = (clusters + 7) / 8 * 32;
   if (b >= behind) {  // the workgroups behind: one block row's column sums each
-    column_sums(a, b - behind, t_begin, t_end, (float*)lds);
+    column_sums<THREADS>(a, b - behind, t_begin, t_end, (float*)lds);
     return;
   }
   const int cluster = (b >> 5) * 8 + (b & 7), quad = cluster / a.nbo, br = cluster - quad * a.nbo;
@@ -98,28 +105,33 @@ __global__ __launch_bounds__(kThreads, C == 1 ? 4 : 2) void f8_grad(F8GradArgs a
       if (__ballot(kept)) continue;
       const int col = c * F8_BLOCK + (tid & 127);
       if (col < a.I)
-        for (int r = tid >> 7; r < F8_BLOCK && br * F8_BLOCK + r < a.O; r += kThreads / 128) a.dW[((int64_t)br * F8_BLOCK + r) * a.I + col] = 0.f;
+        for (int r = tid >> 7; r < F8_BLOCK && br * F8_BLOCK + r < a.O; r += THREADS / 128) a.dW[((int64_t)br * F8_BLOCK + r) * a.I + col] = 0.f;
     }
   }
   const int has = cnt - first < C ? cnt - first : C;  // kept blocks first .. first + has - 1 of the row
   if (has <= 0) return;
 
   // what this thread brings: eight gradients, and 8 C codes of one row
-  const int row = tid >> 4, piece = tid & 15;
-  const int o = br * F8_BLOCK + piece * 8;
+  const int row = tid / kRow, piece = tid % kRow;
   // eight gradients at once: at a row's end its last eight, which are moved into place when they are written
-  const uint32_t col_y = (uint32_t)(o + 8 <= a.O || THIN ? o : a.O - 8) * 2;
-  const int past = o + 8 <= a.O || (THIN && piece == 0) ? 0 : o + 8 - a.O < 8 ? o + 8 - a.O : 8;  // of them
+  uint32_t col_y[kYs];
+  int past[kYs];  // of them
+#pragma unroll
+  for (int q = 0; q < kYs; ++q) {
+    const int o = br * F8_BLOCK + (piece + q * kRow) * 8;
+    col_y[q] = (uint32_t)(o + 8 <= a.O || THIN ? o : a.O - 8) * 2;
+    past[q] = o + 8 <= a.O || (THIN && piece == 0) ? 0 : o + 8 - a.O < 8 ? o + 8 - a.O : 8;
+  }
   const int64_t Kp = (int64_t)f8_blocks(a.I) * F8_BLOCK, srows = f8_scale_rows(a.T);
   const int j_in = (piece * kCodes) >> 7, at_in = (piece * kCodes) & 127;  // the first run's block, and its columns in that; the next lies two blocks on
   uint32_t col_x[kPieces], col_s[kPieces];
 #pragma unroll
   for (int p = 0; p < kPieces; ++p) {
-    const int kb = a.col_idx[n0 + first + (j_in + 2 * p < has ? j_in + 2 * p : 0)];
+    const int kb = a.col_idx[n0 + first + (j_in + kApart * p < has ? j_in + kApart * p : 0)];
     col_x[p] = (uint32_t)kb * F8_BLOCK + at_in;
     col_s[p] = (uint32_t)(kb * srows);
   }
-  u32x4_t y_in[kAhead];
+  u32x4_t y_in[kAhead][kYs];
   u32x2_t x_in[kAhead][kPieces][kCodes / 8];
   int s_in[kAhead][kPieces];
   const int key = chunk_key(row);
@@ -133,11 +145,14 @@ __global__ __launch_bounds__(kThreads, C == 1 ? 4 : 2) void f8_grad(F8GradArgs a
   // and add the base there.)
   auto ask = [&](global_t by, global_t bx, global_t bs, uint32_t r, int j) {
     asm volatile("" : "+s"(by), "+s"(bx), "+s"(bs));
-    if constexpr (THIN) y_in[j] = gradients8((const uint16_t*)by + r * a.ldy, 0, a.O);
-    else {
-      uint32_t at = r * (uint32_t)a.ldy * 2 + col_y;
-      asm volatile("" : "+v"(at));
-      y_in[j] = *(const __attribute__((address_space(1))) u32x4_any*)(by + at);
+#pragma unroll
+    for (int q = 0; q < kYs; ++q) {
+      if constexpr (THIN) y_in[j][q] = gradients8((const uint16_t*)by + r * a.ldy, 0, a.O);
+      else {
+        uint32_t at = r * (uint32_t)a.ldy * 2 + col_y[q];
+        asm volatile("" : "+v"(at));
+        y_in[j][q] = *(const __attribute__((address_space(1))) u32x4_any*)(by + at);
+      }
     }
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
@@ -163,24 +178,27 @@ __global__ __launch_bounds__(kThreads, C == 1 ? 4 : 2) void f8_grad(F8GradArgs a
   // To LDS.  CHECK: step 0, whose missing rows add nothing.  ENDS: the last outputs' block row.
   auto write = [&](int buf, int j, auto ENDS, auto CHECK) {
     const bool in = !decltype(CHECK)::value || row < odd;
-    u32x4_t y = in ? y_in[j] : u32x4_t{0, 0, 0, 0};
-    if constexpr (decltype(ENDS)::value) {
 #pragma unroll
-      for (int d = 1; d < 8; d *= 2) {  // down by `past` values of two bytes, zeros from above
-        const u32x4_t v = d == 1 ? u32x4_t{y.x >> 16 | y.y << 16, y.y >> 16 | y.z << 16, y.z >> 16 | y.w << 16, y.w >> 16}
-                        : d == 2 ? u32x4_t{y.y, y.z, y.w, 0} : u32x4_t{y.z, y.w, 0, 0};
-        y = past & d ? v : y;
+    for (int q = 0; q < kYs; ++q) {
+      u32x4_t y = in ? y_in[j][q] : u32x4_t{0, 0, 0, 0};
+      if constexpr (decltype(ENDS)::value) {
+#pragma unroll
+        for (int d = 1; d < 8; d *= 2) {  // down by `past` values of two bytes, zeros from above
+          const u32x4_t v = d == 1 ? u32x4_t{y.x >> 16 | y.y << 16, y.y >> 16 | y.z << 16, y.z >> 16 | y.w << 16, y.w >> 16}
+                          : d == 2 ? u32x4_t{y.y, y.z, y.w, 0} : u32x4_t{y.z, y.w, 0, 0};
+          y = past[q] & d ? v : y;
+        }
+        y = past[q] == 8 ? u32x4_t{0, 0, 0, 0} : y;
       }
-      y = past == 8 ? u32x4_t{0, 0, 0, 0} : y;
+      *(u32x4_t*)(lds + buf * kBuffer + (to_y ^ 128 * q)) = y;  // the second run lies four chunks on
     }
-    *(u32x4_t*)(lds + buf * kBuffer + to_y) = y;
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {  // (a block more than there are: sums that go nowhere)
       const float s = __uint_as_float((uint32_t)s_in[j][p] << 23);
 #pragma unroll
       for (int h = 0; h < kCodes / 8; ++h) {
         const u32x2_t c = in ? x_in[j][p][h] : u32x2_t{0, 0};
-        *(u32x4_t*)(lds + buf * kBuffer + 2 * p * kTile + (to_x ^ 16 * h)) = f8_decode_bf16x8<E5>(c.x, c.y, s);
+        *(u32x4_t*)(lds + buf * kBuffer + kApart * p * kTile + (to_x ^ 16 * h)) = f8_decode_bf16x8<E5>(c.x, c.y, s);
       }
     }
   };
@@ -321,9 +339,9 @@ __global__ __launch_bounds__(256) void f8_grad_finish(F8GradArgs a) {
 }
 
 // Kept blocks a workgroup: more of them share a block row's gradients and take longer, so it goes by how often the chip is filled.  A CU holds two workgroups of
-// one block or one of more; us a step where it is full: 0.64, 0.55, 0.94, and 6 a workgroup to begin and end.  Measured (us for one, two, four
-// blocks): 8192 x 4096 -> 16384 1241 1115 1017, 8192 x 8192 -> 8192 1183 1060 971 (930, 1037, 1133 TFLOP/s), half of it kept 663 607 645, 2048 x 4096 -> 4096 84 83 75,
-// half of it kept 59 70 67, 2048 x 4096 -> 4097 104 110 121.
+// one or two blocks or one of four; us a step where it is full: 0.62, 0.98, 0.94, and 6 a round to begin and end.  Measured (us for one, two, four
+// blocks): 8192 x 4096 -> 16384 1241 1051 1017, 8192 x 8192 -> 8192 1183 981 971 (930, 1120, 1133 TFLOP/s), half of it kept 663 583 645, 2048 x 4096 -> 4096 84 75 75,
+// half of it kept 59 64 67, 2048 x 4096 -> 4097 104 109 121.
 int blocks_each(const F8GradArgs& a) {
   const double steps = (double)(((int64_t)a.T + kStep - 1) / kStep), row = (double)a.nnzb / a.nbo;
   const bool full = a.nnzb == (int64_t)a.nbo * a.nbi;
@@ -332,9 +350,12 @@ int blocks_each(const F8GradArgs& a) {
   for (int c = 1; c <= 4; c *= 2) {
     // (of rows that keep differing numbers of blocks the last group is half full on average)
     const double groups = a.nbo * (full ? (double)((a.nbi + c - 1) / c) : row / c + (c - 1) / (2.0 * c));
-    const double slots = c == 1 ? 512 : 256, rounds = (double)(int64_t)((groups + slots - 1) / slots);
-    const double step = c == 1 ? (groups <= 256 ? 0.32 : 0.64) : c == 2 ? 0.55 : 0.94;
-    const double us = rounds * (steps * step + 6);
+    const int64_t slots = c == 4 ? 256 : 512, rounds = (int64_t)(groups / slots);
+    const double left = groups - (double)(rounds * slots);
+    // a last round takes half the time where a CU has one workgroup instead of two, and less than a whole one where most have none
+    const double part = left <= 0 ? 0 : left <= 256 && slots == 512 ? 0.5 : slots == 512 || rounds == 0 ? 1 : 0.7;
+    const double step = c == 1 ? 0.62 : c == 2 ? 0.98 : 0.94;
+    const double us = (rounds + part) * steps * step + 6 * (double)(rounds + (left > 0));
     if (us < least) least = us, best = c;
   }
   return best;
@@ -348,7 +369,7 @@ int launch(F8GradArgs a, hipStream_t st) {
   a.groups = a.dW ? (a.nbi + C - 1) / C : 0;
   const int64_t groups = ((int64_t)a.nbo * ((a.groups + 3) / 4) + 7) / 8 * 32;
   if (groups + a.nbo > INT32_MAX) return BSP_ERR_SHAPE;
-  hipLaunchKernelGGL((f8_grad<C, E5, THIN>), dim3((unsigned)(groups + (a.db ? a.nbo : 0)), (unsigned)a.split), dim3(kThreads), lds, st, a);
+  hipLaunchKernelGGL((f8_grad<C, E5, THIN>), dim3((unsigned)(groups + (a.db ? a.nbo : 0)), (unsigned)a.split), dim3(kThreads<C>), lds, st, a);
   return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP;
 }
 
