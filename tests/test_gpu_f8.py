@@ -264,6 +264,12 @@ def test_weight_gradient(T, I, O, density, kind):
     assert (np.abs(_host(gdb) - db) <= (T + 8) * U * Sb).all()
 
 
+@pytest.mark.parametrize("kind", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("T,I,O,density", [(35, 4300, 4100, 1.0), (66, 4200, 4195, 0.6), (65, 5000, 3999, 0.8)])
+def test_weight_gradient_of_many_blocks_whose_outputs_end(T, I, O, density, kind):
+    test_weight_gradient(T, I, O, density, kind)
+
+
 def test_weight_gradient_of_rows_anywhere():
     """Gradients whose rows lie apart, at odd addresses, or are one row (a broadcast); dropped blocks give zeros whatever is there."""
     import torch
