@@ -188,15 +188,19 @@ struct F8Epilogue {
   const void* residual;  // [T][O] of Y's type, or null
   const uint8_t* gate;   // codes [T][128 ceil(O / 128)], or null: a result is kept where its code stands for a value > 0
   int32_t relu, gate_e5;
-  int32_t vec, vec8;     // rows of Y, of the residual and the gate are aligned to four, to eight elements
 };
+
+// several elements at once at any element's address
+typedef f32x4_t __attribute__((aligned(4))) f32x4_any;
+typedef u32x2_t __attribute__((aligned(2))) u32x2_any;
+typedef u32x4_t __attribute__((aligned(2))) u32x4_any;
 
 // channels o .. o+3 (those below O) of row t
 template <bool F32>
 __device__ __forceinline__ void f8_store4(const F8Epilogue& q, int64_t t, int o, int O, float v0, float v1, float v2, float v3) {
   float v[4] = {v0, v1, v2, v3};
   const int n = O - o < 4 ? O - o : 4;
-  const bool whole = q.vec && n == 4;
+  const bool whole = n == 4;
   if (q.bias) {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
@@ -212,7 +216,7 @@ __device__ __forceinline__ void f8_store4(const F8Epilogue& q, int64_t t, int o,
     } else {
       const uint16_t* r = (const uint16_t*)q.residual + at;
       if (whole) {
-        const u32x2_t w = *(const u32x2_t*)r;
+        const u32x2_t w = *(const u32x2_any*)r;
         v[0] += __uint_as_float(w.x << 16);
         v[1] += __uint_as_float(w.x & 0xFFFF0000u);
         v[2] += __uint_as_float(w.y << 16);
@@ -236,7 +240,7 @@ __device__ __forceinline__ void f8_store4(const F8Epilogue& q, int64_t t, int o,
   if constexpr (F32) {
     float* y = (float*)q.Y + at;
     if (whole) {
-      *(f32x4_t*)y = f32x4_t{v[0], v[1], v[2], v[3]};
+      *(f32x4_any*)y = f32x4_t{v[0], v[1], v[2], v[3]};
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
@@ -246,7 +250,7 @@ __device__ __forceinline__ void f8_store4(const F8Epilogue& q, int64_t t, int o,
     uint16_t* y = (uint16_t*)q.Y + at;
     const u32x2_t w = {f8_pack_bf16x2(v[0], v[1]), f8_pack_bf16x2(v[2], v[3])};
     if (whole) {
-      *(u32x2_t*)y = w;
+      *(u32x2_any*)y = w;
     } else {
       const uint32_t h[2] = {w.x, w.y};
 #pragma unroll

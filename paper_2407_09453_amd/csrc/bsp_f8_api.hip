@@ -68,7 +68,7 @@ int check_product(const bsp_weights_f8* w, int32_t transposed, int32_t T, const 
   }
   if (T > 0 && !Y) return BSP_ERR_NULL;
   if (!aligned(Y, 16) || !aligned(residual, 16) || !aligned(bias, 4)) return BSP_ERR_ALIGN;
-  *q = F8Epilogue{Y, bias, residual, gate ? gate->codes : nullptr, relu != 0, gate ? gate->dtype == BSP_E5M2 : 0, out % 4 == 0, out % 8 == 0};
+  *q = F8Epilogue{Y, bias, residual, gate ? gate->codes : nullptr, relu != 0, gate ? gate->dtype == BSP_E5M2 : 0};
   return BSP_OK;
 }
 

@@ -43,7 +43,7 @@ __device__ __forceinline__ void store_tile(const F8Epilogue& q, f32x16_t (&acc)[
   const int lane = threadIdx.x & 63;
   constexpr int kLanes = 4 * MO;  // lanes that hold a row's piece, eight channels each
   const int c = o0 + (lane % kLanes) * 8;
-  if (F32 || q.residual || !q.vec8) {  // fp32 through LDS, then four channels at a time
+  if (F32 || q.residual) {  // fp32 through LDS, then four channels at a time
     constexpr int kRow = 32 * MO * 4 + 16;
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -89,19 +89,32 @@ __device__ __forceinline__ void store_tile(const F8Epilogue& q, f32x16_t (&acc)[
         }
         *(u32x2_t*)(lds + (lane & 31) * kRow + (o * 32 + k * 8 + (lane >> 5) * 4) * 2) = u32x2_t{f8_pack_bf16x2(v[0], v[1]), f8_pack_bf16x2(v[2], v[3])};
       }
+    auto rows = [&](auto WHOLE) {  // of whole pieces; or of pieces at any address, which share lines with others
 #pragma unroll 4
-    for (int r = lane / kLanes; r < 32; r += 64 / kLanes) {
-      const int64_t t = t0 + m * 32 + r;
-      u32x4_t v = *(const u32x4_t*)(lds + r * kRow + (lane % kLanes) * 16);
-      if (t >= T || c >= O) continue;
-      if (q.gate) {
-        const u32x2_t g = *(const u32x2_t*)(q.gate + t * (int64_t)f8_blocks(O) * F8_BLOCK + c);
+      for (int r = lane / kLanes; r < 32; r += 64 / kLanes) {
+        const int64_t t = t0 + m * 32 + r;
+        u32x4_t v = *(const u32x4_t*)(lds + r * kRow + (lane % kLanes) * 16);
+        if (t >= T || c >= O) continue;
+        if (q.gate) {
+          const u32x2_t g = *(const u32x2_t*)(q.gate + t * (int64_t)f8_blocks(O) * F8_BLOCK + c);
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (!f8_positive((g[e >> 2] >> (8 * (e & 3))) & 0xFFu, q.gate_e5)) v[e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+          for (int e = 0; e < 8; ++e)
+            if (!f8_positive((g[e >> 2] >> (8 * (e & 3))) & 0xFFu, q.gate_e5)) v[e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+        }
+        uint16_t* y = (uint16_t*)q.Y + t * O + c;
+        if constexpr (decltype(WHOLE)::value) {
+          __builtin_nontemporal_store(v, (u32x4_t*)y);
+        } else if (c + 8 <= O) {
+          *(u32x4_any*)y = v;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (c + e < O) y[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+        }
       }
-      __builtin_nontemporal_store(v, (u32x4_t*)((uint16_t*)q.Y + t * O + c));
-    }
+    };
+    if (O % 8 == 0) rows(std::true_type{});
+    else rows(std::false_type{});
   }
 }
 
@@ -341,7 +354,7 @@ __global__ __launch_bounds__(64 * WO * WT) void f8_wide(TileArgs a) {
   if constexpr (kSplits) {
     if (a.split > 1) {
       const int ld = (a.w.out + 3) & ~3;
-      const F8Epilogue sums{a.part + (int64_t)share * a.T * ld, nullptr, nullptr, nullptr, 0, 0, 1, 0};
+      const F8Epilogue sums{a.part + (int64_t)share * a.T * ld, nullptr, nullptr, nullptr, 0, 0};
       store_tile<MO, MT, true>(sums, acc, lds + wave * kStoreBytes<MO>, a.T, ld, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32);
       return;
     }

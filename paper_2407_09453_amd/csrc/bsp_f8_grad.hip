@@ -21,7 +21,6 @@ constexpr int kTile = kStep * 256;                     // 32 rows of 128 bf16
 
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 typedef const __attribute__((address_space(1))) uint8_t* global_t;
-typedef u32x4_t __attribute__((aligned(2))) u32x4_any;  // sixteen bytes at any bf16's address
 
 __device__ __forceinline__ u32x4_t read_columns(const uint8_t* p) {  // rows +0..3 and +4..7 of this lane's column
   auto* q = (__attribute__((address_space(3))) s16x4_t*)(uintptr_t)p;
@@ -339,23 +338,32 @@ __global__ __launch_bounds__(256) void f8_grad_finish(F8GradArgs a) {
 }
 
 // Kept blocks a workgroup: more of them share a block row's gradients and take longer, so it goes by how often the chip is filled.  A CU holds two workgroups of
-// one or two blocks or one of four; us a step where it is full: 0.62, 0.98, 0.94, and 6 a round to begin and end.  Measured (us for one, two, four
-// blocks): 8192 x 4096 -> 16384 1241 1051 1017, 8192 x 8192 -> 8192 1183 981 971 (930, 1120, 1133 TFLOP/s), half of it kept 663 583 645, 2048 x 4096 -> 4096 84 75 75,
-// half of it kept 59 64 67, 2048 x 4096 -> 4097 104 109 121.
+// one or two blocks or one of four; us a step where it is full: 0.62, 0.98, 0.94, and 6 a round to begin and end.  Measured (us for one, two, four blocks):
+//   all kept: 8192 x 4096 -> 16384 1241 1051 1017, 8192 x 8192 -> 8192 1183 981 971 (930, 1120, 1133 TFLOP/s), 2048 x 4096 -> 4096 84 75 75, 2048 x 4096 -> 4097 104 109 121
+//   under random masks: 8192 x 8192 -> 8192 half 663 583 645, a quarter 386 391 444, 2048 x 4096 -> 4096 half 61 66 67, 3000 x 16384 -> 1024 0.3 57 63 87,
+//   4096 x 4096 -> 4096 a quarter 72 79 113, 0.7 140 120 123, 4052 x 19902 -> 2966 a quarter 256 298 248
 int blocks_each(const F8GradArgs& a) {
   const double steps = (double)(((int64_t)a.T + kStep - 1) / kStep), row = (double)a.nnzb / a.nbo;
   const bool full = a.nnzb == (int64_t)a.nbo * a.nbi;
   int best = 1;
   double least = 1e30;
   for (int c = 1; c <= 4; c *= 2) {
-    // (of rows that keep differing numbers of blocks the last group is half full on average)
-    const double groups = a.nbo * (full ? (double)((a.nbi + c - 1) / c) : row / c + (c - 1) / (2.0 * c));
-    const int64_t slots = c == 4 ? 256 : 512, rounds = (int64_t)(groups / slots);
-    const double left = groups - (double)(rounds * slots);
-    // a last round takes half the time where a CU has one workgroup instead of two, and less than a whole one where most have none
-    const double part = left <= 0 ? 0 : left <= 256 && slots == 512 ? 0.5 : slots == 512 || rounds == 0 ? 1 : 0.7;
     const double step = c == 1 ? 0.62 : c == 2 ? 0.98 : 0.94;
-    const double us = (rounds + part) * steps * step + 6 * (double)(rounds + (left > 0));
+    const int64_t slots = c == 4 ? 256 : 512;
+    double rounds, whole;
+    if (full) {
+      const int64_t groups = (int64_t)a.nbo * ((a.nbi + c - 1) / c), left = groups % slots;
+      // a last round takes half the time where a CU has one workgroup instead of two, and less than a whole one where most have none
+      const double part = left == 0 ? 0 : left <= 256 && slots == 512 ? 0.5 : slots == 512 || groups < slots ? 1 : 0.7;
+      rounds = (double)(groups / slots) + part, whole = (double)((groups + slots - 1) / slots);
+    } else {
+      // rows keep differing numbers of blocks: the last group of a row is half full on average, and XCDs have more or fewer, which the smaller workgroups even out
+      whole = a.nbo * (row / c + (c - 1) / (2.0 * c)) / (double)slots;
+      rounds = c == 1 ? 1.07 * whole : whole + (c == 2 ? 0.25 : 0.4);
+      const double lowest = c == 1 ? 0.7 : c == 2 ? 0.5 : 0.8;
+      if (rounds < lowest) rounds = lowest;
+    }
+    const double us = rounds * steps * step + 6 * whole;
     if (us < least) least = us, best = c;
   }
   return best;
