@@ -31,32 +31,44 @@ __device__ __forceinline__ u32x4_t read_columns(const uint8_t* p) {  // rows +0.
 
 __device__ __forceinline__ int chunk_key(int t) { return (t & 3) << 1 | ((t >> 3) & 1); }
 
-// eight gradients o .. o+7 of a row, those past the last channel 0
-__device__ __forceinline__ u32x4_t gradients8(const uint16_t* row, int o, int O) {
-  if (o + 8 <= O) return *(const u32x4_any*)(row + o);
+// the gradients of a row of fewer than eight, and zeros
+__device__ __forceinline__ u32x4_t gradients_few(const uint16_t* row, int O) {
   uint32_t v[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    v[k] = row[o + k < O ? o + k : O - 1];
-    v[k] = o + k < O ? v[k] : 0;
+    v[k] = row[k < O ? k : O - 1];
+    v[k] = k < O ? v[k] : 0;
   }
   return u32x4_t{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16};
 }
 
-// Column sums of one block row's gradients over one range of rows: a thread adds eight columns of every 32nd row.
+// Column sums of one block row's gradients over one range of rows: a thread adds eight columns of every 32nd (16th) row, eight rows asked for
+// at once (2966 columns of 4052 rows: 22 us; one by one where a row ends inside a thread's columns 180).
 template <int THREADS>
 __device__ __forceinline__ void column_sums(const F8GradArgs& a, int br, int64_t t_begin, int64_t t_end, float* sums) {
+  constexpr int kRows = THREADS / 16, kAtOnce = 8;
   const int piece = threadIdx.x & 15, o = br * F8_BLOCK + piece * 8;
+  const int from = o + 8 <= a.O || a.O < 8 ? o : a.O - 8;  // at a row's end its last eight
   float s[8] = {};
-  if (o < a.O)
-#pragma unroll 4
-    for (int64_t t = t_begin + (threadIdx.x >> 4); t < t_end; t += THREADS / 16) {
-      const u32x4_t v = gradients8(a.dY + t * a.ldy, o, a.O);
+  auto add = [&](auto get) {
+    for (int64_t t = t_begin + (threadIdx.x >> 4); t < t_end; t += kRows * kAtOnce) {
+      u32x4_t v[kAtOnce];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s[k] += __uint_as_float(k & 1 ? v[k >> 1] & 0xFFFF0000u : v[k >> 1] << 16);
+      for (int j = 0; j < kAtOnce; ++j) v[j] = get(a.dY + (t + j * kRows < t_end ? t + j * kRows : t_end - 1) * a.ldy);
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[k] += t + j * kRows < t_end ? __uint_as_float(k & 1 ? v[j][k >> 1] & 0xFFFF0000u : v[j][k >> 1] << 16) : 0.f;
     }
+  };
+  if (a.O < 8) {
+    if (o < a.O) add([&](const uint16_t* row) { return gradients_few(row, a.O); });
+  } else if (o < a.O) {
+    add([&](const uint16_t* row) { return u32x4_t(*(const u32x4_any*)(row + from)); });
+  }
 #pragma unroll
-  for (int k = 0; k < 8; ++k) sums[(threadIdx.x >> 4) * 129 + piece * 8 + k] = s[k];
+  for (int k = 0; k < 8; ++k)
+    if (from + k >= o) sums[(threadIdx.x >> 4) * 129 + (from + k - br * F8_BLOCK)] = s[k];
   __syncthreads();
   if (threadIdx.x < F8_BLOCK && br * F8_BLOCK + (int)threadIdx.x < a.O) {
     float v = 0.f;
@@ -146,7 +158,7 @@ __global__ __launch_bounds__(kThreads<C>, C == 1 ? 4 : 2) void f8_grad(F8GradArg
     asm volatile("" : "+s"(by), "+s"(bx), "+s"(bs));
 #pragma unroll
     for (int q = 0; q < kYs; ++q) {
-      if constexpr (THIN) y_in[j][q] = gradients8((const uint16_t*)by + r * a.ldy, 0, a.O);
+      if constexpr (THIN) y_in[j][q] = gradients_few((const uint16_t*)by + r * a.ldy, a.O);
       else {
         uint32_t at = r * (uint32_t)a.ldy * 2 + col_y[q];
         asm volatile("" : "+v"(at));
@@ -317,24 +329,40 @@ __global__ __launch_bounds__(kThreads<C>, C == 1 ? 4 : 2) void f8_grad(F8GradArg
 }
 
 // The sums over the ranges of rows, in their order: a kept block's entries, zeros for the others, and the bias's gradient.  A workgroup
-// takes two rows of a block, a thread one entry.
+// takes eight rows of a block at a time, a thread four entries; every sixteenth of the rows, or (many blocks, most of them zeros: the start
+// of a workgroup is what counts: 24 x 156 blocks of which 37 are kept, 4052 rows, 183 us for the call with two rows a workgroup, 93 so) every fourth.
 __global__ __launch_bounds__(256) void f8_grad_finish(F8GradArgs a) {
-  const int cell = blockIdx.x, br = cell / a.nbi, kb = cell - br * a.nbi, c = threadIdx.x & 127;
-  auto sum = [&](const float* p, int64_t step) {
+  const int cell = blockIdx.x, br = cell / a.nbi, kb = cell - br * a.nbi, c = (threadIdx.x & 31) * 4;
+  if (a.db && kb == 0 && blockIdx.y == 0 && threadIdx.x < F8_BLOCK && br * F8_BLOCK + (int)threadIdx.x < a.O) {
+    const float* p = a.part_db + br * F8_BLOCK + threadIdx.x;
     float v = 0.f;
 #pragma unroll 16
-    for (int s = 0; s < a.split; ++s) v += p[s * step];
-    return v;
-  };
-  if (a.db && kb == 0 && blockIdx.y == 0 && threadIdx.x < F8_BLOCK && br * F8_BLOCK + c < a.O) a.db[br * F8_BLOCK + c] = sum(a.part_db + br * F8_BLOCK + c, a.O);
-  const int n0 = a.row_ptr[br], n1 = a.row_ptr[br + 1], r = (int)blockIdx.y * 2 + (threadIdx.x >> 7);
+    for (int s = 0; s < a.split; ++s) v += p[s * (int64_t)a.O];
+    a.db[br * F8_BLOCK + threadIdx.x] = v;
+  }
+  const int n0 = a.row_ptr[br], n1 = a.row_ptr[br + 1];
   int n = -1;
   for (int i = n0 + (threadIdx.x & 63); i < n1; i += 64) n = a.col_idx[i] == kb ? i : n;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) n = max(n, __shfl_xor(n, d));
-  const int64_t o = (int64_t)br * F8_BLOCK + r;
-  if (!a.dW || o >= a.O || kb * F8_BLOCK + c >= a.I) return;
-  a.dW[o * a.I + kb * F8_BLOCK + c] = n < 0 ? 0.f : sum(a.part + (int64_t)n * F8_BLOCK_BYTES + r * F8_BLOCK + c, a.nnzb * F8_BLOCK_BYTES);
+  const int left = a.I - kb * F8_BLOCK - c;  // columns from this thread's on
+  if (!a.dW || left <= 0) return;
+  for (int r = (int)blockIdx.y * 8 + (threadIdx.x >> 5); r < F8_BLOCK && br * F8_BLOCK + r < a.O; r += gridDim.y * 8) {
+    f32x4_t v = {};
+    if (n >= 0) {
+      const float* p = a.part + (int64_t)n * F8_BLOCK_BYTES + r * F8_BLOCK + c;
+#pragma unroll 8
+      for (int s = 0; s < a.split; ++s) v += *(const f32x4_any*)(p + s * (a.nnzb * F8_BLOCK_BYTES));
+    }
+    float* out = a.dW + ((int64_t)br * F8_BLOCK + r) * a.I + (int64_t)kb * F8_BLOCK + c;
+    if (left >= 4) {
+      *(f32x4_any*)out = v;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < left) out[k] = v[k];
+    }
+  }
 }
 
 // Kept blocks a workgroup: more of them share a block row's gradients and take longer, so it goes by how often the chip is filled.  A CU holds two workgroups of
@@ -399,6 +427,6 @@ int f8_launch_grad(const F8GradArgs& a, hipStream_t st) {
     default: rc = a.e5 ? launch<1, true>(a, st) : launch<1, false>(a, st);
   }
   if (rc != BSP_OK || a.split == 1) return rc;
-  hipLaunchKernelGGL(f8_grad_finish, dim3((unsigned)(a.nbo * a.nbi), F8_BLOCK / 2), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(f8_grad_finish, dim3((unsigned)(a.nbo * a.nbi), a.nbo * a.nbi >= 1024 ? 4 : 16), dim3(256), 0, st, a);
   return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP;
 }
