@@ -78,19 +78,19 @@ __device__ __forceinline__ void column_sums(const F8GradArgs& a, int br, int64_t
   }
 }
 
-// THIN: fewer than eight outputs, read one by one
-// Eight waves; of two blocks four, and two such workgroups on a CU, whose barriers then do not keep all waves of a SIMD in step (us at 8192 x 4096 -> 16384 and on half
-// of the blocks of 8192 x 8192 -> 8192: 1115 and 607 with eight waves of half as many outputs, 1051 and 583).
-template <int C>
-constexpr int kThreads = C == 2 ? 256 : 512;
-template <int C, bool E5, bool THIN>
-__global__ __launch_bounds__(kThreads<C>, C == 1 ? 4 : 2) void f8_grad(F8GradArgs a) {
-  constexpr int THREADS = kThreads<C>;
-  constexpr int MO = C == 2 ? 4 : C, WO = 4 / MO;  // 32-row tiles of outputs a wave, waves side by side over the 128 outputs
+// C blocks on WAVES waves: four and two of the workgroups, or three of one block, on a CU, or eight and one, or two of one block.  Four waves of one workgroup and four of
+// another do not keep in step from barrier to barrier, and read less of LDS for each product (us at 2048 x 4096 -> 4096 half kept, one block: 61 on eight waves, 57.6
+// on four; 4096 x 8192 -> 2048 110 and 102; 8192 x 4096 -> 16384, two blocks: 1115 and 1051); where a workgroup has a CU to itself eight waves are faster (37, 1000 x 520
+// 7.9 and 9.8), and of four blocks four waves would be one a SIMD.
+// E5: e5m2 codes.  THIN: fewer than eight outputs, read one by one.
+template <int C, int WAVES, bool E5, bool THIN>
+__global__ __launch_bounds__(64 * WAVES, C > 1 ? 2 : WAVES == 4 ? 3 : 4) void f8_grad(F8GradArgs a) {
+  constexpr int THREADS = 64 * WAVES;
+  constexpr int MO = 8 * C / WAVES, WO = 4 / MO;  // 32-row tiles of outputs a wave, waves side by side over the 128 outputs
   constexpr int kBuffer = (1 + C) * kTile;
-  constexpr int kAhead = C >= 2 ? 2 : 4;  // steps that are on their way to registers (the accumulators of four blocks leave room for two)
+  constexpr int kAhead = MO > 1 ? 2 : 4;  // steps that are on their way to registers (the accumulators of four blocks leave room for two)
   constexpr int kRow = THREADS / kStep, kYs = 16 / kRow;  // threads that bring a row; of eight gradients each
-  constexpr int kCodes = C > 1 ? 16 : 8, kPieces = C * F8_BLOCK / kCodes / kRow, kApart = kRow * kCodes / F8_BLOCK;  // runs of codes a thread brings, each a block, or two, on
+  constexpr int kCodes = MO > 1 ? 16 : 8, kPieces = C * F8_BLOCK / kCodes / kRow, kApart = kRow * kCodes / F8_BLOCK;  // runs of codes a thread brings, each a block, or two, on
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   kernarg_touch<F8GradArgs>();
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(kThreads<C>, C == 1 ? 4 : 2) void f8_grad(F8GradArg
   for (int q = 0; q < kYs; ++q) {
     const int o = br * F8_BLOCK + (piece + q * kRow) * 8;
     col_y[q] = (uint32_t)(o + 8 <= a.O || THIN ? o : a.O - 8) * 2;
-    past[q] = o + 8 <= a.O || (THIN && piece == 0) ? 0 : o + 8 - a.O < 8 ? o + 8 - a.O : 8;
+    past[q] = o + 8 <= a.O || (THIN && piece + q == 0) ? 0 : o + 8 - a.O < 8 ? o + 8 - a.O : 8;
   }
   const int64_t Kp = (int64_t)f8_blocks(a.I) * F8_BLOCK, srows = f8_scale_rows(a.T);
   const int j_in = (piece * kCodes) >> 7, at_in = (piece * kCodes) & 127;  // the first run's block, and its columns in that; the next lies two blocks on
@@ -398,34 +398,44 @@ int blocks_each(const F8GradArgs& a) {
   return best;
 }
 
-template <int C, bool E5, bool THIN = false>
+template <int C, int WAVES, bool E5, bool THIN = false>
 int launch(F8GradArgs a, hipStream_t st) {
   constexpr int lds = 2 * (1 + C) * kTile;
-  static const bool raised = hipFuncSetAttribute((const void*)&f8_grad<C, E5, THIN>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
+  static const bool raised = hipFuncSetAttribute((const void*)&f8_grad<C, WAVES, E5, THIN>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
   if (!raised) return BSP_ERR_HIP;
   a.groups = a.dW ? (a.nbi + C - 1) / C : 0;
   const int64_t groups = ((int64_t)a.nbo * ((a.groups + 3) / 4) + 7) / 8 * 32;
   if (groups + a.nbo > INT32_MAX) return BSP_ERR_SHAPE;
-  hipLaunchKernelGGL((f8_grad<C, E5, THIN>), dim3((unsigned)(groups + (a.db ? a.nbo : 0)), (unsigned)a.split), dim3(kThreads<C>), lds, st, a);
+  hipLaunchKernelGGL((f8_grad<C, WAVES, E5, THIN>), dim3((unsigned)(groups + (a.db ? a.nbo : 0)), (unsigned)a.split), dim3(64 * WAVES), lds, st, a);
   return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP;
 }
 
 }  // namespace
 
-// ... and where even single blocks are too few, ranges of at least four steps that together give the chip a workgroup a CU.
+// ... and where single blocks are a workgroup for every other CU or fewer, ranges of at least four steps: a step takes 0.5 us where a CU has one workgroup, 0.65 where it has two, and
+// the ranges' sums cost a launch and are written and read (us at 16384 rows, 1024 x 1024 in 4 and 8 ranges 74 and 59, 2048 x 1024 in 2 and 4 135 and 97; 2000 rows, 51
+// blocks of 4096 x 4096 in 5 and 10 39 and 51).
 int f8_grad_split(int64_t nnzb, int T) {
-  const int64_t most = (int64_t)T / (4 * kStep), want = nnzb > 0 ? 256 / nnzb : 1;
-  const int64_t s = want < most ? want : most;
-  return s < 1 ? 1 : (int)s;
+  const int64_t steps = ((int64_t)T + kStep - 1) / kStep;
+  if (nnzb == 0 || nnzb > 128) return 1;
+  int best = 1;
+  double least = 0.5 * (double)steps;
+  for (int64_t s = 2; s * 4 <= T / kStep && s * nnzb <= 512; s += 1 + s / 16) {
+    const double us = (double)((steps + s - 1) / s) * (s * nnzb <= 256 ? 0.5 : 0.65) + 4 + 0.033 * (double)(nnzb * s);
+    if (us < least) least = us, best = (int)s;
+  }
+  return best;
 }
 
 int f8_launch_grad(const F8GradArgs& a, hipStream_t st) {
   int rc;
-  if (a.O < 8) rc = a.e5 ? launch<1, true, true>(a, st) : launch<1, false, true>(a, st);
+  if (a.O < 8) rc = a.e5 ? launch<1, 8, true, true>(a, st) : launch<1, 8, false, true>(a, st);
   else switch (a.split > 1 ? 1 : blocks_each(a)) {
-    case 4: rc = a.e5 ? launch<4, true>(a, st) : launch<4, false>(a, st); break;
-    case 2: rc = a.e5 ? launch<2, true>(a, st) : launch<2, false>(a, st); break;
-    default: rc = a.e5 ? launch<1, true>(a, st) : launch<1, false>(a, st);
+    case 4: rc = a.e5 ? launch<4, 8, true>(a, st) : launch<4, 8, false>(a, st); break;
+    case 2: rc = a.e5 ? launch<2, 4, true>(a, st) : launch<2, 4, false>(a, st); break;
+    default:
+      if (a.split == 1 && a.nnzb > 256) rc = a.e5 ? launch<1, 4, true>(a, st) : launch<1, 4, false>(a, st);
+      else rc = a.e5 ? launch<1, 8, true>(a, st) : launch<1, 8, false>(a, st);
   }
   if (rc != BSP_OK || a.split == 1) return rc;
   hipLaunchKernelGGL(f8_grad_finish, dim3((unsigned)(a.nbo * a.nbi), a.nbo * a.nbi >= 1024 ? 4 : 16), dim3(256), 0, st, a);
