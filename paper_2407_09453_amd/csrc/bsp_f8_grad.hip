@@ -46,7 +46,7 @@ __device__ __forceinline__ u32x4_t gradients_few(const uint16_t* row, int O) {
 // Column sums of one block row's gradients over one range of rows: a thread adds eight columns of every 32nd (16th) row, eight rows asked for
 // at once (2966 columns of 4052 rows: 22 us; one by one where a row ends inside a thread's columns 180).
 template <int THREADS>
-__device__ __forceinline__ void column_sums(const F8GradArgs& a, int br, int64_t t_begin, int64_t t_end, float* sums) {
+__device__ __forceinline__ void column_sums(const F8GradArgs& a, int br, int range, int64_t t_begin, int64_t t_end, float* sums) {
   constexpr int kRows = THREADS / 16, kAtOnce = 8;
   const int piece = threadIdx.x & 15, o = br * F8_BLOCK + piece * 8;
   const int from = o + 8 <= a.O || a.O < 8 ? o : a.O - 8;  // at a row's end its last eight
@@ -74,7 +74,7 @@ __device__ __forceinline__ void column_sums(const F8GradArgs& a, int br, int64_t
   if (threadIdx.x < F8_BLOCK && br * F8_BLOCK + (int)threadIdx.x < a.O) {
     float v = 0.f;
     for (int r = 0; r < THREADS / 16; ++r) v += sums[r * 129 + threadIdx.x];
-    (a.split == 1 ? a.db : a.part_db + (int64_t)blockIdx.y * a.O)[br * F8_BLOCK + threadIdx.x] = v;
+    (a.split == 1 ? a.db : a.part_db + (int64_t)range * a.O)[br * F8_BLOCK + threadIdx.x] = v;
   }
 }
 
@@ -96,14 +96,20 @@ __global__ __launch_bounds__(64 * WAVES, C > 1 ? 2 : WAVES == 4 ? 3 : 4) void f8
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int groups = a.groups;  // of C blocks in a block row; 0: the column sums alone are wanted
   const int steps = (int)(((int64_t)a.T + kStep - 1) / kStep), per = (steps + a.split - 1) / a.split;
-  const int64_t t_begin = (int64_t)blockIdx.y * per * kStep;
+  // Ranges of rows in eights: each XCD (workgroups go to the eight in turn) takes its own, with all the blocks, which share what they read in its L2.
+  int b = blockIdx.x, range = blockIdx.y;
+  if ((a.split & 7) == 0) {
+    const unsigned id = blockIdx.y * gridDim.x + blockIdx.x, j = id >> 3, turn = j / gridDim.x;
+    range = (int)(turn * 8 + (id & 7)), b = (int)(j - turn * gridDim.x);
+  }
+  const int64_t t_begin = (int64_t)range * per * kStep;
   const int64_t t_end = t_begin + (int64_t)per * kStep < a.T ? t_begin + (int64_t)per * kStep : a.T;
   // Workgroups go to the eight XCDs in turn.  Four neighbouring groups of a block row go to one, with the same groups of seven other rows: what an
   // XCD runs at one time shares eight rows' gradients and four groups' codes in its L2.  Block rows are dealt to the XCDs one by
   // one, so that rows that keep more blocks than others do not meet on one.
-  const int b = blockIdx.x, quads = (groups + 3) >> 2, clusters = quads * a.nbo, behind = (clusters + 7) / 8 * 32;
+  const int quads = (groups + 3) >> 2, clusters = quads * a.nbo, behind = (clusters + 7) / 8 * 32;
   if (b >= behind) {  // the workgroups behind: one block row's column sums each
-    column_sums<THREADS>(a, b - behind, t_begin, t_end, (float*)lds);
+    column_sums<THREADS>(a, b - behind, range, t_begin, t_end, (float*)lds);
     return;
   }
   const int cluster = (b >> 5) * 8 + (b & 7), quad = cluster / a.nbo, br = cluster - quad * a.nbo;
@@ -313,7 +319,7 @@ __global__ __launch_bounds__(64 * WAVES, C > 1 ? 2 : WAVES == 4 ? 3 : 4) void f8
   const int kb = a.col_idx[n0 + first + (wi >> 1)];
   const bool whole = a.split == 1;
   float* out = whole ? a.dW + (int64_t)br * F8_BLOCK * a.I + (int64_t)kb * F8_BLOCK
-                     : a.part + ((int64_t)blockIdx.y * a.nnzb + n0 + first + (wi >> 1)) * F8_BLOCK_BYTES;
+                     : a.part + ((int64_t)range * a.nnzb + n0 + first + (wi >> 1)) * F8_BLOCK_BYTES;
   const int64_t ld = whole ? a.I : F8_BLOCK;
   const int rows = whole ? a.O - br * F8_BLOCK : F8_BLOCK, cols = whole ? a.I - kb * F8_BLOCK : F8_BLOCK;
 #pragma unroll
@@ -413,14 +419,15 @@ int launch(F8GradArgs a, hipStream_t st) {
 }  // namespace
 
 // ... and where single blocks are a workgroup for every other CU or fewer, ranges of at least four steps: a step takes 0.5 us where a CU has one workgroup, 0.65 where it has two, and
-// the ranges' sums cost a launch and are written and read (us at 16384 rows, 1024 x 1024 in 4 and 8 ranges 74 and 59, 2048 x 1024 in 2 and 4 135 and 97; 2000 rows, 51
+// the ranges' sums cost a launch and are written and read (us at 16384 rows, 1024 x 1024 in 4 and 8 ranges 74 and 55, 2048 x 1024 in 2 and 4 135 and 101; 2000 rows, 51
 // blocks of 4096 x 4096 in 5 and 10 39 and 51).
 int f8_grad_split(int64_t nnzb, int T) {
   const int64_t steps = ((int64_t)T + kStep - 1) / kStep;
   if (nnzb == 0 || nnzb > 128) return 1;
   int best = 1;
   double least = 0.5 * (double)steps;
-  for (int64_t s = 2; s * 4 <= T / kStep && s * nnzb <= 512; s += 1 + s / 16) {
+  for (int64_t s = 2; s * 4 <= T / kStep && s * nnzb <= 512; ++s) {
+    if (s > 8 && (s & 7)) continue;
     const double us = (double)((steps + s - 1) / s) * (s * nnzb <= 256 ? 0.5 : 0.65) + 4 + 0.033 * (double)(nnzb * s);
     if (us < least) least = us, best = (int)s;
   }
