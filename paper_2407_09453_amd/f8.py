@@ -159,8 +159,8 @@ class BspLayerF8:
         self.device, self._index = self.payload.device, self.payload.get_device()
         self._workspace = {}  # bytes that a call takes, by its kind and rows
         self.d_bias = None
-        if bias is not None:
-            b = torch.as_tensor(bias, dtype=torch.float32).to(self.device).contiguous()
+        if bias is not None:  # (a copy, as the weights' codes are: the caller's tensor stays the caller's)
+            b = torch.as_tensor(bias).detach().to(self.device, torch.float32, copy=True, memory_format=torch.contiguous_format)
             assert b.shape == (O,)
             self.d_bias = b
         self.update(W)
