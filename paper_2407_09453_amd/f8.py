@@ -161,22 +161,26 @@ class BspLayerF8:
         self.d_bias = None
         if bias is not None:  # (a copy, as the weights' codes are: the caller's tensor stays the caller's)
             b = torch.as_tensor(bias).detach().to(self.device, torch.float32, copy=True, memory_format=torch.contiguous_format)
-            assert b.shape == (O,)
+            assert b.shape == (O,), "a bias [%d]" % O
             self.d_bias = b
         self.update(W)
 
     def update(self, W, bias=None, stream=None) -> None:
-        """Take new weights (same shape, same mask), and a new bias where one is given, as after a step of an optimiser."""
+        """Take new weights (same shape, same mask), and a new bias where one is given (to a layer that was made with one), as
+        after a step of an optimiser."""
         import torch
-        if bias is not None:
-            self.d_bias.copy_(torch.as_tensor(bias, dtype=torch.float32))
         if not isinstance(W, torch.Tensor):
             W = torch.from_numpy(np.ascontiguousarray(W, dtype=np.float32))
         W = W.to(self.device)
         O, I, ld = _rows(W)
         assert (O, I) == (self.O, self.I)
+        kind = _type(W)
+        if bias is not None:
+            b = torch.as_tensor(bias).detach()
+            assert self.d_bias is not None and b.shape == (O,), "a bias [%d] for a layer made with one" % O
+            self.d_bias.copy_(b)
         st = _current_stream(W) if stream is None else stream
-        _check(load_library().bsp_f8_pack(self.struct, W.data_ptr(), _type(W), ld, st), "bsp_f8_pack")
+        _check(load_library().bsp_f8_pack(self.struct, W.data_ptr(), kind, ld, st), "bsp_f8_pack")
         _keep(W, stream)
 
     def _bytes(self, kind, T):

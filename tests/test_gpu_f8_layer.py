@@ -56,3 +56,27 @@ def test_biases_of_other_places_and_types():
     for b in (v.astype(np.float32), v.astype(np.float64), [float(k) for k in v], torch.from_numpy(v).to(torch.bfloat16).cuda(),
               torch.from_numpy(np.repeat(v, 2).astype(np.float32)).cuda()[::2], torch.from_numpy(v.astype(np.float32))):
         assert (_host(bsp.BspLayerF8(W, bias=b).fc(t)) == x + v).all()
+
+
+def test_new_biases_are_refused_or_taken_whole():
+    """A bias of another shape, or one for a layer that has none, is an error that names it; the layer stays as it was."""
+    import torch
+    bsp = _bsp()
+    W = np.eye(128, dtype=np.float32)
+    x, t = _whole(2, 128, 3)
+    layer = bsp.BspLayerF8(W, bias=np.full(128, 2.0, np.float32))
+    for b in (torch.ones(1, device="cuda"), torch.tensor(1.0, device="cuda"), [1.0], torch.ones(1, 128, device="cuda"), np.ones(127, np.float32)):
+        with pytest.raises(AssertionError, match="bias"):
+            layer.update(2 * W, bias=b)
+        assert (_host(layer.fc(t)) == x + 2).all()
+    for b in (np.arange(128, dtype=np.float64) % 8, torch.arange(128, device="cuda") % 8):
+        layer.update(2 * W, bias=b)
+        assert (_host(layer.fc(t)) == 2 * x + np.arange(128) % 8).all()
+    plain = bsp.BspLayerF8(W)
+    with pytest.raises(AssertionError, match="bias"):
+        plain.update(2 * W, bias=np.ones(128, np.float32))
+    assert (_host(plain.fc(t)) == x).all()
+    for wrong in (np.ones((127, 128), np.float32), torch.ones(128, 128, device="cuda", dtype=torch.float64)):  # no half of an update
+        with pytest.raises(AssertionError):
+            layer.update(wrong, bias=np.full(128, 7.0, np.float32))
+        assert (_host(layer.fc(t)) == 2 * x + np.arange(128) % 8).all()
