@@ -108,13 +108,15 @@ class BspCodes:
         return out
 
 
-def save8(X, kind: str = "e4m3", out: Optional[BspCodes] = None, stream=None) -> BspCodes:
-    """The 8-bit checkpoint of X (torch tensor [T][K], fp32 or bf16, rows contiguous)."""
+def save8(X, kind: Optional[str] = None, out: Optional[BspCodes] = None, stream=None) -> BspCodes:
+    """The 8-bit checkpoint of X (torch tensor [T][K], fp32 or bf16, rows contiguous), in codes of type ``kind``: e4m3 where none
+    is asked for, or the type of ``out``."""
     T, K, ld = _rows(X)
     if out is None:
-        out = BspCodes(T, K, kind, X.device)
+        out = BspCodes(T, K, kind or "e4m3", X.device)
     else:
         assert (out.T, out.K) == (T, K)
+        assert kind is None or kind == out.kind, "codes of %s asked for in a checkpoint of %s" % (kind, out.kind)
         _on(X, out.buffer)
     st = _current_stream(X) if stream is None else stream
     _call(_SAVE, _pack9(X.data_ptr(), _type(X), ld, *out.words, st), "bsp_f8_save")

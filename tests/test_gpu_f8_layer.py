@@ -80,3 +80,20 @@ def test_new_biases_are_refused_or_taken_whole():
         with pytest.raises(AssertionError):
             layer.update(wrong, bias=np.full(128, 7.0, np.float32))
         assert (_host(layer.fc(t)) == 2 * x + np.arange(128) % 8).all()
+
+
+def test_a_checkpoint_given_is_of_the_type_asked_for():
+    """save8 into a BspCodes: its own type where none is asked for, an error where another is, nothing written."""
+    import torch
+    bsp = _bsp()
+    t = torch.randn(5, 200, device="cuda")
+    for have, other in (("e4m3", "e5m2"), ("e5m2", "e4m3")):
+        c = bsp.BspCodes(5, 200, have)
+        c.buffer.fill_(77)
+        with pytest.raises(AssertionError, match=have):
+            bsp.save8(t, other, out=c)
+        assert bool((c.buffer == 77).all())
+        want = bsp.save8(t, have)
+        for got in (bsp.save8(t, out=c), bsp.save8(t, have, out=c)):
+            assert got is c and torch.equal(c.codes, want.codes) and torch.equal(c.scale, want.scale)
+    assert bsp.save8(t).kind == "e4m3"
