@@ -1,6 +1,10 @@
 """FC layers in 8-bit floating point, the 8-bit checkpoints of their inputs, their gradients, and layer norm, on torch
-tensors.  Marshalling only: every call launches on the current stream (or ``stream``, a handle as an integer) of its tensors'
-device and returns before it is done; tensors that it makes come from torch's allocator on the current stream.
+tensors.  Marshalling only: every call launches on the current stream of its tensors' device and returns before it is done;
+tensors that it makes come from torch's allocator on that stream.
+
+With ``stream`` (a handle as an integer) a call does as under ``torch.cuda.stream`` of that stream: what it reads has to be
+ready there, and whoever uses its results elsewhere waits for it.  Nothing has to be kept until then: what it reads
+may be dropped at once, and so may its results behind uses in the stream that was current at the call.
 
 A call's arguments go to the library as one string of words: of a small layer's 9 us on the host ctypes' conversion of 16 arguments
 one by one took 2, and a tensor of torch's takes 1.5 us to make, so a checkpoint is one allocation."""
@@ -58,10 +62,42 @@ def _call(call, words, name):
 
 
 def _keep(t, stream):
-    """A workspace that is dropped while its kernels may still wait in a stream other than torch's current one."""
-    if stream is not None and t is not None:
+    """A tensor that is dropped while its kernels may still wait in a stream other than torch's current one."""
+    if stream is not None:
         import torch
         t.record_stream(torch.cuda.ExternalStream(int(stream), device=t.device))
+
+
+def _memory(v):
+    """The tensors on a GPU that an argument or a result is held in."""
+    if isinstance(v, (tuple, list)):
+        for x in v:
+            yield from _memory(x)
+    elif isinstance(v, BspCodes):
+        yield v.buffer
+    elif isinstance(v, BspLayerF8):
+        yield from _memory((v.payload, v.scale, v.payload_t, v.scale_t, v.d_index, v.d_bias))
+    elif getattr(v, "is_cuda", False):
+        yield v
+
+
+def _on_stream(stream, at, call, *args):
+    """call(*args) in the stream of this handle, on the device of tensor ``at``.  Workspaces and results come from the allocator's pool of
+    that stream: a block of the current stream's pool may be one that was dropped there with work on it still to come, which
+    the call, elsewhere, would not wait for."""
+    import torch
+    here = torch.cuda.current_stream(at.device)
+    if int(stream) == here.cuda_stream:
+        return call(*args)
+    # (an ExternalStream of no handle is not the default stream, but any of torch's)
+    there = torch.cuda.ExternalStream(int(stream), device=at.device) if int(stream) else torch.cuda.default_stream(at.device)
+    with torch.cuda.stream(there):
+        result = call(*args)
+    for t in _memory((getattr(call, "__self__", None), args)):
+        t.record_stream(there)
+    for t in _memory(result):
+        t.record_stream(here)
+    return result
 
 
 class BspCodes:
@@ -95,6 +131,8 @@ class BspCodes:
 
     def load(self, dtype=None, out=None, stream=None):
         """The values, as bf16 (or torch.float32)."""
+        if stream is not None:
+            return _on_stream(stream, self.buffer, self.load, dtype, out)
         if out is None:
             import torch
             out = torch.empty((self.T, self.K), dtype=dtype or torch.bfloat16, device=self.buffer.device)
@@ -103,14 +141,15 @@ class BspCodes:
             T, K, ld = _rows(out)
             assert (T, K) == (self.T, self.K)
             _on(self.buffer, out)
-        st = _current_stream(out) if stream is None else stream
-        _call(_LOAD, _pack9(*self.words, out.data_ptr(), _type(out), ld, st), "bsp_f8_load")
+        _call(_LOAD, _pack9(*self.words, out.data_ptr(), _type(out), ld, _current_stream(out)), "bsp_f8_load")
         return out
 
 
 def save8(X, kind: Optional[str] = None, out: Optional[BspCodes] = None, stream=None) -> BspCodes:
     """The 8-bit checkpoint of X (torch tensor [T][K], fp32 or bf16, rows contiguous), in codes of type ``kind``: e4m3 where none
     is asked for, or the type of ``out``."""
+    if stream is not None:
+        return _on_stream(stream, X, save8, X, kind, out)
     T, K, ld = _rows(X)
     if out is None:
         out = BspCodes(T, K, kind or "e4m3", X.device)
@@ -118,8 +157,7 @@ def save8(X, kind: Optional[str] = None, out: Optional[BspCodes] = None, stream=
         assert (out.T, out.K) == (T, K)
         assert kind is None or kind == out.kind, "codes of %s asked for in a checkpoint of %s" % (kind, out.kind)
         _on(X, out.buffer)
-    st = _current_stream(X) if stream is None else stream
-    _call(_SAVE, _pack9(X.data_ptr(), _type(X), ld, *out.words, st), "bsp_f8_save")
+    _call(_SAVE, _pack9(X.data_ptr(), _type(X), ld, *out.words, _current_stream(X)), "bsp_f8_save")
     return out
 
 
@@ -198,7 +236,7 @@ class BspLayerF8:
             n = self._workspace[(kind, T)] = n.value
         return n
 
-    def _multiply(self, transposed, X, code, bias, residual, relu, gate, dtype, out, stream):
+    def _multiply(self, transposed, X, code, bias, residual, relu, gate, dtype, out):
         codes = type(X) is BspCodes
         if codes:
             T, K, at = X.T, X.K, X.buffer
@@ -223,7 +261,7 @@ class BspLayerF8:
         if gate is not None:
             _on(at, gate.buffer)
             g = gate.words
-        st = _current_stream(out) if stream is None else stream
+        st = _current_stream(out)
         if codes:
             n = self._bytes(transposed * 2 + 1, T)
         else:  # (few whole rows become codes inside the product's kernel)
@@ -236,25 +274,29 @@ class BspLayerF8:
             _call(_FC, _pack20(self._address, transposed, *X.words, *rest), "bsp_f8_fc")
         else:
             _call(_VALUES, _pack20(self._address, transposed, x, _type(X), ld, T, CODES[code], *rest), "bsp_f8_fc_values")
-        if stream is not None:
-            _keep(ws, stream)
         return out
 
     def fc(self, X, relu=False, residual=None, dtype=None, out=None, stream=None):
         """Y [T][O] = act(X W^t + b + residual) for X [T][I]: a torch tensor (fp32 or bf16, brought to e4m3 codes within the
         call; Y has its type unless ``dtype`` says otherwise) or a BspCodes (Y is bf16 unless ``dtype`` says otherwise)."""
-        return self._multiply(0, X, "e4m3", self.d_bias, residual, relu, None, dtype, out, stream)
+        if stream is not None:
+            return _on_stream(stream, self.payload, self.fc, X, relu, residual, dtype, out)
+        return self._multiply(0, X, "e4m3", self.d_bias, residual, relu, None, dtype, out)
 
     def grad_input(self, dY, relu_of: Optional[BspCodes] = None, code: str = "e5m2", dtype=None, out=None, stream=None):
         """dX [T][I] = dY W for dY [T][O] (brought to codes of type ``code`` within the call, or a BspCodes).  ``relu_of``: the
         checkpoint of this layer's input, where that is a ReLU's output; the result is then the gradient of what went
         into the ReLU."""
-        return self._multiply(1, dY, code, None, None, False, relu_of, dtype, out, stream)
+        if stream is not None:
+            return _on_stream(stream, self.payload, self.grad_input, dY, relu_of, code, dtype, out)
+        return self._multiply(1, dY, code, None, None, False, relu_of, dtype, out)
 
     def grad_weight(self, dY, X: BspCodes, bias: bool = True, out=None, stream=None):
         """(dW, db) from dY (bf16 [T][O]) and the checkpoint of the layer's input: dW float [O][I], zero where the mask is; db
         float [O], or None."""
         import torch
+        if stream is not None:
+            return _on_stream(stream, self.payload, self.grad_weight, dY, X, bias, out)
         T, O, ld = _rows(dY)
         assert dY.dtype == torch.bfloat16 and (T, O) == (X.T, self.O)
         _on(self.payload, dY, X.buffer, out)
@@ -265,10 +307,8 @@ class BspLayerF8:
         db = torch.empty(self.O, dtype=torch.float32, device=dY.device) if bias else None
         n = self._bytes("grad", T)
         ws = torch.empty(n, dtype=torch.uint8, device=dY.device) if n else None
-        st = _current_stream(dY) if stream is None else stream
         _call(_GRAD, _pack13(self._address, dY.data_ptr(), ld, *X.words, out.data_ptr(), 0 if db is None else db.data_ptr(),
-                             0 if ws is None else ws.data_ptr(), n, st), "bsp_f8_fc_grad")
-        _keep(ws, stream)
+                             0 if ws is None else ws.data_ptr(), n, _current_stream(dY)), "bsp_f8_fc_grad")
         return out, db
 
 
@@ -283,6 +323,8 @@ def layer_norm(X, weight=None, bias=None, eps: float = 1e-5, code: Optional[str]
     """(Y, mean, rstd) of X [T][D] (fp32 or bf16) over its last axis; ``weight`` and ``bias`` are float [D] or None.  With ``code``
     ("e4m3", "e5m2") Y is a BspCodes, the form in which a BspLayerF8 reads it."""
     import torch
+    if stream is not None:
+        return _on_stream(stream, X, layer_norm, X, weight, bias, eps, code)
     T, D, ld = _rows(X)
     _on(X, weight, bias)
     mean, rstd = torch.empty((2, T), dtype=torch.float32, device=X.device).unbind(0)
@@ -292,15 +334,16 @@ def layer_norm(X, weight=None, bias=None, eps: float = 1e-5, code: Optional[str]
     else:
         Y = BspCodes(T, D, code, X.device)
         y, words = 0, Y.words
-    st = _current_stream(X) if stream is None else stream
     _call(_NORM, _pack_norm(X.data_ptr(), _type(X), ld, T, D, _vector(weight, D), _vector(bias, D), eps, y, D, *words, mean.data_ptr(),
-                            rstd.data_ptr(), st), "bsp_layer_norm")
+                            rstd.data_ptr(), _current_stream(X)), "bsp_layer_norm")
     return Y, mean, rstd
 
 
 def layer_norm_grad(dY, X, mean, rstd, weight=None, stream=None):
     """(dX, dweight, dbias) from the gradient of Y, the input and what ``layer_norm`` returned with it."""
     import torch
+    if stream is not None:
+        return _on_stream(stream, X, layer_norm_grad, dY, X, mean, rstd, weight)
     T, D, ld = _rows(X)
     T2, D2, ld_dy = _rows(dY)
     assert (T2, D2) == (T, D) and dY.dtype == X.dtype and mean.shape == rstd.shape == (T,)
@@ -310,10 +353,8 @@ def layer_norm_grad(dY, X, mean, rstd, weight=None, stream=None):
     dw, db = torch.empty((2, D), dtype=torch.float32, device=X.device).unbind(0)
     n = _norm_bytes(T, D)
     ws = torch.empty(n, dtype=torch.uint8, device=X.device) if n else None
-    st = _current_stream(X) if stream is None else stream
     _call(_NORM_GRAD, _pack17(dY.data_ptr(), ld_dy, X.data_ptr(), ld, _type(X), T, D, mean.data_ptr(), rstd.data_ptr(), _vector(weight, D),
-                              dX.data_ptr(), D, dw.data_ptr(), db.data_ptr(), 0 if ws is None else ws.data_ptr(), n, st), "bsp_layer_norm_grad")
-    _keep(ws, stream)
+                              dX.data_ptr(), D, dw.data_ptr(), db.data_ptr(), 0 if ws is None else ws.data_ptr(), n, _current_stream(X)), "bsp_layer_norm_grad")
     return dX, dw, db
 
 

@@ -1,0 +1,240 @@
+"""Calls of the 8-bit layers with an explicit stream: the other stream's work is held up by a kernel that spins, and what either
+stream reads and writes is compared with the results of calls one after the other."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+HELD = 10_000_000  # clocks of the spinning kernel: some milliseconds, the calls below take microseconds
+
+
+def _bsp():
+    import paper_2407_09453_amd as bsp
+    return bsp
+
+
+def _flat(v):
+    """Clones of a result's tensors, of a checkpoint its codes and the scales of its rows."""
+    if isinstance(v, tuple):
+        return [t for x in v for t in _flat(x)]
+    if isinstance(v, _bsp().BspCodes):
+        return [v.codes.clone(), v.scale[:, :v.T].clone()]
+    return [v.clone()]
+
+
+def _buffers(v):
+    if isinstance(v, tuple):
+        return [t for x in v for t in _buffers(x)]
+    return [v.buffer if isinstance(v, _bsp().BspCodes) else v]
+
+
+@pytest.fixture(scope="module")
+def calls():
+    """Name -> (call with stream=, bytes of the workspaces that it takes)."""
+    import torch
+    bsp = _bsp()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(11)
+    T, I, O = 700, 1024, 640
+    draw = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    layer = bsp.BspLayerF8(draw(O, I) / 32, bias=draw(O))
+    x, dy, w = draw(T, I).to(torch.bfloat16), draw(T, O).to(torch.bfloat16), draw(I)
+    codes = bsp.save8(x)
+    long = bsp.BspLayerF8(draw(128, 16384) / 128)  # few outputs of a long contraction: shares
+    xs = bsp.save8(draw(40, 16384).to(torch.bfloat16))
+    _, mean, rstd = bsp.layer_norm(x, w)
+    some = bsp.BspLayerF8(draw(128, 256) / 16)  # few blocks: ranges of rows
+    dy2, x2 = draw(4096, 128).to(torch.bfloat16), bsp.save8(draw(4096, 256).to(torch.bfloat16))
+    torch.cuda.synchronize()
+    norm_bytes = __import__("paper_2407_09453_amd.f8", fromlist=["f8"])._norm_bytes(T, I)
+    return {
+        "fc": (lambda **k: layer.fc(x, relu=True, **k), layer._bytes(0, T)),
+        "fc, shares": (lambda **k: long.fc(xs, **k), long._bytes(1, 40)),
+        "fc of codes": (lambda **k: layer.fc(codes, dtype=torch.float32, **k), 0),
+        "grad_input": (lambda **k: layer.grad_input(dy, relu_of=codes, **k), layer._bytes(2, T)),
+        "grad_weight": (lambda **k: some.grad_weight(dy2, x2, **k), some._bytes("grad", 4096)),
+        "save8": (lambda **k: bsp.save8(x, **k), 0),
+        "load": (lambda **k: codes.load(**k), 0),
+        "layer_norm": (lambda **k: bsp.layer_norm(x, w, **k), 0),
+        "layer_norm to codes": (lambda **k: bsp.layer_norm(x, w, code="e4m3", **k), 0),
+        "layer_norm_grad": (lambda **k: bsp.layer_norm_grad(x, x, mean, rstd, w, **k), norm_bytes),
+    }
+
+
+NAMES = ["fc", "fc, shares", "fc of codes", "grad_input", "grad_weight", "save8", "load", "layer_norm", "layer_norm to codes", "layer_norm_grad"]
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_blocks_that_wait_elsewhere_are_not_written(calls, name):
+    """Blocks of the call's sizes are dropped in the current stream while a copy of them is still to come there; the call, in a
+    stream that is free, writes its workspace and results meanwhile."""
+    import torch
+    call, ws = calls[name]
+    s = torch.cuda.Stream()
+    want = _flat(call())
+    sizes = [t.numel() * t.element_size() for t in _buffers(call(stream=s.cuda_stream))] + [ws] * (ws > 0)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    blocks = [torch.full((n,), 91, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(2)]
+    at = [b.data_ptr() for b in blocks]
+    copies = [torch.empty_like(b) for b in blocks]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(HELD)
+    for b, c in zip(blocks, copies):
+        c.copy_(b)
+    del b, blocks
+    got = call(stream=s.cuda_stream)
+    assert not {t.data_ptr() for t in _buffers(got)} & set(at)
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert all(bool((c == 91).all()) for c in copies)
+    assert all(torch.equal(a, b) for a, b in zip(_flat(got), want))
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_results_may_be_dropped_behind_their_use(calls, name):
+    """A result read in the current stream, which waited for it, and dropped before the read is done: the next call in the other
+    stream writes another block."""
+    import torch
+    call, _ = calls[name]
+    want = _flat(call())
+    s = torch.cuda.Stream()
+    call(stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    got = call(stream=s.cuda_stream)
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda._sleep(HELD)
+    read = _flat(got)
+    at = {t.data_ptr() for t in _buffers(got)}
+    del got
+    again = call(stream=s.cuda_stream)
+    assert not at & {t.data_ptr() for t in _buffers(again)}
+    for t in _buffers(again):
+        t.record_stream(s)
+        with torch.cuda.stream(s):
+            t.zero_()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(read, want))
+
+
+def test_what_a_call_reads_may_be_dropped():
+    """Activation, codes, residual, gate, weights and the layer itself, dropped while the stream has the call still to do."""
+    import torch
+    bsp = _bsp()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(12)
+    draw = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    W, b, x, r, dy = draw(512, 768) / 28, draw(512), draw(300, 768).to(torch.bfloat16), draw(300, 512).to(torch.bfloat16), draw(300, 512).to(torch.bfloat16)
+
+    def chain(stream, W, b, x, r, dy):
+        layer = bsp.BspLayerF8(W, bias=b)
+        if stream is not None:
+            torch.cuda.synchronize()
+            with torch.cuda.stream(torch.cuda.ExternalStream(stream)):
+                torch.cuda._sleep(HELD)
+        k = {} if stream is None else {"stream": stream}
+        codes = bsp.save8(x, **k)
+        y = layer.fc(x, residual=r, **k)
+        y2 = layer.fc(codes, residual=r, **k)
+        dx = layer.grad_input(dy, relu_of=codes, **k)
+        return y, y2, dx, *layer.grad_weight(dy, codes, **k)
+    want = [t.clone() for t in chain(None, W, b, x, r, dy)]
+    s = torch.cuda.Stream()
+    sizes = [t.numel() * t.element_size() for t in (x, r, dy)] + [bsp.BspCodes(300, 768).buffer.numel(), 512 * 768, 512 * 768, 2048]
+    torch.cuda.synchronize()
+    got = chain(s.cuda_stream, W.clone(), b.clone(), x.clone(), r.clone(), dy.clone())
+    litter = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(3)]  # takes what was dropped
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, w) for a, w in zip(got, want)) and len(litter) == 21
+
+
+def test_the_default_streams_handle():
+    """0 is the default stream, also where another one is current."""
+    import torch
+    bsp = _bsp()
+    x = torch.randn(90, 256, device="cuda").to(torch.bfloat16)
+    layer = bsp.BspLayerF8(torch.randn(130, 256, device="cuda"))
+    want = layer.fc(x)
+    torch.cuda.synchronize()
+    t = torch.empty_like(x)
+    with torch.cuda.stream(torch.cuda.Stream()):
+        torch.cuda.default_stream().synchronize()
+        with torch.cuda.stream(torch.cuda.default_stream()):
+            torch.cuda._sleep(HELD)
+            t.copy_(x)  # in the default stream: the call has to come behind it
+        y = layer.fc(t, stream=0)
+        torch.cuda.synchronize()
+    assert torch.equal(y, want)
+    assert torch.equal(layer.fc(x, stream=torch.cuda.current_stream().cuda_stream), want)
+
+
+def test_in_a_graph_with_a_fork():
+    """A capture that forks to a second stream, calls there by handle, and joins."""
+    import torch
+    bsp = _bsp()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(13)
+    x = torch.randn(130, 512, generator=gen, device="cuda").to(torch.bfloat16)
+    one, two = (bsp.BspLayerF8(torch.randn(384, 512, generator=gen, device="cuda") / 22) for _ in range(2))
+    s = torch.cuda.Stream()
+
+    def step(stream):
+        if stream is None:
+            return one.fc(x), two.fc(bsp.save8(x))
+        here = torch.cuda.current_stream()
+        s.wait_stream(here)
+        a = two.fc(bsp.save8(x, stream=stream), stream=stream)
+        b = one.fc(x)
+        here.wait_stream(s)
+        return b, a
+    step(None), step(s.cuda_stream)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = step(s.cuda_stream)
+    for k in range(3):
+        x.copy_(torch.randn(130, 512, generator=gen, device="cuda").to(torch.bfloat16))
+        for o in got:
+            o.fill_(float("nan"))
+        want = step(None)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_two_host_threads():
+    """Two threads, a stream each, the same layer: each gets the results of its own calls."""
+    import threading
+    import torch
+    bsp = _bsp()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(14)
+    layer = bsp.BspLayerF8(torch.randn(640, 512, generator=gen, device="cuda") / 22)
+    xs = [[torch.randn(T, 512, generator=gen, device="cuda").to(torch.bfloat16) for T in (1, 33, 200, 700)] for _ in range(2)]
+    dys = [[torch.randn(x.shape[0], 640, generator=gen, device="cuda").to(torch.bfloat16) for x in row] for row in xs]
+
+    def step(x, dy):
+        c = bsp.save8(x)
+        return [layer.fc(x), layer.fc(c), layer.grad_input(dy, relu_of=c), *layer.grad_weight(dy, c)]
+    want = [[step(x, dy) for x, dy in zip(a, b)] for a, b in zip(xs, dys)]
+    torch.cuda.synchronize()
+    got, errors = [None, None], []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()) as _:
+                for _ in range(20):
+                    got[i] = [step(x, dy) for x, dy in zip(xs[i], dys[i])]
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:  # (a thread's exception is not the test's)
+            errors.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors
+    for i in range(2):
+        for a, b in zip(got[i], want[i]):
+            assert all(torch.equal(p, q) for p, q in zip(a, b))
