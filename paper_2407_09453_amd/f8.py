@@ -61,13 +61,6 @@ def _call(call, words, name):
         raise BspError(rc, name)
 
 
-def _keep(t, stream):
-    """A tensor that is dropped while its kernels may still wait in a stream other than torch's current one."""
-    if stream is not None:
-        import torch
-        t.record_stream(torch.cuda.ExternalStream(int(stream), device=t.device))
-
-
 def _memory(v):
     """The tensors on a GPU that an argument or a result is held in."""
     if isinstance(v, (tuple, list)):
@@ -209,6 +202,8 @@ class BspLayerF8:
         """Take new weights (same shape, same mask), and a new bias where one is given (to a layer that was made with one), as
         after a step of an optimiser."""
         import torch
+        if stream is not None:
+            return _on_stream(stream, self.payload, self.update, W, bias)
         if not isinstance(W, torch.Tensor):
             W = torch.from_numpy(np.ascontiguousarray(W, dtype=np.float32))
         W = W.to(self.device)
@@ -219,9 +214,7 @@ class BspLayerF8:
             b = torch.as_tensor(bias).detach()
             assert self.d_bias is not None and b.shape == (O,), "a bias [%d] for a layer made with one" % O
             self.d_bias.copy_(b)
-        st = _current_stream(W) if stream is None else stream
-        _check(load_library().bsp_f8_pack(self.struct, W.data_ptr(), kind, ld, st), "bsp_f8_pack")
-        _keep(W, stream)
+        _check(load_library().bsp_f8_pack(self.struct, W.data_ptr(), kind, ld, _current_stream(W)), "bsp_f8_pack")
 
     def _bytes(self, kind, T):
         n = self._workspace.get((kind, T))

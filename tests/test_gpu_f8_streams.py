@@ -238,3 +238,37 @@ def test_two_host_threads():
     for i in range(2):
         for a, b in zip(got[i], want[i]):
             assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def test_new_weights_and_bias_in_a_stream():
+    """update() with a stream puts the bias there too: a call behind it in that stream has both while the current stream is held,
+    and one before it has neither."""
+    import torch
+    bsp = _bsp()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(15)
+    draw = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    W, b, W2, b2, x = draw(384, 256), draw(384), draw(384, 256), draw(384), draw(60, 256).to(torch.bfloat16)
+    old, new = bsp.BspLayerF8(W, bias=b).fc(x), bsp.BspLayerF8(W2, bias=b2).fc(x)
+    layer = bsp.BspLayerF8(W, bias=b)
+    s = torch.cuda.Stream()
+    for _ in range(2):  # the first round warms up
+        layer.update(W, bias=b)
+        Wc, bc = W2.clone(), b2.clone()
+        torch.cuda.synchronize()
+        torch.cuda._sleep(HELD)
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(HELD // 4)
+        first = layer.fc(x, stream=s.cuda_stream)
+        layer.update(Wc, bias=bc, stream=s.cuda_stream)
+        del Wc, bc
+        second = layer.fc(x, stream=s.cuda_stream)
+        s.synchronize()
+        with torch.cuda.stream(s):  # (where the results are ready)
+            got = torch.equal(first, old), torch.equal(second, new)
+        torch.cuda.synchronize()
+    assert got == (True, True)
+    layer.update(W.cpu(), bias=b.cpu().numpy(), stream=s.cuda_stream)
+    y = layer.fc(x, stream=s.cuda_stream)
+    s.synchronize()
+    assert torch.equal(y, old)
