@@ -6,12 +6,16 @@ With ``stream`` (a handle as an integer) a call does as under ``torch.cuda.strea
 ready there, and whoever uses its results elsewhere waits for it.  Nothing has to be kept until then: what it reads
 may be dropped at once, and so may its results behind uses in the stream that was current at the call.
 
+Gradients are calls of their own: none of these records a graph for autograd, and a call whose results would be part of one
+(an input requires a gradient, outside ``torch.no_grad``) says so with a warning.
+
 A call's arguments go to the library as one string of words: of a small layer's 9 us on the host ctypes' conversion of 16 arguments
 one by one took 2, and a tensor of torch's takes 1.5 us to make, so a checkpoint is one allocation."""
 from __future__ import annotations
 
 import ctypes
 import struct
+import warnings
 from typing import Optional
 
 import numpy as np
@@ -59,6 +63,13 @@ def _call(call, words, name):
     rc = load_library().bsp_f8_call_packed(call, words)
     if rc:
         raise BspError(rc, name)
+
+
+def _unrecorded(depth: int):
+    import torch
+    if torch.is_grad_enabled():
+        warnings.warn("an input requires a gradient, but this call records nothing for autograd: see grad_input, grad_weight and "
+                      "layer_norm_grad (torch.no_grad() says that this is meant)", UserWarning, stacklevel=depth)
 
 
 def _memory(v):
@@ -143,6 +154,8 @@ def save8(X, kind: Optional[str] = None, out: Optional[BspCodes] = None, stream=
     is asked for, or the type of ``out``."""
     if stream is not None:
         return _on_stream(stream, X, save8, X, kind, out)
+    if X.requires_grad:
+        _unrecorded(3)
     T, K, ld = _rows(X)
     if out is None:
         out = BspCodes(T, K, kind or "e4m3", X.device)
@@ -234,6 +247,8 @@ class BspLayerF8:
         if codes:
             T, K, at = X.T, X.K, X.buffer
         else:
+            if X.requires_grad:
+                _unrecorded(4)
             T, K, ld = _rows(X)
             at = X
         width, inner = (self.I, self.O) if transposed else (self.O, self.I)
@@ -248,6 +263,8 @@ class BspLayerF8:
             _on(at, out)
         r, g = 0, _NO_CODES
         if residual is not None:
+            if residual.requires_grad:
+                _unrecorded(4)
             assert residual.shape == out.shape and residual.dtype == out.dtype and residual.is_contiguous()
             _on(at, residual)
             r = residual.data_ptr()
@@ -290,6 +307,8 @@ class BspLayerF8:
         import torch
         if stream is not None:
             return _on_stream(stream, self.payload, self.grad_weight, dY, X, bias, out)
+        if dY.requires_grad:
+            _unrecorded(3)
         T, O, ld = _rows(dY)
         assert dY.dtype == torch.bfloat16 and (T, O) == (X.T, self.O)
         _on(self.payload, dY, X.buffer, out)
@@ -318,6 +337,8 @@ def layer_norm(X, weight=None, bias=None, eps: float = 1e-5, code: Optional[str]
     import torch
     if stream is not None:
         return _on_stream(stream, X, layer_norm, X, weight, bias, eps, code)
+    if X.requires_grad or (weight is not None and weight.requires_grad) or (bias is not None and bias.requires_grad):
+        _unrecorded(3)
     T, D, ld = _rows(X)
     _on(X, weight, bias)
     mean, rstd = torch.empty((2, T), dtype=torch.float32, device=X.device).unbind(0)
@@ -337,6 +358,8 @@ def layer_norm_grad(dY, X, mean, rstd, weight=None, stream=None):
     import torch
     if stream is not None:
         return _on_stream(stream, X, layer_norm_grad, dY, X, mean, rstd, weight)
+    if dY.requires_grad or X.requires_grad or (weight is not None and weight.requires_grad):
+        _unrecorded(3)
     T, D, ld = _rows(X)
     T2, D2, ld_dy = _rows(dY)
     assert (T2, D2) == (T, D) and dY.dtype == X.dtype and mean.shape == rstd.shape == (T,)

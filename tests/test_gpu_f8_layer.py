@@ -97,3 +97,40 @@ def test_a_checkpoint_given_is_of_the_type_asked_for():
         for got in (bsp.save8(t, out=c), bsp.save8(t, have, out=c)):
             assert got is c and torch.equal(c.codes, want.codes) and torch.equal(c.scale, want.scale)
     assert bsp.save8(t).kind == "e4m3"
+
+
+def test_a_graph_that_is_not_recorded_is_said_to_be():
+    """No call records what autograd needs: a tensor that requires a gradient is taken with a warning, under no_grad without, with the same results."""
+    import warnings
+    import torch
+    bsp = _bsp()
+    rng = np.random.default_rng(9)
+    layer = bsp.BspLayerF8(rng.standard_normal((130, 256)).astype(np.float32), bias=rng.standard_normal(130).astype(np.float32))
+    x, dy, r = (torch.randn(20, n, device="cuda").to(torch.bfloat16) for n in (256, 130, 130))
+    w, b = torch.ones(256, device="cuda"), torch.zeros(256, device="cuda")
+    codes = bsp.save8(x)
+    _, mean, rstd = bsp.layer_norm(x, w, b)
+    calls = {  # what may require a gradient, and the call
+        "save8": ([x], lambda x: bsp.save8(x).load()),
+        "fc": ([x, r], lambda x, r: layer.fc(x, residual=r)),
+        "grad_input": ([dy], lambda dy: layer.grad_input(dy)),
+        "grad_weight": ([dy], lambda dy: layer.grad_weight(dy, codes)),
+        "layer_norm": ([x, w, b], lambda x, w, b: bsp.layer_norm(x, w, b)),
+        "layer_norm_grad": ([torch.randn_like(x), x, w], lambda d, x, w: bsp.layer_norm_grad(d, x, mean, rstd, w)),
+    }
+    listed = lambda v: list(v) if isinstance(v, tuple) else [v]  # noqa: E731
+    for name, (given, call) in calls.items():
+        with warnings.catch_warnings():
+            warnings.simplefilter("error")
+            want = listed(call(*given))
+        for k in range(len(given)):
+            some = [t.clone().requires_grad_() if i == k else t for i, t in enumerate(given)]
+            with pytest.warns(UserWarning, match="autograd"):
+                got = listed(call(*some))
+            with warnings.catch_warnings(), torch.no_grad():
+                warnings.simplefilter("error")
+                again = listed(call(*some))
+            assert all(torch.equal(g, v) and torch.equal(a, v) and not g.requires_grad for g, a, v in zip(got, again, want)), (name, k)
+    with warnings.catch_warnings():  # new weights are taken as values, as an optimiser's are
+        warnings.simplefilter("error")
+        layer.update(torch.nn.Parameter(torch.randn(130, 256, device="cuda")), bias=torch.nn.Parameter(torch.randn(130, device="cuda")))
