@@ -26,6 +26,12 @@ __host__ __device__ inline int f8_blocks(int n) { return (n + F8_BLOCK - 1) / F8
 // rows of a scale array: one byte for each row of a column block, whole sixteens of them
 __host__ __device__ inline int64_t f8_scale_rows(int T) { return ((int64_t)T + 15) & ~(int64_t)15; }
 
+// A launch has fewer than 2^32 threads along x: workgroups past kGridX go along y, where workgroup x of row y is number y kGridX + x.
+enum { kGridX = 1 << 21 };
+inline dim3 f8_grid(int64_t groups) {
+  return groups <= kGridX ? dim3((unsigned)groups) : dim3(kGridX, (unsigned)((groups + kGridX - 1) / kGridX));
+}
+
 // Exchanges between neighbouring lanes without LDS: the lane whose number differs in bit 0, in bit 1; the mirrored lane of eight, of
 // sixteen; the lane 16 away in a pair of rows, 32 away.
 enum { kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140 };

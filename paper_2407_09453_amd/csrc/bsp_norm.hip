@@ -93,7 +93,7 @@ template <bool F32, bool CODES, int ROWT, int NV>
 __global__ __launch_bounds__(ROWT > 256 ? ROWT : 256) void norm_forward(NormArgs a) {
   __shared__ float sh[ROWT > 256 ? ROWT / 64 : 4][1];
   const int tid = threadIdx.x % ROWT;
-  const int64_t row = ROWT >= 256 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (256 / ROWT) + threadIdx.x / ROWT;
+  const int64_t group = (int64_t)blockIdx.y * kGridX + blockIdx.x, row = ROWT >= 256 ? group : group * (256 / ROWT) + threadIdx.x / ROWT;
   if (row >= a.T) return;  // (whole groups of ROWT)
   const void* x = row_of<F32>(a.X, row, a.ldx);
   const float inv = 1.f / (float)a.D;
@@ -272,7 +272,8 @@ __global__ __launch_bounds__(ROWT > 256 ? ROWT : 256) void norm_backward(NormArg
 template <bool F32>
 __global__ __launch_bounds__(256) void norm_backward_long(NormArgs a) {
   __shared__ float sh[4][2];
-  const int64_t row = blockIdx.x;
+  const int64_t row = (int64_t)blockIdx.y * kGridX + blockIdx.x;
+  if (row >= a.T) return;
   const float inv = 1.f / (float)a.D, mean = a.mean[row], rstd = a.rstd[row];
   float s[2] = {0.f, 0.f}, h[8], g[8];
   for (int c = threadIdx.x * 8; c < a.D; c += 2048) {
@@ -317,7 +318,7 @@ __global__ __launch_bounds__(256) void norm_columns_long(NormArgs a) {
 __global__ __launch_bounds__(1024) void norm_sum(const float* part, int parts, int64_t width, int64_t split_at, float* out, float* out2) {
   __shared__ float sh[16][64];
   const int l = threadIdx.x & 63, q = threadIdx.x >> 6;
-  const int64_t c = (int64_t)blockIdx.x * 64 + l;
+  const int64_t c = ((int64_t)blockIdx.y * kGridX + blockIdx.x) * 64 + l;
   float s = 0.f;
   if (c < width) {
 #pragma unroll 8
@@ -338,7 +339,7 @@ inline int launched() { return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ER
 
 template <bool F32, bool CODES>
 int forward(const NormArgs& a, hipStream_t st) {
-  const dim3 block(256), rows((unsigned)a.T), quads((unsigned)(((int64_t)a.T + 3) / 4)), sixteens((unsigned)(((int64_t)a.T + 15) / 16));
+  const dim3 block(256), rows = f8_grid(a.T), quads = f8_grid(((int64_t)a.T + 3) / 4), sixteens = f8_grid(((int64_t)a.T + 15) / 16);
   if (a.D < 8 || a.Dp > 16384) hipLaunchKernelGGL((norm_forward<F32, CODES, 256, 0>), rows, block, 0, st, a);
   else if (a.Dp <= 128) hipLaunchKernelGGL((norm_forward<F32, CODES, 16, 1>), sixteens, block, 0, st, a);
   else if (a.Dp <= 256) hipLaunchKernelGGL((norm_forward<F32, CODES, 16, 2>), sixteens, block, 0, st, a);
@@ -365,7 +366,7 @@ int backward(const NormArgs& a, hipStream_t st) {
   else if (a.D >= 8 && a.D <= 8192) hipLaunchKernelGGL((norm_backward<F32, 512, 2>), parts, dim3(512), 0, st, a);
   else if (a.D >= 8 && a.D <= 16384) hipLaunchKernelGGL((norm_backward<F32, 1024, 2>), parts, dim3(1024), 0, st, a);
   else {
-    if (a.T > 0) hipLaunchKernelGGL((norm_backward_long<F32>), dim3((unsigned)a.T), block, 0, st, a);
+    if (a.T > 0) hipLaunchKernelGGL((norm_backward_long<F32>), f8_grid(a.T), block, 0, st, a);
     if (launched() != BSP_OK) return BSP_ERR_HIP;
     hipLaunchKernelGGL((norm_columns_long<F32>), dim3((unsigned)((a.D + 255) / 256), (unsigned)a.parts), block, 0, st, a);
   }
@@ -373,7 +374,7 @@ int backward(const NormArgs& a, hipStream_t st) {
 }
 
 int sum(const float* part, int parts, int64_t width, int64_t split_at, float* out, float* out2, hipStream_t st) {
-  hipLaunchKernelGGL(norm_sum, dim3((unsigned)((width + 63) / 64)), dim3(1024), 0, st, part, parts, width, split_at, out, out2);
+  hipLaunchKernelGGL(norm_sum, f8_grid((width + 63) / 64), dim3(1024), 0, st, part, parts, width, split_at, out, out2);
   return launched();
 }
 
