@@ -40,16 +40,18 @@ struct SaveArgs {
   const void* X;
   uint8_t *codes, *scale;
   int64_t ldx, srows;
-  int32_t T, K, Kp;
+  int32_t T, K, Kp, downs;
 };
 
 template <bool F32, bool E5>
 __global__ __launch_bounds__(256) void f8_save(SaveArgs a) {
   __shared__ uint32_t sc[8][4];  // [column block][sixteen rows' bytes]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int across = (a.Kp + 1023) / 1024, down = blockIdx.x / across, chunk = blockIdx.x - down * across;
+  const int across = (a.Kp + 1023) / 1024, turn = blockIdx.x / across, chunk = blockIdx.x - turn * across;
+  const int down = blockIdx.y * a.downs + turn;
   const int c0 = chunk * 1024 + lane * 16;
   const int64_t row0 = (int64_t)down * 16 + wave * 4;
+  if ((int64_t)down * 16 >= a.T) return;  // (a whole workgroup)
   Raw16<F32> raw[4] = {};
   const bool thin = a.K < 8;
 #pragma unroll
@@ -86,15 +88,17 @@ struct LoadArgs {
   const uint8_t *codes, *scale;
   void* Y;
   int64_t ldy, srows;
-  int32_t T, K, Kp;
+  int32_t T, K, Kp, downs;
 };
 
 template <bool F32, bool E5>
 __global__ __launch_bounds__(256) void f8_load(LoadArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int across = (a.Kp + 1023) / 1024, down = blockIdx.x / across, chunk = blockIdx.x - down * across;
+  const int across = (a.Kp + 1023) / 1024, turn = blockIdx.x / across, chunk = blockIdx.x - turn * across;
+  const int down = blockIdx.y * a.downs + turn;
   const int c0 = chunk * 1024 + lane * 16;
   const int64_t row0 = (int64_t)down * 16 + wave * 4;
+  if ((int64_t)down * 16 >= a.T) return;  // (a whole workgroup)
   if (c0 >= a.K) return;
   const int left = a.K - c0;
   u32x4_t q[4];
@@ -230,16 +234,25 @@ __global__ __launch_bounds__(256) void f8_pack(PackArgs a) {
   }
 }
 
+// Workgroups of sixteen rows by 1024 columns: as many sixteens of rows along x as f8_grid takes (`downs`), the rest along y.
+inline bool sixteens(int T, int Kp, int32_t* downs, dim3* grid) {
+  const int64_t across = (Kp + 1023) / 1024, all = ((int64_t)T + 15) / 16, most = kGridX / across;
+  *downs = (int32_t)(all < most ? all : most);
+  const int64_t y = (all + *downs - 1) / *downs;
+  *grid = dim3((unsigned)(across * *downs), (unsigned)y);
+  return y <= 65535;
+}
+
 inline int launched() { return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP; }
 
 }  // namespace
 
 int f8_launch_save(const void* X, int x_f32, int64_t ldx, int T, int K, bool e5, uint8_t* codes, uint8_t* scale, hipStream_t st) {
   const int Kp = f8_blocks(K) * F8_BLOCK;
-  SaveArgs a{X, codes, scale, ldx, f8_scale_rows(T), T, K, Kp};
-  const int64_t groups = ((int64_t)T + 15) / 16 * ((Kp + 1023) / 1024);
-  if (groups > INT32_MAX) return BSP_ERR_SHAPE;
-  const dim3 grid((unsigned)groups), block(256);
+  SaveArgs a{X, codes, scale, ldx, f8_scale_rows(T), T, K, Kp, 0};
+  dim3 grid;
+  const dim3 block(256);
+  if (!sixteens(T, Kp, &a.downs, &grid)) return BSP_ERR_SHAPE;
   if (x_f32) {
     if (e5) hipLaunchKernelGGL((f8_save<true, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((f8_save<true, false>), grid, block, 0, st, a);
@@ -252,10 +265,10 @@ int f8_launch_save(const void* X, int x_f32, int64_t ldx, int T, int K, bool e5,
 
 int f8_launch_load(const uint8_t* codes, const uint8_t* scale, int T, int K, bool e5, void* Y, int y_f32, int64_t ldy, hipStream_t st) {
   const int Kp = f8_blocks(K) * F8_BLOCK;
-  LoadArgs a{codes, scale, Y, ldy, f8_scale_rows(T), T, K, Kp};
-  const int64_t groups = ((int64_t)T + 15) / 16 * ((Kp + 1023) / 1024);
-  if (groups > INT32_MAX) return BSP_ERR_SHAPE;
-  const dim3 grid((unsigned)groups), block(256);
+  LoadArgs a{codes, scale, Y, ldy, f8_scale_rows(T), T, K, Kp, 0};
+  dim3 grid;
+  const dim3 block(256);
+  if (!sixteens(T, Kp, &a.downs, &grid)) return BSP_ERR_SHAPE;
   if (y_f32) {
     if (e5) hipLaunchKernelGGL((f8_load<true, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((f8_load<true, false>), grid, block, 0, st, a);

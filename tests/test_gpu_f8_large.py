@@ -77,3 +77,17 @@ def test_norm_gradient_of_long_rows():
     term = dy[0].float() * ((x[0].float() - 0.25) * 0.5)
     assert bool(((dw - T * term).abs() <= (4 + 9 + 1) * U * T * term.abs()).all())
     assert all(torch.equal(dx[0], dx[t]) for t in range(1, T))
+
+
+@pytest.mark.parametrize("T,K,gib", [((1 << 28) + 17, 3, 40), ((1 << 25) + 1, 1030, 45 + 70)])
+def test_checkpoint_of_many_rows(T, K, gib):
+    """Rows past the sixteens that one dimension holds, of one and of two workgroups across."""
+    import torch
+    import paper_2407_09453_amd as bsp
+    _needs(gib)
+    x = torch.randn(1, K, device="cuda").to(torch.bfloat16)
+    small = bsp.save8(x)
+    c = bsp.save8(x.expand(T, K))
+    assert _all_rows_are(c.codes, small.codes[0])
+    assert all(_all_rows_are(c.scale[k, :T, None], small.scale[k, :1]) for k in range(c.scale.shape[0]))
+    assert _all_rows_are(c.load(), small.load()[0])
