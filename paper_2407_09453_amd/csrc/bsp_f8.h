@@ -31,6 +31,8 @@ enum { kGridX = 1 << 21 };
 inline dim3 f8_grid(int64_t groups) {
   return groups <= kGridX ? dim3((unsigned)groups) : dim3(kGridX, (unsigned)((groups + kGridX - 1) / kGridX));
 }
+// whether so many workgroups along x can be launched
+inline bool f8_fits_x(int64_t groups, int threads) { return groups * threads <= (int64_t)UINT32_MAX; }
 
 // Exchanges between neighbouring lanes without LDS: the lane whose number differs in bit 0, in bit 1; the mirrored lane of eight, of
 // sixteen; the lane 16 away in a pair of rows, 32 away.

@@ -382,7 +382,7 @@ int launch(void (*kernel)(TileArgs), bool raised, int threads, int lds, TileArgs
   if (!raised) return BSP_ERR_HIP;
   a.tiles_o = (a.w.out + NO - 1) / NO;
   a.tiles_t = (int)(((int64_t)a.T + NT - 1) / NT);
-  if ((int64_t)a.tiles_o * a.tiles_t * a.split > INT32_MAX / 8) return BSP_ERR_SHAPE;
+  if (!f8_fits_x((int64_t)a.tiles_o * a.tiles_t * a.split, threads)) return BSP_ERR_SHAPE;
   hipLaunchKernelGGL(kernel, dim3((unsigned)(a.tiles_o * a.tiles_t * a.split)), dim3(threads), lds, st, a);
   return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP;
 }
@@ -466,7 +466,7 @@ int f8_launch_tile(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q
 
 int f8_launch_join(const float* part, int split, int T, int O, const F8Epilogue& q, bool f32, hipStream_t st) {
   const int64_t groups = ((int64_t)T * ((O + 3) / 4) + 255) / 256;
-  if (groups > INT32_MAX) return BSP_ERR_SHAPE;
+  if (!f8_fits_x(groups, 256)) return BSP_ERR_SHAPE;
   if (f32) hipLaunchKernelGGL(f8_join<true>, dim3((unsigned)groups), dim3(256), 0, st, part, split, T, O, q);
   else hipLaunchKernelGGL(f8_join<false>, dim3((unsigned)groups), dim3(256), 0, st, part, split, T, O, q);
   return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP;

@@ -411,7 +411,7 @@ int launch(F8GradArgs a, hipStream_t st) {
   if (!raised) return BSP_ERR_HIP;
   a.groups = a.dW ? (a.nbi + C - 1) / C : 0;
   const int64_t groups = ((int64_t)a.nbo * ((a.groups + 3) / 4) + 7) / 8 * 32;
-  if (groups + a.nbo > INT32_MAX) return BSP_ERR_SHAPE;
+  if (!f8_fits_x(groups + a.nbo, 64 * WAVES)) return BSP_ERR_SHAPE;
   hipLaunchKernelGGL((f8_grad<C, WAVES, E5, THIN>), dim3((unsigned)(groups + (a.db ? a.nbo : 0)), (unsigned)a.split), dim3(64 * WAVES), lds, st, a);
   return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP;
 }
@@ -435,6 +435,10 @@ int f8_grad_split(int64_t nnzb, int T) {
 }
 
 int f8_launch_grad(const F8GradArgs& a, hipStream_t st) {
+  // the second launch: every block of the matrix, or (the bias's gradient alone) one a block row
+  F8GradArgs f = a;
+  if (!f.dW) f.nbi = 1;
+  if (!f8_fits_x((int64_t)f.nbo * f.nbi, 256)) return BSP_ERR_SHAPE;
   int rc;
   if (a.O < 8) rc = a.e5 ? launch<1, 8, true, true>(a, st) : launch<1, 8, false, true>(a, st);
   else switch (a.split > 1 ? 1 : blocks_each(a)) {
@@ -445,6 +449,7 @@ int f8_launch_grad(const F8GradArgs& a, hipStream_t st) {
       else rc = a.e5 ? launch<1, 8, true>(a, st) : launch<1, 8, false>(a, st);
   }
   if (rc != BSP_OK || a.split == 1) return rc;
-  hipLaunchKernelGGL(f8_grad_finish, dim3((unsigned)(a.nbo * a.nbi), a.nbo * a.nbi >= 1024 ? 4 : 16), dim3(256), 0, st, a);
+  const int cells = f.nbo * f.nbi;
+  hipLaunchKernelGGL(f8_grad_finish, dim3((unsigned)cells, !f.dW ? 1 : cells >= 1024 ? 4 : 16), dim3(256), 0, st, f);
   return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP;
 }

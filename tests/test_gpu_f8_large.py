@@ -91,3 +91,32 @@ def test_checkpoint_of_many_rows(T, K, gib):
     assert _all_rows_are(c.codes, small.codes[0])
     assert all(_all_rows_are(c.scale[k, :T, None], small.scale[k, :1]) for k in range(c.scale.shape[0]))
     assert _all_rows_are(c.load(), small.load()[0])
+
+
+def test_bias_gradient_alone_of_many_channels():
+    """Through the C entry point, no dW: 2^24 channels over 2^14, in ranges of rows.  Whole numbers: exact sums."""
+    import ctypes
+    import torch
+    from paper_2407_09453_amd import binding as b
+    _needs(2)
+    T, O, I = 1200, 1 << 24, 1 << 14
+    kept = 3
+    row_ptr = torch.full((O // 128 + 1,), kept, dtype=torch.int32, device="cuda")
+    row_ptr[0] = 0  # all of them in the first block row
+    some = torch.arange(kept, dtype=torch.int32, device="cuda")
+    col_ptr = torch.zeros(I // 128 + 1, dtype=torch.int32, device="cuda")
+    codes = torch.zeros(kept, 128, 128, dtype=torch.uint8, device="cuda")
+    w = b.bsp_weights_f8(O, I, kept, row_ptr.data_ptr(), some.data_ptr(), col_ptr.data_ptr(), some.data_ptr(), codes.data_ptr(), codes.data_ptr(),
+                         codes.data_ptr(), codes.data_ptr())
+    lib = b.load_library()
+    n = ctypes.c_int64(0)
+    assert lib.bsp_f8_fc_grad_workspace(w, T, n) == 0 and n.value > 0
+    ws = torch.empty(n.value, dtype=torch.uint8, device="cuda")
+    import paper_2407_09453_amd as bsp
+    x = bsp.save8(torch.ones(1, I, device="cuda").expand(T, I))
+    dy = torch.randint(-8, 9, (1, O), device="cuda").to(torch.bfloat16)
+    db = torch.full((O,), float("nan"), device="cuda")
+    torch.cuda.synchronize()
+    assert lib.bsp_f8_fc_grad(w, dy.data_ptr(), 0, ctypes.byref(x.struct), None, db.data_ptr(), ws.data_ptr(), n.value,
+                              torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(db, T * dy[0].float())
