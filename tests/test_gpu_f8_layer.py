@@ -134,3 +134,25 @@ def test_a_graph_that_is_not_recorded_is_said_to_be():
     with warnings.catch_warnings():  # new weights are taken as values, as an optimiser's are
         warnings.simplefilter("error")
         layer.update(torch.nn.Parameter(torch.randn(130, 256, device="cuda")), bias=torch.nn.Parameter(torch.randn(130, device="cuda")))
+
+
+@pytest.mark.parametrize("T", [3, 20, 60])
+def test_rows_of_the_smallest_values(T):
+    """fp32 results and the weights' gradient take codes as bf16: whole multiples of 2^-133 exactly, and of a value between them no
+    more than 2^-133 is lost.  Rows of one value and one much smaller; weights of 2^60, so that results are ordinary numbers."""
+    import torch
+    bsp = _bsp()
+    W = np.full((130, 128), 2.0 ** 60, np.float32)
+    layer = bsp.BspLayerF8(W)
+    for small, lost in ((1.0, 0.0), (5.0, 0.0), (0.75, 1.0)):
+        x = torch.zeros(T, 128)
+        x[:, 3], x[:, 77] = 2.0 ** -127, small * 2.0 ** -133
+        c = bsp.save8(x.cuda(), "e4m3")
+        values = _host(c.load(torch.float32))
+        assert (values == x.double().numpy()).all()
+        ref = values.sum(1)[:, None] * 2.0 ** 60
+        assert (np.abs(_host(layer.fc(c, dtype=torch.float32)) - ref) <= lost * 2.0 ** -73 + 2.0 ** -24 * ref).all()
+        dy = torch.full((T, 130), 2.0 ** 60, dtype=torch.bfloat16, device="cuda")
+        dW, _ = layer.grad_weight(dy, c)
+        want = T * values[0] * 2.0 ** 60
+        assert (np.abs(_host(dW) - want) <= T * lost * 2.0 ** -73 + (T + 8) * 2.0 ** -24 * want).all()
