@@ -7,9 +7,11 @@
 // A staged row of 128 bytes is eight pieces of 16; piece p of row r lies at place p ^ (r / 2 mod 8), so sixteen rows' same
 // piece, which sixteen lanes read together, lie in sixteen different bank groups.
 // MO x MT tiles of 32 x 32 a wave, WO x WT waves.
-// Measured: 8192 x 16384 -> 4096 390 us (2.8 PFLOP/s), 16384 x 4096 -> 16384 870 (2.5), 2048 x 4096 -> 4096 35, 512 x 4096 -> 4096 14.5, 197 x 2048 -> 1000 7.  On
-// constant operands the first two take 306 and 702 us: with random codes the card's power sets the clock, and what the
+// Measured: 8192 x 16384 -> 4096 390 to 440 us (2.8 to 2.5 PFLOP/s), 16384 x 4096 -> 16384 870 (2.5), 2048 x 4096 -> 4096 35, 512 x 4096 -> 4096 14.5 to 16.5,
+// 197 x 2048 -> 1000 7 (fp32 results 10).  On constant operands the first two take 306 and 702 us: with random codes the card's power sets the clock, and what the
 // loop leaves (91 % of a register loop's rate) is little.
+// With a residual the same take 560, 1850, 59, 21 and 8.4: its values (and for fp32 results the bias too) are asked for a row at a time in the way
+// out (store_tile's first branch), each waited for before the next.
 #include "bsp_f8.h"
 #include <type_traits>
 

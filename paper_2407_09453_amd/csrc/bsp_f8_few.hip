@@ -2,12 +2,16 @@
 //
 // A workgroup owns 16 output channels and 16 MT rows; its waves share out the kept blocks of the channels' block row, each
 // adding its blocks' products in its own accumulators, and the waves' sums meet in LDS: the long axis is split inside the
-// workgroup, with no second launch and no memory for partial sums.  Operands go from memory to registers, kAhead blocks
-// before they are multiplied: a lane's 32 bytes of a weight row are pieces g and 4 + g of sixteen, so that a request covers whole
+// workgroup.  Only where that leaves many CUs without one (few channels, a long contraction: f8_few_split) are there shares of the block
+// columns too, whose sums a second launch joins.  Operands go from memory to registers, up to kAhead blocks at a time: a lane's 32
+// bytes of a weight row are pieces g and 4 + g of sixteen, so that a request covers whole
 // 64-byte halves of sixteen lines that follow one another, and a block's lines are each asked for once in the chip.
+// The loop asks kAhead blocks ahead where a wave has 2 kAhead of them or more.  With fewer, as on 16 x 25088 -> 4096 half kept (six or seven a
+// wave, 16.6 us, 3.2 TB/s), latency is paid several times: the rows of each block are asked for behind a wait for the number of its column, with
+// the weights of the block before already waited for, and the tail waits for each block that it asks for at once.
 // Up to 16 rows given as bf16 or fp32, in whole aligned pieces of 16 bytes, become codes in LDS first, in every workgroup for itself, while the
 // first weights are on their way: less than a launch of its own takes
-// (us, 1 x 4096 -> 4096: 5.8, with rows that are codes 5.4; 1 x 25088 -> 4096, half of the blocks kept, 13.9; 1 x 4096 -> 16384 14.6, 4.6 TB/s).
+// (us, 1 x 4096 -> 4096: 5.8 to 6.2, with rows that are codes 5.4; 1 x 25088 -> 4096, half of the blocks kept, 13.4; 1 x 4096 -> 16384 14.6 to 15.1, 4.5 TB/s).
 #include "bsp_f8.h"
 
 namespace {

@@ -245,7 +245,8 @@ __global__ __launch_bounds__(64 * WAVES, C > 1 ? 2 : WAVES == 4 ? 3 : 4) void f8
 
   // Step i in buffer i mod 2, a half of it (sixteen rows) read while the other is multiplied; one barrier, between the halves, behind which
   // the next step's buffer is whole and this one's is free for the step after that.  Nothing inside is conditional, so that
-  // a wait for what a register asked for covers no more than that.
+  // a wait for what a register asked for can be by count: it is on one and on four blocks a workgroup.  On two the
+  // compiler moves the shift of the later step's scales up and waits for all that is under way, every second step.
   auto run = [&](auto ENDS) {
     u32x4_t y[2][MO], x[2][2];
     auto meet = [&]() {
@@ -372,8 +373,9 @@ __global__ __launch_bounds__(256) void f8_grad_finish(F8GradArgs a) {
   }
 }
 
-// Kept blocks a workgroup: more of them share a block row's gradients and take longer, so it goes by how often the chip is filled.  A CU holds two workgroups of
-// one or two blocks or one of four; us a step where it is full: 0.62, 0.98, 0.94, and 6 a round to begin and end.  Measured (us for one, two, four blocks):
+// Kept blocks a workgroup: more of them share a block row's gradients and take longer, so it goes by how often the chip is filled.  The model counts two workgroups of
+// one or two blocks a CU or one of four (single blocks on four waves would fit three; their step was taken from those on eight); us a step where it is full: 0.62, 0.98,
+// 0.94, and 6 a round to begin and end.  Measured (us for one, two, four blocks):
 //   all kept: 8192 x 4096 -> 16384 1241 1051 1017, 8192 x 8192 -> 8192 1183 981 971 (930, 1120, 1133 TFLOP/s), 2048 x 4096 -> 4096 84 75 75, 2048 x 4096 -> 4097 104 109 121
 //   under random masks: 8192 x 8192 -> 8192 half 663 583 645, a quarter 386 391 444, 2048 x 4096 -> 4096 half 61 66 67, 3000 x 16384 -> 1024 0.3 57 63 87,
 //   4096 x 4096 -> 4096 a quarter 72 79 113, 0.7 140 120 123, 4052 x 19902 -> 2966 a quarter 256 298 248
@@ -418,7 +420,7 @@ int launch(F8GradArgs a, hipStream_t st) {
 
 }  // namespace
 
-// ... and where single blocks are a workgroup for every other CU or fewer, ranges of at least four steps: a step takes 0.5 us where a CU has one workgroup, 0.65 where it has two, and
+// ... and where single blocks are a workgroup for every other CU or fewer (more blocks in ranges were not measured), ranges of at least four steps: a step takes 0.5 us where a CU has one workgroup, 0.65 where it has two, and
 // the ranges' sums cost a launch and are written and read (us at 16384 rows, 1024 x 1024 in 4 and 8 ranges 74 and 55, 2048 x 1024 in 2 and 4 135 and 101; 2000 rows, 51
 // blocks of 4096 x 4096 in 5 and 10 39 and 51).
 int f8_grad_split(int64_t nnzb, int T) {

@@ -8,8 +8,9 @@
 // The gradient's threads own columns: each adds its columns' dw and db over all the rows that its workgroup takes, and
 // a second launch adds the workgroups' sums in a fixed order (no atomics: the same inputs give the same bits).
 // The forward pass can leave its result as 8-bit codes, from the fp32 values: sixteen neighbouring lanes hold a block of 128.
-// Measured: 16384 x 4096 bf16 forward 45 us (6.0 TB/s, where a copy runs at 6.2), backward 64 (6.3) and 4.6 for the sums; 2019 x 8000 bf16 15 and
-// 20 us; 1021 x 1000 fp32 4.7, 6.6 and 4.0; 2000 x 16001, read again for each pass, 38 and 62 us.  A wave a row instead of four: 97 us forward
+// Measured: 16384 x 4096 bf16 forward 45 us (6.0 TB/s, where a copy runs at 6.2), backward 64 (6.3) and 4.6 for the sums; 2019 x 8000 bf16 12.6,
+// 16.2 and 4.0; 1021 x 1000 fp32 4.7, 6.6 and 4.0; 2000 x 16001 24, 40 (6 of 128 registers in memory) and 8; 2000 x 17001, read again for each
+// pass, 44 forward, 47 for dx, 32 and 9 for the sums.  A wave a row instead of four: 97 us forward
 // at 16384 x 4096 against 60 at that time, since a CU then has a quarter of the requests under way.
 #include "bsp_f8.h"
 
