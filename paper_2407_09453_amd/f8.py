@@ -3,8 +3,8 @@ tensors.  Marshalling only: every call launches on the current stream of its ten
 tensors that it makes come from torch's allocator on that stream.
 
 With ``stream`` (a handle as an integer) a call does as under ``torch.cuda.stream`` of that stream: what it reads has to be
-ready there, and whoever uses its results elsewhere waits for it.  Nothing has to be kept until then: what it reads
-may be dropped at once, and so may its results behind uses in the stream that was current at the call.
+ready there and is kept until it is done there (unless a call in that stream made it), and whoever uses its results elsewhere
+waits for it.  Results may be dropped at any time, also behind uses in the stream that was current at the call.
 
 Gradients are calls of their own: none of these records a graph for autograd, and a call whose results would be part of one
 (an input requires a gradient, outside ``torch.no_grad``) says so with a warning.
@@ -73,32 +73,35 @@ def _unrecorded(depth: int):
 
 
 def _memory(v):
-    """The tensors on a GPU that an argument or a result is held in."""
+    """The tensors that a result is held in."""
     if isinstance(v, (tuple, list)):
         for x in v:
             yield from _memory(x)
     elif isinstance(v, BspCodes):
         yield v.buffer
-    elif isinstance(v, BspLayerF8):
-        yield from _memory((v.payload, v.scale, v.payload_t, v.scale_t, v.d_index, v.d_bias))
-    elif getattr(v, "is_cuda", False):
+    elif v is not None:
         yield v
 
 
 def _on_stream(stream, at, call, *args):
     """call(*args) in the stream of this handle, on the device of tensor ``at``.  Workspaces and results come from the allocator's pool of
     that stream: a block of the current stream's pool may be one that was dropped there with work on it still to come, which
-    the call, elsewhere, would not wait for."""
+    the call, elsewhere, would not wait for.  Nothing is recorded for that stream, which is its owner's: what is recorded
+    for a stream can be freed only while the stream is there."""
     import torch
-    here = torch.cuda.current_stream(at.device)
-    if int(stream) == here.cuda_stream:
+    if int(stream) == _current_stream(at):
         return call(*args)
+    here = torch.cuda.current_stream(at.device)
     # (an ExternalStream of no handle is not the default stream, but any of torch's)
     there = torch.cuda.ExternalStream(int(stream), device=at.device) if int(stream) else torch.cuda.default_stream(at.device)
-    with torch.cuda.stream(there):
+    device = torch.cuda.current_device()
+    torch.cuda.set_stream(there)  # (and its device; torch.cuda.stream's context takes twice as long)
+    try:
         result = call(*args)
-    for t in _memory((getattr(call, "__self__", None), args)):
-        t.record_stream(there)
+    finally:
+        torch.cuda.set_stream(here)
+        if device != there.device.index:
+            torch.cuda.set_device(device)
     for t in _memory(result):
         t.record_stream(here)
     return result

@@ -116,36 +116,57 @@ def test_results_may_be_dropped_behind_their_use(calls, name):
     assert all(torch.equal(a, b) for a, b in zip(read, want))
 
 
-def test_what_a_call_reads_may_be_dropped():
-    """Activation, codes, residual, gate, weights and the layer itself, dropped while the stream has the call still to do."""
+def test_what_calls_of_a_stream_pass_on_may_be_dropped():
+    """Codes, results and workspaces that calls in a stream made and others there read, dropped while the stream has it all to do."""
     import torch
     bsp = _bsp()
     gen = torch.Generator(device="cuda")
     gen.manual_seed(12)
     draw = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
-    W, b, x, r, dy = draw(512, 768) / 28, draw(512), draw(300, 768).to(torch.bfloat16), draw(300, 512).to(torch.bfloat16), draw(300, 512).to(torch.bfloat16)
+    layer, back = bsp.BspLayerF8(draw(512, 768) / 28, bias=draw(512)), bsp.BspLayerF8(draw(768, 512) / 22)
+    x, r, dy = draw(300, 768).to(torch.bfloat16), draw(300, 512).to(torch.bfloat16), draw(300, 512).to(torch.bfloat16)
 
-    def chain(stream, W, b, x, r, dy):
-        layer = bsp.BspLayerF8(W, bias=b)
-        if stream is not None:
-            torch.cuda.synchronize()
-            with torch.cuda.stream(torch.cuda.ExternalStream(stream)):
-                torch.cuda._sleep(HELD)
-        k = {} if stream is None else {"stream": stream}
-        codes = bsp.save8(x, **k)
-        y = layer.fc(x, residual=r, **k)
-        y2 = layer.fc(codes, residual=r, **k)
-        dx = layer.grad_input(dy, relu_of=codes, **k)
-        return y, y2, dx, *layer.grad_weight(dy, codes, **k)
-    want = [t.clone() for t in chain(None, W, b, x, r, dy)]
+    def chain(**k):
+        n, mean, rstd = bsp.layer_norm(x, code="e4m3", **k)
+        y = layer.fc(n, residual=r, relu=True, **k)
+        z = back.fc(bsp.save8(y, **k), **k)
+        dx = layer.grad_input(dy, relu_of=bsp.save8(z, **k), **k)
+        return z, layer.grad_weight(dy, n, **k), bsp.layer_norm_grad(dx, x, mean, rstd, **k)
+    want = _flat(chain())
     s = torch.cuda.Stream()
-    sizes = [t.numel() * t.element_size() for t in (x, r, dy)] + [bsp.BspCodes(300, 768).buffer.numel(), 512 * 768, 512 * 768, 2048]
+    sizes = [300 * 768 * 2, 300 * 512 * 2, bsp.BspCodes(300, 768).buffer.numel(), bsp.BspCodes(300, 512).buffer.numel(), 2 * 300 * 4, layer._bytes("grad", 300)]
     torch.cuda.synchronize()
-    got = chain(s.cuda_stream, W.clone(), b.clone(), x.clone(), r.clone(), dy.clone())
-    litter = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(3)]  # takes what was dropped
-    s.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(HELD)
+    got = chain(stream=s.cuda_stream)
+    litter = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(4)]  # takes what was dropped, where it can
     torch.cuda.synchronize()
-    assert all(torch.equal(a, w) for a, w in zip(got, want)) and len(litter) == 21
+    assert all(torch.equal(a, w) for a, w in zip(_flat(got), want)) and len(litter) == 24
+
+
+def test_a_stream_may_go_before_what_it_worked_on():
+    """A stream that is not torch's, destroyed by its owner when its work is done: inputs, layer and results are freed later."""
+    import ctypes
+    import torch
+    bsp = _bsp()
+    torch.cuda.synchronize()
+    hip = ctypes.CDLL(bsp.lib_path())  # (the runtime that the library itself is linked to)
+    x = torch.randn(700, 512, device="cuda").to(torch.bfloat16)
+    layer = bsp.BspLayerF8(torch.randn(640, 512, device="cuda"))
+    want = layer.fc(x)
+    W = torch.randn(640, 512, device="cuda")
+    torch.cuda.synchronize()
+    h = ctypes.c_void_p()
+    assert hip.hipStreamCreate(ctypes.byref(h)) == 0
+    codes = bsp.save8(x, stream=h.value)
+    y = layer.fc(codes, stream=h.value)
+    layer.update(W, stream=h.value)
+    assert hip.hipStreamSynchronize(h) == 0 and hip.hipStreamDestroy(h) == 0
+    assert torch.equal(y, want)
+    del x, layer, W, codes, y
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    assert torch.equal(torch.ones(1000, device="cuda") + 1, torch.full((1000,), 2.0, device="cuda"))
 
 
 def test_the_default_streams_handle():
@@ -261,7 +282,6 @@ def test_new_weights_and_bias_in_a_stream():
             torch.cuda._sleep(HELD // 4)
         first = layer.fc(x, stream=s.cuda_stream)
         layer.update(Wc, bias=bc, stream=s.cuda_stream)
-        del Wc, bc
         second = layer.fc(x, stream=s.cuda_stream)
         s.synchronize()
         with torch.cuda.stream(s):  # (where the results are ready)
@@ -272,3 +292,20 @@ def test_new_weights_and_bias_in_a_stream():
     y = layer.fc(x, stream=s.cuda_stream)
     s.synchronize()
     assert torch.equal(y, old)
+
+
+def test_the_current_stream_is_the_callers_afterwards():
+    """Also behind a call that is refused, and no other stream's handle is left current."""
+    import torch
+    bsp = _bsp()
+    layer, x = bsp.BspLayerF8(torch.randn(256, 128, device="cuda")), torch.randn(3, 128, device="cuda")
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for here in (torch.cuda.default_stream(), t):
+        with torch.cuda.stream(here):
+            layer.fc(x, stream=s.cuda_stream)
+            assert torch.cuda.current_stream() == here
+            with pytest.raises(AssertionError):
+                layer.fc(x[:, :100], stream=s.cuda_stream)
+            assert torch.cuda.current_stream() == here and torch.cuda.current_device() == 0
+    torch.cuda.synchronize()
