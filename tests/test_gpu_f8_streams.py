@@ -273,7 +273,7 @@ def test_new_weights_and_bias_in_a_stream():
     old, new = bsp.BspLayerF8(W, bias=b).fc(x), bsp.BspLayerF8(W2, bias=b2).fc(x)
     layer = bsp.BspLayerF8(W, bias=b)
     s = torch.cuda.Stream()
-    for _ in range(2):  # the first round warms up
+    for _ in range(2):  # the first turn warms up
         layer.update(W, bias=b)
         Wc, bc = W2.clone(), b2.clone()
         torch.cuda.synchronize()
