@@ -508,9 +508,46 @@ int bsp_layer_norm_grad(const void* dY, int64_t ld_dy, const void* X, int64_t ld
                         const float* mean, const float* rstd, const float* weight, void* dX, int64_t ld_dx,
                         float* dweight, float* dbias, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* Root-mean-square norm over the last axis, the residual stream's addition in the same pass:
+ *   H = X + residual, rounded to their type;  Y = H rstd weight, rstd = 1 / sqrt(mean H^2 + eps)
+ *   X, residual  device [T][D], dtype BSP_F32 or BSP_BF16, rows ldx, ldr elements apart; residual may be null, then H is X itself
+ *   H            device [T][D], rows ldh apart, written where there is a residual (else null); overlaps neither X nor the residual
+ *   weight       device float[D], or null (ones)
+ *   Y, codes     as for bsp_layer_norm: one of the two;  rstd  device float[T], written for the backward pass
+ * Squares are summed in fp32.  Errors: NULL, SHAPE, DTYPE, ALIGN, HIP.  T = 0 does nothing. */
+int bsp_rms_norm(const void* X, int64_t ldx, const void* residual, int64_t ldr, int32_t dtype, int32_t T, int32_t D, const float* weight, float eps,
+                 void* H, int64_t ldh, void* Y, int64_t ldy, const bsp_codes* codes, float* rstd, void* stream);
+/* Its gradient: dX [T][D], the gradient of X and of the residual alike, from dY, from dH (what reaches H along the residual stream,
+ * or null), from H and from rstd, all of one dtype; dweight float[D], or null.  workspace: bsp_rms_norm_grad_workspace bytes,
+ * 16-byte aligned.  Errors: NULL, SHAPE, DTYPE, ALIGN, CAPACITY, HIP.  T = 0 gives zeros. */
+int bsp_rms_norm_grad_workspace(int32_t T, int32_t D, int64_t* bytes);
+int bsp_rms_norm_grad(const void* dY, int64_t ld_dy, const void* H, int64_t ldh, const void* dH, int64_t ld_dh, int32_t dtype, int32_t T, int32_t D,
+                      const float* rstd, const float* weight, void* dX, int64_t ld_dx, float* dweight, void* workspace,
+                      int64_t workspace_bytes, void* stream);
+
+/* Log probabilities from logits.  With z = scale X, for each row of X [T][V] (V <= 2^21):
+ *   lse[t] = log sum e^z;  logp[t] = z[token] - lse;  entropy[t] = - sum p log p, p = e^(z - lse)
+ *   top_logp, top_tokens [T][top]: the largest log probabilities in their order and whose they are; of equal logits the lower token
+ *                 first, NaN before all; top <= 64, top <= V; both null with top = 0
+ *   X             device, BSP_F32 or BSP_BF16, rows ldx elements apart; minus infinity is a token that cannot be
+ *   tokens        device [T], token_bytes 4 (int32) or 8 (int64).  Below 0: none is given (padding), logp[t] = 0; V and above: NaN
+ *   scale         above 0: the inverse of a temperature
+ * A row of minus infinities alone has no token left: lse and log probabilities are minus infinity, the entropy is 0.  A row that holds a NaN or
+ * plus infinity gives NaN.  The results are float; workspace: bsp_log_probs_workspace bytes, 16-byte aligned.
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, CAPACITY, HIP.  T = 0 does nothing. */
+int bsp_log_probs_workspace(int32_t T, int32_t V, int32_t top, int64_t* bytes);
+int bsp_log_probs(const void* X, int64_t ldx, int32_t dtype, int32_t T, int32_t V, const void* tokens, int32_t token_bytes, float scale, int32_t top,
+                  float* logp, float* lse, float* entropy, float* top_logp, int32_t* top_tokens, void* workspace, int64_t workspace_bytes, void* stream);
+/* The logits' gradient from those of logp and of the entropy (float[T], either may be null: zeros):
+ *   dX = scale (dlogp ([token] - p) - dentropy p (log p + entropy))
+ * in X's type, rows ld_dx apart; dX may be X itself.  Rows without a token take nothing from dlogp, rows of minus infinities alone get
+ * zeros, rows with a token of V and above NaN.  lse and entropy: what bsp_log_probs wrote.  Errors: NULL, SHAPE, DTYPE, ALIGN, HIP. */
+int bsp_log_probs_grad(const void* X, int64_t ldx, int32_t dtype, int32_t T, int32_t V, const void* tokens, int32_t token_bytes, float scale,
+                       const float* lse, const float* entropy, const float* dlogp, const float* dentropy, void* dX, int64_t ld_dx, void* stream);
+
 /* The calls above in packed form (as bsp_call_packed, for callers that pay for every argument): one array of words, pointers as
  * addresses, other arguments as signed integers in the order of the call's own arguments, with these differences: a
- * bsp_codes is five words (T, K, dtype, codes, scale), all zero for a null one; eps is the bits of a double in its word.
+ * bsp_codes is five words (T, K, dtype, codes, scale), all zero for a null one; eps and scale are the bits of a double in their word.
  *   BSP_F8_CALL_SAVE       X, x_dtype, ldx, codes c, stream                                                  9 words
  *   BSP_F8_CALL_LOAD       codes c, Y, y_dtype, ldy, stream                                                  9
  *   BSP_F8_CALL_FC         w, transposed, codes X, bias, residual, relu, codes gate, Y, y_dtype, workspace,
@@ -520,10 +557,13 @@ int bsp_layer_norm_grad(const void* dY, int64_t ld_dy, const void* X, int64_t ld
  *   BSP_F8_CALL_GRAD       w, dY, ldy, codes X, dW, db, workspace, workspace_bytes, stream                  13
  *   BSP_F8_CALL_NORM       X, dtype, ldx, T, D, weight, bias, eps, Y, ldy, codes, mean, rstd, stream        18
  *   BSP_F8_CALL_NORM_GRAD  the seventeen of bsp_layer_norm_grad                                             17
+ *   BSP_F8_CALL_RMS_NORM   X, ldx, residual, ldr, dtype, T, D, weight, eps, H, ldh, Y, ldy, codes, rstd, stream   20
+ *   BSP_F8_CALL_RMS_NORM_GRAD, BSP_F8_CALL_LOG_PROBS, BSP_F8_CALL_LOG_PROBS_GRAD: the arguments of the call    17, 17, 15
  * Errors: NULL (words), SHAPE (unknown call), otherwise those of the call. */
 enum bsp_f8_call {
   BSP_F8_CALL_SAVE = 0, BSP_F8_CALL_LOAD = 1, BSP_F8_CALL_FC = 2, BSP_F8_CALL_VALUES = 3, BSP_F8_CALL_GRAD = 4,
-  BSP_F8_CALL_NORM = 5, BSP_F8_CALL_NORM_GRAD = 6
+  BSP_F8_CALL_NORM = 5, BSP_F8_CALL_NORM_GRAD = 6, BSP_F8_CALL_RMS_NORM = 16, BSP_F8_CALL_RMS_NORM_GRAD = 17,
+  BSP_F8_CALL_LOG_PROBS = 18, BSP_F8_CALL_LOG_PROBS_GRAD = 19
 };
 int bsp_f8_call_packed(int32_t call, const int64_t* words);
 

@@ -37,7 +37,8 @@ EXPORTS = ("bsp_strerror", "bsp_version", "bsp_pack_count", "bsp_pack", "bsp_unp
            "bsp_conv2d_only", "bsp_bottleneck", "bsp_call_packed", "bsp_bench_copy", "bsp_bench_mfma_bf16", "bsp_bench_lds_read",
            "bsp_f8_save", "bsp_f8_load", "bsp_f8_count", "bsp_f8_index", "bsp_f8_pack", "bsp_f8_fc", "bsp_f8_fc_workspace",
            "bsp_f8_fc_values", "bsp_f8_fc_grad_workspace", "bsp_f8_fc_grad", "bsp_layer_norm", "bsp_layer_norm_grad_workspace",
-           "bsp_layer_norm_grad", "bsp_f8_call_packed")
+           "bsp_layer_norm_grad", "bsp_f8_call_packed", "bsp_rms_norm", "bsp_rms_norm_grad_workspace", "bsp_rms_norm_grad",
+           "bsp_log_probs_workspace", "bsp_log_probs", "bsp_log_probs_grad")
 
 
 class BspError(RuntimeError):
@@ -161,7 +162,13 @@ def load_library():
                        ("bsp_f8_fc_grad", [fp, vp, i64, cp, vp, vp, vp, i64, vp]),
                        ("bsp_layer_norm", [vp, i32, i64, i32, i32, vp, vp, ctypes.c_float, vp, i64, cp, vp, vp, vp]),
                        ("bsp_layer_norm_grad_workspace", [i32, i32, pi64]),
-                       ("bsp_layer_norm_grad", [vp, i64, vp, i64, i32, i32, i32, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp])):
+                       ("bsp_layer_norm_grad", [vp, i64, vp, i64, i32, i32, i32, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp]),
+                       ("bsp_rms_norm", [vp, i64, vp, i64, i32, i32, i32, vp, ctypes.c_float, vp, i64, vp, i64, cp, vp, vp]),
+                       ("bsp_rms_norm_grad_workspace", [i32, i32, pi64]),
+                       ("bsp_rms_norm_grad", [vp, i64, vp, i64, vp, i64, i32, i32, i32, vp, vp, vp, i64, vp, vp, i64, vp]),
+                       ("bsp_log_probs_workspace", [i32, i32, i32, pi64]),
+                       ("bsp_log_probs", [vp, i64, i32, i32, i32, vp, i32, ctypes.c_float, i32, vp, vp, vp, vp, vp, vp, i64, vp]),
+                       ("bsp_log_probs_grad", [vp, i64, i32, i32, i32, vp, i32, ctypes.c_float, vp, vp, vp, vp, vp, i64, vp])):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = ctypes.c_int, args
     lib.bsp_f8_call_packed.restype, lib.bsp_f8_call_packed.argtypes = ctypes.c_int, [i32, ctypes.c_char_p]

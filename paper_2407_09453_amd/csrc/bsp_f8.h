@@ -314,5 +314,19 @@ int norm_launch_forward(const void* X, bool f32, int64_t ldx, int T, int D, cons
                         void* Y, int64_t ldy, int code, uint8_t* codes, uint8_t* scale, float* mean, float* rstd, hipStream_t st);
 int norm_launch_backward(const void* dY, int64_t ld_dy, const void* X, int64_t ldx, bool f32, const float* mean, const float* rstd, const float* weight,
                          int T, int D, void* dX, int64_t ld_dx, float* dweight, float* dbias, float* part, hipStream_t st);
+// out[c] = sum over p of part[p][c], in their order; columns from split_at on to out2; either may be null
+int norm_launch_sum(const float* part, int parts, int64_t width, int64_t split_at, float* out, float* out2, hipStream_t st);
+// root-mean-square norm: h = x + residual in their type, y = h rstd weight
+int rms_launch_forward(const void* X, int64_t ldx, const void* residual, int64_t ldr, bool f32, int T, int D, const float* weight, float eps, void* H,
+                       int64_t ldh, void* Y, int64_t ldy, int code, uint8_t* codes, uint8_t* scale, float* rstd, hipStream_t st);
+int rms_parts(int T, int D);
+int rms_launch_backward(const void* dY, int64_t ld_dy, const void* H, int64_t ldh, const void* dH, int64_t ld_dh, bool f32, const float* rstd,
+                        const float* weight, int T, int D, void* dX, int64_t ld_dx, float* dweight, float* part, hipStream_t st);
+// log probabilities, entropy and the k likeliest of rows of logits, and the logits' gradient; workspace: logp_workspace bytes
+int64_t logp_workspace(int T, int V, int k);
+int logp_launch(const void* X, bool f32, int64_t ld, int T, int V, const void* tokens, bool wide_tokens, float scale, int k, float* logp, float* lse,
+                float* entropy, float* top, int32_t* ids, void* workspace, hipStream_t st);
+int logp_launch_grad(const void* X, bool f32, int64_t ld, int T, int V, const void* tokens, bool wide_tokens, float scale, const float* lse, const float* entropy,
+                     const float* dlogp, const float* dentropy, void* dX, int64_t ld_dx, hipStream_t st);
 
 #endif

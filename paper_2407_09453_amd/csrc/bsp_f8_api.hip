@@ -1,4 +1,4 @@
-// extern "C" entry points of the 8-bit floating-point layers and of layer norm: argument checks and dispatch.
+// extern "C" entry points of the 8-bit floating-point layers, the norms and log probabilities: argument checks and dispatch.
 #include "bsp_f8.h"
 
 #include <string.h>
@@ -11,6 +11,8 @@ inline bool code_type(int d) { return d == BSP_E4M3 || d == BSP_E5M2; }
 inline unsigned size_of(int d) { return d == BSP_F32 ? 4 : 2; }
 constexpr int32_t kMost = INT32_MAX - 65536;  // rows and columns: sizes rounded up stay in 32 bits
 constexpr int32_t kWide = 1 << 24;            // columns of codes: 256 rows' offsets stay in 32 bits
+constexpr int32_t kVocabulary = 1 << 21;      // logits of a row: 64 chunks of what a workgroup's registers hold
+constexpr int32_t kTop = 64;                  // likeliest tokens: one of 64 groups' largest is below the last of them
 
 // a matrix of values whose rows are `ld` elements apart; rows of an input may be the same one (ld = 0)
 int check_values(const void* p, int dtype, int64_t ld, int T, int K, bool input) {
@@ -256,6 +258,96 @@ int bsp_layer_norm_grad(const void* dY, int64_t ld_dy, const void* X, int64_t ld
   return norm_launch_backward(dY, ld_dy, X, ldx, dtype == BSP_F32, mean, rstd, weight, T, D, dX, ld_dx, dweight, dbias, (float*)workspace, (hipStream_t)stream);
 }
 
+int bsp_rms_norm(const void* X, int64_t ldx, const void* residual, int64_t ldr, int32_t dtype, int32_t T, int32_t D, const float* weight, float eps,
+                 void* H, int64_t ldh, void* Y, int64_t ldy, const bsp_codes* codes, float* rstd, void* stream) {
+  int rc = check_values(X, dtype, ldx, T, D, true);
+  if (rc != BSP_OK) return rc;
+  if (!(eps >= 0.f)) return BSP_ERR_SHAPE;
+  if (T > 0 && ((Y != nullptr) == (codes != nullptr) || (residual != nullptr) != (H != nullptr))) return BSP_ERR_NULL;
+  if (residual) {
+    rc = check_values(residual, dtype, ldr, T, D, true);
+    if (rc == BSP_OK) rc = check_values(H, dtype, ldh, T, D, false);
+    if (rc != BSP_OK) return rc;
+  }
+  if (codes) {
+    rc = check_codes(codes);
+    if (rc != BSP_OK) return rc;
+    if (codes->T != T || codes->K != D) return BSP_ERR_SHAPE;
+  } else {
+    rc = check_values(Y, dtype, ldy, T, D, false);
+    if (rc != BSP_OK) return rc;
+  }
+  if (T == 0) return BSP_OK;
+  if (!rstd) return BSP_ERR_NULL;
+  if (!aligned(rstd, 4) || !aligned(weight, 4)) return BSP_ERR_ALIGN;
+  return rms_launch_forward(X, ldx, residual, ldr, dtype == BSP_F32, T, D, weight, eps, H, ldh, Y, ldy, codes ? codes->dtype : 0,
+                            codes ? codes->codes : nullptr, codes ? codes->scale : nullptr, rstd, (hipStream_t)stream);
+}
+
+int bsp_rms_norm_grad_workspace(int32_t T, int32_t D, int64_t* bytes) {
+  if (!bytes) return BSP_ERR_NULL;
+  if (T < 0 || T > kMost || D < 1 || D > kMost) return BSP_ERR_SHAPE;
+  const int64_t parts = rms_parts(T, D);
+  *bytes = parts > 1 ? parts * D * 4 : 0;
+  return BSP_OK;
+}
+
+int bsp_rms_norm_grad(const void* dY, int64_t ld_dy, const void* H, int64_t ldh, const void* dH, int64_t ld_dh, int32_t dtype, int32_t T, int32_t D,
+                      const float* rstd, const float* weight, void* dX, int64_t ld_dx, float* dweight, void* workspace,
+                      int64_t workspace_bytes, void* stream) {
+  int64_t need = 0;
+  int rc = bsp_rms_norm_grad_workspace(T, D, &need);
+  if (rc == BSP_OK) rc = check_values(dY, dtype, ld_dy, T, D, true);
+  if (rc == BSP_OK) rc = check_values(H, dtype, ldh, T, D, true);
+  if (rc == BSP_OK && dH) rc = check_values(dH, dtype, ld_dh, T, D, true);
+  if (rc == BSP_OK) rc = check_values(dX, dtype, ld_dx, T, D, false);
+  if (rc != BSP_OK) return rc;
+  if (T > 0 && !rstd) return BSP_ERR_NULL;
+  if (!aligned(rstd, 4) || !aligned(weight, 4) || !aligned(dweight, 4)) return BSP_ERR_ALIGN;
+  rc = check_workspace(workspace, workspace_bytes, need);
+  if (rc != BSP_OK) return rc;
+  return rms_launch_backward(dY, ld_dy, H, ldh, dH, ld_dh, dtype == BSP_F32, rstd, weight, T, D, dX, ld_dx, dweight, (float*)workspace, (hipStream_t)stream);
+}
+
+int bsp_log_probs_workspace(int32_t T, int32_t V, int32_t top, int64_t* bytes) {
+  if (!bytes) return BSP_ERR_NULL;
+  if (T < 0 || T > kMost || V < 1 || V > kVocabulary || top < 0 || top > kTop || top > V) return BSP_ERR_SHAPE;
+  *bytes = T > 0 ? logp_workspace(T, V, top) : 0;
+  return BSP_OK;
+}
+
+int bsp_log_probs(const void* X, int64_t ldx, int32_t dtype, int32_t T, int32_t V, const void* tokens, int32_t token_bytes, float scale, int32_t top,
+                  float* logp, float* lse, float* entropy, float* top_logp, int32_t* top_tokens, void* workspace, int64_t workspace_bytes, void* stream) {
+  int64_t need = 0;
+  int rc = bsp_log_probs_workspace(T, V, top, &need);
+  if (rc == BSP_OK) rc = check_values(X, dtype, ldx, T, V, true);
+  if (rc != BSP_OK) return rc;
+  if (token_bytes != 4 && token_bytes != 8) return BSP_ERR_DTYPE;
+  if (!(scale > 0.f) || scale > 3.4028234e38f) return BSP_ERR_SHAPE;
+  if (T == 0) return BSP_OK;
+  if (!tokens || !logp || !lse || !entropy || (top && (!top_logp || !top_tokens))) return BSP_ERR_NULL;
+  if (!aligned(tokens, token_bytes) || !aligned(logp, 4) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(top_logp, 4) || !aligned(top_tokens, 4)) return BSP_ERR_ALIGN;
+  rc = check_workspace(workspace, workspace_bytes, need);
+  if (rc != BSP_OK) return rc;
+  return logp_launch(X, dtype == BSP_F32, ldx, T, V, tokens, token_bytes == 8, scale, top, logp, lse, entropy, top_logp, top_tokens, workspace, (hipStream_t)stream);
+}
+
+int bsp_log_probs_grad(const void* X, int64_t ldx, int32_t dtype, int32_t T, int32_t V, const void* tokens, int32_t token_bytes, float scale,
+                       const float* lse, const float* entropy, const float* dlogp, const float* dentropy, void* dX, int64_t ld_dx, void* stream) {
+  int64_t none = 0;
+  int rc = bsp_log_probs_workspace(T, V, 0, &none);
+  if (rc == BSP_OK) rc = check_values(X, dtype, ldx, T, V, true);
+  if (rc == BSP_OK) rc = check_values(dX, dtype, ld_dx, T, V, false);
+  if (rc != BSP_OK) return rc;
+  if (token_bytes != 4 && token_bytes != 8) return BSP_ERR_DTYPE;
+  if (!(scale > 0.f) || scale > 3.4028234e38f) return BSP_ERR_SHAPE;
+  if (T == 0) return BSP_OK;
+  if (!tokens || !lse || !entropy) return BSP_ERR_NULL;
+  if (!aligned(tokens, token_bytes) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(dlogp, 4) || !aligned(dentropy, 4)) return BSP_ERR_ALIGN;
+  if (X == dX && ldx != ld_dx && T > 1) return BSP_ERR_SHAPE;  // in place row for row
+  return logp_launch_grad(X, dtype == BSP_F32, ldx, T, V, tokens, token_bytes == 8, scale, lse, entropy, dlogp, dentropy, dX, ld_dx, (hipStream_t)stream);
+}
+
 int bsp_f8_call_packed(int32_t call, const int64_t* w) {
   if (!w) return BSP_ERR_NULL;
   auto ptr = [&](int i) { return (void*)(intptr_t)w[i]; };
@@ -264,6 +356,11 @@ int bsp_f8_call_packed(int32_t call, const int64_t* w) {
   auto size = [&](int i) { return w[i] < 0 || w[i] > INT32_MAX ? -1 : (int32_t)w[i]; };
   auto codes = [&](int i) { return bsp_codes{size(i), size(i + 1), num(i + 2), (uint8_t*)ptr(i + 3), (uint8_t*)ptr(i + 4)}; };
   auto none = [&](int i) { return !(w[i] | w[i + 1] | w[i + 2] | w[i + 3] | w[i + 4]); };
+  auto real = [&](int i) {
+    double v;
+    memcpy(&v, &w[i], sizeof v);
+    return v;
+  };
   switch (call) {
     case BSP_F8_CALL_SAVE: {
       const bsp_codes c = codes(3);
@@ -288,14 +385,26 @@ int bsp_f8_call_packed(int32_t call, const int64_t* w) {
     }
     case BSP_F8_CALL_NORM: {
       const bsp_codes c = codes(10);
-      double eps;
-      memcpy(&eps, &w[7], sizeof eps);
-      return bsp_layer_norm(ptr(0), num(1), w[2], size(3), size(4), (const float*)ptr(5), (const float*)ptr(6), (float)eps, ptr(8), w[9],
+      return bsp_layer_norm(ptr(0), num(1), w[2], size(3), size(4), (const float*)ptr(5), (const float*)ptr(6), (float)real(7), ptr(8), w[9],
                             none(10) ? nullptr : &c, (float*)ptr(15), (float*)ptr(16), ptr(17));
     }
     case BSP_F8_CALL_NORM_GRAD:
       return bsp_layer_norm_grad(ptr(0), w[1], ptr(2), w[3], num(4), size(5), size(6), (const float*)ptr(7), (const float*)ptr(8), (const float*)ptr(9),
                                  ptr(10), w[11], (float*)ptr(12), (float*)ptr(13), ptr(14), w[15], ptr(16));
+    case BSP_F8_CALL_RMS_NORM: {
+      const bsp_codes c = codes(13);
+      return bsp_rms_norm(ptr(0), w[1], ptr(2), w[3], num(4), size(5), size(6), (const float*)ptr(7), (float)real(8), ptr(9), w[10], ptr(11), w[12],
+                          none(13) ? nullptr : &c, (float*)ptr(18), ptr(19));
+    }
+    case BSP_F8_CALL_RMS_NORM_GRAD:
+      return bsp_rms_norm_grad(ptr(0), w[1], ptr(2), w[3], ptr(4), w[5], num(6), size(7), size(8), (const float*)ptr(9), (const float*)ptr(10), ptr(11), w[12],
+                               (float*)ptr(13), ptr(14), w[15], ptr(16));
+    case BSP_F8_CALL_LOG_PROBS:
+      return bsp_log_probs(ptr(0), w[1], num(2), size(3), size(4), ptr(5), num(6), (float)real(7), num(8), (float*)ptr(9), (float*)ptr(10), (float*)ptr(11),
+                           (float*)ptr(12), (int32_t*)ptr(13), ptr(14), w[15], ptr(16));
+    case BSP_F8_CALL_LOG_PROBS_GRAD:
+      return bsp_log_probs_grad(ptr(0), w[1], num(2), size(3), size(4), ptr(5), num(6), (float)real(7), (const float*)ptr(8), (const float*)ptr(9),
+                                (const float*)ptr(10), (const float*)ptr(11), ptr(12), w[13], ptr(14));
   }
   return BSP_ERR_SHAPE;
 }

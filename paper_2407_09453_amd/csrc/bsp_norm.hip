@@ -12,7 +12,7 @@
 // 16.2 and 4.0; 1021 x 1000 fp32 4.7, 6.6 and 4.0; 2000 x 16001 24, 40 (6 of 128 registers in memory) and 8; 2000 x 17001, read again for each
 // pass, 44 forward, 47 for dx, 32 and 9 for the sums.  A wave a row instead of four: 97 us forward
 // at 16384 x 4096 against 60 at that time, since a CU then has a quarter of the requests under way.
-#include "bsp_f8.h"
+#include "bsp_norm.h"
 
 namespace {
 
@@ -26,68 +26,6 @@ struct NormArgs {
   int32_t T, D, Dp, e5, parts;
   float eps;
 };
-
-template <bool F32>
-__device__ __forceinline__ const void* row_of(const void* X, int64_t row, int64_t ld) {
-  return F32 ? (const void*)((const float*)X + row * ld) : (const void*)((const uint16_t*)X + row * ld);
-}
-// eight values of a row of any length, one by one
-template <bool F32>
-__device__ __forceinline__ void each8(const void* row, int c, int n, float* v) {
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    v[k] = 0.f;
-    if (c + k < n) v[k] = F32 ? ((const float*)row)[c + k] : bf16_bits_to_f32(((const uint16_t*)row)[c + k]);
-  }
-}
-template <bool F32>
-__device__ __forceinline__ void load8(const void* row, int c, int n, float* v) {
-  if (n >= 8) f8_unpack8<F32>(f8_raw8<F32>(row, c, n), f8_past(c, n), (n & 7) != 0, v);
-  else each8<F32>(row, c, n, v);
-}
-
-// sums of N values over the threads of a row (16 lanes, a wave, the workgroup)
-template <int ROWT, int N>
-__device__ __forceinline__ void row_sum(float* v, float (*sh)[N]) {
-#pragma unroll
-  for (int k = 0; k < N; ++k) v[k] = ROWT == 16 ? f8_row16_sum(v[k]) : f8_wave_sum(v[k]);
-  if constexpr (ROWT >= 256) {
-    __syncthreads();  // the last use of sh is over
-    if ((threadIdx.x & 63) == 0)
-#pragma unroll
-      for (int k = 0; k < N; ++k) sh[threadIdx.x >> 6][k] = v[k];
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      v[k] = 0.f;
-#pragma unroll
-      for (int w = 0; w < ROWT / 64; ++w) v[k] += sh[w][k];
-    }
-  }
-}
-
-// eight results of a row: in X's type, or as codes
-template <bool F32, bool CODES>
-__device__ __forceinline__ void put8(const NormArgs& a, int64_t row, int c, float* y) {
-  if constexpr (CODES) {
-    if (c >= a.Dp) return;  // (whole groups of sixteen lanes: Dp is a multiple of 128)
-    uint32_t m = 0;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) m = max(m, f8_magnitude(y[k]));
-    m = f8_most<16>(m);
-    const int b = a.e5 ? f8_scale_byte<true>(m) : f8_scale_byte<false>(m);
-    const float s = f8_inverse(b);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) y[k] *= s;
-    u32x2_t q;
-    if (a.e5) q = u32x2_t{f8_encode4<true>(y[0], y[1], y[2], y[3]), f8_encode4<true>(y[4], y[5], y[6], y[7])};
-    else q = u32x2_t{f8_encode4<false>(y[0], y[1], y[2], y[3]), f8_encode4<false>(y[4], y[5], y[6], y[7])};
-    *(u32x2_t*)(a.codes + row * a.Dp + c) = q;
-    if ((threadIdx.x & 15) == 0) a.scale[(int64_t)(c >> 7) * a.srows + row] = (uint8_t)b;
-  } else if (c < a.D) {
-    f8_store8<F32>((void*)row_of<F32>(a.Y, row, a.ldy), c, a.D - c, y);
-  }
-}
 
 // NV: groups of eight columns a thread holds; 0: rows of any length, read three times
 template <bool F32, bool CODES, int ROWT, int NV>
@@ -374,12 +312,12 @@ int backward(const NormArgs& a, hipStream_t st) {
   return launched();
 }
 
-int sum(const float* part, int parts, int64_t width, int64_t split_at, float* out, float* out2, hipStream_t st) {
+}  // namespace
+
+int norm_launch_sum(const float* part, int parts, int64_t width, int64_t split_at, float* out, float* out2, hipStream_t st) {
   hipLaunchKernelGGL(norm_sum, f8_grid((width + 63) / 64), dim3(1024), 0, st, part, parts, width, split_at, out, out2);
   return launched();
 }
-
-}  // namespace
 
 // Workgroups that share the rows.  Where one is done with all of them in eight turns its sums are the result: a launch less.
 int norm_parts(int T, int D) {
@@ -404,5 +342,5 @@ int norm_launch_backward(const void* dY, int64_t ld_dy, const void* X, int64_t l
   a.ldx = ldx, a.ld_dy = ld_dy, a.ld_dx = ld_dx, a.T = T, a.D = D, a.parts = norm_parts(T, D);
   const int rc = f32 ? backward<true>(a, st) : backward<false>(a, st);
   if (rc != BSP_OK || a.parts == 1) return rc;
-  return sum(part, a.parts, 2 * (int64_t)D, D, dweight, dbias, st);
+  return norm_launch_sum(part, a.parts, 2 * (int64_t)D, D, dweight, dbias, st);
 }

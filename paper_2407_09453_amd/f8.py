@@ -1,4 +1,4 @@
-"""FC layers in 8-bit floating point, the 8-bit checkpoints of their inputs, their gradients, and layer norm, on torch
+"""FC layers in 8-bit floating point, the 8-bit checkpoints of their inputs, their gradients, and the norms, on torch
 tensors.  Marshalling only: every call launches on the current stream of its tensors' device and returns before it is done;
 tensors that it makes come from torch's allocator on that stream.
 
@@ -25,8 +25,9 @@ from .binding import (BSP_BF16, BSP_E4M3, BSP_E5M2, BSP_F32, BspError, _check, _
 
 CODES = {"e4m3": BSP_E4M3, "e5m2": BSP_E5M2}
 _SAVE, _LOAD, _FC, _VALUES, _GRAD, _NORM, _NORM_GRAD = range(7)
+_RMS, _RMS_GRAD = 16, 17
 _pack9, _pack13, _pack17, _pack18, _pack20 = (struct.Struct("=%dq" % n).pack for n in (9, 13, 17, 18, 20))
-_pack_norm = struct.Struct("=7qd10q").pack
+_pack_norm, _pack_rms = struct.Struct("=7qd10q").pack, struct.Struct("=8qd11q").pack
 _NO_CODES = (0, 0, 0, 0, 0)
 _types = _torch = None
 
@@ -370,22 +371,84 @@ def layer_norm_grad(dY, X, mean, rstd, weight=None, stream=None):
     _on(X, dY, mean, rstd, weight)
     dX = torch.empty((T, D), dtype=X.dtype, device=X.device)
     dw, db = torch.empty((2, D), dtype=torch.float32, device=X.device).unbind(0)
-    n = _norm_bytes(T, D)
+    n = _norm_bytes("bsp_layer_norm_grad_workspace", T, D)
     ws = torch.empty(n, dtype=torch.uint8, device=X.device) if n else None
     _call(_NORM_GRAD, _pack17(dY.data_ptr(), ld_dy, X.data_ptr(), ld, _type(X), T, D, mean.data_ptr(), rstd.data_ptr(), _vector(weight, D),
                               dX.data_ptr(), D, dw.data_ptr(), db.data_ptr(), 0 if ws is None else ws.data_ptr(), n, _current_stream(X)), "bsp_layer_norm_grad")
     return dX, dw, db
 
 
+def rms_norm(X, weight=None, residual=None, eps: float = 1e-6, code: Optional[str] = None, stream=None):
+    """(Y, H, rstd) of X [T][D] (fp32 or bf16): H = X + residual rounded to their type (X itself where there is none), the residual
+    stream as it goes on; Y = H rstd weight, rstd the inverse of H's root mean square over its last axis; ``weight`` is float [D]
+    or None.  With ``code`` ("e4m3", "e5m2") Y is a BspCodes, the form in which a BspLayerF8 reads it."""
+    if stream is not None:
+        Y, H, rstd = _on_stream(stream, X, _rms_norm, X, weight, residual, eps, code)
+        return Y, X if H is None else H, rstd
+    if X.requires_grad or (weight is not None and weight.requires_grad) or (residual is not None and residual.requires_grad):
+        _unrecorded(3)
+    Y, H, rstd = _rms_norm(X, weight, residual, eps, code)
+    return Y, X if H is None else H, rstd
+
+
+def _rms_norm(X, weight, residual, eps, code):
+    import torch
+    T, D, ld = _rows(X)
+    _on(X, weight, residual)
+    kind = _type(X)
+    H, r, ldr, h = None, 0, 0, 0
+    if residual is not None:
+        T2, D2, ldr = _rows(residual)
+        assert (T2, D2) == (T, D) and residual.dtype == X.dtype, "a residual of X's shape and type"
+        H = torch.empty((T, D), dtype=X.dtype, device=X.device)
+        r, h = residual.data_ptr(), H.data_ptr()
+    rstd = torch.empty(T, dtype=torch.float32, device=X.device)
+    if code is None:
+        Y = torch.empty((T, D), dtype=X.dtype, device=X.device)
+        y, words = Y.data_ptr(), _NO_CODES
+    else:
+        Y = BspCodes(T, D, code, X.device)
+        y, words = 0, Y.words
+    _call(_RMS, _pack_rms(X.data_ptr(), ld, r, ldr, kind, T, D, _vector(weight, D), eps, h, D, y, D, *words, rstd.data_ptr(), _current_stream(X)), "bsp_rms_norm")
+    return Y, H, rstd
+
+
+def rms_norm_grad(dY, H, rstd, weight=None, dH=None, stream=None):
+    """(dX, dweight) from the gradient of Y, what ``rms_norm`` returned with it, and the gradient that reaches H itself along the
+    residual stream, where there is one.  dX is the gradient of X and of the residual alike."""
+    import torch
+    if stream is not None:
+        return _on_stream(stream, H, rms_norm_grad, dY, H, rstd, weight, dH)
+    if dY.requires_grad or H.requires_grad or (weight is not None and weight.requires_grad) or (dH is not None and dH.requires_grad):
+        _unrecorded(3)
+    T, D, ld = _rows(H)
+    T2, D2, ld_dy = _rows(dY)
+    assert (T2, D2) == (T, D) and dY.dtype == H.dtype and rstd.shape == (T,)
+    assert _type(rstd) == BSP_F32 and (T < 2 or rstd.stride() == (1,))
+    d, ld_dh = 0, 0
+    if dH is not None:
+        T2, D2, ld_dh = _rows(dH)
+        assert (T2, D2) == (T, D) and dH.dtype == H.dtype
+        d = dH.data_ptr()
+    _on(H, dY, rstd, weight, dH)
+    dX = torch.empty((T, D), dtype=H.dtype, device=H.device)
+    dw = torch.empty(D, dtype=torch.float32, device=H.device)
+    n = _norm_bytes("bsp_rms_norm_grad_workspace", T, D)
+    ws = torch.empty(n, dtype=torch.uint8, device=H.device) if n else None
+    _call(_RMS_GRAD, _pack17(dY.data_ptr(), ld_dy, H.data_ptr(), ld, d, ld_dh, _type(H), T, D, rstd.data_ptr(), _vector(weight, D), dX.data_ptr(), D,
+                             dw.data_ptr(), 0 if ws is None else ws.data_ptr(), n, _current_stream(H)), "bsp_rms_norm_grad")
+    return dX, dw
+
+
 _norm_sizes = {}
 
 
-def _norm_bytes(T, D):
-    n = _norm_sizes.get((T, D))
+def _norm_bytes(call, *sizes):
+    n = _norm_sizes.get((call, sizes))
     if n is None:
         n = ctypes.c_int64(0)
-        _check(load_library().bsp_layer_norm_grad_workspace(T, D, n), "bsp_layer_norm_grad_workspace")
+        _check(getattr(load_library(), call)(*sizes, n), call)
         if len(_norm_sizes) > 4096:
             _norm_sizes.clear()
-        n = _norm_sizes[(T, D)] = n.value
+        n = _norm_sizes[(call, sizes)] = n.value
     return n
