@@ -508,6 +508,54 @@ int bsp_layer_norm_grad(const void* dY, int64_t ld_dy, const void* X, int64_t ld
                         const float* mean, const float* rstd, const float* weight, void* dX, int64_t ld_dx,
                         float* dweight, float* dbias, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* Low-rank adapters of many requests beside a layer.  Row t of a batch belongs to adapter which[t], or to none:
+ *   Y[t] = act(W^ x^_t + bias + residual + s_a B_a (A_a x_t)),  a = which[t]
+ * with x_t as it is handed in (values as they are, codes as the values that they stand for), A_a [R][I] and B_a [O][R] held as bf16.  All is
+ * summed in fp32 and rounded once; A_a x_t enters the second product with 16 bits.
+ * A set holds N adapters (up to 1024) of rank up to R (up to 128) for layers of I inputs and O outputs, in both directions, ranks padded to
+ * Rp = 16, 32, 64 or 128. */
+typedef struct {
+  int32_t N, R, I, O;
+  uint16_t* a;    /* device [N][Rp][128 ceil(I/128)], 16-byte aligned: as many elements an adapter as bsp_f8_adapters_size says for a */
+  uint16_t* a_t;  /* device, as many, transposed */
+  uint16_t* b;    /* device [N][128 ceil(O/128)][Rp]: as it says for b */
+  uint16_t* b_t;  /* device, as many, transposed */
+  float* scale;   /* device [N] */
+} bsp_f8_adapters;
+int bsp_f8_adapters_size(int32_t R, int32_t I, int32_t O, int64_t* a_elements, int64_t* b_elements);
+
+/* Fill slot `slot` from A [rank][I] and B [O][rank] (device, dtype BSP_F32 or BSP_BF16, rows lda, ldb elements apart), rank <= R, rounded to
+ * bf16; rank 0 makes it an adapter that adds nothing.  Every slot is filled before rows may belong to it.  Asynchronous.
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, HIP. */
+int bsp_f8_adapters_set(const bsp_f8_adapters* d, int32_t slot, int32_t rank, const void* A, int64_t lda, const void* B, int64_t ldb, int32_t dtype,
+                        float scale, void* stream);
+
+/* The rows of a batch by their adapters: made once for a batch, read by every layer's calls. */
+typedef struct {
+  int32_t T, N;
+  int32_t* plan;  /* device, 16-byte aligned, bsp_f8_requests_size bytes */
+} bsp_f8_requests;
+int bsp_f8_requests_size(int32_t T, int32_t N, int64_t* bytes);
+/* which: device [T], which_bytes 4 (int32) or 8 (int64); anything but 0 .. N - 1 is a row without an adapter.  Asynchronous.
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, HIP. */
+int bsp_f8_requests_plan(const bsp_f8_requests* r, const void* which, int32_t which_bytes, void* stream);
+
+/* bsp_f8_fc (X: codes) or bsp_f8_fc_values (X null: values of x_dtype) with adapters; transposed, the gradient of the layer's input, in which
+ * a row gets s_a A_a^t (B_a^t x_t).  T, N, I and O have to agree.  workspace: bsp_f8_fc_adapted_workspace bytes (coded: 0 for values, 1 for
+ * codes, and for values that become codes inside the product's kernel).  Errors: as these. */
+int bsp_f8_fc_adapted_workspace(const bsp_weights_f8* w, int32_t transposed, int32_t T, int32_t coded, const bsp_f8_adapters* adapters, int64_t* bytes);
+int bsp_f8_fc_adapted(const bsp_weights_f8* w, int32_t transposed, const bsp_codes* X, const void* values, int32_t x_dtype, int64_t ldx, int32_t T,
+                      int32_t code, const bsp_f8_adapters* adapters, const bsp_f8_requests* requests, const float* bias, const void* residual,
+                      int32_t relu, const bsp_codes* gate, void* Y, int32_t y_dtype, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* The adapters' gradients, from that of Y (device bf16 [T][O], rows ldy apart) and the layer's input (codes, or X null: bf16 values):
+ *   dA [N][R][I], dB [N][O][R]  device float: sums over the rows of each adapter; zeros for one without rows
+ * fp32 sums in an order that depends on the sizes and on `which` alone.  workspace: bsp_f8_adapters_grad_workspace bytes, 16-byte aligned.
+ * Asynchronous.  Errors: NULL, SHAPE, DTYPE, ALIGN, CAPACITY, HIP.  T = 0 gives zeros. */
+int bsp_f8_adapters_grad_workspace(const bsp_f8_adapters* adapters, int32_t T, int64_t* bytes);
+int bsp_f8_adapters_grad(const bsp_f8_adapters* adapters, const void* dY, int64_t ldy, const bsp_codes* X, const void* values, int64_t ldx, int32_t T,
+                         const bsp_f8_requests* requests, float* dA, float* dB, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Root-mean-square norm over the last axis, the residual stream's addition in the same pass:
  *   H = X + residual, rounded to their type;  Y = H rstd weight, rstd = 1 / sqrt(mean H^2 + eps)
  *   X, residual  device [T][D], dtype BSP_F32 or BSP_BF16, rows ldx, ldr elements apart; residual may be null, then H is X itself
@@ -558,12 +606,15 @@ int bsp_log_probs_grad(const void* X, int64_t ldx, int32_t dtype, int32_t T, int
  *   BSP_F8_CALL_NORM       X, dtype, ldx, T, D, weight, bias, eps, Y, ldy, codes, mean, rstd, stream        18
  *   BSP_F8_CALL_NORM_GRAD  the seventeen of bsp_layer_norm_grad                                             17
  *   BSP_F8_CALL_RMS_NORM   X, ldx, residual, ldr, dtype, T, D, weight, eps, H, ldh, Y, ldy, codes, rstd, stream   20
+ *   BSP_F8_CALL_ADAPTED    the nineteen of bsp_f8_fc_adapted                                               27
+ *   BSP_F8_CALL_ADAPTERS_GRAD  the thirteen of bsp_f8_adapters_grad                                         17
  *   BSP_F8_CALL_RMS_NORM_GRAD, BSP_F8_CALL_LOG_PROBS, BSP_F8_CALL_LOG_PROBS_GRAD: the arguments of the call    17, 17, 15
  * Errors: NULL (words), SHAPE (unknown call), otherwise those of the call. */
 enum bsp_f8_call {
   BSP_F8_CALL_SAVE = 0, BSP_F8_CALL_LOAD = 1, BSP_F8_CALL_FC = 2, BSP_F8_CALL_VALUES = 3, BSP_F8_CALL_GRAD = 4,
   BSP_F8_CALL_NORM = 5, BSP_F8_CALL_NORM_GRAD = 6, BSP_F8_CALL_RMS_NORM = 16, BSP_F8_CALL_RMS_NORM_GRAD = 17,
-  BSP_F8_CALL_LOG_PROBS = 18, BSP_F8_CALL_LOG_PROBS_GRAD = 19
+  BSP_F8_CALL_LOG_PROBS = 18, BSP_F8_CALL_LOG_PROBS_GRAD = 19, BSP_F8_CALL_ADAPTED = 20,
+  BSP_F8_CALL_ADAPTERS_GRAD = 21
 };
 int bsp_f8_call_packed(int32_t call, const int64_t* words);
 

@@ -63,3 +63,27 @@ def log_probs_grad(x, tokens, dlogp=None, dentropy=None, scale=1.0):
         g = dl[:, None] * (one - p) - dh[:, None] * np.where(p == 0, 0.0, p * (lp + h[:, None]))
     g = np.where(none[:, None], 0.0, scale * g)
     return np.where((tokens >= V)[:, None] & ~none[:, None], np.nan, g)
+
+
+def low_rank(x, A, B, scale, which):
+    """(u, what each row's adapter adds): scale A x and B u; nothing where there is no adapter."""
+    x = np.asarray(x, np.float64)
+    u = np.zeros((x.shape[0], A.shape[1]))
+    y = np.zeros((x.shape[0], B.shape[1]))
+    for n in range(A.shape[0]):
+        rows = np.flatnonzero(np.asarray(which) == n)
+        u[rows] = float(scale[n]) * (x[rows] @ np.asarray(A[n], np.float64).T)
+        y[rows] = u[rows] @ np.asarray(B[n], np.float64).T
+    return u, y
+
+
+def low_rank_grad(dy, x, A, B, scale, which):
+    """(dA, dB)."""
+    dy, x = np.asarray(dy, np.float64), np.asarray(x, np.float64)
+    u, _ = low_rank(x, A, B, scale, which)
+    v, _ = low_rank(dy, np.swapaxes(B, 1, 2), np.swapaxes(A, 1, 2), scale, which)
+    dA, dB = np.zeros(A.shape), np.zeros(B.shape)
+    for n in range(A.shape[0]):
+        rows = np.flatnonzero(np.asarray(which) == n)
+        dA[n], dB[n] = v[rows].T @ x[rows], dy[rows].T @ u[rows]
+    return dA, dB

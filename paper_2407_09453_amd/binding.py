@@ -38,7 +38,9 @@ EXPORTS = ("bsp_strerror", "bsp_version", "bsp_pack_count", "bsp_pack", "bsp_unp
            "bsp_f8_save", "bsp_f8_load", "bsp_f8_count", "bsp_f8_index", "bsp_f8_pack", "bsp_f8_fc", "bsp_f8_fc_workspace",
            "bsp_f8_fc_values", "bsp_f8_fc_grad_workspace", "bsp_f8_fc_grad", "bsp_layer_norm", "bsp_layer_norm_grad_workspace",
            "bsp_layer_norm_grad", "bsp_f8_call_packed", "bsp_rms_norm", "bsp_rms_norm_grad_workspace", "bsp_rms_norm_grad",
-           "bsp_log_probs_workspace", "bsp_log_probs", "bsp_log_probs_grad")
+           "bsp_log_probs_workspace", "bsp_log_probs", "bsp_log_probs_grad", "bsp_f8_adapters_size", "bsp_f8_adapters_set",
+           "bsp_f8_requests_size", "bsp_f8_requests_plan", "bsp_f8_fc_adapted_workspace", "bsp_f8_fc_adapted",
+           "bsp_f8_adapters_grad_workspace", "bsp_f8_adapters_grad")
 
 
 class BspError(RuntimeError):
@@ -78,6 +80,15 @@ class bsp_weights_f8(ctypes.Structure):
 
 def lib_path() -> str:
     return _LIB_PATH
+
+
+class bsp_f8_adapters(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("R", ctypes.c_int32), ("I", ctypes.c_int32), ("O", ctypes.c_int32),
+                ("a", ctypes.c_void_p), ("a_t", ctypes.c_void_p), ("b", ctypes.c_void_p), ("b_t", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+
+
+class bsp_f8_requests(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("N", ctypes.c_int32), ("plan", ctypes.c_void_p)]
 
 
 def load_library():
@@ -153,6 +164,7 @@ def load_library():
     lib.bsp_fc_i8.restype = ctypes.c_int
     lib.bsp_fc_i8.argtypes = [wp, vp, vp, vp, i32, i32, i32, vp]
     cp, fp, pi64 = ctypes.POINTER(bsp_codes), ctypes.POINTER(bsp_weights_f8), ctypes.POINTER(i64)
+    ap, rp = ctypes.POINTER(bsp_f8_adapters), ctypes.POINTER(bsp_f8_requests)
     for name, args in (("bsp_f8_save", [vp, i32, i64, cp, vp]), ("bsp_f8_load", [cp, vp, i32, i64, vp]),
                        ("bsp_f8_count", [vp, i32, i32, pi64]), ("bsp_f8_index", [vp, i32, i32, i64, vp, vp, vp, vp]),
                        ("bsp_f8_pack", [fp, vp, i32, i64, vp]), ("bsp_f8_fc", [fp, i32, cp, vp, vp, i32, cp, vp, i32, vp, i64, vp]),
@@ -163,6 +175,13 @@ def load_library():
                        ("bsp_layer_norm", [vp, i32, i64, i32, i32, vp, vp, ctypes.c_float, vp, i64, cp, vp, vp, vp]),
                        ("bsp_layer_norm_grad_workspace", [i32, i32, pi64]),
                        ("bsp_layer_norm_grad", [vp, i64, vp, i64, i32, i32, i32, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp]),
+                       ("bsp_f8_adapters_size", [i32, i32, i32, pi64, pi64]),
+                       ("bsp_f8_adapters_set", [ap, i32, i32, vp, i64, vp, i64, i32, ctypes.c_float, vp]),
+                       ("bsp_f8_requests_size", [i32, i32, pi64]), ("bsp_f8_requests_plan", [rp, vp, i32, vp]),
+                       ("bsp_f8_fc_adapted_workspace", [fp, i32, i32, i32, ap, pi64]),
+                       ("bsp_f8_fc_adapted", [fp, i32, cp, vp, i32, i64, i32, i32, ap, rp, vp, vp, i32, cp, vp, i32, vp, i64, vp]),
+                       ("bsp_f8_adapters_grad_workspace", [ap, i32, pi64]),
+                       ("bsp_f8_adapters_grad", [ap, vp, i64, cp, vp, i64, i32, rp, vp, vp, vp, i64, vp]),
                        ("bsp_rms_norm", [vp, i64, vp, i64, i32, i32, i32, vp, ctypes.c_float, vp, i64, vp, i64, cp, vp, vp]),
                        ("bsp_rms_norm_grad_workspace", [i32, i32, pi64]),
                        ("bsp_rms_norm_grad", [vp, i64, vp, i64, vp, i64, i32, i32, i32, vp, vp, vp, i64, vp, vp, i64, vp]),

@@ -1,0 +1,525 @@
+// Low-rank adapters of many requests beside an 8-bit layer: y_t += s_a B_a (A_a x_t) for the adapter a of row t, and their gradients.
+//
+//   down:  u_t = s_a A_a x_t                     here, on rows sorted by adapter, sixteen of one adapter to a workgroup
+//   up:    y_t += B_a u_t                        in the products' own kernels, before their epilogue: one rounding for the whole result
+//   grad:  dB_a = sum_t dy_t u_t^t, dA_a = sum_t v_t x_t^t with v_t = s_a B_a^t dy_t (down, transposed)
+//
+// A and B are held as bf16, in both directions, ranks padded to 16, 32, 64 or 128 with zeros; products are summed in fp32.  u and v are fp32, and
+// where they enter a matrix instruction again they do so as two bf16 parts, which keep 16 bits of them.  Rows enter as they were given:
+// bf16 values and codes are exact in bf16, fp32 values go as two parts too.
+// `down` is bound by the bytes of the rows on many rows, by latency on few.  `grad` reads each block of 128 columns of the rows of an adapter
+// once: both operands are summed over rows, so they lie in LDS as in memory and the transposing read hands a lane a column's
+// rows.  An adapter with many rows is cut into chunks whose sums a second launch joins, in order: no atomics.
+#include "bsp_norm.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+
+inline int launched() { return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP; }
+
+// ------------------------------------------------------------------ which rows are whose
+// Rows sorted by adapter, in their order within each (counted, not compared: one workgroup of sixteen waves, each with a range of the rows).
+// Ids that are no adapter's become -1 and have no place in the order.
+template <class Id>
+__global__ __launch_bounds__(1024) void adapt_plan(const Id* ids, int T, int N, F8Requests q) {
+  extern __shared__ int32_t hist[];  // [16][N], behind them the tiles' first numbers [N + 1]
+  __shared__ int32_t sh[2][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int32_t* first_tile = hist + 16 * N;
+  for (int i = tid; i < 16 * N; i += 1024) hist[i] = 0;
+  __syncthreads();
+  const int64_t per = ((int64_t)T + 1023) / 1024 * 64, begin = wave * per, end = begin + per < T ? begin + per : T;
+  for (int64_t t = begin + lane; t < end; t += 64) {
+    const Id id = ids[t];
+    const int32_t a = id >= 0 && id < N ? (int32_t)id : -1;
+    q.which[t] = a;
+    if (a >= 0) atomicAdd(&hist[wave * N + a], 1);  // (a count: the same in any order)
+  }
+  __syncthreads();
+  // N <= 1024: an adapter a thread
+  int total = 0;
+  if (tid < N)
+    for (int w = 0; w < 16; ++w) {
+      const int n = hist[w * N + tid];
+      hist[w * N + tid] = total;
+      total += n;
+    }
+  int rows = total, tiles = (total + 15) >> 4;  // sums up to and with this thread's
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int r = __shfl_up(rows, d), s = __shfl_up(tiles, d);
+    if (lane >= d) rows += r, tiles += s;
+  }
+  if (lane == 63) sh[0][wave] = rows, sh[1][wave] = tiles;
+  __syncthreads();
+  int all_tiles = 0;
+  for (int w = 0; w < 16; ++w) {
+    if (w < wave) rows += sh[0][w], tiles += sh[1][w];
+    all_tiles += sh[1][w];
+  }
+  if (tid < N) {
+    const int start = rows - total;
+    for (int w = 0; w < 16; ++w) hist[w * N + tid] += start;
+    q.start[tid] = start;
+    first_tile[tid] = tiles - ((total + 15) >> 4);
+    if (tid == N - 1) q.start[N] = rows, first_tile[N] = tiles;
+  }
+  if (tid == 0) q.tiles[0] = all_tiles;
+  __syncthreads();
+  for (int i = tid; i < all_tiles; i += 1024) {  // the last adapter whose first tile is at most i and that has one
+    int lo = 0, hi = N;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first_tile[mid] <= i) lo = mid;
+      else hi = mid;
+    }
+    q.tiles[1 + 2 * i] = lo;
+    q.tiles[2 + 2 * i] = (i - first_tile[lo]) * 16;  // its first row's place among the adapter's
+  }
+  for (int64_t t0 = begin; t0 < end; t0 += 64) {
+    const int64_t t = t0 + lane;
+    const int a = t < end ? q.which[t] : -1;
+    uint64_t todo = __ballot(a >= 0);
+    while (todo) {
+      const int of = __builtin_amdgcn_readlane(a, __builtin_ctzll(todo));
+      const uint64_t same = __ballot(a == of);
+      const int place = hist[wave * N + of];
+      if (a == of) q.order[place + __popcll(same & ((1ull << lane) - 1))] = (int32_t)t;
+      __builtin_amdgcn_wave_barrier();
+      if (lane == 0) hist[wave * N + of] = place + __popcll(same);
+      __builtin_amdgcn_wave_barrier();
+      todo &= ~same;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ an adapter's weights
+// A thread takes one rank of one padded column: m [padded columns][Rp] and its transpose.  COLUMNS: W is [columns][rank], else [rank][columns].
+template <bool F32, bool COLUMNS>
+__device__ __forceinline__ void set_side(const void* W, int64_t ld, int rank, int columns, int padded, int Rp, uint16_t* by_column, uint16_t* by_rank, int64_t i) {
+  const int c = (int)(i / Rp), r = (int)(i - (int64_t)c * Rp);
+  uint16_t v = 0;
+  if (r < rank && c < columns) {
+    const int64_t at = COLUMNS ? c * ld + r : r * ld + c;
+    v = F32 ? f32_to_bf16_rne(((const float*)W)[at]) : ((const uint16_t*)W)[at];
+  }
+  by_column[i] = v;
+  by_rank[(int64_t)r * padded + c] = v;
+}
+template <bool F32>
+__global__ __launch_bounds__(256) void adapt_set(F8Adapters d, int slot, int rank, const void* A, int64_t lda, const void* B, int64_t ldb, float scale) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, na = (int64_t)d.Ip * d.Rp, nb = (int64_t)d.Op * d.Rp;
+  if (i < na) set_side<F32, false>(A, lda, rank, d.I, d.Ip, d.Rp, d.a_t + slot * na, d.a + slot * na, i);
+  else if (i < na + nb) set_side<F32, true>(B, ldb, rank, d.O, d.Op, d.Rp, d.b + slot * nb, d.b_t + slot * nb, i - na);
+  if (i == 0) d.scale[slot] = scale;
+}
+
+// ------------------------------------------------------------------ down
+enum { kBf16, kF32, kE4, kE5 };  // what the rows are given as
+
+struct DownArgs {
+  const void* X;
+  const uint8_t* scale;  // of codes
+  int64_t ld, srows;
+  const uint16_t* down;  // [N][Rp][Kp]
+  const float* factor;   // [N]
+  float* u;              // [T][Rp]
+  F8Requests q;
+  int32_t K, Kp;
+};
+
+__device__ __forceinline__ u32x4_t pack8(const float* v) {
+  return u32x4_t{f8_pack_bf16x2(v[0], v[1]), f8_pack_bf16x2(v[2], v[3]), f8_pack_bf16x2(v[4], v[5]), f8_pack_bf16x2(v[6], v[7])};
+}
+// what eight values lose as bf16, itself as bf16
+__device__ __forceinline__ u32x4_t rest8(const float* v, u32x4_t high) {
+  float r[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    r[2 * k] = v[2 * k] - __uint_as_float(high[k] << 16);
+    r[2 * k + 1] = v[2 * k + 1] - __uint_as_float(high[k] & 0xFFFF0000u);
+  }
+  return pack8(r);
+}
+
+// A workgroup takes sixteen rows of one adapter, its waves share out the blocks of 128 columns.  In a block a lane reads columns
+// 64 q + 16 g + 8 h + 0..7 of its row and of its rank: 16 bytes of a row of codes at a time.  The ranks are the matrix instruction's rows and
+// the rows its columns, so nothing of one row, NaN among it, reaches another's sums.
+template <int SRC, int NR>
+__global__ __launch_bounds__(1024) void adapt_down(DownArgs a) {
+  extern __shared__ float sums[];  // [waves][NR][64][4]
+  constexpr bool kCoded = SRC == kE4 || SRC == kE5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const int r = lane & 15, g = lane >> 4;
+  if ((int)blockIdx.x >= a.q.tiles[0]) return;
+  const int of = a.q.tiles[1 + 2 * blockIdx.x], from = a.q.tiles[2 + 2 * blockIdx.x];
+  const int begin = a.q.start[of] + from, left = a.q.start[of + 1] - begin;  // rows from this tile's first on
+  const int64_t t = a.q.order[begin + (r < left ? r : left - 1)];
+  const uint16_t* w = a.down + ((int64_t)of * 16 * NR + r) * a.Kp + 16 * g;
+  const void* x = kCoded ? (const void*)((const uint8_t*)a.X + t * a.ld) : row_of<SRC == kF32>(a.X, t, a.ld);
+  const int nb = a.Kp >> 7;
+  f32x4_t acc[NR] = {};
+  for (int kb = wave; kb < nb; kb += waves) {
+    u32x4_t wv[NR][4], xv[4], xl[SRC == kF32 ? 4 : 1];
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) wv[n][j] = *(const u32x4_t*)(w + (int64_t)n * 16 * a.Kp + kb * 128 + (j >> 1) * 64 + (j & 1) * 8);
+    if constexpr (kCoded) {
+      const float s = __uint_as_float((uint32_t)a.scale[kb * a.srows + t] << 23);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const u32x4_t c = *(const u32x4_t*)((const uint8_t*)x + kb * 128 + q * 64 + g * 16);
+        xv[2 * q] = f8_decode_bf16x8<SRC == kE5>(c.x, c.y, s);
+        xv[2 * q + 1] = f8_decode_bf16x8<SRC == kE5>(c.z, c.w, s);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int c = kb * 128 + (j >> 1) * 64 + 16 * g + (j & 1) * 8;
+        if constexpr (SRC == kBf16) {
+          if (kb * 128 + 128 <= a.K) {
+            xv[j] = *(const f8_any2_t*)((const uint16_t*)x + c);
+          } else {
+            float v[8];
+            load8<false>(x, c, a.K, v);
+            xv[j] = pack8(v);
+          }
+        } else {
+          float v[8];
+          load8<true>(x, c, a.K, v);
+          xv[j] = pack8(v);
+          xl[j] = rest8(v, xv[j]);
+        }
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        acc[n] = mfma_bf16_16x16x32(wv[n][j], xv[j], acc[n]);
+        if constexpr (SRC == kF32) acc[n] = mfma_bf16_16x16x32(wv[n][j], xl[j], acc[n]);
+      }
+  }
+#pragma unroll
+  for (int n = 0; n < NR; ++n) *(f32x4_t*)(sums + ((wave * NR + n) * 64 + lane) * 4) = acc[n];
+  __syncthreads();
+  for (int i = threadIdx.x; i < NR * 64; i += blockDim.x) {
+    f32x4_t s = *(const f32x4_t*)(sums + i * 4);
+    for (int v = 1; v < waves; ++v) s += *(const f32x4_t*)(sums + (v * NR * 64 + i) * 4);
+    const int row = i & 15;
+    if (row < left) *(f32x4_t*)(a.u + (int64_t)a.q.order[begin + row] * (16 * NR) + (i >> 6) * 16 + ((i >> 4) & 3) * 4) = s * a.factor[of];
+  }
+}
+
+template <int SRC, int NR>
+int down_launch(const DownArgs& a, int T, int N, hipStream_t st) {
+  const int64_t tiles = f8_request_tiles(T, N);
+  const int nb = a.Kp >> 7;
+  constexpr int most = NR > 4 ? 8 : 16;
+  // a wave a block of columns, as many as a workgroup holds where there are few workgroups
+  int waves = tiles >= 512 ? 4 : most;
+  while (waves > 1 && waves > nb) waves >>= 1;
+  if (tiles > INT32_MAX / 2048) return BSP_ERR_SHAPE;
+  static const bool raised = hipFuncSetAttribute((const void*)&adapt_down<SRC, NR>, hipFuncAttributeMaxDynamicSharedMemorySize, most * NR * 1024) == hipSuccess;
+  if (!raised) return BSP_ERR_HIP;
+  hipLaunchKernelGGL((adapt_down<SRC, NR>), dim3((unsigned)tiles), dim3(64 * waves), (size_t)waves * NR * 1024, st, a);
+  return launched();
+}
+template <int SRC>
+int down_rank(const DownArgs& a, int T, int N, int Rp, hipStream_t st) {
+  switch (Rp) {
+    case 16: return down_launch<SRC, 1>(a, T, N, st);
+    case 32: return down_launch<SRC, 2>(a, T, N, st);
+    case 64: return down_launch<SRC, 4>(a, T, N, st);
+    default: return down_launch<SRC, 8>(a, T, N, st);
+  }
+}
+
+// ------------------------------------------------------------------ gradients
+constexpr int kStep = 32;  // rows a step
+
+struct GradArgs {
+  F8Requests q;
+  const uint16_t* dY;     // bf16 [T][O]
+  const void* X;          // bf16 [T][I], or codes
+  const uint8_t* scale;
+  int64_t ldy, ldx, srows;
+  const float *u, *v;     // [T][Rp]
+  float *dA, *dB;         // [N][R][I], [N][O][R]
+  float* part;            // [slots][R I + O R]
+  int32_t N, R, I, O, blocks_o, chunk;
+  int32_t src;            // of X
+};
+
+// Which adapter's rows chunk number k holds, and where its sums go.  The same in all lanes.
+struct Chunk {
+  int of, begin, rows;  // adapter (N: none), first row's place in the order, how many
+  int slot;             // of the partial sums, -1: the adapter has no other chunk
+};
+__device__ __forceinline__ int wave_scan(int v, int lane) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int o = __shfl_up(v, d);
+    if (lane >= d) v += o;
+  }
+  return v;
+}
+__device__ __forceinline__ Chunk find_chunk(const F8Requests& q, int N, int length, int k) {
+  const int lane = threadIdx.x & 63;
+  int chunks = 0, slots = 0;  // of the adapters before
+  for (int a0 = 0; a0 < N; a0 += 64) {
+    const int a = a0 + lane, start = a < N ? q.start[a] : 0, n = a < N ? q.start[a + 1] - start : 0;
+    const int mine = (n + length - 1) / length, kept = mine > 1 ? mine : 0;
+    const int upto = chunks + wave_scan(mine, lane), slot_upto = slots + wave_scan(kept, lane);
+    const uint64_t found = __ballot(k >= upto - mine && k < upto);
+    if (found) {
+      const int l = __builtin_ctzll(found);
+      const int s = __builtin_amdgcn_readlane(start, l), c = __builtin_amdgcn_readlane(n, l), j = k - __builtin_amdgcn_readlane(upto - mine, l);
+      return Chunk{a0 + l, s + j * length, c - j * length < length ? c - j * length : length,
+                   __builtin_amdgcn_readlane(kept, l) ? __builtin_amdgcn_readlane(slot_upto - kept, l) + j : -1};
+    }
+    chunks = __builtin_amdgcn_readlane(upto, 63), slots = __builtin_amdgcn_readlane(slot_upto, 63);
+  }
+  return Chunk{N, 0, 0, -1};
+}
+
+template <int BYTES>
+__device__ __forceinline__ u32x4_t read_columns(const uint8_t* p) {  // rows +0..3 and +4..7 of this lane's column, rows BYTES apart
+  auto* q = (__attribute__((address_space(3))) s16x4_t*)(uintptr_t)p;
+  const u32x2_t a = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(q));
+  const u32x2_t b = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(q + 4 * BYTES / 8));
+  return u32x4_t{a.x, a.y, b.x, b.y};
+}
+__device__ __forceinline__ f32x16_t mfma32(u32x4_t a, u32x4_t b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+// A workgroup: 128 columns of dY (dB) or of X (dA), and a chunk of an adapter's rows.  Four waves of 32 columns each; the other operand is u or v,
+// its high parts beside its low parts in a row of 2 RP bf16.
+template <int RP>
+__global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
+  constexpr int NT = RP / 16;               // tiles of 32 columns of u: high parts, then low
+  constexpr int kQ = 4 * RP + 16;           // bytes from row to row of u in LDS
+  constexpr int kP = kStep * 256, kBuffer = kP + kStep * kQ, kMine = RP / 8;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kBuffer];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Chunk k = find_chunk(a.q, a.N, a.chunk, blockIdx.y);
+  if (k.of >= a.N) return;
+  const bool in_y = (int)blockIdx.x < a.blocks_o;
+  const int kb = in_y ? blockIdx.x : blockIdx.x - a.blocks_o, columns = in_y ? a.O : a.I, c0 = kb * 128;
+  const int src = in_y ? (int)kBf16 : a.src;
+  const void* P = in_y ? (const void*)a.dY : a.X;
+  const int64_t ld = in_y ? a.ldy : a.ldx;
+  const float* Q = in_y ? a.u : a.v;
+  const bool whole = c0 + 128 <= columns;
+  // what this thread brings: sixteen columns of a row, and kMine values of u
+  const int row = tid >> 3, piece = tid & 7;
+  u32x4_t p[2];
+  float u[kMine];
+  int s = 0;
+  auto place = [&](int i) { return a.q.order[k.begin + (i * kStep + row < k.rows ? i * kStep + row : k.rows - 1)]; };
+  auto ask = [&](int64_t t) {
+    const int c = c0 + piece * 16;
+    if (src == kBf16) {
+      if (whole) {
+        const uint16_t* x = (const uint16_t*)P + t * ld + c;
+        p[0] = *(const f8_any2_t*)x;
+        p[1] = *(const f8_any2_t*)(x + 8);
+      } else {
+        float v[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          load8<false>((const uint16_t*)P + t * ld, c + 8 * h, columns, v);
+          p[h] = pack8(v);
+        }
+      }
+    } else {
+      p[0] = *(const u32x4_t*)((const uint8_t*)P + t * ld + c);
+      s = a.scale[kb * a.srows + t];
+    }
+#pragma unroll
+    for (int e = 0; e < kMine; ++e) u[e] = Q[t * RP + piece * kMine + e];
+  };
+  auto write = [&](int buf, int i) {
+    const bool in = i * kStep + row < k.rows;  // rows past the chunk add nothing, whatever they hold
+    uint8_t* to = lds + buf * kBuffer;
+    u32x4_t w[2] = {p[0], p[1]};
+    if (src != kBf16) {
+      const float f = __uint_as_float((uint32_t)s << 23);
+      const u32x4_t c = p[0];
+      w[0] = src == kE5 ? f8_decode_bf16x8<true>(c.x, c.y, f) : f8_decode_bf16x8<false>(c.x, c.y, f);
+      w[1] = src == kE5 ? f8_decode_bf16x8<true>(c.z, c.w, f) : f8_decode_bf16x8<false>(c.z, c.w, f);
+    }
+    const int key = (row & 3) << 1 | ((row >> 3) & 1);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) *(u32x4_t*)(to + row * 256 + ((piece ^ key) << 5) + 16 * h) = in ? w[h] : u32x4_t{0, 0, 0, 0};
+    uint16_t* hi = (uint16_t*)(to + kP + row * kQ) + piece * kMine;
+#pragma unroll
+    for (int e = 0; e < kMine; e += 2) {
+      const float x0 = in ? u[e] : 0.f, x1 = in ? u[e + 1] : 0.f;
+      const uint32_t h = f8_pack_bf16x2(x0, x1);
+      *(uint32_t*)(hi + e) = h;
+      *(uint32_t*)(hi + RP + e) = f8_pack_bf16x2(x0 - __uint_as_float(h << 16), x1 - __uint_as_float(h & 0xFFFF0000u));
+    }
+  };
+  const int half = lane >> 5, trow = half * 8 + ((lane & 15) >> 2), key_r = ((lane & 15) >> 2) << 1 | half;
+  const int at_p = trow * 256 + (((wave * 2 + ((lane >> 4) & 1)) ^ key_r) << 5) + (lane & 3) * 8;
+  const int at_q = kP + trow * kQ + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+  f32x16_t acc[NT] = {};
+  const int steps = (k.rows + kStep - 1) / kStep;
+  int next = place(0);
+  ask(next);
+  next = place(1 < steps ? 1 : 0);
+  write(0, 0);
+  if (steps > 1) ask(next);
+  next = place(2 < steps ? 2 : steps - 1);
+  __syncthreads();
+  for (int i = 0; i < steps; ++i) {
+    const uint8_t* from = lds + (i & 1) * kBuffer;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const u32x4_t x = read_columns<256>(from + h * 16 * 256 + at_p);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) acc[n] = mfma32(x, read_columns<kQ>(from + h * 16 * kQ + at_q + n * 64), acc[n]);
+    }
+    if (i + 1 < steps) {
+      write((i + 1) & 1, i + 1);
+      if (i + 2 < steps) ask(next);
+      next = place(i + 3 < steps ? i + 3 : steps - 1);
+    }
+    __syncthreads();
+  }
+  // high and low parts together
+  constexpr int kTiles = RP == 16 ? 1 : NT / 2;
+  if constexpr (RP == 16) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[0][e] += __shfl_xor(acc[0][e], 16);
+  } else {
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) acc[n] += acc[n + kTiles];
+  }
+  const int64_t na = (int64_t)a.R * a.I, nb = (int64_t)a.O * a.R;
+  float* to_a = k.slot < 0 ? a.dA + k.of * na : a.part + k.slot * (na + nb);
+  float* to_b = k.slot < 0 ? a.dB + k.of * nb : to_a + na;
+#pragma unroll
+  for (int n = 0; n < kTiles; ++n) {
+    const int r = n * 32 + (lane & 31);
+    if (r >= a.R || (RP == 16 && (lane & 16))) continue;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int c = c0 + wave * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
+      if (c >= columns) continue;
+      if (in_y) to_b[(int64_t)c * a.R + r] = acc[n][e];
+      else to_a[(int64_t)r * a.I + c] = acc[n][e];
+    }
+  }
+}
+
+// Adapters of several chunks: their sums in order; of none: zeros.
+__global__ __launch_bounds__(256) void adapt_join(GradArgs a) {
+  const int lane = threadIdx.x & 63, of = blockIdx.y;
+  const int n = a.q.start[of + 1] - a.q.start[of], chunks = (n + a.chunk - 1) / a.chunk;
+  if (chunks == 1) return;
+  int slot = 0;
+  for (int a0 = 0; a0 < of; a0 += 64) {
+    const int b = a0 + lane, m = b < of ? (a.q.start[b + 1] - a.q.start[b] + a.chunk - 1) / a.chunk : 0;
+    slot += __builtin_amdgcn_readlane(wave_scan(m > 1 ? m : 0, lane), 63);
+  }
+  const int64_t na = (int64_t)a.R * a.I, nb = (int64_t)a.O * a.R;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < na + nb; i += (int64_t)gridDim.x * 256) {
+    float s = 0.f;
+    for (int k = 0; k < chunks; ++k) s += a.part[(slot + k) * (na + nb) + i];
+    if (i < na) a.dA[of * na + i] = s;
+    else a.dB[of * nb + i - na] = s;
+  }
+}
+
+// Rows of a chunk: such that there are about four workgroups a CU.
+int chunk_of(int T, int I, int O) {
+  const int64_t blocks = f8_blocks(I) + f8_blocks(O);
+  const int64_t rows = ((int64_t)T * blocks / 1024 + kStep - 1) / kStep * kStep;
+  return rows < 128 ? 128 : (int)(rows < INT32_MAX / 2 ? rows : INT32_MAX / 2 / kStep * kStep);
+}
+
+}  // namespace
+
+int64_t f8_request_tiles(int T, int N) { return (int64_t)T / 16 + (T < N ? T : N); }
+
+F8Requests f8_requests_of(const bsp_f8_requests* r) {
+  int32_t* p = r->plan;
+  F8Requests q{};
+  q.start = p, p += (r->N + 1 + 3) & ~3;
+  q.which = p, p += ((int64_t)r->T + 3) & ~(int64_t)3;
+  q.order = p, p += ((int64_t)r->T + 3) & ~(int64_t)3;
+  q.tiles = p;
+  return q;
+}
+int64_t f8_requests_bytes(int T, int N) {
+  return 4 * (((N + 1 + 3) & ~3) + 2 * (((int64_t)T + 3) & ~(int64_t)3) + 1 + 2 * f8_request_tiles(T, N));
+}
+int f8_launch_plan(const bsp_f8_requests* r, const void* which, bool wide, hipStream_t st) {
+  const F8Requests q = f8_requests_of(r);
+  const size_t lds = (size_t)(17 * r->N + 1) * 4;
+  auto run = [&](auto kernel, auto* ids) {
+    static const bool raised = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (17 * 1024 + 1) * 4) == hipSuccess;
+    if (!raised) return (int)BSP_ERR_HIP;
+    hipLaunchKernelGGL(kernel, dim3(1), dim3(1024), lds, st, ids, r->T, r->N, q);
+    return launched();
+  };
+  return wide ? run(adapt_plan<int64_t>, (const int64_t*)which) : run(adapt_plan<int32_t>, (const int32_t*)which);
+}
+
+F8Adapters f8_adapters_of(const bsp_f8_adapters* d) {
+  F8Adapters v{};
+  v.N = d->N, v.R = d->R, v.I = d->I, v.O = d->O, v.Rp = d->R <= 16 ? 16 : d->R <= 32 ? 32 : d->R <= 64 ? 64 : 128;
+  v.Ip = f8_blocks(d->I) * F8_BLOCK, v.Op = f8_blocks(d->O) * F8_BLOCK;
+  v.a = d->a, v.a_t = d->a_t, v.b = d->b, v.b_t = d->b_t, v.scale = d->scale;
+  return v;
+}
+int f8_launch_set(const F8Adapters& d, int slot, int rank, const void* A, int64_t lda, const void* B, int64_t ldb, bool f32, float scale, hipStream_t st) {
+  const int64_t groups = ((int64_t)(d.Ip + d.Op) * d.Rp + 255) / 256;
+  if (!f8_fits_x(groups, 256)) return BSP_ERR_SHAPE;
+  if (f32) hipLaunchKernelGGL(adapt_set<true>, dim3((unsigned)groups), dim3(256), 0, st, d, slot, rank, A, lda, B, ldb, scale);
+  else hipLaunchKernelGGL(adapt_set<false>, dim3((unsigned)groups), dim3(256), 0, st, d, slot, rank, A, lda, B, ldb, scale);
+  return launched();
+}
+
+int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, hipStream_t st) {
+  DownArgs a{};
+  a.X = x.X, a.scale = x.scale, a.ld = x.ld, a.srows = f8_scale_rows(T), a.down = transposed ? d.b_t : d.a, a.factor = d.scale, a.u = u, a.q = q;
+  a.K = transposed ? d.O : d.I, a.Kp = transposed ? d.Op : d.Ip;
+  switch (x.dtype) {
+    case BSP_BF16: return down_rank<kBf16>(a, T, d.N, d.Rp, st);
+    case BSP_F32: return down_rank<kF32>(a, T, d.N, d.Rp, st);
+    case BSP_E4M3: return down_rank<kE4>(a, T, d.N, d.Rp, st);
+    default: return down_rank<kE5>(a, T, d.N, d.Rp, st);
+  }
+}
+
+int64_t f8_adapt_part_bytes(const F8Adapters& d, int T) {
+  const int64_t slots = 2 * (int64_t)T / chunk_of(T, d.I, d.O);  // (an adapter of several chunks has fewer than twice its rows' share)
+  return slots * ((int64_t)d.R * (d.I + (int64_t)d.O)) * 4;
+}
+int f8_launch_adapt_grad(const F8Adapters& d, const uint16_t* dY, int64_t ldy, const F8Input& x, int T, const F8Requests& q, const float* u, const float* v,
+                         float* part, float* dA, float* dB, hipStream_t st) {
+  GradArgs a{};
+  a.q = q, a.dY = dY, a.X = x.X, a.scale = x.scale, a.ldy = ldy, a.ldx = x.ld, a.srows = f8_scale_rows(T), a.u = u, a.v = v, a.dA = dA, a.dB = dB, a.part = part;
+  a.N = d.N, a.R = d.R, a.I = d.I, a.O = d.O, a.blocks_o = f8_blocks(d.O), a.chunk = chunk_of(T, d.I, d.O);
+  a.src = x.dtype == BSP_BF16 ? kBf16 : x.dtype == BSP_E4M3 ? kE4 : kE5;
+  const int64_t chunks = (int64_t)T / a.chunk + (T < d.N ? T : d.N);
+  const dim3 grid((unsigned)(a.blocks_o + f8_blocks(d.I)), (unsigned)chunks);
+  if (chunks > 65535 || !f8_fits_x(grid.x, 256)) return BSP_ERR_SHAPE;
+  auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a); };
+  if (T > 0) {  // (without rows the sums below are all there is: zeros)
+    if (d.Rp == 16) run(adapt_grad<16>);
+    else if (d.Rp == 32) run(adapt_grad<32>);
+    else if (d.Rp == 64) run(adapt_grad<64>);
+    else run(adapt_grad<128>);
+  }
+  if (launched() != BSP_OK) return BSP_ERR_HIP;
+  const int64_t groups = ((int64_t)d.R * (d.I + (int64_t)d.O) + 1023) / 1024;
+  hipLaunchKernelGGL(adapt_join, dim3((unsigned)(groups < 4096 ? groups : 4096), (unsigned)d.N), dim3(256), 0, st, a);
+  return launched();
+}

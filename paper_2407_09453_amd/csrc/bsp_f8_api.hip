@@ -11,6 +11,7 @@ inline bool code_type(int d) { return d == BSP_E4M3 || d == BSP_E5M2; }
 inline unsigned size_of(int d) { return d == BSP_F32 ? 4 : 2; }
 constexpr int32_t kMost = INT32_MAX - 65536;  // rows and columns: sizes rounded up stay in 32 bits
 constexpr int32_t kWide = 1 << 24;            // columns of codes: 256 rows' offsets stay in 32 bits
+constexpr int32_t kSlots = 1024, kRank = 128;  // adapters of a set, ranks of one
 constexpr int32_t kVocabulary = 1 << 21;      // logits of a row: 64 chunks of what a workgroup's registers hold
 constexpr int32_t kTop = 64;                  // likeliest tokens: one of 64 groups' largest is below the last of them
 
@@ -85,12 +86,23 @@ int64_t sums_bytes(const F8Rows& rows, int T) {
   return split > 1 ? split * T * ((rows.out + 3) / 4) * 16 : 0;
 }
 
-int multiply(const F8Rows& rows, const F8Input& x, int T, const F8Epilogue& q, int32_t y_dtype, void* sums, hipStream_t st) {
+int multiply(const F8Rows& rows, const F8Input& x, int T, const F8Low& low, const F8Epilogue& q, int32_t y_dtype, void* sums, hipStream_t st) {
   const bool f32 = y_dtype == BSP_F32;
-  const int rc = T <= kFewRows ? f8_launch_few(rows, x, T, q, f32, (float*)sums, st) : f8_launch_tile(rows, x, T, q, f32, (float*)sums, st);
+  const int rc = T <= kFewRows ? f8_launch_few(rows, x, T, low, q, f32, (float*)sums, st) : f8_launch_tile(rows, x, T, low, q, f32, (float*)sums, st);
   if (rc != BSP_OK) return rc;
   const int split = split_of(rows, T, f32);
   return split > 1 ? f8_launch_join((const float*)sums, split, T, rows.out, q, f32, st) : BSP_OK;
+}
+
+// rows given as values: workspace holds `sums` bytes, behind them the codes of rows that do not become codes in the product's kernel
+int multiply_values(const F8Rows& rows, const void* X, int x_dtype, int64_t ldx, int T, int K, bool e5, const F8Low& low, const F8Epilogue& q,
+                    int32_t y_dtype, void* workspace, int64_t sums, hipStream_t st) {
+  if (in_kernel(X, x_dtype, ldx, T, K)) return multiply(rows, F8Input{X, nullptr, x_dtype, e5, ldx}, T, low, q, y_dtype, workspace, st);
+  const int64_t ld = (int64_t)f8_blocks(K) * F8_BLOCK;
+  uint8_t *codes = (uint8_t*)workspace + sums, *scale = codes + T * ld;
+  const int rc = f8_launch_save(X, x_dtype == BSP_F32, ldx, T, K, e5, codes, scale, st);
+  if (rc != BSP_OK) return rc;
+  return multiply(rows, F8Input{codes, scale, e5 ? BSP_E5M2 : BSP_E4M3, e5, ld}, T, low, q, y_dtype, workspace, st);
 }
 
 int check_workspace(const void* workspace, int64_t bytes, int64_t need) {
@@ -98,6 +110,21 @@ int check_workspace(const void* workspace, int64_t bytes, int64_t need) {
   if (need > 0 && !workspace) return BSP_ERR_NULL;
   return aligned(workspace, 16) ? BSP_OK : BSP_ERR_ALIGN;
 }
+
+int check_adapters(const bsp_f8_adapters* d) {
+  if (!d) return BSP_ERR_NULL;
+  if (d->N < 1 || d->N > kSlots || d->R < 1 || d->R > kRank || d->I < 1 || d->I > kWide || d->O < 1 || d->O > kWide) return BSP_ERR_SHAPE;
+  if (!d->a || !d->a_t || !d->b || !d->b_t || !d->scale) return BSP_ERR_NULL;
+  return aligned(d->a, 16) && aligned(d->a_t, 16) && aligned(d->b, 16) && aligned(d->b_t, 16) && aligned(d->scale, 4) ? BSP_OK : BSP_ERR_ALIGN;
+}
+int check_requests(const bsp_f8_requests* r) {
+  if (!r) return BSP_ERR_NULL;
+  if (r->T < 0 || r->T > kMost || r->N < 1 || r->N > kSlots) return BSP_ERR_SHAPE;
+  if (r->T > 0 && !r->plan) return BSP_ERR_NULL;
+  return aligned(r->plan, 16) ? BSP_OK : BSP_ERR_ALIGN;
+}
+int64_t in16(int64_t bytes) { return (bytes + 15) & ~(int64_t)15; }
+int64_t low_bytes(const F8Adapters& d, int T) { return (int64_t)T * d.Rp * 4; }
 
 int64_t codes_bytes(int T, int K) { return ((int64_t)T * f8_blocks(K) * F8_BLOCK) + f8_scale_rows(T) * f8_blocks(K); }
 
@@ -141,7 +168,7 @@ int bsp_f8_fc(const bsp_weights_f8* w, int32_t transposed, const bsp_codes* X, c
   const F8Input x{X->codes, X->scale, X->dtype, X->dtype == BSP_E5M2, (int64_t)f8_blocks(X->K) * F8_BLOCK};
   const F8Rows rows = rows_of(w, transposed != 0);
   rc = check_workspace(workspace, workspace_bytes, sums_bytes(rows, X->T));
-  return rc != BSP_OK ? rc : multiply(rows, x, X->T, q, y_dtype, workspace, (hipStream_t)stream);
+  return rc != BSP_OK ? rc : multiply(rows, x, X->T, F8Low{}, q, y_dtype, workspace, (hipStream_t)stream);
 }
 
 int bsp_f8_fc_workspace(const bsp_weights_f8* w, int32_t transposed, int32_t T, int32_t coded, int64_t* bytes) {
@@ -167,15 +194,9 @@ int bsp_f8_fc_values(const bsp_weights_f8* w, int32_t transposed, const void* X,
   hipStream_t st = (hipStream_t)stream;
   const F8Rows rows = rows_of(w, transposed != 0);
   const int64_t sums = sums_bytes(rows, T);
-  const bool inside = in_kernel(X, x_dtype, ldx, T, K);
-  rc = check_workspace(workspace, workspace_bytes, sums + (inside ? 0 : codes_bytes(T, K)));
+  rc = check_workspace(workspace, workspace_bytes, sums + (in_kernel(X, x_dtype, ldx, T, K) ? 0 : codes_bytes(T, K)));
   if (rc != BSP_OK) return rc;
-  if (inside) return multiply(rows, F8Input{X, nullptr, x_dtype, e5, ldx}, T, q, y_dtype, workspace, st);
-  const int64_t ld = (int64_t)f8_blocks(K) * F8_BLOCK;
-  uint8_t *codes = (uint8_t*)workspace + sums, *scale = codes + T * ld;
-  rc = f8_launch_save(X, x_dtype == BSP_F32, ldx, T, K, e5, codes, scale, st);
-  if (rc != BSP_OK) return rc;
-  return multiply(rows, F8Input{codes, scale, code, e5, ld}, T, q, y_dtype, workspace, st);
+  return multiply_values(rows, X, x_dtype, ldx, T, K, e5, F8Low{}, q, y_dtype, workspace, sums, st);
 }
 
 int bsp_f8_fc_grad_workspace(const bsp_weights_f8* w, int32_t T, int64_t* bytes) {
@@ -256,6 +277,135 @@ int bsp_layer_norm_grad(const void* dY, int64_t ld_dy, const void* X, int64_t ld
   if (workspace_bytes < need) return BSP_ERR_CAPACITY;
   if (need > 0 && !workspace) return BSP_ERR_NULL;
   return norm_launch_backward(dY, ld_dy, X, ldx, dtype == BSP_F32, mean, rstd, weight, T, D, dX, ld_dx, dweight, dbias, (float*)workspace, (hipStream_t)stream);
+}
+
+int bsp_f8_adapters_size(int32_t R, int32_t I, int32_t O, int64_t* a_elements, int64_t* b_elements) {
+  if (!a_elements || !b_elements) return BSP_ERR_NULL;
+  if (R < 1 || R > kRank || I < 1 || I > kWide || O < 1 || O > kWide) return BSP_ERR_SHAPE;
+  bsp_f8_adapters d{};
+  d.R = R, d.I = I, d.O = O;
+  const F8Adapters v = f8_adapters_of(&d);
+  *a_elements = (int64_t)v.Rp * v.Ip, *b_elements = (int64_t)v.Rp * v.Op;
+  return BSP_OK;
+}
+
+int bsp_f8_adapters_set(const bsp_f8_adapters* d, int32_t slot, int32_t rank, const void* A, int64_t lda, const void* B, int64_t ldb, int32_t dtype,
+                        float scale, void* stream) {
+  int rc = check_adapters(d);
+  if (rc != BSP_OK) return rc;
+  if (slot < 0 || slot >= d->N || rank < 0 || rank > d->R) return BSP_ERR_SHAPE;
+  if (rank > 0) {
+    rc = check_values(A, dtype, lda, rank, d->I, true);
+    if (rc == BSP_OK) rc = check_values(B, dtype, ldb, d->O, rank, true);
+    if (rc != BSP_OK) return rc;
+  } else if (!value_type(dtype)) {
+    return BSP_ERR_DTYPE;
+  }
+  return f8_launch_set(f8_adapters_of(d), slot, rank, A, lda, B, ldb, dtype == BSP_F32, scale, (hipStream_t)stream);
+}
+
+int bsp_f8_requests_size(int32_t T, int32_t N, int64_t* bytes) {
+  if (!bytes) return BSP_ERR_NULL;
+  if (T < 0 || T > kMost || N < 1 || N > kSlots) return BSP_ERR_SHAPE;
+  *bytes = f8_requests_bytes(T, N);
+  return BSP_OK;
+}
+
+int bsp_f8_requests_plan(const bsp_f8_requests* r, const void* which, int32_t which_bytes, void* stream) {
+  const int rc = check_requests(r);
+  if (rc != BSP_OK) return rc;
+  if (which_bytes != 4 && which_bytes != 8) return BSP_ERR_DTYPE;
+  if (r->T == 0 && !r->plan) return BSP_OK;
+  if (r->T > 0 && !which) return BSP_ERR_NULL;
+  if (!aligned(which, which_bytes)) return BSP_ERR_ALIGN;
+  return f8_launch_plan(r, which, which_bytes == 8, (hipStream_t)stream);
+}
+
+int bsp_f8_fc_adapted_workspace(const bsp_weights_f8* w, int32_t transposed, int32_t T, int32_t coded, const bsp_f8_adapters* adapters, int64_t* bytes) {
+  int rc = bsp_f8_fc_workspace(w, transposed, T, coded, bytes);
+  if (rc == BSP_OK) rc = check_adapters(adapters);
+  if (rc == BSP_OK) *bytes = in16(*bytes) + low_bytes(f8_adapters_of(adapters), T);
+  return rc;
+}
+
+int bsp_f8_fc_adapted(const bsp_weights_f8* w, int32_t transposed, const bsp_codes* X, const void* values, int32_t x_dtype, int64_t ldx, int32_t T,
+                      int32_t code, const bsp_f8_adapters* adapters, const bsp_f8_requests* requests, const float* bias, const void* residual,
+                      int32_t relu, const bsp_codes* gate, void* Y, int32_t y_dtype, void* workspace, int64_t workspace_bytes, void* stream) {
+  F8Epilogue q;
+  int rc = check_product(w, transposed, T, bias, residual, relu, gate, Y, y_dtype, &q);
+  if (rc == BSP_OK) rc = check_adapters(adapters);
+  if (rc == BSP_OK) rc = check_requests(requests);
+  if (rc != BSP_OK) return rc;
+  const int K = transposed ? w->O : w->I;
+  if (T < 0 || T > kMost || requests->T != T || requests->N != adapters->N || adapters->I != w->I || adapters->O != w->O) return BSP_ERR_SHAPE;
+  if (X) {
+    rc = check_codes(X);
+    if (rc != BSP_OK) return rc;
+    if (X->T != T || X->K != K) return BSP_ERR_SHAPE;
+  } else {
+    if (!code_type(code)) return BSP_ERR_DTYPE;
+    rc = check_values(values, x_dtype, ldx, T, K, true);
+    if (rc != BSP_OK) return rc;
+  }
+  if (T == 0) return BSP_OK;
+  const F8Rows rows = rows_of(w, transposed != 0);
+  const F8Adapters d = f8_adapters_of(adapters);
+  const int64_t sums = sums_bytes(rows, T), codes = X || in_kernel(values, x_dtype, ldx, T, K) ? 0 : codes_bytes(T, K);
+  rc = check_workspace(workspace, workspace_bytes, in16(sums + codes) + low_bytes(d, T));
+  if (rc != BSP_OK) return rc;
+  hipStream_t st = (hipStream_t)stream;
+  const F8Requests who = f8_requests_of(requests);
+  float* u = (float*)((uint8_t*)workspace + in16(sums + codes));
+  const int64_t ld = (int64_t)f8_blocks(K) * F8_BLOCK;
+  const F8Input given = X ? F8Input{X->codes, X->scale, X->dtype, X->dtype == BSP_E5M2, ld} : F8Input{values, nullptr, x_dtype, code == BSP_E5M2, ldx};
+  rc = f8_launch_down(d, transposed != 0, given, T, who, u, st);
+  if (rc != BSP_OK) return rc;
+  const F8Low low{who.which, u, transposed ? d.a_t : d.b, (int64_t)d.Rp * (transposed ? d.Ip : d.Op), d.Rp};
+  if (X) return multiply(rows, given, T, low, q, y_dtype, workspace, st);
+  return multiply_values(rows, values, x_dtype, ldx, T, K, code == BSP_E5M2, low, q, y_dtype, workspace, sums, st);
+}
+
+int bsp_f8_adapters_grad_workspace(const bsp_f8_adapters* adapters, int32_t T, int64_t* bytes) {
+  if (!bytes) return BSP_ERR_NULL;
+  const int rc = check_adapters(adapters);
+  if (rc != BSP_OK) return rc;
+  if (T < 0 || T > kMost) return BSP_ERR_SHAPE;
+  const F8Adapters d = f8_adapters_of(adapters);
+  *bytes = 2 * low_bytes(d, T) + f8_adapt_part_bytes(d, T);
+  return BSP_OK;
+}
+
+int bsp_f8_adapters_grad(const bsp_f8_adapters* adapters, const void* dY, int64_t ldy, const bsp_codes* X, const void* values, int64_t ldx, int32_t T,
+                         const bsp_f8_requests* requests, float* dA, float* dB, void* workspace, int64_t workspace_bytes, void* stream) {
+  int64_t need = 0;
+  int rc = bsp_f8_adapters_grad_workspace(adapters, T, &need);
+  if (rc == BSP_OK) rc = check_requests(requests);
+  if (rc == BSP_OK) rc = check_values(dY, BSP_BF16, ldy, T, adapters->O, true);
+  if (rc != BSP_OK) return rc;
+  if (requests->T != T || requests->N != adapters->N) return BSP_ERR_SHAPE;
+  if (X) {
+    rc = check_codes(X);
+    if (rc != BSP_OK) return rc;
+    if (X->T != T || X->K != adapters->I) return BSP_ERR_SHAPE;
+  } else {
+    rc = check_values(values, BSP_BF16, ldx, T, adapters->I, true);
+    if (rc != BSP_OK) return rc;
+  }
+  if (!dA || !dB || !requests->plan) return BSP_ERR_NULL;
+  if (!aligned(dA, 4) || !aligned(dB, 4)) return BSP_ERR_ALIGN;
+  rc = check_workspace(workspace, workspace_bytes, need);
+  if (rc != BSP_OK) return rc;
+  hipStream_t st = (hipStream_t)stream;
+  const F8Adapters d = f8_adapters_of(adapters);
+  const F8Requests who = f8_requests_of(requests);
+  float *u = (float*)workspace, *v = u + (int64_t)T * d.Rp, *part = v + (int64_t)T * d.Rp;
+  const F8Input x = X ? F8Input{X->codes, X->scale, X->dtype, X->dtype == BSP_E5M2, (int64_t)f8_blocks(X->K) * F8_BLOCK} : F8Input{values, nullptr, BSP_BF16, 0, ldx};
+  if (T > 0) {
+    rc = f8_launch_down(d, false, x, T, who, u, st);
+    if (rc == BSP_OK) rc = f8_launch_down(d, true, F8Input{dY, nullptr, BSP_BF16, 0, ldy}, T, who, v, st);
+    if (rc != BSP_OK) return rc;
+  }
+  return f8_launch_adapt_grad(d, (const uint16_t*)dY, ldy, x, T, who, u, v, part, dA, dB, st);
 }
 
 int bsp_rms_norm(const void* X, int64_t ldx, const void* residual, int64_t ldr, int32_t dtype, int32_t T, int32_t D, const float* weight, float eps,
@@ -391,6 +541,17 @@ int bsp_f8_call_packed(int32_t call, const int64_t* w) {
     case BSP_F8_CALL_NORM_GRAD:
       return bsp_layer_norm_grad(ptr(0), w[1], ptr(2), w[3], num(4), size(5), size(6), (const float*)ptr(7), (const float*)ptr(8), (const float*)ptr(9),
                                  ptr(10), w[11], (float*)ptr(12), (float*)ptr(13), ptr(14), w[15], ptr(16));
+    case BSP_F8_CALL_ADAPTED: {
+      const bsp_codes x = codes(2), g = codes(17);
+      return bsp_f8_fc_adapted((const bsp_weights_f8*)ptr(0), num(1), none(2) ? nullptr : &x, ptr(7), num(8), w[9], size(10), num(11),
+                               (const bsp_f8_adapters*)ptr(12), (const bsp_f8_requests*)ptr(13), (const float*)ptr(14), ptr(15), num(16),
+                               none(17) ? nullptr : &g, ptr(22), num(23), ptr(24), w[25], ptr(26));
+    }
+    case BSP_F8_CALL_ADAPTERS_GRAD: {
+      const bsp_codes x = codes(3);
+      return bsp_f8_adapters_grad((const bsp_f8_adapters*)ptr(0), ptr(1), w[2], none(3) ? nullptr : &x, ptr(8), w[9], size(10), (const bsp_f8_requests*)ptr(11),
+                                  (float*)ptr(12), (float*)ptr(13), ptr(14), w[15], ptr(16));
+    }
     case BSP_F8_CALL_RMS_NORM: {
       const bsp_codes c = codes(13);
       return bsp_rms_norm(ptr(0), w[1], ptr(2), w[3], num(4), size(5), size(6), (const float*)ptr(7), (float)real(8), ptr(9), w[10], ptr(11), w[12],

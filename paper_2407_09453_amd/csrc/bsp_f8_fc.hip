@@ -26,6 +26,7 @@ struct TileArgs {
   float* part;  // split > 1: sums of each share of the block columns, [split][T][4 ceil(out / 4)], instead of results
   int32_t split;
   int32_t full;  // blocks in a block row, where all are kept; else 0
+  F8Low low;
 };
 
 __device__ __forceinline__ i32x8_t read_fragment(const uint8_t* p, int at0, int at1) {
@@ -120,6 +121,63 @@ __device__ __forceinline__ void store_tile(const F8Epilogue& q, f32x16_t (&acc)[
     };
     if (O % 8 == 0) rows(std::true_type{});
     else rows(std::false_type{});
+  }
+}
+
+// The rows' adapters: B_a u_t added to a wave's sums, one adapter of its rows after the other.  The rows are the matrix instruction's columns, so a
+// lane holds results of one row, and keeps or drops what an adapter adds to it as that is the row's own or another's: nothing of
+// another adapter's, NaN among it, gets there.  u enters as two bf16 parts.
+template <int MO, int MT>
+__device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT], int T, int64_t t0, int o0) {
+  const int lane = threadIdx.x & 63;
+  int of[MT];
+  const float* u[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int64_t t = t0 + m * 32 + (lane & 31);
+    of[m] = t < T ? low.which[t] : -1;
+    u[m] = low.u + (t < T ? t : T - 1) * low.rank + (lane >> 5) * 8;
+  }
+  uint64_t todo[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) todo[m] = __ballot(of[m] >= 0);
+  for (;;) {
+    int now = -1;
+#pragma unroll
+    for (int m = MT - 1; m >= 0; --m)
+      if (todo[m]) now = __builtin_amdgcn_readlane(of[m], __builtin_ctzll(todo[m]));
+    if (now < 0) break;
+    const uint16_t* b = low.up + now * low.step + (int64_t)(o0 + (lane & 31)) * low.rank + (lane >> 5) * 8;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const bool mine = of[m] == now;
+      const uint64_t those = __ballot(mine);
+      if (!those) continue;
+      todo[m] &= ~those;
+      f32x16_t sum[MO];
+#pragma unroll
+      for (int o = 0; o < MO; ++o) sum[o] = acc[o][m];
+      for (int k = 0; k < low.rank; k += 16) {
+        const f32x4_t x0 = *(const f32x4_t*)(u[m] + k), x1 = *(const f32x4_t*)(u[m] + k + 4);
+        u32x4_t high, rest;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float a0 = (e < 2 ? x0 : x1)[2 * (e & 1)], a1 = (e < 2 ? x0 : x1)[2 * (e & 1) + 1];
+          high[e] = f8_pack_bf16x2(a0, a1);
+          rest[e] = f8_pack_bf16x2(a0 - __uint_as_float(high[e] << 16), a1 - __uint_as_float(high[e] & 0xFFFF0000u));
+        }
+#pragma unroll
+        for (int o = 0; o < MO; ++o) {
+          const u32x4_t w = *(const u32x4_t*)(b + (int64_t)o * 32 * low.rank + k);
+          sum[o] = mfma_bf16_32x32x16(w, high, sum[o]);
+          sum[o] = mfma_bf16_32x32x16(w, rest, sum[o]);
+        }
+      }
+#pragma unroll
+      for (int o = 0; o < MO; ++o)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[o][m][e] = mine ? sum[o][e] : acc[o][m][e];
+    }
   }
 }
 
@@ -254,11 +312,10 @@ struct Wide {
   }
 };
 
-template <int MO, int MT, int WO, int WT, int BUFS, bool E5, bool F32>
-__global__ __launch_bounds__(64 * WO * WT) void f8_wide(TileArgs a) {
+// LOW: with adapters beside the layer.
+template <int MO, int MT, int WO, int WT, int BUFS, bool E5, bool F32, bool LOW>
+__device__ __forceinline__ void wide(const TileArgs& a, uint8_t* lds) {
   using K = Wide<MO, MT, WO, WT, BUFS>;
-  extern __shared__ uint8_t lds[];
-  kernarg_touch<TileArgs>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wo = wave / WT, wt = wave % WT;
   // a share of the block columns, and the tile
@@ -355,6 +412,8 @@ __global__ __launch_bounds__(64 * WO * WT) void f8_wide(TileArgs a) {
     rest(std::integral_constant<int, 1>{});
     rest(std::integral_constant<int, 0>{});
   }
+  if constexpr (LOW)
+    if (share == 0) add_low<MO, MT>(a.low, acc, a.T, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32);
   __syncthreads();
   if constexpr (kSplits) {
     if (a.split > 1) {
@@ -365,6 +424,19 @@ __global__ __launch_bounds__(64 * WO * WT) void f8_wide(TileArgs a) {
     }
   }
   store_tile<MO, MT, F32>(a.q, acc, lds + wave * kStoreBytes<MO>, a.T, a.w.out, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32);
+}
+
+template <int MO, int MT, int WO, int WT, int BUFS, bool E5, bool F32>
+__global__ __launch_bounds__(64 * WO * WT) void f8_wide(TileArgs a) {
+  extern __shared__ uint8_t lds[];
+  kernarg_touch<TileArgs>();
+  wide<MO, MT, WO, WT, BUFS, E5, F32, false>(a, lds);
+}
+template <int MO, int MT, int WO, int WT, int BUFS, bool E5, bool F32>
+__global__ __launch_bounds__(64 * WO * WT) void f8_wide_low(TileArgs a) {
+  extern __shared__ uint8_t lds[];
+  kernarg_touch<TileArgs>();
+  wide<MO, MT, WO, WT, BUFS, E5, F32, true>(a, lds);
 }
 
 // The shares' sums, in their order, and what follows a product: a thread takes four channels of a row.
@@ -390,11 +462,12 @@ int launch(void (*kernel)(TileArgs), bool raised, int threads, int lds, TileArgs
 }
 bool raise(const void* kernel, int lds) { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess; }
 
-template <int MO, int MT, int WO, int WT, int BUFS, bool E5, bool F32>
+template <int MO, int MT, int WO, int WT, int BUFS, bool E5, bool F32, bool LOW>
 int launch_wide(const TileArgs& a, hipStream_t st) {
   using K = Wide<MO, MT, WO, WT, BUFS>;
-  static const bool raised = raise((const void*)&f8_wide<MO, MT, WO, WT, BUFS, E5, F32>, K::kLds);
-  return launch<K::NO, K::NT>(f8_wide<MO, MT, WO, WT, BUFS, E5, F32>, raised, 64 * K::WAVES, K::kLds, a, st);
+  constexpr auto kernel = LOW ? &f8_wide_low<MO, MT, WO, WT, BUFS, E5, F32> : &f8_wide<MO, MT, WO, WT, BUFS, E5, F32>;
+  static const bool raised = raise((const void*)kernel, K::kLds);
+  return launch<K::NO, K::NT>(kernel, raised, 64 * K::WAVES, K::kLds, a, st);
 }
 
 // Which tile: the smaller of the chip's rate on it and of the steps' own latency, one after the other.  `alone`: us a step where a CU has one
@@ -433,21 +506,21 @@ Plan plan_of(int O, int64_t nnzb, int T, bool full, bool f32) {
   return best;
 }
 
-template <bool E5>
+template <bool E5, bool LOW>
 int launch_any(const TileArgs& a, int k, bool f32, hipStream_t st) {
   if (f32) {
     switch (k) {
-      case 3: return launch_wide<2, 1, 2, 2, 3, E5, true>(a, st);
-      case 4: return launch_wide<1, 1, 4, 1, 4, E5, true>(a, st);
-      default: return launch_wide<2, 2, 2, 2, 2, E5, true>(a, st);
+      case 3: return launch_wide<2, 1, 2, 2, 3, E5, true, LOW>(a, st);
+      case 4: return launch_wide<1, 1, 4, 1, 4, E5, true, LOW>(a, st);
+      default: return launch_wide<2, 2, 2, 2, 2, E5, true, LOW>(a, st);
     }
   }
   switch (k) {
-    case 0: return launch_wide<4, 2, 2, 4, 2, E5, false>(a, st);
-    case 1: return launch_wide<4, 2, 1, 4, 3, E5, false>(a, st);
-    case 2: return launch_wide<2, 2, 2, 2, 2, E5, false>(a, st);
-    case 3: return launch_wide<2, 1, 2, 2, 3, E5, false>(a, st);
-    default: return launch_wide<1, 1, 4, 1, 4, E5, false>(a, st);
+    case 0: return launch_wide<4, 2, 2, 4, 2, E5, false, LOW>(a, st);
+    case 1: return launch_wide<4, 2, 1, 4, 3, E5, false, LOW>(a, st);
+    case 2: return launch_wide<2, 2, 2, 2, 2, E5, false, LOW>(a, st);
+    case 3: return launch_wide<2, 1, 2, 2, 3, E5, false, LOW>(a, st);
+    default: return launch_wide<1, 1, 4, 1, 4, E5, false, LOW>(a, st);
   }
 }
 
@@ -459,11 +532,12 @@ bool all_kept(const F8Rows& w) { return w.nnzb == (int64_t)f8_blocks(w.out) * f8
 
 int f8_tile_split(const F8Rows& w, int T, bool f32) { return plan_of(w.out, w.nnzb, T, all_kept(w), f32).split; }
 
-int f8_launch_tile(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, float* part, hipStream_t st) {
+int f8_launch_tile(const F8Rows& w, const F8Input& x, int T, const F8Low& low, const F8Epilogue& q, bool f32, float* part, hipStream_t st) {
   const bool full = all_kept(w);
   const Plan plan = plan_of(w.out, w.nnzb, T, full, f32);
-  TileArgs a{w, (const uint8_t*)x.X, x.scale, q, x.ld, f8_scale_rows(T), T, 0, 0, part, plan.split, full ? f8_blocks(w.in) : 0};
-  return x.e5 ? launch_any<true>(a, plan.tile, f32, st) : launch_any<false>(a, plan.tile, f32, st);
+  TileArgs a{w, (const uint8_t*)x.X, x.scale, q, x.ld, f8_scale_rows(T), T, 0, 0, part, plan.split, full ? f8_blocks(w.in) : 0, low};
+  if (low.rank) return x.e5 ? launch_any<true, true>(a, plan.tile, f32, st) : launch_any<false, true>(a, plan.tile, f32, st);
+  return x.e5 ? launch_any<true, false>(a, plan.tile, f32, st) : launch_any<false, false>(a, plan.tile, f32, st);
 }
 
 int f8_launch_join(const float* part, int split, int T, int O, const F8Epilogue& q, bool f32, hipStream_t st) {

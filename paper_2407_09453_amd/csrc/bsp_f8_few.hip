@@ -25,6 +25,7 @@ struct FewArgs {
   int32_t full;    // blocks in a block row, where all are kept; else 0
   int32_t split;
   float* part;     // split > 1: sums of each share of the block columns, as f8_join reads them
+  F8Low low;
 };
 
 // 128 products per lane row: scaled codes, or (F32) both sides as bf16 so that nothing is lost in the sum.  The instruction on
@@ -82,11 +83,29 @@ __device__ __forceinline__ void few_stage(const FewArgs& a, uint8_t* codes, uint
 template <int MT>
 constexpr int kMostWaves = MT == 1 ? 16 : 8;
 
-template <int MT, int SRC, bool E5, bool F32>
-__global__ __launch_bounds__((64 * kMostWaves<MT>)) void f8_few(FewArgs a) {
+// four channels' share of a row's adapter: fp32 products of u with bf16 weights
+__device__ __forceinline__ f32x4_t few_low(const F8Low& low, int64_t row, int o, f32x4_t s) {
+  const int of = low.which[row];
+  if (of < 0) return s;
+  const uint16_t* b = low.up + of * low.step + (int64_t)o * low.rank;  // (channels are padded to whole blocks)
+  const float* u = low.u + row * low.rank;
+#pragma unroll 2
+  for (int r = 0; r < low.rank; r += 8) {
+    const f32x4_t u0 = *(const f32x4_t*)(u + r), u1 = *(const f32x4_t*)(u + r + 4);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const u32x4_t w = *(const u32x4_t*)(b + c * low.rank + r);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[c] += __uint_as_float(w[e] << 16) * (e < 2 ? u0 : u1)[2 * (e & 1)] + __uint_as_float(w[e] & 0xFFFF0000u) * (e < 2 ? u0 : u1)[2 * (e & 1) + 1];
+    }
+  }
+  return s;
+}
+
+// LOW: with adapters beside the layer.
+template <int MT, int SRC, bool E5, bool F32, bool LOW>
+__device__ __forceinline__ void few(const FewArgs& a, float* sums) {  // sums: [waves][MT][64][4], behind them the rows' codes
   constexpr int kAhead = MT == 1 && F32 ? 3 : 4;
-  extern __shared__ float sums[];  // [waves][MT][64][4], behind them the rows' codes
-  kernarg_touch<FewArgs>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int r = lane & 15, g = lane >> 4;
   const int br = blockIdx.x >> 3;
@@ -185,13 +204,29 @@ __global__ __launch_bounds__((64 * kMostWaves<MT>)) void f8_few(FewArgs a) {
     const int64_t row = t0 + (i >> 6) * 16 + (i & 15);
     const int o = blockIdx.x * 16 + ((i >> 4) & 3) * 4;
     if (row >= a.T || o >= a.w.out) continue;
+    if constexpr (LOW)
+      if (blockIdx.z == 0) s = few_low(a.low, row, o, s);
     if (a.split > 1) *(f32x4_t*)(a.part + (((int64_t)blockIdx.z * a.T + row) * ((a.w.out + 3) >> 2) + (o >> 2)) * 4) = s;
     else f8_store4<F32>(a.q, row, o, a.w.out, s[0], s[1], s[2], s[3]);
   }
 }
 
 template <int MT, int SRC, bool E5, bool F32>
+__global__ __launch_bounds__((64 * kMostWaves<MT>)) void f8_few(FewArgs a) {
+  extern __shared__ float sums[];
+  kernarg_touch<FewArgs>();
+  few<MT, SRC, E5, F32, false>(a, sums);
+}
+template <int MT, int SRC, bool E5, bool F32>
+__global__ __launch_bounds__((64 * kMostWaves<MT>)) void f8_few_low(FewArgs a) {
+  extern __shared__ float sums[];
+  kernarg_touch<FewArgs>();
+  few<MT, SRC, E5, F32, true>(a, sums);
+}
+
+template <int MT, int SRC, bool E5, bool F32, bool LOW>
 int launch(FewArgs a, hipStream_t st) {
+  constexpr auto kernel = LOW ? &f8_few_low<MT, SRC, E5, F32> : &f8_few<MT, SRC, E5, F32>;
   const int strips = (a.w.out + 15) / 16, tiles = (a.T + 16 * MT - 1) / (16 * MT);
   const int64_t per_row = (a.w.nnzb + (int64_t)f8_blocks(a.w.out) * a.split - 1) / ((int64_t)f8_blocks(a.w.out) * a.split);
   // as many waves as a CU holds, on every CU; a wave for every block is enough
@@ -202,19 +237,24 @@ int launch(FewArgs a, hipStream_t st) {
   if constexpr (SRC != kCodes) {
     a.rows = a.T;
     lds += (f8_few_staged(a.T, a.w.in) + 15) & ~15;
-    static const bool raised = hipFuncSetAttribute((const void*)&f8_few<MT, SRC, E5, F32>, hipFuncAttributeMaxDynamicSharedMemorySize, kFewStaged + 16 * 1024 + 16) == hipSuccess;
+    static const bool raised = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kFewStaged + 16 * 1024 + 16) == hipSuccess;
     if (!raised) return BSP_ERR_HIP;
   }
-  hipLaunchKernelGGL((f8_few<MT, SRC, E5, F32>), dim3((unsigned)strips, (unsigned)tiles, (unsigned)a.split), dim3((unsigned)(64 * waves)), (size_t)lds, st, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)strips, (unsigned)tiles, (unsigned)a.split), dim3((unsigned)(64 * waves)), (size_t)lds, st, a);
   return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP;
 }
 
-template <bool E5, bool F32>
+template <bool E5, bool F32, bool LOW>
 int launch_rows(const FewArgs& a, hipStream_t st) {
-  if (a.x.dtype == BSP_BF16) return launch<1, kBf16, E5, F32>(a, st);
-  if (a.x.dtype == BSP_F32) return launch<1, kF32, E5, F32>(a, st);
-  if (a.T <= 16) return launch<1, kCodes, E5, F32>(a, st);
-  return launch<2, kCodes, E5, F32>(a, st);
+  if (a.x.dtype == BSP_BF16) return launch<1, kBf16, E5, F32, LOW>(a, st);
+  if (a.x.dtype == BSP_F32) return launch<1, kF32, E5, F32, LOW>(a, st);
+  if (a.T <= 16) return launch<1, kCodes, E5, F32, LOW>(a, st);
+  return launch<2, kCodes, E5, F32, LOW>(a, st);
+}
+template <bool LOW>
+int launch_any(const FewArgs& a, bool f32, hipStream_t st) {
+  if (f32) return a.x.e5 ? launch_rows<true, true, LOW>(a, st) : launch_rows<false, true, LOW>(a, st);
+  return a.x.e5 ? launch_rows<true, false, LOW>(a, st) : launch_rows<false, false, LOW>(a, st);
 }
 
 }  // namespace
@@ -228,9 +268,8 @@ int f8_few_split(const F8Rows& w, int T) {
   return split;
 }
 
-int f8_launch_few(const F8Rows& w, const F8Input& x, int T, const F8Epilogue& q, bool f32, float* part, hipStream_t st) {
-  FewArgs a{w, x, q, f8_scale_rows(T), T, 0, 0, f8_few_split(w, T), part};
+int f8_launch_few(const F8Rows& w, const F8Input& x, int T, const F8Low& low, const F8Epilogue& q, bool f32, float* part, hipStream_t st) {
+  FewArgs a{w, x, q, f8_scale_rows(T), T, 0, 0, f8_few_split(w, T), part, low};
   if (w.nnzb == (int64_t)f8_blocks(w.out) * f8_blocks(w.in)) a.full = f8_blocks(w.in);
-  if (f32) return x.e5 ? launch_rows<true, true>(a, st) : launch_rows<false, true>(a, st);
-  return x.e5 ? launch_rows<true, false>(a, st) : launch_rows<false, false>(a, st);
+  return low.rank ? launch_any<true>(a, f32, st) : launch_any<false>(a, f32, st);
 }

@@ -25,8 +25,8 @@ from .binding import (BSP_BF16, BSP_E4M3, BSP_E5M2, BSP_F32, BspError, _check, _
 
 CODES = {"e4m3": BSP_E4M3, "e5m2": BSP_E5M2}
 _SAVE, _LOAD, _FC, _VALUES, _GRAD, _NORM, _NORM_GRAD = range(7)
-_RMS, _RMS_GRAD = 16, 17
-_pack9, _pack13, _pack17, _pack18, _pack20 = (struct.Struct("=%dq" % n).pack for n in (9, 13, 17, 18, 20))
+_RMS, _RMS_GRAD, _ADAPTED = 16, 17, 20
+_pack9, _pack13, _pack17, _pack18, _pack20, _pack27 = (struct.Struct("=%dq" % n).pack for n in (9, 13, 17, 18, 20, 27))
 _pack_norm, _pack_rms = struct.Struct("=7qd10q").pack, struct.Struct("=8qd11q").pack
 _NO_CODES = (0, 0, 0, 0, 0)
 _types = _torch = None
@@ -233,20 +233,29 @@ class BspLayerF8:
             self.d_bias.copy_(b)
         _check(load_library().bsp_f8_pack(self.struct, W.data_ptr(), kind, ld, _current_stream(W)), "bsp_f8_pack")
 
-    def _bytes(self, kind, T):
-        n = self._workspace.get((kind, T))
+    def _bytes(self, kind, T, adapters=None):
+        key = (kind, T) if adapters is None else (kind, T, adapters.R)
+        n = self._workspace.get(key)
         if n is None:
             lib, n = load_library(), ctypes.c_int64(0)
-            if kind == "grad":
+            if adapters is not None:
+                _check(lib.bsp_f8_fc_adapted_workspace(self.struct, kind >> 1, T, kind & 1, adapters.struct, n), "bsp_f8_fc_adapted_workspace")
+            elif kind == "grad":
                 _check(lib.bsp_f8_fc_grad_workspace(self.struct, T, n), "bsp_f8_fc_grad_workspace")
             else:
                 _check(lib.bsp_f8_fc_workspace(self.struct, kind >> 1, T, kind & 1, n), "bsp_f8_fc_workspace")
             if len(self._workspace) > 4096:
                 self._workspace.clear()
-            n = self._workspace[(kind, T)] = n.value
+            n = self._workspace[key] = n.value
         return n
 
-    def _multiply(self, transposed, X, code, bias, residual, relu, gate, dtype, out):
+    def _beside(self, adapters, requests, T):
+        assert adapters is not None and requests is not None, "adapters and requests go together"
+        assert (adapters.I, adapters.O) == (self.I, self.O), "adapters of a layer %d -> %d" % (adapters.I, adapters.O)
+        assert (requests.T, requests.N) == (T, adapters.N), "requests of %d rows and %d slots" % (T, adapters.N)
+        assert adapters._index == requests._index == self._index, "tensors on different devices"
+
+    def _multiply(self, transposed, X, code, bias, residual, relu, gate, dtype, out, adapters=None, requests=None):
         codes = type(X) is BspCodes
         if codes:
             T, K, at = X.T, X.K, X.buffer
@@ -276,34 +285,43 @@ class BspLayerF8:
             _on(at, gate.buffer)
             g = gate.words
         st = _current_stream(out)
+        low = adapters is not None or requests is not None
+        if low:
+            self._beside(adapters, requests, T)
         if codes:
-            n = self._bytes(transposed * 2 + 1, T)
+            coded = True
         else:  # (few whole rows become codes inside the product's kernel)
             x, size = X.data_ptr(), X.element_size()
-            inside = T <= 16 and not (x | ld * size | K * size) & 15 and T * (_blocks(K) * 129 + 16) <= 73728
-            n = self._bytes(transposed * 2 + inside, T)
+            coded = T <= 16 and not (x | ld * size | K * size) & 15 and T * (_blocks(K) * 129 + 16) <= 73728
+        n = self._bytes(transposed * 2 + coded, T, adapters)
         ws = _torch.empty(n, dtype=_torch.uint8, device=self.device) if n else None
         rest = (0 if bias is None else bias.data_ptr(), r, 1 if relu else 0, *g, out.data_ptr(), _type(out), 0 if ws is None else ws.data_ptr(), n, st)
-        if codes:
+        if low:
+            given = (*X.words, 0, 0, 0) if codes else (*_NO_CODES, x, _type(X), ld)
+            _call(_ADAPTED, _pack27(self._address, transposed, *given, T, CODES[code], adapters._address, requests._address, *rest), "bsp_f8_fc_adapted")
+        elif codes:
             _call(_FC, _pack20(self._address, transposed, *X.words, *rest), "bsp_f8_fc")
         else:
             _call(_VALUES, _pack20(self._address, transposed, x, _type(X), ld, T, CODES[code], *rest), "bsp_f8_fc_values")
         return out
 
-    def fc(self, X, relu=False, residual=None, dtype=None, out=None, stream=None):
+    def fc(self, X, relu=False, residual=None, dtype=None, out=None, stream=None, adapters=None, requests=None):
         """Y [T][O] = act(X W^t + b + residual) for X [T][I]: a torch tensor (fp32 or bf16, brought to e4m3 codes within the
-        call; Y has its type unless ``dtype`` says otherwise) or a BspCodes (Y is bf16 unless ``dtype`` says otherwise)."""
+        call; Y has its type unless ``dtype`` says otherwise) or a BspCodes (Y is bf16 unless ``dtype`` says otherwise).
+        With ``adapters`` (a BspAdapters) and ``requests`` (a BspRequests) each row's adapter adds scale B (A x) before act, of x as it
+        is given."""
         if stream is not None:
-            return _on_stream(stream, self.payload, self.fc, X, relu, residual, dtype, out)
-        return self._multiply(0, X, "e4m3", self.d_bias, residual, relu, None, dtype, out)
+            return _on_stream(stream, self.payload, self.fc, X, relu, residual, dtype, out, None, adapters, requests)
+        return self._multiply(0, X, "e4m3", self.d_bias, residual, relu, None, dtype, out, adapters, requests)
 
-    def grad_input(self, dY, relu_of: Optional[BspCodes] = None, code: str = "e5m2", dtype=None, out=None, stream=None):
+    def grad_input(self, dY, relu_of: Optional[BspCodes] = None, code: str = "e5m2", dtype=None, out=None, stream=None, adapters=None, requests=None):
         """dX [T][I] = dY W for dY [T][O] (brought to codes of type ``code`` within the call, or a BspCodes).  ``relu_of``: the
         checkpoint of this layer's input, where that is a ReLU's output; the result is then the gradient of what went
-        into the ReLU."""
+        into the ReLU.  ``adapters`` and ``requests``: those of the forward call, each row's adapter adds scale A^t (B^t dy), of dy as it
+        is given (see BspAdapters.grad for their own gradients)."""
         if stream is not None:
-            return _on_stream(stream, self.payload, self.grad_input, dY, relu_of, code, dtype, out)
-        return self._multiply(1, dY, code, None, None, False, relu_of, dtype, out)
+            return _on_stream(stream, self.payload, self.grad_input, dY, relu_of, code, dtype, out, None, adapters, requests)
+        return self._multiply(1, dY, code, None, None, False, relu_of, dtype, out, adapters, requests)
 
     def grad_weight(self, dY, X: BspCodes, bias: bool = True, out=None, stream=None):
         """(dW, db) from dY (bf16 [T][O]) and the checkpoint of the layer's input: dW float [O][I], zero where the mask is; db
@@ -371,7 +389,7 @@ def layer_norm_grad(dY, X, mean, rstd, weight=None, stream=None):
     _on(X, dY, mean, rstd, weight)
     dX = torch.empty((T, D), dtype=X.dtype, device=X.device)
     dw, db = torch.empty((2, D), dtype=torch.float32, device=X.device).unbind(0)
-    n = _norm_bytes("bsp_layer_norm_grad_workspace", T, D)
+    n = _norm_bytes(T, D)
     ws = torch.empty(n, dtype=torch.uint8, device=X.device) if n else None
     _call(_NORM_GRAD, _pack17(dY.data_ptr(), ld_dy, X.data_ptr(), ld, _type(X), T, D, mean.data_ptr(), rstd.data_ptr(), _vector(weight, D),
                               dX.data_ptr(), D, dw.data_ptr(), db.data_ptr(), 0 if ws is None else ws.data_ptr(), n, _current_stream(X)), "bsp_layer_norm_grad")
@@ -433,22 +451,27 @@ def rms_norm_grad(dY, H, rstd, weight=None, dH=None, stream=None):
     _on(H, dY, rstd, weight, dH)
     dX = torch.empty((T, D), dtype=H.dtype, device=H.device)
     dw = torch.empty(D, dtype=torch.float32, device=H.device)
-    n = _norm_bytes("bsp_rms_norm_grad_workspace", T, D)
+    n = _bytes_of("bsp_rms_norm_grad_workspace", T, D)
     ws = torch.empty(n, dtype=torch.uint8, device=H.device) if n else None
     _call(_RMS_GRAD, _pack17(dY.data_ptr(), ld_dy, H.data_ptr(), ld, d, ld_dh, _type(H), T, D, rstd.data_ptr(), _vector(weight, D), dX.data_ptr(), D,
                              dw.data_ptr(), 0 if ws is None else ws.data_ptr(), n, _current_stream(H)), "bsp_rms_norm_grad")
     return dX, dw
 
 
-_norm_sizes = {}
+def _norm_bytes(T, D):
+    return _bytes_of("bsp_layer_norm_grad_workspace", T, D)
 
 
-def _norm_bytes(call, *sizes):
-    n = _norm_sizes.get((call, sizes))
+_sizes = {}
+
+
+def _bytes_of(call, *sizes):
+    """What one of the library's ``*_workspace`` calls says, asked once for each size."""
+    n = _sizes.get((call, sizes))
     if n is None:
         n = ctypes.c_int64(0)
         _check(getattr(load_library(), call)(*sizes, n), call)
-        if len(_norm_sizes) > 4096:
-            _norm_sizes.clear()
-        n = _norm_sizes[(call, sizes)] = n.value
+        if len(_sizes) > 4096:
+            _sizes.clear()
+        n = _sizes[(call, sizes)] = n.value
     return n

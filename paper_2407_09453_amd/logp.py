@@ -5,7 +5,7 @@ from __future__ import annotations
 import struct
 
 from .binding import BSP_F32, _current_stream
-from .f8 import _call, _norm_bytes, _on, _on_stream, _rows, _type, _unrecorded
+from .f8 import _bytes_of, _call, _on, _on_stream, _rows, _type, _unrecorded
 
 _LOG_PROBS, _LOG_PROBS_GRAD = 18, 19
 _pack_logp, _pack_grad = struct.Struct("=7qd9q").pack, struct.Struct("=7qd7q").pack
@@ -39,7 +39,7 @@ def log_probs(logits, tokens, top: int = 0, scale: float = 1.0, stream=None):
     T, V, ld = _rows(logits)
     token, size = _tokens(tokens, logits)
     logp, lse, entropy = torch.empty((3, T), dtype=torch.float32, device=logits.device).unbind(0)
-    n = _norm_bytes("bsp_log_probs_workspace", T, V, top)
+    n = _bytes_of("bsp_log_probs_workspace", T, V, top)
     top_logp = top_tokens = ws = None
     if top:
         top_logp = torch.empty((T, top), dtype=torch.float32, device=logits.device)
