@@ -9,16 +9,16 @@
 // and log S = log1p(s), its log probability and the entropy keep all their bits.  Long rows, and rows of a few tokens' batch, are cut
 // into chunks whose (m, n, s, q) and likeliest a second launch joins, in their order.
 //
-// The k likeliest of a row: the k-th largest of 64 groups' maxima is at most the k-th largest value, so what lies below it is out; what is left,
-// little more than k on logits in any order that is not made for it, goes to LDS and is ranked by counting.  Keys are the value's bits,
-// ordered, and the complement of the index: all differ, and the lowest index wins a tie.  Where more is left than LDS holds (a row of
-// equal values) the k-th key is found bit by bit.
+// The k likeliest of a row: the k-th largest of 64 groups' maxima is at most the k-th largest value, so what lies below it is out (below its
+// upper 16 bits, which is what is searched for); what is left, little more than k on logits in any order that is not made for it, goes to LDS,
+// each wave's to a list of its own, and is ranked by counting.  Keys are the value's bits, ordered, and the complement of the
+// index: all differ, and the lowest index wins a tie.  Where more is left than a list holds (a row of equal values) the k-th key is
+// found bit by bit.
 #include "bsp_norm.h"
 
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kKeys = 512;     // keys kept for ranking
 constexpr int kChunksMost = 64, kTopMost = 64;
 
 struct LogpArgs {
@@ -74,10 +74,9 @@ __device__ __forceinline__ float logit(const LogpArgs& a, int64_t row, int64_t i
 }
 
 // a row's three results: one thread
-__device__ __forceinline__ void put_row(const LogpArgs& a, int64_t row, const Sums& v, bool f32) {
+__device__ __forceinline__ void put_row(const LogpArgs& a, int64_t row, const Sums& v, float log, bool f32) {
   const int64_t token = a.wide_tokens ? ((const int64_t*)a.tokens)[row] : (int64_t)((const int32_t*)a.tokens)[row];
   const bool none = v.n == 0.f && v.s == 0.f;  // no token is left: every probability is zero
-  const float log = log_of(v);
   float p = 0.f;
   if (token >= a.V) p = __builtin_nanf("");
   else if (token >= 0) p = none ? -INFINITY : (logit(a, row, token, f32) - v.m) * a.scale - log;
@@ -85,83 +84,110 @@ __device__ __forceinline__ void put_row(const LogpArgs& a, int64_t row, const Su
   a.lse[row] = none ? -INFINITY : v.m * a.scale + log;
   a.entropy[row] = none ? 0.f : log - v.q / (v.n + v.s);
 }
-__device__ __forceinline__ void put_top(const LogpArgs& a, int64_t row, int r, uint64_t key, const Sums& v) {
+__device__ __forceinline__ void put_top(const LogpArgs& a, int64_t row, int r, uint64_t key, const Sums& v, float log) {
   const bool none = v.n == 0.f && v.s == 0.f;
-  a.top[row * a.k + r] = none ? -INFINITY : (value_of(key) - v.m) * a.scale - log_of(v);
+  a.top[row * a.k + r] = none ? -INFINITY : (value_of(key) - v.m) * a.scale - log;
   a.ids[row * a.k + r] = (int32_t)~(uint32_t)key;
 }
 
-// The place of the k-th largest of 64 lanes' values among them (equal ones by their lane): the lane whose rank is k - 1 has it.
-template <class V>
-__device__ __forceinline__ int lane_rank(V v, int lane) {
-  int rank = 0;
-  for (int j = 0; j < 64; ++j) {
-    V o;
-    if constexpr (sizeof(V) == 8) {
-      o = (V)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, j);
-    } else {
-      o = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), j));
-    }
-    rank += o > v || (o == v && j < lane);
+// The k-th largest of 64 lanes' 16-bit numbers, bit by bit.
+__device__ __forceinline__ uint32_t kth_of_lanes(uint32_t v, int k) {
+  uint32_t kth = 0;
+#pragma unroll
+  for (int bit = 15; bit >= 0; --bit) {
+    const uint32_t trial = kth | 1u << bit;
+    if (__popcll(__ballot(v >= trial)) >= k) kth = trial;
   }
-  return rank;
+  return kth;
 }
+// lanes before this one in a mask
+__device__ __forceinline__ int before(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
 
-// eight logits of a row from column c, minus infinity where none is
-template <bool F32>
+// Eight logits of a row, as they lie in memory.
+template <bool F32, bool SHORT>  // SHORT: the row may have fewer than eight
 struct Eight {
   F8Raw8<F32> raw;
   __device__ __forceinline__ void ask(const void* row, int c, int n) {
-    if (n >= 8) {
+    if (!SHORT || n >= 8) {
       raw = f8_raw8<F32>(row, c, n);
     } else {
       float v[8];
       each8<F32>(row, c, n, v);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        if constexpr (F32) raw.v[k >> 2][k & 3] = __float_as_uint(v[k]);
-        else raw.v[0][k >> 1] = (k & 1 ? raw.v[0][k >> 1] & 0xFFFFu : 0u) | (k & 1 ? __float_as_uint(v[k]) & 0xFFFF0000u : __float_as_uint(v[k]) >> 16);
-      }
+      put(v);
     }
   }
-  // end: the chunk's (a multiple of eight, or n)
-  __device__ __forceinline__ void get(int c, int n, int end, float* v) const {
-    const int past = c >= end ? 8 : n >= 8 ? f8_past(c, n) : 0;
-    f8_unpack8<F32>(raw, past, (n & 7) != 0 && n >= 8, v);
-    if (c + 8 > end) {
+  __device__ __forceinline__ void put(const float* v) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = c + k < end ? v[k] : -INFINITY;
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t u = __float_as_uint(v[k]);
+      if constexpr (F32) raw.v[k >> 2][k & 3] = u;
+      else raw.v[0][k >> 1] = k & 1 ? (raw.v[0][k >> 1] & 0xFFFFu) | (u & 0xFFFF0000u) : u >> 16;
     }
+  }
+  // at a row's end, once: into their places, minus infinity from `end` on (the chunk's: a multiple of eight, or n)
+  __device__ __forceinline__ void place(int c, int n, int end) {
+    const int past = c >= end ? 8 : !SHORT || n >= 8 ? f8_past(c, n) : 0;
+    float v[8];
+    f8_unpack8<F32>(raw, past, (n & 7) != 0 && (!SHORT || n >= 8), v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = c + k < end ? v[k] : -INFINITY;
+    put(v);
+  }
+  __device__ __forceinline__ void get(float* v) {
+    // (hidden from the optimiser, which would keep the unpacked values of one pass for the next)
+#pragma unroll
+    for (int k = 0; k < (F32 ? 2 : 1); ++k) asm volatile("" : "+v"(raw.v[k]));
+    f8_unpack8<F32>(raw, 0, false, v);
   }
 };
+__device__ __forceinline__ float most8(const float* v) {
+  return fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+}
 
 // ROWT threads hold a chunk of up to ROWT x NV x 8 logits.
+// An exponent is one fused multiply-add, t = x c - r with r = m c rounded: the sums are then those relative to r, and the exact difference
+// d = m c - r (one fused multiply-add again) brings them to m.  Nothing is done for single elements that a row in a thousand needs: where the sum
+// of t e^t is no number, as minus infinities make it, a wave adds once more with care, and where the sum is near 1, as a sure token
+// makes it, the workgroup adds once more what does not reach the maximum.
 template <bool F32, bool TOP, int ROWT, int NV>
-__global__ __launch_bounds__(ROWT) void logp_rows(LogpArgs a) {
+__global__ __launch_bounds__(ROWT, (F32 || TOP) && NV == 4 ? 4 : 8) void logp_rows(LogpArgs a) {
   constexpr int WAVES = ROWT / 64, LANES = ROWT / 64;  // waves; lanes of one of the 64 groups
-  __shared__ float sh_max[WAVES], sh_sum[WAVES][3];
-  __shared__ float sh_group[TOP ? 64 : 1], sh_least;
-  __shared__ uint32_t sh_count[2];
-  __shared__ uint64_t sh_key[TOP ? kKeys : 1];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int kList = WAVES == 1 ? 256 : WAVES <= 8 ? 128 : kTopMost, kEights = WAVES == 1 ? 96 : kList / 2;  // keys of a wave; eights that may hold some
+  __shared__ float sh_max[WAVES], sh_sum[2][WAVES][3];
+  __shared__ float sh_group[TOP ? 64 : 1], sh_least, sh_log;
+  __shared__ uint32_t sh_count[WAVES], sh_above;
+  __shared__ uint64_t sh_key[TOP ? WAVES : 1][kList];
+  __shared__ F8Raw8<F32> sh_eight[TOP ? WAVES : 1][kEights];
+  __shared__ int sh_column[TOP ? WAVES : 1][kEights];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t group = (int64_t)blockIdx.y * kGridX + blockIdx.x, row = a.chunks == 1 ? group : group / a.chunks;
   if (row >= a.T) return;
   const int chunk = (int)(group - row * a.chunks), begin = chunk * a.chunk, end = begin + a.chunk < a.V ? begin + a.chunk : a.V;
   const void* x = row_of<F32>(a.X, row, a.ld);
-  Eight<F32> in[NV];
+  Eight<F32, ROWT == 64 && NV == 1> in[NV];
 #pragma unroll
   for (int j = 0; j < NV; ++j) in[j].ask(x, begin + (tid + j * ROWT) * 8, a.V);
-  float m = -INFINITY, v[8];
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+    if (begin + (wave * 64 + 63 + j * ROWT) * 8 + 8 > end) in[j].place(begin + (tid + j * ROWT) * 8, a.V, end);
+  // f(the eight values of group j, their first column), group by group: registers are what lets two workgroups share a CU
+  auto each = [&](int j, auto f) {
+    float v[8];
+    in[j].get(v);
+    int c = tid * 8;
+    asm volatile("" : "+v"(c));  // (a place of its own for every column it would keep, too)
+    f(v, c + begin + j * ROWT * 8);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  float m = -INFINITY, most[NV];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    in[j].get(begin + (tid + j * ROWT) * 8, a.V, end, v);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) m = fmaxf(m, v[k]);
+    each(j, [&](const float* v, int) { most[j] = most8(v); });
+    m = fmaxf(m, most[j]);
   }
   if constexpr (TOP) {
     const float g = lanes_max<LANES>(m);
     if (tid % LANES == 0) sh_group[tid / LANES] = g;
-    if (tid < 2) sh_count[tid] = 0;
   }
   m = lanes_max<64>(m);
   if constexpr (WAVES > 1) {
@@ -174,154 +200,238 @@ __global__ __launch_bounds__(ROWT) void logp_rows(LogpArgs a) {
   }
   if constexpr (TOP) {
     if (wave == 0) {
-      const float g = sh_group[lane];
-      if (lane_rank(g, lane) == a.k - 1) sh_least = g;
+      const uint32_t kth = kth_of_lanes((uint32_t)(key_of(sh_group[lane], 0) >> 48), a.k);
+      if (lane == 0) sh_least = kth <= 0x7Fu ? -INFINITY : value_of((uint64_t)kth << 48);
     }
   }
-  // exponentials
-  const float from = m == -INFINITY ? 0.f : m, c2 = a.scale * kLog2e;
+  const float from = m == -INFINITY ? 0.f : m, c2 = a.scale * kLog2e, r = from * c2, d = fmaf(from, c2, -r);
   float s = 0.f, q = 0.f;
-  uint32_t n = 0;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    in[j].get(begin + (tid + j * ROWT) * 8, a.V, end, v);
+  for (int j = 0; j < NV; ++j)
+    each(j, [&](const float* v, int) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      float t = (v[k] - from) * c2;
-      t = t < -200.f ? -200.f : t;  // 2^-200 is 0, and 0 times it too; a NaN stays one
-      const bool most = t == 0.f;
-      n += __popcll(__ballot(most));
-      const float e = most ? 0.f : __builtin_amdgcn_exp2f(t);
-      s += e;
-      q += t * e;
-    }
+      for (int k = 0; k < 8; ++k) {
+        const float t = fmaf(v[k], c2, -r), e = __builtin_amdgcn_exp2f(t);
+        s += e;
+        q = fmaf(t, e, q);
+      }
+    });
+  if (__ballot(q != q)) {
+    q = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      each(j, [&](const float* v, int) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          float t = fmaf(v[k], c2, -r);
+          t = t < -200.f ? -200.f : t;  // 2^-200 is 0, and 0 times it too; a NaN stays one
+          q = fmaf(t, __builtin_amdgcn_exp2f(t), q);
+        }
+      });
   }
-  s = f8_wave_sum(s);
-  q = f8_wave_sum(q);
-  Sums sum{from, (float)n, s, q};
-  if constexpr (WAVES > 1) {
-    if (lane == 0) sh_sum[wave][0] = sum.n, sh_sum[wave][1] = s, sh_sum[wave][2] = q;
+  // the workgroup's sums, in the order of its waves
+  auto total = [&](float (*sh)[3], float n, float s, float q) {
+    s = f8_wave_sum(s);
+    q = f8_wave_sum(q);
+    if constexpr (WAVES == 1) return Sums{from, n, s, q};
+    if (lane == 0) sh[wave][0] = n, sh[wave][1] = s, sh[wave][2] = q;
     __syncthreads();
-    sum = Sums{from, 0.f, 0.f, 0.f};
+    Sums v{from, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) sum.n += sh_sum[w][0], sum.s += sh_sum[w][1], sum.q += sh_sum[w][2];
-  } else if constexpr (TOP) {
-    __syncthreads();
+    for (int w = 0; w < WAVES; ++w) v.n += sh[w][0], v.s += sh[w][1], v.q += sh[w][2];
+    return v;
+  };
+  Sums sum = total(sh_sum[0], 0.f, s, q);
+  if (sum.s < 1.5f || !(fabsf(r) < 1e30f)) {  // (or m c is past what a float holds)
+    uint32_t n = 0;
+    s = q = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      each(j, [&](const float* v, int) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          float t = (v[k] - from) * c2;
+          t = t < -200.f ? -200.f : t;
+          n += __popcll(__ballot(t == 0.f));
+          const float e = t == 0.f ? 0.f : __builtin_amdgcn_exp2f(t);
+          s += e;
+          q = fmaf(t, e, q);
+        }
+      });
+    sum = total(sh_sum[1], (float)n, s, q);
+  } else {
+    const float f = __builtin_amdgcn_exp2f(-d);
+    sum.q = (sum.q - d * sum.s) * f;
+    sum.s *= f;
   }
   sum.q *= kLn2;
   if (m == -INFINITY && sum.s == 0.f) sum = Sums{-INFINITY, 0.f, 0.f, 0.f};
   if (tid == 0) {
-    if (a.chunks == 1) put_row(a, row, sum, F32);
-    else *(f32x4_t*)(a.part + (row * a.chunks + chunk) * 4) = f32x4_t{sum.m, sum.n, sum.s, sum.q};
+    if (a.chunks == 1) {
+      const float log = log_of(sum);
+      if constexpr (TOP) sh_log = log;
+      put_row(a, row, sum, log, F32);
+    } else {
+      *(f32x4_t*)(a.part + (row * a.chunks + chunk) * 4) = f32x4_t{sum.m, sum.n, sum.s, sum.q};
+    }
   }
   if constexpr (TOP) {
+    if constexpr (WAVES == 1) __syncthreads();
     const float least = sh_least;
+    uint32_t mine = 0;  // keys of this wave, which its list may have no room for
+    // A maximum passes over NaN, and minus infinity is what stands past the row: then every group is looked into.  Where fewer than k groups
+    // hold more than minus infinity, its lowest places that can be wanted are among the first k.
+    const bool careful = sum.s != sum.s || least == -INFINITY;
+    auto keep = [&](auto wanted) {
+      mine = 0;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int c = begin + (tid + j * ROWT) * 8;
-      in[j].get(c, a.V, end, v);
+      for (int j = 0; j < NV; ++j) {
+        each(j, [&](const float* v, int c) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (!(v[k] < least) && c + k < end) {
-          const uint32_t at = atomicAdd(&sh_count[0], 1u);
-          if (at < kKeys) sh_key[at] = key_of(v[k], c + k);
-        }
+          for (int k = 0; k < 8; ++k) {
+            const bool is = !(v[k] < least) && wanted(v[k], c + k);
+            const uint64_t those = __ballot(is);
+            if (!those) continue;
+            const uint32_t at = mine + before(those);
+            if (is && at < kList) sh_key[wave][at] = key_of(v[k], c + k);
+            mine += __popcll(those);
+          }
+        });
+      }
+      if (lane == 0) sh_count[wave] = mine;
+      __syncthreads();
+    };
+    int eights = 0;
+    if (!careful) {
+      // Eights with a key among them go to LDS whole, a few of a hundred, and are looked through there, one value a lane: looked
+      // through in their registers, for all lanes' sake, they take four times the instructions.
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const bool is = !(most[j] < least);
+        const uint64_t those = __ballot(is);
+        if (!those) continue;
+        const int at = eights + before(those);
+        if (is && at < kEights) sh_eight[wave][at] = in[j].raw, sh_column[wave][at] = begin + (tid + j * ROWT) * 8;
+        eights += __popcll(those);
+      }
+      __builtin_amdgcn_wave_barrier();  // (a wave's own; its accesses to LDS are in order)
+      for (int i0 = 0; i0 < (eights < kEights ? eights : kEights) * 8; i0 += 64) {
+        const int i = i0 + lane, at = i >> 3 < eights ? i >> 3 : 0;
+        const uint32_t* words = (const uint32_t*)&sh_eight[wave][at];
+        const float v = __uint_as_float(F32 ? words[i & 7] : i & 1 ? words[(i & 7) >> 1] & 0xFFFF0000u : words[(i & 7) >> 1] << 16);
+        const bool is = i >> 3 < eights && !(v < least);
+        const uint64_t those = __ballot(is);
+        const uint32_t to = mine + before(those);
+        if (is && to < kList) sh_key[wave][to] = key_of(v, sh_column[wave][at] + (i & 7));
+        mine += __popcll(those);
+      }
+      if (lane == 0) sh_count[wave] = eights > kEights ? kList + 1 : mine;
+      __syncthreads();
+    } else {
+      keep([&](float v, int c) { return c < end && (v != -INFINITY || c < begin + a.k); });
     }
-    __syncthreads();
-    uint32_t have = sh_count[0];
-    if (have > kKeys) {  // the k-th largest key, from its highest bit down
+    bool over = false;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) over |= sh_count[w] > kList;
+    if (over) {  // the k-th largest key, from its highest bit down
       uint64_t kth = 0;
       for (int bit = 63; bit >= 0; --bit) {
         const uint64_t trial = kth | 1ull << bit;
         uint32_t above = 0;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          const int c = begin + (tid + j * ROWT) * 8;
-          in[j].get(c, a.V, end, v);
+        for (int j = 0; j < NV; ++j)
+          each(j, [&](const float* v, int c) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) above += __popcll(__ballot(c + k < end && key_of(v[k], c + k) >= trial));
-        }
-        __syncthreads();  // the last count has been read
-        if (tid == 0) sh_count[1] = 0;
+            for (int k = 0; k < 8; ++k) above += __popcll(__ballot(c + k < end && key_of(v[k], c + k) >= trial));
+          });
+        __syncthreads();  // the last counts have been read
+        if (tid == 0) sh_above = 0;
         __syncthreads();
-        if (lane == 0) atomicAdd(&sh_count[1], above);
+        if (lane == 0) atomicAdd(&sh_above, above);
         __syncthreads();
-        if (sh_count[1] >= (uint32_t)a.k) kth = trial;
+        if (sh_above >= (uint32_t)a.k) kth = trial;
       }
-      if (tid == 0) sh_count[0] = 0;
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int c = begin + (tid + j * ROWT) * 8;
-        in[j].get(c, a.V, end, v);
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (c + k < end && key_of(v[k], c + k) >= kth) {
-            const uint32_t at = atomicAdd(&sh_count[0], 1u);
-            if (at < kKeys) sh_key[at] = key_of(v[k], c + k);
-          }
-      }
-      __syncthreads();
-      have = sh_count[0];
+      keep([&](float v, int c) { return c < end && key_of(v, c) >= kth; });
     }
-    for (uint32_t i = tid; i < have; i += ROWT) {
-      const uint64_t mine = sh_key[i];
+    const float log = sh_log;
+    uint32_t total = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) total += sh_count[w];
+    auto put = [&](int rank, uint64_t key) {
+      if (rank >= a.k) return;
+      if (a.chunks == 1) put_top(a, row, rank, key, sum, log);
+      else a.keys[(row * a.chunks + chunk) * a.k + rank] = key;
+    };
+    if (total <= 64) {  // as good as always: one wave, a key a lane
+      if (wave == 0) {
+        uint32_t w = 0, i = lane;
+        for (; w + 1 < WAVES && i >= sh_count[w]; ++w) i -= sh_count[w];
+        const uint64_t key = lane < (int)total ? sh_key[w][i] : 0;
+        int rank = 0;
+#pragma unroll 4
+        for (uint32_t j = 0; j < total; ++j)
+          rank += ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)key, j)) > key;
+        if (lane < (int)total) put(rank, key);
+      }
+      mine = 0;
+    }
+    for (uint32_t i = lane; i < mine; i += 64) {
+      const uint64_t key = sh_key[wave][i];
       int rank = 0;
-      for (uint32_t j = 0; j < have; ++j) rank += sh_key[j] > mine;
-      if (rank >= a.k) continue;
-      if (a.chunks == 1) put_top(a, row, rank, mine, sum);
-      else a.keys[(row * a.chunks + chunk) * a.k + rank] = mine;
+      for (int w = 0; w < WAVES; ++w) {
+        const uint32_t n = sh_count[w];
+#pragma unroll 4
+        for (uint32_t j = 0; j < n; ++j) rank += sh_key[w][j] > key;
+      }
+      put(rank, key);
     }
     if (a.chunks > 1)  // a chunk of fewer than k
-      for (int r = have + tid; r < a.k; r += ROWT) a.keys[(row * a.chunks + chunk) * a.k + r] = 0;
+      for (int r = end - begin + tid; r < a.k; r += ROWT) a.keys[(row * a.chunks + chunk) * a.k + r] = 0;
   }
 }
 
-// A row's chunks joined: one wave a row for the sums; for the likeliest a workgroup of four.
+// A row's chunks joined: one wave a row, four rows a workgroup; with TOP one, and LDS for all of the chunks' keys.
 template <bool F32, bool TOP>
-__global__ __launch_bounds__(256) void logp_join(LogpArgs a) {
-  __shared__ float sh[5];
-  __shared__ uint64_t sh_group[TOP ? 64 : 1], sh_least, sh_key[TOP ? kChunksMost * kTopMost : 1];
-  __shared__ uint32_t sh_count;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int64_t group = (int64_t)blockIdx.y * kGridX + blockIdx.x, row = TOP ? group : group * 4 + (tid >> 6);
-  if (row >= a.T) return;  // (whole waves, and with TOP the whole workgroup)
-  Sums sum{};
-  if (!TOP || tid < 64) {
-    f32x4_t v = {-INFINITY, 0.f, 0.f, 0.f};
-    if (lane < a.chunks) v = *(const f32x4_t*)(a.part + (row * a.chunks + lane) * 4);
-    const float m = lanes_max<64>(v[0]), from = m == -INFINITY ? 0.f : m;
-    const float d = v[0] == from ? 0.f : (v[0] - from) * a.scale, e = v[0] == -INFINITY ? 0.f : expf(d);
-    // what reached a lower chunk's maximum is one of the others here
-    const float all = v[1] + v[2], n = d == 0.f ? v[1] : 0.f, s = d == 0.f ? v[2] : e * all, q = d == 0.f ? v[3] : e == 0.f ? e * all : e * (v[3] + d * all);
-    sum = Sums{m, f8_wave_sum(n), f8_wave_sum(s), f8_wave_sum(q)};
-    if (lane == 0) put_row(a, row, sum, F32);
-    if constexpr (TOP) {
-      if (lane == 0) sh[0] = sum.m, sh[1] = sum.n, sh[2] = sum.s, sh[3] = sum.q, sh_count = 0;
-    }
-  }
+__global__ __launch_bounds__(TOP ? 64 : 256) void logp_join(LogpArgs a) {
+  extern __shared__ uint64_t sh_key[];
+  const int lane = threadIdx.x & 63;
+  const int64_t group = (int64_t)blockIdx.y * kGridX + blockIdx.x, row = TOP ? group : group * 4 + (threadIdx.x >> 6);
+  if (row >= a.T) return;  // (whole waves)
+  f32x4_t v = {-INFINITY, 0.f, 0.f, 0.f};
+  if (lane < a.chunks) v = *(const f32x4_t*)(a.part + (row * a.chunks + lane) * 4);
+  const float m = lanes_max<64>(v[0]), from = m == -INFINITY ? 0.f : m;
+  const float d = v[0] == from ? 0.f : (v[0] - from) * a.scale, e = v[0] == -INFINITY ? 0.f : expf(d);
+  // what reached a lower chunk's maximum is one of the others here
+  const float all = v[1] + v[2], n = d == 0.f ? v[1] : 0.f, s = d == 0.f ? v[2] : e * all, q = d == 0.f ? v[3] : e == 0.f ? e * all : e * (v[3] + d * all);
+  const Sums sum{m, f8_wave_sum(n), f8_wave_sum(s), f8_wave_sum(q)};
+  const float log = log_of(sum);
+  if (lane == 0) put_row(a, row, sum, log, F32);
   if constexpr (TOP) {
-    // keys in 64 groups of every 64th
     const uint64_t* keys = a.keys + row * a.chunks * a.k;
     const int total = a.chunks * a.k;
     uint64_t most = 0;
-    if (tid < 64)
-      for (int i = tid; i < total; i += 64) most = most > keys[i] ? most : keys[i];
-    if (tid < 64 && lane_rank(most, lane) == a.k - 1) sh_least = most;
-    __syncthreads();
-    sum = Sums{sh[0], sh[1], sh[2], sh[3]};
-    const uint64_t least = sh_least;
-    for (int i = tid; i < total; i += 256) {
+#pragma unroll 8
+    for (int i = lane; i < total; i += 64) {
       const uint64_t key = keys[i];
-      if (key && key >= least) sh_key[atomicAdd(&sh_count, 1u)] = key;
+      most = most > key ? most : key;
+    }
+    const uint64_t least = (uint64_t)kth_of_lanes((uint32_t)(most >> 48), a.k) << 48;
+    int have = 0;
+#pragma unroll 8
+    for (int i0 = 0; i0 < total; i0 += 64) {
+      const uint64_t key = i0 + lane < total ? keys[i0 + lane] : 0;
+      const bool is = key && key >= least;
+      const uint64_t those = __ballot(is);
+      if (is) sh_key[have + before(those)] = key;
+      have += __popcll(those);
     }
     __syncthreads();
-    const uint32_t have = sh_count;
-    for (uint32_t i = tid; i < have; i += 256) {
+    for (int i = lane; i < have; i += 64) {
       const uint64_t mine = sh_key[i];
       int rank = 0;
-      for (uint32_t j = 0; j < have; ++j) rank += sh_key[j] > mine;
-      if (rank < a.k) put_top(a, row, rank, mine, sum);
+#pragma unroll 4
+      for (int j = 0; j < have; ++j) rank += sh_key[j] > mine;
+      if (rank < a.k) put_top(a, row, rank, mine, sum, log);
     }
   }
 }
@@ -375,12 +485,14 @@ __global__ __launch_bounds__(256) void logp_grad(LogpGradArgs a) {
 
 inline int launched() { return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP; }
 
-// Chunks of a row and their length.
+// Chunks of a row and their length.  Four waves and 8192 logits a chunk leave a CU several workgroups that wait for memory and add up in turn (us, chunks of
+// 8192, 16384 and 32768: 8192 x 32768 bf16 106, 115, 127, with the 20 likeliest 157, 171, 274; 2048 x 131072 with them 142, 158, 268);
+// shorter ones where rows are too few for the chip.
 struct Cut {
   int chunk, chunks;
 };
 Cut cut_of(int T, int V) {
-  int most = 32768;
+  int most = 8192;
   while (most > 2048 && (int64_t)T * ((V + most - 1) / most) < 512) most /= 2;
   while ((V + most - 1) / most > kChunksMost) most *= 2;
   const int chunks = (V + most - 1) / most;
@@ -400,7 +512,8 @@ int rows(const LogpArgs& a, hipStream_t st) {
   else hipLaunchKernelGGL((logp_rows<F32, TOP, 1024, 4>), grid, dim3(1024), 0, st, a);
   if (launched() != BSP_OK) return BSP_ERR_HIP;
   if (a.chunks == 1) return BSP_OK;
-  hipLaunchKernelGGL((logp_join<F32, TOP>), f8_grid(TOP ? (int64_t)a.T : ((int64_t)a.T + 3) / 4), dim3(256), 0, st, a);
+  if (TOP) hipLaunchKernelGGL((logp_join<F32, TOP>), f8_grid(a.T), dim3(64), (size_t)a.chunks * a.k * 8, st, a);
+  else hipLaunchKernelGGL((logp_join<F32, TOP>), f8_grid(((int64_t)a.T + 3) / 4), dim3(256), 0, st, a);
   return launched();
 }
 
