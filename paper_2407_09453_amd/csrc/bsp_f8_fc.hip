@@ -125,58 +125,52 @@ __device__ __forceinline__ void store_tile(const F8Epilogue& q, f32x16_t (&acc)[
 }
 
 // The rows' adapters: B_a u_t added to a wave's sums, one adapter of its rows after the other.  The rows are the matrix instruction's columns, so a
-// lane holds results of one row, and keeps or drops what an adapter adds to it as that is the row's own or another's: nothing of
-// another adapter's, NaN among it, gets there.  u enters as two bf16 parts.
+// lane holds results of one row, and takes or leaves what an adapter adds as that is the row's own or another's: nothing of
+// another adapter's, NaN among it, gets there.  u enters as two bf16 parts.  The products start from zero and are added with
+// ordinary instructions, 32 channels at a time: kept beside a copy of the sums they would not fit in registers (380 of them in memory).
+struct LowParts {
+  u32x4_t high, rest;
+};
+__device__ __forceinline__ LowParts low_parts(const float* u) {
+  const f32x4_t x0 = *(const f32x4_t*)u, x1 = *(const f32x4_t*)(u + 4);
+  LowParts p;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float a0 = (e < 2 ? x0 : x1)[2 * (e & 1)], a1 = (e < 2 ? x0 : x1)[2 * (e & 1) + 1];
+    p.high[e] = f8_pack_bf16x2(a0, a1);
+    p.rest[e] = f8_pack_bf16x2(a0 - __uint_as_float(p.high[e] << 16), a1 - __uint_as_float(p.high[e] & 0xFFFF0000u));
+  }
+  return p;
+}
 template <int MO, int MT>
 __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT], int T, int64_t t0, int o0) {
   const int lane = threadIdx.x & 63;
-  int of[MT];
-  const float* u[MT];
+  const uint16_t* up = low.up + (int64_t)(o0 + (lane & 31)) * low.rank + (lane >> 5) * 8;
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    const int64_t t = t0 + m * 32 + (lane & 31);
-    of[m] = t < T ? low.which[t] : -1;
-    u[m] = low.u + (t < T ? t : T - 1) * low.rank + (lane >> 5) * 8;
-  }
-  uint64_t todo[MT];
-#pragma unroll
-  for (int m = 0; m < MT; ++m) todo[m] = __ballot(of[m] >= 0);
-  for (;;) {
-    int now = -1;
-#pragma unroll
-    for (int m = MT - 1; m >= 0; --m)
-      if (todo[m]) now = __builtin_amdgcn_readlane(of[m], __builtin_ctzll(todo[m]));
-    if (now < 0) break;
-    const uint16_t* b = low.up + now * low.step + (int64_t)(o0 + (lane & 31)) * low.rank + (lane >> 5) * 8;
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      const bool mine = of[m] == now;
-      const uint64_t those = __ballot(mine);
-      if (!those) continue;
-      todo[m] &= ~those;
-      f32x16_t sum[MO];
-#pragma unroll
-      for (int o = 0; o < MO; ++o) sum[o] = acc[o][m];
+    const int64_t t = t0 + m * 32 + (lane & 31) < T ? t0 + m * 32 + (lane & 31) : T - 1;
+    const float* u = low.u + t * low.rank + (lane >> 5) * 8;
+    const int of = low.which[t];
+    uint64_t todo = __ballot(of >= 0);
+    while (todo) {
+      const int now = __builtin_amdgcn_readlane(of, __builtin_ctzll(todo));
+      const bool mine = of == now;
+      todo &= ~__ballot(mine);
+      const uint16_t* b = up + now * low.step;
       for (int k = 0; k < low.rank; k += 16) {
-        const f32x4_t x0 = *(const f32x4_t*)(u[m] + k), x1 = *(const f32x4_t*)(u[m] + k + 4);
-        u32x4_t high, rest;
+        const LowParts p = low_parts(u + k);
+        u32x4_t w[MO];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float a0 = (e < 2 ? x0 : x1)[2 * (e & 1)], a1 = (e < 2 ? x0 : x1)[2 * (e & 1) + 1];
-          high[e] = f8_pack_bf16x2(a0, a1);
-          rest[e] = f8_pack_bf16x2(a0 - __uint_as_float(high[e] << 16), a1 - __uint_as_float(high[e] & 0xFFFF0000u));
-        }
+        for (int o = 0; o < MO; ++o) w[o] = *(const u32x4_t*)(b + (int64_t)o * 32 * low.rank + k);
 #pragma unroll
         for (int o = 0; o < MO; ++o) {
-          const u32x4_t w = *(const u32x4_t*)(b + (int64_t)o * 32 * low.rank + k);
-          sum[o] = mfma_bf16_32x32x16(w, high, sum[o]);
-          sum[o] = mfma_bf16_32x32x16(w, rest, sum[o]);
+          f32x16_t sum = mfma_bf16_32x32x16(w[o], p.high, f32x16_t{});
+          sum = mfma_bf16_32x32x16(w[o], p.rest, sum);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[o][m][e] += mine ? sum[e] : 0.f;
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
-#pragma unroll
-      for (int o = 0; o < MO; ++o)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[o][m][e] = mine ? sum[o][e] : acc[o][m][e];
     }
   }
 }
