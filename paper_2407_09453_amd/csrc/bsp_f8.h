@@ -282,10 +282,11 @@ struct F8Input {      // rows to multiply: codes with their scales, or values br
   int32_t e5;         // the codes are e5m2
   int64_t ld;         // elements from row to row
 };
-// The rows of a batch by their adapters, as adapt_plan leaves them: adapter a has rows order[start[a]] .. order[start[a + 1] - 1].
+// The rows of a batch by their adapters, as adapt_plan leaves them: adapter a has rows order[start[a]] .. order[start[a + 1] - 1], those behind
+// have none.
 struct F8Requests {
   int32_t *start, *which, *order;  // [N + 1], [T] (-1: none), [T]
-  int32_t* tiles;                  // how many tiles of sixteen rows; then for each its adapter and its first row's place among that one's
+  int32_t* tiles;                  // how many tiles have an adapter, how many there are, two words; then the tiles' records
 };
 struct F8Adapters {  // bf16, ranks padded to Rp with zeros, columns to whole blocks
   uint16_t *a, *a_t, *b, *b_t;  // [N][Rp][Ip], [N][Ip][Rp], [N][Op][Rp], [N][Rp][Op]
@@ -295,10 +296,11 @@ struct F8Adapters {  // bf16, ranks padded to Rp with zeros, columns to whole bl
 // What is added to a product: B_a u_t for the adapter of row t.
 struct F8Low {
   const int32_t* which;
-  const float* u;        // [T][rank]
+  const float* u;        // [slices][T][rank]: u_t is the sum of the slices'
   const uint16_t* up;    // [N][128 ceil(out / 128)][rank]
-  int64_t step;          // elements of an adapter
+  int64_t step, u_step;  // elements of an adapter, of a slice
   int32_t rank;          // 0: nothing is added
+  int32_t slices;
 };
 // Few rows: the contraction split over a workgroup's waves.  Rows given as values become codes in each workgroup's LDS, T <= 16 of them and
 // no more than kFewStaged bytes.
@@ -327,14 +329,16 @@ struct F8GradArgs {
 };
 int f8_grad_split(int64_t nnzb, int T);              // into how many ranges of rows the sums are cut
 int f8_launch_grad(const F8GradArgs& a, hipStream_t st);
-// adapters: which rows are whose, an adapter's weights, u = s A x ([T][Rp] fp32, rows without an adapter left as they were), gradients
+// adapters: which rows are whose, an adapter's weights, u = s A x ([slices][T][Rp] fp32, rows without an adapter left as they were), gradients
 int64_t f8_request_tiles(int T, int N);  // at most so many
 int64_t f8_requests_bytes(int T, int N);
 F8Requests f8_requests_of(const bsp_f8_requests* r);
 F8Adapters f8_adapters_of(const bsp_f8_adapters* d);
 int f8_launch_plan(const bsp_f8_requests* r, const void* which, bool wide, hipStream_t st);
 int f8_launch_set(const F8Adapters& d, int slot, int rank, const void* A, int64_t lda, const void* B, int64_t ldb, bool f32, float scale, hipStream_t st);
-int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, hipStream_t st);
+int f8_down_slices(int T, int N, int K);
+// codes, scale: where values are to become codes (of x.e5) on the way, too; or null
+int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, uint8_t* codes, uint8_t* scale, hipStream_t st);
 int64_t f8_adapt_part_bytes(const F8Adapters& d, int T);
 int f8_launch_adapt_grad(const F8Adapters& d, const uint16_t* dY, int64_t ldy, const F8Input& x, int T, const F8Requests& q, const float* u, const float* v,
                          float* part, float* dA, float* dB, hipStream_t st);

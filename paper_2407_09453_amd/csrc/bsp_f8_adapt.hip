@@ -1,6 +1,6 @@
 // Low-rank adapters of many requests beside an 8-bit layer: y_t += s_a B_a (A_a x_t) for the adapter a of row t, and their gradients.
 //
-//   down:  u_t = s_a A_a x_t                     here, on rows sorted by adapter, sixteen of one adapter to a workgroup
+//   down:  u_t = s_a A_a x_t                     here, on rows sorted by adapter, up to 64 of one adapter to a workgroup
 //   up:    y_t += B_a u_t                        in the products' own kernels, before their epilogue: one rounding for the whole result
 //   grad:  dB_a = sum_t dy_t u_t^t, dA_a = sum_t v_t x_t^t with v_t = s_a B_a^t dy_t (down, transposed)
 //
@@ -15,27 +15,33 @@
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+constexpr int kTileRows = 64, kTileWords = 4 + kTileRows;  // a tile's record: adapter (-1: none), rows, two words, the rows' numbers (past the last: its)
 
 inline int launched() { return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP; }
 
 // ------------------------------------------------------------------ which rows are whose
-// Rows sorted by adapter, in their order within each (counted, not compared: one workgroup of sixteen waves, each with a range of the rows).
-// Ids that are no adapter's become -1 and have no place in the order.
+// Rows sorted by adapter, in their order within each, those of none last (counted, not compared: one workgroup of sixteen waves, each with a range
+// of the rows).  Ids that are no adapter's become -1.  Tiles of up to 64 rows of one adapter hold their rows' numbers themselves, so
+// that a kernel that works on one finds all it needs with one load.
 template <class Id>
 __global__ __launch_bounds__(1024) void adapt_plan(const Id* ids, int T, int N, F8Requests q) {
   extern __shared__ int32_t hist[];  // [16][N], behind them the tiles' first numbers [N + 1]
-  __shared__ int32_t sh[2][16];
+  __shared__ int32_t sh[3][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int32_t* first_tile = hist + 16 * N;
   for (int i = tid; i < 16 * N; i += 1024) hist[i] = 0;
   __syncthreads();
-  const int64_t per = ((int64_t)T + 1023) / 1024 * 64, begin = wave * per, end = begin + per < T ? begin + per : T;
-  for (int64_t t = begin + lane; t < end; t += 64) {
-    const Id id = ids[t];
+  const int64_t per = ((int64_t)T + 1023) / 1024 * 64, begin = wave * per < T ? wave * per : T, end = begin + per < T ? begin + per : T;
+  int with = 0;  // this wave's rows that have an adapter
+  for (int64_t t0 = begin; t0 < end; t0 += 64) {
+    const int64_t t = t0 + lane;
+    const Id id = t < end ? ids[t] : -1;
     const int32_t a = id >= 0 && id < N ? (int32_t)id : -1;
-    q.which[t] = a;
+    if (t < end) q.which[t] = a;
     if (a >= 0) atomicAdd(&hist[wave * N + a], 1);  // (a count: the same in any order)
+    with += __popcll(__ballot(a >= 0));
   }
+  if (lane == 0) sh[2][wave] = with;
   __syncthreads();
   // N <= 1024: an adapter a thread
   int total = 0;
@@ -45,7 +51,7 @@ __global__ __launch_bounds__(1024) void adapt_plan(const Id* ids, int T, int N, 
       hist[w * N + tid] = total;
       total += n;
     }
-  int rows = total, tiles = (total + 15) >> 4;  // sums up to and with this thread's
+  int rows = total, tiles = (total + kTileRows - 1) / kTileRows;  // sums up to and with this thread's
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
     const int r = __shfl_up(rows, d), s = __shfl_up(tiles, d);
@@ -53,30 +59,21 @@ __global__ __launch_bounds__(1024) void adapt_plan(const Id* ids, int T, int N, 
   }
   if (lane == 63) sh[0][wave] = rows, sh[1][wave] = tiles;
   __syncthreads();
-  int all_tiles = 0;
+  int all_rows = 0, all_tiles = 0, none_at = 0;  // none_at: this wave's first row without an adapter, among all such
   for (int w = 0; w < 16; ++w) {
-    if (w < wave) rows += sh[0][w], tiles += sh[1][w];
-    all_tiles += sh[1][w];
+    if (w < wave) rows += sh[0][w], tiles += sh[1][w], none_at -= sh[2][w];
+    all_rows += sh[0][w], all_tiles += sh[1][w];
   }
+  none_at += all_rows + (int)begin;
   if (tid < N) {
     const int start = rows - total;
     for (int w = 0; w < 16; ++w) hist[w * N + tid] += start;
     q.start[tid] = start;
-    first_tile[tid] = tiles - ((total + 15) >> 4);
-    if (tid == N - 1) q.start[N] = rows, first_tile[N] = tiles;
+    first_tile[tid] = tiles - (total + kTileRows - 1) / kTileRows;
   }
-  if (tid == 0) q.tiles[0] = all_tiles;
+  const int none_tiles = (T - all_rows + kTileRows - 1) / kTileRows;
+  if (tid == 0) q.start[N] = all_rows, first_tile[N] = all_tiles, q.tiles[0] = all_tiles, q.tiles[1] = all_tiles + none_tiles;
   __syncthreads();
-  for (int i = tid; i < all_tiles; i += 1024) {  // the last adapter whose first tile is at most i and that has one
-    int lo = 0, hi = N;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (first_tile[mid] <= i) lo = mid;
-      else hi = mid;
-    }
-    q.tiles[1 + 2 * i] = lo;
-    q.tiles[2 + 2 * i] = (i - first_tile[lo]) * 16;  // its first row's place among the adapter's
-  }
   for (int64_t t0 = begin; t0 < end; t0 += 64) {
     const int64_t t = t0 + lane;
     const int a = t < end ? q.which[t] : -1;
@@ -91,6 +88,27 @@ __global__ __launch_bounds__(1024) void adapt_plan(const Id* ids, int T, int N, 
       __builtin_amdgcn_wave_barrier();
       todo &= ~same;
     }
+    const uint64_t none = __ballot(a < 0 && t < end);
+    if (a < 0 && t < end) q.order[none_at + __popcll(none & ((1ull << lane) - 1))] = (int32_t)t;
+    none_at += __popcll(none);
+  }
+  __syncthreads();
+  for (int64_t i = tid; i < (int64_t)(all_tiles + none_tiles) * kTileRows; i += 1024) {
+    const int tile = (int)(i / kTileRows), r = (int)(i % kTileRows);
+    int of = N;  // the last adapter whose first tile is at most this one: none's tiles come behind all
+    if (tile < all_tiles) {
+      int lo = 0, hi = N;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first_tile[mid] <= tile) lo = mid;
+        else hi = mid;
+      }
+      of = lo;
+    }
+    const int from = q.start[of] + (tile - first_tile[of]) * kTileRows, left = (of < N ? q.start[of + 1] : T) - from;
+    int32_t* record = q.tiles + 4 + (int64_t)tile * kTileWords;
+    record[4 + r] = q.order[from + (r < left ? r : left - 1)];
+    if (r == 0) record[0] = of < N ? of : -1, record[1] = left < kTileRows ? left : kTileRows;
   }
 }
 
@@ -124,116 +142,204 @@ struct DownArgs {
   int64_t ld, srows;
   const uint16_t* down;  // [N][Rp][Kp]
   const float* factor;   // [N]
-  float* u;              // [T][Rp]
+  float* u;              // [slices][T][Rp]
   F8Requests q;
-  int32_t K, Kp;
+  int32_t T, K, Kp, Rp, per;  // per: blocks of a slice
+  int32_t e5;
+  uint8_t *codes, *to_scale;  // SAVE: the rows as codes, too
 };
 
 __device__ __forceinline__ u32x4_t pack8(const float* v) {
   return u32x4_t{f8_pack_bf16x2(v[0], v[1]), f8_pack_bf16x2(v[2], v[3]), f8_pack_bf16x2(v[4], v[5]), f8_pack_bf16x2(v[6], v[7])};
 }
-// what eight values lose as bf16, itself as bf16
-__device__ __forceinline__ u32x4_t rest8(const float* v, u32x4_t high) {
-  float r[8];
+__device__ __forceinline__ void unpack8(u32x4_t w, float* v) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    r[2 * k] = v[2 * k] - __uint_as_float(high[k] << 16);
-    r[2 * k + 1] = v[2 * k + 1] - __uint_as_float(high[k] & 0xFFFF0000u);
+    v[2 * k] = __uint_as_float(w[k] << 16);
+    v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
   }
+}
+// what eight values lose as bf16, itself as bf16
+__device__ __forceinline__ u32x4_t rest8(const float* v, u32x4_t high) {
+  float r[8], h[8];
+  unpack8(high, h);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) r[k] = v[k] - h[k];
   return pack8(r);
 }
 
-// A workgroup takes sixteen rows of one adapter, its waves share out the blocks of 128 columns.  In a block a lane reads columns
-// 64 q + 16 g + 8 h + 0..7 of its row and of its rank: 16 bytes of a row of codes at a time.  The ranks are the matrix instruction's rows and
-// the rows its columns, so nothing of one row, NaN among it, reaches another's sums.
-template <int SRC, int NR>
-__global__ __launch_bounds__(1024) void adapt_down(DownArgs a) {
-  extern __shared__ float sums[];  // [waves][NR][64][4]
+// The wait between a matrix instruction and the first use of its result, by hand: the branches over fragments that are not there are ways
+// that meet again, and the compiler counts the instructions of one of them.
+template <int NR, int M>
+__device__ __forceinline__ void settle(f32x4_t (&acc)[NR][M]) {
+  asm volatile("s_nop 15\n\ts_nop 7" : "+v"(acc[0][0]));
+#pragma unroll
+  for (int i = 0; i < NR; ++i)
+#pragma unroll
+    for (int m = 0; m < M; ++m) asm volatile("" : "+v"(acc[i][m]));
+}
+
+// A workgroup takes a tile's rows (of fp32 half of them) and a slice of the blocks of 128 columns, which its waves share out; the slices' sums are
+// added by who reads u.  In a block a lane reads columns 64 q + 16 g + 8 h + 0..7 of its row and of its rank: 16 bytes of a row of
+// codes at a time.  The ranks are the matrix instruction's rows and the rows its columns, so nothing of one row, NaN among it,
+// reaches another's sums.  SAVE: the rows become codes on the way, as f8_save makes them, rows without an adapter too: four lanes
+// hold a row's 128 columns.  (64 rows, for an adapter's columns are read again for every tile.)
+template <int SRC>
+constexpr int kFragments = SRC == kF32 ? 2 : 4;  // of sixteen rows
+
+template <int SRC, int NR, bool SAVE>
+__global__ __launch_bounds__(512) void adapt_down(DownArgs a) {
+  extern __shared__ float sums[];  // [waves][NR][M][64][4]
   constexpr bool kCoded = SRC == kE4 || SRC == kE5;
+  constexpr int M = kFragments<SRC>, kHalves = 4 / M;
+  kernarg_touch<DownArgs>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int r = lane & 15, g = lane >> 4;
-  if ((int)blockIdx.x >= a.q.tiles[0]) return;
-  const int of = a.q.tiles[1 + 2 * blockIdx.x], from = a.q.tiles[2 + 2 * blockIdx.x];
-  const int begin = a.q.start[of] + from, left = a.q.start[of + 1] - begin;  // rows from this tile's first on
-  const int64_t t = a.q.order[begin + (r < left ? r : left - 1)];
-  const uint16_t* w = a.down + ((int64_t)of * 16 * NR + r) * a.Kp + 16 * g;
-  const void* x = kCoded ? (const void*)((const uint8_t*)a.X + t * a.ld) : row_of<SRC == kF32>(a.X, t, a.ld);
-  const int nb = a.Kp >> 7;
-  f32x4_t acc[NR] = {};
-  for (int kb = wave; kb < nb; kb += waves) {
-    u32x4_t wv[NR][4], xv[4], xl[SRC == kF32 ? 4 : 1];
+  const int tile = blockIdx.x / kHalves, half = blockIdx.x % kHalves;
+  const int32_t* record = a.q.tiles + 4 + (int64_t)tile * kTileWords;
+  int64_t t[M];
 #pragma unroll
-    for (int n = 0; n < NR; ++n)
+  for (int m = 0; m < M; ++m) t[m] = record[4 + (half * M + m) * 16 + r];
+  const int of = __builtin_amdgcn_readfirstlane(record[0]), n = __builtin_amdgcn_readfirstlane(record[1]) - half * M * 16;
+  const bool saves = SAVE && blockIdx.z == 0;
+  if (tile >= a.q.tiles[saves ? 1 : 0] || n <= 0) return;
+  const int frags = (n + 15) >> 4;
+  const uint16_t* w = a.down + (((int64_t)(of < 0 ? 0 : of) * a.Rp + blockIdx.z * 16 * NR + r) * a.Kp + 16 * g);
+  const int nb = a.Kp >> 7, kb0 = blockIdx.y * a.per, kb1 = kb0 + a.per < nb ? kb0 + a.per : nb;
+  f32x4_t acc[NR][M] = {};
+  for (int kb = kb0 + wave; kb < kb1; kb += waves) {
+    const bool whole = kb * 128 + 128 <= a.K;
+    u32x4_t wv[NR][4], xv[M][4];
+    float xf[SRC == kF32 ? M : 1][4][8];
+    int s[M];
+    if (of >= 0)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) wv[n][j] = *(const u32x4_t*)(w + (int64_t)n * 16 * a.Kp + kb * 128 + (j >> 1) * 64 + (j & 1) * 8);
-    if constexpr (kCoded) {
-      const float s = __uint_as_float((uint32_t)a.scale[kb * a.srows + t] << 23);
+      for (int i = 0; i < NR; ++i)
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const u32x4_t c = *(const u32x4_t*)((const uint8_t*)x + kb * 128 + q * 64 + g * 16);
-        xv[2 * q] = f8_decode_bf16x8<SRC == kE5>(c.x, c.y, s);
-        xv[2 * q + 1] = f8_decode_bf16x8<SRC == kE5>(c.z, c.w, s);
-      }
-    } else {
+        for (int j = 0; j < 4; ++j) wv[i][j] = *(const u32x4_t*)(w + (int64_t)i * 16 * a.Kp + kb * 128 + (j >> 1) * 64 + (j & 1) * 8);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int c = kb * 128 + (j >> 1) * 64 + 16 * g + (j & 1) * 8;
-        if constexpr (SRC == kBf16) {
-          if (kb * 128 + 128 <= a.K) {
-            xv[j] = *(const f8_any2_t*)((const uint16_t*)x + c);
+    for (int m = 0; m < M; ++m) {
+      if (m >= frags) break;
+      if constexpr (kCoded) {
+        const uint8_t* x = (const uint8_t*)a.X + t[m] * a.ld + kb * 128 + g * 16;
+        s[m] = a.scale[kb * a.srows + t[m]];
+        xv[m][0] = *(const u32x4_t*)x;
+        xv[m][2] = *(const u32x4_t*)(x + 64);
+      } else {
+        const void* x = row_of<SRC == kF32>(a.X, t[m], a.ld);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int c = kb * 128 + (j >> 1) * 64 + 16 * g + (j & 1) * 8;
+          if constexpr (SRC == kBf16) {
+            if (whole) {
+              xv[m][j] = *(const f8_any2_t*)((const uint16_t*)x + c);
+            } else {
+              float v[8];
+              load8<false>(x, c, a.K, v);
+              xv[m][j] = pack8(v);
+            }
           } else {
-            float v[8];
-            load8<false>(x, c, a.K, v);
-            xv[j] = pack8(v);
+            load8<true>(x, c, a.K, xf[m][j]);
           }
-        } else {
-          float v[8];
-          load8<true>(x, c, a.K, v);
-          xv[j] = pack8(v);
-          xl[j] = rest8(v, xv[j]);
         }
       }
     }
 #pragma unroll
-    for (int n = 0; n < NR; ++n)
+    for (int m = 0; m < M; ++m) {
+      if (m >= frags) break;
+      u32x4_t xl[SRC == kF32 ? 4 : 1];
+      if constexpr (kCoded) {
+        const float f = __uint_as_float((uint32_t)s[m] << 23);
+        const u32x4_t c0 = xv[m][0], c1 = xv[m][2];
+        xv[m][0] = f8_decode_bf16x8<SRC == kE5>(c0.x, c0.y, f);
+        xv[m][1] = f8_decode_bf16x8<SRC == kE5>(c0.z, c0.w, f);
+        xv[m][2] = f8_decode_bf16x8<SRC == kE5>(c1.x, c1.y, f);
+        xv[m][3] = f8_decode_bf16x8<SRC == kE5>(c1.z, c1.w, f);
+      } else if constexpr (SRC == kF32) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        acc[n] = mfma_bf16_16x16x32(wv[n][j], xv[j], acc[n]);
-        if constexpr (SRC == kF32) acc[n] = mfma_bf16_16x16x32(wv[n][j], xl[j], acc[n]);
+        for (int j = 0; j < 4; ++j) {
+          xv[m][j] = pack8(xf[m][j]);
+          xl[j] = rest8(xf[m][j], xv[m][j]);
+        }
       }
-  }
+      if (of >= 0)
 #pragma unroll
-  for (int n = 0; n < NR; ++n) *(f32x4_t*)(sums + ((wave * NR + n) * 64 + lane) * 4) = acc[n];
+        for (int i = 0; i < NR; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            acc[i][m] = mfma_bf16_16x16x32(wv[i][j], xv[m][j], acc[i][m]);
+            if constexpr (SRC == kF32) acc[i][m] = mfma_bf16_16x16x32(wv[i][j], xl[j], acc[i][m]);
+          }
+      if constexpr (SAVE) {
+        if (saves) {
+          float v[4][8];
+          uint32_t most = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if constexpr (SRC == kBf16) unpack8(xv[m][j], v[j]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              if constexpr (SRC == kF32) v[j][k] = xf[m][j][k];
+              most = max(most, f8_magnitude(v[j][k]));
+            }
+          }
+          const auto p = __builtin_amdgcn_permlane16_swap(most, most, false, false);
+          most = max(p[0], p[1]);
+          const auto o = __builtin_amdgcn_permlane32_swap(most, most, false, false);
+          most = max(o[0], o[1]);
+          const int b = a.e5 ? f8_scale_byte<true>(most) : f8_scale_byte<false>(most);
+          const float f = f8_inverse(b);
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            u32x4_t c;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float* y = &v[2 * q + (k >> 1)][4 * (k & 1)];
+              c[k] = a.e5 ? f8_encode4<true>(y[0] * f, y[1] * f, y[2] * f, y[3] * f) : f8_encode4<false>(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
+            }
+            if (m * 16 + r < n) *(u32x4_t*)(a.codes + t[m] * a.Kp + kb * 128 + q * 64 + g * 16) = c;
+          }
+          if (g == 0 && m * 16 + r < n) a.to_scale[kb * a.srows + t[m]] = (uint8_t)b;
+        }
+      }
+    }
+  }
+  if (of < 0) return;
+  settle(acc);
+#pragma unroll
+  for (int i = 0; i < NR; ++i)
+#pragma unroll
+    for (int m = 0; m < M; ++m) *(f32x4_t*)(sums + (((wave * NR + i) * M + m) * 64 + lane) * 4) = acc[i][m];
   __syncthreads();
-  for (int i = threadIdx.x; i < NR * 64; i += blockDim.x) {
-    f32x4_t s = *(const f32x4_t*)(sums + i * 4);
-    for (int v = 1; v < waves; ++v) s += *(const f32x4_t*)(sums + (v * NR * 64 + i) * 4);
-    const int row = i & 15;
-    if (row < left) *(f32x4_t*)(a.u + (int64_t)a.q.order[begin + row] * (16 * NR) + (i >> 6) * 16 + ((i >> 4) & 3) * 4) = s * a.factor[of];
+  const float factor = a.factor[of];
+  for (int i = threadIdx.x; i < NR * M * 64; i += blockDim.x) {
+    const int row = ((i >> 6) % M) * 16 + (i & 15);
+    if (row >= n) continue;
+    f32x4_t sum = *(const f32x4_t*)(sums + i * 4);
+    for (int v = 1; v < waves; ++v) sum += *(const f32x4_t*)(sums + (v * NR * M * 64 + i) * 4);
+    const int64_t at = (int64_t)blockIdx.y * a.T + record[4 + half * M * 16 + row];
+    *(f32x4_t*)(a.u + at * a.Rp + (blockIdx.z * NR + i / (M * 64)) * 16 + ((i >> 4) & 3) * 4) = sum * factor;
   }
 }
 
-template <int SRC, int NR>
-int down_launch(const DownArgs& a, int T, int N, hipStream_t st) {
-  const int64_t tiles = f8_request_tiles(T, N);
-  const int nb = a.Kp >> 7;
-  constexpr int most = NR > 4 ? 8 : 16;
-  // a wave a block of columns, as many as a workgroup holds where there are few workgroups
-  int waves = tiles >= 512 ? 4 : most;
-  while (waves > 1 && waves > nb) waves >>= 1;
-  if (tiles > INT32_MAX / 2048) return BSP_ERR_SHAPE;
-  static const bool raised = hipFuncSetAttribute((const void*)&adapt_down<SRC, NR>, hipFuncAttributeMaxDynamicSharedMemorySize, most * NR * 1024) == hipSuccess;
+template <int SRC, int NR, bool SAVE>
+int down_launch(const DownArgs& a, int T, int N, int slices, hipStream_t st) {
+  constexpr int M = kFragments<SRC>, most = NR == 4 ? 4 : 8;
+  const int64_t tiles = f8_request_tiles(T, N) * (4 / M);
+  int waves = most;  // a wave a block of columns at least
+  while (waves > 1 && waves > a.per) waves >>= 1;
+  if (!f8_fits_x(tiles, 512)) return BSP_ERR_SHAPE;
+  static const bool raised = hipFuncSetAttribute((const void*)&adapt_down<SRC, NR, SAVE>, hipFuncAttributeMaxDynamicSharedMemorySize, most * NR * M * 1024) == hipSuccess;
   if (!raised) return BSP_ERR_HIP;
-  hipLaunchKernelGGL((adapt_down<SRC, NR>), dim3((unsigned)tiles), dim3(64 * waves), (size_t)waves * NR * 1024, st, a);
+  hipLaunchKernelGGL((adapt_down<SRC, NR, SAVE>), dim3((unsigned)tiles, (unsigned)slices, (unsigned)(a.Rp / (16 * NR))), dim3(64 * waves), (size_t)waves * NR * M * 1024, st, a);
   return launched();
 }
-template <int SRC>
-int down_rank(const DownArgs& a, int T, int N, int Rp, hipStream_t st) {
-  switch (Rp) {
-    case 16: return down_launch<SRC, 1>(a, T, N, st);
-    case 32: return down_launch<SRC, 2>(a, T, N, st);
-    case 64: return down_launch<SRC, 4>(a, T, N, st);
-    default: return down_launch<SRC, 8>(a, T, N, st);
+template <int SRC, bool SAVE>
+int down_rank(const DownArgs& a, int T, int N, int slices, hipStream_t st) {
+  switch (a.Rp) {
+    case 16: return down_launch<SRC, 1, SAVE>(a, T, N, slices, st);
+    case 32: return down_launch<SRC, 2, SAVE>(a, T, N, slices, st);
+    default: return down_launch<SRC, 4, SAVE>(a, T, N, slices, st);  // (128: in two halves)
   }
 }
 
@@ -246,7 +352,9 @@ struct GradArgs {
   const void* X;          // bf16 [T][I], or codes
   const uint8_t* scale;
   int64_t ldy, ldx, srows;
-  const float *u, *v;     // [T][Rp]
+  const float *u, *v;     // [slices][T][Rp]
+  int64_t u_step;         // T Rp
+  int32_t u_slices, v_slices, Rp;
   float *dA, *dB;         // [N][R][I], [N][O][R]
   float* part;            // [slots][R I + O R]
   int32_t N, R, I, O, blocks_o, chunk;
@@ -296,8 +404,8 @@ __device__ __forceinline__ f32x16_t mfma32(u32x4_t a, u32x4_t b, f32x16_t c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 
-// A workgroup: 128 columns of dY (dB) or of X (dA), and a chunk of an adapter's rows.  Four waves of 32 columns each; the other operand is u or v,
-// its high parts beside its low parts in a row of 2 RP bf16.
+// A workgroup: 128 columns of dY (dB) or of X (dA), a chunk of an adapter's rows, and RP ranks.  Four waves of 32 columns each; the other operand
+// is u or v, its high parts beside its low parts in a row of 2 RP bf16.
 template <int RP>
 __global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
   constexpr int NT = RP / 16;               // tiles of 32 columns of u: high parts, then low
@@ -312,7 +420,8 @@ __global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
   const int src = in_y ? (int)kBf16 : a.src;
   const void* P = in_y ? (const void*)a.dY : a.X;
   const int64_t ld = in_y ? a.ldy : a.ldx;
-  const float* Q = in_y ? a.u : a.v;
+  const int r0 = blockIdx.z * RP, slices = in_y ? a.u_slices : a.v_slices;
+  const float* Q = (in_y ? a.u : a.v) + r0;
   const bool whole = c0 + 128 <= columns;
   // what this thread brings: sixteen columns of a row, and kMine values of u
   const int row = tid >> 3, piece = tid & 7;
@@ -340,7 +449,10 @@ __global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
       s = a.scale[kb * a.srows + t];
     }
 #pragma unroll
-    for (int e = 0; e < kMine; ++e) u[e] = Q[t * RP + piece * kMine + e];
+    for (int e = 0; e < kMine; ++e) u[e] = Q[t * a.Rp + piece * kMine + e];
+    for (int s = 1; s < slices; ++s)
+#pragma unroll
+      for (int e = 0; e < kMine; ++e) u[e] += Q[s * a.u_step + t * a.Rp + piece * kMine + e];
   };
   auto write = [&](int buf, int i) {
     const bool in = i * kStep + row < k.rows;  // rows past the chunk add nothing, whatever they hold
@@ -384,6 +496,9 @@ __global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) acc[n] = mfma32(x, read_columns<kQ>(from + h * 16 * kQ + at_q + n * 64), acc[n]);
     }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) asm volatile("" : "+a"(acc[n]));
+    asm volatile("s_nop 15\n\ts_nop 7");  // (see settle: what follows has ways that meet again)
     if (i + 1 < steps) {
       write((i + 1) & 1, i + 1);
       if (i + 2 < steps) ask(next);
@@ -405,7 +520,7 @@ __global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
   float* to_b = k.slot < 0 ? a.dB + k.of * nb : to_a + na;
 #pragma unroll
   for (int n = 0; n < kTiles; ++n) {
-    const int r = n * 32 + (lane & 31);
+    const int r = r0 + n * 32 + (lane & 31);
     if (r >= a.R || (RP == 16 && (lane & 16))) continue;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -445,7 +560,7 @@ int chunk_of(int T, int I, int O) {
 
 }  // namespace
 
-int64_t f8_request_tiles(int T, int N) { return (int64_t)T / 16 + (T < N ? T : N); }
+int64_t f8_request_tiles(int T, int N) { return (int64_t)T / kTileRows + (T < N + 1 ? T : N + 1); }
 
 F8Requests f8_requests_of(const bsp_f8_requests* r) {
   int32_t* p = r->plan;
@@ -457,7 +572,7 @@ F8Requests f8_requests_of(const bsp_f8_requests* r) {
   return q;
 }
 int64_t f8_requests_bytes(int T, int N) {
-  return 4 * (((N + 1 + 3) & ~3) + 2 * (((int64_t)T + 3) & ~(int64_t)3) + 1 + 2 * f8_request_tiles(T, N));
+  return 4 * (((N + 1 + 3) & ~3) + 2 * (((int64_t)T + 3) & ~(int64_t)3) + 4 + kTileWords * f8_request_tiles(T, N));
 }
 int f8_launch_plan(const bsp_f8_requests* r, const void* which, bool wide, hipStream_t st) {
   const F8Requests q = f8_requests_of(r);
@@ -486,15 +601,23 @@ int f8_launch_set(const F8Adapters& d, int slot, int rank, const void* A, int64_
   return launched();
 }
 
-int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, hipStream_t st) {
+// Into how many slices the columns are cut: where tiles are too few for the chip, of four blocks at least.
+int f8_down_slices(int T, int N, int K) {
+  int slices = 1;
+  while (slices < 8 && f8_request_tiles(T, N) * slices < 256 && f8_blocks(K) >= 8 * slices) slices *= 2;
+  return slices;
+}
+int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, uint8_t* codes, uint8_t* scale, hipStream_t st) {
   DownArgs a{};
   a.X = x.X, a.scale = x.scale, a.ld = x.ld, a.srows = f8_scale_rows(T), a.down = transposed ? d.b_t : d.a, a.factor = d.scale, a.u = u, a.q = q;
-  a.K = transposed ? d.O : d.I, a.Kp = transposed ? d.Op : d.Ip;
+  a.T = T, a.K = transposed ? d.O : d.I, a.Kp = transposed ? d.Op : d.Ip, a.Rp = d.Rp, a.e5 = x.e5, a.codes = codes, a.to_scale = scale;
+  const int slices = f8_down_slices(T, d.N, a.K);
+  a.per = (f8_blocks(a.K) + slices - 1) / slices;
   switch (x.dtype) {
-    case BSP_BF16: return down_rank<kBf16>(a, T, d.N, d.Rp, st);
-    case BSP_F32: return down_rank<kF32>(a, T, d.N, d.Rp, st);
-    case BSP_E4M3: return down_rank<kE4>(a, T, d.N, d.Rp, st);
-    default: return down_rank<kE5>(a, T, d.N, d.Rp, st);
+    case BSP_BF16: return codes ? down_rank<kBf16, true>(a, T, d.N, slices, st) : down_rank<kBf16, false>(a, T, d.N, slices, st);
+    case BSP_F32: return codes ? down_rank<kF32, true>(a, T, d.N, slices, st) : down_rank<kF32, false>(a, T, d.N, slices, st);
+    case BSP_E4M3: return down_rank<kE4, false>(a, T, d.N, slices, st);
+    default: return down_rank<kE5, false>(a, T, d.N, slices, st);
   }
 }
 
@@ -506,17 +629,17 @@ int f8_launch_adapt_grad(const F8Adapters& d, const uint16_t* dY, int64_t ldy, c
                          float* part, float* dA, float* dB, hipStream_t st) {
   GradArgs a{};
   a.q = q, a.dY = dY, a.X = x.X, a.scale = x.scale, a.ldy = ldy, a.ldx = x.ld, a.srows = f8_scale_rows(T), a.u = u, a.v = v, a.dA = dA, a.dB = dB, a.part = part;
+  a.u_step = (int64_t)T * d.Rp, a.u_slices = f8_down_slices(T, d.N, d.I), a.v_slices = f8_down_slices(T, d.N, d.O), a.Rp = d.Rp;
   a.N = d.N, a.R = d.R, a.I = d.I, a.O = d.O, a.blocks_o = f8_blocks(d.O), a.chunk = chunk_of(T, d.I, d.O);
   a.src = x.dtype == BSP_BF16 ? kBf16 : x.dtype == BSP_E4M3 ? kE4 : kE5;
   const int64_t chunks = (int64_t)T / a.chunk + (T < d.N ? T : d.N);
-  const dim3 grid((unsigned)(a.blocks_o + f8_blocks(d.I)), (unsigned)chunks);
+  const dim3 grid((unsigned)(a.blocks_o + f8_blocks(d.I)), (unsigned)chunks, d.Rp == 128 ? 2 : 1);  // (128 ranks in two halves)
   if (chunks > 65535 || !f8_fits_x(grid.x, 256)) return BSP_ERR_SHAPE;
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a); };
   if (T > 0) {  // (without rows the sums below are all there is: zeros)
     if (d.Rp == 16) run(adapt_grad<16>);
     else if (d.Rp == 32) run(adapt_grad<32>);
-    else if (d.Rp == 64) run(adapt_grad<64>);
-    else run(adapt_grad<128>);
+    else run(adapt_grad<64>);
   }
   if (launched() != BSP_OK) return BSP_ERR_HIP;
   const int64_t groups = ((int64_t)d.R * (d.I + (int64_t)d.O) + 1023) / 1024;

@@ -95,14 +95,14 @@ int multiply(const F8Rows& rows, const F8Input& x, int T, const F8Low& low, cons
 }
 
 // rows given as values: workspace holds `sums` bytes, behind them the codes of rows that do not become codes in the product's kernel
-int multiply_values(const F8Rows& rows, const void* X, int x_dtype, int64_t ldx, int T, int K, bool e5, const F8Low& low, const F8Epilogue& q,
-                    int32_t y_dtype, void* workspace, int64_t sums, hipStream_t st) {
-  if (in_kernel(X, x_dtype, ldx, T, K)) return multiply(rows, F8Input{X, nullptr, x_dtype, e5, ldx}, T, low, q, y_dtype, workspace, st);
+int multiply_values(const F8Rows& rows, const void* X, int x_dtype, int64_t ldx, int T, int K, bool e5, const F8Epilogue& q, int32_t y_dtype,
+                    void* workspace, int64_t sums, hipStream_t st) {
+  if (in_kernel(X, x_dtype, ldx, T, K)) return multiply(rows, F8Input{X, nullptr, x_dtype, e5, ldx}, T, F8Low{}, q, y_dtype, workspace, st);
   const int64_t ld = (int64_t)f8_blocks(K) * F8_BLOCK;
   uint8_t *codes = (uint8_t*)workspace + sums, *scale = codes + T * ld;
   const int rc = f8_launch_save(X, x_dtype == BSP_F32, ldx, T, K, e5, codes, scale, st);
   if (rc != BSP_OK) return rc;
-  return multiply(rows, F8Input{codes, scale, e5 ? BSP_E5M2 : BSP_E4M3, e5, ld}, T, low, q, y_dtype, workspace, st);
+  return multiply(rows, F8Input{codes, scale, e5 ? BSP_E5M2 : BSP_E4M3, e5, ld}, T, F8Low{}, q, y_dtype, workspace, st);
 }
 
 int check_workspace(const void* workspace, int64_t bytes, int64_t need) {
@@ -124,7 +124,7 @@ int check_requests(const bsp_f8_requests* r) {
   return aligned(r->plan, 16) ? BSP_OK : BSP_ERR_ALIGN;
 }
 int64_t in16(int64_t bytes) { return (bytes + 15) & ~(int64_t)15; }
-int64_t low_bytes(const F8Adapters& d, int T) { return (int64_t)T * d.Rp * 4; }
+int64_t low_bytes(const F8Adapters& d, int T, int K) { return (int64_t)T * d.Rp * 4 * f8_down_slices(T, d.N, K); }
 
 int64_t codes_bytes(int T, int K) { return ((int64_t)T * f8_blocks(K) * F8_BLOCK) + f8_scale_rows(T) * f8_blocks(K); }
 
@@ -196,7 +196,7 @@ int bsp_f8_fc_values(const bsp_weights_f8* w, int32_t transposed, const void* X,
   const int64_t sums = sums_bytes(rows, T);
   rc = check_workspace(workspace, workspace_bytes, sums + (in_kernel(X, x_dtype, ldx, T, K) ? 0 : codes_bytes(T, K)));
   if (rc != BSP_OK) return rc;
-  return multiply_values(rows, X, x_dtype, ldx, T, K, e5, F8Low{}, q, y_dtype, workspace, sums, st);
+  return multiply_values(rows, X, x_dtype, ldx, T, K, e5, q, y_dtype, workspace, sums, st);
 }
 
 int bsp_f8_fc_grad_workspace(const bsp_weights_f8* w, int32_t T, int64_t* bytes) {
@@ -324,7 +324,7 @@ int bsp_f8_requests_plan(const bsp_f8_requests* r, const void* which, int32_t wh
 int bsp_f8_fc_adapted_workspace(const bsp_weights_f8* w, int32_t transposed, int32_t T, int32_t coded, const bsp_f8_adapters* adapters, int64_t* bytes) {
   int rc = bsp_f8_fc_workspace(w, transposed, T, coded, bytes);
   if (rc == BSP_OK) rc = check_adapters(adapters);
-  if (rc == BSP_OK) *bytes = in16(*bytes) + low_bytes(f8_adapters_of(adapters), T);
+  if (rc == BSP_OK) *bytes = in16(*bytes) + low_bytes(f8_adapters_of(adapters), T, transposed ? w->O : w->I);
   return rc;
 }
 
@@ -351,18 +351,19 @@ int bsp_f8_fc_adapted(const bsp_weights_f8* w, int32_t transposed, const bsp_cod
   const F8Rows rows = rows_of(w, transposed != 0);
   const F8Adapters d = f8_adapters_of(adapters);
   const int64_t sums = sums_bytes(rows, T), codes = X || in_kernel(values, x_dtype, ldx, T, K) ? 0 : codes_bytes(T, K);
-  rc = check_workspace(workspace, workspace_bytes, in16(sums + codes) + low_bytes(d, T));
+  rc = check_workspace(workspace, workspace_bytes, in16(sums + codes) + low_bytes(d, T, K));
   if (rc != BSP_OK) return rc;
   hipStream_t st = (hipStream_t)stream;
   const F8Requests who = f8_requests_of(requests);
   float* u = (float*)((uint8_t*)workspace + in16(sums + codes));
   const int64_t ld = (int64_t)f8_blocks(K) * F8_BLOCK;
   const F8Input given = X ? F8Input{X->codes, X->scale, X->dtype, X->dtype == BSP_E5M2, ld} : F8Input{values, nullptr, x_dtype, code == BSP_E5M2, ldx};
-  rc = f8_launch_down(d, transposed != 0, given, T, who, u, st);
+  // values that the product wants as codes become them where they are read for u
+  uint8_t *to = codes ? (uint8_t*)workspace + sums : nullptr, *to_scale = codes ? to + T * ld : nullptr;
+  rc = f8_launch_down(d, transposed != 0, given, T, who, u, to, to_scale, st);
   if (rc != BSP_OK) return rc;
-  const F8Low low{who.which, u, transposed ? d.a_t : d.b, (int64_t)d.Rp * (transposed ? d.Ip : d.Op), d.Rp};
-  if (X) return multiply(rows, given, T, low, q, y_dtype, workspace, st);
-  return multiply_values(rows, values, x_dtype, ldx, T, K, code == BSP_E5M2, low, q, y_dtype, workspace, sums, st);
+  const F8Low low{who.which, u, transposed ? d.a_t : d.b, (int64_t)d.Rp * (transposed ? d.Ip : d.Op), (int64_t)T * d.Rp, d.Rp, f8_down_slices(T, d.N, K)};
+  return multiply(rows, codes ? F8Input{to, to_scale, code, code == BSP_E5M2, ld} : given, T, low, q, y_dtype, workspace, st);
 }
 
 int bsp_f8_adapters_grad_workspace(const bsp_f8_adapters* adapters, int32_t T, int64_t* bytes) {
@@ -371,7 +372,7 @@ int bsp_f8_adapters_grad_workspace(const bsp_f8_adapters* adapters, int32_t T, i
   if (rc != BSP_OK) return rc;
   if (T < 0 || T > kMost) return BSP_ERR_SHAPE;
   const F8Adapters d = f8_adapters_of(adapters);
-  *bytes = 2 * low_bytes(d, T) + f8_adapt_part_bytes(d, T);
+  *bytes = low_bytes(d, T, d.I) + low_bytes(d, T, d.O) + f8_adapt_part_bytes(d, T);
   return BSP_OK;
 }
 
@@ -398,11 +399,11 @@ int bsp_f8_adapters_grad(const bsp_f8_adapters* adapters, const void* dY, int64_
   hipStream_t st = (hipStream_t)stream;
   const F8Adapters d = f8_adapters_of(adapters);
   const F8Requests who = f8_requests_of(requests);
-  float *u = (float*)workspace, *v = u + (int64_t)T * d.Rp, *part = v + (int64_t)T * d.Rp;
+  float *u = (float*)workspace, *v = u + low_bytes(d, T, d.I) / 4, *part = v + low_bytes(d, T, d.O) / 4;
   const F8Input x = X ? F8Input{X->codes, X->scale, X->dtype, X->dtype == BSP_E5M2, (int64_t)f8_blocks(X->K) * F8_BLOCK} : F8Input{values, nullptr, BSP_BF16, 0, ldx};
   if (T > 0) {
-    rc = f8_launch_down(d, false, x, T, who, u, st);
-    if (rc == BSP_OK) rc = f8_launch_down(d, true, F8Input{dY, nullptr, BSP_BF16, 0, ldy}, T, who, v, st);
+    rc = f8_launch_down(d, false, x, T, who, u, nullptr, nullptr, st);
+    if (rc == BSP_OK) rc = f8_launch_down(d, true, F8Input{dY, nullptr, BSP_BF16, 0, ldy}, T, who, v, nullptr, nullptr, st);
     if (rc != BSP_OK) return rc;
   }
   return f8_launch_adapt_grad(d, (const uint16_t*)dY, ldy, x, T, who, u, v, part, dA, dB, st);

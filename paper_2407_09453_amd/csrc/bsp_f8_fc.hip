@@ -131,8 +131,13 @@ __device__ __forceinline__ void store_tile(const F8Epilogue& q, f32x16_t (&acc)[
 struct LowParts {
   u32x4_t high, rest;
 };
-__device__ __forceinline__ LowParts low_parts(const float* u) {
-  const f32x4_t x0 = *(const f32x4_t*)u, x1 = *(const f32x4_t*)(u + 4);
+__device__ __forceinline__ LowParts low_parts(const F8Low& low, const float* u) {
+  f32x4_t x0 = *(const f32x4_t*)u, x1 = *(const f32x4_t*)(u + 4);
+  for (int s = 1; s < low.slices; ++s) {
+    u += low.u_step;
+    x0 += *(const f32x4_t*)u;
+    x1 += *(const f32x4_t*)(u + 4);
+  }
   LowParts p;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -151,24 +156,43 @@ __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT
     const int64_t t = t0 + m * 32 + (lane & 31) < T ? t0 + m * 32 + (lane & 31) : T - 1;
     const float* u = low.u + t * low.rank + (lane >> 5) * 8;
     const int of = low.which[t];
-    uint64_t todo = __ballot(of >= 0);
-    while (todo) {
-      const int now = __builtin_amdgcn_readlane(of, __builtin_ctzll(todo));
-      const bool mine = of == now;
-      todo &= ~__ballot(mine);
-      const uint16_t* b = up + now * low.step;
-      for (int k = 0; k < low.rank; k += 16) {
-        const LowParts p = low_parts(u + k);
-        u32x4_t w[MO];
+    const uint64_t all = __ballot(of >= 0);
+    if (!all) continue;
+    for (int k = 0; k < low.rank; k += 16) {
+      const LowParts p = low_parts(low, u + k);
+      // the adapters in turn, the next ones' weights asked for while one is multiplied
+      constexpr int kAhead = MO == 4 ? 2 : 4;
+      uint64_t todo = all;
+      int now[kAhead];
+      u32x4_t w[kAhead][MO];
+      auto ask = [&](int d) {
+        now[d] = -1;
+        if (!todo) return;
+        now[d] = __builtin_amdgcn_readlane(of, __builtin_ctzll(todo));
+        todo &= ~__ballot(of == now[d]);
+        const uint16_t* b = up + now[d] * low.step + k;
 #pragma unroll
-        for (int o = 0; o < MO; ++o) w[o] = *(const u32x4_t*)(b + (int64_t)o * 32 * low.rank + k);
+        for (int o = 0; o < MO; ++o) w[d][o] = *(const u32x4_t*)(b + (int64_t)o * 32 * low.rank);
+      };
 #pragma unroll
-        for (int o = 0; o < MO; ++o) {
-          f32x16_t sum = mfma_bf16_32x32x16(w[o], p.high, f32x16_t{});
-          sum = mfma_bf16_32x32x16(w[o], p.rest, sum);
+      for (int d = 0; d < kAhead; ++d) ask(d);
+      while (now[0] >= 0) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) acc[o][m][e] += mine ? sum[e] : 0.f;
-          __builtin_amdgcn_sched_barrier(0);
+        for (int d = 0; d < kAhead; ++d) {
+          if (now[d] < 0) break;
+          const bool mine = of == now[d];
+#pragma unroll
+          for (int o = 0; o < MO; ++o) {
+            f32x16_t sum = mfma_bf16_32x32x16(w[d][o], p.high, f32x16_t{});
+            sum = mfma_bf16_32x32x16(w[d][o], p.rest, sum);
+            // Read here, in the block of the instruction that makes it: where one of two ways that meet again leads past few instructions,
+            // the compiler counts those of the other as the wait that a result needs (channel 31 lost its second part).
+            asm volatile("" : "+v"(sum));
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[o][m][e] += mine ? sum[e] : 0.f;
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          ask(d);
         }
       }
     }

@@ -84,14 +84,19 @@ template <int MT>
 constexpr int kMostWaves = MT == 1 ? 16 : 8;
 
 // four channels' share of a row's adapter: fp32 products of u with bf16 weights
-__device__ __forceinline__ f32x4_t few_low(const F8Low& low, int64_t row, int o, f32x4_t s) {
+__device__ __forceinline__ f32x4_t few_low(const F8Low& low, int64_t row, int o) {
+  f32x4_t s = {};
   const int of = low.which[row];
   if (of < 0) return s;
   const uint16_t* b = low.up + of * low.step + (int64_t)o * low.rank;  // (channels are padded to whole blocks)
   const float* u = low.u + row * low.rank;
-#pragma unroll 2
+#pragma unroll 1
   for (int r = 0; r < low.rank; r += 8) {
-    const f32x4_t u0 = *(const f32x4_t*)(u + r), u1 = *(const f32x4_t*)(u + r + 4);
+    f32x4_t u0 = *(const f32x4_t*)(u + r), u1 = *(const f32x4_t*)(u + r + 4);
+    for (int k = 1; k < low.slices; ++k) {
+      u0 += *(const f32x4_t*)(u + k * low.u_step + r);
+      u1 += *(const f32x4_t*)(u + k * low.u_step + r + 4);
+    }
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const u32x4_t w = *(const u32x4_t*)(b + c * low.rank + r);
@@ -139,6 +144,7 @@ __device__ __forceinline__ void few(const FewArgs& a, float* sums) {  // sums: [
   u32x4_t w[kAhead][2], x[kAhead][MT][2];
   int ws[kAhead], col[kAhead], sx[kAhead][MT];
   f32x4_t acc[MT] = {};
+  f32x4_t low[LOW ? MT : 1];  // the first wave's, for the results that it puts out below
   for (int c = 0; c < mine || c == 0; c += 64) {  // the wave's block columns, 64 at a time, one a lane
     const int of = wave + (c + lane) * waves < cnt ? wave + (c + lane) * waves : cnt - 1;
     const int cols = a.full ? first + of : cnt > 0 ? a.w.idx[n0 + of] : 0;
@@ -178,6 +184,12 @@ __device__ __forceinline__ void few(const FewArgs& a, float* sums) {  // sums: [
         __syncthreads();
       }
     }
+    if constexpr (LOW) {
+      if (c == 0 && wave == 0 && blockIdx.z == 0) {  // (likewise)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) low[m] = few_low(a.low, t0 + m * 16 + r < a.T ? t0 + m * 16 + r : a.T - 1, blockIdx.x * 16 + g * 4);
+      }
+    }
     int s = 0;
     for (; s + 2 * kAhead <= end; s += kAhead)
 #pragma unroll
@@ -195,6 +207,11 @@ __device__ __forceinline__ void few(const FewArgs& a, float* sums) {  // sums: [
     for (int j = 0; j < kAhead; ++j)
       if (s + kAhead + j < end) multiply(j);
   }
+  if constexpr (LOW) {
+    if (wave == 0 && blockIdx.z == 0)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) acc[m] += low[m];
+  }
 #pragma unroll
   for (int m = 0; m < MT; ++m) *(f32x4_t*)(sums + ((wave * MT + m) * 64 + lane) * 4) = acc[m];
   __syncthreads();
@@ -204,8 +221,6 @@ __device__ __forceinline__ void few(const FewArgs& a, float* sums) {  // sums: [
     const int64_t row = t0 + (i >> 6) * 16 + (i & 15);
     const int o = blockIdx.x * 16 + ((i >> 4) & 3) * 4;
     if (row >= a.T || o >= a.w.out) continue;
-    if constexpr (LOW)
-      if (blockIdx.z == 0) s = few_low(a.low, row, o, s);
     if (a.split > 1) *(f32x4_t*)(a.part + (((int64_t)blockIdx.z * a.T + row) * ((a.w.out + 3) >> 2) + (o >> 2)) * 4) = s;
     else f8_store4<F32>(a.q, row, o, a.w.out, s[0], s[1], s[2], s[3]);
   }

@@ -234,7 +234,7 @@ class BspLayerF8:
         _check(load_library().bsp_f8_pack(self.struct, W.data_ptr(), kind, ld, _current_stream(W)), "bsp_f8_pack")
 
     def _bytes(self, kind, T, adapters=None):
-        key = (kind, T) if adapters is None else (kind, T, adapters.R)
+        key = (kind, T) if adapters is None else (kind, T, adapters.R, adapters.N)
         n = self._workspace.get(key)
         if n is None:
             lib, n = load_library(), ctypes.c_int64(0)

@@ -162,7 +162,7 @@ def test_whose_rows(name, which):
 @pytest.mark.parametrize("T", [1, 63, 64, 65, 1024, 5000, 40000])
 @pytest.mark.parametrize("N", [1, 3, 64, 65, 1000, 1024])
 def test_plan(T, N):
-    """Sorted by adapter, rows in their order within each, tiles of sixteen that cover each once."""
+    """Sorted by adapter, rows in their order within each, those of none last; tiles of up to 64 rows that hold each once."""
     import torch
     import paper_2407_09453_amd as bsp
     rng = np.random.default_rng([T, N])
@@ -178,9 +178,13 @@ def test_plan(T, N):
     order, tiles = p[at + t4:at + t4 + T], p[at + 2 * t4:]
     counts = np.bincount(own[own >= 0], minlength=N)
     assert (w == own).all() and (start == np.concatenate([[0], counts.cumsum()])).all()
-    assert (order[:start[N]] == np.argsort(np.where(own < 0, N, own), kind="stable")[:start[N]]).all()
-    want = [(a, j) for a in range(N) for j in range(0, counts[a], 16)]
-    assert tiles[0] == len(want) and (tiles[1:1 + 2 * len(want)].reshape(-1, 2) == np.array(want).reshape(-1, 2)).all()
+    want = np.argsort(np.where(own < 0, N, own), kind="stable")
+    assert (order == want).all()
+    records = [(a, want[s + j:s + min(j + 64, n)]) for a, s, n in [*zip(range(N), start, counts), (-1, start[N], T - start[N])] for j in range(0, n, 64)]
+    assert tiles[1] == len(records) and tiles[0] == sum(a >= 0 for a, _ in records)
+    for k, (a, rows) in enumerate(records):
+        r = tiles[4 + 68 * k:4 + 68 * (k + 1)]
+        assert r[0] == a and r[1] == len(rows) and (r[4:4 + len(rows)] == rows).all() and (r[4 + len(rows):] == rows[-1]).all()
 
 
 def test_nothing_of_another_row_or_adapter():
