@@ -516,10 +516,10 @@ int bsp_layer_norm_grad(const void* dY, int64_t ld_dy, const void* X, int64_t ld
  * Rp = 16, 32, 64 or 128. */
 typedef struct {
   int32_t N, R, I, O;
-  uint16_t* a;    /* device [N][Rp][128 ceil(I/128)], 16-byte aligned: as many elements an adapter as bsp_f8_adapters_size says for a */
-  uint16_t* a_t;  /* device, as many, transposed */
-  uint16_t* b;    /* device [N][128 ceil(O/128)][Rp]: as it says for b */
-  uint16_t* b_t;  /* device, as many, transposed */
+  uint16_t* a;    /* device, 16-byte aligned: Rp 128 ceil(I/128) elements an adapter, as bsp_f8_adapters_size says for a */
+  uint16_t* a_t;  /* device, as many: for the other direction */
+  uint16_t* b;    /* device: as it says for b */
+  uint16_t* b_t;  /* device, as many: for the other direction */
   float* scale;   /* device [N] */
 } bsp_f8_adapters;
 int bsp_f8_adapters_size(int32_t R, int32_t I, int32_t O, int64_t* a_elements, int64_t* b_elements);

@@ -289,7 +289,7 @@ struct F8Requests {
   int32_t* tiles;                  // how many tiles have an adapter, how many there are, two words; then the tiles' records
 };
 struct F8Adapters {  // bf16, ranks padded to Rp with zeros, columns to whole blocks
-  uint16_t *a, *a_t, *b, *b_t;  // [N][Rp][Ip], [N][Ip][Rp], [N][Op][Rp], [N][Rp][Op]
+  uint16_t *a, *a_t, *b, *b_t;  // [N][Rp Ip] by rank and by column, [N][Op Rp] by column and by rank, as adapt_set lays them out
   float* scale;
   int32_t N, R, I, O, Rp, Ip, Op;
 };
@@ -297,7 +297,7 @@ struct F8Adapters {  // bf16, ranks padded to Rp with zeros, columns to whole bl
 struct F8Low {
   const int32_t* which;
   const float* u;        // [slices][T][rank]: u_t is the sum of the slices'
-  const uint16_t* up;    // [N][128 ceil(out / 128)][rank]
+  const uint16_t* up;    // [N][128 ceil(out / 128) rank], by column
   int64_t step, u_step;  // elements of an adapter, of a slice
   int32_t rank;          // 0: nothing is added
   int32_t slices;
@@ -336,7 +336,8 @@ F8Requests f8_requests_of(const bsp_f8_requests* r);
 F8Adapters f8_adapters_of(const bsp_f8_adapters* d);
 int f8_launch_plan(const bsp_f8_requests* r, const void* which, bool wide, hipStream_t st);
 int f8_launch_set(const F8Adapters& d, int slot, int rank, const void* A, int64_t lda, const void* B, int64_t ldb, bool f32, float scale, hipStream_t st);
-int f8_down_slices(int T, int N, int K);
+int f8_down_slices(int T, int N, int K);  // of u in memory
+int f8_low_slices(int T, int N, int K);   // of u as it is left
 // codes, scale: where values are to become codes (of x.e5) on the way, too; or null
 int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, uint8_t* codes, uint8_t* scale, hipStream_t st);
 int64_t f8_adapt_part_bytes(const F8Adapters& d, int T);

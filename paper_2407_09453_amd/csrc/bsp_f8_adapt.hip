@@ -12,9 +12,12 @@
 // rows.  An adapter with many rows is cut into chunks whose sums a second launch joins, in order: no atomics.
 #include "bsp_norm.h"
 
+#include <type_traits>
+
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 constexpr int kTileRows = 64, kTileWords = 4 + kTileRows;  // a tile's record: adapter (-1: none), rows, two words, the rows' numbers (past the last: its)
 
 inline int launched() { return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP; }
@@ -113,23 +116,33 @@ __global__ __launch_bounds__(1024) void adapt_plan(const Id* ids, int T, int N, 
 }
 
 // ------------------------------------------------------------------ an adapter's weights
-// A thread takes one rank of one padded column: m [padded columns][Rp] and its transpose.  COLUMNS: W is [columns][rank], else [rank][columns].
+// Both forms lie as the matrix instructions take them, a lane's eight values together and the lanes' in turn, so that every request of a wave is
+// one kilobyte: where lanes take rows of their own a CU gets 7 bytes a clock, whatever it has under way.
+//   by rank (16 x 32 x 16 products): blocks of 128 columns, of sixteen ranks, four j, 64 lanes: rank lane & 15, columns 64 (j >> 1) + 16 (lane >> 4) + 8 (j & 1)
+//   by column (32 x 16 x 32): 32 columns, sixteen ranks, 64 lanes: column lane & 31, ranks 8 (lane >> 5)
+__device__ __forceinline__ int64_t at_by_rank(int r, int c, int Rp) {
+  return ((((int64_t)(c >> 7) * (Rp >> 4) + (r >> 4)) * 4 + ((c >> 6) & 1) * 2 + ((c >> 3) & 1)) * 64 + ((c >> 4) & 3) * 16 + (r & 15)) * 8 + (c & 7);
+}
+__device__ __forceinline__ int64_t at_by_column(int r, int c, int Rp) {
+  return (((int64_t)(c >> 5) * (Rp >> 4) + (r >> 4)) * 64 + ((r >> 3) & 1) * 32 + (c & 31)) * 8 + (r & 7);
+}
+// A thread takes one rank of one padded column.  COLUMNS: W is [columns][rank], else [rank][columns].
 template <bool F32, bool COLUMNS>
-__device__ __forceinline__ void set_side(const void* W, int64_t ld, int rank, int columns, int padded, int Rp, uint16_t* by_column, uint16_t* by_rank, int64_t i) {
+__device__ __forceinline__ void set_side(const void* W, int64_t ld, int rank, int columns, int Rp, uint16_t* by_column, uint16_t* by_rank, int64_t i) {
   const int c = (int)(i / Rp), r = (int)(i - (int64_t)c * Rp);
   uint16_t v = 0;
   if (r < rank && c < columns) {
     const int64_t at = COLUMNS ? c * ld + r : r * ld + c;
     v = F32 ? f32_to_bf16_rne(((const float*)W)[at]) : ((const uint16_t*)W)[at];
   }
-  by_column[i] = v;
-  by_rank[(int64_t)r * padded + c] = v;
+  by_column[at_by_column(r, c, Rp)] = v;
+  by_rank[at_by_rank(r, c, Rp)] = v;
 }
 template <bool F32>
 __global__ __launch_bounds__(256) void adapt_set(F8Adapters d, int slot, int rank, const void* A, int64_t lda, const void* B, int64_t ldb, float scale) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, na = (int64_t)d.Ip * d.Rp, nb = (int64_t)d.Op * d.Rp;
-  if (i < na) set_side<F32, false>(A, lda, rank, d.I, d.Ip, d.Rp, d.a_t + slot * na, d.a + slot * na, i);
-  else if (i < na + nb) set_side<F32, true>(B, ldb, rank, d.O, d.Op, d.Rp, d.b + slot * nb, d.b_t + slot * nb, i - na);
+  if (i < na) set_side<F32, false>(A, lda, rank, d.I, d.Rp, d.a_t + slot * na, d.a + slot * na, i);
+  else if (i < na + nb) set_side<F32, true>(B, ldb, rank, d.O, d.Rp, d.b + slot * nb, d.b_t + slot * nb, i - na);
   if (i == 0) d.scale[slot] = scale;
 }
 
@@ -140,12 +153,12 @@ struct DownArgs {
   const void* X;
   const uint8_t* scale;  // of codes
   int64_t ld, srows;
-  const uint16_t* down;  // [N][Rp][Kp]
+  const uint16_t* down;  // [N][Rp Kp], by rank
   const float* factor;   // [N]
   float* u;              // [slices][T][Rp]
   F8Requests q;
   int32_t T, K, Kp, Rp, per;  // per: blocks of a slice
-  int32_t e5;
+  int32_t e5, aligned;        // aligned: rows begin at 16 bytes
   uint8_t *codes, *to_scale;  // SAVE: the rows as codes, too
 };
 
@@ -179,108 +192,134 @@ __device__ __forceinline__ void settle(f32x4_t (&acc)[NR][M]) {
     for (int m = 0; m < M; ++m) asm volatile("" : "+v"(acc[i][m]));
 }
 
-// A workgroup takes a tile's rows (of fp32 half of them) and a slice of the blocks of 128 columns, which its waves share out; the slices' sums are
-// added by who reads u.  In a block a lane reads columns 64 q + 16 g + 8 h + 0..7 of its row and of its rank: 16 bytes of a row of
-// codes at a time.  The ranks are the matrix instruction's rows and the rows its columns, so nothing of one row, NaN among it,
-// reaches another's sums.  SAVE: the rows become codes on the way, as f8_save makes them, rows without an adapter too: four lanes
-// hold a row's 128 columns.  (64 rows, for an adapter's columns are read again for every tile.)
-template <int SRC>
-constexpr int kFragments = SRC == kF32 ? 2 : 4;  // of sixteen rows
+// A workgroup takes a tile's rows, or a half or quarter of them, and a slice of the blocks of 128 columns, which its waves share out; the slices'
+// sums are added by who reads u.  A wave's block of rows, 8 KB, goes through LDS, its own part of it: requests cover whole rows of the block,
+// while the matrix instruction wants sixteen rows' pieces side by side.  A row of pieces of 16 bytes is permuted by its number, so that
+// these lie in different banks.  In a block a lane's columns are 64 q + 16 g + 8 h + 0..7.  The ranks are the matrix
+// instruction's rows and the rows its columns, so nothing of one row, NaN among it, reaches another's sums.  SAVE: the rows become
+// codes on the way, as f8_save makes them, rows without an adapter too: four lanes hold a row's 128 columns.
+// (64 rows, for an adapter's columns are read again for every tile.)
+template <int SRC, int NR>
+constexpr int kFragments = SRC == kF32 ? 1 : SRC == kBf16 || NR == 4 ? 2 : 4;  // of sixteen rows
 
 template <int SRC, int NR, bool SAVE>
-__global__ __launch_bounds__(512) void adapt_down(DownArgs a) {
-  extern __shared__ float sums[];  // [waves][NR][M][64][4]
+__global__ __launch_bounds__(512, NR == 4 ? 2 : 4) void adapt_down(DownArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];  // [waves][rows of a block]; then sums [waves][NR][M][64][4]
   constexpr bool kCoded = SRC == kE4 || SRC == kE5;
-  constexpr int M = kFragments<SRC>, kHalves = 4 / M;
+  constexpr int M = kFragments<SRC, NR>, kParts = 4 / M, kSize = SRC == kF32 ? 4 : SRC == kBf16 ? 2 : 1;
+  constexpr int kRow = 128 * kSize, kPieces = kRow / 16, kAtOnce = 64 / kPieces, kAsks = 16 * M / kAtOnce;  // bytes and pieces of a row; rows a request, requests
   kernarg_touch<DownArgs>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int r = lane & 15, g = lane >> 4;
-  const int tile = blockIdx.x / kHalves, half = blockIdx.x % kHalves;
+  const int tile = blockIdx.x / kParts, part = blockIdx.x % kParts;
   const int32_t* record = a.q.tiles + 4 + (int64_t)tile * kTileWords;
-  int64_t t[M];
+  const int32_t* rows = record + 4 + part * M * 16;
+  const int of = __builtin_amdgcn_readfirstlane(record[0]), n = __builtin_amdgcn_readfirstlane(record[1]) - part * M * 16;
+  // the rows that this lane asks for pieces of, and of which piece
+  int64_t asked[kAsks];
 #pragma unroll
-  for (int m = 0; m < M; ++m) t[m] = record[4 + (half * M + m) * 16 + r];
-  const int of = __builtin_amdgcn_readfirstlane(record[0]), n = __builtin_amdgcn_readfirstlane(record[1]) - half * M * 16;
+  for (int q = 0; q < kAsks; ++q) asked[q] = rows[q * kAtOnce + lane / kPieces];
+  int64_t t[SAVE || kCoded ? M : 1];
+  if constexpr (SAVE || kCoded)
+#pragma unroll
+    for (int m = 0; m < M; ++m) t[m] = rows[m * 16 + r];
   const bool saves = SAVE && blockIdx.z == 0;
   if (tile >= a.q.tiles[saves ? 1 : 0] || n <= 0) return;
-  const int frags = (n + 15) >> 4;
-  const uint16_t* w = a.down + (((int64_t)(of < 0 ? 0 : of) * a.Rp + blockIdx.z * 16 * NR + r) * a.Kp + 16 * g);
+  auto key = [](int row) { return kCoded ? (row >> 1) & 7 : row & 15; };
+  const uint8_t* x[kAsks];
+#pragma unroll
+  for (int q = 0; q < kAsks; ++q) x[q] = (const uint8_t*)a.X + asked[q] * a.ld * kSize;
+  uint8_t* mine = lds + wave * 16 * M * kRow;
+  const uint16_t* w = a.down + (int64_t)(of < 0 ? 0 : of) * a.Rp * a.Kp + (blockIdx.z * NR * 4 * 64 + lane) * 8;
   const int nb = a.Kp >> 7, kb0 = blockIdx.y * a.per, kb1 = kb0 + a.per < nb ? kb0 + a.per : nb;
   f32x4_t acc[NR][M] = {};
   for (int kb = kb0 + wave; kb < kb1; kb += waves) {
-    const bool whole = kb * 128 + 128 <= a.K;
-    u32x4_t wv[NR][4], xv[M][4];
-    float xf[SRC == kF32 ? M : 1][4][8];
-    int s[M];
-    if (of >= 0)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the last block has been read
+    if (kCoded || (a.aligned && kb * 128 + 128 <= a.K)) {
+#pragma unroll
+      for (int q = 0; q < kAsks; ++q) {
+        const int piece = (lane % kPieces) ^ key(q * kAtOnce + lane / kPieces);
+        __builtin_amdgcn_global_load_lds((f8_gptr_t)(x[q] + (int64_t)kb * kRow + piece * 16), (f8_lptr_t)(mine + q * 1024), 16, 0, 0);
+      }
+    } else if constexpr (!kCoded) {  // rows at any address, a row's end
+#pragma unroll
+      for (int q = 0; q < kAsks; ++q) {
+        const int c = kb * 128 + ((lane % kPieces) ^ key(q * kAtOnce + lane / kPieces)) * (16 / kSize);
+        u32x4_t v;
+        if constexpr (SRC == kBf16) {
+          if (kb * 128 + 128 <= a.K) {
+            v = *(const f8_any2_t*)((const uint16_t*)x[q] + c);
+          } else {
+            float f[8];
+            load8<false>(x[q], c, a.K, f);
+            v = pack8(f);
+          }
+        } else if (kb * 128 + 128 <= a.K) {
+          v = *(const f8_any4_t*)((const float*)x[q] + c);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] = c + k < a.K ? ((const uint32_t*)x[q])[c + k] : 0;
+        }
+        *(u32x4_t*)(mine + q * 1024 + lane * 16) = v;
+      }
+    }
+    u32x4_t wv[NR][4];
+#pragma unroll
+    for (int i = 0; i < NR; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) wv[i][j] = *(const u32x4_t*)(w + (((int64_t)kb * (a.Rp >> 4) + i) * 4 + j) * 64 * 8);
+    int s[kCoded ? M : 1];
+    if constexpr (kCoded)
+#pragma unroll
+      for (int m = 0; m < M; ++m) s[m] = a.scale[kb * a.srows + t[m]];
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      const uint8_t* row = mine + (m * 16 + r) * kRow;
+      auto piece = [&](int p) { return *(const u32x4_t*)(row + ((p ^ key(m * 16 + r)) << 4)); };
+      u32x4_t xv[4], xl[SRC == kF32 ? 4 : 1];
+      float v[SRC == kF32 ? 4 : 1][8];
+      if constexpr (kCoded) {
+        const float f = __uint_as_float((uint32_t)s[m] << 23);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const u32x4_t c = piece(4 * q + g);
+          xv[2 * q] = f8_decode_bf16x8<SRC == kE5>(c.x, c.y, f);
+          xv[2 * q + 1] = f8_decode_bf16x8<SRC == kE5>(c.z, c.w, f);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int p = 8 * (j >> 1) + 2 * g + (j & 1);  // by eights
+          if constexpr (SRC == kBf16) {
+            xv[j] = piece(p);
+          } else {
+            const u32x4_t p0 = piece(2 * p), p1 = piece(2 * p + 1);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[j][k] = __uint_as_float(k < 4 ? p0[k & 3] : p1[k & 3]);
+            xv[j] = pack8(v[j]);
+            xl[j] = rest8(v[j], xv[j]);
+          }
+        }
+      }
 #pragma unroll
       for (int i = 0; i < NR; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) wv[i][j] = *(const u32x4_t*)(w + (int64_t)i * 16 * a.Kp + kb * 128 + (j >> 1) * 64 + (j & 1) * 8);
-#pragma unroll
-    for (int m = 0; m < M; ++m) {
-      if (m >= frags) break;
-      if constexpr (kCoded) {
-        const uint8_t* x = (const uint8_t*)a.X + t[m] * a.ld + kb * 128 + g * 16;
-        s[m] = a.scale[kb * a.srows + t[m]];
-        xv[m][0] = *(const u32x4_t*)x;
-        xv[m][2] = *(const u32x4_t*)(x + 64);
-      } else {
-        const void* x = row_of<SRC == kF32>(a.X, t[m], a.ld);
-#pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int c = kb * 128 + (j >> 1) * 64 + 16 * g + (j & 1) * 8;
-          if constexpr (SRC == kBf16) {
-            if (whole) {
-              xv[m][j] = *(const f8_any2_t*)((const uint16_t*)x + c);
-            } else {
-              float v[8];
-              load8<false>(x, c, a.K, v);
-              xv[m][j] = pack8(v);
-            }
-          } else {
-            load8<true>(x, c, a.K, xf[m][j]);
-          }
+          acc[i][m] = mfma_bf16_16x16x32(wv[i][j], xv[j], acc[i][m]);
+          if constexpr (SRC == kF32) acc[i][m] = mfma_bf16_16x16x32(wv[i][j], xl[j], acc[i][m]);
         }
-      }
-    }
-#pragma unroll
-    for (int m = 0; m < M; ++m) {
-      if (m >= frags) break;
-      u32x4_t xl[SRC == kF32 ? 4 : 1];
-      if constexpr (kCoded) {
-        const float f = __uint_as_float((uint32_t)s[m] << 23);
-        const u32x4_t c0 = xv[m][0], c1 = xv[m][2];
-        xv[m][0] = f8_decode_bf16x8<SRC == kE5>(c0.x, c0.y, f);
-        xv[m][1] = f8_decode_bf16x8<SRC == kE5>(c0.z, c0.w, f);
-        xv[m][2] = f8_decode_bf16x8<SRC == kE5>(c1.x, c1.y, f);
-        xv[m][3] = f8_decode_bf16x8<SRC == kE5>(c1.z, c1.w, f);
-      } else if constexpr (SRC == kF32) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          xv[m][j] = pack8(xf[m][j]);
-          xl[j] = rest8(xf[m][j], xv[m][j]);
-        }
-      }
-      if (of >= 0)
-#pragma unroll
-        for (int i = 0; i < NR; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            acc[i][m] = mfma_bf16_16x16x32(wv[i][j], xv[m][j], acc[i][m]);
-            if constexpr (SRC == kF32) acc[i][m] = mfma_bf16_16x16x32(wv[i][j], xl[j], acc[i][m]);
-          }
       if constexpr (SAVE) {
-        if (saves) {
-          float v[4][8];
+        if (saves && m * 16 < n) {
           uint32_t most = 0;
+          float y[4][8];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            if constexpr (SRC == kBf16) unpack8(xv[m][j], v[j]);
+            if constexpr (SRC == kBf16) unpack8(xv[j], y[j]);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-              if constexpr (SRC == kF32) v[j][k] = xf[m][j][k];
-              most = max(most, f8_magnitude(v[j][k]));
+              if constexpr (SRC == kF32) y[j][k] = v[j][k];
+              most = max(most, f8_magnitude(y[j][k]));
             }
           }
           const auto p = __builtin_amdgcn_permlane16_swap(most, most, false, false);
@@ -294,8 +333,8 @@ __global__ __launch_bounds__(512) void adapt_down(DownArgs a) {
             u32x4_t c;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const float* y = &v[2 * q + (k >> 1)][4 * (k & 1)];
-              c[k] = a.e5 ? f8_encode4<true>(y[0] * f, y[1] * f, y[2] * f, y[3] * f) : f8_encode4<false>(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
+              const float* z = &y[2 * q + (k >> 1)][4 * (k & 1)];
+              c[k] = a.e5 ? f8_encode4<true>(z[0] * f, z[1] * f, z[2] * f, z[3] * f) : f8_encode4<false>(z[0] * f, z[1] * f, z[2] * f, z[3] * f);
             }
             if (m * 16 + r < n) *(u32x4_t*)(a.codes + t[m] * a.Kp + kb * 128 + q * 64 + g * 16) = c;
           }
@@ -306,6 +345,8 @@ __global__ __launch_bounds__(512) void adapt_down(DownArgs a) {
   }
   if (of < 0) return;
   settle(acc);
+  __syncthreads();
+  float* sums = (float*)lds;
 #pragma unroll
   for (int i = 0; i < NR; ++i)
 #pragma unroll
@@ -317,21 +358,32 @@ __global__ __launch_bounds__(512) void adapt_down(DownArgs a) {
     if (row >= n) continue;
     f32x4_t sum = *(const f32x4_t*)(sums + i * 4);
     for (int v = 1; v < waves; ++v) sum += *(const f32x4_t*)(sums + (v * NR * M * 64 + i) * 4);
-    const int64_t at = (int64_t)blockIdx.y * a.T + record[4 + half * M * 16 + row];
+    const int64_t at = (int64_t)blockIdx.y * a.T + rows[row];
     *(f32x4_t*)(a.u + at * a.Rp + (blockIdx.z * NR + i / (M * 64)) * 16 + ((i >> 4) & 3) * 4) = sum * factor;
   }
 }
 
+// u = the sum of its slices, in their order, in the first one's place
+__global__ __launch_bounds__(256) void adapt_sum(float* u, int slices, int64_t quads) {
+  const int64_t i = ((int64_t)blockIdx.y * kGridX + blockIdx.x) * 256 + threadIdx.x;
+  if (i >= quads) return;
+  f32x4_t s = *(const f32x4_t*)(u + i * 4);
+#pragma unroll 8
+  for (int k = 1; k < slices; ++k) s += *(const f32x4_t*)(u + (k * quads + i) * 4);
+  *(f32x4_t*)(u + i * 4) = s;
+}
+
 template <int SRC, int NR, bool SAVE>
 int down_launch(const DownArgs& a, int T, int N, int slices, hipStream_t st) {
-  constexpr int M = kFragments<SRC>, most = NR == 4 ? 4 : 8;
+  constexpr int M = kFragments<SRC, NR>, most = 8;
+  constexpr int kBytes = 16 * M * (SRC == kF32 ? 512 : SRC == kBf16 ? 256 : 128), kWave = kBytes > NR * M * 1024 ? kBytes : NR * M * 1024;
   const int64_t tiles = f8_request_tiles(T, N) * (4 / M);
   int waves = most;  // a wave a block of columns at least
   while (waves > 1 && waves > a.per) waves >>= 1;
   if (!f8_fits_x(tiles, 512)) return BSP_ERR_SHAPE;
-  static const bool raised = hipFuncSetAttribute((const void*)&adapt_down<SRC, NR, SAVE>, hipFuncAttributeMaxDynamicSharedMemorySize, most * NR * M * 1024) == hipSuccess;
+  static const bool raised = hipFuncSetAttribute((const void*)&adapt_down<SRC, NR, SAVE>, hipFuncAttributeMaxDynamicSharedMemorySize, most * kWave) == hipSuccess;
   if (!raised) return BSP_ERR_HIP;
-  hipLaunchKernelGGL((adapt_down<SRC, NR, SAVE>), dim3((unsigned)tiles, (unsigned)slices, (unsigned)(a.Rp / (16 * NR))), dim3(64 * waves), (size_t)waves * NR * M * 1024, st, a);
+  hipLaunchKernelGGL((adapt_down<SRC, NR, SAVE>), dim3((unsigned)tiles, (unsigned)slices, (unsigned)(a.Rp / (16 * NR))), dim3(64 * waves), (size_t)waves * kWave, st, a);
   return launched();
 }
 template <int SRC, bool SAVE>
@@ -425,52 +477,69 @@ __global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
   const bool whole = c0 + 128 <= columns;
   // what this thread brings: sixteen columns of a row, and kMine values of u
   const int row = tid >> 3, piece = tid & 7;
-  u32x4_t p[2];
-  float u[kMine];
-  int s = 0;
+  // Two steps are on their way to registers while a third is multiplied.
+  struct Coming {
+    u32x4_t p[2];
+    float u[kMine], u2[kMine];  // of two slices (nothing here looks at what is on its way: that would wait for it)
+    int s;
+  } in[2];
   auto place = [&](int i) { return a.q.order[k.begin + (i * kStep + row < k.rows ? i * kStep + row : k.rows - 1)]; };
-  auto ask = [&](int64_t t) {
+  auto read_u = [&](const float* q, float* u) {
+    if constexpr (kMine >= 4) {
+#pragma unroll
+      for (int e = 0; e < kMine; e += 4) {
+        const f32x4_t v = *(const f32x4_t*)(q + e);
+        u[e] = v[0], u[e + 1] = v[1], u[e + 2] = v[2], u[e + 3] = v[3];
+      }
+    } else {
+      const f32x2_t v = *(const f32x2_t*)q;
+      u[0] = v[0], u[1] = v[1];
+    }
+  };
+  auto ask = [&](int64_t t, Coming& to) {
     const int c = c0 + piece * 16;
     if (src == kBf16) {
       if (whole) {
         const uint16_t* x = (const uint16_t*)P + t * ld + c;
-        p[0] = *(const f8_any2_t*)x;
-        p[1] = *(const f8_any2_t*)(x + 8);
+        to.p[0] = *(const f8_any2_t*)x;
+        to.p[1] = *(const f8_any2_t*)(x + 8);
       } else {
         float v[8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           load8<false>((const uint16_t*)P + t * ld, c + 8 * h, columns, v);
-          p[h] = pack8(v);
+          to.p[h] = pack8(v);
         }
       }
     } else {
-      p[0] = *(const u32x4_t*)((const uint8_t*)P + t * ld + c);
-      s = a.scale[kb * a.srows + t];
+      to.p[0] = *(const u32x4_t*)((const uint8_t*)P + t * ld + c);
+      to.s = a.scale[kb * a.srows + t];
     }
+    const float* q = Q + t * a.Rp + piece * kMine;
+    read_u(q, to.u);
+    if (slices > 1) read_u(q + a.u_step, to.u2);
+    for (int s = 2; s < slices; ++s)  // (few rows)
 #pragma unroll
-    for (int e = 0; e < kMine; ++e) u[e] = Q[t * a.Rp + piece * kMine + e];
-    for (int s = 1; s < slices; ++s)
-#pragma unroll
-      for (int e = 0; e < kMine; ++e) u[e] += Q[s * a.u_step + t * a.Rp + piece * kMine + e];
+      for (int e = 0; e < kMine; ++e) to.u[e] += q[s * a.u_step + e];
   };
-  auto write = [&](int buf, int i) {
-    const bool in = i * kStep + row < k.rows;  // rows past the chunk add nothing, whatever they hold
+  auto write = [&](int buf, int i, const Coming& from) {
+    const bool have = i * kStep + row < k.rows;  // rows past the chunk add nothing, whatever they hold
     uint8_t* to = lds + buf * kBuffer;
-    u32x4_t w[2] = {p[0], p[1]};
+    u32x4_t w[2] = {from.p[0], from.p[1]};
     if (src != kBf16) {
-      const float f = __uint_as_float((uint32_t)s << 23);
-      const u32x4_t c = p[0];
+      const float f = __uint_as_float((uint32_t)from.s << 23);
+      const u32x4_t c = from.p[0];
       w[0] = src == kE5 ? f8_decode_bf16x8<true>(c.x, c.y, f) : f8_decode_bf16x8<false>(c.x, c.y, f);
       w[1] = src == kE5 ? f8_decode_bf16x8<true>(c.z, c.w, f) : f8_decode_bf16x8<false>(c.z, c.w, f);
     }
     const int key = (row & 3) << 1 | ((row >> 3) & 1);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) *(u32x4_t*)(to + row * 256 + ((piece ^ key) << 5) + 16 * h) = in ? w[h] : u32x4_t{0, 0, 0, 0};
+    for (int h = 0; h < 2; ++h) *(u32x4_t*)(to + row * 256 + ((piece ^ key) << 5) + 16 * h) = have ? w[h] : u32x4_t{0, 0, 0, 0};
     uint16_t* hi = (uint16_t*)(to + kP + row * kQ) + piece * kMine;
 #pragma unroll
     for (int e = 0; e < kMine; e += 2) {
-      const float x0 = in ? u[e] : 0.f, x1 = in ? u[e + 1] : 0.f;
+      const float y0 = slices > 1 ? from.u[e] + from.u2[e] : from.u[e], y1 = slices > 1 ? from.u[e + 1] + from.u2[e + 1] : from.u[e + 1];
+      const float x0 = have ? y0 : 0.f, x1 = have ? y1 : 0.f;
       const uint32_t h = f8_pack_bf16x2(x0, x1);
       *(uint32_t*)(hi + e) = h;
       *(uint32_t*)(hi + RP + e) = f8_pack_bf16x2(x0 - __uint_as_float(h << 16), x1 - __uint_as_float(h & 0xFFFF0000u));
@@ -481,14 +550,15 @@ __global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
   const int at_q = kP + trow * kQ + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
   f32x16_t acc[NT] = {};
   const int steps = (k.rows + kStep - 1) / kStep;
-  int next = place(0);
-  ask(next);
-  next = place(1 < steps ? 1 : 0);
-  write(0, 0);
-  if (steps > 1) ask(next);
-  next = place(2 < steps ? 2 : steps - 1);
+  // (place clamps to the chunk's last row, so steps past the last ask for that)
+  ask(place(0), in[0]);
+  ask(place(1), in[1]);
+  int next = place(2);
+  write(0, 0, in[0]);
+  ask(next, in[0]);
+  next = place(3);
   __syncthreads();
-  for (int i = 0; i < steps; ++i) {
+  auto step = [&](int i, Coming& coming) {  // multiplies step i, writes step i + 1 from `coming`, asks for step i + 3
     const uint8_t* from = lds + (i & 1) * kBuffer;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -500,11 +570,17 @@ __global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
     for (int n = 0; n < NT; ++n) asm volatile("" : "+a"(acc[n]));
     asm volatile("s_nop 15\n\ts_nop 7");  // (see settle: what follows has ways that meet again)
     if (i + 1 < steps) {
-      write((i + 1) & 1, i + 1);
-      if (i + 2 < steps) ask(next);
-      next = place(i + 3 < steps ? i + 3 : steps - 1);
+      write((i + 1) & 1, i + 1, coming);
+      if (i + 3 < steps) {
+        ask(next, coming);
+        next = place(i + 4);
+      }
     }
     __syncthreads();
+  };
+  for (int i = 0; i < steps; i += 2) {
+    step(i, in[1]);
+    if (i + 1 < steps) step(i + 1, in[0]);
   }
   // high and low parts together
   constexpr int kTiles = RP == 16 ? 1 : NT / 2;
@@ -601,24 +677,42 @@ int f8_launch_set(const F8Adapters& d, int slot, int rank, const void* A, int64_
   return launched();
 }
 
-// Into how many slices the columns are cut: where tiles are too few for the chip, of four blocks at least.
+// Into how many slices the columns are cut, of eight blocks at least, one a wave: few rows want as many workgroups as there are blocks,
+// many rows several rounds of workgroups, whose last round is then a small part.
+#ifndef LARGE_S
+#define LARGE_S 8
+#endif
 int f8_down_slices(int T, int N, int K) {
+  const int64_t tiles = f8_request_tiles(T, N);
+  const int most = T <= 32 ? 4 : tiles < 64 ? 2 : LARGE_S;
   int slices = 1;
-  while (slices < 8 && f8_request_tiles(T, N) * slices < 256 && f8_blocks(K) >= 8 * slices) slices *= 2;
+  while (slices < most && tiles * slices < 1024 && f8_blocks(K) >= 16 * slices) slices *= 2;
   return slices;
+}
+// ... and how many of them are left to whoever reads u: two, or with few rows four, cost less there than a launch that adds them
+int f8_low_slices(int T, int N, int K) {
+  const int slices = f8_down_slices(T, N, K);
+  return slices > 2 && T > 32 ? 1 : slices;
 }
 int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, uint8_t* codes, uint8_t* scale, hipStream_t st) {
   DownArgs a{};
   a.X = x.X, a.scale = x.scale, a.ld = x.ld, a.srows = f8_scale_rows(T), a.down = transposed ? d.b_t : d.a, a.factor = d.scale, a.u = u, a.q = q;
   a.T = T, a.K = transposed ? d.O : d.I, a.Kp = transposed ? d.Op : d.Ip, a.Rp = d.Rp, a.e5 = x.e5, a.codes = codes, a.to_scale = scale;
+  const int64_t size = x.dtype == BSP_F32 ? 4 : x.dtype == BSP_BF16 ? 2 : 1;
+  a.aligned = (((uintptr_t)x.X | (uintptr_t)(x.ld * size)) & 15) == 0;
   const int slices = f8_down_slices(T, d.N, a.K);
   a.per = (f8_blocks(a.K) + slices - 1) / slices;
+  int rc;
   switch (x.dtype) {
-    case BSP_BF16: return codes ? down_rank<kBf16, true>(a, T, d.N, slices, st) : down_rank<kBf16, false>(a, T, d.N, slices, st);
-    case BSP_F32: return codes ? down_rank<kF32, true>(a, T, d.N, slices, st) : down_rank<kF32, false>(a, T, d.N, slices, st);
-    case BSP_E4M3: return down_rank<kE4, false>(a, T, d.N, slices, st);
-    default: return down_rank<kE5, false>(a, T, d.N, slices, st);
+    case BSP_BF16: rc = codes ? down_rank<kBf16, true>(a, T, d.N, slices, st) : down_rank<kBf16, false>(a, T, d.N, slices, st); break;
+    case BSP_F32: rc = codes ? down_rank<kF32, true>(a, T, d.N, slices, st) : down_rank<kF32, false>(a, T, d.N, slices, st); break;
+    case BSP_E4M3: rc = down_rank<kE4, false>(a, T, d.N, slices, st); break;
+    default: rc = down_rank<kE5, false>(a, T, d.N, slices, st);
   }
+  if (rc != BSP_OK || f8_low_slices(T, d.N, a.K) == slices) return rc;
+  const int64_t quads = (int64_t)T * d.Rp / 4;
+  hipLaunchKernelGGL(adapt_sum, f8_grid((quads + 255) / 256), dim3(256), 0, st, u, slices, quads);
+  return launched();
 }
 
 int64_t f8_adapt_part_bytes(const F8Adapters& d, int T) {
@@ -629,7 +723,7 @@ int f8_launch_adapt_grad(const F8Adapters& d, const uint16_t* dY, int64_t ldy, c
                          float* part, float* dA, float* dB, hipStream_t st) {
   GradArgs a{};
   a.q = q, a.dY = dY, a.X = x.X, a.scale = x.scale, a.ldy = ldy, a.ldx = x.ld, a.srows = f8_scale_rows(T), a.u = u, a.v = v, a.dA = dA, a.dB = dB, a.part = part;
-  a.u_step = (int64_t)T * d.Rp, a.u_slices = f8_down_slices(T, d.N, d.I), a.v_slices = f8_down_slices(T, d.N, d.O), a.Rp = d.Rp;
+  a.u_step = (int64_t)T * d.Rp, a.u_slices = f8_low_slices(T, d.N, d.I), a.v_slices = f8_low_slices(T, d.N, d.O), a.Rp = d.Rp;
   a.N = d.N, a.R = d.R, a.I = d.I, a.O = d.O, a.blocks_o = f8_blocks(d.O), a.chunk = chunk_of(T, d.I, d.O);
   a.src = x.dtype == BSP_BF16 ? kBf16 : x.dtype == BSP_E4M3 ? kE4 : kE5;
   const int64_t chunks = (int64_t)T / a.chunk + (T < d.N ? T : d.N);

@@ -362,7 +362,7 @@ int bsp_f8_fc_adapted(const bsp_weights_f8* w, int32_t transposed, const bsp_cod
   uint8_t *to = codes ? (uint8_t*)workspace + sums : nullptr, *to_scale = codes ? to + T * ld : nullptr;
   rc = f8_launch_down(d, transposed != 0, given, T, who, u, to, to_scale, st);
   if (rc != BSP_OK) return rc;
-  const F8Low low{who.which, u, transposed ? d.a_t : d.b, (int64_t)d.Rp * (transposed ? d.Ip : d.Op), (int64_t)T * d.Rp, d.Rp, f8_down_slices(T, d.N, K)};
+  const F8Low low{who.which, u, transposed ? d.a_t : d.b, (int64_t)d.Rp * (transposed ? d.Ip : d.Op), (int64_t)T * d.Rp, d.Rp, f8_low_slices(T, d.N, K)};
   return multiply(rows, codes ? F8Input{to, to_scale, code, code == BSP_E5M2, ld} : given, T, low, q, y_dtype, workspace, st);
 }
 

@@ -124,19 +124,27 @@ __device__ __forceinline__ void store_tile(const F8Epilogue& q, f32x16_t (&acc)[
   }
 }
 
-// The rows' adapters: B_a u_t added to a wave's sums, one adapter of its rows after the other.  The rows are the matrix instruction's columns, so a
-// lane holds results of one row, and takes or leaves what an adapter adds as that is the row's own or another's: nothing of
-// another adapter's, NaN among it, gets there.  u enters as two bf16 parts.  The products start from zero and are added with
-// ordinary instructions, 32 channels at a time: kept beside a copy of the sums they would not fit in registers (380 of them in memory).
+// The rows' adapters: B_a u_t added to a wave's sums, one adapter of its rows after the other, the next ones' weights asked for while one is
+// multiplied.  u enters as two bf16 parts, as zeros in the rows of other adapters: the rows are the matrix instruction's columns, and the
+// sums go on where they are.  Zero times what is no number is none: an adapter with such weights among its
+// rows' neighbours is multiplied from zero, and a lane, which holds results of one row, takes or leaves what it gives (three times the
+// instructions: 16384 x 4096 -> 4096 with rows of twelve adapters mixed 304 us where all go that way).
+// The wait between a matrix instruction and the first use of its result, by hand: where two ways meet again behind it, a branch that is taken or
+// not, the compiler counts the instructions of one of them, be it the longer (found where channel 31 of a result lost its second part).
+__device__ __forceinline__ void settle() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
 struct LowParts {
   u32x4_t high, rest;
 };
 __device__ __forceinline__ LowParts low_parts(const F8Low& low, const float* u) {
   f32x4_t x0 = *(const f32x4_t*)u, x1 = *(const f32x4_t*)(u + 4);
+#pragma unroll 4
   for (int s = 1; s < low.slices; ++s) {
-    u += low.u_step;
-    x0 += *(const f32x4_t*)u;
-    x1 += *(const f32x4_t*)(u + 4);
+    x0 += *(const f32x4_t*)(u + s * low.u_step);
+    x1 += *(const f32x4_t*)(u + s * low.u_step + 4);
   }
   LowParts p;
 #pragma unroll
@@ -147,10 +155,11 @@ __device__ __forceinline__ LowParts low_parts(const F8Low& low, const float* u) 
   }
   return p;
 }
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2_t;
 template <int MO, int MT>
 __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT], int T, int64_t t0, int o0) {
   const int lane = threadIdx.x & 63;
-  const uint16_t* up = low.up + (int64_t)(o0 + (lane & 31)) * low.rank + (lane >> 5) * 8;
+  const uint16_t* up = low.up + (int64_t)o0 * low.rank + lane * 8;  // (as the instruction takes them: 32 channels, sixteen ranks, 64 lanes)
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const int64_t t = t0 + m * 32 + (lane & 31) < T ? t0 + m * 32 + (lane & 31) : T - 1;
@@ -160,8 +169,7 @@ __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT
     if (!all) continue;
     for (int k = 0; k < low.rank; k += 16) {
       const LowParts p = low_parts(low, u + k);
-      // the adapters in turn, the next ones' weights asked for while one is multiplied
-      constexpr int kAhead = MO == 4 ? 2 : 4;
+      constexpr int kAhead = MO == 4 ? 2 : 8;
       uint64_t todo = all;
       int now[kAhead];
       u32x4_t w[kAhead][MO];
@@ -170,7 +178,7 @@ __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT
         if (!todo) return;
         now[d] = __builtin_amdgcn_readlane(of, __builtin_ctzll(todo));
         todo &= ~__ballot(of == now[d]);
-        const uint16_t* b = up + now[d] * low.step + k;
+        const uint16_t* b = up + now[d] * low.step + k * 32;
 #pragma unroll
         for (int o = 0; o < MO; ++o) w[d][o] = *(const u32x4_t*)(b + (int64_t)o * 32 * low.rank);
       };
@@ -181,22 +189,39 @@ __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT
         for (int d = 0; d < kAhead; ++d) {
           if (now[d] < 0) break;
           const bool mine = of == now[d];
+          // an exponent of ones in any half of the weights' words
+          u16x2_t most = {0, 0};
 #pragma unroll
-          for (int o = 0; o < MO; ++o) {
-            f32x16_t sum = mfma_bf16_32x32x16(w[d][o], p.high, f32x16_t{});
-            sum = mfma_bf16_32x32x16(w[d][o], p.rest, sum);
-            // Read here, in the block of the instruction that makes it: where one of two ways that meet again leads past few instructions,
-            // the compiler counts those of the other as the wait that a result needs (channel 31 lost its second part).
-            asm volatile("" : "+v"(sum));
+          for (int o = 0; o < MO; ++o)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[o][m][e] += mine ? sum[e] : 0.f;
-            __builtin_amdgcn_sched_barrier(0);
+            for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2_t, w[d][o][e] & 0x7F807F80u));
+          const bool odd = most.x == 0x7F80 || most.y == 0x7F80;
+          if (__all(mine) || !__any(odd)) {
+            u32x4_t high, rest;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) high[e] = mine ? p.high[e] : 0, rest[e] = mine ? p.rest[e] : 0;
+#pragma unroll
+            for (int o = 0; o < MO; ++o) acc[o][m] = mfma_bf16_32x32x16(w[d][o], high, acc[o][m]);
+#pragma unroll
+            for (int o = 0; o < MO; ++o) acc[o][m] = mfma_bf16_32x32x16(w[d][o], rest, acc[o][m]);
+          } else {
+            settle();
+#pragma unroll
+            for (int o = 0; o < MO; ++o) {
+              f32x16_t sum = mfma_bf16_32x32x16(w[d][o], p.high, f32x16_t{});
+              sum = mfma_bf16_32x32x16(w[d][o], p.rest, sum);
+              asm volatile("" : "+v"(sum));  // (read in the block of the instruction that makes it)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) acc[o][m][e] += mine ? sum[e] : 0.f;
+              __builtin_amdgcn_sched_barrier(0);
+            }
           }
           ask(d);
         }
       }
     }
   }
+  settle();
 }
 
 // Which tile a workgroup takes: workgroups go to the eight XCDs in turn, an XCD takes an eighth of the tiles, and its tiles follow one another

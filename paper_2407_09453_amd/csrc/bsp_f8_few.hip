@@ -88,18 +88,20 @@ __device__ __forceinline__ f32x4_t few_low(const F8Low& low, int64_t row, int o)
   f32x4_t s = {};
   const int of = low.which[row];
   if (of < 0) return s;
-  const uint16_t* b = low.up + of * low.step + (int64_t)o * low.rank;  // (channels are padded to whole blocks)
+  // (channels are padded to whole blocks; 32 channels, sixteen ranks, 64 lanes of eight)
+  const uint16_t* b = low.up + of * low.step + (int64_t)(o & ~31) * low.rank + (o & 31) * 8;
   const float* u = low.u + row * low.rank;
 #pragma unroll 1
   for (int r = 0; r < low.rank; r += 8) {
     f32x4_t u0 = *(const f32x4_t*)(u + r), u1 = *(const f32x4_t*)(u + r + 4);
+#pragma unroll 3
     for (int k = 1; k < low.slices; ++k) {
       u0 += *(const f32x4_t*)(u + k * low.u_step + r);
       u1 += *(const f32x4_t*)(u + k * low.u_step + r + 4);
     }
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      const u32x4_t w = *(const u32x4_t*)(b + c * low.rank + r);
+      const u32x4_t w = *(const u32x4_t*)(b + ((r >> 4) * 64 + ((r >> 3) & 1) * 32 + c) * 8);
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[c] += __uint_as_float(w[e] << 16) * (e < 2 ? u0 : u1)[2 * (e & 1)] + __uint_as_float(w[e] & 0xFFFF0000u) * (e < 2 ? u0 : u1)[2 * (e & 1) + 1];
     }
