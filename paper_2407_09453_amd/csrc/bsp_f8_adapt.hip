@@ -203,7 +203,7 @@ template <int SRC, int NR>
 constexpr int kFragments = SRC == kF32 ? 1 : SRC == kBf16 || NR == 4 ? 2 : 4;  // of sixteen rows
 
 template <int SRC, int NR, bool SAVE>
-__global__ __launch_bounds__(512, NR == 4 ? 2 : 4) void adapt_down(DownArgs a) {
+__global__ __launch_bounds__(SAVE ? 256 : 512, SAVE ? (NR == 4 ? 2 : 3) : NR == 4 ? 2 : 4) void adapt_down(DownArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];  // [waves][rows of a block]; then sums [waves][NR][M][64][4]
   constexpr bool kCoded = SRC == kE4 || SRC == kE5;
   constexpr int M = kFragments<SRC, NR>, kParts = 4 / M, kSize = SRC == kF32 ? 4 : SRC == kBf16 ? 2 : 1;
@@ -223,6 +223,10 @@ __global__ __launch_bounds__(512, NR == 4 ? 2 : 4) void adapt_down(DownArgs a) {
   if constexpr (SAVE || kCoded)
 #pragma unroll
     for (int m = 0; m < M; ++m) t[m] = rows[m * 16 + r];
+  int64_t leaves[SAVE ? 2 * M : 1];  // the rows of the codes that this lane puts out
+  if constexpr (SAVE)
+#pragma unroll
+    for (int q = 0; q < 2 * M; ++q) leaves[q] = rows[q * 8 + (lane >> 3)];
   const bool saves = SAVE && blockIdx.z == 0;
   if (tile >= a.q.tiles[saves ? 1 : 0] || n <= 0) return;
   auto key = [](int row) { return kCoded ? (row >> 1) & 7 : row & 15; };
@@ -273,6 +277,8 @@ __global__ __launch_bounds__(512, NR == 4 ? 2 : 4) void adapt_down(DownArgs a) {
 #pragma unroll
       for (int m = 0; m < M; ++m) s[m] = a.scale[kb * a.srows + t[m]];
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    u32x4_t codes[SAVE ? M : 1][2];
+    int bytes[SAVE ? M : 1];
 #pragma unroll
     for (int m = 0; m < M; ++m) {
       const uint8_t* row = mine + (m * 16 + r) * kRow;
@@ -310,35 +316,48 @@ __global__ __launch_bounds__(512, NR == 4 ? 2 : 4) void adapt_down(DownArgs a) {
           if constexpr (SRC == kF32) acc[i][m] = mfma_bf16_16x16x32(wv[i][j], xl[j], acc[i][m]);
         }
       if constexpr (SAVE) {
-        if (saves && m * 16 < n) {
-          uint32_t most = 0;
-          float y[4][8];
+        uint32_t most = 0;
+        float y[4][8];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if constexpr (SRC == kBf16) unpack8(xv[j], y[j]);
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (SRC == kBf16) unpack8(xv[j], y[j]);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              if constexpr (SRC == kF32) y[j][k] = v[j][k];
-              most = max(most, f8_magnitude(y[j][k]));
-            }
+          for (int k = 0; k < 8; ++k) {
+            if constexpr (SRC == kF32) y[j][k] = v[j][k];
+            most = max(most, f8_magnitude(y[j][k]));
           }
-          const auto p = __builtin_amdgcn_permlane16_swap(most, most, false, false);
-          most = max(p[0], p[1]);
-          const auto o = __builtin_amdgcn_permlane32_swap(most, most, false, false);
-          most = max(o[0], o[1]);
-          const int b = a.e5 ? f8_scale_byte<true>(most) : f8_scale_byte<false>(most);
-          const float f = f8_inverse(b);
+        }
+        const auto p = __builtin_amdgcn_permlane16_swap(most, most, false, false);
+        most = max(p[0], p[1]);
+        const auto o = __builtin_amdgcn_permlane32_swap(most, most, false, false);
+        most = max(o[0], o[1]);
+        bytes[m] = a.e5 ? f8_scale_byte<true>(most) : f8_scale_byte<false>(most);
+        const float f = f8_inverse(bytes[m]);
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            u32x4_t c;
+        for (int q = 0; q < 2; ++q)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float* z = &y[2 * q + (k >> 1)][4 * (k & 1)];
-              c[k] = a.e5 ? f8_encode4<true>(z[0] * f, z[1] * f, z[2] * f, z[3] * f) : f8_encode4<false>(z[0] * f, z[1] * f, z[2] * f, z[3] * f);
-            }
-            if (m * 16 + r < n) *(u32x4_t*)(a.codes + t[m] * a.Kp + kb * 128 + q * 64 + g * 16) = c;
+          for (int k = 0; k < 4; ++k) {
+            const float* z = &y[2 * q + (k >> 1)][4 * (k & 1)];
+            codes[m][q][k] = a.e5 ? f8_encode4<true>(z[0] * f, z[1] * f, z[2] * f, z[3] * f) : f8_encode4<false>(z[0] * f, z[1] * f, z[2] * f, z[3] * f);
           }
-          if (g == 0 && m * 16 + r < n) a.to_scale[kb * a.srows + t[m]] = (uint8_t)b;
+      }
+    }
+    if constexpr (SAVE) {
+      if (saves) {  // through the wave's LDS, whose rows have been read: whole lines leave
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+          const int row = m * 16 + r;
+#pragma unroll
+          for (int q = 0; q < 2; ++q) *(u32x4_t*)(mine + row * 128 + (((4 * q + g) ^ ((row >> 1) & 7)) << 4)) = codes[m][q];
+          if (g == 0 && row < n) a.to_scale[kb * a.srows + t[m]] = (uint8_t)bytes[m];
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int q = 0; q < 2 * M; ++q) {
+          const int row = q * 8 + (lane >> 3), p = lane & 7;
+          const u32x4_t c = *(const u32x4_t*)(mine + row * 128 + ((p ^ ((row >> 1) & 7)) << 4));
+          if (row < n) *(u32x4_t*)(a.codes + leaves[q] * a.Kp + kb * 128 + p * 16) = c;
         }
       }
     }
@@ -375,7 +394,7 @@ __global__ __launch_bounds__(256) void adapt_sum(float* u, int slices, int64_t q
 
 template <int SRC, int NR, bool SAVE>
 int down_launch(const DownArgs& a, int T, int N, int slices, hipStream_t st) {
-  constexpr int M = kFragments<SRC, NR>, most = 8;
+  constexpr int M = kFragments<SRC, NR>, most = SAVE ? 4 : 8;
   constexpr int kBytes = 16 * M * (SRC == kF32 ? 512 : SRC == kBf16 ? 256 : 128), kWave = kBytes > NR * M * 1024 ? kBytes : NR * M * 1024;
   const int64_t tiles = f8_request_tiles(T, N) * (4 / M);
   int waves = most;  // a wave a block of columns at least
@@ -518,9 +537,6 @@ __global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
     const float* q = Q + t * a.Rp + piece * kMine;
     read_u(q, to.u);
     if (slices > 1) read_u(q + a.u_step, to.u2);
-    for (int s = 2; s < slices; ++s)  // (few rows)
-#pragma unroll
-      for (int e = 0; e < kMine; ++e) to.u[e] += q[s * a.u_step + e];
   };
   auto write = [&](int buf, int i, const Coming& from) {
     const bool have = i * kStep + row < k.rows;  // rows past the chunk add nothing, whatever they hold
@@ -677,24 +693,21 @@ int f8_launch_set(const F8Adapters& d, int slot, int rank, const void* A, int64_
   return launched();
 }
 
-// Into how many slices the columns are cut, of eight blocks at least, one a wave: few rows want as many workgroups as there are blocks,
-// many rows several rounds of workgroups, whose last round is then a small part.
-#ifndef LARGE_S
-#define LARGE_S 8
-#endif
+// Into how many slices the columns are cut, of eight blocks at least, one a wave: few rows want as many workgroups as the chip has CUs, many rows
+// several rounds of workgroups, whose last round is then a small part (8192 x 16384 bf16, rank 32: 88, 73, 66 us in one, two and four).
 int f8_down_slices(int T, int N, int K) {
   const int64_t tiles = f8_request_tiles(T, N);
-  const int most = T <= 32 ? 4 : tiles < 64 ? 2 : LARGE_S;
   int slices = 1;
-  while (slices < most && tiles * slices < 1024 && f8_blocks(K) >= 16 * slices) slices *= 2;
+  while (slices < 8 && tiles * slices < (tiles < 64 ? 256 : 1024) && f8_blocks(K) >= 16 * slices) slices *= 2;
   return slices;
 }
-// ... and how many of them are left to whoever reads u: two, or with few rows four, cost less there than a launch that adds them
-int f8_low_slices(int T, int N, int K) {
+// ... and how many of them are left to whoever reads u.  A product reads each once for every tile: on few rows that costs less than a launch that adds
+// them.  The gradients hold two on their way, and read them for every block of 128 columns.
+int f8_low_slices(int T, int N, int K, bool grad) {
   const int slices = f8_down_slices(T, N, K);
-  return slices > 2 && T > 32 ? 1 : slices;
+  return slices > 2 && (grad || f8_request_tiles(T, N) >= 64) ? 1 : slices;
 }
-int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, uint8_t* codes, uint8_t* scale, hipStream_t st) {
+int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, bool grad, uint8_t* codes, uint8_t* scale, hipStream_t st) {
   DownArgs a{};
   a.X = x.X, a.scale = x.scale, a.ld = x.ld, a.srows = f8_scale_rows(T), a.down = transposed ? d.b_t : d.a, a.factor = d.scale, a.u = u, a.q = q;
   a.T = T, a.K = transposed ? d.O : d.I, a.Kp = transposed ? d.Op : d.Ip, a.Rp = d.Rp, a.e5 = x.e5, a.codes = codes, a.to_scale = scale;
@@ -709,7 +722,7 @@ int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T
     case BSP_E4M3: rc = down_rank<kE4, false>(a, T, d.N, slices, st); break;
     default: rc = down_rank<kE5, false>(a, T, d.N, slices, st);
   }
-  if (rc != BSP_OK || f8_low_slices(T, d.N, a.K) == slices) return rc;
+  if (rc != BSP_OK || f8_low_slices(T, d.N, a.K, grad) == slices) return rc;
   const int64_t quads = (int64_t)T * d.Rp / 4;
   hipLaunchKernelGGL(adapt_sum, f8_grid((quads + 255) / 256), dim3(256), 0, st, u, slices, quads);
   return launched();
@@ -723,7 +736,7 @@ int f8_launch_adapt_grad(const F8Adapters& d, const uint16_t* dY, int64_t ldy, c
                          float* part, float* dA, float* dB, hipStream_t st) {
   GradArgs a{};
   a.q = q, a.dY = dY, a.X = x.X, a.scale = x.scale, a.ldy = ldy, a.ldx = x.ld, a.srows = f8_scale_rows(T), a.u = u, a.v = v, a.dA = dA, a.dB = dB, a.part = part;
-  a.u_step = (int64_t)T * d.Rp, a.u_slices = f8_low_slices(T, d.N, d.I), a.v_slices = f8_low_slices(T, d.N, d.O), a.Rp = d.Rp;
+  a.u_step = (int64_t)T * d.Rp, a.u_slices = f8_low_slices(T, d.N, d.I, true), a.v_slices = f8_low_slices(T, d.N, d.O, true), a.Rp = d.Rp;
   a.N = d.N, a.R = d.R, a.I = d.I, a.O = d.O, a.blocks_o = f8_blocks(d.O), a.chunk = chunk_of(T, d.I, d.O);
   a.src = x.dtype == BSP_BF16 ? kBf16 : x.dtype == BSP_E4M3 ? kE4 : kE5;
   const int64_t chunks = (int64_t)T / a.chunk + (T < d.N ? T : d.N);

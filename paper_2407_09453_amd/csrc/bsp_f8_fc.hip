@@ -173,12 +173,13 @@ __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT
       uint64_t todo = all;
       int now[kAhead];
       u32x4_t w[kAhead][MO];
+      // (asked for without a condition, once more the last one's where there is no next: a wait can then be by count)
       auto ask = [&](int d) {
-        now[d] = -1;
-        if (!todo) return;
-        now[d] = __builtin_amdgcn_readlane(of, __builtin_ctzll(todo));
-        todo &= ~__ballot(of == now[d]);
-        const uint16_t* b = up + now[d] * low.step + k * 32;
+        const bool more = todo != 0;
+        const int next = __builtin_amdgcn_readlane(of, more ? __builtin_ctzll(todo) : __builtin_ctzll(all));
+        todo &= ~__ballot(of == next);
+        now[d] = more ? next : -1;
+        const uint16_t* b = up + next * low.step + k * 32;
 #pragma unroll
         for (int o = 0; o < MO; ++o) w[d][o] = *(const u32x4_t*)(b + (int64_t)o * 32 * low.rank);
       };
@@ -187,7 +188,7 @@ __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT
       while (now[0] >= 0) {
 #pragma unroll
         for (int d = 0; d < kAhead; ++d) {
-          if (now[d] < 0) break;
+          if (now[d] >= 0) {
           const bool mine = of == now[d];
           // an exponent of ones in any half of the weights' words
           u16x2_t most = {0, 0};
@@ -215,6 +216,7 @@ __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT
               for (int e = 0; e < 16; ++e) acc[o][m][e] += mine ? sum[e] : 0.f;
               __builtin_amdgcn_sched_barrier(0);
             }
+          }
           }
           ask(d);
         }
