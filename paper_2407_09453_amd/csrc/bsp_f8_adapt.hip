@@ -698,7 +698,7 @@ int f8_launch_set(const F8Adapters& d, int slot, int rank, const void* A, int64_
 int f8_down_slices(int T, int N, int K) {
   const int64_t tiles = f8_request_tiles(T, N);
   int slices = 1;
-  while (slices < 8 && tiles * slices < (tiles < 64 ? 256 : 1024) && f8_blocks(K) >= 16 * slices) slices *= 2;
+  while (slices < 4 && tiles * slices < (tiles < 64 ? 256 : 1024) && f8_blocks(K) >= 16 * slices) slices *= 2;
   return slices;
 }
 // ... and how many of them are left to whoever reads u.  A product reads each once for every tile: on few rows that costs less than a launch that adds

@@ -141,10 +141,18 @@ struct LowParts {
 };
 __device__ __forceinline__ LowParts low_parts(const F8Low& low, const float* u) {
   f32x4_t x0 = *(const f32x4_t*)u, x1 = *(const f32x4_t*)(u + 4);
-#pragma unroll 4
-  for (int s = 1; s < low.slices; ++s) {
-    x0 += *(const f32x4_t*)(u + s * low.u_step);
-    x1 += *(const f32x4_t*)(u + s * low.u_step + 4);
+  if (low.slices > 1) {  // two or four, asked for together
+    f32x4_t y0[3], y1[3];
+#pragma unroll
+    for (int s = 0; s < 3; ++s) {
+      const float* v = u + (s + 1 < low.slices ? s + 1 : 1) * low.u_step;
+      y0[s] = *(const f32x4_t*)v, y1[s] = *(const f32x4_t*)(v + 4);
+    }
+    x0 += y0[0], x1 += y1[0];
+    if (low.slices > 2) {
+      x0 += y0[1], x1 += y1[1];
+      x0 += y0[2], x1 += y1[2];
+    }
   }
   LowParts p;
 #pragma unroll
@@ -160,66 +168,81 @@ template <int MO, int MT>
 __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT], int T, int64_t t0, int o0) {
   const int lane = threadIdx.x & 63;
   const uint16_t* up = low.up + (int64_t)o0 * low.rank + lane * 8;  // (as the instruction takes them: 32 channels, sixteen ranks, 64 lanes)
+  const float* u[MT];
+  int of[MT];
+  uint64_t all[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const int64_t t = t0 + m * 32 + (lane & 31) < T ? t0 + m * 32 + (lane & 31) : T - 1;
-    const float* u = low.u + t * low.rank + (lane >> 5) * 8;
-    const int of = low.which[t];
-    const uint64_t all = __ballot(of >= 0);
-    if (!all) continue;
-    for (int k = 0; k < low.rank; k += 16) {
-      const LowParts p = low_parts(low, u + k);
-      constexpr int kAhead = MO == 4 ? 2 : 8;
-      uint64_t todo = all;
-      int now[kAhead];
-      u32x4_t w[kAhead][MO];
-      // (asked for without a condition, once more the last one's where there is no next: a wait can then be by count)
-      auto ask = [&](int d) {
-        const bool more = todo != 0;
-        const int next = __builtin_amdgcn_readlane(of, more ? __builtin_ctzll(todo) : __builtin_ctzll(all));
-        todo &= ~__ballot(of == next);
-        now[d] = more ? next : -1;
-        const uint16_t* b = up + next * low.step + k * 32;
+    u[m] = low.u + t * low.rank + (lane >> 5) * 8;
+    of[m] = low.which[t];
+  }
 #pragma unroll
-        for (int o = 0; o < MO; ++o) w[d][o] = *(const u32x4_t*)(b + (int64_t)o * 32 * low.rank);
-      };
+  for (int m = 0; m < MT; ++m) all[m] = __ballot(of[m] >= 0);
+  for (int k = 0; k < low.rank; k += 16) {
+    constexpr int kAhead = MO == 4 ? 2 : MT == 2 ? 4 : 8;
+    uint64_t todo[MT];
 #pragma unroll
-      for (int d = 0; d < kAhead; ++d) ask(d);
-      while (now[0] >= 0) {
+    for (int m = 0; m < MT; ++m) todo[m] = all[m];
+    int now[kAhead], last = 0;
+    u32x4_t w[kAhead][MO];
+    // (asked for without a condition, once more the last one's where there is no next: a wait can then be by count)
+    auto ask = [&](int d) {
+      int next = -1;
 #pragma unroll
-        for (int d = 0; d < kAhead; ++d) {
-          if (now[d] >= 0) {
-          const bool mine = of == now[d];
+      for (int m = MT - 1; m >= 0; --m)
+        if (todo[m]) next = __builtin_amdgcn_readlane(of[m], __builtin_ctzll(todo[m]));
+#pragma unroll
+      for (int m = 0; m < MT; ++m) todo[m] &= ~__ballot(of[m] == next);
+      now[d] = next;
+      last = next >= 0 ? next : last;
+      const uint16_t* b = up + last * low.step + k * 32;
+#pragma unroll
+      for (int o = 0; o < MO; ++o) w[d][o] = *(const u32x4_t*)(b + (int64_t)o * 32 * low.rank);
+    };
+#pragma unroll
+    for (int d = 0; d < kAhead; ++d) ask(d);
+    LowParts p[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) p[m] = low_parts(low, u[m] + k);
+    while (now[0] >= 0) {
+#pragma unroll
+      for (int d = 0; d < kAhead; ++d) {
+        if (now[d] >= 0) {
           // an exponent of ones in any half of the weights' words
           u16x2_t most = {0, 0};
 #pragma unroll
           for (int o = 0; o < MO; ++o)
 #pragma unroll
             for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2_t, w[d][o][e] & 0x7F807F80u));
-          const bool odd = most.x == 0x7F80 || most.y == 0x7F80;
-          if (__all(mine) || !__any(odd)) {
-            u32x4_t high, rest;
+          const bool odd = __any(most.x == 0x7F80 || most.y == 0x7F80);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) high[e] = mine ? p.high[e] : 0, rest[e] = mine ? p.rest[e] : 0;
+          for (int m = 0; m < MT; ++m) {
+            const bool mine = of[m] == now[d];
+            if (!__any(mine)) continue;
+            if (!odd || __all(mine)) {
+              u32x4_t high, rest;
 #pragma unroll
-            for (int o = 0; o < MO; ++o) acc[o][m] = mfma_bf16_32x32x16(w[d][o], high, acc[o][m]);
+              for (int e = 0; e < 4; ++e) high[e] = mine ? p[m].high[e] : 0, rest[e] = mine ? p[m].rest[e] : 0;
 #pragma unroll
-            for (int o = 0; o < MO; ++o) acc[o][m] = mfma_bf16_32x32x16(w[d][o], rest, acc[o][m]);
-          } else {
-            settle();
+              for (int o = 0; o < MO; ++o) acc[o][m] = mfma_bf16_32x32x16(w[d][o], high, acc[o][m]);
 #pragma unroll
-            for (int o = 0; o < MO; ++o) {
-              f32x16_t sum = mfma_bf16_32x32x16(w[d][o], p.high, f32x16_t{});
-              sum = mfma_bf16_32x32x16(w[d][o], p.rest, sum);
-              asm volatile("" : "+v"(sum));  // (read in the block of the instruction that makes it)
+              for (int o = 0; o < MO; ++o) acc[o][m] = mfma_bf16_32x32x16(w[d][o], rest, acc[o][m]);
+            } else {
+              settle();
 #pragma unroll
-              for (int e = 0; e < 16; ++e) acc[o][m][e] += mine ? sum[e] : 0.f;
-              __builtin_amdgcn_sched_barrier(0);
+              for (int o = 0; o < MO; ++o) {
+                f32x16_t sum = mfma_bf16_32x32x16(w[d][o], p[m].high, f32x16_t{});
+                sum = mfma_bf16_32x32x16(w[d][o], p[m].rest, sum);
+                asm volatile("" : "+v"(sum));  // (read in the block of the instruction that makes it)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[o][m][e] += mine ? sum[e] : 0.f;
+                __builtin_amdgcn_sched_barrier(0);
+              }
             }
           }
-          }
-          ask(d);
         }
+        ask(d);
       }
     }
   }
