@@ -475,34 +475,29 @@ __device__ __forceinline__ f32x16_t mfma32(u32x4_t a, u32x4_t b, f32x16_t c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 
-// A workgroup: 128 columns of dY (dB) or of X (dA), a chunk of an adapter's rows, and RP ranks.  Four waves of 32 columns each; the other operand
-// is u or v, its high parts beside its low parts in a row of 2 RP bf16.
-template <int RP>
-__global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
+// 128 columns of one side, dY (dB) or X (dA), with a chunk of an adapter's rows and RP ranks.  Four waves of 32 columns each; the other operand
+// is u or v, its high parts beside its low parts in a row of 2 RP bf16.  CODED: the rows are codes; WHOLE: all 128 columns are there.
+template <int RP, bool CODED, bool WHOLE>
+__device__ __forceinline__ void grad_side(const GradArgs& a, const Chunk& k, bool in_y, int kb, uint8_t* lds) {
   constexpr int NT = RP / 16;               // tiles of 32 columns of u: high parts, then low
   constexpr int kQ = 4 * RP + 16;           // bytes from row to row of u in LDS
   constexpr int kP = kStep * 256, kBuffer = kP + kStep * kQ, kMine = RP / 8;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kBuffer];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Chunk k = find_chunk(a.q, a.N, a.chunk, blockIdx.y);
-  if (k.of >= a.N) return;
-  const bool in_y = (int)blockIdx.x < a.blocks_o;
-  const int kb = in_y ? blockIdx.x : blockIdx.x - a.blocks_o, columns = in_y ? a.O : a.I, c0 = kb * 128;
-  const int src = in_y ? (int)kBf16 : a.src;
+  const int columns = in_y ? a.O : a.I, c0 = kb * 128;
   const void* P = in_y ? (const void*)a.dY : a.X;
   const int64_t ld = in_y ? a.ldy : a.ldx;
   const int r0 = blockIdx.z * RP, slices = in_y ? a.u_slices : a.v_slices;
-  const float* Q = (in_y ? a.u : a.v) + r0;
-  const bool whole = c0 + 128 <= columns;
-  // what this thread brings: sixteen columns of a row, and kMine values of u
-  const int row = tid >> 3, piece = tid & 7;
-  // Two steps are on their way to registers while a third is multiplied.
+  // what this thread brings: sixteen columns of a row, and kMine values of u.  Two steps are on their way to registers while a third is
+  // multiplied; nothing about that is conditional, and nothing looks at what is on its way: either would wait for it.
+  const int row = tid >> 3, piece = tid & 7, c = c0 + piece * 16;
+  const float* Q = (in_y ? a.u : a.v) + r0 + piece * kMine;
+  const int64_t second = slices > 1 ? a.u_step : 0;
   struct Coming {
     u32x4_t p[2];
-    float u[kMine], u2[kMine];  // of two slices (nothing here looks at what is on its way: that would wait for it)
+    float u[kMine], u2[kMine];  // of two slices
     int s;
   } in[2];
-  auto place = [&](int i) { return a.q.order[k.begin + (i * kStep + row < k.rows ? i * kStep + row : k.rows - 1)]; };
+  auto place = [&](int i) { return a.q.order[k.begin + (i * kStep + row < k.rows ? i * kStep + row : k.rows - 1)]; };  // (past the last row: the last)
   auto read_u = [&](const float* q, float* u) {
     if constexpr (kMine >= 4) {
 #pragma unroll
@@ -516,37 +511,35 @@ __global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
     }
   };
   auto ask = [&](int64_t t, Coming& to) {
-    const int c = c0 + piece * 16;
-    if (src == kBf16) {
-      if (whole) {
-        const uint16_t* x = (const uint16_t*)P + t * ld + c;
-        to.p[0] = *(const f8_any2_t*)x;
-        to.p[1] = *(const f8_any2_t*)(x + 8);
-      } else {
-        float v[8];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          load8<false>((const uint16_t*)P + t * ld, c + 8 * h, columns, v);
-          to.p[h] = pack8(v);
-        }
-      }
-    } else {
+    if constexpr (CODED) {
       to.p[0] = *(const u32x4_t*)((const uint8_t*)P + t * ld + c);
       to.s = a.scale[kb * a.srows + t];
+    } else if constexpr (WHOLE) {
+      const uint16_t* x = (const uint16_t*)P + t * ld + c;
+      to.p[0] = *(const f8_any2_t*)x;
+      to.p[1] = *(const f8_any2_t*)(x + 8);
+    } else {
+      float v[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        load8<false>((const uint16_t*)P + t * ld, c + 8 * h, columns, v);
+        to.p[h] = pack8(v);
+      }
     }
-    const float* q = Q + t * a.Rp + piece * kMine;
-    read_u(q, to.u);
-    if (slices > 1) read_u(q + a.u_step, to.u2);
+    read_u(Q + t * a.Rp, to.u);
+    read_u(Q + t * a.Rp + second, to.u2);
   };
   auto write = [&](int buf, int i, const Coming& from) {
     const bool have = i * kStep + row < k.rows;  // rows past the chunk add nothing, whatever they hold
     uint8_t* to = lds + buf * kBuffer;
-    u32x4_t w[2] = {from.p[0], from.p[1]};
-    if (src != kBf16) {
+    u32x4_t w[2];
+    if constexpr (CODED) {
       const float f = __uint_as_float((uint32_t)from.s << 23);
-      const u32x4_t c = from.p[0];
-      w[0] = src == kE5 ? f8_decode_bf16x8<true>(c.x, c.y, f) : f8_decode_bf16x8<false>(c.x, c.y, f);
-      w[1] = src == kE5 ? f8_decode_bf16x8<true>(c.z, c.w, f) : f8_decode_bf16x8<false>(c.z, c.w, f);
+      const u32x4_t x = from.p[0];
+      if (a.src == kE5) w[0] = f8_decode_bf16x8<true>(x.x, x.y, f), w[1] = f8_decode_bf16x8<true>(x.z, x.w, f);
+      else w[0] = f8_decode_bf16x8<false>(x.x, x.y, f), w[1] = f8_decode_bf16x8<false>(x.z, x.w, f);
+    } else {
+      w[0] = from.p[0], w[1] = from.p[1];
     }
     const int key = (row & 3) << 1 | ((row >> 3) & 1);
 #pragma unroll
@@ -566,7 +559,6 @@ __global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
   const int at_q = kP + trow * kQ + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
   f32x16_t acc[NT] = {};
   const int steps = (k.rows + kStep - 1) / kStep;
-  // (place clamps to the chunk's last row, so steps past the last ask for that)
   ask(place(0), in[0]);
   ask(place(1), in[1]);
   int next = place(2);
@@ -582,22 +574,18 @@ __global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) acc[n] = mfma32(x, read_columns<kQ>(from + h * 16 * kQ + at_q + n * 64), acc[n]);
     }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) asm volatile("" : "+a"(acc[n]));
-    asm volatile("s_nop 15\n\ts_nop 7");  // (see settle: what follows has ways that meet again)
-    if (i + 1 < steps) {
-      write((i + 1) & 1, i + 1, coming);
-      if (i + 3 < steps) {
-        ask(next, coming);
-        next = place(i + 4);
-      }
-    }
+    write((i + 1) & 1, i + 1, coming);
+    ask(next, coming);
+    next = place(i + 4);
     __syncthreads();
   };
-  for (int i = 0; i < steps; i += 2) {
+  for (int i = 0; i < steps; i += 2) {  // (a step past the last multiplies zeros)
     step(i, in[1]);
-    if (i + 1 < steps) step(i + 1, in[0]);
+    step(i + 1, in[0]);
   }
+#pragma unroll
+  for (int n = 0; n < NT; ++n) asm volatile("" : "+a"(acc[n]));
+  asm volatile("s_nop 15\n\ts_nop 7");  // (see settle)
   // high and low parts together
   constexpr int kTiles = RP == 16 ? 1 : NT / 2;
   if constexpr (RP == 16) {
@@ -616,12 +604,24 @@ __global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
     if (r >= a.R || (RP == 16 && (lane & 16))) continue;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const int c = c0 + wave * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
-      if (c >= columns) continue;
-      if (in_y) to_b[(int64_t)c * a.R + r] = acc[n][e];
-      else to_a[(int64_t)r * a.I + c] = acc[n][e];
+      const int col = c0 + wave * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
+      if (col >= columns) continue;
+      if (in_y) to_b[(int64_t)col * a.R + r] = acc[n][e];
+      else to_a[(int64_t)r * a.I + col] = acc[n][e];
     }
   }
+}
+
+template <int RP>
+__global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * (kStep * 256 + kStep * (4 * RP + 16))];
+  const Chunk k = find_chunk(a.q, a.N, a.chunk, blockIdx.y);
+  if (k.of >= a.N) return;
+  const bool in_y = (int)blockIdx.x < a.blocks_o;
+  const int kb = in_y ? blockIdx.x : blockIdx.x - a.blocks_o;
+  if (!in_y && a.src != kBf16) grad_side<RP, true, true>(a, k, in_y, kb, lds);
+  else if (kb * 128 + 128 <= (in_y ? a.O : a.I)) grad_side<RP, false, true>(a, k, in_y, kb, lds);
+  else grad_side<RP, false, false>(a, k, in_y, kb, lds);
 }
 
 // Adapters of several chunks: their sums in order; of none: zeros.

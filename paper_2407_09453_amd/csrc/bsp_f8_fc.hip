@@ -164,6 +164,48 @@ __device__ __forceinline__ LowParts low_parts(const F8Low& low, const float* u) 
   return p;
 }
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2_t;
+// A fragment's rows by themselves, where they belong to more than sixteen adapters: a lane multiplies its row's u with its own adapter's weights,
+// sixteen channels of every 32, with ordinary instructions (us, an adapter at a time and so: 64 rows of 16 adapters, 512 -> 16384 20.1 and 20.6, of 32
+// 28.7 and 21.4; 2048 x 4096 -> 4096 66 and 79, 82 and 78).  Not in the widest tiles (16384 x 4096 -> 4096 of 32: 428 and 496).
+constexpr int kManyAdapters = 16;
+template <int MO, int MT>
+__device__ __forceinline__ void add_low_rows(const F8Low& low, f32x16_t (&acc)[MO][MT], int m, const float* u, int of, int o0) {
+  const int half = (threadIdx.x & 63) >> 5;
+  const uint16_t* b = low.up + (of < 0 ? 0 : of) * low.step + (int64_t)o0 * low.rank + 4 * half * 8;
+  for (int k = 0; k < low.rank; k += 16) {
+    f32x4_t x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = *(const f32x4_t*)(u + k + 4 * e);
+    for (int s = 1; s < low.slices; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += *(const f32x4_t*)(u + s * low.u_step + k + 4 * e);
+#pragma unroll
+    for (int o = 0; o < MO; ++o)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint16_t* c = b + (int64_t)o * 32 * low.rank + k * 32 + q * 64;
+        u32x4_t w[4][2];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) w[e][h] = *(const u32x4_t*)(c + e * 8 + h * 256);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float s = 0.f;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              s = fmaf(__uint_as_float(w[e][h][i] << 16), x[2 * h + (i >> 1)][2 * (i & 1)], s);
+              s = fmaf(__uint_as_float(w[e][h][i] & 0xFFFF0000u), x[2 * h + (i >> 1)][2 * (i & 1) + 1], s);
+            }
+          acc[o][m][4 * q + e] += of >= 0 ? s : 0.f;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+  }
+}
+
 template <int MO, int MT>
 __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT], int T, int64_t t0, int o0) {
   const int lane = threadIdx.x & 63;
@@ -171,6 +213,7 @@ __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT
   const float* u[MT];
   int of[MT];
   uint64_t all[MT];
+  settle();
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const int64_t t = t0 + m * 32 + (lane & 31) < T ? t0 + m * 32 + (lane & 31) : T - 1;
@@ -178,7 +221,16 @@ __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT
     of[m] = low.which[t];
   }
 #pragma unroll
-  for (int m = 0; m < MT; ++m) all[m] = __ballot(of[m] >= 0);
+  for (int m = 0; m < MT; ++m) {
+    all[m] = __ballot(of[m] >= 0);
+    if constexpr (MO < 4) {
+      uint64_t rest = all[m];
+      for (int n = 0; rest && n < kManyAdapters; ++n) rest &= ~__ballot(of[m] == __builtin_amdgcn_readlane(of[m], __builtin_ctzll(rest)));
+      if (!rest) continue;
+      all[m] = 0;
+      add_low_rows<MO, MT>(low, acc, m, u[m] - (lane >> 5) * 8, of[m], o0);
+    }
+  }
   for (int k = 0; k < low.rank; k += 16) {
     constexpr int kAhead = MO == 4 ? 2 : MT == 2 ? 4 : 8;
     uint64_t todo[MT];
