@@ -336,8 +336,7 @@ F8Requests f8_requests_of(const bsp_f8_requests* r);
 F8Adapters f8_adapters_of(const bsp_f8_adapters* d);
 int f8_launch_plan(const bsp_f8_requests* r, const void* which, bool wide, hipStream_t st);
 int f8_launch_set(const F8Adapters& d, int slot, int rank, const void* A, int64_t lda, const void* B, int64_t ldb, bool f32, float scale, hipStream_t st);
-int f8_down_slices(int T, int N, int K);  // of u in memory
-int f8_low_slices(int T, int N, int K, bool grad);  // of u as it is left for a product, or for the gradients
+int f8_down_slices(int T, int N, int K, bool grad);  // of u: up to eight for a product, two for the gradients
 // codes, scale: where values are to become codes (of x.e5) on the way, too; or null
 int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, bool grad, uint8_t* codes, uint8_t* scale, hipStream_t st);
 int64_t f8_adapt_part_bytes(const F8Adapters& d, int T);

@@ -237,7 +237,11 @@ __global__ __launch_bounds__(SAVE ? 256 : 512, SAVE ? (NR == 4 ? 2 : 3) : NR == 
   const uint16_t* w = a.down + (int64_t)(of < 0 ? 0 : of) * a.Rp * a.Kp + (blockIdx.z * NR * 4 * 64 + lane) * 8;
   const int nb = a.Kp >> 7, kb0 = blockIdx.y * a.per, kb1 = kb0 + a.per < nb ? kb0 + a.per : nb;
   f32x4_t acc[NR][M] = {};
-  for (int kb = kb0 + wave; kb < kb1; kb += waves) {
+  // Workgroups begin at different columns: of rows a power of two apart those at one column lie in one channel of the L2, and all would ask that one
+  // (8192 x 16384 of one adapter 255 us, of two 98).
+  const int blocks = kb1 - kb0, turn = blocks > 0 ? (int)blockIdx.x * waves % blocks : 0;
+  for (int i = wave; i < blocks; i += waves) {
+    const int kb = kb0 + (i + turn < blocks ? i + turn : i + turn - blocks);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the last block has been read
     if (kCoded || (a.aligned && kb * 128 + 128 <= a.K)) {
 #pragma unroll
@@ -380,16 +384,6 @@ __global__ __launch_bounds__(SAVE ? 256 : 512, SAVE ? (NR == 4 ? 2 : 3) : NR == 
     const int64_t at = (int64_t)blockIdx.y * a.T + rows[row];
     *(f32x4_t*)(a.u + at * a.Rp + (blockIdx.z * NR + i / (M * 64)) * 16 + ((i >> 4) & 3) * 4) = sum * factor;
   }
-}
-
-// u = the sum of its slices, in their order, in the first one's place
-__global__ __launch_bounds__(256) void adapt_sum(float* u, int slices, int64_t quads) {
-  const int64_t i = ((int64_t)blockIdx.y * kGridX + blockIdx.x) * 256 + threadIdx.x;
-  if (i >= quads) return;
-  f32x4_t s = *(const f32x4_t*)(u + i * 4);
-#pragma unroll 8
-  for (int k = 1; k < slices; ++k) s += *(const f32x4_t*)(u + (k * quads + i) * 4);
-  *(f32x4_t*)(u + i * 4) = s;
 }
 
 template <int SRC, int NR, bool SAVE>
@@ -693,19 +687,15 @@ int f8_launch_set(const F8Adapters& d, int slot, int rank, const void* A, int64_
   return launched();
 }
 
-// Into how many slices the columns are cut, of eight blocks at least, one a wave: few rows want as many workgroups as the chip has CUs, many rows
-// several rounds of workgroups, whose last round is then a small part (8192 x 16384 bf16, rank 32: 88, 73, 66 us in one, two and four).
-int f8_down_slices(int T, int N, int K) {
+// Into how many slices the columns are cut, of eight blocks at least, one a wave: few rows want as many workgroups as the chip has CUs.  Who reads u
+// adds them: a product once for every tile of results, the gradients, which hold two on their way, for every block of 128 columns.  (8192 x 16384
+// bf16, rank 32: 88, 73, 66 us in one, two and four; a launch that adds four takes 5.)
+int f8_down_slices(int T, int N, int K, bool grad) {
   const int64_t tiles = f8_request_tiles(T, N);
+  const int most = grad || tiles >= 64 ? 2 : 8;
   int slices = 1;
-  while (slices < 4 && tiles * slices < (tiles < 64 ? 256 : 1024) && f8_blocks(K) >= 16 * slices) slices *= 2;
+  while (slices < most && tiles * slices < 256 && f8_blocks(K) >= 16 * slices) slices *= 2;
   return slices;
-}
-// ... and how many of them are left to whoever reads u.  A product reads each once for every tile: on few rows that costs less than a launch that adds
-// them.  The gradients hold two on their way, and read them for every block of 128 columns.
-int f8_low_slices(int T, int N, int K, bool grad) {
-  const int slices = f8_down_slices(T, N, K);
-  return slices > 2 && (grad || f8_request_tiles(T, N) >= 64) ? 1 : slices;
 }
 int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, bool grad, uint8_t* codes, uint8_t* scale, hipStream_t st) {
   DownArgs a{};
@@ -713,19 +703,14 @@ int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T
   a.T = T, a.K = transposed ? d.O : d.I, a.Kp = transposed ? d.Op : d.Ip, a.Rp = d.Rp, a.e5 = x.e5, a.codes = codes, a.to_scale = scale;
   const int64_t size = x.dtype == BSP_F32 ? 4 : x.dtype == BSP_BF16 ? 2 : 1;
   a.aligned = (((uintptr_t)x.X | (uintptr_t)(x.ld * size)) & 15) == 0;
-  const int slices = f8_down_slices(T, d.N, a.K);
+  const int slices = f8_down_slices(T, d.N, a.K, grad);
   a.per = (f8_blocks(a.K) + slices - 1) / slices;
-  int rc;
   switch (x.dtype) {
-    case BSP_BF16: rc = codes ? down_rank<kBf16, true>(a, T, d.N, slices, st) : down_rank<kBf16, false>(a, T, d.N, slices, st); break;
-    case BSP_F32: rc = codes ? down_rank<kF32, true>(a, T, d.N, slices, st) : down_rank<kF32, false>(a, T, d.N, slices, st); break;
-    case BSP_E4M3: rc = down_rank<kE4, false>(a, T, d.N, slices, st); break;
-    default: rc = down_rank<kE5, false>(a, T, d.N, slices, st);
+    case BSP_BF16: return codes ? down_rank<kBf16, true>(a, T, d.N, slices, st) : down_rank<kBf16, false>(a, T, d.N, slices, st);
+    case BSP_F32: return codes ? down_rank<kF32, true>(a, T, d.N, slices, st) : down_rank<kF32, false>(a, T, d.N, slices, st);
+    case BSP_E4M3: return down_rank<kE4, false>(a, T, d.N, slices, st);
+    default: return down_rank<kE5, false>(a, T, d.N, slices, st);
   }
-  if (rc != BSP_OK || f8_low_slices(T, d.N, a.K, grad) == slices) return rc;
-  const int64_t quads = (int64_t)T * d.Rp / 4;
-  hipLaunchKernelGGL(adapt_sum, f8_grid((quads + 255) / 256), dim3(256), 0, st, u, slices, quads);
-  return launched();
 }
 
 int64_t f8_adapt_part_bytes(const F8Adapters& d, int T) {
@@ -736,7 +721,7 @@ int f8_launch_adapt_grad(const F8Adapters& d, const uint16_t* dY, int64_t ldy, c
                          float* part, float* dA, float* dB, hipStream_t st) {
   GradArgs a{};
   a.q = q, a.dY = dY, a.X = x.X, a.scale = x.scale, a.ldy = ldy, a.ldx = x.ld, a.srows = f8_scale_rows(T), a.u = u, a.v = v, a.dA = dA, a.dB = dB, a.part = part;
-  a.u_step = (int64_t)T * d.Rp, a.u_slices = f8_low_slices(T, d.N, d.I, true), a.v_slices = f8_low_slices(T, d.N, d.O, true), a.Rp = d.Rp;
+  a.u_step = (int64_t)T * d.Rp, a.u_slices = f8_down_slices(T, d.N, d.I, true), a.v_slices = f8_down_slices(T, d.N, d.O, true), a.Rp = d.Rp;
   a.N = d.N, a.R = d.R, a.I = d.I, a.O = d.O, a.blocks_o = f8_blocks(d.O), a.chunk = chunk_of(T, d.I, d.O);
   a.src = x.dtype == BSP_BF16 ? kBf16 : x.dtype == BSP_E4M3 ? kE4 : kE5;
   const int64_t chunks = (int64_t)T / a.chunk + (T < d.N ? T : d.N);

@@ -124,7 +124,7 @@ int check_requests(const bsp_f8_requests* r) {
   return aligned(r->plan, 16) ? BSP_OK : BSP_ERR_ALIGN;
 }
 int64_t in16(int64_t bytes) { return (bytes + 15) & ~(int64_t)15; }
-int64_t low_bytes(const F8Adapters& d, int T, int K) { return (int64_t)T * d.Rp * 4 * f8_down_slices(T, d.N, K); }
+int64_t low_bytes(const F8Adapters& d, int T, int K, bool grad) { return (int64_t)T * d.Rp * 4 * f8_down_slices(T, d.N, K, grad); }
 
 int64_t codes_bytes(int T, int K) { return ((int64_t)T * f8_blocks(K) * F8_BLOCK) + f8_scale_rows(T) * f8_blocks(K); }
 
@@ -324,7 +324,7 @@ int bsp_f8_requests_plan(const bsp_f8_requests* r, const void* which, int32_t wh
 int bsp_f8_fc_adapted_workspace(const bsp_weights_f8* w, int32_t transposed, int32_t T, int32_t coded, const bsp_f8_adapters* adapters, int64_t* bytes) {
   int rc = bsp_f8_fc_workspace(w, transposed, T, coded, bytes);
   if (rc == BSP_OK) rc = check_adapters(adapters);
-  if (rc == BSP_OK) *bytes = in16(*bytes) + low_bytes(f8_adapters_of(adapters), T, transposed ? w->O : w->I);
+  if (rc == BSP_OK) *bytes = in16(*bytes) + low_bytes(f8_adapters_of(adapters), T, transposed ? w->O : w->I, false);
   return rc;
 }
 
@@ -351,7 +351,7 @@ int bsp_f8_fc_adapted(const bsp_weights_f8* w, int32_t transposed, const bsp_cod
   const F8Rows rows = rows_of(w, transposed != 0);
   const F8Adapters d = f8_adapters_of(adapters);
   const int64_t sums = sums_bytes(rows, T), codes = X || in_kernel(values, x_dtype, ldx, T, K) ? 0 : codes_bytes(T, K);
-  rc = check_workspace(workspace, workspace_bytes, in16(sums + codes) + low_bytes(d, T, K));
+  rc = check_workspace(workspace, workspace_bytes, in16(sums + codes) + low_bytes(d, T, K, false));
   if (rc != BSP_OK) return rc;
   hipStream_t st = (hipStream_t)stream;
   const F8Requests who = f8_requests_of(requests);
@@ -362,7 +362,7 @@ int bsp_f8_fc_adapted(const bsp_weights_f8* w, int32_t transposed, const bsp_cod
   uint8_t *to = codes ? (uint8_t*)workspace + sums : nullptr, *to_scale = codes ? to + T * ld : nullptr;
   rc = f8_launch_down(d, transposed != 0, given, T, who, u, false, to, to_scale, st);
   if (rc != BSP_OK) return rc;
-  const F8Low low{who.which, u, transposed ? d.a_t : d.b, (int64_t)d.Rp * (transposed ? d.Ip : d.Op), (int64_t)T * d.Rp, d.Rp, f8_low_slices(T, d.N, K, false)};
+  const F8Low low{who.which, u, transposed ? d.a_t : d.b, (int64_t)d.Rp * (transposed ? d.Ip : d.Op), (int64_t)T * d.Rp, d.Rp, f8_down_slices(T, d.N, K, false)};
   return multiply(rows, codes ? F8Input{to, to_scale, code, code == BSP_E5M2, ld} : given, T, low, q, y_dtype, workspace, st);
 }
 
@@ -372,7 +372,7 @@ int bsp_f8_adapters_grad_workspace(const bsp_f8_adapters* adapters, int32_t T, i
   if (rc != BSP_OK) return rc;
   if (T < 0 || T > kMost) return BSP_ERR_SHAPE;
   const F8Adapters d = f8_adapters_of(adapters);
-  *bytes = low_bytes(d, T, d.I) + low_bytes(d, T, d.O) + f8_adapt_part_bytes(d, T);
+  *bytes = low_bytes(d, T, d.I, true) + low_bytes(d, T, d.O, true) + f8_adapt_part_bytes(d, T);
   return BSP_OK;
 }
 
@@ -399,7 +399,7 @@ int bsp_f8_adapters_grad(const bsp_f8_adapters* adapters, const void* dY, int64_
   hipStream_t st = (hipStream_t)stream;
   const F8Adapters d = f8_adapters_of(adapters);
   const F8Requests who = f8_requests_of(requests);
-  float *u = (float*)workspace, *v = u + low_bytes(d, T, d.I) / 4, *part = v + low_bytes(d, T, d.O) / 4;
+  float *u = (float*)workspace, *v = u + low_bytes(d, T, d.I, true) / 4, *part = v + low_bytes(d, T, d.O, true) / 4;
   const F8Input x = X ? F8Input{X->codes, X->scale, X->dtype, X->dtype == BSP_E5M2, (int64_t)f8_blocks(X->K) * F8_BLOCK} : F8Input{values, nullptr, BSP_BF16, 0, ldx};
   if (T > 0) {
     rc = f8_launch_down(d, false, x, T, who, u, true, nullptr, nullptr, st);

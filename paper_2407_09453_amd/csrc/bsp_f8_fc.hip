@@ -139,20 +139,20 @@ __device__ __forceinline__ void settle() {
 struct LowParts {
   u32x4_t high, rest;
 };
+template <int ASK>  // slices asked for together
 __device__ __forceinline__ LowParts low_parts(const F8Low& low, const float* u) {
   f32x4_t x0 = *(const f32x4_t*)u, x1 = *(const f32x4_t*)(u + 4);
-  if (low.slices > 1) {  // two or four, asked for together
-    f32x4_t y0[3], y1[3];
+#pragma unroll 1
+  for (int s = 1; s < low.slices; s += ASK) {  // (two, four or eight)
+    f32x4_t y0[ASK], y1[ASK];
 #pragma unroll
-    for (int s = 0; s < 3; ++s) {
-      const float* v = u + (s + 1 < low.slices ? s + 1 : 1) * low.u_step;
-      y0[s] = *(const f32x4_t*)v, y1[s] = *(const f32x4_t*)(v + 4);
+    for (int e = 0; e < ASK; ++e) {
+      const float* v = u + (s + e < low.slices ? s + e : s) * low.u_step;
+      y0[e] = *(const f32x4_t*)v, y1[e] = *(const f32x4_t*)(v + 4);
     }
-    x0 += y0[0], x1 += y1[0];
-    if (low.slices > 2) {
-      x0 += y0[1], x1 += y1[1];
-      x0 += y0[2], x1 += y1[2];
-    }
+#pragma unroll
+    for (int e = 0; e < ASK; ++e)
+      if (s + e < low.slices) x0 += y0[e], x1 += y1[e];
   }
   LowParts p;
 #pragma unroll
@@ -256,7 +256,7 @@ __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT
     for (int d = 0; d < kAhead; ++d) ask(d);
     LowParts p[MT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) p[m] = low_parts(low, u[m] + k);
+    for (int m = 0; m < MT; ++m) p[m] = low_parts<MO == 4 ? 1 : 3>(low, u[m] + k);
     while (now[0] >= 0) {
 #pragma unroll
       for (int d = 0; d < kAhead; ++d) {
