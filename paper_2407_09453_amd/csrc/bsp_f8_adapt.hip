@@ -5,8 +5,8 @@
 //   grad:  dB_a = sum_t dy_t u_t^t, dA_a = sum_t v_t x_t^t with v_t = s_a B_a^t dy_t (down, transposed)
 //
 // A and B are held as bf16, in both directions, ranks padded to 16, 32, 64 or 128 with zeros; products are summed in fp32.  u and v are fp32, and
-// where they enter a matrix instruction again they do so as two bf16 parts, which keep 16 bits of them.  Rows enter as they were given:
-// bf16 values and codes are exact in bf16, fp32 values go as two parts too.
+// where they enter a matrix instruction again they do so as bf16 parts: as two, which keep 16 bits, for results in bf16, as three, which keep all,
+// for gradients and fp32 results.  Rows enter as they were given: bf16 values and codes are exact in bf16, fp32 values go as three parts.
 // `down` is bound by the bytes of the rows on many rows, by latency on few.  `grad` reads each block of 128 columns of the rows of an adapter
 // once: both operands are summed over rows, so they lie in LDS as in memory and the transposing read hands a lane a column's
 // rows.  An adapter with many rows is cut into chunks whose sums a second launch joins, in order: no atomics.
@@ -172,13 +172,13 @@ __device__ __forceinline__ void unpack8(u32x4_t w, float* v) {
     v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
   }
 }
-// what eight values lose as bf16, itself as bf16
-__device__ __forceinline__ u32x4_t rest8(const float* v, u32x4_t high) {
-  float r[8], h[8];
+// what eight values lose as bf16, and that as bf16
+__device__ __forceinline__ u32x4_t rest8(const float* v, u32x4_t high, float* rest) {
+  float h[8];
   unpack8(high, h);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) r[k] = v[k] - h[k];
-  return pack8(r);
+  for (int k = 0; k < 8; ++k) rest[k] = v[k] - h[k];
+  return pack8(rest);
 }
 
 // The wait between a matrix instruction and the first use of its result, by hand: the branches over fragments that are not there are ways
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(SAVE ? 256 : 512, SAVE ? (NR == 4 ? 2 : 3) : NR == 
     for (int m = 0; m < M; ++m) {
       const uint8_t* row = mine + (m * 16 + r) * kRow;
       auto piece = [&](int p) { return *(const u32x4_t*)(row + ((p ^ key(m * 16 + r)) << 4)); };
-      u32x4_t xv[4], xl[SRC == kF32 ? 4 : 1];
+      u32x4_t xv[4], xl[SRC == kF32 ? 4 : 1], xs[SRC == kF32 ? 4 : 1];
       float v[SRC == kF32 ? 4 : 1][8];
       if constexpr (kCoded) {
         const float f = __uint_as_float((uint32_t)s[m] << 23);
@@ -308,7 +308,10 @@ __global__ __launch_bounds__(SAVE ? 256 : 512, SAVE ? (NR == 4 ? 2 : 3) : NR == 
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[j][k] = __uint_as_float(k < 4 ? p0[k & 3] : p1[k & 3]);
             xv[j] = pack8(v[j]);
-            xl[j] = rest8(v[j], xv[j]);
+            float rest[8];
+            xl[j] = rest8(v[j], xv[j], rest);
+            float none[8];
+            xs[j] = rest8(rest, xl[j], none);
           }
         }
       }
@@ -317,7 +320,10 @@ __global__ __launch_bounds__(SAVE ? 256 : 512, SAVE ? (NR == 4 ? 2 : 3) : NR == 
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           acc[i][m] = mfma_bf16_16x16x32(wv[i][j], xv[j], acc[i][m]);
-          if constexpr (SRC == kF32) acc[i][m] = mfma_bf16_16x16x32(wv[i][j], xl[j], acc[i][m]);
+          if constexpr (SRC == kF32) {
+            acc[i][m] = mfma_bf16_16x16x32(wv[i][j], xl[j], acc[i][m]);
+            acc[i][m] = mfma_bf16_16x16x32(wv[i][j], xs[j], acc[i][m]);
+          }
         }
       if constexpr (SAVE) {
         uint32_t most = 0;
@@ -470,11 +476,11 @@ __device__ __forceinline__ f32x16_t mfma32(u32x4_t a, u32x4_t b, f32x16_t c) {
 }
 
 // 128 columns of one side, dY (dB) or X (dA), with a chunk of an adapter's rows and RP ranks.  Four waves of 32 columns each; the other operand
-// is u or v, its high parts beside its low parts in a row of 2 RP bf16.  CODED: the rows are codes; WHOLE: all 128 columns are there.
+// is u or v, its three parts side by side in a row of 3 RP bf16.  CODED: the rows are codes; WHOLE: all 128 columns are there.
 template <int RP, bool CODED, bool WHOLE>
 __device__ __forceinline__ void grad_side(const GradArgs& a, const Chunk& k, bool in_y, int kb, uint8_t* lds) {
-  constexpr int NT = RP / 16;               // tiles of 32 columns of u: high parts, then low
-  constexpr int kQ = 4 * RP + 16;           // bytes from row to row of u in LDS
+  constexpr int NT = (3 * RP + 31) / 32;    // tiles of 32 columns of u
+  constexpr int kQ = 64 * NT + 16;          // bytes from row to row of u in LDS
   constexpr int kP = kStep * 256, kBuffer = kP + kStep * kQ, kMine = RP / 8;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int columns = in_y ? a.O : a.I, c0 = kb * 128;
@@ -544,8 +550,11 @@ __device__ __forceinline__ void grad_side(const GradArgs& a, const Chunk& k, boo
       const float y0 = slices > 1 ? from.u[e] + from.u2[e] : from.u[e], y1 = slices > 1 ? from.u[e + 1] + from.u2[e + 1] : from.u[e + 1];
       const float x0 = have ? y0 : 0.f, x1 = have ? y1 : 0.f;
       const uint32_t h = f8_pack_bf16x2(x0, x1);
+      const float z0 = x0 - __uint_as_float(h << 16), z1 = x1 - __uint_as_float(h & 0xFFFF0000u);
+      const uint32_t l = f8_pack_bf16x2(z0, z1);
       *(uint32_t*)(hi + e) = h;
-      *(uint32_t*)(hi + RP + e) = f8_pack_bf16x2(x0 - __uint_as_float(h << 16), x1 - __uint_as_float(h & 0xFFFF0000u));
+      *(uint32_t*)(hi + RP + e) = l;
+      *(uint32_t*)(hi + 2 * RP + e) = f8_pack_bf16x2(z0 - __uint_as_float(l << 16), z1 - __uint_as_float(l & 0xFFFF0000u));
     }
   };
   const int half = lane >> 5, trow = half * 8 + ((lane & 15) >> 2), key_r = ((lane & 15) >> 2) << 1 | half;
@@ -580,14 +589,14 @@ __device__ __forceinline__ void grad_side(const GradArgs& a, const Chunk& k, boo
 #pragma unroll
   for (int n = 0; n < NT; ++n) asm volatile("" : "+a"(acc[n]));
   asm volatile("s_nop 15\n\ts_nop 7");  // (see settle)
-  // high and low parts together
-  constexpr int kTiles = RP == 16 ? 1 : NT / 2;
+  // the parts together, the smallest first
+  constexpr int kTiles = RP == 16 ? 1 : RP / 32;
   if constexpr (RP == 16) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) acc[0][e] += __shfl_xor(acc[0][e], 16);
+    for (int e = 0; e < 16; ++e) acc[0][e] += __shfl_xor(acc[0][e], 16) + acc[1][e];
   } else {
 #pragma unroll
-    for (int n = 0; n < kTiles; ++n) acc[n] += acc[n + kTiles];
+    for (int n = 0; n < kTiles; ++n) acc[n] += acc[n + kTiles] + acc[n + 2 * kTiles];
   }
   const int64_t na = (int64_t)a.R * a.I, nb = (int64_t)a.O * a.R;
   float* to_a = k.slot < 0 ? a.dA + k.of * na : a.part + k.slot * (na + nb);
@@ -608,7 +617,7 @@ __device__ __forceinline__ void grad_side(const GradArgs& a, const Chunk& k, boo
 
 template <int RP>
 __global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * (kStep * 256 + kStep * (4 * RP + 16))];
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kStep * (256 + 64 * ((3 * RP + 31) / 32) + 16)];
   const Chunk k = find_chunk(a.q, a.N, a.chunk, blockIdx.y);
   if (k.of >= a.N) return;
   const bool in_y = (int)blockIdx.x < a.blocks_o;

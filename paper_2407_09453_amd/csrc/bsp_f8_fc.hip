@@ -125,7 +125,7 @@ __device__ __forceinline__ void store_tile(const F8Epilogue& q, f32x16_t (&acc)[
 }
 
 // The rows' adapters: B_a u_t added to a wave's sums, one adapter of its rows after the other, the next ones' weights asked for while one is
-// multiplied.  u enters as two bf16 parts, as zeros in the rows of other adapters: the rows are the matrix instruction's columns, and the
+// multiplied.  u enters as two bf16 parts (for fp32 results three), as zeros in the rows of other adapters: the rows are the matrix instruction's columns, and the
 // sums go on where they are.  Zero times what is no number is none: an adapter with such weights among its
 // rows' neighbours is multiplied from zero, and a lane, which holds results of one row, takes or leaves what it gives (three times the
 // instructions: 16384 x 4096 -> 4096 with rows of twelve adapters mixed 304 us where all go that way).
@@ -136,11 +136,12 @@ __device__ __forceinline__ void settle() {
   asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
+template <int PARTS>
 struct LowParts {
-  u32x4_t high, rest;
+  u32x4_t part[PARTS];
 };
-template <int ASK>  // slices asked for together
-__device__ __forceinline__ LowParts low_parts(const F8Low& low, const float* u) {
+template <int PARTS, int ASK>  // ASK: slices asked for together
+__device__ __forceinline__ LowParts<PARTS> low_parts(const F8Low& low, const float* u) {
   f32x4_t x0 = *(const f32x4_t*)u, x1 = *(const f32x4_t*)(u + 4);
 #pragma unroll 1
   for (int s = 1; s < low.slices; s += ASK) {  // (two, four or eight)
@@ -154,12 +155,15 @@ __device__ __forceinline__ LowParts low_parts(const F8Low& low, const float* u) 
     for (int e = 0; e < ASK; ++e)
       if (s + e < low.slices) x0 += y0[e], x1 += y1[e];
   }
-  LowParts p;
+  LowParts<PARTS> p;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const float a0 = (e < 2 ? x0 : x1)[2 * (e & 1)], a1 = (e < 2 ? x0 : x1)[2 * (e & 1) + 1];
-    p.high[e] = f8_pack_bf16x2(a0, a1);
-    p.rest[e] = f8_pack_bf16x2(a0 - __uint_as_float(p.high[e] << 16), a1 - __uint_as_float(p.high[e] & 0xFFFF0000u));
+    float a0 = (e < 2 ? x0 : x1)[2 * (e & 1)], a1 = (e < 2 ? x0 : x1)[2 * (e & 1) + 1];
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+      p.part[i][e] = f8_pack_bf16x2(a0, a1);
+      a0 -= __uint_as_float(p.part[i][e] << 16), a1 -= __uint_as_float(p.part[i][e] & 0xFFFF0000u);
+    }
   }
   return p;
 }
@@ -206,7 +210,7 @@ __device__ __forceinline__ void add_low_rows(const F8Low& low, f32x16_t (&acc)[M
   }
 }
 
-template <int MO, int MT>
+template <int MO, int MT, int PARTS>
 __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT], int T, int64_t t0, int o0) {
   const int lane = threadIdx.x & 63;
   const uint16_t* up = low.up + (int64_t)o0 * low.rank + lane * 8;  // (as the instruction takes them: 32 channels, sixteen ranks, 64 lanes)
@@ -254,9 +258,9 @@ __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT
     };
 #pragma unroll
     for (int d = 0; d < kAhead; ++d) ask(d);
-    LowParts p[MT];
+    LowParts<PARTS> p[MT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) p[m] = low_parts<MO == 4 ? 1 : 3>(low, u[m] + k);
+    for (int m = 0; m < MT; ++m) p[m] = low_parts<PARTS, MO == 4 ? 1 : 3>(low, u[m] + k);
     while (now[0] >= 0) {
 #pragma unroll
       for (int d = 0; d < kAhead; ++d) {
@@ -273,19 +277,21 @@ __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT
             const bool mine = of[m] == now[d];
             if (!__any(mine)) continue;
             if (!odd || __all(mine)) {
-              u32x4_t high, rest;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) high[e] = mine ? p[m].high[e] : 0, rest[e] = mine ? p[m].rest[e] : 0;
+              for (int i = 0; i < PARTS; ++i) {
+                u32x4_t v;
 #pragma unroll
-              for (int o = 0; o < MO; ++o) acc[o][m] = mfma_bf16_32x32x16(w[d][o], high, acc[o][m]);
+                for (int e = 0; e < 4; ++e) v[e] = mine ? p[m].part[i][e] : 0;
 #pragma unroll
-              for (int o = 0; o < MO; ++o) acc[o][m] = mfma_bf16_32x32x16(w[d][o], rest, acc[o][m]);
+                for (int o = 0; o < MO; ++o) acc[o][m] = mfma_bf16_32x32x16(w[d][o], v, acc[o][m]);
+              }
             } else {
               settle();
 #pragma unroll
               for (int o = 0; o < MO; ++o) {
-                f32x16_t sum = mfma_bf16_32x32x16(w[d][o], p[m].high, f32x16_t{});
-                sum = mfma_bf16_32x32x16(w[d][o], p[m].rest, sum);
+                f32x16_t sum = {};
+#pragma unroll
+                for (int i = 0; i < PARTS; ++i) sum = mfma_bf16_32x32x16(w[d][o], p[m].part[i], sum);
                 asm volatile("" : "+v"(sum));  // (read in the block of the instruction that makes it)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[o][m][e] += mine ? sum[e] : 0.f;
@@ -533,7 +539,7 @@ __device__ __forceinline__ void wide(const TileArgs& a, uint8_t* lds) {
     rest(std::integral_constant<int, 0>{});
   }
   if constexpr (LOW)
-    if (share == 0) add_low<MO, MT>(a.low, acc, a.T, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32);
+    if (share == 0) add_low<MO, MT, F32 ? 3 : 2>(a.low, acc, a.T, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32);
   __syncthreads();
   if constexpr (kSplits) {
     if (a.split > 1) {
