@@ -530,7 +530,7 @@ int bsp_f8_adapters_size(int32_t R, int32_t I, int32_t O, int64_t* a_elements, i
 int bsp_f8_adapters_set(const bsp_f8_adapters* d, int32_t slot, int32_t rank, const void* A, int64_t lda, const void* B, int64_t ldb, int32_t dtype,
                         float scale, void* stream);
 
-/* The rows of a batch by their adapters: made once for a batch, read by every layer's calls. */
+/* The rows of a batch (up to 2^26) by their adapters: made once for a batch, read by every layer's calls. */
 typedef struct {
   int32_t T, N;
   int32_t* plan;  /* device, 16-byte aligned, bsp_f8_requests_size bytes */

@@ -12,6 +12,7 @@ inline unsigned size_of(int d) { return d == BSP_F32 ? 4 : 2; }
 constexpr int32_t kMost = INT32_MAX - 65536;  // rows and columns: sizes rounded up stay in 32 bits
 constexpr int32_t kWide = 1 << 24;            // columns of codes: 256 rows' offsets stay in 32 bits
 constexpr int32_t kSlots = 1024, kRank = 128;  // adapters of a set, ranks of one
+constexpr int32_t kRequests = 1 << 26;        // rows of a batch with adapters: their tiles' threads are counted along one dimension of a launch
 constexpr int32_t kVocabulary = 1 << 21;      // logits of a row: 64 chunks of what a workgroup's registers hold
 constexpr int32_t kTop = 64;                  // likeliest tokens: one of 64 groups' largest is below the last of them
 
@@ -119,7 +120,7 @@ int check_adapters(const bsp_f8_adapters* d) {
 }
 int check_requests(const bsp_f8_requests* r) {
   if (!r) return BSP_ERR_NULL;
-  if (r->T < 0 || r->T > kMost || r->N < 1 || r->N > kSlots) return BSP_ERR_SHAPE;
+  if (r->T < 0 || r->T > kRequests || r->N < 1 || r->N > kSlots) return BSP_ERR_SHAPE;
   if (r->T > 0 && !r->plan) return BSP_ERR_NULL;
   return aligned(r->plan, 16) ? BSP_OK : BSP_ERR_ALIGN;
 }
@@ -306,7 +307,7 @@ int bsp_f8_adapters_set(const bsp_f8_adapters* d, int32_t slot, int32_t rank, co
 
 int bsp_f8_requests_size(int32_t T, int32_t N, int64_t* bytes) {
   if (!bytes) return BSP_ERR_NULL;
-  if (T < 0 || T > kMost || N < 1 || N > kSlots) return BSP_ERR_SHAPE;
+  if (T < 0 || T > kRequests || N < 1 || N > kSlots) return BSP_ERR_SHAPE;
   *bytes = f8_requests_bytes(T, N);
   return BSP_OK;
 }
@@ -337,7 +338,7 @@ int bsp_f8_fc_adapted(const bsp_weights_f8* w, int32_t transposed, const bsp_cod
   if (rc == BSP_OK) rc = check_requests(requests);
   if (rc != BSP_OK) return rc;
   const int K = transposed ? w->O : w->I;
-  if (T < 0 || T > kMost || requests->T != T || requests->N != adapters->N || adapters->I != w->I || adapters->O != w->O) return BSP_ERR_SHAPE;
+  if (T < 0 || requests->T != T || requests->N != adapters->N || adapters->I != w->I || adapters->O != w->O) return BSP_ERR_SHAPE;
   if (X) {
     rc = check_codes(X);
     if (rc != BSP_OK) return rc;
@@ -370,7 +371,7 @@ int bsp_f8_adapters_grad_workspace(const bsp_f8_adapters* adapters, int32_t T, i
   if (!bytes) return BSP_ERR_NULL;
   const int rc = check_adapters(adapters);
   if (rc != BSP_OK) return rc;
-  if (T < 0 || T > kMost) return BSP_ERR_SHAPE;
+  if (T < 0 || T > kRequests) return BSP_ERR_SHAPE;
   const F8Adapters d = f8_adapters_of(adapters);
   *bytes = low_bytes(d, T, d.I, true) + low_bytes(d, T, d.O, true) + f8_adapt_part_bytes(d, T);
   return BSP_OK;
