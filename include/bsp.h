@@ -511,7 +511,8 @@ int bsp_layer_norm_grad(const void* dY, int64_t ld_dy, const void* X, int64_t ld
 /* Low-rank adapters of many requests beside a layer.  Row t of a batch belongs to adapter which[t], or to none:
  *   Y[t] = act(W^ x^_t + bias + residual + s_a B_a (A_a x_t)),  a = which[t]
  * with x_t as it is handed in (values as they are, codes as the values that they stand for), A_a [R][I] and B_a [O][R] held as bf16.  All is
- * summed in fp32 and rounded once; A_a x_t enters the second product with 16 bits.
+ * summed in fp32 and rounded once; A_a x_t enters the second product with 16 bits for results in bf16, with 24 for fp32 ones.  What is not finite
+ * among x_t, in bf16 for values in fp32 too, or A_a x_t makes its row's results infinite or NaN, and no other row's.
  * A set holds N adapters (up to 1024) of rank up to R (up to 128) for layers of I inputs and O outputs, in both directions, ranks padded to
  * Rp = 16, 32, 64 or 128. */
 typedef struct {
@@ -562,12 +563,13 @@ int bsp_f8_adapters_grad(const bsp_f8_adapters* adapters, const void* dY, int64_
  *   H            device [T][D], rows ldh apart, written where there is a residual (else null); overlaps neither X nor the residual
  *   weight       device float[D], or null (ones)
  *   Y, codes     as for bsp_layer_norm: one of the two;  rstd  device float[T], written for the backward pass
- * Squares are summed in fp32.  Errors: NULL, SHAPE, DTYPE, ALIGN, HIP.  T = 0 does nothing. */
+ * Squares are summed in fp32 (of values past 2^63 the sum is infinite and the row becomes zeros).  No other result overlaps an input.
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, HIP.  T = 0 does nothing. */
 int bsp_rms_norm(const void* X, int64_t ldx, const void* residual, int64_t ldr, int32_t dtype, int32_t T, int32_t D, const float* weight, float eps,
                  void* H, int64_t ldh, void* Y, int64_t ldy, const bsp_codes* codes, float* rstd, void* stream);
 /* Its gradient: dX [T][D], the gradient of X and of the residual alike, from dY, from dH (what reaches H along the residual stream,
- * or null), from H and from rstd, all of one dtype; dweight float[D], or null.  workspace: bsp_rms_norm_grad_workspace bytes,
- * 16-byte aligned.  Errors: NULL, SHAPE, DTYPE, ALIGN, CAPACITY, HIP.  T = 0 gives zeros. */
+ * or null), from H and from rstd, all of one dtype; dweight float[D], or null.  dX overlaps no input.  workspace:
+ * bsp_rms_norm_grad_workspace bytes, 16-byte aligned.  Errors: NULL, SHAPE, DTYPE, ALIGN, CAPACITY, HIP.  T = 0 gives zeros. */
 int bsp_rms_norm_grad_workspace(int32_t T, int32_t D, int64_t* bytes);
 int bsp_rms_norm_grad(const void* dY, int64_t ld_dy, const void* H, int64_t ldh, const void* dH, int64_t ld_dh, int32_t dtype, int32_t T, int32_t D,
                       const float* rstd, const float* weight, void* dX, int64_t ld_dx, float* dweight, void* workspace,
@@ -579,7 +581,7 @@ int bsp_rms_norm_grad(const void* dY, int64_t ld_dy, const void* H, int64_t ldh,
  *                 first, NaN before all; top <= 64, top <= V; both null with top = 0
  *   X             device, BSP_F32 or BSP_BF16, rows ldx elements apart; minus infinity is a token that cannot be
  *   tokens        device [T], token_bytes 4 (int32) or 8 (int64).  Below 0: none is given (padding), logp[t] = 0; V and above: NaN
- *   scale         above 0: the inverse of a temperature
+ *   scale         above 0, 2^100 at most: the inverse of a temperature
  * A row of minus infinities alone has no token left: lse and log probabilities are minus infinity, the entropy is 0.  A row that holds a NaN or
  * plus infinity gives NaN.  The results are float; workspace: bsp_log_probs_workspace bytes, 16-byte aligned.
  * Errors: NULL, SHAPE, DTYPE, ALIGN, CAPACITY, HIP.  T = 0 does nothing. */

@@ -14,6 +14,7 @@ constexpr int32_t kWide = 1 << 24;            // columns of codes: 256 rows' off
 constexpr int32_t kSlots = 1024, kRank = 128;  // adapters of a set, ranks of one
 constexpr int32_t kRequests = 1 << 26;        // rows of a batch with adapters: their tiles' threads are counted along one dimension of a launch
 constexpr int32_t kVocabulary = 1 << 21;      // logits of a row: 64 chunks of what a workgroup's registers hold
+constexpr float kSharpest = 0x1p100f;         // of a temperature's inverse: times log2 e it is a number
 constexpr int32_t kTop = 64;                  // likeliest tokens: one of 64 groups' largest is below the last of them
 
 // a matrix of values whose rows are `ld` elements apart; rows of an input may be the same one (ld = 0)
@@ -475,7 +476,7 @@ int bsp_log_probs(const void* X, int64_t ldx, int32_t dtype, int32_t T, int32_t 
   if (rc == BSP_OK) rc = check_values(X, dtype, ldx, T, V, true);
   if (rc != BSP_OK) return rc;
   if (token_bytes != 4 && token_bytes != 8) return BSP_ERR_DTYPE;
-  if (!(scale > 0.f) || scale > 3.4028234e38f) return BSP_ERR_SHAPE;
+  if (!(scale > 0.f) || scale > kSharpest) return BSP_ERR_SHAPE;
   if (T == 0) return BSP_OK;
   if (!tokens || !logp || !lse || !entropy || (top && (!top_logp || !top_tokens))) return BSP_ERR_NULL;
   if (!aligned(tokens, token_bytes) || !aligned(logp, 4) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(top_logp, 4) || !aligned(top_tokens, 4)) return BSP_ERR_ALIGN;
@@ -492,7 +493,7 @@ int bsp_log_probs_grad(const void* X, int64_t ldx, int32_t dtype, int32_t T, int
   if (rc == BSP_OK) rc = check_values(dX, dtype, ld_dx, T, V, false);
   if (rc != BSP_OK) return rc;
   if (token_bytes != 4 && token_bytes != 8) return BSP_ERR_DTYPE;
-  if (!(scale > 0.f) || scale > 3.4028234e38f) return BSP_ERR_SHAPE;
+  if (!(scale > 0.f) || scale > kSharpest) return BSP_ERR_SHAPE;
   if (T == 0) return BSP_OK;
   if (!tokens || !lse || !entropy) return BSP_ERR_NULL;
   if (!aligned(tokens, token_bytes) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(dlogp, 4) || !aligned(dentropy, 4)) return BSP_ERR_ALIGN;

@@ -28,9 +28,9 @@ def _each(t, X):
 
 
 def log_probs(logits, tokens, top: int = 0, scale: float = 1.0, stream=None):
-    """(logp, lse, entropy, top_logp, top_tokens) of softmax(scale logits) for logits [T][V] (fp32 or bf16): the log probability of each row's
-    token [T] (int32 or int64; below 0 there is none, and it is 0; V and above: NaN), the log of the sum, the entropy, and the
-    ``top`` (at most 64) largest log probabilities with their tokens (int32), of equal logits the lower token first; None with top = 0."""
+    """(logp, lse, entropy, top_logp, top_tokens) of softmax(scale logits) for logits [T][V] (fp32 or bf16; V <= 2^21, 0 < scale <= 2^100): the
+    log probability of each row's token [T] (int32 or int64; below 0 there is none, and it is 0; V and above: NaN), the log of the sum, the
+    entropy, and the ``top`` (at most 64) largest log probabilities with their tokens (int32), of equal logits the lower token first; None with top = 0."""
     import torch
     if stream is not None:
         return _on_stream(stream, logits, log_probs, logits, tokens, top, scale)

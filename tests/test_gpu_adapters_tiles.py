@@ -1,0 +1,142 @@
+"""Adapters beside the 8-bit product in every tile, in every split and in the kernels for few rows, with the kernel that ran named; rows of one adapter, of
+several and of very many; an adapter whose weights are no numbers among them; offsets past 32 bits.
+
+The references are sums in 64 bits on the GPU, the bounds those of the layer's tests for the product, with S its terms' magnitudes, and for what
+the adapters add, U = 2^-24: u adds I bf16 products in fp32, a sixteenth of them one after the other at most, (I / 16 + 96) U of their
+magnitudes, and enters with 17 bits for bf16 results (2^-17 of it is left) and 24 for fp32 ones (2^-26); 3 rank + 16 sums follow.
+"""
+import pytest
+
+from gpu_util import kernels_of
+from test_gpu_f8_tiles import PRODUCTS, PRODUCTS_F32, TILES, U, _both, _gen, _into, _rows, _weights
+
+pytestmark = pytest.mark.gpu
+
+
+def _low(x, A, B, scale, which):
+    """What each row's adapter adds, and twice that of the magnitudes: with the first product's, with u's own."""
+    import torch
+    y, mag, own = (torch.zeros(x.shape[0], B.shape[1], dtype=torch.float64, device="cuda") for _ in range(3))
+    for n in range(A.shape[0]):
+        rows = (which == n).nonzero()[:, 0]
+        if len(rows):
+            a, b, v = A[n].double(), B[n].double(), x[rows].double()
+            u = scale[n] * (v @ a.t())
+            y[rows], own[rows] = u @ b.t(), u.abs() @ b.abs().t()
+            mag[rows] = scale[n] * (v.abs() @ a.abs().t()) @ b.abs().t()
+    return y, mag, own
+
+
+def _bank(gen, N, R, I, O):
+    import torch
+    import paper_2407_09453_amd as bsp
+    A = (torch.randn(N, R, I, generator=gen, device="cuda") / I ** 0.5).to(torch.bfloat16)
+    B = torch.randn(N, O, R, generator=gen, device="cuda").to(torch.bfloat16)
+    scale = [0.75 * 2.0 ** (n % 4 - 2) for n in range(N)]
+    bank = bsp.BspAdapters(N, R, I, O)
+    for n in range(N):
+        bank.set(n, A[n], B[n], scale[n])
+    return bank, A, B, scale
+
+
+def _near(y, want, S, low, I, R, f32):
+    _, mag, own = low
+    tol = (I + 16) * U * S if f32 else 2.0 ** -10 * S + 2.0 ** -8 * want.abs()
+    tol = tol + (I / 16 + 96) * U * mag + (2.0 ** (-26 if f32 else -17) + (3 * R + 16) * U) * (own + (I / 16 + 96) * U * mag) + 2.0 ** -120
+    ratio = ((y.double() - want).abs() / tol).max()
+    assert float(ratio) <= 1.0, float(ratio)
+
+
+WHOSE = {"one": (1, 33), "some": (5, 16), "many": (150, 5), "wide": (3, 128)}
+
+
+@pytest.mark.parametrize("whose", WHOSE)
+@pytest.mark.parametrize("tile,T,I,O,density,dtype", _both(PRODUCTS[::2], PRODUCTS_F32[::2]) + [("few", 16, 4100, 1000, 0.7, "bf16"), ("few", 32, 9000, 72, 1.0, "bf16"),
+                                                                                                   ("few", 9, 700, 260, 0.5, "f32"), ("few", 30, 4100, 130, 1.0, "f32")])
+def test_in_every_tile(tile, T, I, O, density, dtype, whose):
+    import torch
+    import paper_2407_09453_amd as bsp
+    N, R = WHOSE[whose]
+    gen = _gen(T, I, O, whose)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    W, gamma, Wm = _weights(gen, O, I, density)
+    layer = bsp.BspLayerF8(W, gamma.cpu().numpy())
+    bank, A, B, scale = _bank(gen, N, R, I, O)
+    which = torch.randint(-1 if N > 1 else 0, N, (T,), generator=gen, device="cuda")
+    requests = bsp.BspRequests(which, N)
+    kept = bsp.save8(_rows(gen, T, I))
+    x = kept.load(torch.float32)
+    out, buffer = _into(T, O, dt)
+    names = kernels_of(lambda: layer.fc(kept, out=out, adapters=bank, requests=requests))
+    assert any(("f8_few_low" in n) if tile == "few" else "f8_wide_low" + TILES[tile] in n for n in names), names
+    low = _low(x, A, B, scale, which)
+    S = x.double().abs() @ Wm.abs().t()
+    _near(out, x.double() @ Wm.t() + low[0], S, low, I, R, dtype == "f32")
+    assert bool(buffer[out.numel():].isnan().all())
+    if N > 1:  # one of them no numbers: its rows alone
+        bad = (which == 1)
+        before = out.clone()
+        bank.set(1, torch.full((R, I), 1.0, device="cuda"), torch.full((O, R), float("nan"), device="cuda"), 1.0)
+        layer.fc(kept, out=out, adapters=bank, requests=requests)
+        assert out[bad].isnan().all()
+        _near(out[~bad], before[~bad].double(), 2 * S[~bad], [2 * v[~bad] for v in low], I, R, dtype == "f32")
+        bank.set(1, torch.full((R, I), float("inf"), device="cuda"), torch.full((O, R), 1.0, device="cuda"), 1.0)
+        layer.fc(kept, out=out, adapters=bank, requests=requests)
+        assert not out[bad].isfinite().any()
+        _near(out[~bad], before[~bad].double(), 2 * S[~bad], [2 * v[~bad] for v in low], I, R, dtype == "f32")
+
+
+def test_offsets_past_32_bits():
+    """Rows of values and codes, results and an adapter of a set, each past 2^31 elements."""
+    import torch
+    import paper_2407_09453_amd as bsp
+    gen = _gen("far")
+    T, I, O, R, N = 140000, 16384, 128, 4, 3
+    W, gamma, Wm = _weights(gen, O, I, 1.0)
+    layer = bsp.BspLayerF8(W, gamma.cpu().numpy())
+    bank, A, B, scale = _bank(gen, N, R, I, O)
+    X = torch.empty(T, I, dtype=torch.bfloat16, device="cuda")
+    for t in range(0, T, 10000):
+        X[t:t + 10000] = _rows(gen, 10000, I)
+    at = torch.tensor([0, 5, 131071, 131072, 131073, 139000, 139998, 139999], device="cuda")
+    which = torch.full((T,), -1, device="cuda")
+    which[at] = torch.tensor([0, 1, 2, 0, -1, 1, 2, 0], device="cuda")
+    requests = bsp.BspRequests(which, N)
+    kept = bsp.save8(X)
+    x8 = torch.empty(len(at), I, device="cuda")
+    for i, t in enumerate(at.tolist()):
+        x8[i] = bsp.save8(X[t:t + 1]).load(torch.float32)[0]
+    S = x8.double().abs() @ Wm.abs().t()
+    for given, x in ((kept, x8), (X, X[at].float())):
+        y = layer.fc(given, adapters=bank, requests=requests)[at]
+        low = _low(x, A, B, scale, which[at])
+        _near(y, x8.double() @ Wm.t() + low[0], S, low, I, R, False)
+    dY = torch.randn(T, O, generator=gen, device="cuda").to(torch.bfloat16)
+    for given, x in ((kept, x8), (X, X[at].float())):
+        dA, dB = bank.grad(dY, given, requests)
+        for n in range(N):
+            rows = which[at] == n
+            v, d = x[rows].double(), dY[at][rows].double()
+            a, b = A[n].double(), B[n].double()
+            tol = (I + O + 64) * U
+            wa, wb = scale[n] * (d @ b).t() @ v, scale[n] * d.t() @ (v @ a.t())
+            assert bool(((dA[n] - wa).abs() <= tol * scale[n] * (d.abs() @ b.abs()).t() @ v.abs()).all())
+            assert bool(((dB[n] - wb).abs() <= tol * scale[n] * d.abs().t() @ (v.abs() @ a.abs().t())).all())
+    del X, kept, dY
+    N, R, T = 1024, 128, 3  # a set of 2^31 elements
+    bank = bsp.BspAdapters(N, R, I, O)
+    A = (torch.randn(R, I, generator=gen, device="cuda") / I ** 0.5).to(torch.bfloat16)
+    B = torch.randn(O, R, generator=gen, device="cuda").to(torch.bfloat16)
+    bank.set(N - 1, A, B, 1.0)
+    X = _rows(gen, T, I)
+    which = torch.tensor([N - 1, 0, -1], device="cuda")
+    requests = bsp.BspRequests(which, N)
+    low = _low(X.float(), A[None], B[None], [1.0], torch.tensor([0, -1, -1], device="cuda"))
+    x8 = bsp.save8(X).load(torch.float32)
+    _near(layer.fc(X, adapters=bank, requests=requests), x8.double() @ Wm.t() + low[0], x8.double().abs() @ Wm.abs().t(), low, I, R, False)
+    dY = torch.randn(T, O, generator=gen, device="cuda").to(torch.bfloat16)
+    dA, dB = bank.grad(dY, X, requests)
+    d, v, a, b = dY[:1].double(), X[:1].double(), A.double(), B.double()
+    assert not dA[:-1].any() and not dB[:-1].any()
+    assert bool(((dA[-1] - (d @ b).t() @ v).abs() <= (I + O + 64) * U * (d.abs() @ b.abs()).t() @ v.abs()).all())
+    assert bool(((dB[-1] - d.t() @ (v @ a.t())).abs() <= (I + O + 64) * U * d.abs().t() @ (v.abs() @ a.abs().t())).all())

@@ -200,3 +200,21 @@ def test_autograd_is_told():
     x = torch.randn(4, 64, device="cuda", requires_grad=True)
     with pytest.warns(UserWarning, match="records nothing"):
         bsp.rms_norm(x)
+
+
+@pytest.mark.parametrize("D", [700, 20000])
+def test_offsets_past_32_bits(D):
+    """Rows 2^30 elements apart."""
+    import torch
+    import paper_2407_09453_amd as bsp
+    held = torch.empty(3 * 2 ** 30 + D, dtype=torch.bfloat16, device="cuda")
+    far = held.as_strided((4, D), (2 ** 30, 1))
+    X = torch.randn(4, D, device="cuda").to(torch.bfloat16)
+    far.copy_(X)
+    assert all(torch.equal(p, q) for p, q in zip(bsp.rms_norm(far, residual=far), bsp.rms_norm(X, residual=X)))
+    _, h, rstd = bsp.rms_norm(X)
+    assert all(torch.equal(p, q) for p, q in zip(bsp.rms_norm_grad(far, far, rstd, dH=far), bsp.rms_norm_grad(X, h, rstd, dH=X)))
+    out, r = torch.zeros_like(X), torch.empty(4, device="cuda")
+    assert bsp.load_library().bsp_rms_norm(X.data_ptr(), D, None, 0, 1, 4, D, None, 1e-6, None, 0, far.data_ptr(), 2 ** 30, None, r.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
+    out.copy_(far)
+    assert torch.equal(out, bsp.rms_norm(X)[0])

@@ -69,7 +69,7 @@ def test_rms_gradient_refusals(want, args):
 @pytest.mark.parametrize("want,args", [
     (DTYPE, dict(dt=b.BSP_I8)), (SHAPE, dict(T=-1)), (SHAPE, dict(V=0)), (SHAPE, dict(V=(1 << 21) + 1, ld=1 << 22)), (SHAPE, dict(ld=999)), (NULL, dict(X=None)), (ALIGN, dict(X=P + 1)),
     (DTYPE, dict(tb=2)), (NULL, dict(tok=None)), (ALIGN, dict(tok=P + 4)), (SHAPE, dict(scale=0.0)), (SHAPE, dict(scale=-1.0)), (SHAPE, dict(scale=float("nan"))),
-    (SHAPE, dict(scale=float("inf"))), (SHAPE, dict(top=65)), (SHAPE, dict(top=-1)), (SHAPE, dict(V=5, top=6)), (NULL, dict(lse=None)), (NULL, dict(logp=None)),
+    (SHAPE, dict(scale=float("inf"))), (SHAPE, dict(scale=2.0 ** 101)), (SHAPE, dict(top=65)), (SHAPE, dict(top=-1)), (SHAPE, dict(V=5, top=6)), (NULL, dict(lse=None)), (NULL, dict(logp=None)),
     (NULL, dict(top=3, tl=None)), (NULL, dict(top=3, ti=None)), (ALIGN, dict(entropy=P + 2)), (CAPACITY, dict(V=20000, ld=20000, top=3, n=8 * 10 * 40 - 1)),
     (NULL, dict(V=20000, ld=20000, top=3, ws=None)), (ALIGN, dict(V=20000, ld=20000, ws=P + 8)), (OK, dict(T=0, X=None, tok=None)),
 ])
@@ -81,7 +81,7 @@ def test_log_probs_refusals(want, args):
 
 @pytest.mark.parametrize("want,args", [
     (DTYPE, dict(dt=b.BSP_I8)), (SHAPE, dict(ld=999)), (NULL, dict(X=None)), (NULL, dict(dX=None)), (SHAPE, dict(ldd=0)), (DTYPE, dict(tb=0)), (NULL, dict(tok=None)), (NULL, dict(lse=None)),
-    (NULL, dict(entropy=None)), (ALIGN, dict(dlogp=P + 1)), (ALIGN, dict(dentropy=P + 1)), (SHAPE, dict(scale=0.0)), (SHAPE, dict(dX=P, ldd=1001)), (OK, dict(T=0, X=None, dX=None)),
+    (NULL, dict(entropy=None)), (ALIGN, dict(dlogp=P + 1)), (ALIGN, dict(dentropy=P + 1)), (SHAPE, dict(scale=0.0)), (SHAPE, dict(scale=2.0 ** 101)), (SHAPE, dict(dX=P, ldd=1001)), (OK, dict(T=0, X=None, dX=None)),
 ])
 def test_log_probs_gradient_refusals(want, args):
     a = {**dict(X=P, ld=1000, dt=BF, T=8, V=1000, tok=P, tb=4, scale=1.0, lse=P, entropy=P, dlogp=P, dentropy=P, dX=2 * P, ldd=1000), **args}
