@@ -104,8 +104,8 @@ class BspAdapters:
             words, x = _NO_CODES, X.data_ptr()
         assert (requests.T, requests.N) == (T, self.N), "requests of %d rows and %d slots" % (T, self.N)
         _on(self.scale, dY, requests.plan)
-        dA = torch.empty((self.N, self.R, self.I), dtype=torch.float32, device=self.device)
-        dB = torch.empty((self.N, self.O, self.R), dtype=torch.float32, device=self.device)
+        dA = self.scale.new_empty((self.N, self.R, self.I))
+        dB = self.scale.new_empty((self.N, self.O, self.R))
         n = self._workspace.get(T)
         if n is None:
             n = ctypes.c_int64(0)
@@ -113,7 +113,7 @@ class BspAdapters:
             if len(self._workspace) > 4096:
                 self._workspace.clear()
             n = self._workspace[T] = n.value
-        ws = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+        ws = self.scale.new_empty(n, dtype=torch.uint8) if n else None
         _call(_ADAPTERS_GRAD, _pack17(self._address, dY.data_ptr(), ldy, *words, x, ldx, T, requests._address, dA.data_ptr(), dB.data_ptr(),
                                       0 if ws is None else ws.data_ptr(), n, _current_stream(dY)), "bsp_f8_adapters_grad")
         return dA, dB

@@ -338,7 +338,9 @@ int f8_launch_plan(const bsp_f8_requests* r, const void* which, bool wide, hipSt
 int f8_launch_set(const F8Adapters& d, int slot, int rank, const void* A, int64_t lda, const void* B, int64_t ldb, bool f32, float scale, hipStream_t st);
 int f8_down_slices(int T, int N, int K, bool grad);  // of u: up to eight for a product, two for the gradients
 // codes, scale: where values are to become codes (of x.e5) on the way, too; or null
-int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, bool grad, uint8_t* codes, uint8_t* scale, hipStream_t st);
+int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, uint8_t* codes, uint8_t* scale, hipStream_t st);
+// u of the layer's input and v of its result's gradient (bf16)
+int f8_launch_down_both(const F8Adapters& d, const F8Input& x, const F8Input& dY, int T, const F8Requests& q, float* u, float* v, hipStream_t st);
 int64_t f8_adapt_part_bytes(const F8Adapters& d, int T);
 int f8_launch_adapt_grad(const F8Adapters& d, const uint16_t* dY, int64_t ldy, const F8Input& x, int T, const F8Requests& q, const float* u, const float* v,
                          float* part, float* dA, float* dB, hipStream_t st);

@@ -202,16 +202,15 @@ __device__ __forceinline__ void settle(f32x4_t (&acc)[NR][M]) {
 template <int SRC, int NR>
 constexpr int kFragments = SRC == kF32 ? 1 : SRC == kBf16 || NR == 4 ? 2 : 4;  // of sixteen rows
 
+// lds: [waves][rows of a block]; then sums [waves][NR][M][64][4]
 template <int SRC, int NR, bool SAVE>
-__global__ __launch_bounds__(SAVE ? 256 : 512, SAVE ? (NR == 4 ? 2 : 3) : NR == 4 ? 2 : 4) void adapt_down(DownArgs a) {
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];  // [waves][rows of a block]; then sums [waves][NR][M][64][4]
+__device__ __forceinline__ void down(const DownArgs& a, int block, uint8_t* lds) {
   constexpr bool kCoded = SRC == kE4 || SRC == kE5;
   constexpr int M = kFragments<SRC, NR>, kParts = 4 / M, kSize = SRC == kF32 ? 4 : SRC == kBf16 ? 2 : 1;
   constexpr int kRow = 128 * kSize, kPieces = kRow / 16, kAtOnce = 64 / kPieces, kAsks = 16 * M / kAtOnce;  // bytes and pieces of a row; rows a request, requests
-  kernarg_touch<DownArgs>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int r = lane & 15, g = lane >> 4;
-  const int tile = blockIdx.x / kParts, part = blockIdx.x % kParts;
+  const int tile = block / kParts, part = block % kParts;
   const int32_t* record = a.q.tiles + 4 + (int64_t)tile * kTileWords;
   const int32_t* rows = record + 4 + part * M * 16;
   const int of = __builtin_amdgcn_readfirstlane(record[0]), n = __builtin_amdgcn_readfirstlane(record[1]) - part * M * 16;
@@ -228,18 +227,18 @@ __global__ __launch_bounds__(SAVE ? 256 : 512, SAVE ? (NR == 4 ? 2 : 3) : NR == 
 #pragma unroll
     for (int q = 0; q < 2 * M; ++q) leaves[q] = rows[q * 8 + (lane >> 3)];
   const bool saves = SAVE && blockIdx.z == 0;
-  if (tile >= a.q.tiles[saves ? 1 : 0] || n <= 0) return;
+  const int nb = a.Kp >> 7, kb0 = blockIdx.y * a.per, kb1 = kb0 + a.per < nb ? kb0 + a.per : nb;
+  if (tile >= a.q.tiles[saves ? 1 : 0] || n <= 0 || kb0 >= nb) return;  // (no slice is empty: f8_down_slices)
   auto key = [](int row) { return kCoded ? (row >> 1) & 7 : row & 15; };
   const uint8_t* x[kAsks];
 #pragma unroll
   for (int q = 0; q < kAsks; ++q) x[q] = (const uint8_t*)a.X + asked[q] * a.ld * kSize;
   uint8_t* mine = lds + wave * 16 * M * kRow;
   const uint16_t* w = a.down + (int64_t)(of < 0 ? 0 : of) * a.Rp * a.Kp + (blockIdx.z * NR * 4 * 64 + lane) * 8;
-  const int nb = a.Kp >> 7, kb0 = blockIdx.y * a.per, kb1 = kb0 + a.per < nb ? kb0 + a.per : nb;
   f32x4_t acc[NR][M] = {};
   // Workgroups begin at different columns: of rows a power of two apart those at one column lie in one channel of the L2, and all would ask that one
   // (8192 x 16384 of one adapter 255 us, of two 98).
-  const int blocks = kb1 - kb0, turn = blocks > 0 ? (int)blockIdx.x * waves % blocks : 0;
+  const int blocks = kb1 - kb0, turn = block * waves % blocks;
   for (int i = wave; i < blocks; i += waves) {
     const int kb = kb0 + (i + turn < blocks ? i + turn : i + turn - blocks);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the last block has been read
@@ -393,25 +392,83 @@ __global__ __launch_bounds__(SAVE ? 256 : 512, SAVE ? (NR == 4 ? 2 : 3) : NR == 
 }
 
 template <int SRC, int NR, bool SAVE>
+__global__ __launch_bounds__(SAVE ? 256 : 512, SAVE ? (NR == 4 ? 2 : 3) : NR == 4 ? 2 : 4) void adapt_down(DownArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  kernarg_touch<DownArgs>();
+  down<SRC, NR, SAVE>(a, blockIdx.x, lds);
+}
+// u and v of the gradients in one launch, v of dY first
+struct BothArgs {
+  DownArgs y, x;
+  int32_t first;  // workgroups of y
+};
+template <int SRC, int NR>
+__global__ __launch_bounds__(512, NR == 4 ? 2 : 4) void adapt_down_both(BothArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  kernarg_touch<BothArgs>();
+  if ((int)blockIdx.x < a.first) down<kBf16, NR, false>(a.y, blockIdx.x, lds);
+  else down<SRC, NR, false>(a.x, blockIdx.x - a.first, lds);
+}
+
+template <int SRC, int NR>
+constexpr int down_lds() {  // a wave's bytes
+  constexpr int rows = 16 * kFragments<SRC, NR> * (SRC == kF32 ? 512 : SRC == kBf16 ? 256 : 128), sums = NR * kFragments<SRC, NR> * 1024;
+  return rows > sums ? rows : sums;
+}
+inline int down_waves(int most, int per) {  // a wave a block of columns at least
+  while (most > 1 && most > per) most >>= 1;
+  return most;
+}
+inline bool raise(const void* kernel, int lds) { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess; }
+
+template <int SRC, int NR, bool SAVE>
 int down_launch(const DownArgs& a, int T, int N, int slices, hipStream_t st) {
-  constexpr int M = kFragments<SRC, NR>, most = SAVE ? 4 : 8;
-  constexpr int kBytes = 16 * M * (SRC == kF32 ? 512 : SRC == kBf16 ? 256 : 128), kWave = kBytes > NR * M * 1024 ? kBytes : NR * M * 1024;
-  const int64_t tiles = f8_request_tiles(T, N) * (4 / M);
-  int waves = most;  // a wave a block of columns at least
-  while (waves > 1 && waves > a.per) waves >>= 1;
-  if (!f8_fits_x(tiles, 512)) return BSP_ERR_SHAPE;
-  static const bool raised = hipFuncSetAttribute((const void*)&adapt_down<SRC, NR, SAVE>, hipFuncAttributeMaxDynamicSharedMemorySize, most * kWave) == hipSuccess;
+  constexpr int most = SAVE ? 4 : 8, lds = down_lds<SRC, NR>();
+  const int64_t groups = f8_request_tiles(T, N) * (4 / kFragments<SRC, NR>);
+  const int waves = down_waves(most, a.per);
+  if (!f8_fits_x(groups, 512)) return BSP_ERR_SHAPE;
+  static const bool raised = raise((const void*)&adapt_down<SRC, NR, SAVE>, most * lds);
   if (!raised) return BSP_ERR_HIP;
-  hipLaunchKernelGGL((adapt_down<SRC, NR, SAVE>), dim3((unsigned)tiles, (unsigned)slices, (unsigned)(a.Rp / (16 * NR))), dim3(64 * waves), (size_t)waves * kWave, st, a);
+  hipLaunchKernelGGL((adapt_down<SRC, NR, SAVE>), dim3((unsigned)groups, (unsigned)slices, (unsigned)(a.Rp / (16 * NR))), dim3(64 * waves),
+                     (size_t)waves * lds, st, a);
   return launched();
+}
+template <int SRC, int NR>
+int both_launch(BothArgs& a, int T, int N, int slices, hipStream_t st) {
+  constexpr int lds = down_lds<SRC, NR>() > down_lds<kBf16, NR>() ? down_lds<SRC, NR>() : down_lds<kBf16, NR>();
+  const int64_t tiles = f8_request_tiles(T, N), groups = tiles * (4 / kFragments<kBf16, NR> + 4 / kFragments<SRC, NR>);
+  const int waves = down_waves(8, a.x.per > a.y.per ? a.x.per : a.y.per);
+  if (!f8_fits_x(groups, 512)) return BSP_ERR_SHAPE;
+  a.first = (int32_t)(tiles * (4 / kFragments<kBf16, NR>));
+  static const bool raised = raise((const void*)&adapt_down_both<SRC, NR>, 8 * lds);
+  if (!raised) return BSP_ERR_HIP;
+  hipLaunchKernelGGL((adapt_down_both<SRC, NR>), dim3((unsigned)groups, (unsigned)slices, (unsigned)(a.x.Rp / (16 * NR))), dim3(64 * waves), (size_t)waves * lds, st, a);
+  return launched();
+}
+template <class Run>
+int by_rank(int Rp, Run run) {
+  switch (Rp) {
+    case 16: return run(std::integral_constant<int, 1>{});
+    case 32: return run(std::integral_constant<int, 2>{});
+    default: return run(std::integral_constant<int, 4>{});  // (128: in two halves)
+  }
 }
 template <int SRC, bool SAVE>
 int down_rank(const DownArgs& a, int T, int N, int slices, hipStream_t st) {
-  switch (a.Rp) {
-    case 16: return down_launch<SRC, 1, SAVE>(a, T, N, slices, st);
-    case 32: return down_launch<SRC, 2, SAVE>(a, T, N, slices, st);
-    default: return down_launch<SRC, 4, SAVE>(a, T, N, slices, st);  // (128: in two halves)
-  }
+  return by_rank(a.Rp, [&](auto nr) { return down_launch<SRC, decltype(nr)::value, SAVE>(a, T, N, slices, st); });
+}
+template <int SRC>
+int both_rank(BothArgs& a, int T, int N, int slices, hipStream_t st) {
+  return by_rank(a.x.Rp, [&](auto nr) { return both_launch<SRC, decltype(nr)::value>(a, T, N, slices, st); });
+}
+DownArgs down_args(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, int slices) {
+  DownArgs a{};
+  a.X = x.X, a.scale = x.scale, a.ld = x.ld, a.srows = f8_scale_rows(T), a.down = transposed ? d.b_t : d.a, a.factor = d.scale, a.u = u, a.q = q;
+  a.T = T, a.K = transposed ? d.O : d.I, a.Kp = transposed ? d.Op : d.Ip, a.Rp = d.Rp, a.e5 = x.e5;
+  const int64_t size = x.dtype == BSP_F32 ? 4 : x.dtype == BSP_BF16 ? 2 : 1;
+  a.aligned = (((uintptr_t)x.X | (uintptr_t)(x.ld * size)) & 15) == 0;
+  a.per = (f8_blocks(a.K) + slices - 1) / slices;
+  return a;
 }
 
 // ------------------------------------------------------------------ gradients
@@ -430,6 +487,7 @@ struct GradArgs {
   float* part;            // [slots][R I + O R]
   int32_t N, R, I, O, blocks_o, chunk;
   int32_t src;            // of X
+  int32_t each;           // a chunk is an adapter
 };
 
 // Which adapter's rows chunk number k holds, and where its sums go.  The same in all lanes.
@@ -615,14 +673,27 @@ __device__ __forceinline__ void grad_side(const GradArgs& a, const Chunk& k, boo
   }
 }
 
+// Where no adapter can have more than one chunk a workgroup takes an adapter, and one without rows gets its zeros here: a launch less.
+template <int RP>
+__device__ __forceinline__ void no_rows(const GradArgs& a, int of, bool in_y, int kb) {
+  const int r0 = blockIdx.z * RP;
+  for (int i = threadIdx.x; i < 128 * RP; i += 256) {
+    const int r = r0 + (in_y ? i % RP : i / 128), c = kb * 128 + (in_y ? i / RP : i % 128);
+    if (r >= a.R || c >= (in_y ? a.O : a.I)) continue;
+    if (in_y) a.dB[((int64_t)of * a.O + c) * a.R + r] = 0.f;
+    else a.dA[((int64_t)of * a.R + r) * a.I + c] = 0.f;
+  }
+}
 template <int RP>
 __global__ __launch_bounds__(256) void adapt_grad(GradArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kStep * (256 + 64 * ((3 * RP + 31) / 32) + 16)];
-  const Chunk k = find_chunk(a.q, a.N, a.chunk, blockIdx.y);
+  const int y = blockIdx.y;
+  const Chunk k = a.each ? Chunk{y, a.q.start[y], a.q.start[y + 1] - a.q.start[y], -1} : find_chunk(a.q, a.N, a.chunk, y);
   if (k.of >= a.N) return;
   const bool in_y = (int)blockIdx.x < a.blocks_o;
   const int kb = in_y ? blockIdx.x : blockIdx.x - a.blocks_o;
-  if (!in_y && a.src != kBf16) grad_side<RP, true, true>(a, k, in_y, kb, lds);
+  if (k.rows == 0) no_rows<RP>(a, k.of, in_y, kb);
+  else if (!in_y && a.src != kBf16) grad_side<RP, true, true>(a, k, in_y, kb, lds);
   else if (kb * 128 + 128 <= (in_y ? a.O : a.I)) grad_side<RP, false, true>(a, k, in_y, kb, lds);
   else grad_side<RP, false, false>(a, k, in_y, kb, lds);
 }
@@ -706,14 +777,10 @@ int f8_down_slices(int T, int N, int K, bool grad) {
   while (slices < most && tiles * slices < 256 && f8_blocks(K) >= 16 * slices) slices *= 2;
   return slices;
 }
-int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, bool grad, uint8_t* codes, uint8_t* scale, hipStream_t st) {
-  DownArgs a{};
-  a.X = x.X, a.scale = x.scale, a.ld = x.ld, a.srows = f8_scale_rows(T), a.down = transposed ? d.b_t : d.a, a.factor = d.scale, a.u = u, a.q = q;
-  a.T = T, a.K = transposed ? d.O : d.I, a.Kp = transposed ? d.Op : d.Ip, a.Rp = d.Rp, a.e5 = x.e5, a.codes = codes, a.to_scale = scale;
-  const int64_t size = x.dtype == BSP_F32 ? 4 : x.dtype == BSP_BF16 ? 2 : 1;
-  a.aligned = (((uintptr_t)x.X | (uintptr_t)(x.ld * size)) & 15) == 0;
-  const int slices = f8_down_slices(T, d.N, a.K, grad);
-  a.per = (f8_blocks(a.K) + slices - 1) / slices;
+int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, uint8_t* codes, uint8_t* scale, hipStream_t st) {
+  const int slices = f8_down_slices(T, d.N, transposed ? d.O : d.I, false);
+  DownArgs a = down_args(d, transposed, x, T, q, u, slices);
+  a.codes = codes, a.to_scale = scale;
   switch (x.dtype) {
     case BSP_BF16: return codes ? down_rank<kBf16, true>(a, T, d.N, slices, st) : down_rank<kBf16, false>(a, T, d.N, slices, st);
     case BSP_F32: return codes ? down_rank<kF32, true>(a, T, d.N, slices, st) : down_rank<kF32, false>(a, T, d.N, slices, st);
@@ -721,9 +788,19 @@ int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T
     default: return down_rank<kE5, false>(a, T, d.N, slices, st);
   }
 }
+int f8_launch_down_both(const F8Adapters& d, const F8Input& x, const F8Input& dY, int T, const F8Requests& q, float* u, float* v, hipStream_t st) {
+  const int nu = f8_down_slices(T, d.N, d.I, true), nv = f8_down_slices(T, d.N, d.O, true), slices = nu > nv ? nu : nv;
+  BothArgs a{down_args(d, true, dY, T, q, v, nv), down_args(d, false, x, T, q, u, nu), 0};
+  switch (x.dtype) {
+    case BSP_BF16: return both_rank<kBf16>(a, T, d.N, slices, st);
+    case BSP_E4M3: return both_rank<kE4>(a, T, d.N, slices, st);
+    default: return both_rank<kE5>(a, T, d.N, slices, st);
+  }
+}
 
 int64_t f8_adapt_part_bytes(const F8Adapters& d, int T) {
-  const int64_t slots = 2 * (int64_t)T / chunk_of(T, d.I, d.O);  // (an adapter of several chunks has fewer than twice its rows' share)
+  const int chunk = chunk_of(T, d.I, d.O);
+  const int64_t slots = T <= chunk ? 0 : 2 * (int64_t)T / chunk;  // (an adapter of several chunks has fewer than twice its rows' share)
   return slots * ((int64_t)d.R * (d.I + (int64_t)d.O)) * 4;
 }
 int f8_launch_adapt_grad(const F8Adapters& d, const uint16_t* dY, int64_t ldy, const F8Input& x, int T, const F8Requests& q, const float* u, const float* v,
@@ -733,16 +810,16 @@ int f8_launch_adapt_grad(const F8Adapters& d, const uint16_t* dY, int64_t ldy, c
   a.u_step = (int64_t)T * d.Rp, a.u_slices = f8_down_slices(T, d.N, d.I, true), a.v_slices = f8_down_slices(T, d.N, d.O, true), a.Rp = d.Rp;
   a.N = d.N, a.R = d.R, a.I = d.I, a.O = d.O, a.blocks_o = f8_blocks(d.O), a.chunk = chunk_of(T, d.I, d.O);
   a.src = x.dtype == BSP_BF16 ? kBf16 : x.dtype == BSP_E4M3 ? kE4 : kE5;
-  const int64_t chunks = (int64_t)T / a.chunk + (T < d.N ? T : d.N);
+  a.each = T <= a.chunk;
+  const int64_t chunks = a.each ? d.N : (int64_t)T / a.chunk + (T < d.N ? T : d.N);
   const dim3 grid((unsigned)(a.blocks_o + f8_blocks(d.I)), (unsigned)chunks, d.Rp == 128 ? 2 : 1);  // (128 ranks in two halves)
   if (chunks > 65535 || !f8_fits_x(grid.x, 256)) return BSP_ERR_SHAPE;
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a); };
-  if (T > 0) {  // (without rows the sums below are all there is: zeros)
-    if (d.Rp == 16) run(adapt_grad<16>);
-    else if (d.Rp == 32) run(adapt_grad<32>);
-    else run(adapt_grad<64>);
-  }
+  if (d.Rp == 16) run(adapt_grad<16>);
+  else if (d.Rp == 32) run(adapt_grad<32>);
+  else run(adapt_grad<64>);
   if (launched() != BSP_OK) return BSP_ERR_HIP;
+  if (a.each) return BSP_OK;
   const int64_t groups = ((int64_t)d.R * (d.I + (int64_t)d.O) + 1023) / 1024;
   hipLaunchKernelGGL(adapt_join, dim3((unsigned)(groups < 4096 ? groups : 4096), (unsigned)d.N), dim3(256), 0, st, a);
   return launched();

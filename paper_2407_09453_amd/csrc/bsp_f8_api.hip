@@ -362,7 +362,7 @@ int bsp_f8_fc_adapted(const bsp_weights_f8* w, int32_t transposed, const bsp_cod
   const F8Input given = X ? F8Input{X->codes, X->scale, X->dtype, X->dtype == BSP_E5M2, ld} : F8Input{values, nullptr, x_dtype, code == BSP_E5M2, ldx};
   // values that the product wants as codes become them where they are read for u
   uint8_t *to = codes ? (uint8_t*)workspace + sums : nullptr, *to_scale = codes ? to + T * ld : nullptr;
-  rc = f8_launch_down(d, transposed != 0, given, T, who, u, false, to, to_scale, st);
+  rc = f8_launch_down(d, transposed != 0, given, T, who, u, to, to_scale, st);
   if (rc != BSP_OK) return rc;
   const F8Low low{who.which, u, transposed ? d.a_t : d.b, (int64_t)d.Rp * (transposed ? d.Ip : d.Op), (int64_t)T * d.Rp, d.Rp, f8_down_slices(T, d.N, K, false)};
   return multiply(rows, codes ? F8Input{to, to_scale, code, code == BSP_E5M2, ld} : given, T, low, q, y_dtype, workspace, st);
@@ -404,8 +404,7 @@ int bsp_f8_adapters_grad(const bsp_f8_adapters* adapters, const void* dY, int64_
   float *u = (float*)workspace, *v = u + low_bytes(d, T, d.I, true) / 4, *part = v + low_bytes(d, T, d.O, true) / 4;
   const F8Input x = X ? F8Input{X->codes, X->scale, X->dtype, X->dtype == BSP_E5M2, (int64_t)f8_blocks(X->K) * F8_BLOCK} : F8Input{values, nullptr, BSP_BF16, 0, ldx};
   if (T > 0) {
-    rc = f8_launch_down(d, false, x, T, who, u, true, nullptr, nullptr, st);
-    if (rc == BSP_OK) rc = f8_launch_down(d, true, F8Input{dY, nullptr, BSP_BF16, 0, ldy}, T, who, v, true, nullptr, nullptr, st);
+    rc = f8_launch_down_both(d, x, F8Input{dY, nullptr, BSP_BF16, 0, ldy}, T, who, u, v, st);
     if (rc != BSP_OK) return rc;
   }
   return f8_launch_adapt_grad(d, (const uint16_t*)dY, ldy, x, T, who, u, v, part, dA, dB, st);

@@ -418,11 +418,11 @@ def _rms_norm(X, weight, residual, eps, code):
     if residual is not None:
         T2, D2, ldr = _rows(residual)
         assert (T2, D2) == (T, D) and residual.dtype == X.dtype, "a residual of X's shape and type"
-        H = torch.empty((T, D), dtype=X.dtype, device=X.device)
+        H = X.new_empty((T, D))
         r, h = residual.data_ptr(), H.data_ptr()
-    rstd = torch.empty(T, dtype=torch.float32, device=X.device)
+    rstd = X.new_empty(T, dtype=torch.float32)
     if code is None:
-        Y = torch.empty((T, D), dtype=X.dtype, device=X.device)
+        Y = X.new_empty((T, D))
         y, words = Y.data_ptr(), _NO_CODES
     else:
         Y = BspCodes(T, D, code, X.device)
@@ -449,10 +449,10 @@ def rms_norm_grad(dY, H, rstd, weight=None, dH=None, stream=None):
         assert (T2, D2) == (T, D) and dH.dtype == H.dtype
         d = dH.data_ptr()
     _on(H, dY, rstd, weight, dH)
-    dX = torch.empty((T, D), dtype=H.dtype, device=H.device)
-    dw = torch.empty(D, dtype=torch.float32, device=H.device)
+    dX = H.new_empty((T, D))
+    dw = rstd.new_empty(D)
     n = _bytes_of("bsp_rms_norm_grad_workspace", T, D)
-    ws = torch.empty(n, dtype=torch.uint8, device=H.device) if n else None
+    ws = H.new_empty(n, dtype=torch.uint8) if n else None
     _call(_RMS_GRAD, _pack17(dY.data_ptr(), ld_dy, H.data_ptr(), ld, d, ld_dh, _type(H), T, D, rstd.data_ptr(), _vector(weight, D), dX.data_ptr(), D,
                              dw.data_ptr(), 0 if ws is None else ws.data_ptr(), n, _current_stream(H)), "bsp_rms_norm_grad")
     return dX, dw
