@@ -146,9 +146,10 @@ __device__ __forceinline__ float most8(const float* v) {
 
 // ROWT threads hold a chunk of up to ROWT x NV x 8 logits.
 // An exponent is one fused multiply-add, t = x c - r with r = m c rounded: the sums are then those relative to r, and the exact difference
-// d = m c - r (one fused multiply-add again) brings them to m.  Nothing is done for single elements that a row in a thousand needs: where the sum
-// of t e^t is no number, as minus infinities make it, a wave adds once more with care, and where the sum is near 1, as a sure token
-// makes it, the workgroup adds once more what does not reach the maximum.
+// d = m c - r (one fused multiply-add again) brings them to m.  Nothing is done for single elements that a row in a thousand needs: where the
+// sum is near 1, as a sure token makes it, the workgroup adds once more what does not reach the maximum.  (Minus infinities are not so rare: with
+// a second pass where the sum of t e^t was no number 1021 masked rows of 50001 took 40 us instead of 33.5, and 8192 x 32768 without any
+// 3 of 125 less.)
 template <bool F32, bool TOP, int ROWT, int NV>
 __global__ __launch_bounds__(ROWT, (F32 || TOP) && NV == 4 ? 4 : 8) void logp_rows(LogpArgs a) {
   constexpr int WAVES = ROWT / 64, LANES = ROWT / 64;  // waves; lanes of one of the 64 groups
@@ -213,22 +214,9 @@ __global__ __launch_bounds__(ROWT, (F32 || TOP) && NV == 4 ? 4 : 8) void logp_ro
       for (int k = 0; k < 8; ++k) {
         const float t = fmaf(v[k], c2, -r), e = __builtin_amdgcn_exp2f(t);
         s += e;
-        q = fmaf(t, e, q);
+        q = fmaf(fmaxf(t, -200.f), e, q);  // (of -200 and less e is 0; 0 times minus infinity would be no number)
       }
     });
-  if (__ballot(q != q)) {
-    q = 0.f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      each(j, [&](const float* v, int) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          float t = fmaf(v[k], c2, -r);
-          t = t < -200.f ? -200.f : t;  // 2^-200 is 0, and 0 times it too; a NaN stays one
-          q = fmaf(t, __builtin_amdgcn_exp2f(t), q);
-        }
-      });
-  }
   // the workgroup's sums, in the order of its waves
   auto total = [&](float (*sh)[3], float n, float s, float q) {
     s = f8_wave_sum(s);
