@@ -124,11 +124,6 @@ __device__ __forceinline__ void store_tile(const F8Epilogue& q, f32x16_t (&acc)[
   }
 }
 
-// The rows' adapters: B_a u_t added to a wave's sums, one adapter of its rows after the other, the next ones' weights asked for while one is
-// multiplied.  u enters as two bf16 parts (for fp32 results three), as zeros in the rows of other adapters: the rows are the matrix instruction's columns, and the
-// sums go on where they are.  Zero times what is no number is none: an adapter with such weights among its
-// rows' neighbours is multiplied from zero, and a lane, which holds results of one row, takes or leaves what it gives (three times the
-// instructions: 16384 x 4096 -> 4096 with rows of twelve adapters mixed 304 us where all go that way).
 // The wait between a matrix instruction and the first use of its result, by hand: where two ways meet again behind it, a branch that is taken or
 // not, the compiler counts the instructions of one of them, be it the longer (found where channel 31 of a result lost its second part).
 __device__ __forceinline__ void settle() {
@@ -210,6 +205,13 @@ __device__ __forceinline__ void add_low_rows(const F8Low& low, f32x16_t (&acc)[M
   }
 }
 
+// The rows' adapters: B_a u_t added to a wave's sums, one adapter of its rows after the other, the next ones' weights asked for while one is
+// multiplied.  u enters as two bf16 parts (for fp32 results three), as zeros in the rows of other adapters: the rows are the matrix instruction's
+// columns, and the sums go on where they are.  Zero times what is no number is none: an adapter with such weights among its rows'
+// neighbours is multiplied from zero, and a lane, which holds results of one row, takes or leaves what it gives.
+// Bound by the instructions of each adapter among a wave's rows, behind a product that leaves none of their time free (16384 x 4096 -> 4096 of rank
+// 16, us: the product 225 to 250; with twelve adapters in runs of rows 17 more, their rows mixed 70, 85 where all have weights that are no
+// numbers; with 32 mixed 120.  64 x 4096 -> 16384 of 32 mixed: 15, with them 25).
 template <int MO, int MT, int PARTS>
 __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT], int T, int64_t t0, int o0) {
   const int lane = threadIdx.x & 63;

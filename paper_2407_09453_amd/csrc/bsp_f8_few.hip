@@ -83,7 +83,8 @@ __device__ __forceinline__ void few_stage(const FewArgs& a, uint8_t* codes, uint
 template <int MT>
 constexpr int kMostWaves = MT == 1 ? 16 : 8;
 
-// four channels' share of a row's adapter: fp32 products of u with bf16 weights
+// four channels' share of a row's adapter: fp32 products of u with bf16 weights, while the wave's first blocks are on their way (1 x 4096 -> 4096 of rank 16
+// 6.3 us without, 7.7 with)
 __device__ __forceinline__ f32x4_t few_low(const F8Low& low, int64_t row, int o) {
   f32x4_t s = {};
   const int of = low.which[row];

@@ -7,6 +7,8 @@
 // reads h, differentiates the very function that ran.  A row is read once and stays in the registers of the 16 to 1024 threads that
 // own it; squares are summed in fp32.  Rows too long for that are read again.  As in the layer norm the gradient's threads own columns and
 // add dw over all the rows of their workgroup, and a second launch adds the workgroups' sums in a fixed order.
+// Measured: 16384 x 4096 bf16 with a residual to codes 74 to 83 us (470 MB, 5.7 to 6.3 TB/s), its gradient 100 to 113 (537 MB, 4.8 to 5.4 TB/s) and 5 for
+// the sums; 777 x 2966 fp32 7.8 and 9.6 (18 and 28 MB, from the last-level cache) and 4.2; one row of 4096 3.4.
 #include "bsp_norm.h"
 
 namespace {
@@ -297,7 +299,7 @@ int backward(const RmsArgs& a, hipStream_t st) {
 // Workgroups that share the rows.  Where one is done with all of them in eight turns its sums are the result: a launch less.
 int rms_parts(int T, int D) {
   const int64_t turns = ((int64_t)T + rows_at_once(D) - 1) / rows_at_once(D);
-  const int most = D > 4096 ? 256 : 512;  // as many as the chip holds at one time
+  const int most = D > 4096 ? 256 : 512;  // as many as the chip holds at one time (16384 x 4096: 768 and 1024 are slower)
   return turns <= 8 ? 1 : turns < most ? (int)turns : most;
 }
 
