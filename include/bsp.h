@@ -543,7 +543,8 @@ int bsp_f8_requests_plan(const bsp_f8_requests* r, const void* which, int32_t wh
 
 /* bsp_f8_fc (X: codes) or bsp_f8_fc_values (X null: values of x_dtype) with adapters; transposed, the gradient of the layer's input, in which
  * a row gets s_a A_a^t (B_a^t x_t).  T, N, I and O have to agree.  workspace: bsp_f8_fc_adapted_workspace bytes (coded: 0 for values, 1 for
- * codes, and for values that become codes inside the product's kernel).  Errors: as these. */
+ * codes, and for values that become codes inside the product's kernel; many rows of several adapters may be copied there in the order of their
+ * adapters).  Errors: as these. */
 int bsp_f8_fc_adapted_workspace(const bsp_weights_f8* w, int32_t transposed, int32_t T, int32_t coded, const bsp_f8_adapters* adapters, int64_t* bytes);
 int bsp_f8_fc_adapted(const bsp_weights_f8* w, int32_t transposed, const bsp_codes* X, const void* values, int32_t x_dtype, int64_t ldx, int32_t T,
                       int32_t code, const bsp_f8_adapters* adapters, const bsp_f8_requests* requests, const float* bias, const void* residual,

@@ -286,7 +286,7 @@ struct F8Input {      // rows to multiply: codes with their scales, or values br
 // have none.
 struct F8Requests {
   int32_t *start, *which, *order;  // [N + 1], [T] (-1: none), [T]
-  int32_t* tiles;                  // how many tiles have an adapter, how many there are, two words; then the tiles' records
+  int32_t* tiles;                  // how many tiles have an adapter, how many there are, whether the adapters' rows are mixed, a word; then the tiles' records
 };
 struct F8Adapters {  // bf16, ranks padded to Rp with zeros, columns to whole blocks
   uint16_t *a, *a_t, *b, *b_t;  // [N][Rp Ip] by rank and by column, [N][Op Rp] by column and by rank, as adapt_set lays them out
@@ -301,6 +301,9 @@ struct F8Low {
   int64_t step, u_step;  // elements of an adapter, of a slice
   int32_t rank;          // 0: nothing is added
   int32_t slices;
+  // Where the adapters' rows are mixed many rows are multiplied in the order of their adapters: row i of these codes is row order[i], or null
+  const int32_t *mixed, *order;
+  const uint8_t *codes, *scale;
 };
 // Few rows: the contraction split over a workgroup's waves.  Rows given as values become codes in each workgroup's LDS, T <= 16 of them and
 // no more than kFewStaged bytes.
@@ -337,8 +340,9 @@ F8Adapters f8_adapters_of(const bsp_f8_adapters* d);
 int f8_launch_plan(const bsp_f8_requests* r, const void* which, bool wide, hipStream_t st);
 int f8_launch_set(const F8Adapters& d, int slot, int rank, const void* A, int64_t lda, const void* B, int64_t ldb, bool f32, float scale, hipStream_t st);
 int f8_down_slices(int T, int N, int K, bool grad);  // of u: up to eight for a product, two for the gradients
-// codes, scale: where values are to become codes (of x.e5) on the way, too; or null
-int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, uint8_t* codes, uint8_t* scale, hipStream_t st);
+// codes, scale: where values are to become codes (of x.e5) on the way, too, or where codes go, mixed and `sorts`; or null.  sorts: mixed rows leave in
+// the order of their adapters
+int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, uint8_t* codes, uint8_t* scale, bool sorts, hipStream_t st);
 // u of the layer's input and v of its result's gradient (bf16)
 int f8_launch_down_both(const F8Adapters& d, const F8Input& x, const F8Input& dY, int T, const F8Requests& q, float* u, float* v, hipStream_t st);
 int64_t f8_adapt_part_bytes(const F8Adapters& d, int T);

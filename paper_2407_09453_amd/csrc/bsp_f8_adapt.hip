@@ -10,7 +10,7 @@
 // `down` is bound by the bytes of the rows on many rows, by latency on few.  `grad` reads each block of 128 columns of the rows of an adapter
 // once: both operands are summed over rows, so they lie in LDS as in memory and the transposing read hands a lane a column's
 // rows.  An adapter with many rows is cut into chunks whose sums a second launch joins, in order: no atomics.
-// Measured: A x of 16384 x 4096 codes, rank 16 18 to 20 us (3.5 TB/s), of 8192 x 16384 bf16, rank 32 52 to 62 (4.3 to 5.1 TB/s), with the rows' codes on
+// Measured: A x of 16384 x 4096 codes, rank 16 18 to 20 us (3.5 TB/s), rank 32 22.6, of 8192 x 16384 bf16, rank 32 52 to 62 (4.3 to 5.1 TB/s), with the rows' codes on
 // the way 111 to 125 (403 MB, 3.4 TB/s), of one row of 4096 4.4; grad of 8192 rows, 4096 codes and 16384 bf16, rank 32 80 to 91 (302 MB, 3.3 to 3.8 TB/s)
 // and 4 to 9 to join; 37 rows of 1000 and 520 columns 5.4 for u and v, 6.4 for the gradients.  The plan of 64 rows 5 to 9 us, of 8192 28, of 16384 50.
 #include "bsp_norm.h"
@@ -21,24 +21,27 @@ namespace {
 
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;
-constexpr int kTileRows = 64, kTileWords = 4 + kTileRows;  // a tile's record: adapter (-1: none), rows, two words, the rows' numbers (past the last: its)
+constexpr int kTileRows = 64, kTileWords = 4 + kTileRows;  // a tile's record: adapter (-1: none), rows, place of the first in the order, a word, the rows' numbers (past the last: its)
 
 inline int launched() { return hipGetLastError() == hipSuccess ? BSP_OK : BSP_ERR_HIP; }
 
 // ------------------------------------------------------------------ which rows are whose
 // Rows sorted by adapter, in their order within each, those of none last (counted, not compared: one workgroup of sixteen waves, each with a range
 // of the rows).  Ids that are no adapter's become -1.  Tiles of up to 64 rows of one adapter hold their rows' numbers themselves, so
-// that a kernel that works on one finds all it needs with one load.
+// that a kernel that works on one finds all it needs with one load.  Rows are mixed where more than a row
+// in eight has another adapter than the row before: then the products of many rows go through them in this order (us, A x and the product, as
+// they come and so, the codes' copy included: 16384 x 4096 -> 4096 of rank 16, twelve adapters mixed 322 and 282, 32 364 and 283; 2048 rows of 32
+// 73 and 51; 4877 x 5816 -> 4224 of rank 19, 39 337 and 187; in runs, which stay as they are, 280).
 template <class Id>
 __global__ __launch_bounds__(1024) void adapt_plan(const Id* ids, int T, int N, F8Requests q) {
   extern __shared__ int32_t hist[];  // [16][N], behind them the tiles' first numbers [N + 1]
-  __shared__ int32_t sh[3][16];
+  __shared__ int32_t sh[4][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int32_t* first_tile = hist + 16 * N;
   for (int i = tid; i < 16 * N; i += 1024) hist[i] = 0;
   __syncthreads();
   const int64_t per = ((int64_t)T + 1023) / 1024 * 64, begin = wave * per < T ? wave * per : T, end = begin + per < T ? begin + per : T;
-  int with = 0;  // this wave's rows that have an adapter
+  int with = 0, changes = 0;  // this wave's rows that have an adapter, that have another than the row before
   for (int64_t t0 = begin; t0 < end; t0 += 64) {
     const int64_t t = t0 + lane;
     const Id id = t < end ? ids[t] : -1;
@@ -46,8 +49,10 @@ __global__ __launch_bounds__(1024) void adapt_plan(const Id* ids, int T, int N, 
     if (t < end) q.which[t] = a;
     if (a >= 0) atomicAdd(&hist[wave * N + a], 1);  // (a count: the same in any order)
     with += __popcll(__ballot(a >= 0));
+    const Id id0 = t > 0 && t < end ? ids[t - 1] : id;
+    changes += __popcll(__ballot(a != (id0 >= 0 && id0 < N ? (int32_t)id0 : -1)));
   }
-  if (lane == 0) sh[2][wave] = with;
+  if (lane == 0) sh[2][wave] = with, sh[3][wave] = changes;
   __syncthreads();
   // N <= 1024: an adapter a thread
   int total = 0;
@@ -65,10 +70,10 @@ __global__ __launch_bounds__(1024) void adapt_plan(const Id* ids, int T, int N, 
   }
   if (lane == 63) sh[0][wave] = rows, sh[1][wave] = tiles;
   __syncthreads();
-  int all_rows = 0, all_tiles = 0, none_at = 0;  // none_at: this wave's first row without an adapter, among all such
+  int all_rows = 0, all_tiles = 0, all_changes = 0, none_at = 0;  // none_at: this wave's first row without an adapter, among all such
   for (int w = 0; w < 16; ++w) {
     if (w < wave) rows += sh[0][w], tiles += sh[1][w], none_at -= sh[2][w];
-    all_rows += sh[0][w], all_tiles += sh[1][w];
+    all_rows += sh[0][w], all_tiles += sh[1][w], all_changes += sh[3][w];
   }
   none_at += all_rows + (int)begin;
   if (tid < N) {
@@ -78,7 +83,7 @@ __global__ __launch_bounds__(1024) void adapt_plan(const Id* ids, int T, int N, 
     first_tile[tid] = tiles - (total + kTileRows - 1) / kTileRows;
   }
   const int none_tiles = (T - all_rows + kTileRows - 1) / kTileRows;
-  if (tid == 0) q.start[N] = all_rows, first_tile[N] = all_tiles, q.tiles[0] = all_tiles, q.tiles[1] = all_tiles + none_tiles;
+  if (tid == 0) q.start[N] = all_rows, first_tile[N] = all_tiles, q.tiles[0] = all_tiles, q.tiles[1] = all_tiles + none_tiles, q.tiles[2] = all_changes > T / 8;
   __syncthreads();
   for (int64_t t0 = begin; t0 < end; t0 += 64) {
     const int64_t t = t0 + lane;
@@ -114,7 +119,7 @@ __global__ __launch_bounds__(1024) void adapt_plan(const Id* ids, int T, int N, 
     const int from = q.start[of] + (tile - first_tile[of]) * kTileRows, left = (of < N ? q.start[of + 1] : T) - from;
     int32_t* record = q.tiles + 4 + (int64_t)tile * kTileWords;
     record[4 + r] = q.order[from + (r < left ? r : left - 1)];
-    if (r == 0) record[0] = of < N ? of : -1, record[1] = left < kTileRows ? left : kTileRows;
+    if (r == 0) record[0] = of < N ? of : -1, record[1] = left < kTileRows ? left : kTileRows, record[2] = from;
   }
 }
 
@@ -163,6 +168,7 @@ struct DownArgs {
   int32_t T, K, Kp, Rp, per;  // per: blocks of a slice
   int32_t e5, aligned;        // aligned: rows begin at 16 bytes
   uint8_t *codes, *to_scale;  // SAVE: the rows as codes, too
+  int32_t sorts;              // mixed rows' codes go in the order of their adapters
 };
 
 __device__ __forceinline__ u32x4_t pack8(const float* v) {
@@ -200,10 +206,11 @@ __device__ __forceinline__ void settle(f32x4_t (&acc)[NR][M]) {
 // while the matrix instruction wants sixteen rows' pieces side by side.  A row of pieces of 16 bytes is permuted by its number, so that
 // these lie in different banks.  In a block a lane's columns are 64 q + 16 g + 8 h + 0..7.  The ranks are the matrix
 // instruction's rows and the rows its columns, so nothing of one row, NaN among it, reaches another's sums.  SAVE: the rows become
-// codes on the way, as f8_save makes them, rows without an adapter too: four lanes hold a row's 128 columns.
+// codes on the way, as f8_save makes them, rows without an adapter too: four lanes hold a row's 128 columns.  Rows that are codes are copied where
+// they are mixed.
 // (64 rows, for an adapter's columns are read again for every tile.)
 template <int SRC, int NR>
-constexpr int kFragments = SRC == kF32 ? 1 : SRC == kBf16 || NR == 4 ? 2 : 4;  // of sixteen rows
+constexpr int kFragments = SRC == kF32 ? 1 : SRC == kBf16 || NR > 1 ? 2 : 4;  // of sixteen rows
 
 // lds: [waves][rows of a block]; then sums [waves][NR][M][64][4]
 template <int SRC, int NR, bool SAVE>
@@ -221,15 +228,14 @@ __device__ __forceinline__ void down(const DownArgs& a, int block, uint8_t* lds)
   int64_t asked[kAsks];
 #pragma unroll
   for (int q = 0; q < kAsks; ++q) asked[q] = rows[q * kAtOnce + lane / kPieces];
-  int64_t t[SAVE || kCoded ? M : 1];
-  if constexpr (SAVE || kCoded)
+  int32_t t[kCoded ? M : 1];
+  if constexpr (kCoded)
 #pragma unroll
     for (int m = 0; m < M; ++m) t[m] = rows[m * 16 + r];
-  int64_t leaves[SAVE ? 2 * M : 1];  // the rows of the codes that this lane puts out
-  if constexpr (SAVE)
-#pragma unroll
-    for (int q = 0; q < 2 * M; ++q) leaves[q] = rows[q * 8 + (lane >> 3)];
-  const bool saves = SAVE && blockIdx.z == 0;
+  // where the codes go, by their row in this part of the tile
+  const bool sorted = SAVE && a.sorts && a.q.tiles[2], saves = SAVE && blockIdx.z == 0 && (!kCoded || sorted);
+  const int first = SAVE ? __builtin_amdgcn_readfirstlane(record[2]) + part * M * 16 : 0;
+  auto goes = [&](int row) { return (int64_t)(kCoded || sorted ? first + row : rows[row]); };
   const int nb = a.Kp >> 7, kb0 = blockIdx.y * a.per, kb1 = kb0 + a.per < nb ? kb0 + a.per : nb;
   if (tile >= a.q.tiles[saves ? 1 : 0] || n <= 0 || kb0 >= nb) return;  // (no slice is empty: f8_down_slices)
   auto key = [](int row) { return kCoded ? (row >> 1) & 7 : row & 15; };
@@ -283,8 +289,8 @@ __device__ __forceinline__ void down(const DownArgs& a, int block, uint8_t* lds)
 #pragma unroll
       for (int m = 0; m < M; ++m) s[m] = a.scale[kb * a.srows + t[m]];
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    u32x4_t codes[SAVE ? M : 1][2];
-    int bytes[SAVE ? M : 1];
+    u32x4_t codes[SAVE && !kCoded ? M : 1][2];
+    int bytes[SAVE && !kCoded ? M : 1];
 #pragma unroll
     for (int m = 0; m < M; ++m) {
       const uint8_t* row = mine + (m * 16 + r) * kRow;
@@ -327,7 +333,7 @@ __device__ __forceinline__ void down(const DownArgs& a, int block, uint8_t* lds)
             acc[i][m] = mfma_bf16_16x16x32(wv[i][j], xs[j], acc[i][m]);
           }
         }
-      if constexpr (SAVE) {
+      if constexpr (SAVE && !kCoded) {
         uint32_t most = 0;
         float y[4][8];
 #pragma unroll
@@ -360,16 +366,17 @@ __device__ __forceinline__ void down(const DownArgs& a, int block, uint8_t* lds)
 #pragma unroll
         for (int m = 0; m < M; ++m) {
           const int row = m * 16 + r;
+          if constexpr (!kCoded)  // (as codes lie there from the start)
 #pragma unroll
-          for (int q = 0; q < 2; ++q) *(u32x4_t*)(mine + row * 128 + (((4 * q + g) ^ ((row >> 1) & 7)) << 4)) = codes[m][q];
-          if (g == 0 && row < n) a.to_scale[kb * a.srows + t[m]] = (uint8_t)bytes[m];
+            for (int q = 0; q < 2; ++q) *(u32x4_t*)(mine + row * 128 + (((4 * q + g) ^ ((row >> 1) & 7)) << 4)) = codes[m][q];
+          if (g == 0 && row < n) a.to_scale[kb * a.srows + goes(row)] = (uint8_t)(kCoded ? s[kCoded ? m : 0] : bytes[kCoded ? 0 : m]);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
         for (int q = 0; q < 2 * M; ++q) {
           const int row = q * 8 + (lane >> 3), p = lane & 7;
           const u32x4_t c = *(const u32x4_t*)(mine + row * 128 + ((p ^ ((row >> 1) & 7)) << 4));
-          if (row < n) *(u32x4_t*)(a.codes + leaves[q] * a.Kp + kb * 128 + p * 16) = c;
+          if (row < n) *(u32x4_t*)(a.codes + goes(row) * a.Kp + kb * 128 + p * 16) = c;
         }
       }
     }
@@ -394,8 +401,10 @@ __device__ __forceinline__ void down(const DownArgs& a, int block, uint8_t* lds)
   }
 }
 
+template <int SRC>
+constexpr bool kValues = SRC == kBf16 || SRC == kF32;
 template <int SRC, int NR, bool SAVE>
-__global__ __launch_bounds__(SAVE ? 256 : 512, SAVE ? (NR == 4 ? 2 : 3) : NR == 4 ? 2 : 4) void adapt_down(DownArgs a) {
+__global__ __launch_bounds__(SAVE && kValues<SRC> ? 256 : 512, SAVE && kValues<SRC> ? (NR == 4 ? 2 : 3) : NR == 4 ? 2 : 4) void adapt_down(DownArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   kernarg_touch<DownArgs>();
   down<SRC, NR, SAVE>(a, blockIdx.x, lds);
@@ -427,7 +436,7 @@ inline bool raise(const void* kernel, int lds) { return hipFuncSetAttribute(kern
 
 template <int SRC, int NR, bool SAVE>
 int down_launch(const DownArgs& a, int T, int N, int slices, hipStream_t st) {
-  constexpr int most = SAVE ? 4 : 8, lds = down_lds<SRC, NR>();
+  constexpr int most = SAVE && kValues<SRC> ? 4 : 8, lds = down_lds<SRC, NR>();
   const int64_t groups = f8_request_tiles(T, N) * (4 / kFragments<SRC, NR>);
   const int waves = down_waves(most, a.per);
   if (!f8_fits_x(groups, 512)) return BSP_ERR_SHAPE;
@@ -784,15 +793,15 @@ int f8_down_slices(int T, int N, int K, bool grad) {
   while (slices < most && tiles * slices < 256 && f8_blocks(K) >= 16 * slices) slices *= 2;
   return slices;
 }
-int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, uint8_t* codes, uint8_t* scale, hipStream_t st) {
+int f8_launch_down(const F8Adapters& d, bool transposed, const F8Input& x, int T, const F8Requests& q, float* u, uint8_t* codes, uint8_t* scale, bool sorts, hipStream_t st) {
   const int slices = f8_down_slices(T, d.N, transposed ? d.O : d.I, false);
   DownArgs a = down_args(d, transposed, x, T, q, u, slices);
-  a.codes = codes, a.to_scale = scale;
+  a.codes = codes, a.to_scale = scale, a.sorts = sorts;
   switch (x.dtype) {
     case BSP_BF16: return codes ? down_rank<kBf16, true>(a, T, d.N, slices, st) : down_rank<kBf16, false>(a, T, d.N, slices, st);
     case BSP_F32: return codes ? down_rank<kF32, true>(a, T, d.N, slices, st) : down_rank<kF32, false>(a, T, d.N, slices, st);
-    case BSP_E4M3: return down_rank<kE4, false>(a, T, d.N, slices, st);
-    default: return down_rank<kE5, false>(a, T, d.N, slices, st);
+    case BSP_E4M3: return codes ? down_rank<kE4, true>(a, T, d.N, slices, st) : down_rank<kE4, false>(a, T, d.N, slices, st);
+    default: return codes ? down_rank<kE5, true>(a, T, d.N, slices, st) : down_rank<kE5, false>(a, T, d.N, slices, st);
   }
 }
 int f8_launch_down_both(const F8Adapters& d, const F8Input& x, const F8Input& dY, int T, const F8Requests& q, float* u, float* v, hipStream_t st) {

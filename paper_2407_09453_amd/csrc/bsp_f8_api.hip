@@ -125,6 +125,8 @@ int check_requests(const bsp_f8_requests* r) {
   if (r->T > 0 && !r->plan) return BSP_ERR_NULL;
   return aligned(r->plan, 16) ? BSP_OK : BSP_ERR_ALIGN;
 }
+// whether rows of several adapters may be multiplied in another order than their own (see F8Low)
+bool sorts(const F8Adapters& d, int T) { return d.N > 1 && T > kFewRows; }
 int64_t in16(int64_t bytes) { return (bytes + 15) & ~(int64_t)15; }
 int64_t low_bytes(const F8Adapters& d, int T, int K, bool grad) { return (int64_t)T * d.Rp * 4 * f8_down_slices(T, d.N, K, grad); }
 
@@ -324,9 +326,11 @@ int bsp_f8_requests_plan(const bsp_f8_requests* r, const void* which, int32_t wh
 }
 
 int bsp_f8_fc_adapted_workspace(const bsp_weights_f8* w, int32_t transposed, int32_t T, int32_t coded, const bsp_f8_adapters* adapters, int64_t* bytes) {
-  int rc = bsp_f8_fc_workspace(w, transposed, T, coded, bytes);
-  if (rc == BSP_OK) rc = check_adapters(adapters);
-  if (rc == BSP_OK) *bytes = in16(*bytes) + low_bytes(f8_adapters_of(adapters), T, transposed ? w->O : w->I, false);
+  int rc = bytes ? check_adapters(adapters) : BSP_ERR_NULL;
+  if (rc != BSP_OK) return rc;
+  const F8Adapters d = f8_adapters_of(adapters);
+  rc = bsp_f8_fc_workspace(w, transposed, T, coded && !sorts(d, T), bytes);
+  if (rc == BSP_OK) *bytes = in16(*bytes) + low_bytes(d, T, transposed ? w->O : w->I, false);
   return rc;
 }
 
@@ -352,7 +356,7 @@ int bsp_f8_fc_adapted(const bsp_weights_f8* w, int32_t transposed, const bsp_cod
   if (T == 0) return BSP_OK;
   const F8Rows rows = rows_of(w, transposed != 0);
   const F8Adapters d = f8_adapters_of(adapters);
-  const int64_t sums = sums_bytes(rows, T), codes = X || in_kernel(values, x_dtype, ldx, T, K) ? 0 : codes_bytes(T, K);
+  const int64_t sums = sums_bytes(rows, T), codes = (X && !sorts(d, T)) || (!X && in_kernel(values, x_dtype, ldx, T, K)) ? 0 : codes_bytes(T, K);
   rc = check_workspace(workspace, workspace_bytes, in16(sums + codes) + low_bytes(d, T, K, false));
   if (rc != BSP_OK) return rc;
   hipStream_t st = (hipStream_t)stream;
@@ -360,12 +364,13 @@ int bsp_f8_fc_adapted(const bsp_weights_f8* w, int32_t transposed, const bsp_cod
   float* u = (float*)((uint8_t*)workspace + in16(sums + codes));
   const int64_t ld = (int64_t)f8_blocks(K) * F8_BLOCK;
   const F8Input given = X ? F8Input{X->codes, X->scale, X->dtype, X->dtype == BSP_E5M2, ld} : F8Input{values, nullptr, x_dtype, code == BSP_E5M2, ldx};
-  // values that the product wants as codes become them where they are read for u
+  // values that the product wants as codes become them where they are read for u, where codes that it wants in another order are copied, too
   uint8_t *to = codes ? (uint8_t*)workspace + sums : nullptr, *to_scale = codes ? to + T * ld : nullptr;
-  rc = f8_launch_down(d, transposed != 0, given, T, who, u, to, to_scale, st);
+  rc = f8_launch_down(d, transposed != 0, given, T, who, u, to, to_scale, sorts(d, T), st);
   if (rc != BSP_OK) return rc;
-  const F8Low low{who.which, u, transposed ? d.a_t : d.b, (int64_t)d.Rp * (transposed ? d.Ip : d.Op), (int64_t)T * d.Rp, d.Rp, f8_down_slices(T, d.N, K, false)};
-  return multiply(rows, codes ? F8Input{to, to_scale, code, code == BSP_E5M2, ld} : given, T, low, q, y_dtype, workspace, st);
+  F8Low low{who.which, u, transposed ? d.a_t : d.b, (int64_t)d.Rp * (transposed ? d.Ip : d.Op), (int64_t)T * d.Rp, d.Rp, f8_down_slices(T, d.N, K, false)};
+  if (sorts(d, T)) low.mixed = who.tiles + 2, low.order = who.order, low.codes = to, low.scale = to_scale;
+  return multiply(rows, !X && codes ? F8Input{to, to_scale, code, code == BSP_E5M2, ld} : given, T, low, q, y_dtype, workspace, st);
 }
 
 int bsp_f8_adapters_grad_workspace(const bsp_f8_adapters* adapters, int32_t T, int64_t* bytes) {

@@ -44,8 +44,9 @@ __device__ __forceinline__ f32x16_t mfma_bf16_32x32x16(u32x4_t a, u32x4_t b, f32
 template <int MO>
 constexpr int kStoreBytes = 32 * (32 * MO * 4 + 16);
 
-template <int MO, int MT, bool F32>
-__device__ __forceinline__ void store_tile(const F8Epilogue& q, f32x16_t (&acc)[MO][MT], uint8_t* lds, int T, int O, int64_t t0, int o0) {
+// order: where the rows go, or null: they go as they come.
+template <int MO, int MT, bool F32, bool LOW>
+__device__ __forceinline__ void store_tile(const F8Epilogue& q, f32x16_t (&acc)[MO][MT], uint8_t* lds, int T, int O, int64_t t0, int o0, const int32_t* order) {
   const int lane = threadIdx.x & 63;
   constexpr int kLanes = 4 * MO;  // lanes that hold a row's piece, eight channels each
   const int c = o0 + (lane % kLanes) * 8;
@@ -61,10 +62,12 @@ __device__ __forceinline__ void store_tile(const F8Epilogue& q, f32x16_t (&acc)[
               f32x4_t{acc[o][m][4 * k], acc[o][m][4 * k + 1], acc[o][m][4 * k + 2], acc[o][m][4 * k + 3]};
 #pragma unroll 1
       for (int r = lane / (8 * MO); r < 32; r += 8 / MO) {
-        const int64_t t = t0 + m * 32 + r;
+        int64_t t = t0 + m * 32 + r;
         const int ch = o0 + (lane % (8 * MO)) * 4;
         const f32x4_t v = *(const f32x4_t*)(lds + r * kRow + (lane % (8 * MO)) * 16);
-        if (t < T && ch < O) f8_store4<F32>(q, t, ch, O, v[0], v[1], v[2], v[3]);
+        if (t >= T || ch >= O) continue;
+        if (LOW && order) t = order[t];
+        f8_store4<F32>(q, t, ch, O, v[0], v[1], v[2], v[3]);
       }
     }
     return;
@@ -98,9 +101,10 @@ __device__ __forceinline__ void store_tile(const F8Epilogue& q, f32x16_t (&acc)[
     auto rows = [&](auto WHOLE) {  // of whole pieces; or of pieces at any address, which share lines with others
 #pragma unroll 4
       for (int r = lane / kLanes; r < 32; r += 64 / kLanes) {
-        const int64_t t = t0 + m * 32 + r;
+        int64_t t = t0 + m * 32 + r;
         u32x4_t v = *(const u32x4_t*)(lds + r * kRow + (lane % kLanes) * 16);
         if (t >= T || c >= O) continue;
+        if (LOW && order) t = order[t];
         if (q.gate) {
           const u32x2_t g = *(const u32x2_t*)(q.gate + t * (int64_t)f8_blocks(O) * F8_BLOCK + c);
 #pragma unroll
@@ -164,8 +168,8 @@ __device__ __forceinline__ LowParts<PARTS> low_parts(const F8Low& low, const flo
 }
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2_t;
 // A fragment's rows by themselves, where they belong to more than sixteen adapters: a lane multiplies its row's u with its own adapter's weights,
-// sixteen channels of every 32, with ordinary instructions (us, an adapter at a time and so: 64 rows of 16 adapters, 512 -> 16384 20.1 and 20.6, of 32
-// 28.7 and 21.4; 2048 x 4096 -> 4096 66 and 79, 82 and 78).  Not in the widest tiles (16384 x 4096 -> 4096 of 32: 428 and 496).
+// sixteen channels of every 32, with ordinary instructions (us, an adapter at a time and so: 64 x 512 -> 16384 of 64 adapters 18 and 13.6, of rank 64
+// 64 x 4096 -> 4096 41 and 31, 512 of 512 32 and 26).  Not in the widest tiles (16384 x 4096 -> 4096 of 32 mixed as they come: 428 and 496).
 constexpr int kManyAdapters = 16;
 template <int MO, int MT>
 __device__ __forceinline__ void add_low_rows(const F8Low& low, f32x16_t (&acc)[MO][MT], int m, const float* u, int of, int o0) {
@@ -210,10 +214,10 @@ __device__ __forceinline__ void add_low_rows(const F8Low& low, f32x16_t (&acc)[M
 // columns, and the sums go on where they are.  Zero times what is no number is none: an adapter with such weights among its rows'
 // neighbours is multiplied from zero, and a lane, which holds results of one row, takes or leaves what it gives.
 // Bound by the instructions of each adapter among a wave's rows, behind a product that leaves none of their time free (16384 x 4096 -> 4096 of rank
-// 16, us: the product 225 to 250; with twelve adapters in runs of rows 17 more, their rows mixed 70, 85 where all have weights that are no
-// numbers; with 32 mixed 120.  64 x 4096 -> 16384 of 32 mixed: 15, with them 25).
+// 16, us: the product 225 to 250, with adapters 15 to 20 more; 64 x 4096 -> 16384 15, with 32 adapters' rows mixed 25).
+// order: the rows' numbers where they are not multiplied as they come.
 template <int MO, int MT, int PARTS>
-__device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT], int T, int64_t t0, int o0) {
+__device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT], int T, int64_t t0, int o0, const int32_t* order) {
   const int lane = threadIdx.x & 63;
   const uint16_t* up = low.up + (int64_t)o0 * low.rank + lane * 8;  // (as the instruction takes them: 32 channels, sixteen ranks, 64 lanes)
   const float* u[MT];
@@ -222,7 +226,8 @@ __device__ __forceinline__ void add_low(const F8Low& low, f32x16_t (&acc)[MO][MT
   settle();
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    const int64_t t = t0 + m * 32 + (lane & 31) < T ? t0 + m * 32 + (lane & 31) : T - 1;
+    int64_t t = t0 + m * 32 + (lane & 31) < T ? t0 + m * 32 + (lane & 31) : T - 1;
+    if (order) t = order[t];
     u[m] = low.u + t * low.rank + (lane >> 5) * 8;
     of[m] = low.which[t];
   }
@@ -466,8 +471,9 @@ __device__ __forceinline__ void wide(const TileArgs& a, uint8_t* lds) {
 
   K k;
   k.payload = a.w.payload + (int64_t)n0 * F8_BLOCK_BYTES;
-  k.X = a.X + t0 * a.ld;
-  k.S = a.scale + t0;
+  const bool mixed = LOW && a.low.mixed && *(const __attribute__((address_space(4))) int32_t*)a.low.mixed;
+  k.X = (mixed ? a.low.codes : a.X) + t0 * a.ld;
+  k.S = (mixed ? a.low.scale : a.scale) + t0;
   k.srows = a.srows;
   k.cnt = cnt;
   k.wave = wave;
@@ -540,18 +546,19 @@ __device__ __forceinline__ void wide(const TileArgs& a, uint8_t* lds) {
     rest(std::integral_constant<int, 1>{});
     rest(std::integral_constant<int, 0>{});
   }
+  const int32_t* order = mixed ? a.low.order : nullptr;
   if constexpr (LOW)
-    if (share == 0) add_low<MO, MT, F32 ? 3 : 2>(a.low, acc, a.T, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32);
+    if (share == 0) add_low<MO, MT, F32 ? 3 : 2>(a.low, acc, a.T, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32, order);
   __syncthreads();
   if constexpr (kSplits) {
     if (a.split > 1) {
       const int ld = (a.w.out + 3) & ~3;
       const F8Epilogue sums{a.part + (int64_t)share * a.T * ld, nullptr, nullptr, nullptr, 0, 0};
-      store_tile<MO, MT, true>(sums, acc, lds + wave * kStoreBytes<MO>, a.T, ld, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32);
+      store_tile<MO, MT, true, LOW>(sums, acc, lds + wave * kStoreBytes<MO>, a.T, ld, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32, order);
       return;
     }
   }
-  store_tile<MO, MT, F32>(a.q, acc, lds + wave * kStoreBytes<MO>, a.T, a.w.out, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32);
+  store_tile<MO, MT, F32, LOW>(a.q, acc, lds + wave * kStoreBytes<MO>, a.T, a.w.out, t0 + wt * MT * 32, tile_o * K::NO + wo * MO * 32, order);
 }
 
 template <int MO, int MT, int WO, int WT, int BUFS, bool E5, bool F32>

@@ -125,6 +125,11 @@ def test_adapted_product_refusals(want, args):
     n = ctypes.c_int64(-1)
     assert lib.bsp_f8_fc_adapted_workspace(_weights(), 0, 8, 1, _adapters(), n) == OK and n.value == 8 * 16 * 4
     assert lib.bsp_f8_fc_adapted_workspace(_weights(), 0, 17, 0, _adapters(), n) == OK and n.value == (17 * 384 + 32 * 3 + 15) // 16 * 16 + 17 * 16 * 4
+    for T, N, coded, copied in ((32, 4, 1, 0), (33, 4, 1, 1), (33, 1, 1, 0), (33, 1, 0, 1)):  # many rows of several adapters: room for their codes
+        assert lib.bsp_f8_fc_adapted_workspace(_weights(), 0, T, coded, _adapters(N=N), n) == OK
+        plain = ctypes.c_int64(0)
+        assert lib.bsp_f8_fc_workspace(_weights(), 0, T, 1 - copied, plain) == OK
+        assert n.value == (plain.value + 15) // 16 * 16 + T * 16 * 4
     assert lib.bsp_f8_fc_adapted_workspace(_weights(), 0, 8, 1, None, n) == NULL and lib.bsp_f8_fc_adapted_workspace(_weights(), 0, 8, 1, _adapters(), None) == NULL
 
 
