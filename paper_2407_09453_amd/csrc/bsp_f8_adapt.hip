@@ -235,7 +235,15 @@ __device__ __forceinline__ void down(const DownArgs& a, int block, uint8_t* lds)
   // where the codes go, by their row in this part of the tile
   const bool sorted = SAVE && a.sorts && a.q.tiles[2], saves = SAVE && blockIdx.z == 0 && (!kCoded || sorted);
   const int first = SAVE ? __builtin_amdgcn_readfirstlane(record[2]) + part * M * 16 : 0;
-  auto goes = [&](int row) { return (int64_t)(kCoded || sorted ? first + row : rows[row]); };
+  auto goes = [&](int row) { return kCoded || sorted ? first + row : rows[row]; };
+  // (held: asked for again in the loop they take 7 us of 119 at 8192 x 16384 of rank 32)
+  int32_t leaves[SAVE && !kCoded ? 2 * M : 1], scales_of[SAVE && !kCoded ? M : 1];
+  if constexpr (SAVE && !kCoded) {
+#pragma unroll
+    for (int q = 0; q < 2 * M; ++q) leaves[q] = goes(q * 8 + (lane >> 3));
+#pragma unroll
+    for (int m = 0; m < M; ++m) scales_of[m] = goes(m * 16 + r);
+  }
   const int nb = a.Kp >> 7, kb0 = blockIdx.y * a.per, kb1 = kb0 + a.per < nb ? kb0 + a.per : nb;
   if (tile >= a.q.tiles[saves ? 1 : 0] || n <= 0 || kb0 >= nb) return;  // (no slice is empty: f8_down_slices)
   auto key = [](int row) { return kCoded ? (row >> 1) & 7 : row & 15; };
@@ -349,15 +357,19 @@ __device__ __forceinline__ void down(const DownArgs& a, int block, uint8_t* lds)
         most = max(p[0], p[1]);
         const auto o = __builtin_amdgcn_permlane32_swap(most, most, false, false);
         most = max(o[0], o[1]);
-        bytes[m] = a.e5 ? f8_scale_byte<true>(most) : f8_scale_byte<false>(most);
-        const float f = f8_inverse(bytes[m]);
+        auto encode = [&](auto E5) {
+          bytes[m] = f8_scale_byte<decltype(E5)::value>(most);
+          const float f = f8_inverse(bytes[m]);
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
+          for (int q = 0; q < 2; ++q)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float* z = &y[2 * q + (k >> 1)][4 * (k & 1)];
-            codes[m][q][k] = a.e5 ? f8_encode4<true>(z[0] * f, z[1] * f, z[2] * f, z[3] * f) : f8_encode4<false>(z[0] * f, z[1] * f, z[2] * f, z[3] * f);
-          }
+            for (int k = 0; k < 4; ++k) {
+              const float* z = &y[2 * q + (k >> 1)][4 * (k & 1)];
+              codes[m][q][k] = f8_encode4<decltype(E5)::value>(z[0] * f, z[1] * f, z[2] * f, z[3] * f);
+            }
+        };
+        if (a.e5) encode(std::true_type{});
+        else encode(std::false_type{});
       }
     }
     if constexpr (SAVE) {
@@ -369,14 +381,14 @@ __device__ __forceinline__ void down(const DownArgs& a, int block, uint8_t* lds)
           if constexpr (!kCoded)  // (as codes lie there from the start)
 #pragma unroll
             for (int q = 0; q < 2; ++q) *(u32x4_t*)(mine + row * 128 + (((4 * q + g) ^ ((row >> 1) & 7)) << 4)) = codes[m][q];
-          if (g == 0 && row < n) a.to_scale[kb * a.srows + goes(row)] = (uint8_t)(kCoded ? s[kCoded ? m : 0] : bytes[kCoded ? 0 : m]);
+          if (g == 0 && row < n) a.to_scale[kb * a.srows + (kCoded ? goes(row) : scales_of[kCoded ? 0 : m])] = (uint8_t)(kCoded ? s[kCoded ? m : 0] : bytes[kCoded ? 0 : m]);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
         for (int q = 0; q < 2 * M; ++q) {
           const int row = q * 8 + (lane >> 3), p = lane & 7;
           const u32x4_t c = *(const u32x4_t*)(mine + row * 128 + ((p ^ ((row >> 1) & 7)) << 4));
-          if (row < n) *(u32x4_t*)(a.codes + goes(row) * a.Kp + kb * 128 + p * 16) = c;
+          if (row < n) *(u32x4_t*)(a.codes + (int64_t)(kCoded ? goes(row) : leaves[kCoded ? 0 : q]) * a.Kp + kb * 128 + p * 16) = c;
         }
       }
     }
