@@ -11,7 +11,7 @@
 // once: both operands are summed over rows, so they lie in LDS as in memory and the transposing read hands a lane a column's
 // rows.  An adapter with many rows is cut into chunks whose sums a second launch joins, in order: no atomics.
 // Measured: A x of 16384 x 4096 codes, rank 16 18 to 20 us (3.5 TB/s), rank 32 22.6, of 8192 x 16384 bf16, rank 32 52 to 62 (4.3 to 5.1 TB/s), with the rows' codes on
-// the way 111 to 125 (403 MB, 3.4 TB/s), of one row of 4096 4.4; grad of 8192 rows, 4096 codes and 16384 bf16, rank 32 80 to 91 (302 MB, 3.3 to 3.8 TB/s)
+// the way 101 to 118 (403 MB, 3.4 to 4.0 TB/s; of rank 16 87, of rank 64 117: a workgroup's rows read the adapters' columns again), of one row of 4096 4.4; grad of 8192 rows, 4096 codes and 16384 bf16, rank 32 80 to 91 (302 MB, 3.3 to 3.8 TB/s)
 // and 4 to 9 to join; 37 rows of 1000 and 520 columns 5.4 for u and v, 6.4 for the gradients.  The plan of 64 rows 5 to 9 us, of 8192 28, of 16384 50.
 #include "bsp_norm.h"
 
