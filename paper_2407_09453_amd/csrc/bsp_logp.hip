@@ -19,6 +19,8 @@
 // chunks a row are three and a half rounds of what the chip holds); vector instructions take nine tenths of the time, too; 1 x 131072 with 20 5.1 and 7.9 to join; 253 x 1000 fp32 with 5 5.3, gradient 3.3.
 #include "bsp_norm.h"
 
+#include <type_traits>
+
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -363,7 +365,6 @@ __global__ __launch_bounds__(ROWT, (F32 || TOP) && NV == 4 ? 4 : 8) void logp_ro
         for (; w + 1 < WAVES && i >= sh_count[w]; ++w) i -= sh_count[w];
         const uint64_t key = lane < (int)total ? sh_key[w][i] : 0;
         int rank = 0;
-#pragma unroll 4
         for (uint32_t j = 0; j < total; ++j)
           rank += ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)key, j)) > key;
         if (lane < (int)total) put(rank, key);
@@ -404,22 +405,34 @@ __global__ __launch_bounds__(TOP ? 64 : 256) void logp_join(LogpArgs a) {
   if constexpr (TOP) {
     const uint64_t* keys = a.keys + row * a.chunks * a.k;
     const int total = a.chunks * a.k;
+    // 64 keys' turn after turn, four turns' keys asked for together: a loop of ballots is not unrolled, and each would wait for its own
+    auto turns = [&](auto at_once, auto f) {
+      constexpr int kAtOnce = decltype(at_once)::value;
+      for (int i0 = 0; i0 < total; i0 += 64 * kAtOnce) {
+        uint64_t key[kAtOnce];
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) {
+          const int i = i0 + e * 64 + lane;
+          key[e] = keys[i < total ? i : total - 1];
+        }
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) f(i0 + e * 64 + lane < total ? key[e] : 0);
+      }
+    };
+    auto all = [&](auto f) {
+      if (total <= 64) turns(std::integral_constant<int, 1>{}, f);
+      else turns(std::integral_constant<int, 4>{}, f);
+    };
     uint64_t most = 0;
-#pragma unroll 8
-    for (int i = lane; i < total; i += 64) {
-      const uint64_t key = keys[i];
-      most = most > key ? most : key;
-    }
+    all([&](uint64_t key) { most = most > key ? most : key; });
     const uint64_t least = (uint64_t)kth_of_lanes((uint32_t)(most >> 48), a.k) << 48;
     int have = 0;
-#pragma unroll 8
-    for (int i0 = 0; i0 < total; i0 += 64) {
-      const uint64_t key = i0 + lane < total ? keys[i0 + lane] : 0;
+    all([&](uint64_t key) {
       const bool is = key && key >= least;
       const uint64_t those = __ballot(is);
       if (is) sh_key[have + before(those)] = key;
       have += __popcll(those);
-    }
+    });
     __syncthreads();
     for (int i = lane; i < have; i += 64) {
       const uint64_t mine = sh_key[i];
