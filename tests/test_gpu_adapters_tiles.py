@@ -126,6 +126,41 @@ def test_rows_in_another_order(T, I, O, density):
         _near(a[order], b.double(), S[order], [v[order] for v in _low(X.float(), A, B, scale, which)], I, R, False, 2)
 
 
+@pytest.mark.parametrize("T", [40, 700])
+def test_a_captured_call_serves_mixed_rows_and_runs(T):
+    """One graph, replayed on rows in runs, mixed, of no adapter and mixed again: each time the eager call's bits."""
+    import torch
+    import paper_2407_09453_amd as bsp
+    gen = _gen("graph", T)
+    N, R, I, O = 7, 12, 900, 520
+    W, gamma, _ = _weights(gen, O, I, 0.7)
+    layer = bsp.BspLayerF8(W, gamma.cpu().numpy())
+    bank, *_ = _bank(gen, N, R, I, O)
+    X, which = _rows(gen, T, I), torch.zeros(T, dtype=torch.int64, device="cuda")
+    kept, requests = bsp.save8(X), bsp.BspRequests(which, N)
+    dY = _rows(gen, T, O)
+
+    def calls():
+        return (layer.fc(X, adapters=bank, requests=requests), layer.fc(kept, dtype=torch.float32, adapters=bank, requests=requests),
+                layer.grad_input(dY, adapters=bank, requests=requests), *bank.grad(dY, kept, requests))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = calls()
+    mixed = torch.randint(-1, N, (T,), generator=gen, device="cuda")
+    for which in (torch.sort(mixed).values, mixed, torch.full_like(mixed, -1), mixed.flip(0), torch.sort(mixed, descending=True).values):
+        X.copy_(_rows(gen, T, I))
+        bsp.save8(X, out=kept)
+        requests.update(which)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(calls(), out))
+
+
 def test_offsets_past_32_bits():
     """Rows of values and codes, results and an adapter of a set, each past 2^31 elements."""
     import torch
