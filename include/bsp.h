@@ -564,8 +564,8 @@ int bsp_f8_adapters_grad(const bsp_f8_adapters* adapters, const void* dY, int64_
  *   H            device [T][D], rows ldh apart, written where there is a residual (else null); overlaps neither X nor the residual
  *   weight       device float[D], or null (ones)
  *   Y, codes     as for bsp_layer_norm: one of the two;  rstd  device float[T], written for the backward pass
- * Squares are summed in fp32 (of values past 2^63 the sum is infinite and the row becomes zeros).  No other result overlaps an input.
- * Errors: NULL, SHAPE, DTYPE, ALIGN, HIP.  T = 0 does nothing. */
+ * Squares are summed in fp32 by a row's threads, whose sums meet in 64 bits (of values past 2^63 a sum is infinite and the row becomes zeros).
+ * No other result overlaps an input.  Errors: NULL, SHAPE, DTYPE, ALIGN, HIP.  T = 0 does nothing. */
 int bsp_rms_norm(const void* X, int64_t ldx, const void* residual, int64_t ldr, int32_t dtype, int32_t T, int32_t D, const float* weight, float eps,
                  void* H, int64_t ldh, void* Y, int64_t ldy, const bsp_codes* codes, float* rstd, void* stream);
 /* Its gradient: dX [T][D], the gradient of X and of the residual alike, from dY, from dH (what reaches H along the residual stream,

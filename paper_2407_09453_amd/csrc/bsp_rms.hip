@@ -5,10 +5,10 @@
 //
 // The sum is rounded to its type before it is squared: the norm is that of what the residual stream holds, and the backward pass, which
 // reads h, differentiates the very function that ran.  A row is read once and stays in the registers of the 16 to 1024 threads that
-// own it; squares are summed in fp32.  Rows too long for that are read again.  As in the layer norm the gradient's threads own columns and
+// own it; squares are summed in fp32 in a thread, in 64 bits over a row.  Rows too long for that are read again.  As in the layer norm the gradient's threads own columns and
 // add dw over all the rows of their workgroup, and a second launch adds the workgroups' sums in a fixed order.
 // Measured: 16384 x 4096 bf16 with a residual to codes 74 to 83 us (470 MB, 5.7 to 6.3 TB/s), its gradient 100 to 113 (537 MB, 4.8 to 5.4 TB/s) and 5 for
-// the sums; 777 x 2966 fp32 7.8 and 9.6 (18 and 28 MB, from the last-level cache) and 4.2; one row of 4096 3.4.
+// the sums; 777 x 2966 fp32 7.8 and 9.6 (18 and 28 MB, from the last-level cache) and 4.2; one row of 4096 4.2.
 #include "bsp_norm.h"
 
 namespace {
@@ -22,6 +22,7 @@ struct RmsArgs {
   int64_t ldx, ldr, ldh, ldy, ld_dy, ld_dh, ld_dx, srows;
   int32_t T, D, Dp, e5, parts;
   float eps;
+  double inv;  // 1 / D
 };
 
 // eight values of the residual stream: x + residual as its type holds it
@@ -39,17 +40,61 @@ __device__ __forceinline__ void add8(float* v, const float* r) {
   }
 }
 
+// The inverse root of a row's mean square, from its threads' sums (fp32, some sixteen terms each), and what 32 bits leave of it.  The threads' sums
+// meet in 64 bits and h q w is rounded once, for the sake of codes: where a block's largest value lies at the border between two scales the
+// wrong side costs 128 codes a step (16384 x 4096 drawn 150 times, 79 million scales: 2 differ from the exact values', with a sum and three roundings in 32 bits
+// 6; q is 4.7e-8 of it off at most, with these 1.5e-7).  The time is the same, one row takes 4.2 us instead of 3.7.
+struct Root {
+  float r, rest;
+};
+__device__ __forceinline__ double lane_double(double v, uint32_t lo, uint32_t hi) { return v + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo); }
+template <int CTRL>
+__device__ __forceinline__ double add_from_lane(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return lane_double(v, f8_from_lane<CTRL>((uint32_t)u), f8_from_lane<CTRL>((uint32_t)(u >> 32)));
+}
+template <int ROWT>
+__device__ __forceinline__ double row_sum_double(double v, double* sh) {
+  v = add_from_lane<kMirror16>(add_from_lane<kMirror8>(add_from_lane<kXor2>(add_from_lane<kXor1>(v))));
+  if constexpr (ROWT > 16) {
+    const int lane = threadIdx.x & 63;
+    uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const auto l16 = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false), h16 = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+    v = lane_double(__builtin_bit_cast(double, (uint64_t)h16[0] << 32 | l16[0]), l16[1], h16[1]);
+    u = __builtin_bit_cast(uint64_t, v);
+    const auto l32 = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false), h32 = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+    v = lane_double(__builtin_bit_cast(double, (uint64_t)h32[0] << 32 | l32[0]), l32[1], h32[1]);
+    if constexpr (ROWT >= 256) {
+      if (lane == 0) sh[threadIdx.x >> 6] = v;
+      __syncthreads();
+      v = 0.;
+#pragma unroll
+      for (int w = 0; w < ROWT / 64; ++w) v += sh[w];
+    }
+  }
+  return v;
+}
+template <int ROWT>
+__device__ __forceinline__ Root inverse_root(const RmsArgs& a, float s, double* sh) {
+  const double x = fma(row_sum_double<ROWT>(s, sh), a.inv, (double)a.eps);
+  const float r = 1.f / sqrtf((float)x), more = (float)(0.5 * r * fma(-x * r, (double)r, 1.)), better = r + more;
+  return fabsf(more) < 1e-6f * r ? Root{better, more - (better - r)} : Root{r, 0.f};  // (infinities, zeros, NaN)
+}
+__device__ __forceinline__ float scaled(float h, const Root& q, float w) {
+  const float p = h * q.r, y = p * w, rest = fmaf(fmaf(h, q.rest, fmaf(h, q.r, -p)), w, fmaf(p, w, -y));
+  return fabsf(y) < INFINITY ? y + rest : y;
+}
+
 // NV: groups of eight columns a thread holds; 0: rows of any length, read twice (three times with a residual's sum)
 template <bool F32, bool CODES, int ROWT, int NV>
 __global__ __launch_bounds__(ROWT > 256 ? ROWT : 256) void rms_forward(RmsArgs a) {
-  __shared__ float sh[ROWT > 256 ? ROWT / 64 : 4][1];
+  __shared__ double sh[ROWT > 256 ? ROWT / 64 : 4];
   const int tid = threadIdx.x % ROWT;
   const int64_t group = (int64_t)blockIdx.y * kGridX + blockIdx.x, row = ROWT >= 256 ? group : group * (256 / ROWT) + threadIdx.x / ROWT;
   if (row >= a.T) return;  // (whole groups of ROWT)
   const void *x = row_of<F32>(a.X, row, a.ldx), *r = row_of<F32>(a.residual, row, a.ldr);
   void* h = (void*)row_of<F32>(a.H, row, a.ldh);
-  const float inv = 1.f / (float)a.D;
-  float s[1] = {0.f};
+  float s = 0.f;
   if constexpr (NV > 0) {  // (D >= 8)
     const bool ragged = a.D & 7;
     float v[NV][8];
@@ -70,11 +115,10 @@ __global__ __launch_bounds__(ROWT > 256 ? ROWT : 256) void rms_forward(RmsArgs a
         if (c < a.D) f8_store8<F32>(h, c, a.D - c, v[j]);
       }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s[0] += v[j][k] * v[j][k];  // (zeros past the row)
+      for (int k = 0; k < 8; ++k) s += v[j][k] * v[j][k];  // (zeros past the row)
     }
-    row_sum<ROWT, 1>(s, sh);
-    const float rstd = 1.f / sqrtf(s[0] * inv + a.eps);
-    if (tid == 0) a.rstd[row] = rstd;
+    const Root root = inverse_root<ROWT>(a, s, sh);
+    if (tid == 0) a.rstd[row] = root.r;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int c = (tid + j * ROWT) * 8;
@@ -83,7 +127,7 @@ __global__ __launch_bounds__(ROWT > 256 ? ROWT : 256) void rms_forward(RmsArgs a
       for (int k = 0; k < 8; ++k) w[k] = 1.f;
       if (a.weight) load8<true>(a.weight, c, a.D, w);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[j][k] = c + k < a.D ? v[j][k] * rstd * w[k] : 0.f;
+      for (int k = 0; k < 8; ++k) v[j][k] = c + k < a.D ? scaled(v[j][k], root, w[k]) : 0.f;
       put8<F32, CODES>(a, row, c, v[j]);
     }
   } else {
@@ -99,17 +143,16 @@ __global__ __launch_bounds__(ROWT > 256 ? ROWT : 256) void rms_forward(RmsArgs a
     for (int c = tid * 8; c < a.D; c += ROWT * 8) {
       stream(c);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s[0] += v[k] * v[k];
+      for (int k = 0; k < 8; ++k) s += v[k] * v[k];
     }
-    row_sum<ROWT, 1>(s, sh);
-    const float rstd = 1.f / sqrtf(s[0] * inv + a.eps);
-    if (tid == 0) a.rstd[row] = rstd;
+    const Root root = inverse_root<ROWT>(a, s, sh);
+    if (tid == 0) a.rstd[row] = root.r;
     for (int c = tid * 8; c < a.Dp; c += ROWT * 8) {
       const int left = a.D - c;
       stream(c);
       if (a.residual && left > 0) f8_store8<F32>(h, c, left, v);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = k < left ? v[k] * rstd * (a.weight ? a.weight[c + k] : 1.f) : 0.f;
+      for (int k = 0; k < 8; ++k) v[k] = k < left ? scaled(v[k], root, a.weight ? a.weight[c + k] : 1.f) : 0.f;
       put8<F32, CODES>(a, row, c, v);
     }
   }
@@ -307,7 +350,7 @@ int rms_launch_forward(const void* X, int64_t ldx, const void* residual, int64_t
                        int64_t ldh, void* Y, int64_t ldy, int code, uint8_t* codes, uint8_t* scale, float* rstd, hipStream_t st) {
   RmsArgs a{};
   a.X = X, a.residual = residual, a.weight = weight, a.H = H, a.Y = Y, a.codes = codes, a.scale = scale, a.rstd = rstd;
-  a.ldx = ldx, a.ldr = ldr, a.ldh = ldh, a.ldy = ldy, a.srows = f8_scale_rows(T), a.T = T, a.D = D, a.Dp = f8_blocks(D) * F8_BLOCK, a.e5 = code == BSP_E5M2, a.eps = eps;
+  a.ldx = ldx, a.ldr = ldr, a.ldh = ldh, a.ldy = ldy, a.srows = f8_scale_rows(T), a.T = T, a.D = D, a.Dp = f8_blocks(D) * F8_BLOCK, a.e5 = code == BSP_E5M2, a.eps = eps, a.inv = 1. / D;
   if (codes) return f32 ? forward<true, true>(a, st) : forward<false, true>(a, st);
   return f32 ? forward<true, false>(a, st) : forward<false, false>(a, st);
 }
