@@ -591,8 +591,11 @@ int bsp_log_probs(const void* X, int64_t ldx, int32_t dtype, int32_t T, int32_t 
                   float* logp, float* lse, float* entropy, float* top_logp, int32_t* top_tokens, void* workspace, int64_t workspace_bytes, void* stream);
 /* The logits' gradient from those of logp and of the entropy (float[T], either may be null: zeros):
  *   dX = scale (dlogp ([token] - p) - dentropy p (log p + entropy))
- * in X's type, rows ld_dx apart; dX may be X itself.  Rows without a token take nothing from dlogp, rows of minus infinities alone get
- * zeros, rows with a token of V and above NaN.  lse and entropy: what bsp_log_probs wrote.  Errors: NULL, SHAPE, DTYPE, ALIGN, HIP. */
+ * in X's type, rows ld_dx apart; dX may be X itself, and shares no element with it otherwise.  Rows without a token take nothing from
+ * dlogp, rows of minus infinities alone get zeros, rows with a token of V and above NaN.  lse and entropy: what bsp_log_probs wrote for these
+ * logits.  Where 32 bits of lse no longer hold the log of the sum, and for fp32 logits always, the row is added up anew, so that p and 1 - p
+ * are off by less than the results' rounding at any scale and size of logits.  A row's result does not depend on the other rows.
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, HIP. */
 int bsp_log_probs_grad(const void* X, int64_t ldx, int32_t dtype, int32_t T, int32_t V, const void* tokens, int32_t token_bytes, float scale,
                        const float* lse, const float* entropy, const float* dlogp, const float* dentropy, void* dX, int64_t ld_dx, void* stream);
 

@@ -15,8 +15,9 @@
 // index: all differ, and the lowest index wins a tie.  Where more is left than a list holds (a row of equal values) the k-th key is
 // found bit by bit.
 // Measured: 8192 x 32768 bf16 90 to 140 us after kernels that left 500 MB to be written back, 102 by itself (537 MB, 5.3 TB/s), 7 to join, the gradient
-// 190 to 210 (1.07 GB, 5.1 to 5.6 TB/s); with the 1, 8, 20 and 50 likeliest 117, 127, 136, 190; 1021 x 50001 with none 28, with 8 33.5 (102 MB, 3 TB/s: seven
-// chunks a row are three and a half rounds of what the chip holds); vector instructions take nine tenths of the time, too; 1 x 131072 with 20 5.1 and 7.9 to join; 253 x 1000 fp32 with 5 5.3, gradient 3.3.
+// 192, in the logits' place 186 (1.07 GB, 5.6 to 5.8 TB/s), of rows that it adds up anew 223 and 244; with the 1, 8, 20 and 50 likeliest 117, 127, 136, 190; 1021 x 50001
+// with none 28, with 8 33.5 (102 MB, 3 TB/s: seven chunks a row are three and a half rounds of what the chip holds); vector instructions take nine tenths of
+// the time, too; 1 x 131072 with 20 5.1 and 7.9 to join; 253 x 1000 fp32 with 5 5.3, gradient 3.7.
 #include "bsp_norm.h"
 
 #include <type_traits>
@@ -450,45 +451,139 @@ struct LogpGradArgs {
   const float *lse, *entropy, *dlogp, *dentropy;
   void* dX;
   int64_t ld, ld_dx;
-  int32_t T, V, chunks, wide_tokens;
+  int32_t T, V, shares, alone, wide_tokens;  // workgroups of a long row; whether one of them does all of a row that is added up anew
   float scale;
 };
 
-// A thread takes NV groups of eight columns, and reads them before it writes any: the gradient may replace the logits.
-template <bool F32, int NV>
-__global__ __launch_bounds__(256) void logp_grad(LogpGradArgs a) {
-  const int64_t group = (int64_t)blockIdx.y * kGridX + blockIdx.x, row = group / a.chunks;
+// Whether lse, in its 32 bits, still holds the log of the sum for a gradient in bf16: a probability from it is up to U |lse| of itself off (U = 2^-24),
+// at most 2^-18, and what the likeliest leaves, 1 - p >= entropy / 25, up to 25 U |lse| / entropy, at most 2^-11: a quarter of what the result's
+// rounding takes.  (At a scale of 10^4 a probability would be 10^-2 of itself off, at 10^6 anything.)
+__device__ __forceinline__ bool lse_holds(float lse, float entropy) { return fabsf(lse) <= fminf(64.f, 256.f * entropy); }
+
+// p = e^(z-m) / S.  A row's workgroup forms m, n and s anew, as above but with a running maximum for each wave, and takes 1 - p of the likeliest from what does not
+// reach the maximum; only where lse holds enough for results in bf16 it is e^(z-lse).  A row of up to ROWT NV 8 logits stays in registers; a longer one
+// is shared out among workgroups, each of which adds up all of it where it has to be, or the first does all (many rows, or the gradient takes
+// the logits' place), reading the row twice, the second time from the last-level cache.  What is added up is read before any gradient is written,
+// and a thread that writes has itself read what stood there.
+template <bool F32, int ROWT, int NV, bool LONG>
+__global__ __launch_bounds__(ROWT, F32 && NV >= 4 ? 4 : LONG ? 6 : 8) void logp_grad(LogpGradArgs a) {
+  constexpr int WAVES = ROWT / 64, kTurn = ROWT * NV * 8;
+  __shared__ float sh[WAVES][3];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t group = (int64_t)blockIdx.y * kGridX + blockIdx.x, row = LONG ? group / a.shares : group;
   if (row >= a.T) return;
-  const int begin = (int)(group - row * a.chunks) * (256 * 8 * NV);
-  const int64_t token = a.wide_tokens ? ((const int64_t*)a.tokens)[row] : (int64_t)((const int32_t*)a.tokens)[row];
-  const float lse = a.lse[row], h = a.entropy[row];
-  const float dl = token >= 0 && a.dlogp ? a.dlogp[row] * a.scale : 0.f, dh = a.dentropy ? a.dentropy[row] * a.scale : 0.f;
-  const float bad = token >= a.V ? __builtin_nanf("") : 0.f;  // (as the log probability)
+  const int share = LONG ? (int)(group - row * a.shares) : 0;
   const void* x = row_of<F32>(a.X, row, a.ld);
-  void* y = (void*)row_of<F32>(a.dX, row, a.ld_dx);
-  F8Raw8<F32> raw[NV];
+  const int64_t token = a.wide_tokens ? ((const int64_t*)a.tokens)[row] : (int64_t)((const int32_t*)a.tokens)[row];
+  const float lse = a.lse[row], entropy = a.entropy[row], dh = a.dentropy ? a.dentropy[row] * a.scale : 0.f;
+  const float dl = a.dlogp && token >= 0 ? a.dlogp[row] * a.scale : 0.f;
+  const bool anew = F32 || !lse_holds(lse, entropy);
+  if (LONG && anew && a.alone && share != (int)((row + row / 8) % a.shares)) return;  // (which goes by the row, for the XCDs' sake)
+  Eight<F32, ROWT == 64 && NV == 1> in[NV];
+  auto ask = [&](int begin) {
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int c = begin + (threadIdx.x + j * 256) * 8;
-    if (c + 8 <= a.V) raw[j] = f8_raw8<F32>(x, c, a.V);
-  }
+    for (int j = 0; j < NV; ++j) in[j].ask(x, begin + (tid + j * ROWT) * 8, a.V);
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int c = begin + (threadIdx.x + j * 256) * 8;
-    if (c >= a.V) continue;
-    float v[8];
-    if (c + 8 <= a.V) f8_unpack8<F32>(raw[j], 0, false, v);
-    else each8<F32>(x, c, a.V, v);  // a row's end by itself: its last eight would be another thread's too
+    for (int j = 0; j < NV; ++j)
+      if (begin + (wave * 64 + 63 + j * ROWT) * 8 + 8 > a.V) in[j].place(begin + (tid + j * ROWT) * 8, a.V, a.V);
+  };
+  if (!LONG) ask(0);
+  // log2 of p S: (factor z - minus) by_log2
+  float factor = a.scale, minus = lse, by_log2 = kLog2e, top = __builtin_nanf(""), inv = 1.f, log = 0.f, rest = 0.f;
+  bool none = false;
+  if (anew) {
+    const float c2 = a.scale * kLog2e;
+    float m = -INFINITY, n = 0.f, s = 0.f;  // the wave's maximum, a lane's sums
+    for (int begin = 0; begin < (LONG ? a.V : 1); begin += kTurn) {
+      if (LONG) ask(begin);
+      float most[NV], now = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      float lp = v[k] * a.scale - lse;
-      lp = lp < -200.f ? -200.f : lp;  // no probability, and nothing times minus infinity
-      const float p = __builtin_amdgcn_exp2f(lp * kLog2e);
-      float g = -p * (dl + dh * (lp + h)) + bad;
-      if (c + k == token) g += dl;
-      v[k] = lse == -INFINITY ? 0.f : g;
+      for (int j = 0; j < NV; ++j) {
+        float v[8];
+        in[j].get(v);
+        most[j] = most8(v);
+        now = fmaxf(now, most[j]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      now = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(lanes_max<64>(now))));
+      if (now > m) {
+        if (LONG) s = (s + n) * __builtin_amdgcn_exp2f((m - now) * c2), n = 0.f;
+        m = now;
+      }
+      const float from = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        float v[8];
+        in[j].get(v);
+        if (__any(most[j] == from)) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float e = __builtin_amdgcn_exp2f((v[k] - from) * c2);
+            n += v[k] == from ? 1.f : 0.f;
+            s += v[k] == from ? 0.f : e;
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s += __builtin_amdgcn_exp2f((v[k] - from) * c2);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
-    f8_store8<F32>(y, c, a.V - c, v);
+    n = f8_wave_sum(n);
+    s = f8_wave_sum(s);
+    if constexpr (WAVES > 1) {
+      if (lane == 0) sh[wave][0] = m, sh[wave][1] = n, sh[wave][2] = s;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) m = fmaxf(m, sh[w][0]);
+      n = s = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {  // (what reached a lower maximum is one of the others)
+        const bool same = sh[w][0] == m;
+        n += same ? sh[w][1] : 0.f;
+        s += same ? sh[w][2] : __builtin_amdgcn_exp2f((sh[w][0] - m) * c2) * (sh[w][1] + sh[w][2]);
+      }
+    }
+    none = n == 0.f && s == 0.f;
+    factor = 1.f, minus = top = m == -INFINITY ? 0.f : m, by_log2 = c2, inv = 1.f / (n + s), rest = n - 1.f + s, log = log_of(Sums{m, n, s, 0.f});
+  }
+  // -(log p + entropy) dentropy / S = t h1 + h0
+  float h1 = 0.f - dh * kLn2 * inv, h0 = 0.f - dh * (entropy - log) * inv, l0 = h0 - dl * inv;
+  if (token >= a.V) l0 = __builtin_nanf("");  // (as the log probability)
+  if (none) h0 = h1 = l0 = 0.f;
+  const int at = token >= 0 && token < a.V && !none ? (int)token : -8;
+  void* y = (void*)row_of<F32>(a.dX, row, a.ld_dx);
+  const bool all = LONG && anew && a.alone;
+  for (int begin = all ? 0 : share * kTurn; begin < a.V; begin += kTurn) {
+    if constexpr (LONG) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int c = begin + (tid + j * ROWT) * 8;
+        if (c + 8 <= a.V) in[j].raw = f8_raw8<F32>(x, c, a.V);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = begin + (tid + j * ROWT) * 8;
+      if (c >= a.V) continue;
+      float v[8], g[8];
+      if (!LONG || c + 8 <= a.V) in[j].get(v);
+      else each8<F32>(x, c, a.V, v);  // a row's end by itself: its last eight would be another thread's too
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float t = fmaxf(fmaf(v[k], factor, -minus) * by_log2, -200.f);  // (of -200 and less e is 0; 0 times minus infinity would be no number)
+        g[k] = __builtin_amdgcn_exp2f(t) * fmaf(t, h1, l0);
+      }
+      if (at >= c && at < c + 8) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float t = fmaxf(fmaf(v[k], factor, -minus) * by_log2, -200.f), e = __builtin_amdgcn_exp2f(t);
+          if (c + k == at) g[k] = fmaf(dl, v[k] == top ? rest * inv : 1.f - e * inv, e * fmaf(t, h1, h0));
+        }
+      }
+      f8_store8<F32>(y, c, a.V - c, g);
+    }
+    if (!all) break;
   }
 }
 
@@ -526,6 +621,29 @@ int rows(const LogpArgs& a, hipStream_t st) {
   return launched();
 }
 
+template <bool F32>
+int grad(LogpGradArgs& a, hipStream_t st) {
+  // Long rows of bf16 come in shares of 256 threads, which is what those want that lse holds: 2048 x 131072 190, in shares of 1024
+  // threads 306, 8192 x 32768 192 and 186 in the logits' place, held in 1024 threads' registers 213 and 202 (added up 223 and 244, held 210 and 200).  fp32,
+  // always added up, is held longer and comes in shares of 1024: 2048 x 32768 108, 1024 x 131072 283, in shares of 256 364.  One workgroup does all
+  // of a row as soon as there are about 1024 (us): 16 x 131072 bf16 43, shared out 20, 64 x 131072 45 and 45.
+  constexpr int kHeld = F32 ? 32768 : 16384, kThreads = F32 ? 1024 : 256, kShare = kThreads * 8 * 4;
+  if (a.V > kHeld) {
+    a.shares = (a.V + kShare - 1) / kShare;
+    a.alone = a.X == a.dX || (int64_t)a.T * a.shares >= 1024;
+  }
+  const dim3 grid = f8_grid((int64_t)a.T * a.shares);
+  if (a.V <= 512) hipLaunchKernelGGL((logp_grad<F32, 64, 1, false>), grid, dim3(64), 0, st, a);
+  else if (a.V <= 1024) hipLaunchKernelGGL((logp_grad<F32, 64, 2, false>), grid, dim3(64), 0, st, a);
+  else if (a.V <= 2048) hipLaunchKernelGGL((logp_grad<F32, 256, 1, false>), grid, dim3(256), 0, st, a);
+  else if (a.V <= 4096) hipLaunchKernelGGL((logp_grad<F32, 256, 2, false>), grid, dim3(256), 0, st, a);
+  else if (a.V <= 8192) hipLaunchKernelGGL((logp_grad<F32, 256, 4, false>), grid, dim3(256), 0, st, a);
+  else if (a.V <= 16384) hipLaunchKernelGGL((logp_grad<F32, 512, 4, false>), grid, dim3(512), 0, st, a);
+  else if (F32 && a.V <= kHeld) hipLaunchKernelGGL((logp_grad<true, 512, 8, false>), grid, dim3(512), 0, st, a);
+  else hipLaunchKernelGGL((logp_grad<F32, kThreads, 4, true>), grid, dim3(kThreads), 0, st, a);
+  return launched();
+}
+
 }  // namespace
 
 int64_t logp_workspace(int T, int V, int k) {
@@ -546,12 +664,6 @@ int logp_launch(const void* X, bool f32, int64_t ld, int T, int V, const void* t
 
 int logp_launch_grad(const void* X, bool f32, int64_t ld, int T, int V, const void* tokens, bool wide_tokens, float scale, const float* lse, const float* entropy,
                      const float* dlogp, const float* dentropy, void* dX, int64_t ld_dx, hipStream_t st) {
-  LogpGradArgs a{X, tokens, lse, entropy, dlogp, dentropy, dX, ld, ld_dx, T, V, 0, wide_tokens, scale};
-  auto run = [&](auto kernel, int nv) {
-    a.chunks = (V + 256 * 8 * nv - 1) / (256 * 8 * nv);
-    hipLaunchKernelGGL(kernel, f8_grid((int64_t)T * a.chunks), dim3(256), 0, st, a);
-    return launched();
-  };
-  if (V <= 2048) return f32 ? run(logp_grad<true, 1>, 1) : run(logp_grad<false, 1>, 1);
-  return f32 ? run(logp_grad<true, 2>, 2) : run(logp_grad<false, 4>, 4);
+  LogpGradArgs a{X, tokens, lse, entropy, dlogp, dentropy, dX, ld, ld_dx, T, V, 1, 0, wide_tokens, scale};
+  return f32 ? grad<true>(a, st) : grad<false>(a, st);
 }

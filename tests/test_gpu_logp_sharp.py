@@ -4,6 +4,9 @@ Bounds.  U = 2^-24; d = (max - x) scale.  An exponent carries the rounding of a 
 the constant's own rounding adds.  A sum's term, e^-d, carries that and 160 U for the exponential and the additions (up to 32 in a thread, then in
 pairs, then up to 64 chunks).  Where the sum is near 1 the terms that reach the maximum are counted, not added, and carry nothing.  Nothing
 here grows with the logits themselves but lse, which is rounded once at its own size, from m scale, rounded at that.
+
+The gradient's probabilities carry their exponent's rounding and the sum's; for results in bf16 those of ordinary rows come from lse, at most 64 U off, and
+what the likeliest token leaves, 1 - p, at most 2^-11 of itself.  In fp32, and in every other row, that is the sum of the others, over S.
 """
 import numpy as np
 import pytest
@@ -115,3 +118,87 @@ def test_forward_where_no_float_holds_the_sum():
     tokens = np.array([5, 0, 9, 2])
     x = _host(X)
     _check(x, tokens, 3, 2.0 ** 100, bsp.log_probs(X, torch.from_numpy(tokens).cuda(), 3, 2.0 ** 100))
+
+
+def _check_grad(x, tokens, dl, dh, scale, got, bf16):
+    r = _Row(x, scale)
+    rows = np.arange(len(x))
+    held = 64 * U if bf16 else 0.0
+    al, ah, S, h, log = (v[:, None] for v in (np.abs(dl), np.abs(dh), r.S, r.h, np.abs(r.log)))
+    p = r.e / S
+    with np.errstate(invalid="ignore"):
+        lph = np.where(p == 0, 0.0, r.lp + h)
+        d = np.where(p == 0, 0.0, r.d)
+    one = np.zeros(x.shape, bool)
+    one[rows, tokens] = True
+    # 1 - p of each value: what does not reach the maximum, where it is the only one that does
+    rest = np.where(r.at, (r.n - 1 + np.where(r.at, 0.0, r.e).sum(1))[:, None] / S, 1 - p)
+    p_tol = p * ((6 * d + 16) * U + (r.sum / r.S)[:, None] + held)
+    rest_tol = np.where(r.at, r.others[:, None] / S + rest * ((r.sum / r.S)[:, None] + 16 * U), p_tol + 4 * U) + (2.0 ** -11 * rest if bf16 else 0.0)
+    want = scale * (dl[:, None] * np.where(one, rest, -p) - dh[:, None] * p * lph)
+    lph_tol = r.h_tol[:, None] + r.log_tol[:, None] + 6 * U * d + 8 * U * (h + log + d) + held
+    tol = p_tol * (np.where(one, 0.0, al) + ah * np.abs(lph)) + p * (ah * lph_tol + 8 * U * (al + ah * (h + log + d))) + np.where(one, al * (rest_tol + 4 * U * rest), 0.0)
+    # (a probability below 2^-125 may be 0)
+    tol = scale * (tol + 2.0 ** -125 * (al + ah * 200)) + (2.0 ** -8 if bf16 else 4 * U) * np.abs(want) + 2.0 ** -120
+    _same(_host(got), want, tol)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [70, 1000, 3000, 5000, 12000, 30000, 33000, 70001])
+@pytest.mark.parametrize("scale,most", [(1.0, 20.0)] + SCALES + SIZES)
+def test_gradient_at_any_temperature(scale, most, V, dtype):
+    import torch
+    import paper_2407_09453_amd as bsp
+    X = _logits(V, scale, most, dtype)
+    x, scale = _host(X), float(np.float32(scale))
+    tokens = _tokens(x, V)
+    rng = np.random.default_rng(V + 1)
+    dl, dh = (rng.standard_normal(len(x)).astype(np.float32) for _ in range(2))
+    tok, dlt, dht = (torch.from_numpy(t).cuda() for t in (tokens, dl, dh))
+    _, lse, entropy, _, _ = bsp.log_probs(X, tok, 0, scale)
+    g = bsp.log_probs_grad(X, tok, lse, entropy, dlt, dht, scale)
+    _check_grad(x, tokens, dl.astype(np.float64), dh.astype(np.float64), scale, g, dtype == "bf16")
+    _check_grad(x, tokens, dl.astype(np.float64), 0 * dh.astype(np.float64), scale, bsp.log_probs_grad(X, tok, lse, entropy, dlt, None, scale), dtype == "bf16")
+    again = bsp.log_probs_grad(X, tok, lse, entropy, dlt, dht, scale, out=X)
+    assert again is X and torch.equal(g, X)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_sure_token_keeps_its_gradient(dtype):
+    """A token that leaves a 2^-21st to the others: its gradient is minus the sum of theirs, to what the results' own rounding leaves."""
+    import torch
+    import paper_2407_09453_amd as bsp
+    X = torch.zeros(2, 1000, device="cuda", dtype=torch.bfloat16 if dtype == "bf16" else torch.float32)
+    X[:, 7] = 25.0
+    X[1] += 1000.0 if dtype == "f32" else 0.0
+    x, tokens = _host(X), np.array([7, 7])
+    tok, one = torch.tensor(tokens, device="cuda"), torch.ones(2, device="cuda")
+    _, lse, entropy, _, _ = bsp.log_probs(X, tok)
+    g = bsp.log_probs_grad(X, tok, lse, entropy, one)
+    _check_grad(x, tokens, np.ones(2), np.zeros(2), 1.0, g, dtype == "bf16")
+    g = _host(g)
+    assert (g[:, 7] > 0).all() and (np.abs(g.sum(1)) <= (2.0 ** -7 if dtype == "bf16" else 400 * U) * g[:, 7]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [1000, 33000, 140000])
+def test_a_row_has_the_same_gradient_in_any_batch(V, dtype):
+    """Ordinary and sharp rows in turn, by themselves, among a few and among many (whose workgroups share them out otherwise)."""
+    import torch
+    import paper_2407_09453_amd as bsp
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(V)
+    X = torch.randn(260, V, generator=gen, device="cuda")
+    X[::2] *= 300
+    X = X.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    tok = torch.randint(0, V, (260,), generator=gen, device="cuda")
+    dl, dh = (torch.randn(260, generator=gen, device="cuda") for _ in range(2))
+    _, lse, entropy, _, _ = bsp.log_probs(X, tok)
+    assert (lse.abs()[::2] > 64).all() and (lse.abs()[1::2] < 64).all()
+    g = bsp.log_probs_grad(X, tok, lse, entropy, dl, dh)
+    for n in (1, 5, 40):
+        for at in (0, 1, 219):
+            r = slice(at, at + n)
+            assert torch.equal(g[r], bsp.log_probs_grad(X[r].clone(), tok[r], lse[r], entropy[r], dl[r], dh[r]))
+    bsp.log_probs_grad(X, tok, lse, entropy, dl, dh, out=X)
+    assert torch.equal(g, X)
