@@ -400,12 +400,12 @@ def rms_norm(X, weight=None, residual=None, eps: float = 1e-6, code: Optional[st
     """(Y, H, rstd) of X [T][D] (fp32 or bf16): H = X + residual rounded to their type (X itself where there is none), the residual
     stream as it goes on; Y = H rstd weight, rstd the inverse of H's root mean square over its last axis; ``weight`` is float [D]
     or None.  With ``code`` ("e4m3", "e5m2") Y is a BspCodes, the form in which a BspLayerF8 reads it."""
-    if stream is not None:
-        Y, H, rstd = _on_stream(stream, X, _rms_norm, X, weight, residual, eps, code)
-        return Y, X if H is None else H, rstd
     if X.requires_grad or (weight is not None and weight.requires_grad) or (residual is not None and residual.requires_grad):
         _unrecorded(3)
-    Y, H, rstd = _rms_norm(X, weight, residual, eps, code)
+    if stream is not None:
+        Y, H, rstd = _on_stream(stream, X, _rms_norm, X, weight, residual, eps, code)
+    else:
+        Y, H, rstd = _rms_norm(X, weight, residual, eps, code)
     return Y, X if H is None else H, rstd
 
 

@@ -57,7 +57,7 @@ def log_probs_grad(logits, tokens, lse, entropy, dlogp=None, dentropy=None, scal
     ``log_probs`` returned.  ``out`` may be the logits themselves, which it then replaces."""
     if stream is not None:
         return _on_stream(stream, logits, log_probs_grad, logits, tokens, lse, entropy, dlogp, dentropy, scale, out)
-    if logits.requires_grad:
+    if logits.requires_grad or (dlogp is not None and dlogp.requires_grad) or (dentropy is not None and dentropy.requires_grad):
         _unrecorded(3)
     T, V, ld = _rows(logits)
     token, size = _tokens(tokens, logits)
