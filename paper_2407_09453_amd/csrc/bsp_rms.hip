@@ -5,7 +5,7 @@
 //
 // The sum is rounded to its type before it is squared: the norm is that of what the residual stream holds, and the backward pass, which
 // reads h, differentiates the very function that ran.  A row is read once and stays in the registers of the 16 to 1024 threads that
-// own it; squares are summed in fp32 in a thread, in 64 bits over a row.  Rows too long for that are read again.  As in the layer norm the gradient's threads own columns and
+// own it; squares are summed in fp32 in a thread, in 64 bits over a row.  Rows too long for that are read again, and their sums are in 64 bits in a thread, too.  As in the layer norm the gradient's threads own columns and
 // add dw over all the rows of their workgroup, and a second launch adds the workgroups' sums in a fixed order.
 // Measured: 16384 x 4096 bf16 with a residual to codes 74 to 83 us (470 MB, 5.7 to 6.3 TB/s), its gradient 100 to 113 (537 MB, 4.8 to 5.4 TB/s) and 5 for
 // the sums; 777 x 2966 fp32 7.8 and 9.6 (18 and 28 MB, from the last-level cache) and 4.2; one row of 4096 4.2.
@@ -40,7 +40,8 @@ __device__ __forceinline__ void add8(float* v, const float* r) {
   }
 }
 
-// The inverse root of a row's mean square, from its threads' sums (fp32, some sixteen terms each), and what 32 bits leave of it.  The threads' sums
+// The inverse root of a row's mean square, from its threads' sums (fp32, some sixteen terms each, or in 64 bits where a thread has any number of terms: 4096 equal
+// ones in fp32, as in a row of 2^20, drift by 500 2^-24 of their sum), and what 32 bits leave of it.  The threads' sums
 // meet in 64 bits and h q w is rounded once, for the sake of codes: where a block's largest value lies at the border between two scales the
 // wrong side costs 128 codes a step (16384 x 4096 drawn 150 times, 79 million scales: 2 differ from the exact values', with a sum and three roundings in 32 bits
 // 6; q is 4.7e-8 of it off at most, with these 1.5e-7).  The time is the same, one row takes 4.2 us instead of 3.7.
@@ -75,7 +76,7 @@ __device__ __forceinline__ double row_sum_double(double v, double* sh) {
   return v;
 }
 template <int ROWT>
-__device__ __forceinline__ Root inverse_root(const RmsArgs& a, float s, double* sh) {
+__device__ __forceinline__ Root inverse_root(const RmsArgs& a, double s, double* sh) {
   const double x = fma(row_sum_double<ROWT>(s, sh), a.inv, (double)a.eps);
   const float r = 1.f / sqrtf((float)x), more = (float)(0.5 * r * fma(-x * r, (double)r, 1.)), better = r + more;
   return fabsf(more) < 1e-6f * r ? Root{better, more - (better - r)} : Root{r, 0.f};  // (infinities, zeros, NaN)
@@ -94,8 +95,8 @@ __global__ __launch_bounds__(ROWT > 256 ? ROWT : 256) void rms_forward(RmsArgs a
   if (row >= a.T) return;  // (whole groups of ROWT)
   const void *x = row_of<F32>(a.X, row, a.ldx), *r = row_of<F32>(a.residual, row, a.ldr);
   void* h = (void*)row_of<F32>(a.H, row, a.ldh);
-  float s = 0.f;
   if constexpr (NV > 0) {  // (D >= 8)
+    float s = 0.f;
     const bool ragged = a.D & 7;
     float v[NV][8];
     F8Raw8<F32> raw[NV], more[NV];
@@ -131,6 +132,7 @@ __global__ __launch_bounds__(ROWT > 256 ? ROWT : 256) void rms_forward(RmsArgs a
       put8<F32, CODES>(a, row, c, v[j]);
     }
   } else {
+    double s = 0.;
     float v[8];
     auto stream = [&](int c) {  // computed anew where it is needed again: H may have been written by other threads' stores
       load8<F32>(x, c, a.D, v);
@@ -143,7 +145,7 @@ __global__ __launch_bounds__(ROWT > 256 ? ROWT : 256) void rms_forward(RmsArgs a
     for (int c = tid * 8; c < a.D; c += ROWT * 8) {
       stream(c);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s += v[k] * v[k];
+      for (int k = 0; k < 8; ++k) s = fma((double)v[k], (double)v[k], s);
     }
     const Root root = inverse_root<ROWT>(a, s, sh);
     if (tid == 0) a.rstd[row] = root.r;
@@ -257,11 +259,12 @@ __global__ __launch_bounds__(ROWT > 256 ? ROWT : 256) void rms_backward(RmsArgs 
 // Rows of any length: dx, reading the row twice, and a second kernel for the columns' sums.
 template <bool F32>
 __global__ __launch_bounds__(256) void rms_backward_long(RmsArgs a) {
-  __shared__ float sh[4][1];
+  __shared__ double sh[4];
   const int64_t row = (int64_t)blockIdx.y * kGridX + blockIdx.x;
   if (row >= a.T) return;
   const float rstd = a.rstd[row];
-  float s[1] = {0.f}, h[8], g[8], d[8];
+  double s = 0.;
+  float h[8], g[8], d[8];
   auto load = [&](int c) {
     load8<F32>(row_of<F32>(a.H, row, a.ldh), c, a.D, h);
     load8<F32>(row_of<F32>(a.dY, row, a.ld_dy), c, a.D, g);
@@ -274,10 +277,9 @@ __global__ __launch_bounds__(256) void rms_backward_long(RmsArgs a) {
   for (int c = threadIdx.x * 8; c < a.D; c += 2048) {
     load(c);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) s[0] += g[k] * h[k];
+    for (int k = 0; k < 8; ++k) s = fma((double)g[k], (double)h[k], s);
   }
-  row_sum<256, 1>(s, sh);
-  const float mean = s[0] / (float)a.D;
+  const float mean = (float)(row_sum_double<256>(s, sh) * a.inv);
   for (int c = threadIdx.x * 8; c < a.D; c += 2048) {
     load(c);
     if (a.dH) load8<F32>(row_of<F32>(a.dH, row, a.ld_dh), c, a.D, d);
@@ -359,7 +361,7 @@ int rms_launch_backward(const void* dY, int64_t ld_dy, const void* H, int64_t ld
                         const float* weight, int T, int D, void* dX, int64_t ld_dx, float* dweight, float* part, hipStream_t st) {
   RmsArgs a{};
   a.dY = dY, a.H = (void*)H, a.dH = dH, a.weight = weight, a.dX = dX, a.rstd = (float*)rstd, a.part = part, a.dweight = dweight;
-  a.ld_dy = ld_dy, a.ldh = ldh, a.ld_dh = ld_dh, a.ld_dx = ld_dx, a.T = T, a.D = D, a.parts = rms_parts(T, D);
+  a.ld_dy = ld_dy, a.ldh = ldh, a.ld_dh = ld_dh, a.ld_dx = ld_dx, a.T = T, a.D = D, a.parts = rms_parts(T, D), a.inv = 1. / D;
   const int rc = f32 ? backward<true>(a, st) : backward<false>(a, st);
   if (rc != BSP_OK || a.parts == 1 || !dweight) return rc;
   return norm_launch_sum(part, a.parts, D, D, dweight, nullptr, st);
