@@ -367,10 +367,10 @@ def bsp_fc(w: bsp_weights, X: int, bias: Optional[int], Y: int, B: int, stream: 
     _check(load_library().bsp_fc(ctypes.byref(w), X, bias, Y, B, stream), "bsp_fc")
 
 
-_raw_stream = None
+_raw_stream = _several = None
 
 
-def _current_stream(t) -> int:
+def _stream_of(t) -> int:
     """The handle of the current stream on the device of torch tensor ``t``.  torch.cuda.current_stream
     builds a Stream object to hold it: 1.9 us of the 6.2 us that a call of a small layer takes on
     the host, against 0.1 us for the handle itself.  (A tensor elsewhere is refused by the former.)"""
@@ -382,6 +382,20 @@ def _current_stream(t) -> int:
         return _raw_stream(t.get_device())
     import torch
     return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def _current_stream(t) -> int:
+    """That handle, for a launch.  A default stream's is 0 on every device, and a launch with it goes to the current device: with
+    tensors on another one it would run there, on memory that is not its own."""
+    global _several
+    st = _stream_of(t)
+    if not st and _several is not False:
+        import torch
+        if _several is None:
+            _several = torch.cuda.device_count() > 1
+        if _several and t.get_device() != torch.cuda.current_device():
+            raise RuntimeError("tensors on cuda:%d, but the current device is cuda:%d (torch.cuda.set_device)" % (t.get_device(), torch.cuda.current_device()))
+    return st
 
 
 def bsp_conv2d(w: bsp_weights, X: int, bias: Optional[int], Y: int, B: int, L: int, J: int,

@@ -20,7 +20,7 @@ from typing import Optional
 
 import numpy as np
 
-from .binding import (BSP_BF16, BSP_E4M3, BSP_E5M2, BSP_F32, BspError, _check, _current_stream, _np_ptr, bsp_codes,
+from .binding import (BSP_BF16, BSP_E4M3, BSP_E5M2, BSP_F32, BspError, _check, _current_stream, _np_ptr, _stream_of, bsp_codes,
                       bsp_weights_f8, load_library)
 
 CODES = {"e4m3": BSP_E4M3, "e5m2": BSP_E5M2}
@@ -90,12 +90,12 @@ def _on_stream(stream, at, call, *args):
     the call, elsewhere, would not wait for.  Nothing is recorded for that stream, which is its owner's: what is recorded
     for a stream can be freed only while the stream is there."""
     import torch
-    if int(stream) == _current_stream(at):
+    device = torch.cuda.current_device()
+    if int(stream) == _stream_of(at) and at.get_device() == device:
         return call(*args)
     here = torch.cuda.current_stream(at.device)
     # (an ExternalStream of no handle is not the default stream, but any of torch's)
     there = torch.cuda.ExternalStream(int(stream), device=at.device) if int(stream) else torch.cuda.default_stream(at.device)
-    device = torch.cuda.current_device()
     torch.cuda.set_stream(there)  # (and its device; torch.cuda.stream's context takes twice as long)
     try:
         result = call(*args)
