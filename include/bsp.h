@@ -512,7 +512,9 @@ int bsp_layer_norm_grad(const void* dY, int64_t ld_dy, const void* X, int64_t ld
  *   Y[t] = act(W^ x^_t + bias + residual + s_a B_a (A_a x_t)),  a = which[t]
  * with x_t as it is handed in (values as they are, codes as the values that they stand for), A_a [R][I] and B_a [O][R] held as bf16.  All is
  * summed in fp32 and rounded once; A_a x_t enters the second product with 16 bits for results in bf16, with 24 for fp32 ones.  What is not finite
- * among x_t, in bf16 for values in fp32 too, or A_a x_t makes its row's results infinite or NaN, and no other row's.
+ * among x_t, in bf16 for values in fp32 too, or A_a x_t makes its row's results infinite or NaN, and no other row's.  The same call gives the same
+ * bits; the order in which a row's A_a x_t is summed goes by its place among the rows of its adapter, so other requests in a batch may move a
+ * row's result within its roundings.
  * A set holds N adapters (up to 1024) of rank up to R (up to 128) for layers of I inputs and O outputs, in both directions, ranks padded to
  * Rp = 16, 32, 64 or 128. */
 typedef struct {
@@ -543,8 +545,9 @@ int bsp_f8_requests_plan(const bsp_f8_requests* r, const void* which, int32_t wh
 
 /* bsp_f8_fc (X: codes) or bsp_f8_fc_values (X null: values of x_dtype) with adapters; transposed, the gradient of the layer's input, in which
  * a row gets s_a A_a^t (B_a^t x_t).  T, N, I and O have to agree.  workspace: bsp_f8_fc_adapted_workspace bytes (coded: 0 for values, 1 for
- * codes, and for values that become codes inside the product's kernel; many rows of several adapters may be copied there in the order of their
- * adapters).  Errors: as these. */
+ * codes, and for values that become codes inside the product's kernel; more than 32 rows beside a set of several adapters have room there for a copy
+ * of their codes in the order of their adapters, T 128 ceil(K/128) bytes and the scales, whether or not `requests` finds them mixed: it is known on
+ * the device alone).  Errors: as these. */
 int bsp_f8_fc_adapted_workspace(const bsp_weights_f8* w, int32_t transposed, int32_t T, int32_t coded, const bsp_f8_adapters* adapters, int64_t* bytes);
 int bsp_f8_fc_adapted(const bsp_weights_f8* w, int32_t transposed, const bsp_codes* X, const void* values, int32_t x_dtype, int64_t ldx, int32_t T,
                       int32_t code, const bsp_f8_adapters* adapters, const bsp_f8_requests* requests, const float* bias, const void* residual,
@@ -583,6 +586,7 @@ int bsp_rms_norm_grad(const void* dY, int64_t ld_dy, const void* H, int64_t ldh,
  *   X             device, BSP_F32 or BSP_BF16, rows ldx elements apart; minus infinity is a token that cannot be
  *   tokens        device [T], token_bytes 4 (int32) or 8 (int64).  Below 0: none is given (padding), logp[t] = 0; V and above: NaN
  *   scale         above 0, 2^100 at most: the inverse of a temperature
+ * Sums are fp32, in an order that T and V alone decide.  lse is infinite where no float holds the largest logit times scale; the other results are not.
  * A row of minus infinities alone has no token left: lse and log probabilities are minus infinity, the entropy is 0.  A row that holds a NaN or
  * plus infinity gives NaN.  The results are float; workspace: bsp_log_probs_workspace bytes, 16-byte aligned.
  * Errors: NULL, SHAPE, DTYPE, ALIGN, CAPACITY, HIP.  T = 0 does nothing. */

@@ -7,8 +7,8 @@
 // reads h, differentiates the very function that ran.  A row is read once and stays in the registers of the 16 to 1024 threads that
 // own it; squares are summed in fp32 in a thread, in 64 bits over a row.  Rows too long for that are read again, and their sums are in 64 bits in a thread, too.  As in the layer norm the gradient's threads own columns and
 // add dw over all the rows of their workgroup, and a second launch adds the workgroups' sums in a fixed order.
-// Measured: 16384 x 4096 bf16 with a residual to codes 74 to 83 us (470 MB, 5.7 to 6.3 TB/s), its gradient 100 to 113 (537 MB, 4.8 to 5.4 TB/s) and 5 for
-// the sums; 777 x 2966 fp32 7.8 and 9.6 (18 and 28 MB, from the last-level cache) and 4.2; one row of 4096 4.2.
+// Measured: 16384 x 4096 bf16 with a residual to codes 74 to 87 us (470 MB, 5.4 to 6.3 TB/s), its gradient 100 to 113 (537 MB, 4.8 to 5.4 TB/s) and 5 for
+// the sums; 777 x 2966 fp32 8.2 and 9.8 (18 and 28 MB, from the last-level cache) and 4.2; one row of 4096 3.9.
 #include "bsp_norm.h"
 
 namespace {
@@ -44,7 +44,7 @@ __device__ __forceinline__ void add8(float* v, const float* r) {
 // ones in fp32, as in a row of 2^20, drift by 500 2^-24 of their sum), and what 32 bits leave of it.  The threads' sums
 // meet in 64 bits and h q w is rounded once, for the sake of codes: where a block's largest value lies at the border between two scales the
 // wrong side costs 128 codes a step (16384 x 4096 drawn 150 times, 79 million scales: 2 differ from the exact values', with a sum and three roundings in 32 bits
-// 6; q is 4.7e-8 of it off at most, with these 1.5e-7).  The time is the same, one row takes 4.2 us instead of 3.7.
+// 6; q is 4.7e-8 of it off at most, with these 1.5e-7).  The time is the same, one row takes 3.9 us instead of 3.7.
 struct Root {
   float r, rest;
 };
